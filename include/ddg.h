@@ -380,6 +380,70 @@ ddg_status ddg_bn_bwd_reduce(int precision, const void *dout, const void *out, c
                              const float *invstd, float *dgamma, float *dbeta, float *scratch, int B, int HW, int C,
                              int relu, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * The tail of a language-model training step: dropout, root-mean-square norm with the residual's addition, and the
+ * vocabulary projection with its softmax cross entropy.  The paper has no counterpart; the calls stand beside the
+ * fully connected layer, the batch norm and the loss of the training step.  All pointers are device pointers to
+ * contiguous tensors on the current device (anything else: DDG_ERR_INVALID_ARG), `stream` is a cudaStream_t of that
+ * device (NULL = default stream).  The calls only enqueue, allocate nothing and can be captured into a CUDA graph;
+ * results do not depend on the order in which blocks run.  Sizes below one: DDG_ERR_UNSUPPORTED.
+ * --------------------------------------------------------------------------------------------------------- */
+
+/* Loss of the last layer z = x W^T + b under softmax cross entropy, without the logits ever being in memory.
+ *   lse[n] = log sum_v exp z_nv;  row_loss[n] = lse[n] - z_n,label, 0 for a row that does not count;
+ *   loss = mean of row_loss over the rows that count, 0 when none does.
+ * A row counts when its label is in [0, out); any other label (-1, say) leaves it out.  x [B][in], W [out][in] and bias
+ * [out] (nullable) in the precision's element type; labels int32 [B]; loss, row_loss [B], lse [B] fp32, each nullable
+ * (one at least is given).  workspace: device, 256-byte aligned, ddg_linear_ce_workspace_bytes(..., backward) bytes,
+ * contents undefined on entry and exit; two calls that may run at the same time need one each.  The products run on the tensor
+ * cores with fp32 accumulation; fp32 tensors are split into three bf16 terms.  W and x are read in place when
+ * precision is DDG_BF16 and in is a multiple of 8 (both then start on 16-byte boundaries), else through a copy in the
+ * workspace.  At most 2^24 rows and outputs and 2^20 inputs.  If a bounded device-side wait runs out, the results
+ * are NaN. */
+size_t ddg_linear_ce_workspace_bytes(int precision, int B, int in, int out, int backward);
+ddg_status ddg_linear_ce_fwd(int precision, const void *x, const void *W, const void *bias, const int *labels, float *loss,
+                             float *row_loss, float *lse, void *workspace, size_t workspace_bytes, int B, int in, int out,
+                             void *stream);
+/* Its gradients, with lse as ddg_linear_ce_fwd left it:
+ *   dz_nv = (exp(z_nv - lse[n]) - [v = label]) g_n, 0 for rows that do not count (whatever x holds there);
+ *   dx = dz W [B][in];  dW = dz^T x [out][in];  db = sum_n dz_n [out] fp32; each nullable, one at least is given.
+ * g_n = drow[n] (the gradient of row_loss[n]) when drow is given, else dloss / (rows that count) with dloss the gradient
+ * of loss (fp32 scalar; NULL = 1); not both.  dx in the element type; dW in the element type, or fp32 when dw_f32 != 0
+ * (as ddg_sgd_update reads it).  dz is rounded to bf16 before the products (three bf16 terms for fp32 tensors, two for an
+ * fp32 dW of bf16 tensors).  dx may be x; dW may not be W. */
+ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const void *bias, const int *labels,
+                             const float *lse, const float *dloss, const float *drow, void *dx, void *dW, float *db,
+                             void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32, void *stream);
+
+/* Root-mean-square norm of rows of C <= 16384 values, with the residual's addition:
+ *   h = x + res;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd gamma;
+ *   y8 = e4m3(y / scale8), one scale per row (group = 0: scale8 [rows]) or per 128 neighbouring values of a row (group =
+ *   128, C a multiple of 128: scale8 [rows][C / 128]); scale8 = max |y| / 448, or 1 where that is zero.
+ * x, res (nullable), gamma [C], h (nullable without res), y in the precision's element type; y8 one byte per value;
+ * scale8, rstd (nullable) [rows] fp32.  One of y and y8 at least is given, y8 with scale8.  y and y8 are taken from the unrounded sum.
+ * h and y may be x or res. */
+ddg_status ddg_add_rmsnorm_fwd(int precision, const void *x, const void *res, const void *gamma, void *h, void *y, void *y8,
+                               float *scale8, float *rstd, int rows, int C, int group, float eps, void *stream);
+/* Its gradients from the stored h (x itself without a residual) and rstd:
+ *   dx = dh + rstd (gamma dy - h rstd^2 mean(gamma dy h)), the gradient of x and of res alike;  dgamma = sum dy h rstd.
+ * dh (nullable): the gradient that reaches h past the norm.  dgamma fp32 [C]; scratch: ddg_rmsnorm_scratch_elems(rows, C)
+ * floats.  dx may be dy, dh or h. */
+size_t ddg_rmsnorm_scratch_elems(int rows, int C);
+ddg_status ddg_add_rmsnorm_bwd(int precision, const void *dy, const void *dh, const void *h, const void *gamma,
+                               const float *rstd, void *dx, float *dgamma, float *scratch, int rows, int C, void *stream);
+
+/* Dropout of n values whose mask is never stored: y = res + keep x / (1 - p) with keep_i = (u_i >= rint(65536 p)), where
+ * u_i is the 16-bit lane i % 8 (low half of word 0 first) of the Philox4x32-10 block with key rng[0] and counter
+ * (rng[1] + i / 8 as 64 bits, layer, 0); 1 - p is that of the rounded probability.  rng: two unsigned 64-bit integers in
+ * device memory, {seed, position}, read when the kernel runs, so that a recorded call draws new numbers when they were
+ * changed in between; a call uses ceil(n / 8) positions.  res nullable; y may be x or res.
+ * The backward pass regenerates the mask from the same rng, layer, n and p: dx = keep dy / (1 - p).  A module whose backward
+ * pass runs iterations later (K > 1) keeps the two integers of that iteration instead of a mask.  dx may be dy. */
+ddg_status ddg_dropout_fwd(int precision, const void *x, const void *res, void *y, const void *rng, size_t n, float p,
+                           unsigned layer, void *stream);
+ddg_status ddg_dropout_bwd(int precision, const void *dy, void *dx, const void *rng, size_t n, float p, unsigned layer,
+                           void *stream);
+
 /* Fused SGD update over n parameters (Eq. 9 with momentum and weight decay): d = g + wd*w; v = mu*v + d;
  * w -= lr*v; w_version = cast(w).  w, v, g fp32; w_version in the precision's element type. */
 ddg_status ddg_sgd_update(int precision, float *w, float *v, const float *g, void *w_version, size_t n, float lr,

@@ -35,7 +35,9 @@ EXPORTS = ["ddg_create", "ddg_step", "ddg_step_host", "ddg_set_lr", "ddg_param_c
            "ddg_conv1x1_wgrad", "ddg_conv3x3_bnrelu_fwd_stats", "ddg_conv3x3_fwd_partials",
            "ddg_bn_fwd_partials", "ddg_conv3x3_dgrad_partials", "ddg_bn_bwd_partials", "ddg_conv3x3_fwd_stats_prepared",
            "ddg_piece_times", "ddg_conv3x3_fwd_stats_shared",
-           "ddg_step_host_pipelined", "ddg_pipelined_loss", "ddg_conv3x3_dgrad_fused_shared"]
+           "ddg_step_host_pipelined", "ddg_pipelined_loss", "ddg_conv3x3_dgrad_fused_shared",
+           "ddg_linear_ce_workspace_bytes", "ddg_linear_ce_fwd", "ddg_linear_ce_bwd", "ddg_rmsnorm_scratch_elems",
+           "ddg_add_rmsnorm_fwd", "ddg_add_rmsnorm_bwd", "ddg_dropout_fwd", "ddg_dropout_bwd"]
 
 
 class Layer(ctypes.Structure):
@@ -118,6 +120,16 @@ _lib.ddg_fc_fwd.argtypes = [_i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.ddg_fc_bwd.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.ddg_bn_fwd_noalloc.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]
 _lib.ddg_bn_bwd_reduce.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]
+_lib.ddg_linear_ce_workspace_bytes.argtypes = [_i] * 5
+_lib.ddg_linear_ce_workspace_bytes.restype = _sz
+_lib.ddg_linear_ce_fwd.argtypes = [_i] + [_vp] * 8 + [_sz] + [_i] * 3 + [_vp]
+_lib.ddg_linear_ce_bwd.argtypes = [_i] + [_vp] * 11 + [_sz] + [_i] * 4 + [_vp]
+_lib.ddg_rmsnorm_scratch_elems.argtypes = [_i] * 2
+_lib.ddg_rmsnorm_scratch_elems.restype = _sz
+_lib.ddg_add_rmsnorm_fwd.argtypes = [_i] + [_vp] * 8 + [_i] * 3 + [_f, _vp]
+_lib.ddg_add_rmsnorm_bwd.argtypes = [_i] + [_vp] * 8 + [_i] * 2 + [_vp]
+_lib.ddg_dropout_fwd.argtypes = [_i] + [_vp] * 4 + [_sz, _f, ctypes.c_uint, _vp]
+_lib.ddg_dropout_bwd.argtypes = [_i] + [_vp] * 3 + [_sz, _f, ctypes.c_uint, _vp]
 _lib.ddg_sgd_update.argtypes = [_i, _vp, _vp, _vp, _vp, _sz, _f, _f, _f, _vp]
 
 
@@ -428,3 +440,90 @@ def bn_bwd_reduce(prec, dout, out, x, mean, invstd, dgamma, dbeta, scratch, B, H
 
 def sgd_update(prec, w, v, g, w_version, n, lr, momentum, weight_decay, stream=None):
     _ok(_lib.ddg_sgd_update(prec, _ptr(w), _ptr(v), _ptr(g), _ptr(w_version), n, lr, momentum, weight_decay, stream))
+
+
+# ---- the tail of a language-model step ----------------------------------------------------------------------------
+def _tensor(a, n, size, what):
+    """The address of a tensor argument that the caller says has n elements of `size` bytes.  A torch tensor that is too
+    small, strided or of another element size is refused here: the C call sees an address only."""
+    if a is None or isinstance(a, int):
+        return a
+    if hasattr(a, "is_contiguous"):
+        if not a.is_contiguous():
+            raise ValueError("%s has to be contiguous" % what)
+        if a.element_size() != size:
+            raise ValueError("%s has elements of %d bytes instead of %d" % (what, a.element_size(), size))
+        if a.numel() < n:
+            raise ValueError("%s has %d elements instead of %d" % (what, a.numel(), n))
+    return _ptr(a)
+
+
+def _elem(prec):
+    return 2 if prec == BF16 else 4
+
+
+def _workspace(a):
+    """(address, bytes) of a workspace tensor."""
+    if a is None:
+        return None, 0
+    return _ptr(a), a.numel() * a.element_size()
+
+
+def linear_ce_workspace_bytes(prec, B, n_in, n_out, backward):
+    return _lib.ddg_linear_ce_workspace_bytes(prec, B, n_in, n_out, int(backward))
+
+
+def linear_ce_fwd(prec, x, W, bias, labels, loss, row_loss, lse, workspace, B, n_in, n_out, stream=None):
+    """Softmax cross entropy of x W^T + bias without the logits in memory; workspace: a tensor of
+    linear_ce_workspace_bytes(prec, B, n_in, n_out, False) bytes."""
+    e = _elem(prec)
+    ws, ws_bytes = _workspace(workspace)
+    _ok(_lib.ddg_linear_ce_fwd(prec, _tensor(x, B * n_in, e, "x"), _tensor(W, n_out * n_in, e, "W"),
+                               _tensor(bias, n_out, e, "bias"), _tensor(labels, B, 4, "labels"),
+                               _tensor(loss, 1, 4, "loss"), _tensor(row_loss, B, 4, "row_loss"), _tensor(lse, B, 4, "lse"),
+                               ws, ws_bytes, B, n_in, n_out, stream))
+
+
+def linear_ce_bwd(prec, x, W, bias, labels, lse, dloss, drow, dx, dW, db, workspace, B, n_in, n_out, dw_f32=False,
+                  stream=None):
+    """Gradients of linear_ce_fwd's loss (dloss) or row losses (drow); workspace: as there, with backward=True."""
+    e = _elem(prec)
+    ws, ws_bytes = _workspace(workspace)
+    _ok(_lib.ddg_linear_ce_bwd(prec, _tensor(x, B * n_in, e, "x"), _tensor(W, n_out * n_in, e, "W"),
+                               _tensor(bias, n_out, e, "bias"), _tensor(labels, B, 4, "labels"), _tensor(lse, B, 4, "lse"),
+                               _tensor(dloss, 1, 4, "dloss"), _tensor(drow, B, 4, "drow"), _tensor(dx, B * n_in, e, "dx"),
+                               _tensor(dW, n_out * n_in, 4 if dw_f32 else e, "dW"), _tensor(db, n_out, 4, "db"),
+                               ws, ws_bytes, B, n_in, n_out, int(dw_f32), stream))
+
+
+def rmsnorm_scratch_elems(rows, C):
+    return _lib.ddg_rmsnorm_scratch_elems(rows, C)
+
+
+def add_rmsnorm_fwd(prec, x, res, gamma, h, y, y8, scale8, rstd, rows, C, group=0, eps=1e-6, stream=None):
+    e, n = _elem(prec), rows * C
+    _ok(_lib.ddg_add_rmsnorm_fwd(prec, _tensor(x, n, e, "x"), _tensor(res, n, e, "res"), _tensor(gamma, C, e, "gamma"),
+                                 _tensor(h, n, e, "h"), _tensor(y, n, e, "y"), _tensor(y8, n, 1, "y8"),
+                                 _tensor(scale8, rows * (C // group) if group > 0 else rows, 4, "scale8"),
+                                 _tensor(rstd, rows, 4, "rstd"), rows, C, group, eps, stream))
+
+
+def add_rmsnorm_bwd(prec, dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, stream=None):
+    e, n = _elem(prec), rows * C
+    _ok(_lib.ddg_add_rmsnorm_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dh, n, e, "dh"), _tensor(h, n, e, "h"),
+                                 _tensor(gamma, C, e, "gamma"), _tensor(rstd, rows, 4, "rstd"), _tensor(dx, n, e, "dx"),
+                                 _tensor(dgamma, C, 4, "dgamma"),
+                                 _tensor(scratch, rmsnorm_scratch_elems(rows, C), 4, "scratch"), rows, C, stream))
+
+
+def dropout_fwd(prec, x, res, y, rng, n, p, layer=0, stream=None):
+    """rng: two 64-bit integers on the device, {seed, position}; the call uses ceil(n / 8) positions."""
+    e = _elem(prec)
+    _ok(_lib.ddg_dropout_fwd(prec, _tensor(x, n, e, "x"), _tensor(res, n, e, "res"), _tensor(y, n, e, "y"),
+                             _tensor(rng, 2, 8, "rng"), n, p, layer, stream))
+
+
+def dropout_bwd(prec, dy, dx, rng, n, p, layer=0, stream=None):
+    e = _elem(prec)
+    _ok(_lib.ddg_dropout_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dx, n, e, "dx"), _tensor(rng, 2, 8, "rng"), n, p,
+                             layer, stream))

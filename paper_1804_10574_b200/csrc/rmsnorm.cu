@@ -1,0 +1,316 @@
+// Root-mean-square norm with the residual's addition, its 8-bit output and its backward pass.
+//
+//   h = x + res;  r = 1 / sqrt(mean(h^2) + eps);  y = h r gamma;  q = e4m3(y / s), s = amax(|y| of the group) / 448
+//   dx = dh + r (gamma dy - h r^2 mean(gamma dy h));  dgamma = sum over rows of dy h r
+//
+// Bound by memory: the forward pass reads x and res and writes h and y (or q) once, the backward pass reads dy, h and dh
+// and writes dx once.  A row stays in the registers of its threads between the loads, the reduction and the stores; y is
+// taken from the unrounded sum.  A row of at most four 16-byte vectors per lane is one warp's (no barrier), a longer one a
+// block's.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "lm_ops.h"
+
+namespace ddg {
+
+namespace {
+
+constexpr float kE4m3Max = 448.f;
+
+// Sum (or maximum) over the threads of a row: a warp, or the block through shared memory.  Every thread gets the result.
+template <bool MAX> __device__ __forceinline__ float row_reduce(float v, bool one_warp, float *red) {
+    v = MAX ? warp_max(v) : warp_sum(v);
+    if (one_warp) return v;
+    const int nw = blockDim.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();  // the previous reduction's values are read
+    if (lane == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = lane < nw ? red[lane] : (MAX ? -INFINITY : 0.f);
+    return MAX ? warp_max(v) : warp_sum(v);
+}
+
+// what rms_plan gives a row of at most 16384 values
+constexpr int rms_max_threads(int vec, int iter) { return (vec == 4 && iter == 4) || (vec == 1 && iter == 16) ? 1024 : 512; }
+
+template <int VEC> __device__ __forceinline__ void store_q(uint8_t *p, const float (&v)[VEC]) {
+    if (VEC == 1) {
+        *p = __nv_cvt_float_to_fp8(v[0], __NV_SATFINITE, __NV_E4M3);
+    } else {
+        uint16_t w[(VEC + 1) / 2];
+#pragma unroll
+        for (int j = 0; j < VEC / 2; ++j) w[j] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * j], v[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
+        if (VEC == 8)
+            *reinterpret_cast<uint2 *>(p) = make_uint2((uint32_t)w[0] | ((uint32_t)w[1] << 16), (uint32_t)w[VEC == 8 ? 2 : 0] | ((uint32_t)w[VEC == 8 ? 3 : 0] << 16));
+        else
+            *reinterpret_cast<uint32_t *>(p) = (uint32_t)w[0] | ((uint32_t)w[1] << 16);
+    }
+}
+
+// x, res, h and y may be the same tensor (a thread reads its elements before it writes them).  group: 128 (vector forms
+// only: 128 / VEC neighbouring lanes hold a group) or 0 (the row).
+template <typename T, int VEC, int ITER>
+__global__ void __launch_bounds__(rms_max_threads(VEC, ITER)) rms_fwd_kernel(const T *x, const T *res, const T *__restrict__ gamma, T *h, T *y, uint8_t *__restrict__ q,
+                                                       float *__restrict__ scale, float *__restrict__ rstd, int rows, int C, int tpr, int group, float eps) {
+    __shared__ float red[32];
+    pdl_launch();
+    pdl_wait();
+    const bool one_warp = tpr == 32;
+    const int t = one_warp ? (threadIdx.x & 31) : threadIdx.x;
+    const int row = one_warp ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+    if (row >= rows) return;  // whole warps, and only where a row is one warp's
+    const size_t at = (size_t)row * C;
+    float v[ITER][VEC];
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int c = (i * tpr + t) * VEC;
+        if (c < C) {
+            load_f<T, VEC>(x + at + c, v[i]);
+            if (res) {
+                float b[VEC];
+                load_f<T, VEC>(res + at + c, b);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) v[i][j] += b[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i][j] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int c = (i * tpr + t) * VEC;
+        if (h && c < C) store_f<T, VEC>(h + at + c, v[i]);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+    }
+    ss = row_reduce<false>(ss, one_warp, red);
+    const float r = rsqrtf(ss / (float)C + eps);
+    if (rstd && t == 0) rstd[row] = r;
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int c = (i * tpr + t) * VEC;
+        if (c < C) {
+            float g[VEC];
+            load_f<T, VEC>(gamma + c, g);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i][j] = v[i][j] * r * g[j];
+            if (y) store_f<T, VEC>(y + at + c, v[i]);
+        }
+    }
+    if (!q) return;
+    float top[ITER];
+    float all = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        top[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) top[i] = fmaxf(top[i], fabsf(v[i][j]));
+        all = fmaxf(all, top[i]);
+    }
+    if (group == 0) {
+        all = row_reduce<true>(all, one_warp, red);
+    } else {
+#pragma unroll
+        for (int i = 0; i < ITER; ++i)
+#pragma unroll
+            for (int o = 64 / VEC; o > 0; o >>= 1)
+                if (o < 32) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+    }
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int c = (i * tpr + t) * VEC;
+        if (c < C) {
+            const float a = group == 0 ? all : top[i];
+            const float s = a > 0.f ? a / kE4m3Max : 1.f;  // a group of zeros (or of NaN) has scale 1
+            const float inv = 1.f / s;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i][j] *= inv;
+            store_q<VEC>(q + at + c, v[i]);
+            if (group == 0) { if (t == 0 && i == 0) scale[row] = s; }
+            else if (c % 128 == 0) scale[(size_t)row * (C / 128) + c / 128] = s;
+        }
+    }
+}
+
+// Blocks (or warps, where a row is one warp's) walk the rows; each keeps its share of dgamma in registers and leaves it in
+// part[walker][C] for the folding kernel.  dx may be dy, dh or h.
+template <typename T, int VEC, int ITER>
+__global__ void __launch_bounds__(rms_max_threads(VEC, ITER)) rms_bwd_kernel(const T *dy, const T *dh, const T *h, const T *__restrict__ gamma, const float *__restrict__ rstd, T *dx,
+                                                       float *__restrict__ part, int rows, int C, int tpr) {
+    __shared__ float red[32];
+    pdl_launch();
+    pdl_wait();
+    const bool one_warp = tpr == 32;
+    const int t = one_warp ? (threadIdx.x & 31) : threadIdx.x;
+    const int walkers = one_warp ? gridDim.x * (blockDim.x >> 5) : gridDim.x;
+    const int walker = one_warp ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+    if (walker >= rows) return;  // a spare warp of the last block
+    float acc[ITER][VEC];
+#pragma unroll
+    for (int i = 0; i < ITER; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[i][j] = 0.f;
+    for (int row = walker; row < rows; row += walkers) {
+        const size_t at = (size_t)row * C;
+        const float r = rstd[row];
+        float a[ITER][VEC], b[ITER][VEC];  // gamma dy, h
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * tpr + t) * VEC;
+            if (c < C) {
+                load_f<T, VEC>(dy + at + c, a[i]);
+                load_f<T, VEC>(h + at + c, b[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) a[i][j] = b[i][j] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * tpr + t) * VEC;
+            if (c < C) {
+                float g[VEC];
+                load_f<T, VEC>(gamma + c, g);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    acc[i][j] = fmaf(a[i][j], b[i][j] * r, acc[i][j]);
+                    a[i][j] *= g[j];
+                    dot = fmaf(a[i][j], b[i][j], dot);
+                }
+            }
+        }
+        dot = row_reduce<false>(dot, one_warp, red);
+        const float k = dot / (float)C * r * r;
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * tpr + t) * VEC;
+            if (c < C) {
+                float d[VEC];
+                if (dh) {
+                    load_f<T, VEC>(dh + at + c, d);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) d[j] = 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) d[j] = fmaf(r, a[i][j] - b[i][j] * k, d[j]);
+                store_f<T, VEC>(dx + at + c, d);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int c = (i * tpr + t) * VEC;
+        if (c < C) store_f<float, VEC>(part + (size_t)walker * C + c, acc[i]);
+    }
+}
+
+// dgamma[c] = sum over walkers, 32 columns per block, walkers in index order per warp and warps in index order
+__global__ void __launch_bounds__(512) rms_fold_kernel(const float *__restrict__ part, int walkers, float *__restrict__ dgamma, int C) {
+    __shared__ float fold[16][32];
+    pdl_launch();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float a = 0.f;
+    if (c < C) {
+#pragma unroll 8
+        for (int i = w; i < walkers; i += 16) a += part[(size_t)i * C + c];
+    }
+    fold[w][lane] = a;
+    __syncthreads();
+    if (w == 0 && c < C) {
+        for (int i = 1; i < 16; ++i) a += fold[i][lane];
+        dgamma[c] = a;
+    }
+}
+
+bool vec_ok(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// threads of a row, vectors per thread, threads of a block and rows of a block
+struct RmsPlan { int tpr, iter, threads, rpb; };
+RmsPlan rms_plan(int nvec, bool vec) {
+    RmsPlan p;
+    const int warp_iter = (nvec + 31) / 32;
+    if (warp_iter <= 4) {
+        p.iter = warp_iter <= 1 ? 1 : (warp_iter <= 2 ? 2 : 4);
+        p.tpr = 32; p.threads = 128; p.rpb = 4;
+        return p;
+    }
+    p.iter = 1;
+    while (p.iter < (vec ? 4 : 16) && nvec > p.iter * 512) p.iter *= 2;
+    p.threads = std::min(1024, ((nvec + p.iter - 1) / p.iter + 31) / 32 * 32);
+    p.tpr = p.threads; p.rpb = 1;
+    return p;
+}
+
+constexpr int kMaxWalkers = 148 * 4;
+
+}  // namespace
+
+size_t rmsnorm_scratch_elems(int rows, int C) { return (size_t)std::min(rows, kMaxWalkers) * C; }
+
+template <typename T, int VEC>
+static int rms_fwd(const void *x, const void *res, const void *gamma, void *h, void *y, void *y8, float *scale8, float *rstd, int rows, int C, int group,
+                   float eps, const Launch &s) {
+    const RmsPlan p = rms_plan(C / VEC, VEC > 1);
+    const int grid = (rows + p.rpb - 1) / p.rpb;
+    auto go = [&](auto kernel) {
+        launch_k(kernel, grid, p.threads, 0, s, (const T *)x, (const T *)res, (const T *)gamma, (T *)h, (T *)y, (uint8_t *)y8, scale8, rstd, rows, C, p.tpr, group, eps);
+    };
+    switch (p.iter) {
+    case 1: go(rms_fwd_kernel<T, VEC, 1>); break;
+    case 2: go(rms_fwd_kernel<T, VEC, 2>); break;
+    case 4: go(rms_fwd_kernel<T, VEC, 4>); break;
+    case 8: if (VEC == 1) { go(rms_fwd_kernel<T, 1, 8>); break; } return -1;
+    case 16: if (VEC == 1) { go(rms_fwd_kernel<T, 1, 16>); break; } return -1;
+    default: return -1;
+    }
+    return 1;
+}
+
+template <typename T, int VEC>
+static int rms_bwd(const void *dy, const void *dh, const void *h, const void *gamma, const float *rstd, void *dx, float *dgamma, float *scratch, int rows, int C,
+                   const Launch &s) {
+    const RmsPlan p = rms_plan(C / VEC, VEC > 1);
+    const int walkers = std::min(rows, kMaxWalkers);
+    const int grid = (walkers + p.rpb - 1) / p.rpb;
+    auto go = [&](auto kernel) {
+        launch_k(kernel, grid, p.threads, 0, s, (const T *)dy, (const T *)dh, (const T *)h, (const T *)gamma, rstd, (T *)dx, scratch, rows, C, p.tpr);
+    };
+    switch (p.iter) {
+    case 1: go(rms_bwd_kernel<T, VEC, 1>); break;
+    case 2: go(rms_bwd_kernel<T, VEC, 2>); break;
+    case 4: go(rms_bwd_kernel<T, VEC, 4>); break;
+    case 8: if (VEC == 1) { go(rms_bwd_kernel<T, 1, 8>); break; } return -1;
+    case 16: if (VEC == 1) { go(rms_bwd_kernel<T, 1, 16>); break; } return -1;
+    default: return -1;
+    }
+    launch_k(rms_fold_kernel, (C + 31) / 32, 512, 0, s, (const float *)scratch, walkers, dgamma, C);
+    return 2;
+}
+
+int launch_add_rmsnorm_fwd(int prec, const void *x, const void *res, const void *gamma, void *h, void *y, void *y8, float *scale8, float *rstd, int rows, int C,
+                           int group, float eps, Launch s) {
+    const int vec = prec == P_BF16 ? 8 : 4;
+    const bool v = C % vec == 0 && vec_ok(x) && vec_ok(res) && vec_ok(gamma) && vec_ok(h) && vec_ok(y) && (reinterpret_cast<uintptr_t>(y8) & 7) == 0;
+    if (group != 0 && !v) return -1;
+    if (prec == P_BF16)
+        return v ? rms_fwd<bf16, 8>(x, res, gamma, h, y, y8, scale8, rstd, rows, C, group, eps, s) : rms_fwd<bf16, 1>(x, res, gamma, h, y, y8, scale8, rstd, rows, C, group, eps, s);
+    return v ? rms_fwd<float, 4>(x, res, gamma, h, y, y8, scale8, rstd, rows, C, group, eps, s) : rms_fwd<float, 1>(x, res, gamma, h, y, y8, scale8, rstd, rows, C, group, eps, s);
+}
+
+int launch_add_rmsnorm_bwd(int prec, const void *dy, const void *dh, const void *h, const void *gamma, const float *rstd, void *dx, float *dgamma, float *scratch,
+                           int rows, int C, Launch s) {
+    const int vec = prec == P_BF16 ? 8 : 4;
+    const bool v = C % vec == 0 && vec_ok(dy) && vec_ok(dh) && vec_ok(h) && vec_ok(gamma) && vec_ok(dx) && vec_ok(scratch);
+    if (prec == P_BF16)
+        return v ? rms_bwd<bf16, 8>(dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, s) : rms_bwd<bf16, 1>(dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, s);
+    return v ? rms_bwd<float, 4>(dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, s) : rms_bwd<float, 1>(dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, s);
+}
+
+}  // namespace ddg

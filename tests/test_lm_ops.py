@@ -1,0 +1,764 @@
+"""Dropout, RMS norm with the residual's addition, and the vocabulary projection with softmax cross entropy, against
+plain implementations in 64 bits.
+
+Tolerances count roundings.  A rounding to a type is off by at most U[type] relative to the value (half a step).  The
+tensor cores add 16 products and the accumulator at a time; every such step is taken to lose at most four units of 2^-24
+of the sum of the absolute values (the products' alignment and the accumulator's truncation)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+U = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+DT = {0: torch.float32, 1: torch.bfloat16}
+PREC = pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+gpu = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture
+def binding():
+    from paper_1804_10574_b200 import binding as b
+    return b
+
+
+def randn(*size, seed, prec, std=1.0, mean=0.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.empty(size, device="cuda", dtype=torch.float32).normal_(mean, std, generator=g).to(DT[prec])
+
+
+def f32(*size, fill=7.0):
+    return torch.full(size, fill, dtype=torch.float32, device="cuda")
+
+
+def within(got, ref, tol, what):
+    """got within tol of ref elementwise; NaN and infinities in the same places."""
+    got, ref, tol = got.double(), ref.double(), torch.as_tensor(tol, dtype=torch.float64, device="cuda").expand_as(ref)
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)), what
+    fine = torch.isfinite(ref)
+    assert torch.equal(got[~fine & ~torch.isnan(ref)], ref[~fine & ~torch.isnan(ref)]), what
+    over = ((got - ref).abs() - tol)[fine]
+    if over.numel():
+        i = int(over.argmax())
+        assert float(over[i]) <= 0, "%s: off by %.3e, %.3e allowed, value %.3e" % (what, float((got - ref).abs()[fine][i]), float(tol[fine][i]), float(ref[fine][i]))
+
+
+# ---- vocabulary projection with softmax cross entropy ---------------------------------------------------------------
+class Ce:
+    """Inputs, the 64-bit reference and its tolerances."""
+
+    def __init__(self, B, D, V, prec, bias=False, ignored=0.0, seed=0, logit_std=2.0):
+        self.B, self.D, self.V, self.prec = B, D, V, prec
+        self.x = randn(B, D, seed=seed + 1, prec=prec)
+        self.w = randn(V, D, seed=seed + 2, prec=prec, std=logit_std / math.sqrt(D))
+        self.bias = randn(V, seed=seed + 3, prec=prec) if bias else None
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed + 4)
+        self.labels = torch.randint(0, V, (B,), device="cuda", generator=g, dtype=torch.int32)
+        if ignored:
+            self.labels[torch.rand(B, device="cuda", generator=g) < ignored] = -1
+
+    def reference(self, drow=None, dloss=1.0, dz_u=None):
+        x, w = self.x.double(), self.w.double()
+        counted = (self.labels >= 0) & (self.labels < self.V)
+        x = torch.where(counted[:, None], x, torch.nan_to_num(x, nan=0.0, posinf=0.0, neginf=0.0))
+        z = x @ w.t()
+        mass = x.abs() @ w.abs().t()
+        if self.bias is not None:
+            z = z + self.bias.double()
+            mass = mass + torch.nan_to_num(self.bias.double(), neginf=0.0).abs()
+        parts = 6 if self.prec == 0 else 1
+        # steps of the accumulator; the terms an fp32 product leaves out (m l, l m, l l and what l rounds off) are below
+        # 4 x 2^-24; adding the bias rounds once
+        ez = (4 * parts * math.ceil(self.D / 16) + 8) * 2.0 ** -24 * mass
+        self.z, self.ez = z, ez
+        self.lse = torch.logsumexp(z, 1)
+        top = z.amax(1)
+        # exp2 and its argument: 2^-22 and 2 roundings of |z - max| (terms far below the maximum weigh less than
+        # 2^-24 |z - max| exp(z - max) < 2^-24); sums of V terms in pieces of 128 and a tree: 64 + 32 roundings; the
+        # logarithm's and the sum's final roundings
+        self.e_lse = torch.softmax(z, 1).mul(ez).sum(1) * 1.01 + 2.0 ** -21 + 100 * 2.0 ** -24 + 4 * 2.0 ** -24 * (top.abs() + self.lse.abs())
+        y = self.labels.clamp(0, self.V - 1).long()[:, None]
+        zl = z.gather(1, y)[:, 0]
+        self.row = torch.where(counted, self.lse - zl, 0.0)
+        self.e_row = self.e_lse + ez.gather(1, y)[:, 0] + 2.0 ** -23 * (self.lse.abs() + zl.abs())
+        n = int(counted.sum())
+        self.loss = self.row.sum() / max(1, n)
+        self.e_loss = torch.where(counted, self.e_row, 0.0).sum() / max(1, n) + 2.0 ** -23 * self.loss.abs()
+        g = drow.double() if drow is not None else torch.full_like(self.row, dloss / max(1, n))
+        g = torch.where(counted, g, 0.0)
+        p = torch.softmax(z, 1)
+        hit = torch.zeros_like(p).scatter_(1, y, 1.0)
+        dz = (p - hit) * g[:, None]
+        dz = torch.where(counted[:, None], dz, 0.0)
+        # p: the logit's and lse's errors, exp2 as above; then the subtraction's, the weight's and the scale's roundings
+        ep = p * (ez + self.e_lse[:, None] + 2.0 ** -21 + 2.0 ** -23 * (z - self.lse[:, None]).abs())
+        ep = torch.where(counted[:, None], (ep + 2.0 ** -24) * g.abs()[:, None], 0.0)
+        # dz as the products see it: one, two or three terms of bf16
+        edz = ep + dz.abs() * (2.0 ** -8 if self.prec == 1 else 2.0 ** -24)
+        edz16 = ep + dz.abs() * (2.0 ** -16 if self.prec == 1 else 2.0 ** -24)
+        self.db, self.e_db = dz.sum(0), ep.sum(0) * 1.01 + 64 * 2.0 ** -24 * dz.abs().sum(0)
+        aw, ax, az = w.abs(), x.abs(), dz.abs()
+        steps_v, steps_b = 4 * parts * math.ceil(self.V / 16) + 80, 4 * parts * math.ceil(self.B / 16) + 16
+        self.dx = dz @ w
+        self.e_dx = edz @ aw + steps_v * 2.0 ** -24 * (az @ aw) + U[DT[self.prec]] * self.dx.abs() + 1e-30
+        self.dw = dz.t() @ x
+        self.e_dw = edz.t() @ ax + steps_b * 2.0 ** -24 * (az.t() @ ax) + U[DT[self.prec]] * self.dw.abs() + 1e-30
+        self.e_dw32 = edz16.t() @ ax + 2 * steps_b * 2.0 ** -24 * (az.t() @ ax) + 2.0 ** -24 * self.dw.abs() + 1e-30
+        return self
+
+    def fwd(self, b, stream=None):
+        ws = torch.full((b.linear_ce_workspace_bytes(self.prec, self.B, self.D, self.V, False),), 255, dtype=torch.uint8, device="cuda")
+        loss, row, lse = f32(1), f32(self.B), f32(self.B)
+        b.linear_ce_fwd(self.prec, self.x, self.w, self.bias, self.labels, loss, row, lse, ws, self.B, self.D, self.V, stream)
+        return loss, row, lse
+
+    def bwd(self, b, lse, dloss=None, drow=None, want="xwb", dw_f32=False, stream=None):
+        ws = torch.full((b.linear_ce_workspace_bytes(self.prec, self.B, self.D, self.V, True),), 255, dtype=torch.uint8, device="cuda")
+        dx = torch.full_like(self.x, 7.0) if "x" in want else None
+        dw = torch.full(self.w.shape, 7.0, dtype=torch.float32 if dw_f32 else self.w.dtype, device="cuda") if "w" in want else None
+        db = f32(self.V) if "b" in want else None
+        b.linear_ce_bwd(self.prec, self.x, self.w, self.bias, self.labels, lse, dloss, drow, dx, dw, db, ws, self.B, self.D, self.V, dw_f32, stream)
+        return dx, dw, db
+
+
+CE_SHAPES = [(1, 8, 1), (1, 64, 100), (3, 5, 7), (128, 64, 100), (130, 72, 257), (257, 264, 513), (300, 521, 1000), (33, 1000, 4099),
+             (2, 4096, 300), (511, 16, 255), (64, 2048, 12000)]
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("shape", CE_SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_linear_ce_forward(binding, shape, prec):
+    """One row to several tiles; widths and vocabularies that fill no tile, widths that TMA cannot read in place."""
+    for bias, ignored in ((False, 0.0), (True, 0.3)):
+        c = Ce(*shape, prec, bias, ignored, seed=5).reference()
+        loss, row, lse = c.fwd(binding)
+        within(lse, c.lse, c.e_lse, "lse")
+        within(row, c.row, c.e_row, "row_loss")
+        within(loss[0], c.loss, c.e_loss, "loss")
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("shape", CE_SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_linear_ce_backward(binding, shape, prec):
+    for bias, ignored, dw_f32 in ((False, 0.0, False), (True, 0.3, True)):
+        c = Ce(*shape, prec, bias, ignored, seed=6).reference(dloss=0.75)
+        dx, dw, db = c.bwd(binding, c.lse.float(), dloss=f32(1, fill=0.75), dw_f32=dw_f32)
+        within(dx, c.dx, c.e_dx, "dx")
+        within(dw, c.dw, c.e_dw32 if dw_f32 else c.e_dw, "dW")
+        within(db, c.db, c.e_db, "db")
+
+
+@gpu
+@PREC
+def test_linear_ce_row_gradients(binding, prec):
+    """drow: a gradient of its own for every row, zeros and signs among them; each output asked for alone."""
+    c = Ce(260, 136, 777, prec, True, 0.2, seed=7)
+    drow = torch.linspace(-2, 2, 260, device="cuda")
+    drow[5] = 0.0
+    c.reference(drow=drow)
+    lse = c.lse.float()
+    full = c.bwd(binding, lse, drow=drow)
+    for got, ref, tol, what in zip(full, (c.dx, c.dw, c.db), (c.e_dx, c.e_dw, c.e_db), ("dx", "dW", "db")):
+        within(got, ref, tol, what)
+    for k, want in enumerate("xwb"):
+        assert torch.equal(c.bwd(binding, lse, drow=drow, want=want)[k], full[k]), want
+
+
+@gpu
+@pytest.mark.parametrize("prec,V", [(1, 17000), (0, 6000)], ids=["bf16", "fp32"])
+def test_linear_ce_backward_in_chunks(binding, prec, V):
+    """More rows times vocabulary than one chunk of dz holds: sums over chunks, a short last one."""
+    c = Ce(8200, 40, V, prec, True, 0.1, seed=8)
+    lse = c.fwd(binding)[2]
+    dx, dw, db = c.bwd(binding, lse)
+    c.reference()
+    within(lse, c.lse, c.e_lse, "lse")
+    within(dx, c.dx, c.e_dx, "dx")
+    within(dw, c.dw, c.e_dw, "dW")
+    within(db, c.db, c.e_db, "db")
+
+
+@gpu
+@PREC
+def test_linear_ce_rows_that_do_not_count(binding, prec):
+    """Labels outside the vocabulary leave a row out, whatever stands in it; without any row the results are zero."""
+    c = Ce(140, 64, 300, prec, True, seed=9)
+    c.labels[3], c.labels[17], c.labels[139], c.labels[70] = -1, 300, -2 ** 31, 2 ** 31 - 1
+    c.x[3], c.x[17, 5], c.x[139, 0], c.x[70] = NAN, INF, -INF, torch.finfo(c.x.dtype).min
+    c.reference()
+    loss, row, lse = c.fwd(binding)
+    counted = (c.labels >= 0) & (c.labels < 300)
+    within(row, c.row, torch.where(counted, c.e_row, 0.0), "row_loss")
+    within(loss[0], c.loss, c.e_loss, "loss")
+    within(lse[counted], c.lse[counted], c.e_lse[counted], "lse")
+    dx, dw, db = c.bwd(binding, lse)
+    within(dx, c.dx, torch.where(counted[:, None], c.e_dx, 0.0), "dx")
+    within(dw, c.dw, c.e_dw, "dW")
+    within(db, c.db, c.e_db, "db")
+    c.labels.fill_(-1)
+    loss, row, lse = c.fwd(binding)
+    assert float(loss[0]) == 0.0 and not row.any()
+    for g in c.bwd(binding, lse):
+        assert not g.any()
+
+
+@gpu
+@PREC
+def test_linear_ce_masked_vocabulary(binding, prec):
+    """A bias of minus infinity or of the type's lowest value takes entries out of the softmax, whole tiles of them too; a
+    label among them has infinite loss."""
+    c = Ce(40, 64, 900, prec, True, seed=10)
+    c.bias[0:600] = -INF
+    c.bias[700:710] = torch.finfo(c.bias.dtype).min
+    c.labels.clamp_(min=710)
+    c.labels[4] = 5
+    loss, row, lse = c.fwd(binding)
+    z = c.x.double() @ c.w.double().t() + c.bias.double()
+    ref = torch.logsumexp(z, 1)
+    tol = (8 * 6 * 4 + 300) * 2.0 ** -24 * 64
+    within(lse, ref, tol, "lse")
+    assert math.isinf(float(row[4])) and math.isinf(float(loss[0]))
+    keep = torch.arange(40, device="cuda") != 4
+    within(row[keep], (ref - z.gather(1, c.labels.long()[:, None])[:, 0])[keep], tol, "row_loss")
+    c.labels[4] = 800
+    lse = c.fwd(binding)[2]
+    dx, dw, db = c.bwd(binding, lse)
+    assert not dw[0:600].any() and not dw[700:710].any() and not db[0:600].any()
+    assert torch.isfinite(dx).all() and torch.isfinite(dw).all() and torch.isfinite(db).all()
+
+
+@gpu
+@PREC
+def test_linear_ce_non_finite_rows_stay_their_own(binding, prec):
+    """NaN in a row that counts: its own loss and dx are NaN, the other rows' are not touched."""
+    c = Ce(300, 64, 600, prec, False, seed=11)
+    clean_loss, clean_row, clean_lse = c.fwd(binding)
+    clean_dx = c.bwd(binding, clean_lse)[0]
+    c.x[200, 3] = NAN
+    loss, row, lse = c.fwd(binding)
+    assert math.isnan(float(loss[0])) and math.isnan(float(row[200])) and math.isnan(float(lse[200]))
+    keep = torch.arange(300, device="cuda") != 200
+    assert torch.equal(row[keep], clean_row[keep]) and torch.equal(lse[keep], clean_lse[keep])
+    dx = c.bwd(binding, lse)[0]
+    assert torch.isnan(dx[200]).all() and torch.equal(dx[keep], clean_dx[keep])
+
+
+@gpu
+@PREC
+def test_linear_ce_large_logits(binding, prec):
+    """Logits of hundreds: the maximum is subtracted before the exponential; p is zero or one for most."""
+    c = Ce(70, 128, 1500, prec, False, seed=12, logit_std=120.0).reference()
+    loss, row, lse = c.fwd(binding)
+    within(lse, c.lse, c.e_lse, "lse")
+    within(row, c.row, c.e_row, "row_loss")
+    assert float(lse.max()) > 200
+    dx, dw, _ = c.bwd(binding, lse)
+    within(dx, c.dx, c.e_dx, "dx")
+    within(dw, c.dw, c.e_dw, "dW")
+
+
+@gpu
+def test_linear_ce_gradient_against_differences(binding):
+    """The loss's change along a direction of x, of W and of the bias, by central differences of the forward pass."""
+    c = Ce(96, 80, 500, 0, True, 0.2, seed=13)
+    dx, dw, db = c.bwd(binding, c.fwd(binding)[2])
+    h = 2.0 ** -5
+    for name, grad in (("x", dx), ("w", dw), ("bias", db)):
+        t = getattr(c, name)
+        d = randn(*t.shape, seed=14, prec=0)
+        d /= d.norm()
+        kept, at = t.clone(), []
+        for s in (h, -h):
+            t.copy_(kept + s * d)
+            at.append(float(c.fwd(binding)[0]))
+        t.copy_(kept)
+        slope, want = (at[0] - at[1]) / (2 * h), float((grad.double() * d.double()).sum())
+        # the loss is rounded to 2^-24 of ~8 and summed from rows within 1e-6: 2 x 2e-6 / 2h; the third derivative of the
+        # loss along a unit direction is below the logits' change cubed, at most max |W row|^3 < 27 for x and |x row|^3 /
+        # ... for W a single entry of the direction is below 1/10 of it: h^2 / 6 x 27 / 96 bounds both
+        assert abs(slope - want) < 2e-6 / h + h * h / 6 * 27 / 96, (name, slope, want)
+
+
+@gpu
+@PREC
+def test_linear_ce_other_stream_and_recorded(binding, prec):
+    """On a stream of its own; forward and backward recorded into a graph and replayed on new inputs in the same
+    buffers; the same bits every time."""
+    c = Ce(300, 72, 900, prec, True, 0.2, seed=15)
+    other = Ce(300, 72, 900, prec, True, 0.5, seed=16)
+    ref = [c.fwd(binding), other.fwd(binding)]
+    refs = [r + c_.bwd(binding, r[2]) for c_, r in zip((c, other), ref)]
+    stream = torch.cuda.Stream()
+    n, d, v = 300, 72, 900
+    ws = torch.empty(max(binding.linear_ce_workspace_bytes(prec, n, d, v, k) for k in (False, True)), dtype=torch.uint8, device="cuda")
+    out = [f32(1), f32(n), f32(n), torch.empty_like(c.x), torch.empty_like(c.w), f32(v)]
+    torch.cuda.synchronize()
+
+    def step():
+        s = stream.cuda_stream
+        binding.linear_ce_fwd(prec, c.x, c.w, c.bias, c.labels, out[0], out[1], out[2], ws, n, d, v, s)
+        binding.linear_ce_bwd(prec, c.x, c.w, c.bias, c.labels, out[2], None, None, out[3], out[4], out[5], ws, n, d, v, False, s)
+
+    step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, refs[0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for k, src in enumerate((c, other, c)):
+        if k:
+            kept = [t.clone() for t in (src.x, src.w, src.bias, src.labels)] if src is other else first
+            for dst, t in zip((c.x, c.w, c.bias, c.labels), kept):
+                dst.copy_(t)
+        else:
+            first = [t.clone() for t in (c.x, c.w, c.bias, c.labels)]
+        for o in out:
+            o.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, refs[k % 2])), k
+
+
+@gpu
+def test_linear_ce_leaves_what_it_does_not_own(binding):
+    """Buffers with more rows than the call names keep the rows behind the last; inputs are not written."""
+    for prec in (0, 1):
+        c = Ce(300, 65, 270, prec, True, 0.1, seed=17)
+        kept = [t.clone() for t in (c.x, c.w, c.bias, c.labels)]
+        n, d, v = 290, 65, 260
+        ws_bytes = binding.linear_ce_workspace_bytes(prec, n, d, v, True)
+        ws = torch.full((ws_bytes + 4096,), 77, dtype=torch.uint8, device="cuda")
+        loss, row, lse = f32(1), f32(300), f32(300)
+        dx, dw, db = torch.full_like(c.x, 7.0), torch.full_like(c.w, 7.0), f32(270)
+        fws = torch.full((binding.linear_ce_workspace_bytes(prec, n, d, v, False),), 255, dtype=torch.uint8, device="cuda")
+        binding.linear_ce_fwd(prec, c.x, c.w, c.bias, c.labels, loss, row, lse, fws, n, d, v)
+        binding.linear_ce_bwd(prec, c.x, c.w, c.bias, c.labels, lse, None, None, dx, dw, db, ws[:ws_bytes], n, d, v)
+        torch.cuda.synchronize()
+        assert (row[n:] == 7).all() and (lse[n:] == 7).all() and (dx[n:] == 7).all() and (dw[v:] == 7).all() and (db[v:] == 7).all()
+        assert (ws[ws_bytes:] == 77).all()
+        assert all(torch.equal(a, b) for a, b in zip(kept, (c.x, c.w, c.bias, c.labels)))
+
+
+@gpu
+def test_linear_ce_refuses_on_the_gpu(binding):
+    c = Ce(4, 64, 100, 1, seed=18)
+    ws = torch.empty(binding.linear_ce_workspace_bytes(1, 4, 64, 100, False) + 512, dtype=torch.uint8, device="cuda")
+    row = f32(4)
+
+    def call(x=c.x, labels=c.labels, w=c.w, ws=ws, row=row):
+        binding.linear_ce_fwd(1, x, w, None, labels, None, row, None, ws, 4, 64, 100)
+
+    call()
+    for kw in ({"x": c.x.data_ptr() + 2}, {"ws": ws[:512]}, {"ws": ws[8:]}, {"labels": c.labels.cpu()}, {"row": row.cpu()}):
+        with pytest.raises(binding.DdgError) as e:
+            call(**kw)
+        assert e.value.status == 1
+    for kw in ({"x": c.x.float()}, {"w": c.w.t()}, {"labels": c.labels.long()}, {"row": row[:3]}):
+        with pytest.raises(ValueError):
+            call(**kw)
+    torch.cuda.synchronize()
+
+
+# ---- RMS norm -------------------------------------------------------------------------------------------------------
+RMS_SHAPES = [(1, 1), (1, 8), (3, 7), (5, 64), (7, 128), (2, 1000), (9, 1021), (33, 1024), (130, 2048), (4, 4096), (700, 136), (3, 5000),
+              (2, 8192), (3, 16384), (2, 16383), (1300, 40)]
+
+
+def rms_inputs(rows, C, prec, seed):
+    return (randn(rows, C, seed=seed, prec=prec), randn(rows, C, seed=seed + 1, prec=prec, std=3.0),
+            randn(C, seed=seed + 2, prec=prec, std=0.2, mean=1.0))
+
+
+def rms_reference(x, res, gamma, eps):
+    h = x.double() + (res.double() if res is not None else 0.0)
+    rstd = 1.0 / (h.square().mean(1) + eps).sqrt()
+    return h, rstd, h * rstd[:, None] * gamma.double()
+
+
+def rms_rel(C):
+    """Relative error of rstd and, above it, of y in 32 bits: a sum of squares over at most 16 values per thread and a
+    tree of 10 steps (half of it after the root), the addition, the division, rsqrt (2 steps)."""
+    return (13 + 6) * 2.0 ** -24
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("shape", RMS_SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_add_rmsnorm_forward(binding, shape, prec):
+    rows, C = shape
+    x, res, gamma = rms_inputs(rows, C, prec, 21)
+    for r in (res, None):
+        h, y, rstd = torch.full_like(x, 7.0), torch.full_like(x, 7.0), f32(rows)
+        binding.add_rmsnorm_fwd(prec, x, r, gamma, h if r is not None else None, y, None, None, rstd, rows, C)
+        h_ref, rstd_ref, y_ref = rms_reference(x, r, gamma, 1e-6)
+        u, e = U[x.dtype], rms_rel(C) + 2.0 ** -23
+        if r is not None:
+            within(h, h_ref, u * h_ref.abs() + 2.0 ** -24 * h_ref.abs(), "h")
+        within(rstd, rstd_ref, e * rstd_ref, "rstd")
+        within(y, y_ref, (u + e + 2.0 ** -22) * y_ref.abs() + 1e-37, "y")
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("shape", [(1, 128), (5, 4096), (300, 512), (2, 16384), (3, 1021), (1, 1), (17, 2944)], ids=lambda s: "x".join(map(str, s)))
+def test_add_rmsnorm_to_8_bits(binding, shape, prec, group):
+    """Scales against the reference's; the stored values within half a step of e4m3 (2^-4 of the value, 2^-10 below the
+    smallest normal one) of y / scale, and y and q from one call."""
+    rows, C = shape
+    if group and C % group:
+        pytest.skip("no whole groups")
+    x, res, gamma = rms_inputs(rows, C, prec, 31)
+    x[0, : min(C, 128)] = 0.0
+    res[0, : min(C, 128)] = 0.0  # a group of zeros, a row of them where that is all
+    h, y = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    q, scale = torch.empty(rows, C, dtype=torch.float8_e4m3fn, device="cuda"), f32(rows, C // (group or C))
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, q, scale, None, rows, C, group)
+    _, _, y_ref = rms_reference(x, res, gamma, 1e-6)
+    blocks = y_ref.view(rows, -1, group or C)
+    top = blocks.abs().amax(2)
+    s_ref = torch.where(top > 0, top / 448.0, 1.0)
+    e = rms_rel(C) + 2.0 ** -21
+    within(scale, s_ref, e * s_ref, "scale")
+    within(y, y_ref, (U[x.dtype] + e) * y_ref.abs(), "y")
+    got = q.double().view_as(blocks) * scale.double()[..., None]
+    within(got, blocks, (2.0 ** -4 + 2 * e) * blocks.abs() + 2.0 ** -10 * s_ref[..., None] * 1.01, "q")
+    assert float(q.float().abs().max()) == 448.0 or not y_ref.any()
+    q2, scale2 = torch.empty_like(q), torch.empty_like(scale)
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, None, q2, scale2, None, rows, C, group)
+    assert torch.equal(q.view(torch.uint8), q2.view(torch.uint8)) and torch.equal(scale, scale2)
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("shape", RMS_SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_add_rmsnorm_backward(binding, shape, prec):
+    rows, C = shape
+    h, dh, gamma = rms_inputs(rows, C, prec, 41)
+    dy = randn(rows, C, seed=44, prec=prec)
+    rstd = (1.0 / (h.double().square().mean(1) + 1e-6).sqrt()).float()
+    for extra in (dh, None):
+        dx, dgamma = torch.full_like(h, 7.0), f32(C)
+        scratch = f32(binding.rmsnorm_scratch_elems(rows, C), fill=NAN)
+        binding.add_rmsnorm_bwd(prec, dy, extra, h, gamma, rstd, dx, dgamma, scratch, rows, C)
+        r, k, g, d = rstd.double()[:, None], h.double(), gamma.double(), dy.double()
+        dot = (g * d * k).mean(1, keepdim=True)
+        add = extra.double() if extra is not None else torch.zeros_like(k)
+        ref = add + r * (g * d - k * r * r * dot)
+        # products and their sum (at most 16 per thread, a tree), then four roundings of every term
+        e = (16 + 10 + 6) * 2.0 ** -24
+        mass = add.abs() + r * (g * d).abs() + (k * r ** 3).abs() * (g * d * k).abs().mean(1, keepdim=True)
+        within(dx, ref, U[h.dtype] * ref.abs() + e * mass, "dx")
+        dg, dg_mass = (d * k * r).sum(0), (d * k * r).abs().sum(0)
+        # rows / walkers + walkers / 16 + 16 additions
+        within(dgamma, dg, (math.ceil(rows / 592) + 37 + 16 + 3) * 2.0 ** -24 * dg_mass, "dgamma")
+
+
+@gpu
+@PREC
+def test_add_rmsnorm_special_rows(binding, prec):
+    """A row of zeros, of NaN, with an infinity: each row its own."""
+    rows, C = 6, 256
+    x, res, gamma = rms_inputs(rows, C, prec, 51)
+    x[1], res[1] = 0.0, 0.0
+    x[2, 7], x[3, 9] = NAN, INF
+    h, y, q, scale, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, C, dtype=torch.float8_e4m3fn, device="cuda"), f32(rows), f32(rows)
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, q, scale, rstd, rows, C)
+    assert not y[1].any() and float(scale[1]) == 1.0 and not q[1].float().any() and float(rstd[1]) == pytest.approx(1000.0)
+    assert torch.isnan(y[2]).all() and torch.isnan(q[2].float()).all()
+    assert float(rstd[3]) == 0.0 and torch.isnan(y[3, 9]) and not y[3, :9].any()
+    for r in (0, 4, 5):
+        assert torch.isfinite(y[r].float()).all() and torch.isfinite(q[r].float()).all()
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("C", [4096, 1021])
+def test_add_rmsnorm_in_place(binding, prec, C):
+    """h over x or res, y over x, dx over dy, dh or h: the same bits as into buffers of their own."""
+    rows = 19
+    x, res, gamma = rms_inputs(rows, C, prec, 61)
+    h, y, rstd = torch.empty_like(x), torch.empty_like(x), f32(rows)
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, None, None, rstd, rows, C)
+    a, b = x.clone(), res.clone()
+    binding.add_rmsnorm_fwd(prec, a, b, gamma, b, a, None, None, None, rows, C)
+    assert torch.equal(a, y) and torch.equal(b, h)
+    dy, dg, scratch = randn(rows, C, seed=64, prec=prec), f32(C), f32(binding.rmsnorm_scratch_elems(rows, C))
+    dx = torch.empty_like(x)
+    binding.add_rmsnorm_bwd(prec, dy, res, h, gamma, rstd, dx, dg, scratch, rows, C)
+    for k in range(3):
+        t = [dy.clone(), res.clone(), h.clone()]
+        binding.add_rmsnorm_bwd(prec, t[0], t[1], t[2], gamma, rstd, t[k], dg, scratch, rows, C)
+        assert torch.equal(t[k], dx), k
+
+
+@gpu
+@PREC
+def test_add_rmsnorm_off_16_byte_boundaries(binding, prec):
+    """Tensors that start anywhere give the aligned ones' results; only scales per group need the boundary."""
+    rows, C = 5, 512
+    x, res, gamma = rms_inputs(rows, C, prec, 71)
+    y, y2 = torch.empty_like(x), torch.empty(rows * C + 1, dtype=x.dtype, device="cuda")[1:].view(rows, C)
+    h = torch.empty_like(x)
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, None, None, None, rows, C)
+    off = [torch.cat([t.flatten()[:1], t.flatten()])[1:].view(t.shape) for t in (x, res, gamma)]
+    assert off[0].data_ptr() % 16
+    binding.add_rmsnorm_fwd(prec, *off, torch.empty_like(x), y2, None, None, None, rows, C)
+    _, _, ref = rms_reference(x, res, gamma, 1e-6)
+    within(y2, ref, (U[x.dtype] + rms_rel(C) + 2.0 ** -22) * ref.abs(), "y")
+    with pytest.raises(binding.DdgError) as e:
+        binding.add_rmsnorm_fwd(prec, *off, torch.empty_like(x), None, torch.empty(rows, C, dtype=torch.uint8, device="cuda"), f32(rows, 4), None, rows, C, 128)
+    assert e.value.status == 1
+
+
+@gpu
+def test_add_rmsnorm_gradient_against_differences(binding):
+    rows, C = 12, 96
+    x, res, gamma = rms_inputs(rows, C, 0, 81)
+    dy = randn(rows, C, seed=84, prec=0)
+    dh = randn(rows, C, seed=85, prec=0)
+
+    def value(x, gamma):
+        h, y = torch.empty_like(x), torch.empty_like(x)
+        binding.add_rmsnorm_fwd(0, x, res, gamma, h, y, None, None, None, rows, C)
+        return float((y.double() * dy.double()).sum() + (h.double() * dh.double()).sum())
+
+    h, y, rstd, dx, dg = torch.empty_like(x), torch.empty_like(x), f32(rows), torch.empty_like(x), f32(C)
+    binding.add_rmsnorm_fwd(0, x, res, gamma, h, y, None, None, rstd, rows, C)
+    binding.add_rmsnorm_bwd(0, dy, dh, h, gamma, rstd, dx, dg, f32(binding.rmsnorm_scratch_elems(rows, C)), rows, C)
+    step = 2.0 ** -4
+    for t, grad in ((x, dx), (gamma, dg)):
+        d = randn(*t.shape, seed=86, prec=0)
+        d /= d.norm()
+        args = [(t + s * d, gamma) if t is x else (x, t + s * d) for s in (step, -step)]
+        slope, want = (value(*args[0]) - value(*args[1])) / (2 * step), float((grad.double() * d.double()).sum())
+        # values: about sqrt(1152) sums of terms rounded to 2^-22; third derivative: |dy| rstd^3 along a unit direction
+        assert abs(slope - want) < 1152 * 3 * 2.0 ** -22 / step + step ** 2 / 6 * 6 * 40 * 0.05, (slope, want)
+
+
+# ---- dropout --------------------------------------------------------------------------------------------------------
+def philox(key, counter, layer, count):
+    """Philox4x32-10, plain integers."""
+    out = np.empty((count, 4), dtype=np.uint32)
+    for i in range(count):
+        at = (counter + i) % 2 ** 64
+        c, k = [at % 2 ** 32, at >> 32, layer, 0], [key % 2 ** 32, key >> 32]
+        for _ in range(10):
+            p, q = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+            c = [(q >> 32) ^ c[1] ^ k[0], q % 2 ** 32, (p >> 32) ^ c[3] ^ k[1], p % 2 ** 32]
+            k = [(k[0] + 0x9E3779B9) % 2 ** 32, (k[1] + 0xBB67AE85) % 2 ** 32]
+        out[i] = c
+    return out
+
+
+def keep_mask(key, counter, layer, n, p):
+    return (philox(key, counter, layer, -(-n // 8)).view(np.uint16).reshape(-1)[:n] >= round(p * 65536))
+
+
+def rng_of(key, counter):
+    return torch.from_numpy(np.array([key, counter], dtype=np.uint64).view(np.int64)).cuda()
+
+
+def test_philox_of_this_file_gives_the_published_numbers():
+    """The known answers for counter and key of zeros and of ones (Salmon et al., 2011)."""
+    assert [hex(v) for v in philox(0, 0, 0, 1)[0].tolist()] == ["0x6627e8d5", "0xe169c58d", "0xbc57ac4c", "0x9b00dbd8"]
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 255, 4096, 20011])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 1.0])
+def test_dropout(binding, n, p, prec):
+    """Every element against the generator's definition; positions that pass 32 and 64 bits; a layer of its own."""
+    for key, counter, layer in ((0, 0, 0), (0x123456789ABCDEF0, 2 ** 32 - 3, 5), (2 ** 64 - 1, 2 ** 64 - 2, 2 ** 32 - 1)):
+        keep = torch.from_numpy(keep_mask(key, counter, layer, n, p)).cuda()
+        x, res, rng = randn(n, seed=91, prec=prec), randn(n, seed=92, prec=prec), rng_of(key, counter)
+        scale = 65536 / (65536 - round(p * 65536)) if p < 1 else 0.0
+        for r in (res, None):
+            y = torch.full_like(x, 7.0)
+            binding.dropout_fwd(prec, x, r, y, rng, n, p, layer)
+            kept = torch.where(keep, x.double() * scale, 0.0)
+            ref = kept + (r.double() if r is not None else 0.0)
+            within(y, ref, U[x.dtype] * ref.abs() + 3 * 2.0 ** -24 * (kept.abs() + ref.abs()), "y")
+        dx = torch.full_like(x, 7.0)
+        binding.dropout_bwd(prec, x, dx, rng, n, p, layer)
+        assert torch.equal(dx, y), "the backward pass is the forward pass without a residual"
+
+
+@gpu
+@PREC
+def test_dropout_special_values_in_place_and_unaligned(binding, prec):
+    n, p, rng = 1003, 0.5, rng_of(3, 4)
+    keep = torch.from_numpy(keep_mask(3, 4, 0, n, p)).cuda()
+    x, res = torch.full((n,), NAN, device="cuda", dtype=DT[prec]), randn(n, seed=93, prec=prec)
+    y = torch.empty_like(x)
+    binding.dropout_fwd(prec, x, res, y, rng, n, p)
+    assert torch.isnan(y[keep]).all() and torch.equal(y[~keep], res[~keep])
+    x = randn(n, seed=94, prec=prec)
+    binding.dropout_fwd(prec, x, res, y, rng, n, p)
+    for k in range(2):
+        t = [x.clone(), res.clone()]
+        binding.dropout_fwd(prec, t[0], t[1], t[k], rng, n, p)
+        assert torch.equal(t[k], y), k
+    off = torch.full((n + 2,), 7.0, device="cuda", dtype=DT[prec])
+    binding.dropout_fwd(prec, x, res, off[1:], rng, n, p)
+    assert torch.equal(off[1:-1], y) and float(off[0]) == 7.0 and float(off[-1]) == 7.0
+
+
+@gpu
+def test_dropout_share_and_recorded_positions(binding):
+    """The share of dropped values (four standard deviations); a recorded call draws new numbers when the position in
+    device memory moved on, and the old ones when it went back."""
+    n, p = 1 << 20, 0.3
+    x, y, rng = torch.ones(n, device="cuda"), torch.empty(n, device="cuda"), rng_of(7, 0)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        binding.dropout_fwd(0, x, None, y, rng, n, p, 0, torch.cuda.current_stream().cuda_stream)
+    seen = []
+    for at in (0, n // 8, 0):
+        rng[1] = at
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        seen.append(y.clone())
+        share = float((y == 0).double().mean())
+        t = round(p * 65536) / 65536
+        assert abs(share - t) < 4 * math.sqrt(t * (1 - t) / n)
+    assert torch.equal(seen[0], seen[2]) and not torch.equal(seen[0], seen[1])
+    both = (seen[0] == 0) & (seen[1] == 0)
+    assert abs(float(both.double().mean()) - t * t) < 4 * math.sqrt(t * t * (1 - t * t) / n)
+
+
+# ---- the three in a row ---------------------------------------------------------------------------------------------
+@gpu
+def test_tail_of_a_training_step(binding):
+    """dropout + residual -> RMS norm -> projection and loss, and all of it backwards and into the update, in 32 bits,
+    against automatic differentiation of the formulas in 64."""
+    n, d, v, p, eps, lr = 200, 96, 700, 0.25, 1e-5, 0.5
+    x, res, gamma = randn(n, d, seed=101, prec=0), randn(n, d, seed=102, prec=0), randn(d, seed=103, prec=0, std=0.2, mean=1.0)
+    w = randn(v, d, seed=104, prec=0, std=0.2)
+    labels = torch.randint(0, v, (n,), device="cuda", dtype=torch.int32)
+    labels[::7] = -1
+    rng = rng_of(11, 12)
+    h, y, rstd = torch.empty_like(x), torch.empty_like(x), f32(n)
+    loss, lse = f32(1), f32(n)
+    ws = torch.empty(max(binding.linear_ce_workspace_bytes(0, n, d, v, k) for k in (0, 1)), dtype=torch.uint8, device="cuda")
+    binding.dropout_fwd(0, x, res, h, rng, n * d, p)
+    binding.add_rmsnorm_fwd(0, h, None, gamma, None, y, None, None, rstd, n, d, 0, eps)
+    binding.linear_ce_fwd(0, y, w, None, labels, loss, None, lse, ws, n, d, v)
+    dy, dw, dh, dgamma, dx = torch.empty_like(x), torch.empty_like(w), torch.empty_like(x), f32(d), torch.empty_like(x)
+    binding.linear_ce_bwd(0, y, w, None, labels, lse, None, None, dy, dw, None, ws, n, d, v, True)
+    binding.add_rmsnorm_bwd(0, dy, None, h, gamma, rstd, dh, dgamma, f32(binding.rmsnorm_scratch_elems(n, d)), n, d)
+    binding.dropout_bwd(0, dh, dx, rng, n * d, p)
+    w_new, mom, version = w.clone(), torch.zeros_like(w), torch.empty_like(w)
+    binding.sgd_update(0, w_new, mom, dw, version, v * d, lr, 0.0, 0.0)
+    keep = torch.from_numpy(keep_mask(11, 12, 0, n * d, p)).cuda().view(n, d)
+    leaves = [t.double().requires_grad_() for t in (x, res, gamma, w)]
+    X, R, G, W = leaves
+    hh = R + torch.where(keep, X / (1 - p), 0.0)
+    yy = hh * torch.rsqrt(hh.square().mean(1, keepdim=True) + eps) * G
+    z = yy @ W.t()
+    counted = labels >= 0
+    ref = (torch.logsumexp(z, 1) - z.gather(1, labels.clamp(min=0).long()[:, None])[:, 0])[counted].mean()
+    ref.backward()
+    # the longest way to a gradient: 6 x 6 steps of the projection's accumulator (four units each), 6 x 44 of the gradient's,
+    # and under 100 single roundings; every step relative to sums of absolute values, which exceed the sums' norm by less
+    # than a factor sqrt(700)
+    tol = (4 * (36 + 264) + 100) * 2.0 ** -24 * math.sqrt(700)
+    assert abs(float(loss[0]) - float(ref)) < 2.0 ** -16 * float(ref)
+    for got, leaf, name in ((dx, X, "x"), (dh, R, "res"), (dgamma, G, "gamma"), (dw, W, "w")):
+        assert float((got.double() - leaf.grad).norm() / leaf.grad.norm()) < tol, name
+    assert torch.equal(version, w_new)
+    within(w_new, W.detach() - lr * W.grad, lr * tol * W.grad.norm() + 2.0 ** -23 * W.detach().abs(), "the updated projection")
+
+
+# ---- refusals without a GPU -----------------------------------------------------------------------------------------
+def status(fn, *args):
+    from paper_1804_10574_b200 import binding as b
+    with pytest.raises(b.DdgError) as e:
+        fn(*args)
+    return e.value.status
+
+
+P = 1 << 20  # an address that no refused call looks at
+
+
+class Ws:
+    """A workspace of a size of its own at that address."""
+
+    def __init__(self, n, at=P):
+        self.n, self.at = n, at
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return 1
+
+    def data_ptr(self):
+        return self.at
+
+
+def test_linear_ce_refusals(binding):
+    need = binding.linear_ce_workspace_bytes(1, 4, 64, 100, False)
+    assert need > 0 and binding.linear_ce_workspace_bytes(1, 4, 64, 100, True) > 0
+    for bad in ((2, 4, 64, 100), (1, 0, 64, 100), (1, 4, 0, 100), (1, 4, 64, 0), (1, 4, 64, (1 << 24) + 1)):
+        assert binding.linear_ce_workspace_bytes(*bad, False) == 0
+    ok = dict(prec=1, x=P, W=P, bias=None, labels=P, loss=P, row_loss=P, lse=P, ws=Ws(need), B=4, n_in=64, n_out=100)
+    fwd = lambda **kw: status(binding.linear_ce_fwd, *{**ok, **kw}.values())  # noqa: E731
+    assert fwd(prec=2) == 1 and fwd(prec=-1) == 1
+    for name in ("x", "W", "labels", "ws"):
+        assert fwd(**{name: None}) == 1
+    assert fwd(loss=None, row_loss=None, lse=None) == 1
+    for name in ("B", "n_in", "n_out"):
+        assert fwd(**{name: 0}) == 3 and fwd(**{name: -5}) == 3 and fwd(**{name: 1 << 25}) == 3
+    assert fwd(x=P + 2) == 1 and fwd(W=P + 8) == 1                 # read in place: 16-byte boundaries
+    assert fwd(ws=Ws(need - 1)) == 1 and fwd(ws=Ws(need, P + 16)) == 1
+    assert b"workspace" in binding.lib().ddg_last_error(None)
+    need = binding.linear_ce_workspace_bytes(1, 4, 64, 100, True)
+    okb = dict(prec=1, x=P, W=P, bias=None, labels=P, lse=P, dloss=None, drow=None, dx=P, dW=P, db=None, ws=Ws(need), B=4, n_in=64, n_out=100)
+    bwd = lambda **kw: status(binding.linear_ce_bwd, *{**okb, **kw}.values())  # noqa: E731
+    for name in ("x", "W", "labels", "lse", "ws"):
+        assert bwd(**{name: None}) == 1
+    assert bwd(dx=None, dW=None) == 1 and bwd(dloss=P, drow=P) == 1
+    assert bwd(B=0) == 3 and bwd(ws=Ws(need - 1)) == 1 and bwd(prec=7) == 1
+
+
+def test_rmsnorm_refusals(binding):
+    ok = dict(prec=1, x=P, res=P, gamma=P, h=P, y=P, y8=None, s8=None, rstd=None, rows=3, C=256, group=0, eps=1e-6)
+    fwd = lambda **kw: status(binding.add_rmsnorm_fwd, *{**ok, **kw}.values())  # noqa: E731
+    assert fwd(prec=3) == 1 and fwd(x=None) == 1 and fwd(gamma=None) == 1 and fwd(y=None) == 1 and fwd(h=None) == 1
+    assert fwd(y8=P) == 1 and fwd(s8=P) == 1                       # values and scales come together
+    assert fwd(eps=-1.0) == 1 and fwd(eps=NAN) == 1 and fwd(eps=INF) == 1
+    assert fwd(group=64) == 1 and fwd(y8=P, s8=P, group=128, C=200) == 3 and fwd(y8=P, s8=P, group=128, x=P + 2) == 1
+    assert fwd(rows=0) == 3 and fwd(C=0) == 3 and fwd(C=16385) == 3
+    okb = dict(prec=1, dy=P, dh=None, h=P, gamma=P, rstd=P, dx=P, dgamma=P, scratch=P, rows=3, C=256)
+    bwd = lambda **kw: status(binding.add_rmsnorm_bwd, *{**okb, **kw}.values())  # noqa: E731
+    for name in ("dy", "h", "gamma", "rstd", "dx", "dgamma", "scratch"):
+        assert bwd(**{name: None}) == 1
+    assert bwd(rows=0) == 3 and bwd(C=16385) == 3
+    assert binding.rmsnorm_scratch_elems(0, 8) == 0 and binding.rmsnorm_scratch_elems(2, 16385) == 0 and binding.rmsnorm_scratch_elems(2, 8) > 0
+
+
+def test_dropout_refusals(binding):
+    ok = dict(prec=1, x=P, res=None, y=P, rng=P, n=8, p=0.1)
+    fwd = lambda **kw: status(binding.dropout_fwd, *{**ok, **kw}.values())  # noqa: E731
+    assert fwd(prec=9) == 1 and fwd(x=None) == 1 and fwd(y=None) == 1 and fwd(rng=None) == 1
+    assert fwd(p=-0.1) == 1 and fwd(p=1.5) == 1 and fwd(p=NAN) == 1 and fwd(rng=P + 4) == 1 and fwd(n=0) == 3
+    assert status(binding.dropout_bwd, 1, None, P, P, 8, 0.1) == 1
+
+
+def test_tensor_arguments_are_checked_in_the_binding(binding):
+    """What a C call cannot see: strides, element sizes and lengths of the tensors behind the addresses."""
+    x = torch.zeros(4, 8)
+    for bad in (x.t(), x.half(), x[:2]):
+        with pytest.raises(ValueError):
+            binding.dropout_fwd(0, bad, None, P, P, 32, 0.1)
