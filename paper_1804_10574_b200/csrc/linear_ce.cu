@@ -11,10 +11,17 @@
 //              and at the end dx = scale * (sum of its partials).
 //
 // All four products run on one tcgen05 kernel.  What bounds it: 2NVD (forward) and 6NVD (backward) multiply-adds on the
-// tensor cores; for a few rows the bytes of W.  Two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each
-// loads half of A and half of B (32 KB for 64 values of K instead of 48 KB for two tiles of their own), so that the L2
-// can feed the tensor cores; six such stages are in flight by TMA, and two accumulators (512 TMEM columns) let the
-// epilogue of a tile run under the next tile's products.
+// tensor cores; for a few rows the bytes of W.  Two CTAs of a cluster work on one tile of 256 x 512 or 256 x 256
+// (cta_group::2): each loads half of A and half of B by TMA, four stages of 48 KB or six of 32 KB in flight.  The tensor
+// cores are fed from the L2, and the wide tile asks a quarter less of it for the same products (halving B's loads took
+// 8192 x 4096 x 65536 from 3.09 to 2.69 ms in an experiment, one to three more stages changed nothing).  The 512 TMEM
+// columns are two accumulators of 256: the halves of a wide tile, or successive tiles of the narrow one.  The epilogue
+// warps copy an accumulator to registers (128 columns of a row per thread) and hand it back at once; what they do with
+// the values runs under the next products.
+//
+// The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
+// 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
+// cut after 128 steps (16 for fp32 tensors) and the pieces added in registers, rounded to nearest.
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,
 // l h are accumulated, smallest first: what is left out is below 2^-24 of the value.
@@ -29,50 +36,64 @@ namespace ddg {
 
 namespace {
 
-constexpr int kTile = 256;        // rows and columns of a tile of the CTA pair
-constexpr int kHalf = 128;        // rows of A and of B that one CTA of the pair loads
-constexpr int kKBox = 64;         // K values of a stage: 128 bytes of bf16, one swizzle row
-constexpr int kStages = 6;
-constexpr int kStageBytes = 2 * kHalf * kKBox * 2;  // per CTA: A half + B half
-constexpr int kEpiWarps = 8;      // two per TMEM lane quarter, each half of the columns
+constexpr int kTile = 256;        // rows of a tile of the CTA pair, columns of an accumulator
+constexpr int kHalf = 128;        // rows of A, and of B per accumulator, that one CTA of the pair loads
+constexpr int kKBox = 64;         // K values of a box: 128 bytes of bf16, one swizzle row
+// A stage, per CTA: 128 rows of A and 128 or 256 of B, 128 or 64 K values wide.  What a stage costs the thread that
+// issues its products (two barriers, descriptors) has to stay below the 1024 cycles they take.
+template <int NT> struct Stage {  // NT: columns of a tile
+    static constexpr int kw = NT == kTile ? 2 * kKBox : kKBox;
+    static constexpr int block = kHalf * kw * 2;  // one operand's 128 rows
+    static constexpr int bytes = (1 + NT / kTile) * block;
+    static constexpr int count = 192 * 1024 / bytes;
+};
+constexpr int kEpiWarps = 8;      // two per TMEM lane quarter, each half of an accumulator's columns
 constexpr int kThreads = 64 + 32 * kEpiWarps;
-constexpr int kCeSmem = kStages * kStageBytes + 1024;
+constexpr int kStageRing = 192 * 1024;
+constexpr int kOutBuf = 32 * kKBox * 2;  // an epilogue warp's 32 rows of 64 bf16 values on their way out
+constexpr int kCeSmem = kStageRing + kEpiWarps * kOutBuf + 1024;
 constexpr int kMaxSeg = 6;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kLse, kDz, kPartial, kWeightGrad };
 
+// Set when a bounded wait ran out, and never cleared: from then on results on this device are NaN.
+__device__ int g_ce_error;
+
 // What the workspace starts with.
 struct CeHeader {
-    int err;            // a bounded wait ran out: the kernels that write the results turn them into NaN
     unsigned ticket;    // blocks of the joining kernel that are done
     float scale;        // factor on dx and dW: upstream gradient / counted rows
-    int pad[61];
+    int pad[62];
 };
 static_assert(sizeof(CeHeader) == 256, "the buffers behind the header stay aligned");
 
+enum Out { kStore, kAdd, kFinal };
+
 struct CeGemm {
     int M, N;                 // rows of A, rows of B (columns of the result)
-    int kblocks, n_seg;       // 64-wide K blocks per segment; segments: pairs of bf16 terms
+    int K, kblocks, n_seg;    // K values and blocks of a segment; segments: pairs of bf16 terms
     int a_off[kMaxSeg], b_off[kMaxSeg];  // where a segment's term starts: in K (K-major operand) or in M / N
-    int a_r0, b_r0, b_k0;     // coordinates of the first row of A and of B and of B's first K value
+    int b_r0, b_k0;           // coordinates of B's first row and of its first K value
     int tiles_m, tiles_n, splits, group_m;
+    int piece;                // K blocks of a chain (with PROMOTE)
     CeHeader *head;
     // kLse, kDz
     const void *bias;         // nullable, at column 0 of this launch
     int bias_bf16;
     const int *labels;        // label of every row; columns are v0 + n
     int v0, V;
-    float2 *part;             // kLse: [2 tiles_n][M] (maximum, sum)
+    float2 *part;             // kLse: [ceil(N / 128)][M] (maximum, sum)
     float *zlab;              // kLse: logit of the label
     const float *lse, *drow;  // kDz
-    bf16 *dz;                 // kDz: [M][planes * dz_plane]
-    int planes, dz_plane;
+    int planes, dz_plane;     // kDz: dz is [M][planes * dz_plane]
     float *db_part;           // kDz, nullable: [ceil(M / 32)][dz_plane]
-    // kPartial: fp32 [splits][M][ld];  kWeightGrad: [M][ld] in the element type
+    // kPartial (dx): fp32 sums [splits][M][ld] stored or added to, or, as kFinal, dx itself [M][N] from the product and
+    // the sums so far (part_in, nullable).  kWeightGrad: [M][N].
     void *out;
+    int out_kind, out_bf16, out_tma, out_vec, ld;  // out_tma: bf16 that a tensor map can write
     size_t out_split;
-    int ld, accumulate, out_bf16, out_vec;
+    const float *part_in;
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
@@ -84,8 +105,10 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// Hands an accumulator back.  What it orders are the tcgen05 loads before the fence, not memory: a releasing arrival would
+// wait for the stores of the tile before (gradient of the logits, 4096 x 512 x 16384: 94 us with it, 75 us without).
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // one half of a stage: lands in this CTA's shared memory, counts on the barrier of the pair's first CTA
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, uint32_t cluster_bar, int c0, int c1) {
@@ -102,6 +125,11 @@ __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t adesc, uint64
         ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
 // arrives on the barrier at this offset in both CTAs when the MMAs issued so far are done
 __device__ __forceinline__ void commit_pair(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
@@ -111,24 +139,27 @@ __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx
 
 // Which tile a work item is: all tiles of a split, in bands of group_m tile rows that are walked column by column, so
 // that the operands of the tiles in flight stay in the L2.
-struct CeItem { int split, m, n, kb0, kb1; };
-__device__ __forceinline__ CeItem ce_item(const CeGemm &g, int item) {
-    CeItem it;
-    const int per = g.tiles_m * g.tiles_n;
-    it.split = item / per;
-    int r = item - it.split * per;
-    const int band = r / (g.group_m * g.tiles_n);
-    r -= band * g.group_m * g.tiles_n;
-    const int rows = min(g.group_m, g.tiles_m - band * g.group_m);
-    it.n = r / rows;
-    it.m = band * g.group_m + r - it.n * rows;
+// Divisions by sizes known at launch only cost an issuing thread a hundred cycles each, in which the tensor cores run
+// dry: the K range has none without splits, and the product of the two factors fits 32 bits (at most 2^21 x 74).
+struct CeTile { int m, n; };
+__device__ __forceinline__ int ce_split(const CeGemm &g, int item) { return g.splits == 1 ? 0 : item / (g.tiles_m * g.tiles_n); }
+__device__ __forceinline__ void ce_range(const CeGemm &g, int split, int &kb0, int &kb1) {
     const int kb = g.kblocks * g.n_seg;
-    it.kb0 = (int)((long long)kb * it.split / g.splits);
-    it.kb1 = (int)((long long)kb * (it.split + 1) / g.splits);
-    return it;
+    kb0 = 0;
+    kb1 = kb;
+    if (g.splits > 1) {
+        kb0 = (int)((unsigned)(kb * split) / (unsigned)g.splits);
+        kb1 = (int)((unsigned)(kb * (split + 1)) / (unsigned)g.splits);
+    }
+}
+__device__ __forceinline__ CeTile ce_tile(const CeGemm &g, int item, int split) {
+    unsigned r = (unsigned)(item - split * g.tiles_m * g.tiles_n);
+    const unsigned band = r / (unsigned)(g.group_m * g.tiles_n);
+    r -= band * g.group_m * g.tiles_n;
+    const unsigned rows = min(g.group_m, g.tiles_m - (int)band * g.group_m), n = r / rows;
+    return CeTile{(int)(band * g.group_m + r - n * rows), (int)n};
 }
 
-// 32 columns of one row, v[0..32) in two halves, to the three places a value can go
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -159,151 +190,209 @@ __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
     return v[0];
 }
 
+__device__ __forceinline__ void red_add4(float *p, float a, float b, float c, float d) {
+    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
+
+// 32 values of a row at columns col .. of a [.][n] matrix in the element type
+__device__ __forceinline__ void store_row32(void *out, int bf16_out, int vec, size_t row, int col, int n, const float *v) {
+    const size_t at = row * n + col;
+    if (bf16_out) {
+        bf16 *dst = (bf16 *)out + at;
+        if (vec) {  // n is a multiple of 8
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+                if (col + j < n)
+                    *reinterpret_cast<uint4 *>(dst + j) = make_uint4(pack2(v[j], v[j + 1]), pack2(v[j + 2], v[j + 3]), pack2(v[j + 4], v[j + 5]), pack2(v[j + 6], v[j + 7]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (col + j < n) dst[j] = __float2bfloat16_rn(v[j]);
+        }
+    } else {
+        float *dst = (float *)out + at;
+        if (vec) {  // n is a multiple of 4
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+                if (col + j < n) *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (col + j < n) dst[j] = v[j];
+        }
+    }
+}
+
+// 64 columns of the warp's 32 rows as bf16 to (x, y) of a matrix, through shared memory: whole 128-byte lines leave by
+// TMA, and rows and columns past the matrix are clipped.  (Stores of 64 bytes a thread, straight from registers, took the
+// logits' gradient at 4096 x 512 x 16384 89 us.)
+__device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t buf, int lane, int x, int y, const float *v) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the box before has been read
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)  // the 128-byte swizzle of the map
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(pack2(v[8 * j], v[8 * j + 1])),
+                     "r"(pack2(v[8 * j + 2], v[8 * j + 3])), "r"(pack2(v[8 * j + 4], v[8 * j + 5])), "r"(pack2(v[8 * j + 6], v[8 * j + 7]))
+                     : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(buf), "r"(x), "r"(y) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+
+// What becomes of 128 columns of one row: v at columns col0 .., which are piece `part` (of 128 columns) of the row.
 template <int MODE>
-__device__ __forceinline__ void ce_epilogue(const CeGemm &g, const CeItem &it, uint32_t acc, int quarter, int half, int rank, int lane,
-                                            uint32_t release_bar) {
-    const int row = it.m * kTile + rank * kHalf + 32 * quarter + lane;
-    const int col0 = it.n * kTile + half * kHalf;
-    const uint32_t taddr = acc + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(half * kHalf);
+__device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *map_out, uint32_t buf, float (&v)[kHalf], int split, int row, int col0, int lane) {
     const bool live = row < g.M;
-    float top = -INFINITY, sum = 0.f, lse = 0.f, weight = 0.f;
+    float lse = 0.f, weight = 0.f;
     int label = -1;
     if ((MODE == kLse || MODE == kDz) && live) {
         const int y = g.labels[row];
-        label = y >= 0 && y < g.V ? y - g.v0 : -1 - kTile;  // column of this launch (a label of another chunk meets none)
+        const bool counted = y >= 0 && y < g.V;
+        label = counted ? y - g.v0 : -1 - 2 * kTile;  // column of this launch (a label of another chunk meets none)
         if (MODE == kDz) {
             lse = g.lse[row];
-            weight = y >= 0 && y < g.V ? (g.drow ? g.drow[row] : 1.f) : 0.f;
+            weight = counted ? (g.drow ? g.drow[row] : 1.f) : 0.f;
         }
     }
-#pragma unroll 1
-    for (int c = 0; c < kHalf; c += 32) {
-        float v[32];
-        tc_ld32(taddr + (uint32_t)c, reinterpret_cast<float(&)[16]>(v[0]), reinterpret_cast<float(&)[16]>(v[16]));
-        tc_wait_ld();
-        if (c + 32 == kHalf) {  // the accumulator is read: the next tile's products may overwrite it
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(release_bar);
-        }
-        const int col = col0 + c;
-        if (MODE == kLse || MODE == kDz) {
-            if (g.bias) {
+    if (MODE == kLse || MODE == kDz) {
+        if (g.bias) {
+#pragma unroll
+            for (int c = 0; c < kHalf; c += 32) {
                 float b[32];
-                load_bias32(g, col, b);
+                load_bias32(g, col0 + c, b);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] += b[j];
+                for (int j = 0; j < 32; ++j) v[c + j] += b[j];
             }
         }
-        if (MODE == kLse) {
-            if (col + 32 > g.N) {
+    }
+    if (MODE == kLse) {
+        if (col0 + kHalf > g.N) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (col + j >= g.N) v[j] = -INFINITY;
-            }
-            float m = v[0];
+            for (int j = 0; j < kHalf; ++j)
+                if (col0 + j >= g.N) v[j] = -INFINITY;
+        }
+        if (label >= col0 && label < col0 + kHalf) {
+            float z = 0.f;
 #pragma unroll
-            for (int j = 1; j < 32; ++j) m = fmaxf(m, v[j]);
-            m = fmaxf(top, m);
-            const float ref = m == -INFINITY ? 0.f : m;  // nothing but -inf so far
-            float s0 = sum * exp2_approx((top - ref) * kLog2e), s1 = 0.f;
+            for (int j = 0; j < kHalf; ++j)
+                if (label == col0 + j) z = v[j];
+            g.zlab[row] = z;
+        }
+        float m[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                s0 += exp2_approx((v[j] - ref) * kLog2e);
-                s1 += exp2_approx((v[j + 1] - ref) * kLog2e);
-            }
-            top = m;
-            sum = s0 + s1;
-            if (label >= col && label < col + 32) {
-                float z = 0.f;
+        for (int j = 4; j < kHalf; ++j) m[j & 3] = fmaxf(m[j & 3], v[j]);
+        const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        const float ref = top == -INFINITY ? 0.f : top;  // nothing but -inf
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (label == col + j) z = v[j];
-                g.zlab[row] = z;
-            }
-        } else if (MODE == kDz) {
+        for (int j = 0; j < kHalf; ++j) s[j & 3] += exp2_approx((v[j] - ref) * kLog2e);
+        if (live && col0 < g.N) g.part[(size_t)(col0 / kHalf) * g.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+    } else if (MODE == kDz) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const float p = exp2_approx((v[j] - lse) * kLog2e) - (label == col + j ? 1.f : 0.f);
-                // a row that does not count gives exact zeros whatever its logits are; so do columns past the vocabulary
-                v[j] = weight != 0.f && col + j < g.N ? p * weight : 0.f;
-            }
-            if (g.db_part) {  // rows that are not there hold zeros
+        for (int j = 0; j < kHalf; ++j) v[j] = exp2_approx((v[j] - lse) * kLog2e);
+        if (label >= col0 && label < col0 + kHalf) {
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j)
+                if (label == col0 + j) v[j] -= 1.f;
+        }
+        if (g.drow) {
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) v[j] *= weight;
+        }
+        // a row that does not count gives exact zeros whatever its logits are; so do columns past the vocabulary
+        if (__any_sync(0xffffffffu, weight == 0.f)) {
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) v[j] = weight == 0.f ? 0.f : v[j];
+        }
+        if (col0 + kHalf > g.N) {
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j)
+                if (col0 + j >= g.N) v[j] = 0.f;
+        }
+        if (g.db_part) {  // rows that are not there hold zeros
+            const int block = (row - lane) / 32;
+#pragma unroll
+            for (int c = 0; c < kHalf; c += 32) {
                 float t[32];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) t[j] = v[j];
+                for (int j = 0; j < 32; ++j) t[j] = v[c + j];
                 const float cs = column_sums(t, lane);
-                const int block = (it.m * kTile + rank * kHalf) / 32 + quarter;
-                if (block * 32 < g.M) g.db_part[(size_t)block * g.dz_plane + col + lane] = cs;
-            }
-            if (live) {
-                bf16 *dst = g.dz + (size_t)row * g.planes * g.dz_plane + col;
-                for (int p = 0; p < g.planes; ++p, dst += g.dz_plane) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) w[j] = pack2(v[2 * j], v[2 * j + 1]);
-                    st_global_32(dst, reinterpret_cast<const uint32_t(&)[8]>(w[0]));
-                    st_global_32(dst + 16, reinterpret_cast<const uint32_t(&)[8]>(w[8]));
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] -= bf16_round(v[j]);
-                }
-            }
-        } else if (MODE == kPartial) {
-            if (live) {
-                float *dst = (float *)g.out + it.split * g.out_split + (size_t)row * g.ld + col;
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    if (col + j < g.ld) {  // ld is a multiple of 4
-                        float4 q = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                        if (g.accumulate) {
-                            const float4 o = *reinterpret_cast<const float4 *>(dst + j);
-                            q = make_float4(q.x + o.x, q.y + o.y, q.z + o.z, q.w + o.w);
-                        }
-                        *reinterpret_cast<float4 *>(dst + j) = q;
-                    }
-                }
-            }
-        } else {
-            if (live) {
-                const float scale = g.head->scale;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] *= scale;
-                const size_t at = (size_t)row * g.ld + col;
-                if (g.out_bf16) {
-                    bf16 *dst = (bf16 *)g.out + at;
-                    if (g.out_vec) {  // ld is a multiple of 8
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            if (col + j < g.ld)
-                                *reinterpret_cast<uint4 *>(dst + j) = make_uint4(pack2(v[j], v[j + 1]), pack2(v[j + 2], v[j + 3]),
-                                                                                 pack2(v[j + 4], v[j + 5]), pack2(v[j + 6], v[j + 7]));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j < g.ld) dst[j] = __float2bfloat16_rn(v[j]);
-                    }
-                } else {
-                    float *dst = (float *)g.out + at;
-                    if (g.out_vec) {  // ld is a multiple of 4
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            if (col + j < g.ld) *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j < g.ld) dst[j] = v[j];
-                    }
-                }
+                if (block * 32 < g.M && col0 + c < g.dz_plane) g.db_part[(size_t)block * g.dz_plane + col0 + c + lane] = cs;
             }
         }
+        if (row - lane >= g.M) return;
+        for (int p = 0;;) {
+#pragma unroll
+            for (int c = 0; c < kHalf; c += kKBox)
+                if (col0 + c < g.dz_plane) store_box(map_out, buf, lane, p * g.dz_plane + col0 + c, row - lane, v + c);
+            if (++p == g.planes) break;
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) v[j] -= bf16_round(v[j]);
+        }
+    } else if (MODE == kPartial) {
+        if (row - lane >= g.M) return;
+        if (g.out_kind == kFinal) {
+            const float scale = g.head->scale;
+            const int y = live ? g.labels[row] : -1;
+            const bool counted = y >= 0 && y < g.V;
+#pragma unroll
+            for (int c = 0; c < kHalf; c += 32) {
+                if (col0 + c >= g.N) break;
+                if (g.part_in && live) {
+                    const float *src = g.part_in + (size_t)row * g.ld + col0 + c;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        if (col0 + c + j < g.ld) {
+                            const float4 o = *reinterpret_cast<const float4 *>(src + j);
+                            v[c + j] += o.x; v[c + j + 1] += o.y; v[c + j + 2] += o.z; v[c + j + 3] += o.w;
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[c + j] = counted ? v[c + j] * scale : 0.f;
+                if (g.out_tma) {
+                    if (c % kKBox == 32) store_box(map_out, buf, lane, col0 + c - 32, row - lane, v + c - 32);
+                    else if (col0 + c + 32 >= g.N) store_box(map_out, buf, lane, col0 + c, row - lane, v + c);  // what follows is clipped
+                } else if (live) {
+                    store_row32(g.out, g.out_bf16, g.out_vec, row, col0 + c, g.N, v + c);
+                }
+            }
+        } else if (live) {
+            float *dst = (float *)g.out + split * g.out_split + (size_t)row * g.ld + col0;
+#pragma unroll
+            for (int j = 0; j < kHalf; j += 4) {
+                if (col0 + j >= g.ld) break;  // ld is a multiple of 4
+                if (g.out_kind == kAdd) red_add4(dst + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+                else *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
+        }
+    } else {
+        if (row - lane >= g.M) return;
+        const float scale = g.head->scale;
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) v[j] *= scale;
+        if (g.out_tma) {
+#pragma unroll
+            for (int c = 0; c < kHalf; c += kKBox)
+                if (col0 + c < g.N) store_box(map_out, buf, lane, col0 + c, row - lane, v + c);
+        } else if (live) {
+#pragma unroll
+            for (int c = 0; c < kHalf; c += 32)
+                if (col0 + c < g.N) store_row32(g.out, g.out_bf16, g.out_vec, row, col0 + c, g.N, v + c);
+        }
     }
-    if (MODE == kLse && live) g.part[(size_t)(2 * it.n + half) * g.M + row] = make_float2(top, sum);
 }
 
-// A_MN / B_MN: the operand lies with M / N innermost (its rows are K values) instead of K.
-template <int MODE, bool A_MN, bool B_MN>
+// A_MN / B_MN: the operand lies with M / N innermost (its rows are K values) instead of K.  NT: columns of a tile.
+// PROMOTE (NT = 256): an accumulator holds at most g.piece K blocks, the epilogue adds the pieces.
+template <int MODE, bool A_MN, bool B_MN, int NT, bool PROMOTE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CeGemm g) {
+ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CeGemm g) {
+    static_assert(NT == kTile || (NT == 2 * kTile && !PROMOTE), "tiles are one or two accumulators wide");
+    constexpr int kStages = Stage<NT>::count, kStageBytes = Stage<NT>::bytes, kBlockBytes = Stage<NT>::block, kw = Stage<NT>::kw, kHalves = NT / kTile;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_holder;
@@ -311,7 +400,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const Waiter wt{&abort_flag, &g.head->err, kSpinLimit};
+    const Waiter wt{&abort_flag, &g_ce_error, kSpinLimit};
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 2 * kEpiWarps); }
@@ -323,7 +412,8 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     pdl_launch();
-    pdl_wait();
+    pdl_wait();  // nothing above touches global memory
+    if (MODE == kLse && blockIdx.x == 0 && threadIdx.x == 0) g.head->ticket = 0;
     tc_fence_before();
     __syncthreads();
     cluster_sync();  // both CTAs' barriers are ready
@@ -335,31 +425,38 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (warp == 0) {
         if (lane == 0) {  // loads
             bool ok = true;
-            uint32_t n = 0;
+            uint32_t s = 0, ph = 0;
             for (int item = first; item < n_items && ok; item += step) {
-                const CeItem it = ce_item(g, item);
-                const int m0 = it.m * kTile + (int)rank * kHalf, n0 = it.n * kTile + (int)rank * kHalf;
-                int seg = it.kb0 / g.kblocks, kb = it.kb0 - seg * g.kblocks;
-                for (int i = it.kb0; i < it.kb1; ++i, ++n) {
-                    const uint32_t s = n % kStages, ph = (n / kStages) & 1u;
+                const int split = ce_split(g, item);
+                const CeTile t = ce_tile(g, item, split);
+                int kb0, kb1;
+                ce_range(g, split, kb0, kb1);
+                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * NT + (int)rank * kHalf;
+                int seg = kb0 == 0 ? 0 : kb0 / g.kblocks, kb = kb0 - seg * g.kblocks;
+                for (int i = kb0; i < kb1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 51)) { ok = false; break; }
                     if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * kStageBytes);
                     const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
-                    const uint32_t a = base + s * kStageBytes, b = a + kStageBytes / 2;
-                    const int k = kb * kKBox;
-                    if (A_MN) {
-                        tma_load_pair(a, &map_a, bar, g.a_off[seg] + m0, k);
-                        tma_load_pair(a + 8192, &map_a, bar, g.a_off[seg] + m0 + 64, k);
-                    } else {
-                        tma_load_pair(a, &map_a, bar, g.a_off[seg] + k, g.a_r0 + m0);
+                    const uint32_t a = base + s * kStageBytes;
+                    const int k = kb * kw;
+                    // K-major: a box is 64 K values of 128 rows.  MN-major: 64 rows of kw K values.
+#pragma unroll
+                    for (int j = 0; j < (A_MN ? 2 : kw / kKBox); ++j) {
+                        if (A_MN) tma_load_pair(a + j * (kBlockBytes / 2), &map_a, bar, g.a_off[seg] + m0 + kKBox * j, k);
+                        else tma_load_pair(a + j * (kHalf * kKBox * 2), &map_a, bar, g.a_off[seg] + k + kKBox * j, m0);
                     }
-                    if (B_MN) {
-                        tma_load_pair(b, &map_b, bar, g.b_off[seg] + n0, g.b_k0 + k);
-                        tma_load_pair(b + 8192, &map_b, bar, g.b_off[seg] + n0 + 64, g.b_k0 + k);
-                    } else {
-                        tma_load_pair(b, &map_b, bar, g.b_off[seg] + k, g.b_r0 + n0);
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h) {
+                        const uint32_t b = a + (1 + h) * kBlockBytes;
+                        const int nn = n0 + h * kTile;
+#pragma unroll
+                        for (int j = 0; j < (B_MN ? 2 : kw / kKBox); ++j) {
+                            if (B_MN) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, g.b_off[seg] + nn + kKBox * j, g.b_k0 + k);
+                            else tma_load_pair(b + j * (kHalf * kKBox * 2), &map_b, bar, g.b_off[seg] + k + kKBox * j, g.b_r0 + nn);
+                        }
                     }
                     if (++kb == g.kblocks) { kb = 0; ++seg; }
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
             if (!ok)
@@ -367,45 +464,114 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {  // products, for both CTAs
+        if (rank == 0) {
+            // Products, for both CTAs.  The tensor cores wait for this loop when a K block takes it longer to issue than to
+            // multiply, so it is kept straight: the whole warp walks it and one elected lane issues; waits for an
+            // accumulator and what follows its last K block stand outside (with them inside, under one lane,
+            // 8192 x 4096 x 65536 took 3.56 ms instead of 2.92).
+            const bool issuer = elect_one();
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                                    ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-            bool ok = true;
-            uint32_t n = 0, t = 0;
-            for (int item = first; item < n_items && ok; item += step, ++t) {
-                const CeItem it = ce_item(g, item);
-                const uint32_t acc = t & 1u;
-                if (!mbar_wait(smem_u32(&acc_empty[acc]), ((t >> 1) & 1u) ^ 1u, wt, 52)) break;
-                tc_fence_after();
-                for (int i = it.kb0; i < it.kb1; ++i, ++n) {
-                    const uint32_t s = n % kStages, ph = (n / kStages) & 1u;
-                    if (!mbar_wait(smem_u32(&full[s]), ph, wt, 53)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t a = base + s * kStageBytes, b = a + kStageBytes / 2;
-                    // K-major: 16 K values are 32 bytes of a swizzle row.  MN-major: 16 rows of 128 bytes; the next 64
-                    // of the 128 M / N values lie 8 KB further.
-                    const uint64_t ad = A_MN ? make_desc(a, 1024, 2u, 8192) : make_desc(a, 1024, 2u);
-                    const uint64_t bd = B_MN ? make_desc(b, 1024, 2u, 8192) : make_desc(b, 1024, 2u);
+            // K-major: 16 K values are 32 bytes of a swizzle row, the next 64 values 16 KB further.  MN-major: 16 rows of
+            // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
+            const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
+            const uint64_t bd0 = B_MN ? make_desc(base + kBlockBytes, 1024, 2u, kBlockBytes / 2) : make_desc(base + kBlockBytes, 1024, 2u);
+            auto multiply = [&](uint32_t s, int h, uint32_t acc, bool fresh) {
 #pragma unroll
-                    for (int k = 0; k < kKBox / 16; ++k)
-                        mma_pair(tmem + acc * kTile, ad + (A_MN ? 128 : 2) * k, bd + (B_MN ? 128 : 2) * k, idesc, i > it.kb0 || k > 0);
-                    commit_pair(smem_u32(&empty[s]));
+                for (int k = 0; k < kw / 16; ++k) {
+                    const uint32_t at = s * (kStageBytes >> 4), kk = (uint32_t)((k >> 2) * (kHalf * kKBox * 2 >> 4) + (k & 3) * 2);
+                    mma_pair(tmem + acc * kTile, ad0 + (uint64_t)(at + (A_MN ? 128u * k : kk)),
+                             bd0 + (uint64_t)(at + h * (kBlockBytes >> 4) + (B_MN ? 128u * k : kk)), idesc, !fresh || k > 0);
                 }
-                if (ok) commit_pair(smem_u32(&acc_full[acc]));
+            };
+            bool ok = true;
+            uint32_t s = 0, ph = 0, u = 0;  // stage, its parity, accumulators used so far
+            for (int item = first; item < n_items && ok; item += step) {
+                int kb0, kb1;
+                ce_range(g, ce_split(g, item), kb0, kb1);
+                for (int i0 = kb0; i0 < kb1; u += kHalves) {
+                    const int i1 = PROMOTE ? min(i0 + g.piece, kb1) : kb1;
+                    // the first K block waits for the accumulators, one after the other
+                    ok = mbar_wait(smem_u32(&full[s]), ph, wt, 53);
+#pragma unroll
+                    for (int h = 0; h < kHalves && ok; ++h) {
+                        const uint32_t acc = (u + h) & 1u;
+                        ok = mbar_wait(smem_u32(&acc_empty[acc]), (((u + h) >> 1) & 1u) ^ 1u, wt, 52);
+                        tc_fence_after();
+                        if (ok && issuer) multiply(s, h, acc, true);
+                    }
+                    if (!ok) break;
+                    if (issuer) commit_pair(smem_u32(&empty[s]));
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                    for (int i = i0 + 1; i < i1; ++i) {
+                        if (!mbar_wait(smem_u32(&full[s]), ph, wt, 53)) { ok = false; break; }
+                        tc_fence_after();
+                        if (issuer) {
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h) multiply(s, h, (u + h) & 1u, false);
+                            commit_pair(smem_u32(&empty[s]));
+                        }
+                        if (++s == kStages) { s = 0; ph ^= 1u; }
+                    }
+                    if (!ok) break;
+                    if (issuer) {
+#pragma unroll
+                        for (int h = 0; h < kHalves; ++h) commit_pair(smem_u32(&acc_full[(u + h) & 1u]));
+                    }
+                    i0 = i1;
+                }
             }
         }
         __syncwarp();
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        uint32_t t = 0;
-        for (int item = first; item < n_items; item += step, ++t) {
-            const CeItem it = ce_item(g, item);
-            const uint32_t acc = t & 1u;
-            bool ok = mbar_wait(smem_u32(&acc_full[acc]), (t >> 1) & 1u, wt, 54);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            tc_fence_after();
-            ce_epilogue<MODE>(g, it, tmem + acc * kTile, quarter, half, (int)rank, lane, map_rank(smem_u32(&acc_empty[acc]), 0));
+        uint32_t u = 0;
+        bool ok = true;
+        for (int item = first; item < n_items && ok; item += step) {
+            const int split = ce_split(g, item);
+            const CeTile t = ce_tile(g, item, split);
+            const int row = t.m * kTile + (int)rank * kHalf + 32 * quarter + lane;
+            int pieces = 1;
+            if (PROMOTE) {
+                int kb0, kb1;
+                ce_range(g, split, kb0, kb1);
+                pieces = (kb1 - kb0 + g.piece - 1) / g.piece;
+            }
+#pragma unroll 1
+            for (int h = 0; h < kHalves; ++h) {
+                float v[kHalf];
+#pragma unroll 1
+                for (int piece = 0; piece < pieces; ++piece, ++u) {
+                    const uint32_t acc = u & 1u;
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&acc_full[acc]), (u >> 1) & 1u, wt, 54));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t taddr = tmem + acc * kTile + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(half * kHalf);
+                    if (!PROMOTE || piece == 0) {
+#pragma unroll
+                        for (int c = 0; c < kHalf; c += 32)
+                            tc_ld32(taddr + (uint32_t)c, reinterpret_cast<float(&)[16]>(v[c]), reinterpret_cast<float(&)[16]>(v[c + 16]));
+                        tc_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < kHalf; c += 32) {
+                            float w[32];
+                            tc_ld32(taddr + (uint32_t)c, reinterpret_cast<float(&)[16]>(w[0]), reinterpret_cast<float(&)[16]>(w[16]));
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[c + j] += w[j];
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(map_rank(smem_u32(&acc_empty[acc]), 0));
+                }
+                if (!ok) break;
+                ce_finish<MODE>(g, &map_out, base + kStageRing + (uint32_t)(warp - 2) * kOutBuf, v, split, row, t.n * NT + h * kTile + half * kHalf, lane);
+            }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
     tc_fence_before();
     __syncthreads();
@@ -414,34 +580,41 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
+    if ((MODE == kPartial || MODE == kWeightGrad) && threadIdx.x == 0 && *(volatile int *)&g_ce_error) {
+        if ((MODE == kWeightGrad || g.out_kind == kFinal) && g.out_bf16) *(bf16 *)g.out = __float2bfloat16_rn(__int_as_float(0x7fffffff));
+        else *(float *)g.out = __int_as_float(0x7fffffff);
+    }
     cluster_sync();
 }
 
 // ---- joining the forward pass ----------------------------------------------------------------------------------------
-// rows rows per block of 256 threads, the other 256 / rows threads share a row's pieces.  The mean is taken by the block
+// rows rows per block of 512 threads, the 512 / rows threads of a row share its pieces, eight loads in flight each.  The mean is taken by the block
 // that finishes last, over the blocks' sums in index order.
-__global__ void __launch_bounds__(256) ce_join_kernel(const float2 *__restrict__ part, int n_part, const float *__restrict__ zlab, const int *__restrict__ labels,
+constexpr int kJoin = 512;
+__global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict__ part, int n_part, const float *__restrict__ zlab, const int *__restrict__ labels,
                                                       float *__restrict__ loss, float *__restrict__ row_loss, float *__restrict__ lse_out,
                                                       double *__restrict__ sums, CeHeader *head, int B, int V, int rows) {
-    __shared__ float sm[256], ss[256];
+    __shared__ float sm[kJoin], ss[kJoin];
     __shared__ double bl[32];
     __shared__ int bc[32], last;
     pdl_launch();
     pdl_wait();
-    const int r = threadIdx.x & (rows - 1), t0 = threadIdx.x / rows, lanes = 256 / rows;
+    const int r = threadIdx.x & (rows - 1), t0 = threadIdx.x / rows, lanes = kJoin / rows;
     const int row = blockIdx.x * rows + r;
     float m = -INFINITY, s = 0.f;
     if (row < B) {
-        for (int t = t0; t < n_part; t += 4 * lanes) {  // four loads in flight
-            float2 q[4];
+        for (int t = t0; t < n_part; t += 8 * lanes) {
+            float2 q[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) q[u] = t + u * lanes < n_part ? part[(size_t)(t + u * lanes) * B + row] : make_float2(-INFINITY, 0.f);
+            for (int u = 0; u < 8; ++u) q[u] = t + u * lanes < n_part ? part[(size_t)(t + u * lanes) * B + row] : make_float2(-INFINITY, 0.f);
+            float top = m;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float top = fmaxf(m, q[u].x), ref = top == -INFINITY ? 0.f : top;
-                s = s * expf(m - ref) + q[u].y * expf(q[u].x - ref);
-                m = top;
-            }
+            for (int u = 0; u < 8; ++u) top = fmaxf(top, q[u].x);
+            const float ref = top == -INFINITY ? 0.f : top;
+            s *= expf(m - ref);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += q[u].y * expf(q[u].x - ref);
+            m = top;
         }
     }
     sm[threadIdx.x] = m;
@@ -456,7 +629,7 @@ __global__ void __launch_bounds__(256) ce_join_kernel(const float2 *__restrict__
         }
         __syncthreads();
     }
-    const bool failed = head->err != 0;
+    const bool failed = g_ce_error != 0;
     if (t0 == 0) {
         float l = 0.f;
         int counted = 0;
@@ -483,14 +656,14 @@ __global__ void __launch_bounds__(256) ce_join_kernel(const float2 *__restrict__
     }
     __syncthreads();
     if (last && loss) {
-        __shared__ double fa[256], fc[256];
+        __shared__ double fa[kJoin], fc[kJoin];
         __threadfence();
         double a = 0.0, c = 0.0;
-        for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) { a += __ldcg(sums + 2 * i); c += __ldcg(sums + 2 * i + 1); }
+        for (int i = threadIdx.x; i < (int)gridDim.x; i += kJoin) { a += __ldcg(sums + 2 * i); c += __ldcg(sums + 2 * i + 1); }
         fa[threadIdx.x] = a;
         fc[threadIdx.x] = c;
         __syncthreads();
-        for (int o = 128; o > 0; o >>= 1) {
+        for (int o = kJoin / 2; o > 0; o >>= 1) {
             if ((int)threadIdx.x < o) { fa[threadIdx.x] += fa[threadIdx.x + o]; fc[threadIdx.x] += fc[threadIdx.x + o]; }
             __syncthreads();
         }
@@ -569,22 +742,18 @@ __global__ void __launch_bounds__(256) ce_db_kernel(const float *__restrict__ db
     __syncthreads();
     if (w == 0 && c < cols) {
         for (int i = 1; i < 8; ++i) a += fold[i][lane];
-        db[c] = head->err ? __int_as_float(0x7fffffff) : (float)(a * (double)head->scale);
+        db[c] = g_ce_error ? __int_as_float(0x7fffffff) : (float)(a * (double)head->scale);
     }
 }
 
 // dx[n][c] = scale * sum_s part[s][n][c]; rows that do not count are zero
 template <typename T>
 __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ part, int splits, size_t split_stride, int ld, const int *__restrict__ labels, T *__restrict__ dx,
-                                                    int B, int in, int V, int vec, const CeHeader *head, void *dW, int dw_bf16) {
+                                                    int B, int in, int V, int vec, const CeHeader *head) {
     pdl_launch();
     pdl_wait();
-    const bool failed = head->err != 0;
+    const bool failed = g_ce_error != 0;
     const float scale = head->scale, nan = __int_as_float(0x7fffffff);
-    if (failed && dW && blockIdx.x == 0 && threadIdx.x == 0) {
-        if (dw_bf16) *(bf16 *)dW = __float2bfloat16_rn(nan); else *(float *)dW = nan;
-    }
-    if (!dx) return;
     const size_t total = (size_t)B * (ld / 4);
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
         const size_t row = i / (ld / 4);
@@ -623,6 +792,10 @@ int sm_count() {
 // read twice; larger chunks mean fewer passes over the fp32 partial sums of dx.
 constexpr size_t kDzBytes = (size_t)256 << 20;
 constexpr int kPairs = 74;  // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
+constexpr double kWideCost = 0.97;  // time of a product in a 256 x 512 tile against a 256 x 256 one
+constexpr int kPieceBf16 = 2048, kPieceF32 = 256;  // K values of a chain whose result stays in 32 bits
+
+double ce_rounds(int M, int N, int nt, int splits);
 
 struct CePlan {
     int planes, plane;       // terms of an element, columns of a term in a packed operand
@@ -636,14 +809,14 @@ struct CePlan {
 CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     CePlan p{};
     p.planes = prec == P_F32 ? 3 : 1;
-    p.plane = prec == P_F32 ? up(in, 64) : up(in, 8);
+    p.plane = prec == P_F32 ? up(in, 2 * kKBox) : up(in, 8);  // a stage never reaches into the next term
     p.pack_w = prec == P_F32 || in % 8 != 0;
     p.pack_x = p.pack_w || backward;
     // an fp32 dW of bf16 operands gets 16 bits of dz (two terms), as the fully connected layer's loss gradient does; a bf16
     // dW or dx is rounded to 8 bits itself and takes dz rounded once to bf16
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = 2 * ((out + kTile - 1) / kTile);
+    p.n_part = (out + kHalf - 1) / kHalf;
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -657,12 +830,18 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
         const size_t fit = kDzBytes / ((size_t)B * p.dz_planes * 2) / kTile * kTile;
         p.chunk = (int)std::min<size_t>((size_t)up(out, kTile), std::max<size_t>(kTile, fit));
         p.dx_ld = up(in, 4);
-        const int tiles = p.tiles_m * ((in + kTile - 1) / kTile);
-        const int kb = std::min(p.chunk, up(out, kKBox)) / kKBox * (prec == P_F32 ? 6 : 1);
-        p.splits = std::max(1, std::min(kPairs / tiles, kb / 8));
+        // dx: K is the chunk's columns.  It is split over CTA pairs where the tiles alone fill the GPU badly; each split
+        // costs a write and a read of its partial sums.  Seconds by 1.4 PFLOP/s and 6 TB/s.
+        const int kb = (int)std::min<long>(p.chunk, up(out, kKBox)) / kKBox * (prec == P_F32 ? 6 : 1);
+        double best = 1e30;
+        for (int n = 1; n <= std::max(1, std::min(kPairs, kb / 8)); ++n) {
+            const double rounds = prec == P_F32 ? ce_rounds(B, in, kTile, n) : std::min(ce_rounds(B, in, kTile, n), in > kTile ? ce_rounds(B, in, 2 * kTile, n) : 1e30);
+            const double t = rounds * 2.0 * kTile * kTile * kKBox * kb * kPairs / 1.4e15 + (n > 1 ? 2e-6 + 8.0 * n * B * p.dx_ld / 6e12 : 0.0);
+            if (t < best) { best = t; p.splits = n; }
+        }
         p.dz = take((size_t)B * p.dz_planes * p.chunk * 2);
         p.db = take((size_t)((B + 31) / 32) * p.chunk * 4);
-        p.dx = take((size_t)p.splits * B * p.dx_ld * 4);
+        if (p.splits > 1 || p.chunk < out) p.dx = take((size_t)p.splits * B * p.dx_ld * 4);
     }
     p.bytes = at;
     return p;
@@ -680,25 +859,56 @@ bool ce_map(const void *ptr, int rows, int cols, size_t ld, int box_rows, CUtens
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, bool A_MN, bool B_MN>
-int ce_launch(const CUtensorMap &a, const CUtensorMap &b, CeGemm &g, const Launch &s) {
-    g.tiles_m = (g.M + kTile - 1) / kTile;
-    g.tiles_n = (g.N + kTile - 1) / kTile;
-    if (g.splits < 1) g.splits = 1;
-    g.group_m = 16;
+// An operand: a row-major bf16 matrix in memory.
+struct CeOperand { const void *ptr; int rows, cols; };
+
+template <int MODE, bool A_MN, bool B_MN, int NT, bool PROMOTE>
+int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, CeGemm &g, const Launch &s) {
+    constexpr int kw = Stage<NT>::kw;
+    CUtensorMap ma, mb, mo{};
+    if (out.ptr && !ce_map(out.ptr, out.rows, out.cols, out.cols, 32, &mo)) return -1;
+    if (!ce_map(a.ptr, a.rows, a.cols, a.cols, A_MN ? kw : kHalf, &ma) || !ce_map(b.ptr, b.rows, b.cols, b.cols, B_MN ? kw : kHalf, &mb)) return -1;
+    g.kblocks = (g.K + kw - 1) / kw;
+    g.piece = (g.n_seg > 2 ? kPieceF32 : kPieceBf16) / kw;
+    g.tiles_n = (g.N + NT - 1) / NT;
+    g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
     const long items = (long)g.tiles_m * g.tiles_n * g.splits;
     if (items > 0x7fffffff) return -1;
     static thread_local int ready_dev = -1;  // the attribute belongs to a device
     int dev = 0;
     cudaGetDevice(&dev);
     if (ready_dev != dev) {
-        if (cudaFuncSetAttribute(ce_gemm_kernel<MODE, A_MN, B_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCeSmem) != cudaSuccess) return -1;
+        if (cudaFuncSetAttribute(ce_gemm_kernel<MODE, A_MN, B_MN, NT, PROMOTE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCeSmem) != cudaSuccess) return -1;
         ready_dev = dev;
     }
     const int pairs = (int)std::min<long>(items, sm_count() / 2);
-    Launch plain(s.s, 0, s.shared, s.err);
-    launch_k(ce_gemm_kernel<MODE, A_MN, B_MN>, 2 * pairs, kThreads, kCeSmem, plain, a, b, g);
+    launch_k(ce_gemm_kernel<MODE, A_MN, B_MN, NT, PROMOTE>, 2 * pairs, kThreads, kCeSmem, s, ma, mb, mo, g);
     return 1;
+}
+
+// Rounds of the GPU's CTA pairs that `tiles` tiles (times splits) take, in units of one 256 x 256 tile of the whole K.
+double ce_rounds(int M, int N, int nt, int splits) {
+    const long items = (long)((M + kTile - 1) / kTile) * ((N + nt - 1) / nt) * splits;
+    return (double)((items + kPairs - 1) / kPairs) * (nt / kTile) * (nt > kTile ? kWideCost : 1.0) / splits;
+}
+bool ce_wide(int M, int N, int splits) {
+    return N > kTile && ce_rounds(M, N, 2 * kTile, splits) <= ce_rounds(M, N, kTile, splits);
+}
+
+// exact: the result stays in 32 bits, so that long chains are cut (see the top of the file)
+template <int MODE, bool A_MN, bool B_MN>
+int ce_launch(const CeOperand &a, const CeOperand &b, const CeOperand &out, CeGemm &g, bool exact, const Launch &s) {
+    g.tiles_m = (g.M + kTile - 1) / kTile;
+    if (g.splits < 1) g.splits = 1;
+    g.group_m = 16;
+    const long chain = (long)g.K * g.n_seg / g.splits;
+    if (exact && chain > (g.n_seg > 2 ? kPieceF32 : kPieceBf16)) return ce_launch_as<MODE, A_MN, B_MN, kTile, true>(a, b, out, g, s);
+    // The softmax's epilogues are long, and a wide tile leaves no accumulator to multiply into meanwhile (forward pass,
+    // 4096 x 1024 x 32000: 223 us wide, 200 us narrow); the other products' are short (dW, 8192 x 4096 x 16384: 691 us
+    // wide, 809 us narrow), so that there the rounds decide.
+    if constexpr (MODE == kPartial || MODE == kWeightGrad)
+        if (ce_wide(g.M, g.N, g.splits)) return ce_launch_as<MODE, A_MN, B_MN, 2 * kTile, false>(a, b, out, g, s);
+    return ce_launch_as<MODE, A_MN, B_MN, kTile, false>(a, b, out, g, s);
 }
 
 // terms of A and of B that are multiplied, smallest products first
@@ -735,24 +945,20 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
     const CePlan p = ce_plan(prec, B, in, out, false, false);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
-    const Launch plain(s.s, 0, s.shared, s.err);
-    if (cudaMemsetAsync(head, 0, sizeof(CeHeader), s) != cudaSuccess) return -1;
     int n = 0;
-    if (p.pack_x) { n += pack(prec, x, base + p.x, nullptr, B, in, p, out, head, 0, 0, nullptr, plain); x = base + p.x; }
-    if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, plain); W = base + p.w; }
+    if (p.pack_x) { n += pack(prec, x, base + p.x, nullptr, B, in, p, out, head, 0, 0, nullptr, s); x = base + p.x; }
+    if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, s); W = base + p.w; }
     const int cols = p.pack_w ? p.planes * p.plane : in;
-    CUtensorMap ma, mb;
-    if (!ce_map(x, B, cols, cols, kHalf, &ma) || !ce_map(W, out, cols, cols, kHalf, &mb)) return -1;
     CeGemm g{};
-    g.M = B; g.N = out; g.kblocks = (p.plane + kKBox - 1) / kKBox; g.head = head;
+    g.M = B; g.N = out; g.K = p.plane; g.head = head;
     ce_segments(g, p.planes, p.plane, p.planes, p.plane);
     g.bias = bias; g.bias_bf16 = prec == P_BF16; g.labels = labels; g.V = out;
     g.part = (float2 *)(base + p.part); g.zlab = (float *)(base + p.zlab);
-    const int r = ce_launch<kLse, false, false>(ma, mb, g, s);
+    const int r = ce_launch<kLse, false, false>(CeOperand{x, B, cols}, CeOperand{W, out, cols}, CeOperand{}, g, true, s);
     if (r < 0) return r;
     int rows = 1;
     while (rows < 32 && rows < B) rows *= 2;
-    launch_k(ce_join_kernel, (B + rows - 1) / rows, 256, 0, plain, (const float2 *)g.part, p.n_part, (const float *)g.zlab, labels, loss, row_loss, lse,
+    launch_k(ce_join_kernel, (B + rows - 1) / rows, kJoin, 0, s, (const float2 *)g.part, p.n_part, (const float *)g.zlab, labels, loss, row_loss, lse,
              (double *)(base + p.sums), head, B, out, rows);
     return n + r + 1;
 }
@@ -762,44 +968,51 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
     const CePlan p = ce_plan(prec, B, in, out, true, dw_f32 != 0);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
-    const Launch plain(s.s, 0, s.shared, s.err);
-    if (cudaMemsetAsync(head, 0, sizeof(CeHeader), s) != cudaSuccess) return -1;
-    int n = pack(prec, x, base + p.x, labels, B, in, p, out, head, 1, drow == nullptr, dloss, plain);
+    int n = pack(prec, x, base + p.x, labels, B, in, p, out, head, 1, drow == nullptr, dloss, s);
     const void *xp = base + p.x;
-    if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, plain); W = base + p.w; }
+    if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, s); W = base + p.w; }
     const int x_cols = p.planes * p.plane, w_cols = p.pack_w ? p.planes * p.plane : in;
     const int dz_cols = p.dz_planes * p.chunk;
     bf16 *dz = (bf16 *)(base + p.dz);
-    CUtensorMap mx, mw, mx_mn, mw_mn, mz, mz_mn;
-    if (!ce_map(xp, B, x_cols, x_cols, kHalf, &mx) || !ce_map(W, out, w_cols, w_cols, kHalf, &mw) || !ce_map(xp, B, x_cols, x_cols, kKBox, &mx_mn) ||
-        !ce_map(W, out, w_cols, w_cols, kKBox, &mw_mn) || !ce_map(dz, B, dz_cols, dz_cols, kHalf, &mz) || !ce_map(dz, B, dz_cols, dz_cols, kKBox, &mz_mn))
-        return -1;
+    const CeOperand ox{xp, B, x_cols}, ow{W, out, w_cols}, oz{dz, B, dz_cols};
     const int es = prec == P_BF16 ? 2 : 4;
+    const bool dx_direct = p.splits == 1;  // the last chunk's product writes dx itself
     for (int v0 = 0; v0 < out; v0 += p.chunk) {
         const int cols = std::min(p.chunk, out - v0);
         {
             CeGemm g{};
-            g.M = B; g.N = cols; g.kblocks = (p.plane + kKBox - 1) / kKBox; g.head = head; g.b_r0 = v0;
+            g.M = B; g.N = cols; g.K = p.plane; g.head = head; g.b_r0 = v0;
             ce_segments(g, p.planes, p.plane, p.planes, p.plane);
             g.bias = bias ? (const uint8_t *)bias + (size_t)v0 * es : nullptr;
             g.bias_bf16 = prec == P_BF16; g.labels = labels; g.v0 = v0; g.V = out;
-            g.lse = lse; g.drow = drow; g.dz = dz; g.planes = p.dz_planes; g.dz_plane = p.chunk;
+            g.lse = lse; g.drow = drow; g.planes = p.dz_planes; g.dz_plane = p.chunk;
             g.db_part = db ? (float *)(base + p.db) : nullptr;
-            const int r = ce_launch<kDz, false, false>(mx, mw, g, s);
+            const int r = ce_launch<kDz, false, false>(ox, ow, oz, g, prec == P_F32 || db, s);
             if (r < 0) return r;
             n += r;
         }
         if (db) {
-            launch_k(ce_db_kernel, ceil_div(cols, 32), 256, 0, plain, (const float *)(base + p.db), (B + 31) / 32, p.chunk, db + v0, cols, (const CeHeader *)head);
+            launch_k(ce_db_kernel, ceil_div(cols, 32), 256, 0, s, (const float *)(base + p.db), (B + 31) / 32, p.chunk, db + v0, cols, (const CeHeader *)head);
             ++n;
         }
         if (dx) {
             CeGemm g{};
-            g.M = B; g.N = in; g.kblocks = (cols + kKBox - 1) / kKBox; g.head = head; g.b_k0 = v0;
+            CeOperand o{};  // written by TMA
+            g.M = B; g.N = in; g.K = cols; g.head = head; g.b_k0 = v0;
             ce_segments(g, p.planes, p.chunk, p.planes, p.plane);
-            g.splits = std::min(p.splits, g.kblocks * g.n_seg);  // a short last chunk adds to the first partials only
-            g.out = base + p.dx; g.ld = p.dx_ld; g.out_split = (size_t)B * p.dx_ld; g.accumulate = v0 > 0;
-            const int r = ce_launch<kPartial, false, true>(mz, mw_mn, g, s);
+            g.splits = p.splits;  // a short last chunk may take fewer: it adds to the first partials only
+            g.ld = p.dx_ld; g.out_split = (size_t)B * p.dx_ld;
+            if (dx_direct && v0 + cols >= out) {
+                g.out = dx; g.out_kind = kFinal; g.labels = labels; g.V = out;
+                g.part_in = v0 > 0 ? (const float *)(base + p.dx) : nullptr;
+                g.out_bf16 = prec == P_BF16;
+                g.out_vec = (in * es) % 16 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15) == 0;
+                g.out_tma = g.out_bf16 && g.out_vec;
+                if (g.out_tma) o = CeOperand{dx, B, in};
+            } else {
+                g.out = base + p.dx; g.out_kind = v0 > 0 ? kAdd : kStore;
+            }
+            const int r = ce_launch<kPartial, false, true>(oz, ow, o, g, prec == P_F32, s);
             if (r < 0) return r;
             n += r;
         }
@@ -807,24 +1020,26 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
             const bool out_bf16 = prec == P_BF16 && !dw_f32;
             const int oe = out_bf16 ? 2 : 4;
             CeGemm g{};
-            g.M = cols; g.N = in; g.kblocks = (B + kKBox - 1) / kKBox; g.head = head;
+            g.M = cols; g.N = in; g.K = B; g.head = head;
             ce_segments(g, p.dz_planes, p.chunk, p.planes, p.plane);
-            g.out = (uint8_t *)dW + (size_t)v0 * in * oe; g.ld = in; g.out_bf16 = out_bf16;
+            g.out = (uint8_t *)dW + (size_t)v0 * in * oe; g.out_bf16 = out_bf16;
             g.out_vec = (in * oe) % 16 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0;
-            const int r = ce_launch<kWeightGrad, true, true>(mz_mn, mx_mn, g, s);
+            g.out_tma = out_bf16 && g.out_vec;
+            const CeOperand o = g.out_tma ? CeOperand{g.out, cols, in} : CeOperand{};
+            const int r = ce_launch<kWeightGrad, true, true>(oz, ox, o, g, !out_bf16, s);
             if (r < 0) return r;
             n += r;
         }
     }
-    const int grid = dx ? grid_for((size_t)B * (p.dx_ld / 4)) : 1;
+    if (!dx || dx_direct) return n;
+    const int grid = grid_for((size_t)B * (p.dx_ld / 4));
     const int vec = in % 4 == 0 && (reinterpret_cast<uintptr_t>(dx) & (4 * es - 1)) == 0;
-    const int dw_bf16 = prec == P_BF16 && !dw_f32;
     if (prec == P_BF16)
-        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, plain, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec,
-                 (const CeHeader *)head, dW, dw_bf16);
+        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec,
+                 (const CeHeader *)head);
     else
-        launch_k(ce_dx_kernel<float>, grid, 256, 0, plain, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec,
-                 (const CeHeader *)head, dW, dw_bf16);
+        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec,
+                 (const CeHeader *)head);
     return n + 1;
 }
 
