@@ -33,6 +33,7 @@ template <bool MAX> __device__ __forceinline__ float row_reduce(float v, bool on
 }
 
 // what rms_plan gives a row of at most 16384 values
+constexpr int kWarpRowThreads = 256;  // of a backward block whose warps have a row each
 constexpr int rms_max_threads(int vec, int iter) { return (vec == 4 && iter == 4) || (vec == 1 && iter == 16) ? 1024 : 512; }
 
 template <int VEC> __device__ __forceinline__ void store_q(uint8_t *p, const float (&v)[VEC]) {
@@ -136,95 +137,131 @@ __global__ void __launch_bounds__(rms_max_threads(VEC, ITER)) rms_fwd_kernel(con
     }
 }
 
-// Blocks (or warps, where a row is one warp's) walk the rows; each keeps its share of dgamma in registers and leaves it in
-// part[walker][C] for the folding kernel.  dx may be dy, dh or h.
-template <typename T, int VEC, int ITER>
-__global__ void __launch_bounds__(rms_max_threads(VEC, ITER)) rms_bwd_kernel(const T *dy, const T *dh, const T *h, const T *__restrict__ gamma, const float *__restrict__ rstd, T *dx,
-                                                       float *__restrict__ part, int rows, int C, int tpr) {
+// One row's share of a thread as it lies in memory.
+template <typename T, int VEC, int ITER> struct RawRow {
+    Pack<T, VEC> v[ITER];
+    __device__ __forceinline__ void load(const T *p, int t, int tpr, int C) {
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * tpr + t) * VEC;
+            if (c < C) v[i] = *reinterpret_cast<const Pack<T, VEC> *>(p + c);
+        }
+    }
+    __device__ __forceinline__ float at(int i, int j) const { return to_f(v[i].v[j]); }
+};
+
+// Blocks (or warps, where a row is one warp's) walk the rows; each keeps its share of dgamma in registers, a block's warps
+// add theirs up, and part[block][C] goes to the folding kernel.  With up to two vectors a thread, the next row's dy, h and dh
+// are loaded before this row's reduction, so that memory stays busy through its two barriers; with more there are no
+// registers for it.  dx may be dy, dh or h: a row is written after it was read, and the row that is loaded ahead is
+// the same walker's.
+template <typename T, int VEC, int ITER, bool WARP>
+__global__ void __launch_bounds__(WARP ? kWarpRowThreads : rms_max_threads(VEC, ITER), WARP ? (ITER == 1 ? 3 : 2) : (ITER == 1 ? 2 : 1))
+rms_bwd_kernel(const T *dy, const T *dh, const T *h, const T *__restrict__ gamma, const float *__restrict__ rstd, T *dx, float *__restrict__ part, int rows, int C) {
+    constexpr bool kAhead = ITER <= 2;
     __shared__ float red[32];
+    extern __shared__ float shares[];  // WARP: [warps][C]
     pdl_launch();
     pdl_wait();
-    const bool one_warp = tpr == 32;
-    const int t = one_warp ? (threadIdx.x & 31) : threadIdx.x;
-    const int walkers = one_warp ? gridDim.x * (blockDim.x >> 5) : gridDim.x;
-    const int walker = one_warp ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-    if (walker >= rows) return;  // a spare warp of the last block
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int tpr = WARP ? 32 : blockDim.x, t = WARP ? (threadIdx.x & 31) : threadIdx.x;
+    const int walkers = WARP ? gridDim.x * warps : gridDim.x;
+    int row = WARP ? blockIdx.x * warps + warp : blockIdx.x;
     float acc[ITER][VEC];
 #pragma unroll
     for (int i = 0; i < ITER; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) acc[i][j] = 0.f;
-    for (int row = walker; row < rows; row += walkers) {
-        const size_t at = (size_t)row * C;
-        const float r = rstd[row];
-        float a[ITER][VEC], b[ITER][VEC];  // gamma dy, h
+    typedef RawRow<T, VEC, ITER> Raw;
+    Raw g, a, b, d, next_a, next_b, next_d;
+    float r = 0.f, next_r = 0.f;
+    if (kAhead) g.load(gamma, t, tpr, C);
+    if (row < rows) {
+        a.load(dy + (size_t)row * C, t, tpr, C);
+        b.load(h + (size_t)row * C, t, tpr, C);
+        if (dh && kAhead) d.load(dh + (size_t)row * C, t, tpr, C);
+        r = rstd[row];
+    }
+    for (; row < rows; row += walkers) {
+        if (kAhead && row + walkers < rows) {
+            const size_t next = (size_t)(row + walkers) * C;
+            next_a.load(dy + next, t, tpr, C);
+            next_b.load(h + next, t, tpr, C);
+            if (dh) next_d.load(dh + next, t, tpr, C);
+            next_r = rstd[row + walkers];
+        }
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
             const int c = (i * tpr + t) * VEC;
             if (c < C) {
-                load_f<T, VEC>(dy + at + c, a[i]);
-                load_f<T, VEC>(h + at + c, b[i]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) a[i][j] = b[i][j] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < ITER; ++i) {
-            const int c = (i * tpr + t) * VEC;
-            if (c < C) {
-                float g[VEC];
-                load_f<T, VEC>(gamma + c, g);
+                float w[VEC];
+                if (!kAhead) load_f<T, VEC>(gamma + c, w);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    acc[i][j] = fmaf(a[i][j], b[i][j] * r, acc[i][j]);
-                    a[i][j] *= g[j];
-                    dot = fmaf(a[i][j], b[i][j], dot);
+                    const float y = a.at(i, j), x = b.at(i, j);
+                    acc[i][j] = fmaf(y, x * r, acc[i][j]);
+                    dot = fmaf(y * (kAhead ? g.at(i, j) : w[j]), x, dot);
                 }
             }
         }
-        dot = row_reduce<false>(dot, one_warp, red);
+        dot = row_reduce<false>(dot, WARP, red);
         const float k = dot / (float)C * r * r;
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
             const int c = (i * tpr + t) * VEC;
             if (c < C) {
-                float d[VEC];
-                if (dh) {
-                    load_f<T, VEC>(dh + at + c, d);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) d[j] = 0.f;
+                float w[VEC], o[VEC];
+                if (!kAhead) {
+                    load_f<T, VEC>(gamma + c, w);
+                    if (dh) d.v[i] = *reinterpret_cast<const Pack<T, VEC> *>(dh + (size_t)row * C + c);
                 }
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) d[j] = fmaf(r, a[i][j] - b[i][j] * k, d[j]);
-                store_f<T, VEC>(dx + at + c, d);
+                for (int j = 0; j < VEC; ++j) o[j] = fmaf(r, a.at(i, j) * (kAhead ? g.at(i, j) : w[j]) - b.at(i, j) * k, dh ? d.at(i, j) : 0.f);
+                store_f<T, VEC>(dx + (size_t)row * C + c, o);
             }
+        }
+        if (kAhead) {
+            a = next_a; b = next_b; d = next_d; r = next_r;
+        } else if (row + walkers < rows) {
+            a.load(dy + (size_t)(row + walkers) * C, t, tpr, C);
+            b.load(h + (size_t)(row + walkers) * C, t, tpr, C);
+            r = rstd[row + walkers];
         }
     }
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
         const int c = (i * tpr + t) * VEC;
-        if (c < C) store_f<float, VEC>(part + (size_t)walker * C + c, acc[i]);
+        if (c < C) {
+            if (WARP) store_f<float, VEC>(shares + warp * C + c, acc[i]);
+            else store_f<float, VEC>(part + (size_t)blockIdx.x * C + c, acc[i]);
+        }
+    }
+    if (WARP) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < C; c += blockDim.x) {
+            float sum = shares[c];
+            for (int w = 1; w < warps; ++w) sum += shares[w * C + c];
+            part[(size_t)blockIdx.x * C + c] = sum;
+        }
     }
 }
 
 // dgamma[c] = sum over walkers, 32 columns per block, walkers in index order per warp and warps in index order
-__global__ void __launch_bounds__(512) rms_fold_kernel(const float *__restrict__ part, int walkers, float *__restrict__ dgamma, int C) {
-    __shared__ float fold[16][32];
+__global__ void __launch_bounds__(1024) rms_fold_kernel(const float *__restrict__ part, int walkers, float *__restrict__ dgamma, int C) {
+    __shared__ float fold[32][32];
     pdl_launch();
     pdl_wait();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float a = 0.f;
     if (c < C) {
 #pragma unroll 8
-        for (int i = w; i < walkers; i += 16) a += part[(size_t)i * C + c];
+        for (int i = w; i < walkers; i += 32) a += part[(size_t)i * C + c];
     }
     fold[w][lane] = a;
     __syncthreads();
     if (w == 0 && c < C) {
-        for (int i = 1; i < 16; ++i) a += fold[i][lane];
+        for (int i = 1; i < 32; ++i) a += fold[i][lane];
         dgamma[c] = a;
     }
 }
@@ -233,12 +270,12 @@ bool vec_ok(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; 
 
 // threads of a row, vectors per thread, threads of a block and rows of a block
 struct RmsPlan { int tpr, iter, threads, rpb; };
-RmsPlan rms_plan(int nvec, bool vec) {
+RmsPlan rms_plan(int nvec, bool vec, int warp_iters, int warp_threads) {
     RmsPlan p;
     const int warp_iter = (nvec + 31) / 32;
-    if (warp_iter <= 4) {
+    if (warp_iter <= warp_iters) {
         p.iter = warp_iter <= 1 ? 1 : (warp_iter <= 2 ? 2 : 4);
-        p.tpr = 32; p.threads = 128; p.rpb = 4;
+        p.tpr = 32; p.threads = warp_threads; p.rpb = warp_threads / 32;
         return p;
     }
     p.iter = 1;
@@ -247,17 +284,28 @@ RmsPlan rms_plan(int nvec, bool vec) {
     p.tpr = p.threads; p.rpb = 1;
     return p;
 }
-
-constexpr int kMaxWalkers = 148 * 4;
+RmsPlan rms_fwd_plan(int nvec, bool vec) { return rms_plan(nvec, vec, 4, 128); }
+RmsPlan rms_bwd_plan(int nvec, bool vec) { return rms_plan(nvec, vec, 2, kWarpRowThreads); }
+// Blocks of the backward pass: as many as the kernel's registers (its launch bounds) let stay resident, so that none waits
+// for a second round with rows of its own.
+int rms_bwd_blocks(const RmsPlan &p, int rows) {
+    const int per_sm = p.tpr == 32 ? (p.iter == 1 ? 3 : 2) : std::max(1, (p.iter == 1 ? 1024 : 512) / p.threads);
+    return std::min((rows + p.rpb - 1) / p.rpb, 148 * per_sm);
+}
 
 }  // namespace
 
-size_t rmsnorm_scratch_elems(int rows, int C) { return (size_t)std::min(rows, kMaxWalkers) * C; }
+size_t rmsnorm_scratch_elems(int rows, int C) {
+    int most = rms_bwd_blocks(rms_bwd_plan(C, false), rows);
+    for (int vec : {4, 8})
+        if (C % vec == 0) most = std::max(most, rms_bwd_blocks(rms_bwd_plan(C / vec, true), rows));
+    return (size_t)most * C;
+}
 
 template <typename T, int VEC>
 static int rms_fwd(const void *x, const void *res, const void *gamma, void *h, void *y, void *y8, float *scale8, float *rstd, int rows, int C, int group,
                    float eps, const Launch &s) {
-    const RmsPlan p = rms_plan(C / VEC, VEC > 1);
+    const RmsPlan p = rms_fwd_plan(C / VEC, VEC > 1);
     const int grid = (rows + p.rpb - 1) / p.rpb;
     auto go = [&](auto kernel) {
         launch_k(kernel, grid, p.threads, 0, s, (const T *)x, (const T *)res, (const T *)gamma, (T *)h, (T *)y, (uint8_t *)y8, scale8, rstd, rows, C, p.tpr, group, eps);
@@ -276,21 +324,25 @@ static int rms_fwd(const void *x, const void *res, const void *gamma, void *h, v
 template <typename T, int VEC>
 static int rms_bwd(const void *dy, const void *dh, const void *h, const void *gamma, const float *rstd, void *dx, float *dgamma, float *scratch, int rows, int C,
                    const Launch &s) {
-    const RmsPlan p = rms_plan(C / VEC, VEC > 1);
-    const int walkers = std::min(rows, kMaxWalkers);
-    const int grid = (walkers + p.rpb - 1) / p.rpb;
-    auto go = [&](auto kernel) {
-        launch_k(kernel, grid, p.threads, 0, s, (const T *)dy, (const T *)dh, (const T *)h, (const T *)gamma, rstd, (T *)dx, scratch, rows, C, p.tpr);
+    const RmsPlan p = rms_bwd_plan(C / VEC, VEC > 1);
+    const int grid = rms_bwd_blocks(p, rows);
+    auto go = [&](auto kernel, size_t smem) {
+        launch_k(kernel, grid, p.threads, smem, s, (const T *)dy, (const T *)dh, (const T *)h, (const T *)gamma, rstd, (T *)dx, scratch, rows, C);
     };
-    switch (p.iter) {
-    case 1: go(rms_bwd_kernel<T, VEC, 1>); break;
-    case 2: go(rms_bwd_kernel<T, VEC, 2>); break;
-    case 4: go(rms_bwd_kernel<T, VEC, 4>); break;
-    case 8: if (VEC == 1) { go(rms_bwd_kernel<T, 1, 8>); break; } return -1;
-    case 16: if (VEC == 1) { go(rms_bwd_kernel<T, 1, 16>); break; } return -1;
-    default: return -1;
+    if (p.tpr == 32) {
+        const size_t smem = (size_t)p.rpb * C * sizeof(float);
+        if (p.iter == 1) go(rms_bwd_kernel<T, VEC, 1, true>, smem); else go(rms_bwd_kernel<T, VEC, 2, true>, smem);
+    } else {
+        switch (p.iter) {
+        case 1: go(rms_bwd_kernel<T, VEC, 1, false>, 0); break;
+        case 2: go(rms_bwd_kernel<T, VEC, 2, false>, 0); break;
+        case 4: go(rms_bwd_kernel<T, VEC, 4, false>, 0); break;
+        case 8: if (VEC == 1) { go(rms_bwd_kernel<T, 1, 8, false>, 0); break; } return -1;
+        case 16: if (VEC == 1) { go(rms_bwd_kernel<T, 1, 16, false>, 0); break; } return -1;
+        default: return -1;
+        }
     }
-    launch_k(rms_fold_kernel, (C + 31) / 32, 512, 0, s, (const float *)scratch, walkers, dgamma, C);
+    launch_k(rms_fold_kernel, (C + 31) / 32, 1024, 0, s, (const float *)scratch, grid, dgamma, C);
     return 2;
 }
 
