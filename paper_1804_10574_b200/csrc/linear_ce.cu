@@ -15,9 +15,8 @@
 // (cta_group::2): each loads half of A and half of B by TMA, four stages of 48 KB or six of 32 KB in flight.  The tensor
 // cores are fed from the L2, and the wide tile asks a quarter less of it for the same products (halving B's loads took
 // 8192 x 4096 x 65536 from 3.09 to 2.69 ms in an experiment, one to three more stages changed nothing).  The 512 TMEM
-// columns are two accumulators of 256: the halves of a wide tile, or successive tiles of the narrow one.  The epilogue
-// warps copy an accumulator to registers (128 columns of a row per thread) and hand it back at once; what they do with
-// the values runs under the next products.
+// columns are two accumulators of 256: the halves of a wide tile, or successive tiles of the narrow one; what the epilogue
+// warps do with one (128 columns of a row per thread) runs under the products of the other.
 //
 // The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
 // 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
@@ -53,6 +52,7 @@ constexpr int kStageRing = 192 * 1024;
 constexpr int kOutBuf = 32 * kKBox * 2;  // an epilogue warp's 32 rows of 64 bf16 values on their way out
 constexpr int kCeSmem = kStageRing + kEpiWarps * kOutBuf + 1024;
 constexpr int kMaxSeg = 6;
+constexpr int kPieceBf16 = 2048, kPieceF32 = 256;  // K values of a chain whose result stays in 32 bits
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kLse, kDz, kPartial, kWeightGrad };
@@ -166,13 +166,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 __device__ __forceinline__ float bf16_round(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 
-__device__ __forceinline__ void load_bias32(const CeGemm &g, int c0, float (&b)[32]) {
-    // every lane reads the same 32 values (one transaction each); columns past the vocabulary are masked by the caller
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        const int c = min(c0 + j, g.N - 1);
-        b[j] = g.bias_bf16 ? __bfloat162float(((const bf16 *)g.bias)[c]) : ((const float *)g.bias)[c];
-    }
+__device__ __forceinline__ float load_bias(const void *bias, int is_bf16, int c) {
+    return is_bf16 ? __bfloat162float(((const bf16 *)bias)[c]) : ((const float *)bias)[c];
 }
 
 // The sum over the warp's 32 rows of each of 32 columns: lane j ends with column j's.
@@ -242,145 +237,134 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t buf, 
     }
 }
 
-// What becomes of 128 columns of one row: v at columns col0 .., which are piece `part` (of 128 columns) of the row.
-template <int MODE>
-__device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *map_out, uint32_t buf, float (&v)[kHalf], int split, int row, int col0, int lane) {
-    const bool live = row < g.M;
-    float lse = 0.f, weight = 0.f;
-    int label = -1;
-    if ((MODE == kLse || MODE == kDz) && live) {
+// What a thread knows of its row, and the softmax's running maximum and sum over the row's 128 columns.
+struct CeRow {
+    int split, row, label;  // label: column of this launch
+    float lse, weight, top, sum;
+};
+template <int MODE> __device__ __forceinline__ CeRow ce_row(const CeGemm &g, int split, int row) {
+    CeRow r{split, row, -1 - 2 * kTile, 0.f, 0.f, -INFINITY, 0.f};
+    if (MODE != kWeightGrad && (MODE != kPartial || g.out_kind == kFinal) && row < g.M) {
         const int y = g.labels[row];
         const bool counted = y >= 0 && y < g.V;
-        label = counted ? y - g.v0 : -1 - 2 * kTile;  // column of this launch (a label of another chunk meets none)
-        if (MODE == kDz) {
-            lse = g.lse[row];
-            weight = counted ? (g.drow ? g.drow[row] : 1.f) : 0.f;
-        }
+        if (counted) r.label = y - g.v0;  // a label of another chunk meets no column
+        if (MODE == kDz) r.lse = g.lse[row];
+        r.weight = counted ? (MODE == kDz && g.drow ? g.drow[row] : 1.f) : 0.f;
     }
-    if (MODE == kLse || MODE == kDz) {
-        if (g.bias) {
+    return r;
+}
+// first column that an epilogue has nothing to do with (kDz: a stage of the next product reads up to 128 columns)
+template <int MODE> __device__ __forceinline__ int ce_columns(const CeGemm &g) { return MODE == kDz ? (g.N + 127) / 128 * 128 : g.N; }
+
+// What becomes of 64 columns of the warp's 32 rows: v at columns col .. of row r.row.
+template <int MODE>
+__device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *map_out, uint32_t buf, float *v, CeRow &r, int col, int lane) {
+    const bool live = r.row < g.M;
+    if ((MODE == kLse || MODE == kDz) && g.bias) {
+        // every lane reads the same values (one transaction each); columns past the vocabulary are masked below
 #pragma unroll
-            for (int c = 0; c < kHalf; c += 32) {
-                float b[32];
-                load_bias32(g, col0 + c, b);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[c + j] += b[j];
-            }
-        }
+        for (int j = 0; j < kKBox; ++j) v[j] += load_bias(g.bias, g.bias_bf16, min(col + j, g.N - 1));
     }
     if (MODE == kLse) {
-        if (col0 + kHalf > g.N) {
+        if (col + kKBox > g.N) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j)
-                if (col0 + j >= g.N) v[j] = -INFINITY;
+            for (int j = 0; j < kKBox; ++j)
+                if (col + j >= g.N) v[j] = -INFINITY;
         }
-        if (label >= col0 && label < col0 + kHalf) {
+        if (r.label >= col && r.label < col + kKBox) {
             float z = 0.f;
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j)
-                if (label == col0 + j) z = v[j];
-            g.zlab[row] = z;
+            for (int j = 0; j < kKBox; ++j)
+                if (r.label == col + j) z = v[j];
+            g.zlab[r.row] = z;
         }
-        float m[4] = {v[0], v[1], v[2], v[3]};
+        float m[4] = {r.top, v[1], v[2], v[3]};
 #pragma unroll
-        for (int j = 4; j < kHalf; ++j) m[j & 3] = fmaxf(m[j & 3], v[j]);
+        for (int j = 0; j < kKBox; ++j) m[j & 3] = fmaxf(m[j & 3], v[j]);
         const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-        const float ref = top == -INFINITY ? 0.f : top;  // nothing but -inf
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        const float ref = top == -INFINITY ? 0.f : top;  // nothing but -inf so far
+        float s[4] = {r.sum * exp2_approx((r.top - ref) * kLog2e), 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) s[j & 3] += exp2_approx((v[j] - ref) * kLog2e);
-        if (live && col0 < g.N) g.part[(size_t)(col0 / kHalf) * g.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+        for (int j = 0; j < kKBox; ++j) s[j & 3] += exp2_approx((v[j] - ref) * kLog2e);
+        r.top = top;
+        r.sum = (s[0] + s[1]) + (s[2] + s[3]);
     } else if (MODE == kDz) {
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) v[j] = exp2_approx((v[j] - lse) * kLog2e);
-        if (label >= col0 && label < col0 + kHalf) {
+        for (int j = 0; j < kKBox; ++j) v[j] = exp2_approx((v[j] - r.lse) * kLog2e);
+        if (r.label >= col && r.label < col + kKBox) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j)
-                if (label == col0 + j) v[j] -= 1.f;
+            for (int j = 0; j < kKBox; ++j)
+                if (r.label == col + j) v[j] -= 1.f;
         }
         if (g.drow) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j) v[j] *= weight;
+            for (int j = 0; j < kKBox; ++j) v[j] *= r.weight;
         }
         // a row that does not count gives exact zeros whatever its logits are; so do columns past the vocabulary
-        if (__any_sync(0xffffffffu, weight == 0.f)) {
+        if (__any_sync(0xffffffffu, r.weight == 0.f)) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j) v[j] = weight == 0.f ? 0.f : v[j];
+            for (int j = 0; j < kKBox; ++j) v[j] = r.weight == 0.f ? 0.f : v[j];
         }
-        if (col0 + kHalf > g.N) {
+        if (col + kKBox > g.N) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j)
-                if (col0 + j >= g.N) v[j] = 0.f;
+            for (int j = 0; j < kKBox; ++j)
+                if (col + j >= g.N) v[j] = 0.f;
         }
         if (g.db_part) {  // rows that are not there hold zeros
-            const int block = (row - lane) / 32;
+            const int block = (r.row - lane) / 32;
 #pragma unroll
-            for (int c = 0; c < kHalf; c += 32) {
+            for (int c = 0; c < kKBox; c += 32) {
                 float t[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) t[j] = v[c + j];
                 const float cs = column_sums(t, lane);
-                if (block * 32 < g.M && col0 + c < g.dz_plane) g.db_part[(size_t)block * g.dz_plane + col0 + c + lane] = cs;
+                if (block * 32 < g.M) g.db_part[(size_t)block * g.dz_plane + col + c + lane] = cs;
             }
         }
-        if (row - lane >= g.M) return;
-        for (int p = 0;;) {
+        if (r.row - lane < g.M) {
+            for (int p = 0;;) {
+                store_box(map_out, buf, lane, p * g.dz_plane + col, r.row - lane, v);
+                if (++p == g.planes) break;
 #pragma unroll
-            for (int c = 0; c < kHalf; c += kKBox)
-                if (col0 + c < g.dz_plane) store_box(map_out, buf, lane, p * g.dz_plane + col0 + c, row - lane, v + c);
-            if (++p == g.planes) break;
-#pragma unroll
-            for (int j = 0; j < kHalf; ++j) v[j] -= bf16_round(v[j]);
+                for (int j = 0; j < kKBox; ++j) v[j] -= bf16_round(v[j]);
+            }
         }
-    } else if (MODE == kPartial) {
-        if (row - lane >= g.M) return;
-        if (g.out_kind == kFinal) {
-            const float scale = g.head->scale;
-            const int y = live ? g.labels[row] : -1;
-            const bool counted = y >= 0 && y < g.V;
+    } else if (r.row - lane < g.M) {
+        if (MODE == kPartial && g.out_kind != kFinal) {
+            if (live) {
+                float *dst = (float *)g.out + r.split * g.out_split + (size_t)r.row * g.ld + col;
 #pragma unroll
-            for (int c = 0; c < kHalf; c += 32) {
-                if (col0 + c >= g.N) break;
-                if (g.part_in && live) {
-                    const float *src = g.part_in + (size_t)row * g.ld + col0 + c;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4)
-                        if (col0 + c + j < g.ld) {
-                            const float4 o = *reinterpret_cast<const float4 *>(src + j);
-                            v[c + j] += o.x; v[c + j + 1] += o.y; v[c + j + 2] += o.z; v[c + j + 3] += o.w;
-                        }
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[c + j] = counted ? v[c + j] * scale : 0.f;
-                if (g.out_tma) {
-                    if (c % kKBox == 32) store_box(map_out, buf, lane, col0 + c - 32, row - lane, v + c - 32);
-                    else if (col0 + c + 32 >= g.N) store_box(map_out, buf, lane, col0 + c, row - lane, v + c);  // what follows is clipped
-                } else if (live) {
-                    store_row32(g.out, g.out_bf16, g.out_vec, row, col0 + c, g.N, v + c);
+                for (int j = 0; j < kKBox; j += 4) {
+                    if (col + j < g.ld) {  // ld is a multiple of 4
+                        if (g.out_kind == kAdd) red_add4(dst + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        else *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    }
                 }
             }
-        } else if (live) {
-            float *dst = (float *)g.out + split * g.out_split + (size_t)row * g.ld + col0;
-#pragma unroll
-            for (int j = 0; j < kHalf; j += 4) {
-                if (col0 + j >= g.ld) break;  // ld is a multiple of 4
-                if (g.out_kind == kAdd) red_add4(dst + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
-                else *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-            }
+            return;
         }
-    } else {
-        if (row - lane >= g.M) return;
         const float scale = g.head->scale;
+        if (MODE == kPartial) {
+            if (g.part_in && live) {
+                const float *src = g.part_in + (size_t)r.row * g.ld + col;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) v[j] *= scale;
+                for (int j = 0; j < kKBox; j += 4)
+                    if (col + j < g.ld) {
+                        const float4 o = *reinterpret_cast<const float4 *>(src + j);
+                        v[j] += o.x; v[j + 1] += o.y; v[j + 2] += o.z; v[j + 3] += o.w;
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < kKBox; ++j) v[j] = r.weight != 0.f ? v[j] * scale : 0.f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kKBox; ++j) v[j] *= scale;
+        }
         if (g.out_tma) {
-#pragma unroll
-            for (int c = 0; c < kHalf; c += kKBox)
-                if (col0 + c < g.N) store_box(map_out, buf, lane, col0 + c, row - lane, v + c);
+            store_box(map_out, buf, lane, col, r.row - lane, v);
         } else if (live) {
-#pragma unroll
-            for (int c = 0; c < kHalf; c += 32)
-                if (col0 + c < g.N) store_row32(g.out, g.out_bf16, g.out_vec, row, col0 + c, g.N, v + c);
+            store_row32(g.out, g.out_bf16, g.out_vec, r.row, col, g.N, v);
+            if (col + 32 < g.N) store_row32(g.out, g.out_bf16, g.out_vec, r.row, col + 32, g.N, v + 32);
         }
     }
 }
@@ -537,9 +521,17 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 ce_range(g, split, kb0, kb1);
                 pieces = (kb1 - kb0 + g.piece - 1) / g.piece;
             }
+            const uint32_t buf = base + kStageRing + (uint32_t)(warp - 2) * kOutBuf;
 #pragma unroll 1
-            for (int h = 0; h < kHalves; ++h) {
-                float v[kHalf];
+            for (int h = 0; h < kHalves && ok; ++h) {
+                const int col0 = t.n * NT + h * kTile + half * kHalf, live = ce_columns<MODE>(g) - col0;
+                CeRow r;
+                if (!PROMOTE) r = ce_row<MODE>(g, split, row);
+                float v[PROMOTE ? kHalf : kKBox];
+                if (PROMOTE) {
+#pragma unroll
+                    for (int j = 0; j < kHalf; ++j) v[PROMOTE ? j : 0] = 0.f;
+                }
 #pragma unroll 1
                 for (int piece = 0; piece < pieces; ++piece, ++u) {
                     const uint32_t acc = u & 1u;
@@ -547,27 +539,44 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t taddr = tmem + acc * kTile + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(half * kHalf);
-                    if (!PROMOTE || piece == 0) {
+                    auto hand_back = [&]() {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_remote(map_rank(smem_u32(&acc_empty[acc]), 0));
+                    };
+                    if (!PROMOTE) {
+                        // 64 columns at a time in a loop that is not unrolled: short code
+#pragma unroll 1
+                        for (int c = 0; c < kHalf; c += kKBox) {
+                            if (c < live) {
 #pragma unroll
-                        for (int c = 0; c < kHalf; c += 32)
-                            tc_ld32(taddr + (uint32_t)c, reinterpret_cast<float(&)[16]>(v[c]), reinterpret_cast<float(&)[16]>(v[c + 16]));
-                        tc_wait_ld();
+                                for (int j = 0; j < kKBox; j += 32)
+                                    tc_ld32(taddr + (uint32_t)(c + j), reinterpret_cast<float(&)[16]>(v[j]), reinterpret_cast<float(&)[16]>(v[j + 16]));
+                                tc_wait_ld();
+                            }
+                            if (c == kHalf - kKBox) hand_back();
+                            if (c < live) ce_finish<MODE>(g, &map_out, buf, v, r, col0 + c, lane);
+                        }
                     } else {
 #pragma unroll
-                        for (int c = 0; c < kHalf; c += 32) {
-                            float w[32];
-                            tc_ld32(taddr + (uint32_t)c, reinterpret_cast<float(&)[16]>(w[0]), reinterpret_cast<float(&)[16]>(w[16]));
+                        for (int c = 0; c < kHalf; c += 16) {
+                            float w[16];
+                            tc_ld16(taddr + (uint32_t)c, w);
                             tc_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[c + j] += w[j];
+                            for (int j = 0; j < 16; ++j) v[c + j] += w[j];
                         }
+                        hand_back();
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_remote(map_rank(smem_u32(&acc_empty[acc]), 0));
                 }
                 if (!ok) break;
-                ce_finish<MODE>(g, &map_out, base + kStageRing + (uint32_t)(warp - 2) * kOutBuf, v, split, row, t.n * NT + h * kTile + half * kHalf, lane);
+                if (PROMOTE) {
+                    r = ce_row<MODE>(g, split, row);
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += kKBox)
+                        if (c < live) ce_finish<MODE>(g, &map_out, buf, v + c, r, col0 + c, lane);
+                }
+                if (MODE == kLse && row < g.M && live > 0) g.part[(size_t)(col0 / kHalf) * g.M + row] = make_float2(r.top, r.sum);
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -586,6 +595,8 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     cluster_sync();
 }
+
+#include "linear_ce_rows.cuh"
 
 // ---- joining the forward pass ----------------------------------------------------------------------------------------
 // rows rows per block of 512 threads, the 512 / rows threads of a row share its pieces, eight loads in flight each.  The mean is taken by the block
@@ -793,7 +804,6 @@ int sm_count() {
 constexpr size_t kDzBytes = (size_t)256 << 20;
 constexpr int kPairs = 74;  // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
 constexpr double kWideCost = 0.97;  // time of a product in a 256 x 512 tile against a 256 x 256 one
-constexpr int kPieceBf16 = 2048, kPieceF32 = 256;  // K values of a chain whose result stays in 32 bits
 
 double ce_rounds(int M, int N, int nt, int splits);
 
@@ -802,9 +812,26 @@ struct CePlan {
     int dz_planes, chunk;    // terms of dz, columns of a chunk
     int tiles_m, n_part;
     int splits, dx_ld;
+    bool rows;               // a few rows: the kernels of linear_ce_rows.cuh
     bool pack_x, pack_w;
     size_t part, zlab, sums, x, w, dz, db, dx, bytes;
 };
+
+// Few rows: CTAs of the forward pass and of dz, at least one unit of the vocabulary each.
+constexpr int kRowsGridMax = 160;
+int rows_grid(int out, int sms) { return std::min(std::min(sms, kRowsGridMax), (out + kRowsUnit - 1) / kRowsUnit); }
+// Few rows, dx: splits of the vocabulary, so that the tiles of 128 columns fill the SMs.  Seconds by the bytes of W and of
+// the partial sums at 6 TB/s.
+int rows_splits(int B, int in, int out, int ld) {
+    const int tiles = (in + kHalf - 1) / kHalf, kb = (out + kRowsKw - 1) / kRowsKw, sms = 2 * kPairs;
+    int best = 1;
+    double least = 1e30;
+    for (int n = 1; n <= std::max(1, std::min(sms, kb / 2)); ++n) {
+        const double t = 2.0 * in * out / 6e12 * (double)((tiles * n + sms - 1) / sms) * sms / (tiles * n) + 8.0 * n * B * ld / 6e12;
+        if (t < least) { least = t; best = n; }
+    }
+    return best;
+}
 
 CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     CePlan p{};
@@ -815,8 +842,9 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     // an fp32 dW of bf16 operands gets 16 bits of dz (two terms), as the fully connected layer's loss gradient does; a bf16
     // dW or dx is rounded to 8 bits itself and takes dz rounded once to bf16
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
+    p.rows = prec == P_BF16 && B <= kRowsMax;
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = (out + kHalf - 1) / kHalf;
+    p.n_part = p.rows ? 4 * rows_grid(out, kRowsGridMax) : (out + kHalf - 1) / kHalf;
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -826,7 +854,13 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     }
     if (p.pack_x) p.x = take((size_t)B * p.planes * p.plane * 2);
     if (p.pack_w) p.w = take((size_t)out * p.planes * p.plane * 2);
-    if (backward) {
+    if (backward && p.rows) {
+        p.chunk = out;
+        p.dx_ld = up(in, 4);
+        p.splits = rows_splits(B, in, out, p.dx_ld);
+        p.dz = take((size_t)out * p.dz_planes * kRowsPitch * 2);
+        p.dx = take((size_t)p.splits * B * p.dx_ld * 4);
+    } else if (backward) {
         const size_t fit = kDzBytes / ((size_t)B * p.dz_planes * 2) / kTile * kTile;
         p.chunk = (int)std::min<size_t>((size_t)up(out, kTile), std::max<size_t>(kTile, fit));
         p.dx_ld = up(in, 4);
@@ -911,6 +945,27 @@ int ce_launch(const CeOperand &a, const CeOperand &b, const CeOperand &out, CeGe
     return ce_launch_as<MODE, A_MN, B_MN, kTile, false>(a, b, out, g, s);
 }
 
+template <int MODE, int NT> int rows_launch_as(const CUtensorMap &w, const CUtensorMap &x, const CeRowsArgs &g, int grid, const Launch &s) {
+    static thread_local int ready_dev = -1;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(ce_rows_kernel<MODE, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem) != cudaSuccess) return -1;
+        ready_dev = dev;
+    }
+    launch_k(ce_rows_kernel<MODE, NT>, grid, kRowsThreads, kRowsSmem, s, w, x, g);
+    return 1;
+}
+// the columns of the MMA: 16, 32 or 64 rows of x
+template <int MODE> int rows_launch(const CeOperand &w, const CeOperand &x, const CeRowsArgs &g, const Launch &s) {
+    const int nt = g.B <= 16 ? 16 : (g.B <= 32 ? 32 : 64);
+    CUtensorMap mw, mx;
+    const bool partial = MODE == kPartial;
+    if (!ce_map(w.ptr, w.rows, w.cols, w.cols, partial ? kRowsKw : kRowsUnit, &mw) || !ce_map(x.ptr, x.rows, x.cols, x.cols, partial ? kRowsKw : nt, &mx)) return -1;
+    const int grid = partial ? std::min(g.tiles * g.splits, sm_count()) : rows_grid(g.V, sm_count());
+    return nt == 16 ? rows_launch_as<MODE, 16>(mw, mx, g, grid, s) : (nt == 32 ? rows_launch_as<MODE, 32>(mw, mx, g, grid, s) : rows_launch_as<MODE, 64>(mw, mx, g, grid, s));
+}
+
 // terms of A and of B that are multiplied, smallest products first
 void ce_segments(CeGemm &g, int a_planes, int a_plane, int b_planes, int b_plane) {
     g.n_seg = 0;
@@ -949,16 +1004,28 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
     if (p.pack_x) { n += pack(prec, x, base + p.x, nullptr, B, in, p, out, head, 0, 0, nullptr, s); x = base + p.x; }
     if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, s); W = base + p.w; }
     const int cols = p.pack_w ? p.planes * p.plane : in;
-    CeGemm g{};
-    g.M = B; g.N = out; g.K = p.plane; g.head = head;
-    ce_segments(g, p.planes, p.plane, p.planes, p.plane);
-    g.bias = bias; g.bias_bf16 = prec == P_BF16; g.labels = labels; g.V = out;
-    g.part = (float2 *)(base + p.part); g.zlab = (float *)(base + p.zlab);
-    const int r = ce_launch<kLse, false, false>(CeOperand{x, B, cols}, CeOperand{W, out, cols}, CeOperand{}, g, true, s);
+    float2 *part = (float2 *)(base + p.part);
+    float *zlab = (float *)(base + p.zlab);
+    const CeOperand ox{x, B, cols}, ow{W, out, cols};
+    int r, n_part = p.n_part;
+    if (p.rows) {
+        CeRowsArgs g{};
+        g.B = B; g.D = in; g.V = out; g.kblocks = (in + kRowsKw - 1) / kRowsKw; g.head = head;
+        g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.part = part; g.zlab = zlab;
+        n_part = 4 * rows_grid(out, sm_count());
+        r = rows_launch<kLse>(ow, ox, g, s);
+    } else {
+        CeGemm g{};
+        g.M = B; g.N = out; g.K = p.plane; g.head = head;
+        ce_segments(g, p.planes, p.plane, p.planes, p.plane);
+        g.bias = bias; g.bias_bf16 = prec == P_BF16; g.labels = labels; g.V = out;
+        g.part = part; g.zlab = zlab;
+        r = ce_launch<kLse, false, false>(ox, ow, CeOperand{}, g, true, s);
+    }
     if (r < 0) return r;
     int rows = 1;
     while (rows < 32 && rows < B) rows *= 2;
-    launch_k(ce_join_kernel, (B + rows - 1) / rows, kJoin, 0, s, (const float2 *)g.part, p.n_part, (const float *)g.zlab, labels, loss, row_loss, lse,
+    launch_k(ce_join_kernel, (B + rows - 1) / rows, kJoin, 0, s, (const float2 *)part, n_part, (const float *)zlab, labels, loss, row_loss, lse,
              (double *)(base + p.sums), head, B, out, rows);
     return n + r + 1;
 }
@@ -976,7 +1043,45 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
     bf16 *dz = (bf16 *)(base + p.dz);
     const CeOperand ox{xp, B, x_cols}, ow{W, out, w_cols}, oz{dz, B, dz_cols};
     const int es = prec == P_BF16 ? 2 : 4;
-    const bool dx_direct = p.splits == 1;  // the last chunk's product writes dx itself
+    const bool out_bf16 = prec == P_BF16 && !dw_f32;
+    // dW for the vocabulary entries [v0, v0 + cols), from dz with entries innermost (general) or rows of x (few rows)
+    auto weight_gradient = [&](int v0, int cols) {
+        const int oe = out_bf16 ? 2 : 4;
+        CeGemm g{};
+        g.M = cols; g.N = in; g.head = head;
+        g.out = (uint8_t *)dW + (size_t)v0 * in * oe; g.out_bf16 = out_bf16;
+        g.out_vec = (in * oe) % 16 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0;
+        g.out_tma = out_bf16 && g.out_vec;
+        const CeOperand o = g.out_tma ? CeOperand{g.out, cols, in} : CeOperand{};
+        if (p.rows) {
+            g.K = kRowsPitch;
+            ce_segments(g, p.dz_planes, kRowsPitch, 1, 0);
+            return ce_launch<kWeightGrad, false, true>(CeOperand{dz, out, p.dz_planes * kRowsPitch}, ox, o, g, !out_bf16, s);
+        }
+        g.K = B;
+        ce_segments(g, p.dz_planes, p.chunk, p.planes, p.plane);
+        return ce_launch<kWeightGrad, true, true>(oz, ox, o, g, !out_bf16, s);
+    };
+    const bool dx_direct = !p.rows && p.splits == 1;  // the last chunk's product writes dx itself
+    if (p.rows) {
+        CeRowsArgs g{};
+        g.B = B; g.D = in; g.V = out; g.kblocks = (in + kRowsKw - 1) / kRowsKw; g.head = head;
+        g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.lse = lse; g.drow = drow;
+        g.dz = dz; g.db = db; g.planes = p.dz_planes;
+        int r = rows_launch<kDz>(ow, ox, g, s);
+        if (r < 0) return r;
+        n += r;
+        if (dx) {
+            g.tiles = (in + kHalf - 1) / kHalf; g.splits = p.splits;
+            g.dx_part = (float *)(base + p.dx); g.dx_split = (size_t)B * p.dx_ld; g.ld = p.dx_ld;
+            if ((r = rows_launch<kPartial>(ow, CeOperand{dz, out, p.dz_planes * kRowsPitch}, g, s)) < 0) return r;
+            n += r;
+        }
+        if (dW) {
+            if ((r = weight_gradient(0, out)) < 0) return r;
+            n += r;
+        }
+    } else
     for (int v0 = 0; v0 < out; v0 += p.chunk) {
         const int cols = std::min(p.chunk, out - v0);
         {
@@ -1017,16 +1122,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
             n += r;
         }
         if (dW) {
-            const bool out_bf16 = prec == P_BF16 && !dw_f32;
-            const int oe = out_bf16 ? 2 : 4;
-            CeGemm g{};
-            g.M = cols; g.N = in; g.K = B; g.head = head;
-            ce_segments(g, p.dz_planes, p.chunk, p.planes, p.plane);
-            g.out = (uint8_t *)dW + (size_t)v0 * in * oe; g.out_bf16 = out_bf16;
-            g.out_vec = (in * oe) % 16 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0;
-            g.out_tma = out_bf16 && g.out_vec;
-            const CeOperand o = g.out_tma ? CeOperand{g.out, cols, in} : CeOperand{};
-            const int r = ce_launch<kWeightGrad, true, true>(oz, ox, o, g, !out_bf16, s);
+            const int r = weight_gradient(v0, cols);
             if (r < 0) return r;
             n += r;
         }
