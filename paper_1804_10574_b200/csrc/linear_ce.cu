@@ -24,6 +24,8 @@
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,
 // l h are accumulated, smallest first: what is left out is below 2^-24 of the value.
+#include <float.h>
+
 #include <algorithm>
 
 #include "common.cuh"
@@ -772,6 +774,7 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ pa
         const int y = labels[row];
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
         if (y >= 0 && y < V) {
+#pragma unroll 8
             for (int s = 0; s < splits; ++s) {
                 const float4 q = *reinterpret_cast<const float4 *>(part + s * split_stride + row * ld + c);
                 a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
@@ -844,7 +847,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.rows = prec == P_BF16 && B <= kRowsMax;
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = p.rows ? 4 * rows_grid(out, kRowsGridMax) : (out + kHalf - 1) / kHalf;
+    p.n_part = p.rows ? rows_grid(out, kRowsGridMax) : (out + kHalf - 1) / kHalf;
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -1012,7 +1015,7 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
         CeRowsArgs g{};
         g.B = B; g.D = in; g.V = out; g.kblocks = (in + kRowsKw - 1) / kRowsKw; g.head = head;
         g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.part = part; g.zlab = zlab;
-        n_part = 4 * rows_grid(out, sm_count());
+        n_part = rows_grid(out, sm_count());
         r = rows_launch<kLse>(ow, ox, g, s);
     } else {
         CeGemm g{};
@@ -1023,8 +1026,8 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
         r = ce_launch<kLse, false, false>(ox, ow, CeOperand{}, g, true, s);
     }
     if (r < 0) return r;
-    int rows = 1;
-    while (rows < 32 && rows < B) rows *= 2;
+    int rows = 1;  // of a block: as many blocks as SMs before rows share one
+    while (rows < 32 && rows * 2 * kPairs < B) rows *= 2;
     launch_k(ce_join_kernel, (B + rows - 1) / rows, kJoin, 0, s, (const float2 *)part, n_part, (const float *)zlab, labels, loss, row_loss, lse,
              (double *)(base + p.sums), head, B, out, rows);
     return n + r + 1;

@@ -7,8 +7,8 @@
 // 160 KB and more of W in flight.  (Against the 256 x 256 tiles of the general kernel, one row, 65536 x 2048:
 // 85 -> 49 us.)
 //
-//   kLse      per lane the running maximum and sum of every row of x over the CTA's entries, joined over the lanes at
-//             the end: one (maximum, sum) per warp and row of x
+//   kLse      per lane the running maximum and sum of every row of x over the CTA's entries, joined over the CTA at
+//             the end: one (maximum, sum) per CTA and row of x
 //   kDz       dz of an entry for all rows of x: 64 bf16 values, one 128-byte line, [V][planes * 64]; db is the lane's own sum
 //   kPartial  dx^T = W^T dz^T in splits of the vocabulary: fp32 [splits][B][ld]
 //
@@ -36,7 +36,7 @@ struct CeRowsArgs {
     const void *bias;
     int bias_bf16;
     const int *labels;
-    float2 *part;            // kLse: [4 grid][B]
+    float2 *part;            // kLse: [grid][B]
     float *zlab;
     const float *lse, *drow; // kDz
     bf16 *dz;                // kDz: [V][planes * 64]
@@ -93,6 +93,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __shared__ int abort_flag;
     __shared__ int s_label[NT];
     __shared__ float s_lse[NT], s_weight[NT];
+    __shared__ float2 s_part[4][MODE == kLse ? NT : 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const Waiter wt{&abort_flag, &g_ce_error, kSpinLimit};
@@ -192,7 +193,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const int quarter = warp & 3;
         float top[MODE == kLse ? NT : 1], sum[MODE == kLse ? NT : 1];
 #pragma unroll
-        for (int j = 0; j < (MODE == kLse ? NT : 1); ++j) { top[j] = -INFINITY; sum[j] = 0.f; }
+        for (int j = 0; j < (MODE == kLse ? NT : 1); ++j) { top[j] = -FLT_MAX; sum[j] = 0.f; }
         const float scale = MODE == kDz && g.db ? g.head->scale : 1.f;
         bool ok = true;
         uint32_t u = 0;
@@ -234,11 +235,13 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             if (MODE == kLse) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
+                    // one exponential: of the new logit below the maximum, or of the old maximum below the new one.
+                    // The maximum starts at the lowest finite value, so that minus infinity adds nothing.
                     const float z = live ? v[j] + bias : -INFINITY;
                     if (live && s_label[j] == row) g.zlab[j] = z;
-                    const float m = fmaxf(top[j], z), ref = m == -INFINITY ? 0.f : m;
-                    sum[j] = sum[j] * exp2_approx((top[j] - ref) * kLog2e) + exp2_approx((z - ref) * kLog2e);
-                    top[j] = m;
+                    const float d = z - top[j], e = exp2_approx(-fabsf(d) * kLog2e);
+                    sum[j] = d > 0.f ? fmaf(sum[j], e, 1.f) : sum[j] + e;
+                    top[j] = fmaxf(top[j], z);
                 }
             } else if (live) {
                 float total = 0.f;
@@ -267,16 +270,21 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 }
             }
         }
-        if (MODE == kLse) {
-            // over the lanes; a warp without entries leaves (-inf, 0)
-            float2 *dst = g.part + (size_t)(blockIdx.x * 4 + quarter) * g.B;
+        if (MODE == kLse) {  // over the lanes
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const float m = warp_max(top[j]), ref = m == -INFINITY ? 0.f : m;
-                const float t = warp_sum(sum[j] * exp2_approx((top[j] - ref) * kLog2e));
-                if (lane == 0 && j < g.B) dst[j] = make_float2(m, t);
+                const float m = warp_max(top[j]), t = warp_sum(sum[j] * exp2_approx((top[j] - m) * kLog2e));
+                if (lane == 0) s_part[quarter][j] = make_float2(m, t);
             }
         }
+    }
+    __syncthreads();
+    if (MODE == kLse && threadIdx.x < g.B) {  // over the warps
+        const int j = threadIdx.x;
+        float m = s_part[0][j].x, t = 0.f;
+        for (int q = 1; q < 4; ++q) m = fmaxf(m, s_part[q][j].x);
+        for (int q = 0; q < 4; ++q) t += s_part[q][j].y * exp2_approx((s_part[q][j].x - m) * kLog2e);
+        g.part[(size_t)blockIdx.x * g.B + j] = make_float2(m, t);
     }
     tc_fence_before();
     __syncthreads();
