@@ -20,7 +20,8 @@
 //
 // The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
 // 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
-// cut after 128 steps (16 for fp32 tensors) and the pieces added in registers, rounded to nearest.
+// cut after 128 steps (16 for fp32 tensors, where it is the product of the leading terms) and the pieces added in
+// registers, rounded to nearest.
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,
 // l h are accumulated, smallest first: what is left out is below 2^-24 of the value.
@@ -79,6 +80,7 @@ struct CeGemm {
     int b_r0, b_k0;           // coordinates of B's first row and of its first K value
     int tiles_m, tiles_n, splits, group_m;
     int piece;                // K blocks of a chain (with PROMOTE)
+    int tail;                 // steps of 16 in a segment's last K block
     CeHeader *head;
     // kLse, kDz
     const void *bias;         // nullable, at column 0 of this launch
@@ -153,6 +155,12 @@ __device__ __forceinline__ void ce_range(const CeGemm &g, int split, int &kb0, i
         kb0 = (int)((unsigned)(kb * split) / (unsigned)g.splits);
         kb1 = (int)((unsigned)(kb * (split + 1)) / (unsigned)g.splits);
     }
+}
+// End of the chain that starts at K block i (with PROMOTE): the terms before the last, h h, are at most 2^-8 of the result, so
+// that what their chain loses does not show and they are one piece; h h is cut every g.piece blocks.
+__device__ __forceinline__ int ce_piece_end(const CeGemm &g, int i, int kb1) {
+    const int last = (g.n_seg - 1) * g.kblocks;
+    return min(i < last ? last : i + g.piece, kb1);
 }
 __device__ __forceinline__ CeTile ce_tile(const CeGemm &g, int item, int split) {
     unsigned r = (unsigned)(item - split * g.tiles_m * g.tiles_n);
@@ -462,9 +470,10 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
             const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
             const uint64_t bd0 = B_MN ? make_desc(base + kBlockBytes, 1024, 2u, kBlockBytes / 2) : make_desc(base + kBlockBytes, 1024, 2u);
-            auto multiply = [&](uint32_t s, int h, uint32_t acc, bool fresh) {
+            auto multiply = [&](uint32_t s, int h, uint32_t acc, bool fresh, int steps) {
 #pragma unroll
                 for (int k = 0; k < kw / 16; ++k) {
+                    if (k >= steps) break;
                     const uint32_t at = s * (kStageBytes >> 4), kk = (uint32_t)((k >> 2) * (kHalf * kKBox * 2 >> 4) + (k & 3) * 2);
                     mma_pair(tmem + acc * kTile, ad0 + (uint64_t)(at + (A_MN ? 128u * k : kk)),
                              bd0 + (uint64_t)(at + h * (kBlockBytes >> 4) + (B_MN ? 128u * k : kk)), idesc, !fresh || k > 0);
@@ -475,8 +484,9 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int item = first; item < n_items && ok; item += step) {
                 int kb0, kb1;
                 ce_range(g, ce_split(g, item), kb0, kb1);
+                int kb = kb0 == 0 ? 0 : kb0 % g.kblocks;  // within its segment: the last one has g.tail steps of 16
                 for (int i0 = kb0; i0 < kb1; u += kHalves) {
-                    const int i1 = PROMOTE ? min(i0 + g.piece, kb1) : kb1;
+                    const int i1 = PROMOTE ? ce_piece_end(g, i0, kb1) : kb1;
                     // the first K block waits for the accumulators, one after the other
                     ok = mbar_wait(smem_u32(&full[s]), ph, wt, 53);
 #pragma unroll
@@ -484,20 +494,27 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         const uint32_t acc = (u + h) & 1u;
                         ok = mbar_wait(smem_u32(&acc_empty[acc]), (((u + h) >> 1) & 1u) ^ 1u, wt, 52);
                         tc_fence_after();
-                        if (ok && issuer) multiply(s, h, acc, true);
+                        if (ok && issuer) multiply(s, h, acc, true, kb == g.kblocks - 1 ? g.tail : kw / 16);
                     }
                     if (!ok) break;
                     if (issuer) commit_pair(smem_u32(&empty[s]));
                     if (++s == kStages) { s = 0; ph ^= 1u; }
+                    if (++kb == g.kblocks) kb = 0;
                     for (int i = i0 + 1; i < i1; ++i) {
                         if (!mbar_wait(smem_u32(&full[s]), ph, wt, 53)) { ok = false; break; }
                         tc_fence_after();
                         if (issuer) {
+                            if (kb == g.kblocks - 1) {
 #pragma unroll
-                            for (int h = 0; h < kHalves; ++h) multiply(s, h, (u + h) & 1u, false);
+                                for (int h = 0; h < kHalves; ++h) multiply(s, h, (u + h) & 1u, false, g.tail);
+                            } else {
+#pragma unroll
+                                for (int h = 0; h < kHalves; ++h) multiply(s, h, (u + h) & 1u, false, kw / 16);
+                            }
                             commit_pair(smem_u32(&empty[s]));
                         }
                         if (++s == kStages) { s = 0; ph ^= 1u; }
+                        if (++kb == g.kblocks) kb = 0;
                     }
                     if (!ok) break;
                     if (issuer) {
@@ -521,7 +538,8 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (PROMOTE) {
                 int kb0, kb1;
                 ce_range(g, split, kb0, kb1);
-                pieces = (kb1 - kb0 + g.piece - 1) / g.piece;
+                pieces = 0;
+                for (int i = kb0; i < kb1; i = ce_piece_end(g, i, kb1)) ++pieces;
             }
             const uint32_t buf = base + kStageRing + (uint32_t)(warp - 2) * kOutBuf;
 #pragma unroll 1
@@ -906,6 +924,7 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
     if (out.ptr && !ce_map(out.ptr, out.rows, out.cols, out.cols, 32, &mo)) return -1;
     if (!ce_map(a.ptr, a.rows, a.cols, a.cols, A_MN ? kw : kHalf, &ma) || !ce_map(b.ptr, b.rows, b.cols, b.cols, B_MN ? kw : kHalf, &mb)) return -1;
     g.kblocks = (g.K + kw - 1) / kw;
+    g.tail = (g.K - (g.kblocks - 1) * kw + 15) / 16;
     g.piece = (g.n_seg > 2 ? kPieceF32 : kPieceBf16) / kw;
     g.tiles_n = (g.N + NT - 1) / NT;
     g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
@@ -1019,7 +1038,7 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
         r = rows_launch<kLse>(ow, ox, g, s);
     } else {
         CeGemm g{};
-        g.M = B; g.N = out; g.K = p.plane; g.head = head;
+        g.M = B; g.N = out; g.K = in; g.head = head;
         ce_segments(g, p.planes, p.plane, p.planes, p.plane);
         g.bias = bias; g.bias_bf16 = prec == P_BF16; g.labels = labels; g.V = out;
         g.part = part; g.zlab = zlab;
@@ -1089,7 +1108,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         const int cols = std::min(p.chunk, out - v0);
         {
             CeGemm g{};
-            g.M = B; g.N = cols; g.K = p.plane; g.head = head; g.b_r0 = v0;
+            g.M = B; g.N = cols; g.K = in; g.head = head; g.b_r0 = v0;
             ce_segments(g, p.planes, p.plane, p.planes, p.plane);
             g.bias = bias ? (const uint8_t *)bias + (size_t)v0 * es : nullptr;
             g.bias_bf16 = prec == P_BF16; g.labels = labels; g.v0 = v0; g.V = out;
