@@ -146,6 +146,10 @@ __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx
 // Divisions by sizes known at launch only cost an issuing thread a hundred cycles each, in which the tensor cores run
 // dry: the K range has none without splits, and the product of the two factors fits 32 bits (at most 2^21 x 74).
 struct CeTile { int m, n; };
+// Columns the MMAs of column tile n compute: all, or for the last tile what is left, in steps of 32 (16 rows of B per CTA).
+template <int NT> __device__ __forceinline__ int ce_width(const CeGemm &g, int n) {
+    return NT == kTile ? min(kTile, (g.N - n * NT + 31) & ~31) : kTile;
+}
 __device__ __forceinline__ int ce_split(const CeGemm &g, int item) { return g.splits == 1 ? 0 : item / (g.tiles_m * g.tiles_n); }
 __device__ __forceinline__ void ce_range(const CeGemm &g, int split, int &kb0, int &kb1) {
     const int kb = g.kblocks * g.n_seg;
@@ -425,7 +429,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const CeTile t = ce_tile(g, item, split);
                 int kb0, kb1;
                 ce_range(g, split, kb0, kb1);
-                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * NT + (int)rank * kHalf;
+                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * NT + (int)rank * (ce_width<NT>(g, t.n) / 2);
                 int seg = kb0 == 0 ? 0 : kb0 / g.kblocks, kb = kb0 - seg * g.kblocks;
                 for (int i = kb0; i < kb1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 51)) { ok = false; break; }
@@ -464,8 +468,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             // accumulator and what follows its last K block stand outside (with them inside, under one lane,
             // 8192 x 4096 x 65536 took 3.56 ms instead of 2.92).
             const bool issuer = elect_one();
-            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
-                                   ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+            uint32_t idesc = 0;
             // K-major: 16 K values are 32 bytes of a swizzle row, the next 64 values 16 KB further.  MN-major: 16 rows of
             // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
             const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
@@ -483,7 +486,11 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             uint32_t s = 0, ph = 0, u = 0;  // stage, its parity, accumulators used so far
             for (int item = first; item < n_items && ok; item += step) {
                 int kb0, kb1;
-                ce_range(g, ce_split(g, item), kb0, kb1);
+                const int split = ce_split(g, item);
+                ce_range(g, split, kb0, kb1);
+                const int width = g.tiles_n * NT == g.N ? kTile : ce_width<NT>(g, ce_tile(g, item, split).n);
+                idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(width >> 3) << 17) |
+                        ((uint32_t)(kTile >> 4) << 24);
                 int kb = kb0 == 0 ? 0 : kb0 % g.kblocks;  // within its segment: the last one has g.tail steps of 16
                 for (int i0 = kb0; i0 < kb1; u += kHalves) {
                     const int i1 = PROMOTE ? ce_piece_end(g, i0, kb1) : kb1;
@@ -857,8 +864,12 @@ int rows_splits(int B, int in, int out, int ld) {
 CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     CePlan p{};
     p.planes = prec == P_F32 ? 3 : 1;
-    p.plane = prec == P_F32 ? up(in, 2 * kKBox) : up(in, 8);  // a stage never reaches into the next term
-    p.pack_w = prec == P_F32 || in % 8 != 0;
+    // fp32: a stage never reaches into the next term.  bf16: rows that start on 128-byte lines
+    p.plane = prec == P_F32 ? up(in, 2 * kKBox) : up(in, kKBox);
+    // Rows of W that TMA can read but that do not start on 32-byte sectors cost every read of them a third more time (4096
+    // rows, 32000 entries: 210 us at 1000 columns, 166 us at 1024); the copy costs the bytes of W twice and is paid for
+    // by about 2000 rows (2001 x 1000 x 50021: 179 us without, about as much with it).
+    p.pack_w = prec == P_F32 || in % 8 != 0 || (in % 16 != 0 && B >= 2048);
     p.pack_x = p.pack_w || backward;
     // an fp32 dW of bf16 operands gets 16 bits of dz (two terms), as the fully connected layer's loss gradient does; a bf16
     // dW or dx is rounded to 8 bits itself and takes dz rounded once to bf16

@@ -126,7 +126,7 @@ class Ce:
 
 CE_SHAPES = [(1, 8, 1), (1, 64, 100), (3, 5, 7), (128, 64, 100), (130, 72, 257), (257, 264, 513), (300, 521, 1000), (33, 1000, 4099),
              (2, 4096, 300), (511, 16, 255), (64, 2048, 12000),
-             (16, 256, 20000), (20, 136, 3001), (65, 128, 640)]
+             (16, 256, 20000), (20, 136, 3001), (65, 128, 640), (2050, 136, 520)]
 
 
 @gpu
