@@ -625,6 +625,8 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
 #include "linear_ce_rows.cuh"
 
+#include "linear_ce_head.cuh"
+
 // ---- joining the forward pass ----------------------------------------------------------------------------------------
 // rows rows per block of 512 threads, the 512 / rows threads of a row share its pieces, eight loads in flight each.  The mean is taken by the block
 // that finishes last, over the blocks' sums in index order.
@@ -1008,6 +1010,35 @@ void ce_segments(CeGemm &g, int a_planes, int a_plane, int b_planes, int b_plane
     add(2, 0); add(0, 2); add(1, 1); add(1, 0); add(0, 1); add(0, 0);
 }
 
+// Small heads: one launch per direction on the CUDA cores.  The forward pass has eight CTAs: from 17 rows of bf16 each, the
+// general path's two launches are faster (256 x 64 x 100: 13.3 us, 10.5 us; fp32, which the general path has to split,
+// 14.3 us, 18 us).
+bool head_fits(int prec, int B, int in, int out, bool backward) {
+    return B <= (backward || prec == P_F32 ? kHeadMaxB : 128) && in <= kHeadMaxD && head_smem(B, in, out) <= (size_t)kHeadSmem;
+}
+template <typename K> bool head_ready(K kernel, int &ready_dev) {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem) != cudaSuccess) return false;
+        ready_dev = dev;
+    }
+    return true;
+}
+template <typename T> int head_fwd(const CeHeadArgs &g, const Launch &s) {
+    static thread_local int ready = -1;
+    if (!head_ready(ce_head_fwd_kernel<T>, ready)) return -1;
+    launch_k(ce_head_fwd_kernel<T>, 8, kHeadThreads, head_smem(g.B, g.D, g.V), s, g);
+    return 1;
+}
+template <typename T> int head_bwd(const CeHeadArgs &g, const Launch &s) {
+    static thread_local int ready = -1;
+    if (!head_ready(ce_head_bwd_kernel<T>, ready)) return -1;
+    const int row_ctas = g.dx ? (g.B + kHeadRows - 1) / kHeadRows : 0, slices = g.dW || g.db ? (g.V + kHeadRows - 1) / kHeadRows : 0;
+    launch_k(ce_head_bwd_kernel<T>, row_ctas + slices, kHeadThreads, head_smem(g.B, g.D, g.V), s, g, row_ctas);
+    return 1;
+}
+
 int grid_for(size_t threads) { return (int)std::max<size_t>(1, std::min<size_t>((threads + 255) / 256, 148 * 8)); }
 
 int pack(int prec, const void *src, void *dst, const int *labels, int rows, int cols, const CePlan &p, int V, CeHeader *head, int count, int mean,
@@ -1030,6 +1061,11 @@ size_t linear_ce_workspace_bytes(int prec, int B, int in, int out, int backward)
 
 int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bias, const int *labels, float *loss, float *row_loss, float *lse,
                          void *ws, int B, int in, int out, Launch s) {
+    if (head_fits(prec, B, in, out, false)) {
+        CeHeadArgs g{};
+        g.x = x; g.W = W; g.bias = bias; g.labels = labels; g.loss = loss; g.row_loss = row_loss; g.lse_out = lse; g.B = B; g.D = in; g.V = out;
+        return prec == P_BF16 ? head_fwd<bf16>(g, s) : head_fwd<float>(g, s);
+    }
     const CePlan p = ce_plan(prec, B, in, out, false, false);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
@@ -1065,6 +1101,12 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
 
 int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bias, const int *labels, const float *lse, const float *dloss,
                          const float *drow, void *dx, void *dW, float *db, void *ws, int B, int in, int out, int dw_f32, Launch s) {
+    if (head_fits(prec, B, in, out, true) && dx != x) {  // its CTAs read x while others write dx
+        CeHeadArgs g{};
+        g.x = x; g.W = W; g.bias = bias; g.labels = labels; g.lse = lse; g.dloss = dloss; g.drow = drow; g.dx = dx; g.dW = dW; g.db = db;
+        g.B = B; g.D = in; g.V = out; g.dw_f32 = dw_f32;
+        return prec == P_BF16 ? head_bwd<bf16>(g, s) : head_bwd<float>(g, s);
+    }
     const CePlan p = ce_plan(prec, B, in, out, true, dw_f32 != 0);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;

@@ -126,7 +126,8 @@ class Ce:
 
 CE_SHAPES = [(1, 8, 1), (1, 64, 100), (3, 5, 7), (128, 64, 100), (130, 72, 257), (257, 264, 513), (300, 521, 1000), (33, 1000, 4099),
              (2, 4096, 300), (511, 16, 255), (64, 2048, 12000),
-             (16, 256, 20000), (20, 136, 3001), (65, 128, 640), (2050, 136, 520)]
+             (16, 256, 20000), (20, 136, 3001), (65, 128, 640), (2050, 136, 520),
+             (256, 64, 100), (200, 63, 90), (40, 512, 50), (9, 300, 60)]
 
 
 @gpu
@@ -324,6 +325,22 @@ def test_linear_ce_other_stream_and_recorded(binding, prec):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, refs[k % 2])), k
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("shape", [(128, 64, 100), (200, 63, 90), (40, 512, 50), (20, 136, 3001), (300, 72, 900)], ids=lambda s: "x".join(map(str, s)))
+def test_linear_ce_gradient_over_the_rows(binding, shape, prec):
+    """dx may be x itself: the same bits as into a buffer of its own where both take the same kernels, within the
+    tolerance everywhere."""
+    c = Ce(*shape, prec, True, 0.2, seed=19).reference()
+    x, lse = c.x.clone(), c.lse.float()
+    ws = torch.empty(binding.linear_ce_workspace_bytes(prec, *shape, True), dtype=torch.uint8, device="cuda")
+    dw, db = torch.empty_like(c.w), f32(c.V)
+    binding.linear_ce_bwd(prec, x, c.w, c.bias, c.labels, lse, None, None, x, dw, db, ws, c.B, c.D, c.V)
+    within(x, c.dx, c.e_dx, "dx")
+    within(dw, c.dw, c.e_dw, "dW")
+    within(db, c.db, c.e_db, "db")
 
 
 @gpu
