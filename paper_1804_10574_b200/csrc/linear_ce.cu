@@ -79,6 +79,7 @@ struct CeGemm {
     int a_off[kMaxSeg], b_off[kMaxSeg];  // where a segment's term starts: in K (K-major operand) or in M / N
     int b_r0, b_k0;           // coordinates of B's first row and of its first K value
     int tiles_m, tiles_n, splits, group_m;
+    int width;                // columns of a tile: at most NT, a multiple of 64, alike for all tiles of a launch
     int piece;                // K blocks of a chain (with PROMOTE)
     int tail;                 // steps of 16 in a segment's last K block
     CeHeader *head;
@@ -87,7 +88,7 @@ struct CeGemm {
     int bias_bf16;
     const int *labels;        // label of every row; columns are v0 + n
     int v0, V;
-    float2 *part;             // kLse: [ceil(N / 128)][M] (maximum, sum)
+    float2 *part;             // kLse: [2 tiles_n][M] (maximum, sum)
     float *zlab;              // kLse: logit of the label
     const float *lse, *drow;  // kDz
     int planes, dz_plane;     // kDz: dz is [M][planes * dz_plane]
@@ -146,10 +147,6 @@ __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx
 // Divisions by sizes known at launch only cost an issuing thread a hundred cycles each, in which the tensor cores run
 // dry: the K range has none without splits, and the product of the two factors fits 32 bits (at most 2^21 x 74).
 struct CeTile { int m, n; };
-// Columns the MMAs of column tile n compute: all, or for the last tile what is left, in steps of 32 (16 rows of B per CTA).
-template <int NT> __device__ __forceinline__ int ce_width(const CeGemm &g, int n) {
-    return NT == kTile ? min(kTile, (g.N - n * NT + 31) & ~31) : kTile;
-}
 __device__ __forceinline__ int ce_split(const CeGemm &g, int item) { return g.splits == 1 ? 0 : item / (g.tiles_m * g.tiles_n); }
 __device__ __forceinline__ void ce_range(const CeGemm &g, int split, int &kb0, int &kb1) {
     const int kb = g.kblocks * g.n_seg;
@@ -267,8 +264,6 @@ template <int MODE> __device__ __forceinline__ CeRow ce_row(const CeGemm &g, int
     }
     return r;
 }
-// first column that an epilogue has nothing to do with (kDz: a stage of the next product reads up to 128 columns)
-template <int MODE> __device__ __forceinline__ int ce_columns(const CeGemm &g) { return MODE == kDz ? (g.N + 127) / 128 * 128 : g.N; }
 
 // What becomes of 64 columns of the warp's 32 rows: v at columns col .. of row r.row.
 template <int MODE>
@@ -429,7 +424,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const CeTile t = ce_tile(g, item, split);
                 int kb0, kb1;
                 ce_range(g, split, kb0, kb1);
-                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * NT + (int)rank * (ce_width<NT>(g, t.n) / 2);
+                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * g.width + (int)rank * (NT == kTile ? g.width / 2 : kHalf);
                 int seg = kb0 == 0 ? 0 : kb0 / g.kblocks, kb = kb0 - seg * g.kblocks;
                 for (int i = kb0; i < kb1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 51)) { ok = false; break; }
@@ -468,7 +463,8 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             // accumulator and what follows its last K block stand outside (with them inside, under one lane,
             // 8192 x 4096 x 65536 took 3.56 ms instead of 2.92).
             const bool issuer = elect_one();
-            uint32_t idesc = 0;
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                                   ((uint32_t)((NT == kTile ? g.width : kTile) >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
             // K-major: 16 K values are 32 bytes of a swizzle row, the next 64 values 16 KB further.  MN-major: 16 rows of
             // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
             const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
@@ -488,9 +484,6 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 int kb0, kb1;
                 const int split = ce_split(g, item);
                 ce_range(g, split, kb0, kb1);
-                const int width = g.tiles_n * NT == g.N ? kTile : ce_width<NT>(g, ce_tile(g, item, split).n);
-                idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(width >> 3) << 17) |
-                        ((uint32_t)(kTile >> 4) << 24);
                 int kb = kb0 == 0 ? 0 : kb0 % g.kblocks;  // within its segment: the last one has g.tail steps of 16
                 for (int i0 = kb0; i0 < kb1; u += kHalves) {
                     const int i1 = PROMOTE ? ce_piece_end(g, i0, kb1) : kb1;
@@ -551,7 +544,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t buf = base + kStageRing + (uint32_t)(warp - 2) * kOutBuf;
 #pragma unroll 1
             for (int h = 0; h < kHalves && ok; ++h) {
-                const int col0 = t.n * NT + h * kTile + half * kHalf, live = ce_columns<MODE>(g) - col0;
+                const int first_col = h * kTile + half * kHalf, col0 = t.n * g.width + first_col, live = min(g.width - first_col, g.N - col0);
                 CeRow r;
                 if (!PROMOTE) r = ce_row<MODE>(g, split, row);
                 float v[PROMOTE ? kHalf : kKBox];
@@ -603,7 +596,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     for (int c = 0; c < kHalf; c += kKBox)
                         if (c < live) ce_finish<MODE>(g, &map_out, buf, v + c, r, col0 + c, lane);
                 }
-                if (MODE == kLse && row < g.M && live > 0) g.part[(size_t)(col0 / kHalf) * g.M + row] = make_float2(r.top, r.sum);
+                if (MODE == kLse && row < g.M) g.part[(size_t)(2 * t.n + half) * g.M + row] = make_float2(r.top, r.sum);
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -835,6 +828,12 @@ constexpr size_t kDzBytes = (size_t)256 << 20;
 constexpr int kPairs = 74;  // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
 constexpr double kWideCost = 0.97;  // time of a product in a 256 x 512 tile against a 256 x 256 one
 
+// Columns of the tiles that cover N columns: as many tiles as it takes at `nt` columns, alike (520 columns: three of 192
+// rather than 256, 256 and 8, which loads as much of A as the others).
+int ce_width(int N, int nt) {
+    const int tiles = (N + nt - 1) / nt;
+    return nt == kTile ? ((N + tiles - 1) / tiles + kKBox - 1) / kKBox * kKBox : nt;
+}
 double ce_rounds(int M, int N, int nt, int splits);
 
 struct CePlan {
@@ -878,7 +877,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.rows = prec == P_BF16 && B <= kRowsMax;
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = p.rows ? rows_grid(out, kRowsGridMax) : (out + kHalf - 1) / kHalf;
+    p.n_part = p.rows ? rows_grid(out, kRowsGridMax) : 2 * ((out + kTile - 1) / kTile);
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -940,6 +939,7 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
     g.tail = (g.K - (g.kblocks - 1) * kw + 15) / 16;
     g.piece = (g.n_seg > 2 ? kPieceF32 : kPieceBf16) / kw;
     g.tiles_n = (g.N + NT - 1) / NT;
+    g.width = ce_width(g.N, NT);
     g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
     const long items = (long)g.tiles_m * g.tiles_n * g.splits;
     if (items > 0x7fffffff) return -1;
@@ -955,10 +955,10 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
     return 1;
 }
 
-// Rounds of the GPU's CTA pairs that `tiles` tiles (times splits) take, in units of one 256 x 256 tile of the whole K.
+// Rounds of the GPU's CTA pairs that the tiles (times splits) take, in units of one 256 x 256 tile of the whole K.
 double ce_rounds(int M, int N, int nt, int splits) {
     const long items = (long)((M + kTile - 1) / kTile) * ((N + nt - 1) / nt) * splits;
-    return (double)((items + kPairs - 1) / kPairs) * (nt / kTile) * (nt > kTile ? kWideCost : 1.0) / splits;
+    return (double)((items + kPairs - 1) / kPairs) * ce_width(N, nt) / kTile * (nt > kTile ? kWideCost : 1.0) / splits;
 }
 bool ce_wide(int M, int N, int splits) {
     return N > kTile && ce_rounds(M, N, 2 * kTile, splits) <= ce_rounds(M, N, kTile, splits);
