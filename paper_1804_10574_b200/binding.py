@@ -446,16 +446,16 @@ def sgd_update(prec, w, v, g, w_version, n, lr, momentum, weight_decay, stream=N
 def _tensor(a, n, size, what):
     """The address of a tensor argument that the caller says has n elements of `size` bytes.  A torch tensor that is too
     small, strided or of another element size is refused here: the C call sees an address only."""
-    if a is None or isinstance(a, int):
-        return a
-    if hasattr(a, "is_contiguous"):
-        if not a.is_contiguous():
-            raise ValueError("%s has to be contiguous" % what)
-        if a.element_size() != size:
-            raise ValueError("%s has elements of %d bytes instead of %d" % (what, a.element_size(), size))
-        if a.numel() < n:
-            raise ValueError("%s has %d elements instead of %d" % (what, a.numel(), n))
-    return _ptr(a)
+    if a is None:
+        return None
+    try:
+        if a.is_contiguous() and a.element_size() == size and a.numel() >= n:
+            return a.data_ptr()
+    except AttributeError:
+        return _ptr(a)
+    if not a.is_contiguous():
+        raise ValueError("%s has to be contiguous" % what)
+    raise ValueError("%s has %d elements of %d bytes instead of %d of %d" % (what, a.numel(), a.element_size(), n, size))
 
 
 def _elem(prec):

@@ -97,6 +97,7 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
                              const float *drow, void *dx, void *dW, float *db, void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32,
                              void *stream) {
     if (bad_prec(precision) || !x || !W || !labels || !lse || !workspace || (!dx && !dW && !db) || (dloss && drow)) return DDG_ERR_INVALID_ARG;
+    if (dW == W) return refuse(DDG_ERR_INVALID_ARG, "linear_ce: dW may not be W");
     if (!ce_sizes_ok(B, in, out)) return DDG_ERR_UNSUPPORTED;
     ddg_status st = ce_check(precision, x, W, workspace, workspace_bytes, B, in, out, 1);
     if (st != DDG_OK) return st;

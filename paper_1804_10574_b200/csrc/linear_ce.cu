@@ -29,6 +29,7 @@
 
 #include <algorithm>
 
+#include "cluster.cuh"
 #include "common.cuh"
 #include "conv_tc.h"
 #include "lm_ops.h"
@@ -101,15 +102,6 @@ struct CeGemm {
     const float *part_in;
 };
 
-__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
 // Hands an accumulator back.  What it orders are the tcgen05 loads before the fence, not memory: a releasing arrival would
 // wait for the stores of the tile before (gradient of the logits, 4096 x 512 x 16384: 94 us with it, 75 us without).
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
@@ -706,18 +698,21 @@ __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict
 
 // ---- operands that TMA cannot read in place --------------------------------------------------------------------------
 // dst [rows][planes * plane] bf16: term p of column c at p * plane + c, zero past `cols`.  labels (nullable): rows that do
-// not count become zero, so that what stands in them (NaN among it) stays out of dW.  When `count` is set the
-// last block sets the scale of the backward pass instead of copying.
+// not count become zero, so that what stands in them (NaN among it) stays out of dW.  One launch copies up to two
+// matrices (x and W), by `blocks` blocks each; when `count` is set one more block sets the scale of the backward pass.
+struct CePackJob { const void *src; bf16 *dst; const int *labels; int rows, blocks; };
 template <typename T>
-__global__ void __launch_bounds__(256) ce_pack_kernel(const T *__restrict__ src, bf16 *__restrict__ dst, const int *__restrict__ labels, int rows, int cols,
-                                                      int plane, int planes, int V, CeHeader *head, int count, int mean, const float *__restrict__ dloss) {
+__global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, const CePackJob job_w, int cols, int plane, int planes, int V, CeHeader *head, int count, int mean,
+                                                      const int *__restrict__ labels_of_rows, int rows_of_labels, const float *__restrict__ dloss) {
     pdl_launch();
     pdl_wait();
     if (count && blockIdx.x == gridDim.x - 1) {
         __shared__ int part[256];
         int n = 0;
-        if (mean)
-            for (int i = threadIdx.x; i < rows; i += 256) n += labels[i] >= 0 && labels[i] < V;
+        if (mean) {
+#pragma unroll 16
+            for (int i = threadIdx.x; i < rows_of_labels; i += 256) n += labels_of_rows[i] >= 0 && labels_of_rows[i] < V;
+        }
         part[threadIdx.x] = n;
         __syncthreads();
         for (int o = 128; o > 0; o >>= 1) {
@@ -727,17 +722,21 @@ __global__ void __launch_bounds__(256) ce_pack_kernel(const T *__restrict__ src,
         if (threadIdx.x == 0) head->scale = mean ? (dloss ? *dloss : 1.f) / (float)max(part[0], 1) : 1.f;
         return;
     }
+    const bool second = (int)blockIdx.x >= job_x.blocks;
+    const CePackJob &job = second ? job_w : job_x;
+    const T *src = (const T *)job.src;
+    const int *labels = job.labels;
+    bf16 *dst = job.dst;
     // eight columns per step; plane is a multiple of 8
-    const size_t total = (size_t)rows * (plane / 8);
-    const size_t blocks = gridDim.x - (count ? 1 : 0);
-    const bool vec = cols % (16 / (int)sizeof(T)) == 0 && (reinterpret_cast<uintptr_t>(src) & 15) == 0 && cols == plane;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += blocks * 256) {
+    const size_t total = (size_t)job.rows * (plane / 8), stride = (size_t)job.blocks * 256;
+    const bool vec = cols % (16 / (int)sizeof(T)) == 0 && (reinterpret_cast<uintptr_t>(src) & 15) == 0;
+    for (size_t i = (size_t)(blockIdx.x - (second ? job_x.blocks : 0)) * 256 + threadIdx.x; i < total; i += stride) {
         const size_t row = i / (plane / 8);
         const int c = (int)(i - row * (plane / 8)) * 8;
         float v[8];
         bool live = true;
         if (labels) { const int y = labels[row]; live = y >= 0 && y < V; }
-        if (live && vec) {
+        if (live && vec && c + 8 <= cols) {
             if (sizeof(T) == 2) {
                 load_f<T, 8>(src + row * cols + c, v);
             } else {
@@ -762,33 +761,44 @@ __global__ void __launch_bounds__(256) ce_pack_kernel(const T *__restrict__ src,
 }
 
 // ---- ends of the backward pass ---------------------------------------------------------------------------------------
-// db[v0 + c] = scale * sum over row blocks of db_part[block][c], blocks in index order per thread, threads in index order
-__global__ void __launch_bounds__(256) ce_db_kernel(const float *__restrict__ db_part, int blocks, int plane, float *__restrict__ db, int cols, const CeHeader *head) {
+// db[c] = scale * sum over row blocks of part[block][c], for 32 columns per block of 256 threads: row blocks in index order
+// per warp, warps in index order
+struct CeDb { const float *part; float *db; int row_blocks, plane, cols; };
+__device__ __forceinline__ void ce_db(const CeDb &g, int block, float scale) {
     __shared__ double fold[8][32];
-    pdl_launch();
-    pdl_wait();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = block * 32 + lane;
     double a = 0.0;
-    if (c < cols)
-        for (int b = w; b < blocks; b += 8) a += (double)db_part[(size_t)b * plane + c];
+    if (c < g.cols) {
+#pragma unroll 8
+        for (int b = w; b < g.row_blocks; b += 8) a += (double)g.part[(size_t)b * g.plane + c];
+    }
     fold[w][lane] = a;
     __syncthreads();
-    if (w == 0 && c < cols) {
+    if (w == 0 && c < g.cols) {
         for (int i = 1; i < 8; ++i) a += fold[i][lane];
-        db[c] = g_ce_error ? __int_as_float(0x7fffffff) : (float)(a * (double)head->scale);
+        g.db[c] = g_ce_error ? __int_as_float(0x7fffffff) : (float)(a * (double)scale);
     }
 }
-
-// dx[n][c] = scale * sum_s part[s][n][c]; rows that do not count are zero
-template <typename T>
-__global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ part, int splits, size_t split_stride, int ld, const int *__restrict__ labels, T *__restrict__ dx,
-                                                    int B, int in, int V, int vec, const CeHeader *head) {
+__global__ void __launch_bounds__(256) ce_db_kernel(const CeDb g, const CeHeader *head) {
     pdl_launch();
     pdl_wait();
+    ce_db(g, blockIdx.x, head->scale);
+}
+
+// dx[n][c] = scale * sum_s part[s][n][c]; rows that do not count are zero.  The first db_blocks blocks fold db.
+template <typename T>
+__global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ part, int splits, size_t split_stride, int ld, const int *__restrict__ labels, T *__restrict__ dx,
+                                                    int B, int in, int V, int vec, const CeHeader *head, const CeDb db, int db_blocks) {
+    pdl_launch();
+    pdl_wait();
+    if ((int)blockIdx.x < db_blocks) {
+        ce_db(db, blockIdx.x, head->scale);
+        return;
+    }
     const bool failed = g_ce_error != 0;
     const float scale = head->scale, nan = __int_as_float(0x7fffffff);
     const size_t total = (size_t)B * (ld / 4);
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
+    for (size_t i = (size_t)(blockIdx.x - db_blocks) * 256 + threadIdx.x; i < total; i += (size_t)(gridDim.x - db_blocks) * 256) {
         const size_t row = i / (ld / 4);
         const int c = (int)(i - row * (ld / 4)) * 4;
         const int y = labels[row];
@@ -842,7 +852,7 @@ struct CePlan {
     int tiles_m, n_part;
     int splits, dx_ld;
     bool rows;               // a few rows: the kernels of linear_ce_rows.cuh
-    bool pack_x, pack_w;
+    bool pack_x, pack_w;     // backward: x always, with the rows that do not count as zeros
     size_t part, zlab, sums, x, w, dz, db, dx, bytes;
 };
 
@@ -901,7 +911,8 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
         // costs a write and a read of its partial sums.  Seconds by 1.4 PFLOP/s and 6 TB/s.
         const int kb = (int)std::min<long>(p.chunk, up(out, kKBox)) / kKBox * (prec == P_F32 ? 6 : 1);
         double best = 1e30;
-        for (int n = 1; n <= std::max(1, std::min(kPairs, kb / 8)); ++n) {
+        const int tiles = p.tiles_m * ((in + kTile - 1) / kTile), most = std::min(2 * kPairs / tiles, kb / 8);  // two rounds of pairs
+        for (int n = 1; n <= std::max(1, most); ++n) {
             const double rounds = prec == P_F32 ? ce_rounds(B, in, kTile, n) : std::min(ce_rounds(B, in, kTile, n), in > kTile ? ce_rounds(B, in, 2 * kTile, n) : 1e30);
             const double t = rounds * 2.0 * kTile * kTile * kKBox * kb * kPairs / 1.4e15 + (n > 1 ? 2e-6 + 8.0 * n * B * p.dx_ld / 6e12 : 0.0);
             if (t < best) { best = t; p.splits = n; }
@@ -1041,13 +1052,14 @@ template <typename T> int head_bwd(const CeHeadArgs &g, const Launch &s) {
 
 int grid_for(size_t threads) { return (int)std::max<size_t>(1, std::min<size_t>((threads + 255) / 256, 148 * 8)); }
 
-int pack(int prec, const void *src, void *dst, const int *labels, int rows, int cols, const CePlan &p, int V, CeHeader *head, int count, int mean,
-         const float *dloss, const Launch &s) {
-    const int grid = grid_for((size_t)rows * (p.plane / 8)) + (count ? 1 : 0);
-    if (prec == P_BF16)
-        launch_k(ce_pack_kernel<bf16>, grid, 256, 0, s, (const bf16 *)src, (bf16 *)dst, labels, rows, cols, p.plane, p.planes, V, head, count, mean, dloss);
-    else
-        launch_k(ce_pack_kernel<float>, grid, 256, 0, s, (const float *)src, (bf16 *)dst, labels, rows, cols, p.plane, p.planes, V, head, count, mean, dloss);
+// Copies x (nullable) and W (nullable) for TMA; backward: labels mask x's rows, and the scale is set.
+int pack(int prec, const void *x, void *x_dst, const void *W, void *w_dst, const int *labels, const CePlan &p, int B, int in, int out, CeHeader *head, bool backward,
+         bool mean, const float *dloss, const Launch &s) {
+    CePackJob jx{x, (bf16 *)x_dst, backward ? labels : nullptr, B, x ? grid_for((size_t)B * (p.plane / 8)) : 0};
+    CePackJob jw{W, (bf16 *)w_dst, nullptr, out, W ? grid_for((size_t)out * (p.plane / 8)) : 0};
+    const int grid = jx.blocks + jw.blocks + (backward ? 1 : 0);
+    if (prec == P_BF16) launch_k(ce_pack_kernel<bf16>, grid, 256, 0, s, jx, jw, in, p.plane, p.planes, out, head, backward ? 1 : 0, mean ? 1 : 0, labels, B, dloss);
+    else launch_k(ce_pack_kernel<float>, grid, 256, 0, s, jx, jw, in, p.plane, p.planes, out, head, backward ? 1 : 0, mean ? 1 : 0, labels, B, dloss);
     return 1;
 }
 
@@ -1070,8 +1082,11 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
     int n = 0;
-    if (p.pack_x) { n += pack(prec, x, base + p.x, nullptr, B, in, p, out, head, 0, 0, nullptr, s); x = base + p.x; }
-    if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, s); W = base + p.w; }
+    if (p.pack_w) {
+        n += pack(prec, x, base + p.x, W, base + p.w, labels, p, B, in, out, head, false, false, nullptr, s);
+        x = base + p.x;
+        W = base + p.w;
+    }
     const int cols = p.pack_w ? p.planes * p.plane : in;
     float2 *part = (float2 *)(base + p.part);
     float *zlab = (float *)(base + p.zlab);
@@ -1110,9 +1125,9 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
     const CePlan p = ce_plan(prec, B, in, out, true, dw_f32 != 0);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
-    int n = pack(prec, x, base + p.x, labels, B, in, p, out, head, 1, drow == nullptr, dloss, s);
+    int n = pack(prec, x, base + p.x, p.pack_w ? W : nullptr, base + p.w, labels, p, B, in, out, head, true, drow == nullptr, dloss, s);
     const void *xp = base + p.x;
-    if (p.pack_w) { n += pack(prec, W, base + p.w, nullptr, out, in, p, out, head, 0, 0, nullptr, s); W = base + p.w; }
+    if (p.pack_w) W = base + p.w;
     const int x_cols = p.planes * p.plane, w_cols = p.pack_w ? p.planes * p.plane : in;
     const int dz_cols = p.dz_planes * p.chunk;
     bf16 *dz = (bf16 *)(base + p.dz);
@@ -1138,6 +1153,8 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         return ce_launch<kWeightGrad, true, true>(oz, ox, o, g, !out_bf16, s);
     };
     const bool dx_direct = !p.rows && p.splits == 1;  // the last chunk's product writes dx itself
+    const bool db_last = db && dx && !p.rows && !dx_direct && p.chunk >= out;  // db is folded beside dx's partial sums
+    const CeDb db_all{(const float *)(base + p.db), db, (B + 31) / 32, p.chunk, out};
     if (p.rows) {
         CeRowsArgs g{};
         g.B = B; g.D = in; g.V = out; g.kblocks = (in + kRowsKw - 1) / kRowsKw; g.head = head;
@@ -1171,8 +1188,11 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
             if (r < 0) return r;
             n += r;
         }
-        if (db) {
-            launch_k(ce_db_kernel, ceil_div(cols, 32), 256, 0, s, (const float *)(base + p.db), (B + 31) / 32, p.chunk, db + v0, cols, (const CeHeader *)head);
+        if (db && !db_last) {
+            CeDb d = db_all;
+            d.db = db + v0;
+            d.cols = cols;
+            launch_k(ce_db_kernel, ceil_div(cols, 32), 256, 0, s, d, (const CeHeader *)head);
             ++n;
         }
         if (dx) {
@@ -1203,14 +1223,14 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         }
     }
     if (!dx || dx_direct) return n;
-    const int grid = grid_for((size_t)B * (p.dx_ld / 4));
+    const int db_blocks = db_last ? ceil_div(out, 32) : 0, grid = grid_for((size_t)B * (p.dx_ld / 4)) + db_blocks;
     const int vec = in % 4 == 0 && (reinterpret_cast<uintptr_t>(dx) & (4 * es - 1)) == 0;
     if (prec == P_BF16)
         launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec,
-                 (const CeHeader *)head);
+                 (const CeHeader *)head, db_all, db_blocks);
     else
         launch_k(ce_dx_kernel<float>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec,
-                 (const CeHeader *)head);
+                 (const CeHeader *)head, db_all, db_blocks);
     return n + 1;
 }
 

@@ -11,6 +11,7 @@
 
 #include <algorithm>
 
+#include "cluster.cuh"
 #include "common.cuh"
 #include "lm_ops.h"
 
@@ -33,6 +34,7 @@ template <bool MAX> __device__ __forceinline__ float row_reduce(float v, bool on
 }
 
 // what rms_plan gives a row of at most 16384 values
+constexpr int kRmsCluster = 8;
 constexpr int kWarpRowThreads = 256;  // of a backward block whose warps have a row each
 constexpr int rms_max_threads(int vec, int iter) { return (vec == 4 && iter == 4) || (vec == 1 && iter == 16) ? 1024 : 512; }
 
@@ -154,14 +156,16 @@ template <typename T, int VEC, int ITER> struct RawRow {
 // Blocks (or warps, where a row is one warp's) walk the rows; each keeps its share of dgamma in registers, a block's warps
 // add theirs up, and part[block][C] goes to the folding kernel.  With up to two vectors a thread, the next row's dy, h and dh
 // are loaded before this row's reduction, so that memory stays busy through its two barriers; with more there are no
-// registers for it.  dx may be dy, dh or h: a row is written after it was read, and the row that is loaded ahead is
+// registers for it.  Few rows are one cluster's (dgamma given), whose blocks fold their shares over one another's shared
+// memory instead: one launch less, which is what such a call costs.  dx may be dy, dh or h: a row is written after it was read, and the row that is loaded ahead is
 // the same walker's.
 template <typename T, int VEC, int ITER, bool WARP>
 __global__ void __launch_bounds__(WARP ? kWarpRowThreads : rms_max_threads(VEC, ITER), WARP ? (ITER == 1 ? 3 : 2) : (ITER == 1 ? 2 : 1))
-rms_bwd_kernel(const T *dy, const T *dh, const T *h, const T *__restrict__ gamma, const float *__restrict__ rstd, T *dx, float *__restrict__ part, int rows, int C) {
+rms_bwd_kernel(const T *dy, const T *dh, const T *h, const T *__restrict__ gamma, const float *__restrict__ rstd, T *dx, float *__restrict__ part, int rows, int C,
+               float *__restrict__ dgamma) {
     constexpr bool kAhead = ITER <= 2;
     __shared__ float red[32];
-    extern __shared__ float shares[];  // WARP: [warps][C]
+    extern __shared__ float shares[];  // WARP: [warps][C]; then, in a cluster, the block's [C]
     pdl_launch();
     pdl_wait();
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -230,21 +234,35 @@ rms_bwd_kernel(const T *dy, const T *dh, const T *h, const T *__restrict__ gamma
             r = rstd[row + walkers];
         }
     }
+    float *own = dgamma ? shares + (WARP ? warps * ((C + 3) & ~3) : 0) : part + (size_t)blockIdx.x * C;
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
         const int c = (i * tpr + t) * VEC;
-        if (c < C) {
-            if (WARP) store_f<float, VEC>(shares + warp * C + c, acc[i]);
-            else store_f<float, VEC>(part + (size_t)blockIdx.x * C + c, acc[i]);
-        }
+        if (c < C) store_f<float, VEC>(WARP ? shares + warp * ((C + 3) & ~3) + c : own + c, acc[i]);
     }
     if (WARP) {
         __syncthreads();
         for (int c = threadIdx.x; c < C; c += blockDim.x) {
             float sum = shares[c];
-            for (int w = 1; w < warps; ++w) sum += shares[w * C + c];
-            part[(size_t)blockIdx.x * C + c] = sum;
+            for (int w = 1; w < warps; ++w) sum += shares[w * ((C + 3) & ~3) + c];
+            own[c] = sum;
         }
+    }
+    if (dgamma) {  // a block's slice of the columns, blocks in index order
+        __syncthreads();
+        cluster_sync();
+        const uint32_t base = (uint32_t)__cvta_generic_to_shared(own);
+        for (int c = (int)cluster_rank() * blockDim.x + threadIdx.x; c < C; c += kRmsCluster * blockDim.x) {
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < kRmsCluster; ++r) {
+                float v;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_rank(base + 4u * c, r)));
+                sum += v;
+            }
+            dgamma[c] = sum;
+        }
+        cluster_sync();  // no block leaves while its share is read
     }
 }
 
@@ -326,12 +344,30 @@ template <typename T, int VEC>
 static int rms_bwd(const void *dy, const void *dh, const void *h, const void *gamma, const float *rstd, void *dx, float *dgamma, float *scratch, int rows, int C,
                    const Launch &s) {
     const RmsPlan p = rms_bwd_plan(C / VEC, VEC > 1);
-    const int grid = rms_bwd_blocks(p, rows);
+    // one cluster of eight blocks while a warp (or block) has at most four rows
+    const bool cluster = rows <= kRmsCluster * p.rpb * 4 && (p.tpr == 32 || C <= 8192);
+    const int grid = cluster ? kRmsCluster : rms_bwd_blocks(p, rows);
     auto go = [&](auto kernel, size_t smem) {
-        launch_k(kernel, grid, p.threads, smem, s, (const T *)dy, (const T *)dh, (const T *)h, (const T *)gamma, rstd, (T *)dx, scratch, rows, C);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(grid); cfg.blockDim = dim3(p.threads); cfg.stream = s.s;
+        cfg.dynamicSmemBytes = smem + (cluster ? (size_t)C * sizeof(float) : 0);
+        cudaLaunchAttribute attr[2];
+        cfg.attrs = attr;
+        if (cluster) {
+            attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+            attr[cfg.numAttrs].val.clusterDim.x = kRmsCluster;
+            attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+            ++cfg.numAttrs;
+        }
+        if (s.pdl == 1) {
+            attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+            ++cfg.numAttrs;
+        }
+        cudaLaunchKernelEx(&cfg, kernel, (const T *)dy, (const T *)dh, (const T *)h, (const T *)gamma, rstd, (T *)dx, scratch, rows, C, cluster ? dgamma : (float *)nullptr);
     };
     if (p.tpr == 32) {
-        const size_t smem = (size_t)p.rpb * C * sizeof(float);
+        const size_t smem = (size_t)p.rpb * ((C + 3) & ~3) * sizeof(float);
         if (p.iter == 1) go(rms_bwd_kernel<T, VEC, 1, true>, smem); else go(rms_bwd_kernel<T, VEC, 2, true>, smem);
     } else {
         switch (p.iter) {
@@ -343,6 +379,7 @@ static int rms_bwd(const void *dy, const void *dh, const void *h, const void *ga
         default: return -1;
         }
     }
+    if (cluster) return 1;
     launch_k(rms_fold_kernel, (C + 31) / 32, 1024, 0, s, (const float *)scratch, grid, dgamma, C);
     return 2;
 }

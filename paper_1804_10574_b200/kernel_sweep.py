@@ -1,4 +1,5 @@
-"""Per-kernel sweep over the ResNet-110 layer shapes through the single-kernel C-ABI entry points.
+"""Per-kernel sweep over the ResNet-110 layer shapes, and over the tail of a language-model step (dropout, RMS norm,
+vocabulary projection with cross entropy), through the single-kernel C-ABI entry points.
 
     python -m paper_1804_10574_b200.kernel_sweep [--batch 1024] [--only NAME] [--iters 20] [--json] [--warm]
 
@@ -100,7 +101,37 @@ def cases(B):
     w, v, gr = (torch.randn(n, device="cuda") for _ in range(3))
     wv = torch.empty(n, dtype=bf, device="cuda")
     out.append(("sgd_update 1.73M params", lambda: binding.sgd_update(1, w, v, gr, wv, n, 0.01, 0.9, 5e-4), n * 22, 0.0, 0, (w, v, gr, wv)))
-    return out
+    return out + tail_cases(B)
+
+
+def tail_cases(B, D=1024, V=32000):
+    """The tail of a language-model step on B rows: bytes and flops that the operations cannot do without (the backward
+    pass of the projection multiplies half as much again: it computes the logits a second time)."""
+    bf = torch.bfloat16
+    x, res, dy, dh = (torch.randn(B, D, device="cuda").to(bf) for _ in range(4))
+    g = torch.ones(D, device="cuda").to(bf)
+    w = (torch.randn(V, D, device="cuda") * D ** -0.5).to(bf)
+    labels = torch.randint(0, V, (B,), device="cuda", dtype=torch.int32)
+    rng = torch.tensor([1, 0], dtype=torch.int64, device="cuda")
+    y, h, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty_like(w)
+    q = torch.empty(B, D, dtype=torch.uint8, device="cuda")
+    loss, rstd, lse, dg, sc8 = (torch.ones(n, device="cuda") for n in (1, B, B, D, B * D // 128))
+    sc = torch.empty(binding.rmsnorm_scratch_elems(B, D), device="cuda")
+    ws = torch.empty(max(binding.linear_ce_workspace_bytes(1, B, D, V, k) for k in (False, True)), dtype=torch.uint8, device="cuda")
+    keep = (x, res, dy, dh, g, w, labels, rng, y, h, dx, dw, q, loss, rstd, lse, dg, sc8, sc, ws)
+    binding.linear_ce_fwd(1, x, w, None, labels, loss, None, lse, ws, B, D, V)
+    n, flops, tag = B * D * 2, 2.0 * B * D * V, "%dx%d" % (B, D)
+    wtag = tag + "x%d" % V
+    return [
+        ("dropout_residual_fwd " + tag, lambda: binding.dropout_fwd(1, x, res, y, rng, B * D, 0.1), 3 * n, 0.0, 0, keep),
+        ("dropout_bwd " + tag, lambda: binding.dropout_bwd(1, dy, dx, rng, B * D, 0.1), 2 * n, 0.0, 0, keep),
+        ("add_rmsnorm_fwd " + tag, lambda: binding.add_rmsnorm_fwd(1, x, res, g, h, y, None, None, rstd, B, D), 4 * n, 0.0, 0, keep),
+        ("add_rmsnorm_fwd e4m3 " + tag, lambda: binding.add_rmsnorm_fwd(1, x, res, g, h, None, q, sc8, rstd, B, D, 128), 3 * n + n // 2, 0.0, 0, keep),
+        ("add_rmsnorm_bwd " + tag, lambda: binding.add_rmsnorm_bwd(1, dy, dh, x, g, rstd, dx, dg, sc, B, D), 4 * n, 0.0, 0, keep),
+        ("linear_ce_fwd " + wtag, lambda: binding.linear_ce_fwd(1, x, w, None, labels, loss, None, lse, ws, B, D, V), n + V * D * 2, flops, 1, keep),
+        ("linear_ce_bwd " + wtag, lambda: binding.linear_ce_bwd(1, x, w, None, labels, lse, None, None, dx, dw, None, ws, B, D, V),
+         2 * (n + V * D * 2), 2 * flops, 1, keep),
+    ]
 
 
 def main():
