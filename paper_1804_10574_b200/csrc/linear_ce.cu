@@ -785,10 +785,13 @@ __global__ void __launch_bounds__(256) ce_db_kernel(const CeDb g, const CeHeader
     ce_db(g, blockIdx.x, head->scale);
 }
 
-// dx[n][c] = scale * sum_s part[s][n][c]; rows that do not count are zero.  The first db_blocks blocks fold db.
+// dx[n][c] = scale * sum_s part[s][n][c]; rows that do not count are zero.  The first db_blocks blocks fold db.  A block takes
+// 256 / lanes groups of four columns at a time; `lanes` threads (1, or 8 where there are many splits and few columns)
+// share a group's splits and are added in index order.
 template <typename T>
 __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ part, int splits, size_t split_stride, int ld, const int *__restrict__ labels, T *__restrict__ dx,
-                                                    int B, int in, int V, int vec, const CeHeader *head, const CeDb db, int db_blocks) {
+                                                    int B, int in, int V, int vec, int lanes, const CeHeader *head, const CeDb db, int db_blocks) {
+    __shared__ float4 fold[256];
     pdl_launch();
     pdl_wait();
     if ((int)blockIdx.x < db_blocks) {
@@ -797,19 +800,35 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ pa
     }
     const bool failed = g_ce_error != 0;
     const float scale = head->scale, nan = __int_as_float(0x7fffffff);
+    const int groups = 256 / lanes, g = threadIdx.x & (groups - 1), lane = threadIdx.x / groups;
     const size_t total = (size_t)B * (ld / 4);
-    for (size_t i = (size_t)(blockIdx.x - db_blocks) * 256 + threadIdx.x; i < total; i += (size_t)(gridDim.x - db_blocks) * 256) {
-        const size_t row = i / (ld / 4);
+    for (size_t i0 = (size_t)(blockIdx.x - db_blocks) * groups; i0 < total; i0 += (size_t)(gridDim.x - db_blocks) * groups) {
+        const size_t i = i0 + g, row = i / (ld / 4);
         const int c = (int)(i - row * (ld / 4)) * 4;
-        const int y = labels[row];
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (y >= 0 && y < V) {
+        bool counted = false;
+        if (i < total) {
+            const int y = labels[row];
+            counted = y >= 0 && y < V;
+        }
+        if (counted) {
 #pragma unroll 8
-            for (int s = 0; s < splits; ++s) {
+            for (int s = lane; s < splits; s += lanes) {
                 const float4 q = *reinterpret_cast<const float4 *>(part + s * split_stride + row * ld + c);
                 a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
             }
         }
+        if (lanes > 1) {
+            __syncthreads();
+            fold[threadIdx.x] = a;
+            __syncthreads();
+            if (lane != 0) continue;
+            for (int l = 1; l < lanes; ++l) {
+                const float4 q = fold[l * groups + g];
+                a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
+            }
+        }
+        if (i >= total) continue;
         float v[4] = {a.x * scale, a.y * scale, a.z * scale, a.w * scale};
         if (failed) v[0] = v[1] = v[2] = v[3] = nan;
         if (vec) {
@@ -1094,7 +1113,7 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
     int r, n_part = p.n_part;
     if (p.rows) {
         CeRowsArgs g{};
-        g.B = B; g.D = in; g.V = out; g.kblocks = (in + kRowsKw - 1) / kRowsKw; g.head = head;
+        g.B = B; g.D = in; g.V = out; g.head = head;
         g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.part = part; g.zlab = zlab;
         n_part = rows_grid(out, sm_count());
         r = rows_launch<kLse>(ow, ox, g, s);
@@ -1157,7 +1176,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
     const CeDb db_all{(const float *)(base + p.db), db, (B + 31) / 32, p.chunk, out};
     if (p.rows) {
         CeRowsArgs g{};
-        g.B = B; g.D = in; g.V = out; g.kblocks = (in + kRowsKw - 1) / kRowsKw; g.head = head;
+        g.B = B; g.D = in; g.V = out; g.head = head;
         g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.lse = lse; g.drow = drow;
         g.dz = dz; g.db = db; g.planes = p.dz_planes;
         int r = rows_launch<kDz>(ow, ox, g, s);
@@ -1223,13 +1242,14 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         }
     }
     if (!dx || dx_direct) return n;
-    const int db_blocks = db_last ? ceil_div(out, 32) : 0, grid = grid_for((size_t)B * (p.dx_ld / 4)) + db_blocks;
+    const int db_blocks = db_last ? ceil_div(out, 32) : 0, lanes = p.splits >= 8 && (size_t)B * (p.dx_ld / 4) < 148 * 256 ? 8 : 1;
+    const int grid = grid_for((size_t)B * (p.dx_ld / 4) * lanes) + db_blocks;
     const int vec = in % 4 == 0 && (reinterpret_cast<uintptr_t>(dx) & (4 * es - 1)) == 0;
     if (prec == P_BF16)
-        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec,
+        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec, lanes,
                  (const CeHeader *)head, db_all, db_blocks);
     else
-        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec,
+        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec, lanes,
                  (const CeHeader *)head, db_all, db_blocks);
     return n + 1;
 }
