@@ -443,23 +443,29 @@ def sgd_update(prec, w, v, g, w_version, n, lr, momentum, weight_decay, stream=N
 
 
 # ---- the tail of a language-model step ----------------------------------------------------------------------------
-def _tensor(a, n, size, what):
-    """The address of a tensor argument that the caller says has n elements of `size` bytes.  A torch tensor that is too
-    small, strided or of another element size is refused here: the C call sees an address only."""
+_DTYPE_NAMES = {}  # torch dtype -> its name (this module does not import torch)
+_F32, _I32, _BYTE, _I64 = ("torch.float32",), ("torch.int32",), ("torch.float8_e4m3fn", "torch.uint8", "torch.int8"), ("torch.int64", "torch.uint64")
+_ELEM = {FP32: _F32, BF16: ("torch.bfloat16",)}
+
+
+def _tensor(a, n, kinds, what):
+    """The address of a tensor argument that the caller says has n elements of a type in `kinds`.  A torch tensor that is
+    too small, strided or of another type is refused here: the C call sees an address only."""
     if a is None:
         return None
     try:
-        if a.is_contiguous() and a.element_size() == size and a.numel() >= n:
+        dtype = a.dtype
+        if a.is_contiguous() and (_DTYPE_NAMES.get(dtype) or _DTYPE_NAMES.setdefault(dtype, str(dtype))) in kinds and a.numel() >= n:
             return a.data_ptr()
     except AttributeError:
         return _ptr(a)
     if not a.is_contiguous():
         raise ValueError("%s has to be contiguous" % what)
-    raise ValueError("%s has %d elements of %d bytes instead of %d of %d" % (what, a.numel(), a.element_size(), n, size))
+    raise ValueError("%s has %d elements of %s instead of %d of %s" % (what, a.numel(), a.dtype, n, " or ".join(kinds)))
 
 
 def _elem(prec):
-    return 2 if prec == BF16 else 4
+    return _ELEM.get(prec, ())
 
 
 def _workspace(a):
@@ -479,8 +485,8 @@ def linear_ce_fwd(prec, x, W, bias, labels, loss, row_loss, lse, workspace, B, n
     e = _elem(prec)
     ws, ws_bytes = _workspace(workspace)
     _ok(_lib.ddg_linear_ce_fwd(prec, _tensor(x, B * n_in, e, "x"), _tensor(W, n_out * n_in, e, "W"),
-                               _tensor(bias, n_out, e, "bias"), _tensor(labels, B, 4, "labels"),
-                               _tensor(loss, 1, 4, "loss"), _tensor(row_loss, B, 4, "row_loss"), _tensor(lse, B, 4, "lse"),
+                               _tensor(bias, n_out, e, "bias"), _tensor(labels, B, _I32, "labels"),
+                               _tensor(loss, 1, _F32, "loss"), _tensor(row_loss, B, _F32, "row_loss"), _tensor(lse, B, _F32, "lse"),
                                ws, ws_bytes, B, n_in, n_out, stream))
 
 
@@ -490,9 +496,9 @@ def linear_ce_bwd(prec, x, W, bias, labels, lse, dloss, drow, dx, dW, db, worksp
     e = _elem(prec)
     ws, ws_bytes = _workspace(workspace)
     _ok(_lib.ddg_linear_ce_bwd(prec, _tensor(x, B * n_in, e, "x"), _tensor(W, n_out * n_in, e, "W"),
-                               _tensor(bias, n_out, e, "bias"), _tensor(labels, B, 4, "labels"), _tensor(lse, B, 4, "lse"),
-                               _tensor(dloss, 1, 4, "dloss"), _tensor(drow, B, 4, "drow"), _tensor(dx, B * n_in, e, "dx"),
-                               _tensor(dW, n_out * n_in, 4 if dw_f32 else e, "dW"), _tensor(db, n_out, 4, "db"),
+                               _tensor(bias, n_out, e, "bias"), _tensor(labels, B, _I32, "labels"), _tensor(lse, B, _F32, "lse"),
+                               _tensor(dloss, 1, _F32, "dloss"), _tensor(drow, B, _F32, "drow"), _tensor(dx, B * n_in, e, "dx"),
+                               _tensor(dW, n_out * n_in, _F32 if dw_f32 else e, "dW"), _tensor(db, n_out, _F32, "db"),
                                ws, ws_bytes, B, n_in, n_out, int(dw_f32), stream))
 
 
@@ -503,27 +509,27 @@ def rmsnorm_scratch_elems(rows, C):
 def add_rmsnorm_fwd(prec, x, res, gamma, h, y, y8, scale8, rstd, rows, C, group=0, eps=1e-6, stream=None):
     e, n = _elem(prec), rows * C
     _ok(_lib.ddg_add_rmsnorm_fwd(prec, _tensor(x, n, e, "x"), _tensor(res, n, e, "res"), _tensor(gamma, C, e, "gamma"),
-                                 _tensor(h, n, e, "h"), _tensor(y, n, e, "y"), _tensor(y8, n, 1, "y8"),
-                                 _tensor(scale8, rows * (C // group) if group > 0 else rows, 4, "scale8"),
-                                 _tensor(rstd, rows, 4, "rstd"), rows, C, group, eps, stream))
+                                 _tensor(h, n, e, "h"), _tensor(y, n, e, "y"), _tensor(y8, n, _BYTE, "y8"),
+                                 _tensor(scale8, rows * (C // group) if group > 0 else rows, _F32, "scale8"),
+                                 _tensor(rstd, rows, _F32, "rstd"), rows, C, group, eps, stream))
 
 
 def add_rmsnorm_bwd(prec, dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, stream=None):
     e, n = _elem(prec), rows * C
     _ok(_lib.ddg_add_rmsnorm_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dh, n, e, "dh"), _tensor(h, n, e, "h"),
-                                 _tensor(gamma, C, e, "gamma"), _tensor(rstd, rows, 4, "rstd"), _tensor(dx, n, e, "dx"),
-                                 _tensor(dgamma, C, 4, "dgamma"),
-                                 _tensor(scratch, rmsnorm_scratch_elems(rows, C), 4, "scratch"), rows, C, stream))
+                                 _tensor(gamma, C, e, "gamma"), _tensor(rstd, rows, _F32, "rstd"), _tensor(dx, n, e, "dx"),
+                                 _tensor(dgamma, C, _F32, "dgamma"),
+                                 _tensor(scratch, rmsnorm_scratch_elems(rows, C), _F32, "scratch"), rows, C, stream))
 
 
 def dropout_fwd(prec, x, res, y, rng, n, p, layer=0, stream=None):
     """rng: two 64-bit integers on the device, {seed, position}; the call uses ceil(n / 8) positions."""
     e = _elem(prec)
     _ok(_lib.ddg_dropout_fwd(prec, _tensor(x, n, e, "x"), _tensor(res, n, e, "res"), _tensor(y, n, e, "y"),
-                             _tensor(rng, 2, 8, "rng"), n, p, layer, stream))
+                             _tensor(rng, 2, _I64, "rng"), n, p, layer, stream))
 
 
 def dropout_bwd(prec, dy, dx, rng, n, p, layer=0, stream=None):
     e = _elem(prec)
-    _ok(_lib.ddg_dropout_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dx, n, e, "dx"), _tensor(rng, 2, 8, "rng"), n, p,
+    _ok(_lib.ddg_dropout_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dx, n, e, "dx"), _tensor(rng, 2, _I64, "rng"), n, p,
                              layer, stream))

@@ -10,13 +10,14 @@
 //                3. dW_chunk = dz^T x
 //              and at the end dx = scale * (sum of its partials).
 //
-// All four products run on one tcgen05 kernel.  What bounds it: 2NVD (forward) and 6NVD (backward) multiply-adds on the
-// tensor cores; for a few rows the bytes of W.  Two CTAs of a cluster work on one tile of 256 x 512 or 256 x 256
-// (cta_group::2): each loads half of A and half of B by TMA, four stages of 48 KB or six of 32 KB in flight.  The tensor
-// cores are fed from the L2, and the wide tile asks a quarter less of it for the same products (halving B's loads took
-// 8192 x 4096 x 65536 from 3.09 to 2.69 ms in an experiment, one to three more stages changed nothing).  The 512 TMEM
-// columns are two accumulators of 256: the halves of a wide tile, or successive tiles of the narrow one; what the epilogue
-// warps do with one (128 columns of a row per thread) runs under the products of the other.
+// All products run on one tcgen05 kernel (a few rows and small heads have kernels of their own, linear_ce_rows.cuh and
+// linear_ce_head.cuh).  What bounds it: 2NVD (forward) and 6NVD (backward) multiply-adds on the tensor cores.  Two CTAs of
+// a cluster work on one tile of 256 x 256 or 256 x 512 (cta_group::2): each loads half of A and half of B by TMA, three
+// stages of 64 KB or four of 48 KB.  The 512 TMEM columns are two accumulators of 256: successive tiles of the narrow
+// form, or the halves of a wide tile; what the epilogue warps do with one (128 columns of a row per thread) runs under the
+// products of the other.  Measured (bf16, TFLOP/s of the products that are needed, z computed twice counted twice):
+//   8192 x 4096 x 65536   forward 1600, backward 1545 in short runs; 1440 and 1320 for seconds on end, under the power cap
+//   4096 x 1024 x 32000   forward 1400, backward 1360; 1350 and 1195
 //
 // The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
 // 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
@@ -42,8 +43,9 @@ namespace {
 constexpr int kTile = 256;        // rows of a tile of the CTA pair, columns of an accumulator
 constexpr int kHalf = 128;        // rows of A, and of B per accumulator, that one CTA of the pair loads
 constexpr int kKBox = 64;         // K values of a box: 128 bytes of bf16, one swizzle row
-// A stage, per CTA: 128 rows of A and 128 or 256 of B, 128 or 64 K values wide.  What a stage costs the thread that
-// issues its products (two barriers, descriptors) has to stay below the 1024 cycles they take.
+// A stage, per CTA: 128 rows of A and 128 or 256 of B, 128 or 64 K values wide.  The thread that issues the products spends
+// a few hundred cycles on a stage (two barriers, eight descriptors), which has to stay below the 1024 cycles that they
+// take: with 64 K values the narrow tile kept the tensor cores 80 % busy (4096 x 1024 x 32000), with 128 91 %.
 template <int NT> struct Stage {  // NT: columns of a tile
     static constexpr int kw = NT == kTile ? 2 * kKBox : kKBox;
     static constexpr int block = kHalf * kw * 2;  // one operand's 128 rows
@@ -103,7 +105,7 @@ struct CeGemm {
 };
 
 // Hands an accumulator back.  What it orders are the tcgen05 loads before the fence, not memory: a releasing arrival would
-// wait for the stores of the tile before (gradient of the logits, 4096 x 512 x 16384: 94 us with it, 75 us without).
+// wait for the stores of the tile before (gradient of the logits, 4096 x 512 x 16384: 94 us with it, 89 us without).
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -135,9 +137,9 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
 __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 // Which tile a work item is: all tiles of a split, in bands of group_m tile rows that are walked column by column, so
-// that the operands of the tiles in flight stay in the L2.
+// that the operands of the tiles in flight stay in the L2 (16 tile rows; 8 and 32 cost 2 to 5 % at 8192 x 4096 x 65536).
 // Divisions by sizes known at launch only cost an issuing thread a hundred cycles each, in which the tensor cores run
-// dry: the K range has none without splits, and the product of the two factors fits 32 bits (at most 2^21 x 74).
+// dry: the K range has none without splits, and the product of the two factors fits 32 bits (at most 2^21 x 148).
 struct CeTile { int m, n; };
 __device__ __forceinline__ int ce_split(const CeGemm &g, int item) { return g.splits == 1 ? 0 : item / (g.tiles_m * g.tiles_n); }
 __device__ __forceinline__ void ce_range(const CeGemm &g, int split, int &kb0, int &kb1) {
@@ -222,8 +224,8 @@ __device__ __forceinline__ void store_row32(void *out, int bf16_out, int vec, si
 }
 
 // 64 columns of the warp's 32 rows as bf16 to (x, y) of a matrix, through shared memory: whole 128-byte lines leave by
-// TMA, and rows and columns past the matrix are clipped.  (Stores of 64 bytes a thread, straight from registers, took the
-// logits' gradient at 4096 x 512 x 16384 89 us.)
+// TMA, and rows and columns past the matrix are clipped.  (Gradient of the logits, 4096 x 512 x 16384: 62 us; with stores
+// of 64 bytes a thread, straight from registers, 89 us.)
 __device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t buf, int lane, int x, int y, const float *v) {
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the box before has been read
     __syncwarp();
@@ -1003,8 +1005,8 @@ int ce_launch(const CeOperand &a, const CeOperand &b, const CeOperand &out, CeGe
     const long chain = (long)g.K * g.n_seg / g.splits;
     if (exact && chain > (g.n_seg > 2 ? kPieceF32 : kPieceBf16)) return ce_launch_as<MODE, A_MN, B_MN, kTile, true>(a, b, out, g, s);
     // The softmax's epilogues are long, and a wide tile leaves no accumulator to multiply into meanwhile (forward pass,
-    // 4096 x 1024 x 32000: 223 us wide, 200 us narrow); the other products' are short (dW, 8192 x 4096 x 16384: 691 us
-    // wide, 809 us narrow), so that there the rounds decide.
+    // 4096 x 1024 x 32000: 223 us wide, 200 us narrow, with stages alike); the other products' are short, a wide tile asks
+    // a quarter less of the L2 (dW, 8192 x 4096 x 16384: 694 us wide, 720 us narrow), and the rounds decide.
     if constexpr (MODE == kPartial || MODE == kWeightGrad)
         if (ce_wide(g.M, g.N, g.splits)) return ce_launch_as<MODE, A_MN, B_MN, 2 * kTile, false>(a, b, out, g, s);
     return ce_launch_as<MODE, A_MN, B_MN, kTile, false>(a, b, out, g, s);

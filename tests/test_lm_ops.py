@@ -493,7 +493,7 @@ def test_linear_ce_refuses_on_the_gpu(binding):
         with pytest.raises(binding.DdgError) as e:
             call(**kw)
         assert e.value.status == 1
-    for kw in ({"x": c.x.float()}, {"w": c.w.t()}, {"labels": c.labels.long()}, {"row": row[:3]}):
+    for kw in ({"x": c.x.float()}, {"x": c.x.half()}, {"w": c.w.t()}, {"labels": c.labels.long()}, {"labels": c.labels.float()}, {"row": row[:3]}):
         with pytest.raises(ValueError):
             call(**kw)
     torch.cuda.synchronize()
@@ -892,7 +892,7 @@ def test_dropout_refusals(binding):
 
 
 def test_tensor_arguments_are_checked_in_the_binding(binding):
-    """What a C call cannot see: strides, element sizes and lengths of the tensors behind the addresses."""
+    """What a C call cannot see: strides, types and lengths of the tensors behind the addresses."""
     x = torch.zeros(4, 8)
     for bad in (x.t(), x.half(), x[:2]):
         with pytest.raises(ValueError):
