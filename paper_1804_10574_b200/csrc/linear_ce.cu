@@ -16,8 +16,8 @@
 // stages of 64 KB or four of 48 KB.  The 512 TMEM columns are two accumulators of 256: successive tiles of the narrow
 // form, or the halves of a wide tile; what the epilogue warps do with one (128 columns of a row per thread) runs under the
 // products of the other.  Measured (bf16, TFLOP/s of the products that are needed, z computed twice counted twice):
-//   8192 x 4096 x 65536   forward 1600, backward 1545 in short runs; 1440 and 1320 for seconds on end, under the power cap
-//   4096 x 1024 x 32000   forward 1400, backward 1360; 1350 and 1195
+//   8192 x 4096 x 65536   forward 1660, backward 1580 in short runs; 1460 and 1360 for seconds on end, under the power cap
+//   4096 x 1024 x 32000   forward 1450, backward 1400; 1390 and 1240
 //
 // The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
 // 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
@@ -83,6 +83,7 @@ struct CeGemm {
     int b_r0, b_k0;           // coordinates of B's first row and of its first K value
     int tiles_m, tiles_n, splits, group_m;
     int width;                // columns of a tile: at most NT, a multiple of 64, alike for all tiles of a launch
+    int b_bytes;              // of B in a stage, per accumulator and CTA
     int piece;                // K blocks of a chain (with PROMOTE)
     int tail;                 // steps of 16 in a segment's last K block
     CeHeader *head;
@@ -422,7 +423,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 int seg = kb0 == 0 ? 0 : kb0 / g.kblocks, kb = kb0 - seg * g.kblocks;
                 for (int i = kb0; i < kb1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 51)) { ok = false; break; }
-                    if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * kStageBytes);
+                    if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + kHalves * g.b_bytes));
                     const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
                     const uint32_t a = base + s * kStageBytes;
                     const int k = kb * kw;
@@ -438,6 +439,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         const int nn = n0 + h * kTile;
 #pragma unroll
                         for (int j = 0; j < (B_MN ? 2 : kw / kKBox); ++j) {
+                            if (B_MN && j * kKBox >= g.width / 2) break;
                             if (B_MN) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, g.b_off[seg] + nn + kKBox * j, g.b_k0 + k);
                             else tma_load_pair(b + j * (kHalf * kKBox * 2), &map_b, bar, g.b_off[seg] + k + kKBox * j, g.b_r0 + nn);
                         }
@@ -859,11 +861,20 @@ constexpr size_t kDzBytes = (size_t)256 << 20;
 constexpr int kPairs = 74;  // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
 constexpr double kWideCost = 0.97;  // time of a product in a 256 x 512 tile against a 256 x 256 one
 
-// Columns of the tiles that cover N columns: as many tiles as it takes at `nt` columns, alike (520 columns: three of 192
-// rather than 256, 256 and 8, which loads as much of A as the others).
-int ce_width(int N, int nt) {
-    const int tiles = (N + nt - 1) / nt;
-    return nt == kTile ? ((N + tiles - 1) / tiles + kKBox - 1) / kKBox * kKBox : nt;
+// Columns of the tiles of M x N (times splits): at most 256, as many tiles as that takes, alike (520 columns: three of 192
+// rather than 256, 256 and 8).  Where that leaves CTA pairs without work, narrower ones: half of a tile's loads, A's, stay.
+// (105 x 1048 x 5130: forward 17.9 -> 17.0 us, backward 45.6 -> 39.5 us.)
+int ce_width(int M, int N, int splits) {
+    const long rows = (long)((M + kTile - 1) / kTile) * splits;
+    int best = kTile;
+    double least = 1e30;
+    for (int most = kTile; most >= kKBox; most /= 2) {
+        const int tiles = (N + most - 1) / most, width = ((N + tiles - 1) / tiles + kKBox - 1) / kKBox * kKBox;
+        const double t = (double)((rows * tiles + kPairs - 1) / kPairs) * (0.5 + 0.5 * width / kTile);
+        if (t < 0.98 * least) { least = t; best = width; }
+        if (rows * tiles >= kPairs) break;
+    }
+    return best;
 }
 double ce_rounds(int M, int N, int nt, int splits);
 
@@ -908,7 +919,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.rows = prec == P_BF16 && B <= kRowsMax;
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = p.rows ? rows_grid(out, kRowsGridMax) : 2 * ((out + kTile - 1) / kTile);
+    p.n_part = p.rows ? rows_grid(out, kRowsGridMax) : 2 * ((out + ce_width(B, out, 1) - 1) / ce_width(B, out, 1));
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -964,15 +975,17 @@ struct CeOperand { const void *ptr; int rows, cols; };
 template <int MODE, bool A_MN, bool B_MN, int NT, bool PROMOTE>
 int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, CeGemm &g, const Launch &s) {
     constexpr int kw = Stage<NT>::kw;
-    CUtensorMap ma, mb, mo{};
-    if (out.ptr && !ce_map(out.ptr, out.rows, out.cols, out.cols, 32, &mo)) return -1;
-    if (!ce_map(a.ptr, a.rows, a.cols, a.cols, A_MN ? kw : kHalf, &ma) || !ce_map(b.ptr, b.rows, b.cols, b.cols, B_MN ? kw : kHalf, &mb)) return -1;
     g.kblocks = (g.K + kw - 1) / kw;
     g.tail = (g.K - (g.kblocks - 1) * kw + 15) / 16;
     g.piece = (g.n_seg > 2 ? kPieceF32 : kPieceBf16) / kw;
-    g.tiles_n = (g.N + NT - 1) / NT;
-    g.width = ce_width(g.N, NT);
     g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
+    g.width = NT == kTile ? ce_width(g.M, g.N, g.splits) : NT;
+    g.tiles_n = (g.N + g.width - 1) / g.width;
+    const int b_rows = NT == kTile ? g.width / 2 : kHalf;  // per CTA and accumulator
+    g.b_bytes = (B_MN ? (b_rows + kKBox - 1) / kKBox * kKBox : b_rows) * kw * 2;
+    CUtensorMap ma, mb, mo{};
+    if (out.ptr && !ce_map(out.ptr, out.rows, out.cols, out.cols, 32, &mo)) return -1;
+    if (!ce_map(a.ptr, a.rows, a.cols, a.cols, A_MN ? kw : kHalf, &ma) || !ce_map(b.ptr, b.rows, b.cols, b.cols, B_MN ? kw : b_rows, &mb)) return -1;
     const long items = (long)g.tiles_m * g.tiles_n * g.splits;
     if (items > 0x7fffffff) return -1;
     static thread_local int ready_dev = -1;  // the attribute belongs to a device
@@ -989,8 +1002,9 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
 
 // Rounds of the GPU's CTA pairs that the tiles (times splits) take, in units of one 256 x 256 tile of the whole K.
 double ce_rounds(int M, int N, int nt, int splits) {
-    const long items = (long)((M + kTile - 1) / kTile) * ((N + nt - 1) / nt) * splits;
-    return (double)((items + kPairs - 1) / kPairs) * ce_width(N, nt) / kTile * (nt > kTile ? kWideCost : 1.0) / splits;
+    const int width = nt == kTile ? ce_width(M, N, splits) : nt;
+    const long items = (long)((M + kTile - 1) / kTile) * ((N + width - 1) / width) * splits;
+    return (double)((items + kPairs - 1) / kPairs) * (nt == kTile ? 0.5 + 0.5 * width / kTile : 2 * kWideCost) / splits;
 }
 bool ce_wide(int M, int N, int splits) {
     return N > kTile && ce_rounds(M, N, 2 * kTile, splits) <= ce_rounds(M, N, kTile, splits);
