@@ -943,8 +943,10 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
         // costs a write and a read of its partial sums.  Seconds by 1.4 PFLOP/s and 6 TB/s.
         const int kb = (int)std::min<long>(p.chunk, up(out, kKBox)) / kKBox * (prec == P_F32 ? 6 : 1);
         double best = 1e30;
-        const int tiles = p.tiles_m * ((in + kTile - 1) / kTile), most = std::min(2 * kPairs / tiles, kb / 8);  // two rounds of pairs
-        for (int n = 1; n <= std::max(1, most); ++n) {
+        const int tiles = p.tiles_m * ((in + kTile - 1) / kTile), most = std::max(1, std::min(2 * kPairs / tiles, kb / 8));
+        for (int i = 1; i <= 10; ++i) {  // 1 to 8, and one or two rounds of pairs
+            const int n = std::min(most, i <= 8 ? i : (i - 8) * kPairs / tiles);
+            if (n < 1) continue;
             const double rounds = prec == P_F32 ? ce_rounds(B, in, kTile, n) : std::min(ce_rounds(B, in, kTile, n), in > kTile ? ce_rounds(B, in, 2 * kTile, n) : 1e30);
             const double t = rounds * 2.0 * kTile * kTile * kKBox * kb * kPairs / 1.4e15 + (n > 1 ? 2e-6 + 8.0 * n * B * p.dx_ld / 6e12 : 0.0);
             if (t < best) { best = t; p.splits = n; }
