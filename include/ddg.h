@@ -415,7 +415,7 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
                              const float *lse, const float *dloss, const float *drow, void *dx, void *dW, float *db,
                              void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32, void *stream);
 
-/* Root-mean-square norm of rows of C <= 16384 values, with the residual's addition:
+/* Root-mean-square norm of (at most 2^30) rows of C <= 16384 values, with the residual's addition:
  *   h = x + res;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd gamma;
  *   y8 = e4m3(y / scale8), one scale per row (group = 0: scale8 [rows]) or per 128 neighbouring values of a row (group =
  *   128, C a multiple of 128: scale8 [rows][C / 128]); scale8 = max |y| / 448, or 1 where that is zero.

@@ -106,14 +106,14 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
     return done(launch_linear_ce_bwd(precision, x, W, bias, labels, lse, dloss, drow, dx, dW, db, workspace, B, in, out, dw_f32, (cudaStream_t)stream));
 }
 
-size_t ddg_rmsnorm_scratch_elems(int rows, int C) { return rows >= 1 && C >= 1 && C <= kRmsMaxC ? rmsnorm_scratch_elems(rows, C) : 0; }
+size_t ddg_rmsnorm_scratch_elems(int rows, int C) { return rows >= 1 && rows <= kRmsMaxRows && C >= 1 && C <= kRmsMaxC ? rmsnorm_scratch_elems(rows, C) : 0; }
 
 ddg_status ddg_add_rmsnorm_fwd(int precision, const void *x, const void *res, const void *gamma, void *h, void *y, void *y8, float *scale8, float *rstd,
                                int rows, int C, int group, float eps, void *stream) {
     if (bad_prec(precision) || !x || !gamma || (!y && !y8) || (y8 == nullptr) != (scale8 == nullptr) || (res && !h)) return DDG_ERR_INVALID_ARG;
     if (!(eps >= 0.f) || isinf(eps)) return refuse(DDG_ERR_INVALID_ARG, "add_rmsnorm: eps has to be finite and not negative");
     if (group != 0 && group != 128) return refuse(DDG_ERR_INVALID_ARG, "add_rmsnorm: group has to be 0 (a row) or 128");
-    if (rows < 1 || C < 1 || C > kRmsMaxC) return DDG_ERR_UNSUPPORTED;
+    if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kRmsMaxC) return DDG_ERR_UNSUPPORTED;
     if (y8 && group != 0) {
         if (C % group != 0) return refuse(DDG_ERR_UNSUPPORTED, "add_rmsnorm: C has to be a multiple of the group");
         for (const void *p : {x, res, gamma, (const void *)h, (const void *)y, (const void *)y8})
@@ -127,7 +127,7 @@ ddg_status ddg_add_rmsnorm_fwd(int precision, const void *x, const void *res, co
 ddg_status ddg_add_rmsnorm_bwd(int precision, const void *dy, const void *dh, const void *h, const void *gamma, const float *rstd, void *dx, float *dgamma,
                                float *scratch, int rows, int C, void *stream) {
     if (bad_prec(precision) || !dy || !h || !gamma || !rstd || !dx || !dgamma || !scratch) return DDG_ERR_INVALID_ARG;
-    if (rows < 1 || C < 1 || C > kRmsMaxC) return DDG_ERR_UNSUPPORTED;
+    if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kRmsMaxC) return DDG_ERR_UNSUPPORTED;
     const ddg_status st = ready({dy, dh, h, gamma, rstd, dx, dgamma, scratch});
     if (st != DDG_OK) return st;
     return done(launch_add_rmsnorm_bwd(precision, dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C, (cudaStream_t)stream));

@@ -5,7 +5,8 @@
 //
 // One block of the generator gives eight elements their 16 bits each, so that ten rounds of two 32-bit multiplications are
 // shared by eight values and the kernel stays bound by memory: x, res and y once each.  Eight elements per thread and step
-// are one 16-byte vector of bf16 or two of fp32.
+// are one 16-byte vector of bf16 or two of fp32.  Measured at 33.5 M values: bf16 37 us with a residual (5.5 TB/s), 29 us
+// without (4.7 TB/s, the generator takes two thirds of the issue slots); fp32 61 and 44 us (6.6 and 6.1 TB/s).
 #include <algorithm>
 
 #include "common.cuh"

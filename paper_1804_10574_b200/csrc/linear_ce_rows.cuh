@@ -4,8 +4,8 @@
 // 128 rows of an MMA (vocabulary entries, or in the product for dx the columns of W) and the rows of x are its 16, 32 or 64
 // columns; the accumulator has a vocabulary entry per lane and a row of x per column.  Every CTA works alone
 // (cta_group::1) on a stretch of the vocabulary cut at multiples of 32 entries, so that all SMs read the same amount, with
-// 160 KB and more of W in flight.  (Against the 256 x 256 tiles of the general kernel, one row, 65536 x 2048:
-// 85 -> 49 us.)
+// 128 KB and more of W in flight.  Measured, one row, 65536 x 2048 (268 MB): z 48 us (5.6 TB/s), dx 45 us (6.0 TB/s); the
+// general kernel's 256 x 256 tiles take 85 us.  64 rows: z 58 us (their own loads are half as many bytes as W's).
 //
 //   kLse      per lane the running maximum and sum of every row of x over the CTA's entries, joined over the CTA at
 //             the end: one (maximum, sum) per CTA and row of x

