@@ -10,8 +10,8 @@
 //                3. dW_chunk = dz^T x
 //              and at the end dx = scale * (sum of its partials).
 //
-// All products run on one tcgen05 kernel (a few rows and small heads have kernels of their own, linear_ce_rows.cuh and
-// linear_ce_head.cuh).  What bounds it: 2NVD (forward) and 6NVD (backward) multiply-adds on the tensor cores.  Two CTAs of
+// All products run on one tcgen05 kernel (a few rows and small heads have kernels of their own, linear_ce_rows.cuh,
+// linear_ce_rows32.cuh and linear_ce_head.cuh).  What bounds it: 2NVD (forward) and 6NVD (backward) multiply-adds on the tensor cores.  Two CTAs of
 // a cluster work on one tile of 256 x 256 or 256 x 512 (cta_group::2): each loads half of A and half of B by TMA, three
 // stages of 64 KB or four of 48 KB.  The 512 TMEM columns are two accumulators of 256: successive tiles of the narrow
 // form, or the halves of a wide tile; what the epilogue warps do with one (128 columns of a row per thread) runs under the
@@ -616,6 +616,8 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
 #include "linear_ce_head.cuh"
 
+#include "linear_ce_rows32.cuh"
+
 // ---- joining the forward pass ----------------------------------------------------------------------------------------
 // rows rows per block of 512 threads, the 512 / rows threads of a row share its pieces, eight loads in flight each.  The mean is taken by the block
 // that finishes last, over the blocks' sums in index order.
@@ -883,13 +885,13 @@ struct CePlan {
     int dz_planes, chunk;    // terms of dz, columns of a chunk
     int tiles_m, n_part;
     int splits, dx_ld;
-    bool rows;               // a few rows: the kernels of linear_ce_rows.cuh
+    bool rows, rows32;       // a few rows: the kernels of linear_ce_rows.cuh, of linear_ce_rows32.cuh
     bool pack_x, pack_w;     // backward: x always, with the rows that do not count as zeros
     size_t part, zlab, sums, x, w, dz, db, dx, bytes;
 };
 
 // Few rows: CTAs of the forward pass and of dz, at least one unit of the vocabulary each.
-constexpr int kRowsGridMax = 160;
+constexpr int kRowsGridMax = 160, kR32PerSm = 2;
 int rows_grid(int out, int sms) { return std::min(std::min(sms, kRowsGridMax), (out + kRowsUnit - 1) / kRowsUnit); }
 // Few rows, dx: splits of the vocabulary, so that the tiles of 128 columns fill the SMs.  Seconds by the bytes of W and of
 // the partial sums at 6 TB/s.
@@ -913,13 +915,15 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     // rows, 32000 entries: 210 us at 1000 columns, 166 us at 1024); the copy costs the bytes of W twice and is paid for
     // by about 2000 rows (2001 x 1000 x 50021: 179 us without, about as much with it).
     p.pack_w = prec == P_F32 || in % 8 != 0 || (in % 16 != 0 && B >= 2048);
-    p.pack_x = p.pack_w || backward;
+    p.rows32 = r32_fits(prec, B, in);
+    if (p.rows32) p.pack_w = false;
+    p.pack_x = p.pack_w || (backward && !p.rows32);
     // an fp32 dW of bf16 operands gets 16 bits of dz (two terms), as the fully connected layer's loss gradient does; a bf16
     // dW or dx is rounded to 8 bits itself and takes dz rounded once to bf16
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.rows = prec == P_BF16 && B <= kRowsMax;
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = p.rows ? rows_grid(out, kRowsGridMax) : 2 * ((out + ce_width(B, out, 1) - 1) / ce_width(B, out, 1));
+    p.n_part = p.rows || p.rows32 ? kRowsGridMax * (p.rows32 ? kR32PerSm : 1) : 2 * ((out + ce_width(B, out, 1) - 1) / ce_width(B, out, 1));
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -929,7 +933,13 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     }
     if (p.pack_x) p.x = take((size_t)B * p.planes * p.plane * 2);
     if (p.pack_w) p.w = take((size_t)out * p.planes * p.plane * 2);
-    if (backward && p.rows) {
+    if (backward && p.rows32) {
+        p.chunk = out;
+        p.dx_ld = up(in, 4);
+        p.splits = std::max(1, std::min(4 * kPairs / ((in + kR32Cols - 1) / kR32Cols), out / kR32Chunk));  // two CTAs per SM
+        p.dz = take((size_t)out * r32_nb(B) * 4);
+        p.dx = take((size_t)p.splits * B * p.dx_ld * 4);
+    } else if (backward && p.rows) {
         p.chunk = out;
         p.dx_ld = up(in, 4);
         p.splits = rows_splits(B, in, out, p.dx_ld);
@@ -1058,6 +1068,44 @@ void ce_segments(CeGemm &g, int a_planes, int a_plane, int b_planes, int b_plane
     add(2, 0); add(0, 2); add(1, 1); add(1, 0); add(0, 1); add(0, 0);
 }
 
+template <int MODE, int NB, int VEC> int r32_logits_as(const CeR32Args &g, int grid, const Launch &s) {
+    static thread_local int ready_dev = -1;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(ce_r32_logits_kernel<MODE, NB, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kR32Smem) != cudaSuccess) return -1;
+        ready_dev = dev;
+    }
+    launch_k(ce_r32_logits_kernel<MODE, NB, VEC>, grid, kR32Threads, (size_t)NB * r32_pitch(g.D) * sizeof(float), s, g);
+    return 1;
+}
+template <int MODE> int r32_logits(const CeR32Args &g, int grid, const Launch &s) {
+    const bool vec = g.D % 4 == 0 && (reinterpret_cast<uintptr_t>(g.W) & 15) == 0;
+    switch (r32_nb(g.B)) {
+    case 4: return vec ? r32_logits_as<MODE, 4, 4>(g, grid, s) : r32_logits_as<MODE, 4, 1>(g, grid, s);
+    case 8: return vec ? r32_logits_as<MODE, 8, 4>(g, grid, s) : r32_logits_as<MODE, 8, 1>(g, grid, s);
+    default: return vec ? r32_logits_as<MODE, 16, 4>(g, grid, s) : r32_logits_as<MODE, 16, 1>(g, grid, s);
+    }
+}
+// CTAs of the logits: two per SM where their shared memory allows it, no more than there are groups of four entries
+int r32_grid(int B, int in, int out) {
+    const int per_sm = (size_t)r32_nb(B) * r32_pitch(in) * 4 <= (size_t)kR32Smem / 2 ? kR32PerSm : 1;
+    return std::max(1, std::min(std::min(sm_count(), kRowsGridMax) * per_sm, (out + 4 * kR32Warps - 1) / (4 * kR32Warps)));
+}
+template <int NB> int r32_gradients(const CeR32Args &g, bool dx, const Launch &s) {
+    const int slabs = (g.D + kR32Cols - 1) / kR32Cols;
+    int n = 0;
+    if (dx) {
+        launch_k(ce_r32_dx_kernel<NB>, dim3(slabs, g.splits), kR32Threads, 0, s, g);
+        ++n;
+    }
+    if (g.dW) {
+        launch_k(ce_r32_dw_kernel<NB>, dim3(slabs, std::max(1, std::min(8 * kPairs / slabs, (g.V + kR32Chunk - 1) / kR32Chunk))), kR32Threads, 0, s, g);
+        ++n;
+    }
+    return n;
+}
+
 // Small heads: one launch per direction on the CUDA cores.  The forward pass has eight CTAs: from 17 rows of bf16 each, the
 // general path's two launches are faster (256 x 64 x 100: 13.3 us, 10.5 us; fp32, which the general path has to split,
 // 14.3 us, 18 us).
@@ -1100,6 +1148,18 @@ int pack(int prec, const void *x, void *x_dst, const void *W, void *w_dst, const
     return 1;
 }
 
+int join_dx(int prec, const CePlan &p, uint8_t *base, const int *labels, void *dx, int B, int in, int out, const CeDb &db, int db_blocks, const Launch &s) {
+    const int lanes = p.splits >= 8 && (size_t)B * (p.dx_ld / 4) < 148 * 256 ? 8 : 1, grid = grid_for((size_t)B * (p.dx_ld / 4) * lanes) + db_blocks;
+    const int vec = in % 4 == 0 && (reinterpret_cast<uintptr_t>(dx) & (4 * elem_size(prec) - 1)) == 0;
+    const float *part = (const float *)(base + p.dx);
+    const CeHeader *head = (const CeHeader *)base;
+    if (prec == P_BF16)
+        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, part, p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec, lanes, head, db, db_blocks);
+    else
+        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, part, p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec, lanes, head, db, db_blocks);
+    return 1;
+}
+
 }  // namespace
 
 bool linear_ce_in_place(int prec, int in) { return prec == P_BF16 && in % 8 == 0; }
@@ -1129,7 +1189,13 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
     float *zlab = (float *)(base + p.zlab);
     const CeOperand ox{x, B, cols}, ow{W, out, cols};
     int r, n_part = p.n_part;
-    if (p.rows) {
+    if (p.rows32) {
+        CeR32Args g{};
+        g.x = (const float *)x; g.W = (const float *)W; g.bias = (const float *)bias; g.labels = labels; g.head = head;
+        g.part = part; g.zlab = zlab; g.B = B; g.D = in; g.V = out;
+        n_part = r32_grid(B, in, out);
+        r = r32_logits<kLse>(g, n_part, s);
+    } else if (p.rows) {
         CeRowsArgs g{};
         g.B = B; g.D = in; g.V = out; g.head = head;
         g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.part = part; g.zlab = zlab;
@@ -1162,6 +1228,16 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
     const CePlan p = ce_plan(prec, B, in, out, true, dw_f32 != 0);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
+    if (p.rows32) {
+        CeR32Args g{};
+        g.x = (const float *)x; g.W = (const float *)W; g.bias = (const float *)bias; g.labels = labels; g.head = head;
+        g.lse = lse; g.dloss = dloss; g.drow = drow; g.dz = (float *)(base + p.dz); g.db = db; g.dW = (float *)dW;
+        g.dx_part = (float *)(base + p.dx); g.dx_split = (size_t)B * p.dx_ld; g.B = B; g.D = in; g.V = out; g.ld = p.dx_ld; g.splits = p.splits;
+        const int r = r32_logits<kDz>(g, r32_grid(B, in, out), s);
+        if (r < 0) return r;
+        const int nb = r32_nb(B), k = r + (nb == 4 ? r32_gradients<4>(g, dx, s) : (nb == 8 ? r32_gradients<8>(g, dx, s) : r32_gradients<16>(g, dx, s)));
+        return dx ? k + join_dx(prec, p, base, labels, dx, B, in, out, CeDb{}, 0, s) : k;
+    }
     int n = pack(prec, x, base + p.x, p.pack_w ? W : nullptr, base + p.w, labels, p, B, in, out, head, true, drow == nullptr, dloss, s);
     const void *xp = base + p.x;
     if (p.pack_w) W = base + p.w;
@@ -1260,16 +1336,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         }
     }
     if (!dx || dx_direct) return n;
-    const int db_blocks = db_last ? ceil_div(out, 32) : 0, lanes = p.splits >= 8 && (size_t)B * (p.dx_ld / 4) < 148 * 256 ? 8 : 1;
-    const int grid = grid_for((size_t)B * (p.dx_ld / 4) * lanes) + db_blocks;
-    const int vec = in % 4 == 0 && (reinterpret_cast<uintptr_t>(dx) & (4 * es - 1)) == 0;
-    if (prec == P_BF16)
-        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec, lanes,
-                 (const CeHeader *)head, db_all, db_blocks);
-    else
-        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, (const float *)(base + p.dx), p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec, lanes,
-                 (const CeHeader *)head, db_all, db_blocks);
-    return n + 1;
+    return n + join_dx(prec, p, base, labels, dx, B, in, out, db_all, db_last ? ceil_div(out, 32) : 0, s);
 }
 
 }  // namespace ddg

@@ -130,7 +130,8 @@ class Ce:
 CE_SHAPES = [(1, 8, 1), (1, 64, 100), (3, 5, 7), (128, 64, 100), (130, 72, 257), (257, 264, 513), (300, 521, 1000), (33, 1000, 4099),
              (2, 4096, 300), (511, 16, 255), (64, 2048, 12000),
              (16, 256, 20000), (20, 136, 3001), (65, 128, 640), (2050, 136, 520),
-             (256, 64, 100), (200, 63, 90), (40, 512, 50), (9, 300, 60)]
+             (256, 64, 100), (200, 63, 90), (40, 512, 50), (9, 300, 60),
+             (11, 89, 5000), (4, 1021, 1500), (16, 3100, 600), (16, 3300, 500), (7, 132, 1)]
 
 
 @gpu
@@ -159,7 +160,7 @@ def test_linear_ce_backward(binding, shape, prec):
 
 
 # one of each way a call is worked: a small head, at most 64 rows, more rows
-WAYS = pytest.mark.parametrize("shape", [(140, 64, 300), (45, 136, 3000), (300, 136, 777)], ids=["head", "few_rows", "rows"])
+WAYS = pytest.mark.parametrize("shape", [(140, 64, 300), (45, 136, 3000), (300, 136, 777), (14, 200, 2000)], ids=["head", "few_rows", "rows", "fewest_rows"])
 
 
 @gpu
@@ -200,8 +201,8 @@ def test_linear_ce_backward_in_chunks(binding, prec, D, V):
 def test_linear_ce_rows_that_do_not_count(binding, shape, prec):
     """Labels outside the vocabulary leave a row out, whatever stands in it; without any row the results are zero."""
     c = Ce(*shape, prec, True, seed=9)
-    c.labels[3], c.labels[17], c.labels[c.B - 1], c.labels[20] = -1, c.V, -2 ** 31, 2 ** 31 - 1
-    c.x[3], c.x[17, 5], c.x[c.B - 1, 0], c.x[20] = NAN, INF, -INF, torch.finfo(c.x.dtype).min
+    c.labels[3], c.labels[7], c.labels[c.B - 1], c.labels[10] = -1, c.V, -2 ** 31, 2 ** 31 - 1
+    c.x[3], c.x[7, 5], c.x[c.B - 1, 0], c.x[10] = NAN, INF, -INF, torch.finfo(c.x.dtype).min
     c.reference()
     loss, row, lse = c.fwd(binding)
     counted = (c.labels >= 0) & (c.labels < c.V)
@@ -221,7 +222,7 @@ def test_linear_ce_rows_that_do_not_count(binding, shape, prec):
 
 @gpu
 @PREC
-@pytest.mark.parametrize("rows,width", [(40, 32), (40, 64), (300, 64)], ids=["head", "few_rows", "rows"])
+@pytest.mark.parametrize("rows,width", [(40, 32), (40, 64), (300, 64), (12, 64)], ids=["head", "few_rows", "rows", "fewest_rows"])
 def test_linear_ce_masked_vocabulary(binding, rows, width, prec):
     """A bias of minus infinity or of the type's lowest value takes entries out of the softmax, whole tiles of them too; a
     label among them has infinite loss."""
