@@ -1068,6 +1068,8 @@ void ce_segments(CeGemm &g, int a_planes, int a_plane, int b_planes, int b_plane
     add(2, 0); add(0, 2); add(1, 1); add(1, 0); add(0, 1); add(0, 0);
 }
 
+bool r32_two(int B, int in) { return (size_t)r32_nb(B) * r32_pitch(in) * 4 <= (size_t)kR32Smem / 2; }  // two CTAs fit an SM
+int r32_warps(int B, int in) { return r32_two(B, in) ? 8 : kR32MostWarps; }
 template <int MODE, int NB, int VEC> int r32_logits_as(const CeR32Args &g, int grid, const Launch &s) {
     static thread_local int ready_dev = -1;
     int dev = 0;
@@ -1076,7 +1078,7 @@ template <int MODE, int NB, int VEC> int r32_logits_as(const CeR32Args &g, int g
         if (cudaFuncSetAttribute(ce_r32_logits_kernel<MODE, NB, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kR32Smem) != cudaSuccess) return -1;
         ready_dev = dev;
     }
-    launch_k(ce_r32_logits_kernel<MODE, NB, VEC>, grid, kR32Threads, (size_t)NB * r32_pitch(g.D) * sizeof(float), s, g);
+    launch_k(ce_r32_logits_kernel<MODE, NB, VEC>, grid, 32 * r32_warps(g.B, g.D), (size_t)NB * r32_pitch(g.D) * sizeof(float), s, g);
     return 1;
 }
 template <int MODE> int r32_logits(const CeR32Args &g, int grid, const Launch &s) {
@@ -1089,8 +1091,7 @@ template <int MODE> int r32_logits(const CeR32Args &g, int grid, const Launch &s
 }
 // CTAs of the logits: two per SM where their shared memory allows it, no more than there are groups of four entries
 int r32_grid(int B, int in, int out) {
-    const int per_sm = (size_t)r32_nb(B) * r32_pitch(in) * 4 <= (size_t)kR32Smem / 2 ? kR32PerSm : 1;
-    return std::max(1, std::min(std::min(sm_count(), kRowsGridMax) * per_sm, (out + 4 * kR32Warps - 1) / (4 * kR32Warps)));
+    return std::max(1, std::min(std::min(sm_count(), kRowsGridMax) * (r32_two(B, in) ? kR32PerSm : 1), (out + 31) / 32));
 }
 template <int NB> int r32_gradients(const CeR32Args &g, bool dx, const Launch &s) {
     const int slabs = (g.D + kR32Cols - 1) / kR32Cols;

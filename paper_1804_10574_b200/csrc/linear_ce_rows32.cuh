@@ -9,7 +9,8 @@
 //   dx         a thread has four columns of W and all rows of x; splits of the vocabulary, joined by ce_dx_kernel
 //   dW         a thread has four columns of x for all rows in registers and walks entries
 // Any width, no alignment: lanes take neighbouring columns, or float4s of them where rows of W allow it.
-constexpr int kR32Max = 16, kR32Threads = 256, kR32Warps = 8;
+constexpr int kR32Max = 16, kR32Threads = 256;
+constexpr int kR32MostWarps = 16;  // of the logits: 16 where x leaves room for one CTA on an SM, else 8
 constexpr int kR32Smem = 200 * 1024;
 constexpr int kR32Cols = 256;     // columns of a CTA of dx and dW: 64 threads of four, four threads along the entries
 constexpr int kR32Chunk = 64;     // entries of dz that a CTA of dx and dW has in shared memory at a time
@@ -39,16 +40,16 @@ template <int NB> __device__ __forceinline__ float r32_scale(const CeR32Args &g)
 }
 
 template <int MODE, int NB, int VEC>
-__global__ void __launch_bounds__(kR32Threads) ce_r32_logits_kernel(const CeR32Args g) {
+__global__ void __launch_bounds__(32 * kR32MostWarps) ce_r32_logits_kernel(const CeR32Args g) {
     constexpr int kEntries = NB == 16 ? 4 : 32 / NB, kSets = kEntries * NB / 32;  // entries of a warp at a time; values per lane of them
     extern __shared__ float4 r32_smem[];
-    __shared__ float2 s_part[kR32Warps][NB];
+    __shared__ float2 s_part[kR32MostWarps][NB];
     float *xs = reinterpret_cast<float *>(r32_smem);  // [NB][P]
-    const int P = r32_pitch(g.D), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane % NB;
+    const int P = r32_pitch(g.D), warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31, n = lane % NB;
     pdl_launch();
     pdl_wait();
     if (MODE == kLse && blockIdx.x == 0 && threadIdx.x == 0) g.head->ticket = 0;
-    for (int i = threadIdx.x; i < NB * P; i += kR32Threads) {
+    for (int i = threadIdx.x; i < NB * P; i += blockDim.x) {
         const int r = i / P, c = i - r * P;
         xs[i] = r < g.B && c < g.D ? g.x[(size_t)r * g.D + c] : 0.f;
     }
@@ -62,8 +63,8 @@ __global__ void __launch_bounds__(kR32Threads) ce_r32_logits_kernel(const CeR32A
         if (blockIdx.x == 0 && threadIdx.x == 0) g.head->scale = scale;
     }
     __syncthreads();
-    const int groups = (g.V + kEntries - 1) / kEntries, walkers = gridDim.x * kR32Warps;
-    for (int group = blockIdx.x * kR32Warps + warp; group < groups; group += walkers) {
+    const int groups = (g.V + kEntries - 1) / kEntries, walkers = gridDim.x * warps;
+    for (int group = blockIdx.x * warps + warp; group < groups; group += walkers) {
         const int v0 = group * kEntries;
         float acc[kEntries * NB];
 #pragma unroll
@@ -124,9 +125,9 @@ __global__ void __launch_bounds__(kR32Threads) ce_r32_logits_kernel(const CeR32A
         __syncthreads();
         if ((int)threadIdx.x < g.B) {
             m = s_part[0][threadIdx.x].x;
-            for (int q = 1; q < kR32Warps; ++q) m = fmaxf(m, s_part[q][threadIdx.x].x);
+            for (int q = 1; q < warps; ++q) m = fmaxf(m, s_part[q][threadIdx.x].x);
             t = 0.f;
-            for (int q = 0; q < kR32Warps; ++q) t += s_part[q][threadIdx.x].y * exp2_approx((s_part[q][threadIdx.x].x - m) * kLog2e);
+            for (int q = 0; q < warps; ++q) t += s_part[q][threadIdx.x].y * exp2_approx((s_part[q][threadIdx.x].x - m) * kLog2e);
             g.part[(size_t)blockIdx.x * g.B + threadIdx.x] = make_float2(m, t);
         }
     }
