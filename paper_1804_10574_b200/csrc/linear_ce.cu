@@ -891,7 +891,7 @@ struct CePlan {
 };
 
 // Few rows: CTAs of the forward pass and of dz, at least one unit of the vocabulary each.
-constexpr int kRowsGridMax = 160, kR32PerSm = 2;
+constexpr int kRowsGridMax = 160, kR32PerSm = 3;
 int rows_grid(int out, int sms) { return std::min(std::min(sms, kRowsGridMax), (out + kRowsUnit - 1) / kRowsUnit); }
 // Few rows, dx: splits of the vocabulary, so that the tiles of 128 columns fill the SMs.  Seconds by the bytes of W and of
 // the partial sums at 6 TB/s.
@@ -936,7 +936,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     if (backward && p.rows32) {
         p.chunk = out;
         p.dx_ld = up(in, 4);
-        p.splits = std::max(1, std::min(4 * kPairs / ((in + kR32Cols - 1) / kR32Cols), out / kR32Chunk));  // two CTAs per SM
+        p.splits = std::max(1, std::min((r32_nb(B) == 16 ? 4 : 8) * kPairs / ((in + kR32Cols - 1) / kR32Cols), out / 64));  // two or four CTAs per SM
         p.dz = take((size_t)out * r32_nb(B) * 4);
         p.dx = take((size_t)p.splits * B * p.dx_ld * 4);
     } else if (backward && p.rows) {
@@ -1068,8 +1068,9 @@ void ce_segments(CeGemm &g, int a_planes, int a_plane, int b_planes, int b_plane
     add(2, 0); add(0, 2); add(1, 1); add(1, 0); add(0, 1); add(0, 0);
 }
 
-bool r32_two(int B, int in) { return (size_t)r32_nb(B) * r32_pitch(in) * 4 <= (size_t)kR32Smem / 2; }  // two CTAs fit an SM
-int r32_warps(int B, int in) { return r32_two(B, in) ? 8 : kR32MostWarps; }
+// CTAs of the logits on an SM: two or three (registers) where x in shared memory leaves room for them
+int r32_per_sm(int B, int in) { return std::max(1, std::min(r32_nb(B) == 16 ? 2 : kR32PerSm, (int)(kR32Smem / ((size_t)r32_nb(B) * r32_pitch(in) * 4)))); }
+int r32_warps(int B, int in) { return r32_per_sm(B, in) > 1 ? 8 : kR32MostWarps; }
 template <int MODE, int NB, int VEC> int r32_logits_as(const CeR32Args &g, int grid, const Launch &s) {
     static thread_local int ready_dev = -1;
     int dev = 0;
@@ -1089,9 +1090,9 @@ template <int MODE> int r32_logits(const CeR32Args &g, int grid, const Launch &s
     default: return vec ? r32_logits_as<MODE, 16, 4>(g, grid, s) : r32_logits_as<MODE, 16, 1>(g, grid, s);
     }
 }
-// CTAs of the logits: two per SM where their shared memory allows it, no more than there are groups of four entries
+// CTAs of the logits: no more than give every warp a group of four entries
 int r32_grid(int B, int in, int out) {
-    return std::max(1, std::min(std::min(sm_count(), kRowsGridMax) * (r32_two(B, in) ? kR32PerSm : 1), (out + 31) / 32));
+    return std::max(1, std::min(std::min(sm_count(), kRowsGridMax) * r32_per_sm(B, in), (out + 31) / 32));
 }
 template <int NB> int r32_gradients(const CeR32Args &g, bool dx, const Launch &s) {
     const int slabs = (g.D + kR32Cols - 1) / kR32Cols;
@@ -1101,7 +1102,7 @@ template <int NB> int r32_gradients(const CeR32Args &g, bool dx, const Launch &s
         ++n;
     }
     if (g.dW) {
-        launch_k(ce_r32_dw_kernel<NB>, dim3(slabs, std::max(1, std::min(8 * kPairs / slabs, (g.V + kR32Chunk - 1) / kR32Chunk))), kR32Threads, 0, s, g);
+        launch_k(ce_r32_dw_kernel<NB>, dim3(slabs, std::max(1, std::min(8 * kPairs / slabs, (g.V + 63) / 64))), kR32Threads, 0, s, g);
         ++n;
     }
     return n;

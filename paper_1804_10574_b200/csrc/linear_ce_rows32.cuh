@@ -8,12 +8,14 @@
 //              keeps that row's running maximum and sum (forward), or writes dz [V][NB] (backward)
 //   dx         a thread has four columns of W and all rows of x; splits of the vocabulary, joined by ce_dx_kernel
 //   dW         a thread has four columns of x for all rows in registers and walks entries
+// Measured, 65536 x 2048 (537 MB), one row: logits 95 us (5.6 TB/s), dx 145 us, dW 91 us; 32000 x 1024, 16 rows: 57 us (LDS
+// and FMA, 53 % of the issue slots), 63 and 50 us.  The general path takes 635 us forward and 1279 us backward for the first.
 // Any width, no alignment: lanes take neighbouring columns, or float4s of them where rows of W allow it.
 constexpr int kR32Max = 16, kR32Threads = 256;
 constexpr int kR32MostWarps = 16;  // of the logits: 16 where x leaves room for one CTA on an SM, else 8
 constexpr int kR32Smem = 200 * 1024;
 constexpr int kR32Cols = 256;     // columns of a CTA of dx and dW: 64 threads of four, four threads along the entries
-constexpr int kR32Chunk = 64;     // entries of dz that a CTA of dx and dW has in shared memory at a time
+constexpr int kR32Chunk = 256;    // entries of dz that a CTA of dx and dW has in shared memory at a time
 
 __host__ __device__ inline int r32_pitch(int D) { return (D + 127) / 128 * 128; }  // whole strides of a warp's float4s
 inline int r32_nb(int B) { return B <= 4 ? 4 : (B <= 8 ? 8 : 16); }
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(kR32Threads) ce_r32_dx_kernel(const CeR32Args 
         __syncthreads();
         for (int i = threadIdx.x; i < n * (NB / 4); i += kR32Threads) s_dz[i / (NB / 4)][i % (NB / 4)] = reinterpret_cast<const float4 *>(g.dz + (size_t)v0 * NB)[i];
         __syncthreads();
-#pragma unroll 4
+#pragma unroll 8
         for (int i = ty; i < n; i += 4) {
             float w[4];
 #pragma unroll
