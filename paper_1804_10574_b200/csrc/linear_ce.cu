@@ -100,7 +100,7 @@ struct CeGemm {
     // kPartial (dx): fp32 sums [splits][M][ld] stored or added to, or, as kFinal, dx itself [M][N] from the product and
     // the sums so far (part_in, nullable).  kWeightGrad: [M][N].
     void *out;
-    int out_kind, out_bf16, out_tma, out_vec, ld;  // out_tma: bf16 that a tensor map can write
+    int out_kind, out_bf16, out_tma, ld;  // out_tma: bf16 that a tensor map can write
     size_t out_split;
     const float *part_in;
 };
@@ -195,35 +195,6 @@ __device__ __forceinline__ void red_add4(float *p, float a, float b, float c, fl
     asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
 }
 
-// 32 values of a row at columns col .. of a [.][n] matrix in the element type
-__device__ __forceinline__ void store_row32(void *out, int bf16_out, int vec, size_t row, int col, int n, const float *v) {
-    const size_t at = row * n + col;
-    if (bf16_out) {
-        bf16 *dst = (bf16 *)out + at;
-        if (vec) {  // n is a multiple of 8
-#pragma unroll
-            for (int j = 0; j < 32; j += 8)
-                if (col + j < n)
-                    *reinterpret_cast<uint4 *>(dst + j) = make_uint4(pack2(v[j], v[j + 1]), pack2(v[j + 2], v[j + 3]), pack2(v[j + 4], v[j + 5]), pack2(v[j + 6], v[j + 7]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (col + j < n) dst[j] = __float2bfloat16_rn(v[j]);
-        }
-    } else {
-        float *dst = (float *)out + at;
-        if (vec) {  // n is a multiple of 4
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-                if (col + j < n) *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (col + j < n) dst[j] = v[j];
-        }
-    }
-}
-
 // 64 columns of the warp's 32 rows as bf16 to (x, y) of a matrix, through shared memory: whole 128-byte lines leave by
 // TMA, and rows and columns past the matrix are clipped.  (Gradient of the logits, 4096 x 512 x 16384: 62 us; with stores
 // of 64 bytes a thread, straight from registers, 89 us.)
@@ -240,6 +211,44 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t buf, 
     if (lane == 0) {
         asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(buf), "r"(x), "r"(y) : "memory");
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+
+// The same for matrices that a tensor map cannot write (rows off 16-byte boundaries, fp32): rows row0 .. of a [rows][n]
+// matrix, columns col .. col + 63 as far as there are; the lanes write neighbouring values of a row.  (7244 x 3955 x 223,
+// forward and backward: 230 us; with a row per lane, two bytes at a time, here and in the copies, 499 us.)
+template <bool BF16>
+__device__ __forceinline__ void store_rows(void *out, uint32_t buf, int lane, int row0, int rows, int col, int n, const float *v) {
+    const int last = min(32, rows - row0);
+#pragma unroll
+    for (int half = 0; half < (BF16 ? 1 : 2); ++half) {  // 128 bytes of a row at a time
+        __syncwarp();  // what stood there has been read
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float *f = v + (BF16 ? 8 * j : 32 * half + 4 * j);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(BF16 ? pack2(f[0], f[1]) : __float_as_uint(f[0])),
+                         "r"(BF16 ? pack2(f[2], f[3]) : __float_as_uint(f[1])), "r"(BF16 ? pack2(f[BF16 ? 4 : 0], f[BF16 ? 5 : 0]) : __float_as_uint(f[2])),
+                         "r"(BF16 ? pack2(f[BF16 ? 6 : 0], f[BF16 ? 7 : 0]) : __float_as_uint(f[3])) : "memory");
+        }
+        __syncwarp();
+        const int c = col + 32 * half + lane;
+#pragma unroll 4
+        for (int r = 0; r < last; ++r) {
+            const size_t at = (size_t)(row0 + r) * n + c;
+            if (BF16) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {  // columns lane and lane + 32
+                    const int e = lane + 32 * k;
+                    uint16_t w;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(buf + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2));
+                    if (c + 32 * k < n) reinterpret_cast<uint16_t *>(out)[at + 32 * k] = w;
+                }
+            } else {
+                float w;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+                if (c < n) reinterpret_cast<float *>(out)[at] = w;
+            }
+        }
     }
 }
 
@@ -334,16 +343,16 @@ __device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *ma
             }
         }
     } else if (r.row - lane < g.M) {
-        if (MODE == kPartial && g.out_kind != kFinal) {
+        if (MODE == kPartial && g.out_kind == kStore) {
+            store_rows<false>((float *)g.out + r.split * g.out_split, buf, lane, r.row - lane, g.M, col, g.ld, v);
+            return;
+        }
+        if (MODE == kPartial && g.out_kind == kAdd) {
             if (live) {
                 float *dst = (float *)g.out + r.split * g.out_split + (size_t)r.row * g.ld + col;
 #pragma unroll
-                for (int j = 0; j < kKBox; j += 4) {
-                    if (col + j < g.ld) {  // ld is a multiple of 4
-                        if (g.out_kind == kAdd) red_add4(dst + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
-                        else *reinterpret_cast<float4 *>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                    }
-                }
+                for (int j = 0; j < kKBox; j += 4)
+                    if (col + j < g.ld) red_add4(dst + j, v[j], v[j + 1], v[j + 2], v[j + 3]);  // ld is a multiple of 4
             }
             return;
         }
@@ -364,12 +373,9 @@ __device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *ma
 #pragma unroll
             for (int j = 0; j < kKBox; ++j) v[j] *= scale;
         }
-        if (g.out_tma) {
-            store_box(map_out, buf, lane, col, r.row - lane, v);
-        } else if (live) {
-            store_row32(g.out, g.out_bf16, g.out_vec, r.row, col, g.N, v);
-            if (col + 32 < g.N) store_row32(g.out, g.out_bf16, g.out_vec, r.row, col + 32, g.N, v + 32);
-        }
+        if (g.out_tma) store_box(map_out, buf, lane, col, r.row - lane, v);
+        else if (g.out_bf16) store_rows<true>(g.out, buf, lane, r.row - lane, g.M, col, g.N, v);
+        else store_rows<false>(g.out, buf, lane, r.row - lane, g.M, col, g.N, v);
     }
 }
 
@@ -733,35 +739,62 @@ __global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, con
     const T *src = (const T *)job.src;
     const int *labels = job.labels;
     bf16 *dst = job.dst;
+    const int first = blockIdx.x - (second ? job_x.blocks : 0);
+    // an infinity or NaN stays in the first term alone (inf - inf would spread NaN into its row's others)
+    auto rest = [](float v) {
+        const float h = bf16_round(v);
+        return isinf(h) || isnan(h) ? 0.f : v - h;
+    };
+    if (cols % (16 / (int)sizeof(T)) != 0 || (reinterpret_cast<uintptr_t>(src) & 15) != 0) {
+        // rows off 16-byte boundaries: a warp per row, two neighbouring columns per lane
+        const int lane = threadIdx.x & 31;
+        for (int row = first * 8 + (threadIdx.x >> 5); row < job.rows; row += job.blocks * 8) {
+            const int y = labels ? labels[row] : 0;
+            const bool live = !labels || (y >= 0 && y < V);
+            const T *from = src + (size_t)row * cols;
+            bf16 *to = dst + (size_t)row * planes * plane;
+#pragma unroll 8
+            for (int c = 2 * lane; c < plane; c += 64) {
+                float a = live && c < cols ? to_f(from[c]) : 0.f, b = live && c + 1 < cols ? to_f(from[c + 1]) : 0.f;
+                for (int p = 0; p < planes; ++p) {
+                    *reinterpret_cast<uint32_t *>(to + (size_t)p * plane + c) = pack2(a, b);
+                    a = rest(a);
+                    b = rest(b);
+                }
+            }
+        }
+        return;
+    }
     // eight columns per step; plane is a multiple of 8
     const size_t total = (size_t)job.rows * (plane / 8), stride = (size_t)job.blocks * 256;
-    const bool vec = cols % (16 / (int)sizeof(T)) == 0 && (reinterpret_cast<uintptr_t>(src) & 15) == 0;
-    for (size_t i = (size_t)(blockIdx.x - (second ? job_x.blocks : 0)) * 256 + threadIdx.x; i < total; i += stride) {
-        const size_t row = i / (plane / 8);
-        const int c = (int)(i - row * (plane / 8)) * 8;
+    const unsigned per_row = plane / 8;
+    for (size_t i = (size_t)first * 256 + threadIdx.x; i < total; i += stride) {
+        const size_t row = total <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
+        const int c = (int)(i - row * per_row) * 8;
         float v[8];
         bool live = true;
         if (labels) { const int y = labels[row]; live = y >= 0 && y < V; }
-        if (live && vec && c + 8 <= cols) {
+        if (live && c < cols) {  // whole vectors: cols is a multiple of their length
             if (sizeof(T) == 2) {
                 load_f<T, 8>(src + row * cols + c, v);
             } else {
                 load_f<T, 4>(src + row * cols + c, reinterpret_cast<float(&)[4]>(v[0]));
-                load_f<T, 4>(src + row * cols + c + 4, reinterpret_cast<float(&)[4]>(v[4]));
+                if (c + 4 < cols) {
+                    load_f<T, 4>(src + row * cols + c + 4, reinterpret_cast<float(&)[4]>(v[4]));
+                } else {
+#pragma unroll
+                    for (int j = 4; j < 8; ++j) v[j] = 0.f;
+                }
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = live && c + j < cols ? to_f(src[row * cols + c + j]) : 0.f;
+            for (int j = 0; j < 8; ++j) v[j] = 0.f;
         }
         for (int p = 0; p < planes; ++p) {
             *reinterpret_cast<uint4 *>(dst + row * planes * plane + (size_t)p * plane + c) =
                 make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                // an infinity or NaN stays in the first term alone (inf - inf would spread NaN into its row's others)
-                const float h = bf16_round(v[j]);
-                v[j] = isinf(h) || isnan(h) ? 0.f : v[j] - h;
-            }
+            for (int j = 0; j < 8; ++j) v[j] = rest(v[j]);
         }
     }
 }
@@ -1255,8 +1288,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         CeGemm g{};
         g.M = cols; g.N = in; g.head = head;
         g.out = (uint8_t *)dW + (size_t)v0 * in * oe; g.out_bf16 = out_bf16;
-        g.out_vec = (in * oe) % 16 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0;
-        g.out_tma = out_bf16 && g.out_vec;
+        g.out_tma = out_bf16 && in % 8 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0;
         const CeOperand o = g.out_tma ? CeOperand{g.out, cols, in} : CeOperand{};
         if (p.rows) {
             g.K = kRowsPitch;
@@ -1321,8 +1353,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
                 g.out = dx; g.out_kind = kFinal; g.labels = labels; g.V = out;
                 g.part_in = v0 > 0 ? (const float *)(base + p.dx) : nullptr;
                 g.out_bf16 = prec == P_BF16;
-                g.out_vec = (in * es) % 16 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15) == 0;
-                g.out_tma = g.out_bf16 && g.out_vec;
+                g.out_tma = g.out_bf16 && in % 8 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15) == 0;
                 if (g.out_tma) o = CeOperand{dx, B, in};
             } else {
                 g.out = base + p.dx; g.out_kind = v0 > 0 ? kAdd : kStore;
