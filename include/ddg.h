@@ -418,7 +418,8 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
 /* Root-mean-square norm of (at most 2^30) rows of C <= 16384 values, with the residual's addition:
  *   h = x + res;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd gamma;
  *   y8 = e4m3(y / scale8), one scale per row (group = 0: scale8 [rows]) or per 128 neighbouring values of a row (group =
- *   128, C a multiple of 128: scale8 [rows][C / 128]); scale8 = max |y| / 448, or 1 where that is zero.
+ *   128, C a multiple of 128: scale8 [rows][C / 128]); scale8 = max |y| / 448, at least 2^-126, or 1
+ *   where max |y| is zero.
  * x, res (nullable), gamma [C], h (nullable without res), y in the precision's element type; y8 one byte per value;
  * scale8, rstd (nullable) [rows] fp32.  One of y and y8 at least is given, y8 with scale8.  y and y8 are taken from the unrounded sum.
  * h and y may be x or res. */

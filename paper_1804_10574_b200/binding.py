@@ -472,6 +472,8 @@ def _workspace(a):
     """(address, bytes) of a workspace tensor."""
     if a is None:
         return None, 0
+    if hasattr(a, "is_contiguous") and not a.is_contiguous():
+        raise ValueError("the workspace has to be contiguous")
     return _ptr(a), a.numel() * a.element_size()
 
 

@@ -356,6 +356,28 @@ def test_linear_ce_gradient_over_the_rows(binding, shape, prec):
 
 
 @gpu
+@pytest.mark.parametrize("shape,prec", [((5, 64, 3000), 0), ((300, 64, 700), 0), ((30, 32, 100), 0), ((300, 65, 700), 1), ((20, 33, 3000), 1)])
+def test_linear_ce_off_16_byte_boundaries(binding, shape, prec):
+    """Tensors that start anywhere, where rows are not read in place: outputs as well."""
+    c = Ce(*shape, prec, True, 0.2, seed=43).reference()
+
+    def off(t):
+        return torch.cat([t.flatten()[:1], t.flatten()])[1:].view(t.shape)
+
+    c.x, c.w, c.bias, c.labels = off(c.x), off(c.w), off(c.bias), off(c.labels)
+    assert c.x.data_ptr() % 16 and c.w.data_ptr() % 16
+    loss, row, lse = c.fwd(binding)
+    within(lse, c.lse, c.e_lse, "lse")
+    within(row, c.row, c.e_row, "row_loss")
+    dx, dw, db = off(torch.full_like(c.x, 7.0)), off(torch.full_like(c.w, 7.0)), off(f32(c.V))
+    ws = torch.empty(binding.linear_ce_workspace_bytes(prec, *shape, True), dtype=torch.uint8, device="cuda")
+    binding.linear_ce_bwd(prec, c.x, c.w, c.bias, c.labels, lse, None, None, dx, dw, db, ws, *shape)
+    within(dx, c.dx, c.e_dx, "dx")
+    within(dw, c.dw, c.e_dw, "dW")
+    within(db, c.db, c.e_db, "db")
+
+
+@gpu
 def test_linear_ce_two_streams_at_once(binding):
     """Calls that run at the same time, each with a workspace of its own, give what they give alone."""
     pairs = [Ce(300, 72, 9000, 1, True, 0.2, seed=31), Ce(20, 136, 30000, 1, True, 0.2, seed=32), Ce(100, 72, 2000, 0, False, 0.0, seed=33)]
@@ -610,6 +632,26 @@ def test_add_rmsnorm_special_rows(binding, prec):
     assert float(rstd[3]) == 0.0 and torch.isnan(y[3, 9]) and not y[3, :9].any()
     for r in (0, 4, 5):
         assert torch.isfinite(y[r].float()).all() and torch.isfinite(q[r].float()).all()
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("gain", [2.0 ** -120, 2.0 ** -130])
+def test_add_rmsnorm_to_8_bits_of_tiny_values(binding, prec, group, gain):
+    """Values whose maximum over 448 is below the smallest normal number: the scale stops at 2^-126, a power of two, so
+    that y / scale is off by the rounding of y alone (2^-150 at least) before it is rounded to e4m3."""
+    rows, C = 5, 256
+    x, res, gamma = rms_inputs(rows, C, prec, 33)
+    gamma.fill_(gain)
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    q, scale = torch.empty(rows, C, dtype=torch.float8_e4m3fn, device="cuda"), f32(rows, C // (group or C))
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, q, scale, None, rows, C, group)
+    _, _, y_ref = rms_reference(x, res, gamma, 1e-6)
+    assert float(y_ref.abs().max()) < 448 * 2.0 ** -126
+    assert (scale == 2.0 ** -126).all()
+    e = rms_rel(C) + 2.0 ** -22
+    within(q.double() * 2.0 ** -126, y_ref, (2.0 ** -4 + 2 * e) * y_ref.abs() + 2.0 ** -10 * 2.0 ** -126 + 2.0 ** -150, "q")
 
 
 @gpu
@@ -890,6 +932,33 @@ def test_dropout_refusals(binding):
     assert fwd(prec=9) == 1 and fwd(x=None) == 1 and fwd(y=None) == 1 and fwd(rng=None) == 1
     assert fwd(p=-0.1) == 1 and fwd(p=1.5) == 1 and fwd(p=NAN) == 1 and fwd(rng=P + 4) == 1 and fwd(n=0) == 3
     assert status(binding.dropout_bwd, 1, None, P, P, 8, 0.1) == 1
+
+
+def test_workspace_has_to_be_contiguous(binding):
+    """Its length is counted from its elements, which an expanded tensor does not have."""
+    x, ws = torch.zeros(4, 8), torch.zeros(1, dtype=torch.uint8).expand(1 << 20)
+    with pytest.raises(ValueError):
+        binding.linear_ce_fwd(0, x, x, None, torch.zeros(4, dtype=torch.int32), torch.zeros(1), None, None, ws, 4, 8, 4)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(2000, 4096), (2000, 512), (40, 4096)], ids=lambda s: "x".join(map(str, s)))
+def test_add_rmsnorm_backward_scratch_at_any_16_byte_boundary(binding, shape):
+    rows, C = shape
+    h, dh, gamma = rms_inputs(rows, C, 1, 91)
+    dy, rstd = randn(rows, C, seed=94, prec=1), f32(rows, fill=0.3)
+    n = binding.rmsnorm_scratch_elems(rows, C)
+    got = []
+    for skip in (0, 4, 1):
+        dx, dgamma = torch.empty_like(h), f32(C)
+        scratch = f32(n + skip)[skip:]
+        binding.add_rmsnorm_bwd(1, dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C)
+        got.append((dx, dgamma))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    # off 16 bytes the sums are split over the threads in another way
+    d, k, r = dy.double(), h.double(), rstd.double()[:, None]
+    bound = 2 * (math.ceil(rows / 148) + 37 + 16 + 3) * 2.0 ** -24 * (d * k * r).abs().sum(0)
+    within(got[2][1], got[0][1].double(), bound, "dgamma")
 
 
 def test_tensor_arguments_are_checked_in_the_binding(binding):
