@@ -21,11 +21,15 @@
 //
 // The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
 // 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
-// cut after 128 steps (16 for fp32 tensors, where it is the product of the leading terms) and the pieces added in
-// registers, rounded to nearest.
+// cut after 128 steps, for fp32 tensors after every block of 128 K values, and the pieces added in registers, rounded to
+// nearest.
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,
-// l h are accumulated, smallest first: what is left out is below 2^-24 of the value.
+// l h are accumulated: what is left out is below 2^-24 of the value.  A block of K values goes through all six, smallest
+// first, before the next block: the five small ones, 2^-8 of the result at most, lose nothing that shows, so that h h's
+// eight steps are the chain (1111 x 520 x 10007: dx 2.1e-7 off 64 bits, the plain form 7.5e-7), and a block's terms are read
+// from memory once and from the L2 after that (214 x 3816 x 16384, forward and backward: 868 -> 806 us against one product
+// after the other over all of K).
 #include <float.h>
 
 #include <algorithm>
@@ -58,7 +62,7 @@ constexpr int kStageRing = 192 * 1024;
 constexpr int kOutBuf = 32 * kKBox * 2;  // an epilogue warp's 32 rows of 64 bf16 values on their way out
 constexpr int kCeSmem = kStageRing + kEpiWarps * kOutBuf + 1024;
 constexpr int kMaxSeg = 6;
-constexpr int kPieceBf16 = 2048, kPieceF32 = 256;  // K values of a chain whose result stays in 32 bits
+constexpr int kPieceBf16 = 2048, kPieceF32 = 256;  // K values (times products) of a chain that need not be cut
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kLse, kDz, kPartial, kWeightGrad };
@@ -84,7 +88,7 @@ struct CeGemm {
     int tiles_m, tiles_n, splits, group_m;
     int width;                // columns of a tile: at most NT, a multiple of 64, alike for all tiles of a launch
     int b_bytes;              // of B in a stage, per accumulator and CTA
-    int piece;                // K blocks of a chain (with PROMOTE)
+    int piece;                // steps of the K range (K blocks times segments) of a chain (with PROMOTE)
     int tail;                 // steps of 16 in a segment's last K block
     CeHeader *head;
     // kLse, kDz
@@ -152,11 +156,9 @@ __device__ __forceinline__ void ce_range(const CeGemm &g, int split, int &kb0, i
         kb1 = (int)((unsigned)(kb * (split + 1)) / (unsigned)g.splits);
     }
 }
-// End of the chain that starts at K block i (with PROMOTE): the terms before the last, h h, are at most 2^-8 of the result, so
-// that what their chain loses does not show and they are one piece; h h is cut every g.piece blocks.
+// End of the chain that starts at step i of the K range (with PROMOTE): chains end where a K block's last product, h h, does.
 __device__ __forceinline__ int ce_piece_end(const CeGemm &g, int i, int kb1) {
-    const int last = (g.n_seg - 1) * g.kblocks;
-    return min(i < last ? last : i + g.piece, kb1);
+    return min(i + g.piece - (int)((unsigned)i % (unsigned)g.piece), kb1);
 }
 __device__ __forceinline__ CeTile ce_tile(const CeGemm &g, int item, int split) {
     unsigned r = (unsigned)(item - split * g.tiles_m * g.tiles_n);
@@ -269,14 +271,30 @@ template <int MODE> __device__ __forceinline__ CeRow ce_row(const CeGemm &g, int
     return r;
 }
 
-// What becomes of 64 columns of the warp's 32 rows: v at columns col .. of row r.row.
+// The bias of a warp's 128 columns, 32 per register and lane; columns past the vocabulary are masked later.
+template <int MODE> __device__ __forceinline__ void ce_bias(const CeGemm &g, int col, int lane, float (&b)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) b[q] = (MODE == kLse || MODE == kDz) && g.bias ? load_bias(g.bias, g.bias_bf16, min(col + 32 * q + lane, g.N - 1)) : 0.f;
+}
+
+// What becomes of 64 columns of the warp's 32 rows: v at columns col .. of row r.row; b0 and b1: the columns' bias, a lane
+// each, which the rows read from shared memory (s_bias, the warp's own).  (4096 x 64 x 18944, forward: 56 us; with the
+// bias read from memory by every row, a column at a time, 83 us; without a bias 51 us.)
 template <int MODE>
-__device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *map_out, uint32_t buf, float *v, CeRow &r, int col, int lane) {
+__device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *map_out, uint32_t buf, float *v, CeRow &r, int col, int lane, float *s_bias, float b0, float b1) {
     const bool live = r.row < g.M;
     if ((MODE == kLse || MODE == kDz) && g.bias) {
-        // every lane reads the same values (one transaction each); columns past the vocabulary are masked below
 #pragma unroll
-        for (int j = 0; j < kKBox; ++j) v[j] += load_bias(g.bias, g.bias_bf16, min(col + j, g.N - 1));
+        for (int q = 0; q < 2; ++q) {
+            __syncwarp();  // what stood there has been read
+            s_bias[lane] = q ? b1 : b0;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 t = *reinterpret_cast<const float4 *>(s_bias + j);
+                v[32 * q + j] += t.x; v[32 * q + j + 1] += t.y; v[32 * q + j + 2] += t.z; v[32 * q + j + 3] += t.w;
+            }
+        }
     }
     if (MODE == kLse) {
         if (col + kKBox > g.N) {
@@ -380,7 +398,7 @@ __device__ __forceinline__ void ce_finish(const CeGemm &g, const CUtensorMap *ma
 }
 
 // A_MN / B_MN: the operand lies with M / N innermost (its rows are K values) instead of K.  NT: columns of a tile.
-// PROMOTE (NT = 256): an accumulator holds at most g.piece K blocks, the epilogue adds the pieces.
+// PROMOTE (NT = 256): an accumulator holds at most g.piece steps, the epilogue adds the pieces.
 template <int MODE, bool A_MN, bool B_MN, int NT, bool PROMOTE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -391,6 +409,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_holder;
     __shared__ int abort_flag;
+    __shared__ float4 s_bias[MODE == kLse || MODE == kDz ? kEpiWarps : 1][8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -426,7 +445,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 int kb0, kb1;
                 ce_range(g, split, kb0, kb1);
                 const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * g.width + (int)rank * (NT == kTile ? g.width / 2 : kHalf);
-                int seg = kb0 == 0 ? 0 : kb0 / g.kblocks, kb = kb0 - seg * g.kblocks;
+                int kb = kb0 == 0 ? 0 : kb0 / g.n_seg, seg = kb0 - kb * g.n_seg;
                 for (int i = kb0; i < kb1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 51)) { ok = false; break; }
                     if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + kHalves * g.b_bytes));
@@ -450,7 +469,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             else tma_load_pair(b + j * (kHalf * kKBox * 2), &map_b, bar, g.b_off[seg] + k + kKBox * j, g.b_r0 + nn);
                         }
                     }
-                    if (++kb == g.kblocks) { kb = 0; ++seg; }
+                    if (++seg == g.n_seg) { seg = 0; ++kb; }
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
@@ -486,7 +505,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 int kb0, kb1;
                 const int split = ce_split(g, item);
                 ce_range(g, split, kb0, kb1);
-                int kb = kb0 == 0 ? 0 : kb0 % g.kblocks;  // within its segment: the last one has g.tail steps of 16
+                const int short_from = (g.kblocks - 1) * g.n_seg;  // the last K block has g.tail steps of 16
                 for (int i0 = kb0; i0 < kb1; u += kHalves) {
                     const int i1 = PROMOTE ? ce_piece_end(g, i0, kb1) : kb1;
                     // the first K block waits for the accumulators, one after the other
@@ -496,17 +515,16 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         const uint32_t acc = (u + h) & 1u;
                         ok = mbar_wait(smem_u32(&acc_empty[acc]), (((u + h) >> 1) & 1u) ^ 1u, wt, 52);
                         tc_fence_after();
-                        if (ok && issuer) multiply(s, h, acc, true, kb == g.kblocks - 1 ? g.tail : kw / 16);
+                        if (ok && issuer) multiply(s, h, acc, true, i0 >= short_from ? g.tail : kw / 16);
                     }
                     if (!ok) break;
                     if (issuer) commit_pair(smem_u32(&empty[s]));
                     if (++s == kStages) { s = 0; ph ^= 1u; }
-                    if (++kb == g.kblocks) kb = 0;
                     for (int i = i0 + 1; i < i1; ++i) {
                         if (!mbar_wait(smem_u32(&full[s]), ph, wt, 53)) { ok = false; break; }
                         tc_fence_after();
                         if (issuer) {
-                            if (kb == g.kblocks - 1) {
+                            if (i >= short_from) {
 #pragma unroll
                                 for (int h = 0; h < kHalves; ++h) multiply(s, h, (u + h) & 1u, false, g.tail);
                             } else {
@@ -516,7 +534,6 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             commit_pair(smem_u32(&empty[s]));
                         }
                         if (++s == kStages) { s = 0; ph ^= 1u; }
-                        if (++kb == g.kblocks) kb = 0;
                     }
                     if (!ok) break;
                     if (issuer) {
@@ -543,12 +560,17 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 pieces = 0;
                 for (int i = kb0; i < kb1; i = ce_piece_end(g, i, kb1)) ++pieces;
             }
+            float *const bias_s = reinterpret_cast<float *>(s_bias[MODE == kLse || MODE == kDz ? warp - 2 : 0]);
             const uint32_t buf = base + kStageRing + (uint32_t)(warp - 2) * kOutBuf;
 #pragma unroll 1
             for (int h = 0; h < kHalves && ok; ++h) {
                 const int first_col = h * kTile + half * kHalf, col0 = t.n * g.width + first_col, live = min(g.width - first_col, g.N - col0);
                 CeRow r;
-                if (!PROMOTE) r = ce_row<MODE>(g, split, row);
+                float b[4];
+                if (!PROMOTE) {  // loaded while the products run
+                    r = ce_row<MODE>(g, split, row);
+                    ce_bias<MODE>(g, col0, lane, b);
+                }
                 float v[PROMOTE ? kHalf : kKBox];
                 if (PROMOTE) {
 #pragma unroll
@@ -577,7 +599,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                                 tc_wait_ld();
                             }
                             if (c == kHalf - kKBox) hand_back();
-                            if (c < live) ce_finish<MODE>(g, &map_out, buf, v, r, col0 + c, lane);
+                            if (c < live) ce_finish<MODE>(g, &map_out, buf, v, r, col0 + c, lane, bias_s, c == 0 ? b[0] : b[2], c == 0 ? b[1] : b[3]);
                         }
                     } else {
 #pragma unroll
@@ -594,9 +616,10 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (!ok) break;
                 if (PROMOTE) {
                     r = ce_row<MODE>(g, split, row);
+                    ce_bias<MODE>(g, col0, lane, b);
 #pragma unroll
                     for (int c = 0; c < kHalf; c += kKBox)
-                        if (c < live) ce_finish<MODE>(g, &map_out, buf, v + c, r, col0 + c, lane);
+                        if (c < live) ce_finish<MODE>(g, &map_out, buf, v + c, r, col0 + c, lane, bias_s, b[c / 32], b[c / 32 + 1]);
                 }
                 if (MODE == kLse && row < g.M) g.part[(size_t)(2 * t.n + half) * g.M + row] = make_float2(r.top, r.sum);
             }
@@ -1022,7 +1045,7 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
     constexpr int kw = Stage<NT>::kw;
     g.kblocks = (g.K + kw - 1) / kw;
     g.tail = (g.K - (g.kblocks - 1) * kw + 15) / 16;
-    g.piece = (g.n_seg > 2 ? kPieceF32 : kPieceBf16) / kw;
+    g.piece = g.n_seg > 2 ? g.n_seg : std::max(1, kPieceBf16 / kw / g.n_seg) * g.n_seg;
     g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
     g.width = NT == kTile ? ce_width(g.M, g.N, g.splits) : NT;
     g.tiles_n = (g.N + g.width - 1) / g.width;
