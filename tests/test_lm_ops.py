@@ -934,6 +934,55 @@ def test_dropout_refusals(binding):
     assert status(binding.dropout_bwd, 1, None, P, P, 8, 0.1) == 1
 
 
+@gpu
+@PREC
+@pytest.mark.parametrize("shape", [(1, 2), (9, 3), (3, 9), (70, 33), (2000, 129), (300, 517), (1500, 1023), (40, 8191), (700, 8189), (20, 12289), (5, 16383)], ids=lambda s: "x".join(map(str, s)))
+def test_add_rmsnorm_of_odd_widths(binding, prec, shape):
+    """Rows that start anywhere: forward, to 8 bits and backward, in buffers between guards and in place."""
+    rows, C = shape
+    x, res, gamma = rms_inputs(rows, C, prec, 101)
+    dh, dy = randn(rows, C, seed=104, prec=prec), randn(rows, C, seed=105, prec=prec)
+    guard = 64
+
+    def guarded(dtype):
+        t = torch.zeros(rows * C + guard, dtype=torch.float32, device="cuda").to(dtype)
+        t[rows * C:] = 3.0
+        return t, t[: rows * C].view(rows, C)
+
+    bufs = [guarded(x.dtype) for _ in range(3)] + [guarded(torch.float8_e4m3fn)]
+    h, y, dx, q = (b[1] for b in bufs)
+    scale, rstd = f32(rows), f32(rows)
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, q, scale, rstd, rows, C)
+    h_ref, rstd_ref, y_ref = rms_reference(x, res, gamma, 1e-6)
+    e = rms_rel(C) + 2.0 ** -21
+    within(h, h_ref, (U[x.dtype] + 2.0 ** -24) * h_ref.abs(), "h")
+    within(rstd, rstd_ref, e * rstd_ref, "rstd")
+    # h itself is off by its sum's rounding, 2^-24 of it
+    within(y, y_ref, (U[x.dtype] + e) * y_ref.abs() + 1e-37, "y")
+    s_ref = y_ref.abs().amax(1) / 448.0
+    within(scale, s_ref, e * s_ref, "scale")
+    within(q.double() * scale.double()[:, None], y_ref, (2.0 ** -4 + 2 * e) * y_ref.abs() + 2.0 ** -10 * s_ref[:, None] * 1.01, "q")
+    dgamma, scratch = f32(C), f32(binding.rmsnorm_scratch_elems(rows, C), fill=NAN)
+    binding.add_rmsnorm_bwd(prec, dy, dh, h, gamma, rstd, dx, dgamma, scratch, rows, C)
+    r, k, g, d = rstd.double()[:, None], h.double(), gamma.double(), dy.double()
+    ref = dh.double() + r * (g * d - k * r * r * (g * d * k).mean(1, keepdim=True))
+    mass = dh.double().abs() + r * (g * d).abs() + (k * r ** 3).abs() * (g * d * k).abs().mean(1, keepdim=True)
+    # at most 32 products per thread, a tree over 1024 threads, then four roundings of every term
+    within(dx, ref, U[x.dtype] * ref.abs() + (32 + 10 + 6) * 2.0 ** -24 * mass, "dx")
+    dg, dg_mass = (d * k * r).sum(0), (d * k * r).abs().sum(0)
+    # at least 144 walkers of at most 888 in the fold, two roundings of a product
+    within(dgamma, dg, (math.ceil(rows / 144) + 888 / 32 + 32 + 3) * 2.0 ** -24 * dg_mass, "dgamma")
+    for t, _ in bufs:
+        assert (t[rows * C:].float() == 3.0).all()
+    a, b = x.clone(), res.clone()
+    binding.add_rmsnorm_fwd(prec, a, b, gamma, b, a, None, None, None, rows, C)
+    assert torch.equal(a, y) and torch.equal(b, h)
+    for j in range(3):
+        t = [dy.clone(), dh.clone(), h.clone()]
+        binding.add_rmsnorm_bwd(prec, t[0], t[1], t[2], gamma, rstd, t[j], dgamma, scratch, rows, C)
+        assert torch.equal(t[j], dx), j
+
+
 def test_workspace_has_to_be_contiguous(binding):
     """Its length is counted from its elements, which an expanded tensor does not have."""
     x, ws = torch.zeros(4, 8), torch.zeros(1, dtype=torch.uint8).expand(1 << 20)
