@@ -415,6 +415,11 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
                              const float *lse, const float *dloss, const float *drow, void *dx, void *dW, float *db,
                              void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32, void *stream);
 
+/* Diagnostics, as ddg_debug_wait_timeout is for a context: the bounded device-side waits of the ddg_linear_ce_* calls
+ * that this thread enqueues from now on give up after `polls` polls (a few hundred nanoseconds each); 0: the default, about
+ * a second.  A kernel that gives up lets its copies and products in flight end before it returns. */
+void ddg_debug_linear_ce_wait_polls(unsigned polls);
+
 /* Root-mean-square norm of (at most 2^30) rows of C <= 16384 values, with the residual's addition:
  *   h = x + res;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd gamma;
  *   y8 = e4m3(y / scale8), one scale per row (group = 0: scale8 [rows]) or per 128 neighbouring values of a row (group =

@@ -36,7 +36,7 @@ EXPORTS = ["ddg_create", "ddg_step", "ddg_step_host", "ddg_set_lr", "ddg_param_c
            "ddg_bn_fwd_partials", "ddg_conv3x3_dgrad_partials", "ddg_bn_bwd_partials", "ddg_conv3x3_fwd_stats_prepared",
            "ddg_piece_times", "ddg_conv3x3_fwd_stats_shared",
            "ddg_step_host_pipelined", "ddg_pipelined_loss", "ddg_conv3x3_dgrad_fused_shared",
-           "ddg_linear_ce_workspace_bytes", "ddg_linear_ce_fwd", "ddg_linear_ce_bwd", "ddg_rmsnorm_scratch_elems",
+           "ddg_linear_ce_workspace_bytes", "ddg_linear_ce_fwd", "ddg_linear_ce_bwd", "ddg_debug_linear_ce_wait_polls", "ddg_rmsnorm_scratch_elems",
            "ddg_add_rmsnorm_fwd", "ddg_add_rmsnorm_bwd", "ddg_dropout_fwd", "ddg_dropout_bwd"]
 
 
@@ -124,6 +124,8 @@ _lib.ddg_linear_ce_workspace_bytes.argtypes = [_i] * 5
 _lib.ddg_linear_ce_workspace_bytes.restype = _sz
 _lib.ddg_linear_ce_fwd.argtypes = [_i] + [_vp] * 8 + [_sz] + [_i] * 3 + [_vp]
 _lib.ddg_linear_ce_bwd.argtypes = [_i] + [_vp] * 11 + [_sz] + [_i] * 4 + [_vp]
+_lib.ddg_debug_linear_ce_wait_polls.argtypes = [ctypes.c_uint]
+_lib.ddg_debug_linear_ce_wait_polls.restype = None
 _lib.ddg_rmsnorm_scratch_elems.argtypes = [_i] * 2
 _lib.ddg_rmsnorm_scratch_elems.restype = _sz
 _lib.ddg_add_rmsnorm_fwd.argtypes = [_i] + [_vp] * 8 + [_i] * 3 + [_f, _vp]
@@ -502,6 +504,12 @@ def linear_ce_bwd(prec, x, W, bias, labels, lse, dloss, drow, dx, dW, db, worksp
                                _tensor(dloss, 1, _F32, "dloss"), _tensor(drow, B, _F32, "drow"), _tensor(dx, B * n_in, e, "dx"),
                                _tensor(dW, n_out * n_in, _F32 if dw_f32 else e, "dW"), _tensor(db, n_out, _F32, "db"),
                                ws, ws_bytes, B, n_in, n_out, int(dw_f32), stream))
+
+
+def debug_linear_ce_wait_polls(polls):
+    """Diagnostics: the device-side waits of the linear_ce calls that this thread enqueues from now on give up after
+    `polls` polls; 0: the default."""
+    _lib.ddg_debug_linear_ce_wait_polls(polls)
 
 
 def rmsnorm_scratch_elems(rows, C):

@@ -107,6 +107,7 @@ struct CeGemm {
     int out_kind, out_bf16, out_tma, ld;  // out_tma: bf16 that a tensor map can write
     size_t out_split;
     const float *part_in;
+    unsigned polls;           // of a bounded wait
 };
 
 // Hands an accumulator back.  What it orders are the tcgen05 loads before the fence, not memory: a releasing arrival would
@@ -139,6 +140,14 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
+// Waits for work that is known to be in flight, which ends by itself: the limit is there for broken hardware alone.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+    for (unsigned i = 0; i < kSpinLimit; ++i) {
+        if (mbar_try(bar, parity)) return;
+        if (i > 4096) __nanosleep(64);
+    }
+}
+constexpr uint32_t kGaveUp = 1u << 31;
 __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 // Which tile a work item is: all tiles of a split, in bands of group_m tile rows that are walked column by column, so
@@ -406,17 +415,18 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     static_assert(NT == kTile || (NT == 2 * kTile && !PROMOTE), "tiles are one or two accumulators wide");
     constexpr int kStages = Stage<NT>::count, kStageBytes = Stage<NT>::bytes, kBlockBytes = Stage<NT>::block, kw = Stage<NT>::kw, kHalves = NT / kTile;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
-    __shared__ uint32_t tmem_holder;
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
+    __shared__ uint32_t tmem_holder, s_peer;
     __shared__ int abort_flag;
     __shared__ float4 s_bias[MODE == kLse || MODE == kDz ? kEpiWarps : 1][8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const Waiter wt{&abort_flag, &g_ce_error, kSpinLimit};
+    const Waiter wt{&abort_flag, &g_ce_error, g.polls};
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 2 * kEpiWarps); }
+        mbar_init(smem_u32(&drained), 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -434,6 +444,31 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const uint32_t tmem = tmem_holder;
     const int n_items = g.tiles_m * g.tiles_n * g.splits;
     const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    // Copies into stage s of this CTA's halves of A and B: one step of the K range.
+    auto load_step = [&](uint32_t s, int seg, int k, int m0, int n0) {
+        if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + kHalves * g.b_bytes));
+        const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
+        const uint32_t a = base + s * kStageBytes;
+        // K-major: a box is 64 K values of 128 rows.  MN-major: 64 rows of kw K values.
+#pragma unroll
+        for (int j = 0; j < (A_MN ? 2 : kw / kKBox); ++j) {
+            if (A_MN) tma_load_pair(a + j * (kBlockBytes / 2), &map_a, bar, g.a_off[seg] + m0 + kKBox * j, k);
+            else tma_load_pair(a + j * (kHalf * kKBox * 2), &map_a, bar, g.a_off[seg] + k + kKBox * j, m0);
+        }
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+            const uint32_t b = a + (1 + h) * kBlockBytes;
+            const int nn = n0 + h * kTile;
+#pragma unroll
+            for (int j = 0; j < (B_MN ? 2 : kw / kKBox); ++j) {
+                if (B_MN && j * kKBox >= g.width / 2) break;
+                if (B_MN) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, g.b_off[seg] + nn + kKBox * j, g.b_k0 + k);
+                else tma_load_pair(b + j * (kHalf * kKBox * 2), &map_b, bar, g.b_off[seg] + k + kKBox * j, g.b_r0 + nn);
+            }
+        }
+    };
+    uint32_t issued = 0;   // steps that this CTA's thread of the loads has issued
+    bool issuer = false;   // the thread of the pair that issues the products
 
     if (warp == 0) {
         if (lane == 0) {  // loads
@@ -448,33 +483,12 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 int kb = kb0 == 0 ? 0 : kb0 / g.n_seg, seg = kb0 - kb * g.n_seg;
                 for (int i = kb0; i < kb1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 51)) { ok = false; break; }
-                    if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + kHalves * g.b_bytes));
-                    const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
-                    const uint32_t a = base + s * kStageBytes;
-                    const int k = kb * kw;
-                    // K-major: a box is 64 K values of 128 rows.  MN-major: 64 rows of kw K values.
-#pragma unroll
-                    for (int j = 0; j < (A_MN ? 2 : kw / kKBox); ++j) {
-                        if (A_MN) tma_load_pair(a + j * (kBlockBytes / 2), &map_a, bar, g.a_off[seg] + m0 + kKBox * j, k);
-                        else tma_load_pair(a + j * (kHalf * kKBox * 2), &map_a, bar, g.a_off[seg] + k + kKBox * j, m0);
-                    }
-#pragma unroll
-                    for (int h = 0; h < kHalves; ++h) {
-                        const uint32_t b = a + (1 + h) * kBlockBytes;
-                        const int nn = n0 + h * kTile;
-#pragma unroll
-                        for (int j = 0; j < (B_MN ? 2 : kw / kKBox); ++j) {
-                            if (B_MN && j * kKBox >= g.width / 2) break;
-                            if (B_MN) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, g.b_off[seg] + nn + kKBox * j, g.b_k0 + k);
-                            else tma_load_pair(b + j * (kHalf * kKBox * 2), &map_b, bar, g.b_off[seg] + k + kKBox * j, g.b_r0 + nn);
-                        }
-                    }
+                    load_step(s, seg, kb * kw, m0, n0);
+                    ++issued;
                     if (++seg == g.n_seg) { seg = 0; ++kb; }
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
-            if (!ok)
-                for (int i = 0; i < 2000; ++i) __nanosleep(100);  // copies in flight land before the CTA can exit
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -483,7 +497,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             // multiply, so it is kept straight: the whole warp walks it and one elected lane issues; waits for an
             // accumulator and what follows its last K block stand outside (with them inside, under one lane,
             // 8192 x 4096 x 65536 took 3.56 ms instead of 2.92).
-            const bool issuer = elect_one();
+            issuer = elect_one();
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                                    ((uint32_t)((NT == kTile ? g.width : kTile) >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
             // K-major: 16 K values are 32 bytes of a swizzle row, the next 64 values 16 KB further.  MN-major: 16 rows of
@@ -629,7 +643,28 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync();  // no MMA of the pair reads this CTA's shared memory or writes its TMEM any more
+    if (threadIdx.x == 0)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(smem_u32(&s_peer), rank ^ 1u)), "r"(issued | (abort_flag ? kGaveUp : 0u)) : "memory");
+    cluster_sync();
+    if (abort_flag || (s_peer & kGaveUp)) {
+        // A wait of the pair ran out, so that products or copies may still be in flight; they would land in the shared memory
+        // and TMEM of whoever has them next.  The products end by themselves, and after them nothing reads the stages.  A
+        // step that only one of the CTAs has issued is completed by the other (any box will do), so that the barriers of all
+        // steps complete: a step is at most kStages ahead of the products, so that no two of one stage are open.
+        if (issuer) commit_pair(smem_u32(&drained));
+        if (threadIdx.x == 0) mbar_drain(smem_u32(&drained), 0);
+        __syncthreads();
+        cluster_sync();
+        if (threadIdx.x == 0) {
+            const uint32_t peer = s_peer & ~kGaveUp, last = max(issued, peer);
+            for (uint32_t i = issued; i < peer; ++i) load_step(i % kStages, 0, 0, 0, 0);
+            if (rank == 0)
+                for (uint32_t i = last > kStages ? last - kStages : 0; i < last; ++i) mbar_drain(smem_u32(&full[i % kStages]), (i / kStages) & 1u);
+        }
+        __syncthreads();
+        cluster_sync();
+    }
+    // no MMA of the pair reads this CTA's shared memory or writes its TMEM any more
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
@@ -907,6 +942,10 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ pa
 int up(int v, int to) { return (v + to - 1) / to * to; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
+// Polls of a bounded wait, for the calls of this thread (0: the default).
+thread_local unsigned t_wait_polls = 0;
+unsigned wait_polls() { return t_wait_polls ? t_wait_polls : kSpinLimit; }
+
 int sm_count() {
     int dev = 0, n = 148;
     if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
@@ -1063,6 +1102,7 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
         if (cudaFuncSetAttribute(ce_gemm_kernel<MODE, A_MN, B_MN, NT, PROMOTE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCeSmem) != cudaSuccess) return -1;
         ready_dev = dev;
     }
+    g.polls = wait_polls();
     const int pairs = (int)std::min<long>(items, sm_count() / 2);
     launch_k(ce_gemm_kernel<MODE, A_MN, B_MN, NT, PROMOTE>, 2 * pairs, kThreads, kCeSmem, s, ma, mb, mo, g);
     return 1;
@@ -1106,7 +1146,8 @@ template <int MODE, int NT> int rows_launch_as(const CUtensorMap &w, const CUten
     return 1;
 }
 // the columns of the MMA: 16, 32 or 64 rows of x
-template <int MODE> int rows_launch(const CeOperand &w, const CeOperand &x, const CeRowsArgs &g, const Launch &s) {
+template <int MODE> int rows_launch(const CeOperand &w, const CeOperand &x, CeRowsArgs &g, const Launch &s) {
+    g.polls = wait_polls();
     const int nt = g.B <= 16 ? 16 : (g.B <= 32 ? 32 : 64);
     CUtensorMap mw, mx;
     const bool partial = MODE == kPartial;
@@ -1219,6 +1260,8 @@ int join_dx(int prec, const CePlan &p, uint8_t *base, const int *labels, void *d
 }
 
 }  // namespace
+
+void linear_ce_wait_polls(unsigned polls) { t_wait_polls = polls; }
 
 bool linear_ce_in_place(int prec, int in) { return prec == P_BF16 && in % 8 == 0; }
 

@@ -45,6 +45,7 @@ struct CeRowsArgs {
     float *dx_part;          // kPartial
     size_t dx_split;
     int ld;
+    unsigned polls;          // of a bounded wait
 };
 
 __device__ __forceinline__ void tma_load_1(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
@@ -88,7 +89,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     constexpr int kStages = St::count, kw = St::kw, kPiece = kPieceBf16 / kw;
     constexpr bool kMn = MODE == kPartial;  // both operands lie with K outermost
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_holder;
     __shared__ int abort_flag;
     __shared__ int s_label[NT];
@@ -96,11 +97,12 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __shared__ float2 s_part[4][MODE == kLse ? NT : 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const Waiter wt{&abort_flag, &g_ce_error, kSpinLimit};
+    const Waiter wt{&abort_flag, &g_ce_error, g.polls};
     constexpr uint32_t kTmem = 2 * NT <= 32 ? 32 : 2 * NT;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 4); }
+        mbar_init(smem_u32(&drained), 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -124,6 +126,8 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
+    uint32_t issued = 0;   // steps that the thread of the loads has issued
+    bool issuer = false;   // the thread that issues the products
 
     if (warp == 0) {
         if (lane == 0) {  // loads
@@ -149,15 +153,14 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                             tma_load_1(b + j * (NT * 128), &map_x, bar, k + kKBox * j, 0);
                         }
                     }
+                    ++issued;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
-            if (!ok)
-                for (int i = 0; i < 2000; ++i) __nanosleep(100);  // copies in flight land before the CTA can exit
         }
         __syncwarp();
     } else if (warp == 1) {
-        const bool issuer = elect_one();
+        issuer = elect_one();
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (kMn ? (1u << 15) | (1u << 16) : 0u) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(kHalf >> 4) << 24);
         const uint64_t ad0 = kMn ? make_desc(base, 1024, 2u, St::a_bytes / 2) : make_desc(base, 1024, 2u);
         const uint64_t bd0 = make_desc(base + St::a_bytes, 1024, 2u);
@@ -288,6 +291,15 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
+    if (abort_flag) {
+        // A wait ran out: the products in flight end by themselves, so do the copies of the last kStages steps
+        if (issuer) tc_commit(smem_u32(&drained));
+        if (threadIdx.x == 0) {
+            mbar_drain(smem_u32(&drained), 0);
+            for (uint32_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_drain(smem_u32(&full[i % kStages]), (i / kStages) & 1u);
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmem) : "memory");

@@ -1016,3 +1016,31 @@ def test_tensor_arguments_are_checked_in_the_binding(binding):
     for bad in (x.t(), x.half(), x[:2]):
         with pytest.raises(ValueError):
             binding.dropout_fwd(0, bad, None, P, P, 32, 0.1)
+
+
+WAITS_RUN_OUT = """
+import torch
+from paper_1804_10574_b200 import binding as b
+for prec, n, d, v in ((1, 300, 136, 3000), (1, 700, 2200, 1100), (0, 300, 136, 700), (1, 8200, 64, 17000), (1, 1, 2048, 9000), (1, 20, 136, 3001), (1, 64, 2048, 12000)):
+    dt = torch.bfloat16 if prec else torch.float32
+    x, w = torch.randn(n, d, device="cuda").to(dt), torch.randn(v, d, device="cuda").to(dt)
+    y = torch.randint(0, v, (n,), device="cuda", dtype=torch.int32)
+    out = [torch.zeros(k, device="cuda") for k in (1, n, n)] + [torch.empty_like(x), torch.empty_like(w), torch.zeros(v, device="cuda")]
+    ws = torch.empty(max(b.linear_ce_workspace_bytes(prec, n, d, v, k) for k in (0, 1)), dtype=torch.uint8, device="cuda")
+    for polls in (1, 2, 3, 5, 9, 17, 40, 200, 1):
+        b.debug_linear_ce_wait_polls(polls)
+        b.linear_ce_fwd(prec, x, w, None, y, out[0], out[1], out[2], ws, n, d, v)
+        b.linear_ce_bwd(prec, x, w, None, y, out[2], None, None, out[3], out[4], out[5], ws, n, d, v)
+        torch.cuda.synchronize()
+    assert all(bool(torch.isnan(t).all()) for t in out[:3])
+    assert float((torch.ones(8, device="cuda") * 2).sum()) == 16.0
+"""
+
+
+@gpu
+def test_linear_ce_waits_that_run_out_end_cleanly(binding):
+    """Waits with limits from one poll on, at every way that waits on the device: each kernel lets its copies and products
+    land, frees its tensor memory and returns; the forward pass's results are NaN.  In a process of its own."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", WAITS_RUN_OUT], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
