@@ -398,8 +398,8 @@ ddg_status ddg_bn_bwd_reduce(int precision, const void *dout, const void *out, c
  * contents undefined on entry and exit; two calls that may run at the same time need one each.  The products run on the tensor
  * cores with fp32 accumulation; fp32 tensors are split into three bf16 terms.  W and x are read in place when
  * precision is DDG_BF16 and in is a multiple of 8 (both then start on 16-byte boundaries), else through a copy in the
- * workspace.  At most 2^24 rows and outputs and 2^20 inputs.  If a bounded device-side wait runs out, the results
- * are NaN. */
+ * workspace.  At most 2^24 rows and outputs and 2^20 inputs.  If a bounded device-side wait runs out, all
+ * results of that call are NaN, forward and backward; other calls are not touched. */
 size_t ddg_linear_ce_workspace_bytes(int precision, int B, int in, int out, int backward);
 ddg_status ddg_linear_ce_fwd(int precision, const void *x, const void *W, const void *bias, const int *labels, float *loss,
                              float *row_loss, float *lse, void *workspace, size_t workspace_bytes, int B, int in, int out,
@@ -416,9 +416,9 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
                              void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32, void *stream);
 
 /* Diagnostics, as ddg_debug_wait_timeout is for a context: the bounded device-side waits of the ddg_linear_ce_* calls
- * that this thread enqueues from now on give up after `polls` polls (a few hundred nanoseconds each); 0: the default, about
- * a second.  A kernel that gives up lets its copies and products in flight end before it returns. */
-void ddg_debug_linear_ce_wait_polls(unsigned polls);
+ * that this thread enqueues from now on give up after `polls` polls (a few hundred nanoseconds each; 0: at once);
+ * negative: the default, about a second.  A kernel that gives up lets its copies and products in flight end before it returns. */
+void ddg_debug_linear_ce_wait_polls(int polls);
 
 /* Root-mean-square norm of (at most 2^30) rows of C <= 16384 values, with the residual's addition:
  *   h = x + res;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd gamma;

@@ -124,7 +124,7 @@ _lib.ddg_linear_ce_workspace_bytes.argtypes = [_i] * 5
 _lib.ddg_linear_ce_workspace_bytes.restype = _sz
 _lib.ddg_linear_ce_fwd.argtypes = [_i] + [_vp] * 8 + [_sz] + [_i] * 3 + [_vp]
 _lib.ddg_linear_ce_bwd.argtypes = [_i] + [_vp] * 11 + [_sz] + [_i] * 4 + [_vp]
-_lib.ddg_debug_linear_ce_wait_polls.argtypes = [ctypes.c_uint]
+_lib.ddg_debug_linear_ce_wait_polls.argtypes = [_i]
 _lib.ddg_debug_linear_ce_wait_polls.restype = None
 _lib.ddg_rmsnorm_scratch_elems.argtypes = [_i] * 2
 _lib.ddg_rmsnorm_scratch_elems.restype = _sz
@@ -508,7 +508,7 @@ def linear_ce_bwd(prec, x, W, bias, labels, lse, dloss, drow, dx, dW, db, worksp
 
 def debug_linear_ce_wait_polls(polls):
     """Diagnostics: the device-side waits of the linear_ce calls that this thread enqueues from now on give up after
-    `polls` polls; 0: the default."""
+    `polls` polls (0: at once); negative: the default."""
     _lib.ddg_debug_linear_ce_wait_polls(polls)
 
 

@@ -106,7 +106,7 @@ ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const 
     return done(launch_linear_ce_bwd(precision, x, W, bias, labels, lse, dloss, drow, dx, dW, db, workspace, B, in, out, dw_f32, (cudaStream_t)stream));
 }
 
-void ddg_debug_linear_ce_wait_polls(unsigned polls) { linear_ce_wait_polls(polls); }
+void ddg_debug_linear_ce_wait_polls(int polls) { linear_ce_wait_polls(polls); }
 
 size_t ddg_rmsnorm_scratch_elems(int rows, int C) { return rows >= 1 && rows <= kRmsMaxRows && C >= 1 && C <= kRmsMaxC ? rmsnorm_scratch_elems(rows, C) : 0; }
 

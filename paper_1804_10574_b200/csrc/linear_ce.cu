@@ -67,16 +67,18 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kLse, kDz, kPartial, kWeightGrad };
 
-// Set when a bounded wait ran out, and never cleared: from then on results on this device are NaN.
-__device__ int g_ce_error;
-
-// What the workspace starts with.
+// What the workspace starts with.  A wait that runs out makes the results of its call NaN, all of them, and no other
+// call's: the backward pass, whose first kernel clears `failed`, ends with a kernel that looks at it; the forward pass may
+// have no kernel before the one that waits, so there every block leaves a word of its own, whatever stood there before.
+constexpr int kMostBlocks = 160;  // of a kernel that waits
 struct CeHeader {
     unsigned ticket;    // blocks of the joining kernel that are done
     float scale;        // factor on dx and dW: upstream gradient / counted rows
-    int pad[62];
+    int failed;         // backward: a wait of this call ran out
+    int pad[93];
+    int status[kMostBlocks];  // forward: a wait of this block ran out
 };
-static_assert(sizeof(CeHeader) == 256, "the buffers behind the header stay aligned");
+static_assert(sizeof(CeHeader) == 1024, "the buffers behind the header stay aligned");
 
 enum Out { kStore, kAdd, kFinal };
 
@@ -108,6 +110,7 @@ struct CeGemm {
     size_t out_split;
     const float *part_in;
     unsigned polls;           // of a bounded wait
+    int pairs;                // CTA pairs of the launch
 };
 
 // Hands an accumulator back.  What it orders are the tcgen05 loads before the fence, not memory: a releasing arrival would
@@ -422,7 +425,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const Waiter wt{&abort_flag, &g_ce_error, g.polls};
+    const Waiter wt{&abort_flag, &abort_flag, g.polls};
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 2 * kEpiWarps); }
@@ -669,9 +672,9 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
-    if ((MODE == kPartial || MODE == kWeightGrad) && threadIdx.x == 0 && *(volatile int *)&g_ce_error) {
-        if ((MODE == kWeightGrad || g.out_kind == kFinal) && g.out_bf16) *(bf16 *)g.out = __float2bfloat16_rn(__int_as_float(0x7fffffff));
-        else *(float *)g.out = __int_as_float(0x7fffffff);
+    if (threadIdx.x == 0) {
+        if (MODE == kLse) g.head->status[blockIdx.x] = abort_flag;
+        else if (abort_flag) g.head->failed = 1;
     }
     cluster_sync();
 }
@@ -688,7 +691,7 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 constexpr int kJoin = 512;
 __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict__ part, int n_part, const float *__restrict__ zlab, const int *__restrict__ labels,
                                                       float *__restrict__ loss, float *__restrict__ row_loss, float *__restrict__ lse_out,
-                                                      double *__restrict__ sums, CeHeader *head, int B, int V, int rows) {
+                                                      double *__restrict__ sums, CeHeader *head, int n_status, int B, int V, int rows) {
     __shared__ float sm[kJoin], ss[kJoin];
     __shared__ double bl[32];
     __shared__ int bc[32], last;
@@ -696,6 +699,7 @@ __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict
     pdl_wait();
     const int r = threadIdx.x & (rows - 1), t0 = threadIdx.x / rows, lanes = kJoin / rows;
     const int row = blockIdx.x * rows + r;
+    const int status = (int)threadIdx.x < n_status ? head->status[threadIdx.x] : 0;
     float m = -INFINITY, s = 0.f;
     if (row < B) {
         for (int t = t0; t < n_part; t += 8 * lanes) {
@@ -714,7 +718,7 @@ __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict
     }
     sm[threadIdx.x] = m;
     ss[threadIdx.x] = s;
-    __syncthreads();
+    const bool failed = __syncthreads_or(status) != 0;
     for (int o = lanes / 2; o > 0; o >>= 1) {
         if (t0 < o) {
             const int i = threadIdx.x, j = i + o * rows;
@@ -724,7 +728,6 @@ __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict
         }
         __syncthreads();
     }
-    const bool failed = g_ce_error != 0;
     if (t0 == 0) {
         float l = 0.f;
         int counted = 0;
@@ -769,7 +772,7 @@ __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict
 // ---- operands that TMA cannot read in place --------------------------------------------------------------------------
 // dst [rows][planes * plane] bf16: term p of column c at p * plane + c, zero past `cols`.  labels (nullable): rows that do
 // not count become zero, so that what stands in them (NaN among it) stays out of dW.  One launch copies up to two
-// matrices (x and W), by `blocks` blocks each; when `count` is set one more block sets the scale of the backward pass.
+// matrices (x and W), by `blocks` blocks each; when `count` is set one more block starts the backward pass's header.
 struct CePackJob { const void *src; bf16 *dst; const int *labels; int rows, blocks; };
 template <typename T>
 __global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, const CePackJob job_w, int cols, int plane, int planes, int V, CeHeader *head, int count, int mean,
@@ -789,7 +792,10 @@ __global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, con
             if ((int)threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
             __syncthreads();
         }
-        if (threadIdx.x == 0) head->scale = mean ? (dloss ? *dloss : 1.f) / (float)max(part[0], 1) : 1.f;
+        if (threadIdx.x == 0) {
+            head->scale = mean ? (dloss ? *dloss : 1.f) / (float)max(part[0], 1) : 1.f;
+            head->failed = 0;
+        }
         return;
     }
     const bool second = (int)blockIdx.x >= job_x.blocks;
@@ -873,8 +879,28 @@ __device__ __forceinline__ void ce_db(const CeDb &g, int block, float scale) {
     __syncthreads();
     if (w == 0 && c < g.cols) {
         for (int i = 1; i < 8; ++i) a += fold[i][lane];
-        g.db[c] = g_ce_error ? __int_as_float(0x7fffffff) : (float)(a * (double)scale);
+        g.db[c] = (float)(a * (double)scale);
     }
+}
+// The results of a backward pass.
+struct CeResults { void *dx, *dW; float *db; size_t n_dx, n_dw; int n_db, dx_bf16, dw_bf16; };
+__device__ __forceinline__ void ce_fill_nan(void *p, size_t n, bool is_bf16) {
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (size_t)gridDim.x * blockDim.x) {
+        if (is_bf16) ((uint16_t *)p)[i] = 0x7fff; else ((uint32_t *)p)[i] = 0x7fffffffu;
+    }
+}
+__device__ __forceinline__ bool ce_failed(const CeHeader *head, const CeResults &r) {
+    if (!head->failed) return false;
+    if (r.dx) ce_fill_nan(r.dx, r.n_dx, r.dx_bf16);
+    if (r.dW) ce_fill_nan(r.dW, r.n_dw, r.dw_bf16);
+    if (r.db) ce_fill_nan(r.db, r.n_db, false);
+    return true;
+}
+// The end of a backward pass whose last kernel is not ce_dx_kernel.
+__global__ void __launch_bounds__(256) ce_end_kernel(const CeHeader *head, const __grid_constant__ CeResults results) {
+    pdl_launch();
+    pdl_wait();
+    ce_failed(head, results);
 }
 __global__ void __launch_bounds__(256) ce_db_kernel(const CeDb g, const CeHeader *head) {
     pdl_launch();
@@ -887,16 +913,17 @@ __global__ void __launch_bounds__(256) ce_db_kernel(const CeDb g, const CeHeader
 // share a group's splits and are added in index order.
 template <typename T>
 __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ part, int splits, size_t split_stride, int ld, const int *__restrict__ labels, T *__restrict__ dx,
-                                                    int B, int in, int V, int vec, int lanes, const CeHeader *head, const CeDb db, int db_blocks) {
+                                                    int B, int in, int V, int vec, int lanes, const CeHeader *head, const CeDb db, int db_blocks,
+                                                    const __grid_constant__ CeResults results) {
     __shared__ float4 fold[256];
     pdl_launch();
     pdl_wait();
+    if (ce_failed(head, results)) return;
     if ((int)blockIdx.x < db_blocks) {
         ce_db(db, blockIdx.x, head->scale);
         return;
     }
-    const bool failed = g_ce_error != 0;
-    const float scale = head->scale, nan = __int_as_float(0x7fffffff);
+    const float scale = head->scale;
     const int groups = 256 / lanes, g = threadIdx.x & (groups - 1), lane = threadIdx.x / groups;
     const size_t total = (size_t)B * (ld / 4);
     for (size_t i0 = (size_t)(blockIdx.x - db_blocks) * groups; i0 < total; i0 += (size_t)(gridDim.x - db_blocks) * groups) {
@@ -927,7 +954,6 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ pa
         }
         if (i >= total) continue;
         float v[4] = {a.x * scale, a.y * scale, a.z * scale, a.w * scale};
-        if (failed) v[0] = v[1] = v[2] = v[3] = nan;
         if (vec) {
             if (c < in) store_f<T, 4>(dx + row * in + c, v);
         } else {
@@ -942,9 +968,9 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const float *__restrict__ pa
 int up(int v, int to) { return (v + to - 1) / to * to; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Polls of a bounded wait, for the calls of this thread (0: the default).
-thread_local unsigned t_wait_polls = 0;
-unsigned wait_polls() { return t_wait_polls ? t_wait_polls : kSpinLimit; }
+// Polls of a bounded wait, for the calls of this thread (negative: the default).
+thread_local int t_wait_polls = -1;
+unsigned wait_polls() { return t_wait_polls >= 0 ? (unsigned)t_wait_polls : kSpinLimit; }
 
 int sm_count() {
     int dev = 0, n = 148;
@@ -986,8 +1012,8 @@ struct CePlan {
 };
 
 // Few rows: CTAs of the forward pass and of dz, at least one unit of the vocabulary each.
-constexpr int kRowsGridMax = 160, kR32PerSm = 3;
-int rows_grid(int out, int sms) { return std::min(std::min(sms, kRowsGridMax), (out + kRowsUnit - 1) / kRowsUnit); }
+constexpr int kR32PerSm = 3;
+int rows_grid(int out, int sms) { return std::min(std::min(sms, kMostBlocks), (out + kRowsUnit - 1) / kRowsUnit); }
 // Few rows, dx: splits of the vocabulary, so that the tiles of 128 columns fill the SMs.  Seconds by the bytes of W and of
 // the partial sums at 6 TB/s.
 int rows_splits(int B, int in, int out, int ld) {
@@ -1018,7 +1044,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.rows = prec == P_BF16 && B <= kRowsMax;
     p.tiles_m = (B + kTile - 1) / kTile;
-    p.n_part = p.rows || p.rows32 ? kRowsGridMax * (p.rows32 ? kR32PerSm : 1) : 2 * ((out + ce_width(B, out, 1) - 1) / ce_width(B, out, 1));
+    p.n_part = p.rows || p.rows32 ? kMostBlocks * (p.rows32 ? kR32PerSm : 1) : 2 * ((out + ce_width(B, out, 1) - 1) / ce_width(B, out, 1));
     size_t at = sizeof(CeHeader);
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     if (!backward) {
@@ -1103,8 +1129,8 @@ int ce_launch_as(const CeOperand &a, const CeOperand &b, const CeOperand &out, C
         ready_dev = dev;
     }
     g.polls = wait_polls();
-    const int pairs = (int)std::min<long>(items, sm_count() / 2);
-    launch_k(ce_gemm_kernel<MODE, A_MN, B_MN, NT, PROMOTE>, 2 * pairs, kThreads, kCeSmem, s, ma, mb, mo, g);
+    g.pairs = (int)std::min<long>(items, std::min(sm_count(), kMostBlocks) / 2);
+    launch_k(ce_gemm_kernel<MODE, A_MN, B_MN, NT, PROMOTE>, 2 * g.pairs, kThreads, kCeSmem, s, ma, mb, mo, g);
     return 1;
 }
 
@@ -1152,7 +1178,7 @@ template <int MODE> int rows_launch(const CeOperand &w, const CeOperand &x, CeRo
     CUtensorMap mw, mx;
     const bool partial = MODE == kPartial;
     if (!ce_map(w.ptr, w.rows, w.cols, w.cols, partial ? kRowsKw : kRowsUnit, &mw) || !ce_map(x.ptr, x.rows, x.cols, x.cols, partial ? kRowsKw : nt, &mx)) return -1;
-    const int grid = partial ? std::min(g.tiles * g.splits, sm_count()) : rows_grid(g.V, sm_count());
+    const int grid = partial ? std::min(g.tiles * g.splits, std::min(sm_count(), kMostBlocks)) : rows_grid(g.V, sm_count());
     return nt == 16 ? rows_launch_as<MODE, 16>(mw, mx, g, grid, s) : (nt == 32 ? rows_launch_as<MODE, 32>(mw, mx, g, grid, s) : rows_launch_as<MODE, 64>(mw, mx, g, grid, s));
 }
 
@@ -1189,7 +1215,7 @@ template <int MODE> int r32_logits(const CeR32Args &g, int grid, const Launch &s
 }
 // CTAs of the logits: no more than give every warp a group of four entries
 int r32_grid(int B, int in, int out) {
-    return std::max(1, std::min(std::min(sm_count(), kRowsGridMax) * r32_per_sm(B, in), (out + 31) / 32));
+    return std::max(1, std::min(std::min(sm_count(), kMostBlocks) * r32_per_sm(B, in), (out + 31) / 32));
 }
 template <int NB> int r32_gradients(const CeR32Args &g, bool dx, const Launch &s) {
     const int slabs = (g.D + kR32Cols - 1) / kR32Cols;
@@ -1247,21 +1273,22 @@ int pack(int prec, const void *x, void *x_dst, const void *W, void *w_dst, const
     return 1;
 }
 
-int join_dx(int prec, const CePlan &p, uint8_t *base, const int *labels, void *dx, int B, int in, int out, const CeDb &db, int db_blocks, const Launch &s) {
+int join_dx(int prec, const CePlan &p, uint8_t *base, const int *labels, const CeResults &results, int B, int in, int out, const CeDb &db, int db_blocks, const Launch &s) {
+    void *dx = results.dx;
     const int lanes = p.splits >= 8 && (size_t)B * (p.dx_ld / 4) < 148 * 256 ? 8 : 1, grid = grid_for((size_t)B * (p.dx_ld / 4) * lanes) + db_blocks;
     const int vec = in % 4 == 0 && (reinterpret_cast<uintptr_t>(dx) & (4 * elem_size(prec) - 1)) == 0;
     const float *part = (const float *)(base + p.dx);
     const CeHeader *head = (const CeHeader *)base;
     if (prec == P_BF16)
-        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, part, p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec, lanes, head, db, db_blocks);
+        launch_k(ce_dx_kernel<bf16>, grid, 256, 0, s, part, p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (bf16 *)dx, B, in, out, vec, lanes, head, db, db_blocks, results);
     else
-        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, part, p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec, lanes, head, db, db_blocks);
+        launch_k(ce_dx_kernel<float>, grid, 256, 0, s, part, p.splits, (size_t)B * p.dx_ld, p.dx_ld, labels, (float *)dx, B, in, out, vec, lanes, head, db, db_blocks, results);
     return 1;
 }
 
 }  // namespace
 
-void linear_ce_wait_polls(unsigned polls) { t_wait_polls = polls; }
+void linear_ce_wait_polls(int polls) { t_wait_polls = polls; }
 
 bool linear_ce_in_place(int prec, int in) { return prec == P_BF16 && in % 8 == 0; }
 
@@ -1289,18 +1316,19 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
     float2 *part = (float2 *)(base + p.part);
     float *zlab = (float *)(base + p.zlab);
     const CeOperand ox{x, B, cols}, ow{W, out, cols};
-    int r, n_part = p.n_part;
+    int r, n_part = p.n_part, n_status;
     if (p.rows32) {
         CeR32Args g{};
         g.x = (const float *)x; g.W = (const float *)W; g.bias = (const float *)bias; g.labels = labels; g.head = head;
         g.part = part; g.zlab = zlab; g.B = B; g.D = in; g.V = out;
         n_part = r32_grid(B, in, out);
+        n_status = 0;  // nothing waits
         r = r32_logits<kLse>(g, n_part, s);
     } else if (p.rows) {
         CeRowsArgs g{};
         g.B = B; g.D = in; g.V = out; g.head = head;
         g.bias = bias; g.bias_bf16 = 1; g.labels = labels; g.part = part; g.zlab = zlab;
-        n_part = rows_grid(out, sm_count());
+        n_part = n_status = rows_grid(out, sm_count());
         r = rows_launch<kLse>(ow, ox, g, s);
     } else {
         CeGemm g{};
@@ -1309,12 +1337,13 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
         g.bias = bias; g.bias_bf16 = prec == P_BF16; g.labels = labels; g.V = out;
         g.part = part; g.zlab = zlab;
         r = ce_launch<kLse, false, false>(ox, ow, CeOperand{}, g, true, s);
+        n_status = 2 * g.pairs;
     }
     if (r < 0) return r;
     int rows = 1;  // of a block: as many blocks as SMs before rows share one
     while (rows < 32 && rows * 2 * kPairs < B) rows *= 2;
     launch_k(ce_join_kernel, (B + rows - 1) / rows, kJoin, 0, s, (const float2 *)part, n_part, (const float *)zlab, labels, loss, row_loss, lse,
-             (double *)(base + p.sums), head, B, out, rows);
+             (double *)(base + p.sums), head, n_status, B, out, rows);
     return n + r + 1;
 }
 
@@ -1329,6 +1358,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
     const CePlan p = ce_plan(prec, B, in, out, true, dw_f32 != 0);
     uint8_t *base = (uint8_t *)ws;
     CeHeader *head = (CeHeader *)base;
+    const CeResults results{dx, dW, db, (size_t)B * in, (size_t)out * in, out, prec == P_BF16, prec == P_BF16 && !dw_f32};
     if (p.rows32) {
         CeR32Args g{};
         g.x = (const float *)x; g.W = (const float *)W; g.bias = (const float *)bias; g.labels = labels; g.head = head;
@@ -1337,7 +1367,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         const int r = r32_logits<kDz>(g, r32_grid(B, in, out), s);
         if (r < 0) return r;
         const int nb = r32_nb(B), k = r + (nb == 4 ? r32_gradients<4>(g, dx, s) : (nb == 8 ? r32_gradients<8>(g, dx, s) : r32_gradients<16>(g, dx, s)));
-        return dx ? k + join_dx(prec, p, base, labels, dx, B, in, out, CeDb{}, 0, s) : k;
+        return dx ? k + join_dx(prec, p, base, labels, results, B, in, out, CeDb{}, 0, s) : k;
     }
     int n = pack(prec, x, base + p.x, p.pack_w ? W : nullptr, base + p.w, labels, p, B, in, out, head, true, drow == nullptr, dloss, s);
     const void *xp = base + p.x;
@@ -1434,8 +1464,11 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
             n += r;
         }
     }
-    if (!dx || dx_direct) return n;
-    return n + join_dx(prec, p, base, labels, dx, B, in, out, db_all, db_last ? ceil_div(out, 32) : 0, s);
+    if (!dx || dx_direct) {
+        launch_k(ce_end_kernel, 148, 256, 0, s, (const CeHeader *)head, results);
+        return n + 1;
+    }
+    return n + join_dx(prec, p, base, labels, results, B, in, out, db_all, db_last ? ceil_div(out, 32) : 0, s);
 }
 
 }  // namespace ddg

@@ -97,7 +97,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __shared__ float2 s_part[4][MODE == kLse ? NT : 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const Waiter wt{&abort_flag, &g_ce_error, g.polls};
+    const Waiter wt{&abort_flag, &abort_flag, g.polls};
     constexpr uint32_t kTmem = 2 * NT <= 32 ? 32 : 2 * NT;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
@@ -304,5 +304,8 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmem) : "memory");
     }
-    if (MODE == kPartial && threadIdx.x == 0 && *(volatile int *)&g_ce_error) *g.dx_part = __int_as_float(0x7fffffff);
+    if (threadIdx.x == 0) {
+        if (MODE == kLse) g.head->status[blockIdx.x] = abort_flag;
+        else if (abort_flag) g.head->failed = 1;
+    }
 }

@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(32 * kR32MostWarps) ce_r32_logits_kernel(const
         lse = n < g.B ? g.lse[n] : 0.f;
         weight = counted ? (g.drow ? g.drow[n] : 1.f) : 0.f;
         scale = r32_scale<NB>(g);
-        if (blockIdx.x == 0 && threadIdx.x == 0) g.head->scale = scale;
+        if (blockIdx.x == 0 && threadIdx.x == 0) { g.head->scale = scale; g.head->failed = 0; }
     }
     __syncthreads();
     const int groups = (g.V + kEntries - 1) / kEntries, walkers = gridDim.x * warps;

@@ -17,8 +17,8 @@ int launch_linear_ce_fwd(int prec, const void *x, const void *W, const void *bia
 int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bias, const int *labels, const float *lse,
                          const float *dloss, const float *drow, void *dx, void *dW, float *db, void *ws, int B, int in,
                          int out, int dw_f32, Launch s);
-// Polls before a device-side wait of the calls of this thread gives up; 0: the default.
-void linear_ce_wait_polls(unsigned polls);
+// Polls before a device-side wait of the calls of this thread gives up; negative: the default.
+void linear_ce_wait_polls(int polls);
 // x and W are read in place (and have to start on 16-byte boundaries) when this is true, else through a copy
 bool linear_ce_in_place(int prec, int in);
 

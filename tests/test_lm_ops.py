@@ -1027,7 +1027,7 @@ for prec, n, d, v in ((1, 300, 136, 3000), (1, 700, 2200, 1100), (0, 300, 136, 7
     y = torch.randint(0, v, (n,), device="cuda", dtype=torch.int32)
     out = [torch.zeros(k, device="cuda") for k in (1, n, n)] + [torch.empty_like(x), torch.empty_like(w), torch.zeros(v, device="cuda")]
     ws = torch.empty(max(b.linear_ce_workspace_bytes(prec, n, d, v, k) for k in (0, 1)), dtype=torch.uint8, device="cuda")
-    for polls in (1, 2, 3, 5, 9, 17, 40, 200, 1):
+    for polls in (1, 2, 3, 5, 9, 17, 40, 200, 0):
         b.debug_linear_ce_wait_polls(polls)
         b.linear_ce_fwd(prec, x, w, None, y, out[0], out[1], out[2], ws, n, d, v)
         b.linear_ce_bwd(prec, x, w, None, y, out[2], None, None, out[3], out[4], out[5], ws, n, d, v)
@@ -1039,8 +1039,40 @@ for prec, n, d, v in ((1, 300, 136, 3000), (1, 700, 2200, 1100), (0, 300, 136, 7
 
 @gpu
 def test_linear_ce_waits_that_run_out_end_cleanly(binding):
-    """Waits with limits from one poll on, at every way that waits on the device: each kernel lets its copies and products
+    """Waits with limits of few polls and of none, at every way that waits on the device: each kernel lets its copies and products
     land, frees its tensor memory and returns; the forward pass's results are NaN.  In a process of its own."""
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", WAITS_RUN_OUT], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+# every way of a call that waits on the device: rows with one chunk, with a K range that is cut, with splits, fp32, several chunks,
+# 16 / 32 / 64 rows
+WAYS_THAT_WAIT = [(300, 136, 777, 1), (700, 2200, 1100, 1), (2100, 264, 9000, 1), (300, 136, 700, 0), (8200, 40, 17000, 1), (1, 2048, 9000, 1), (20, 136, 3001, 1), (64, 2048, 12000, 1)]
+
+
+@gpu
+@pytest.mark.parametrize("shape", WAYS_THAT_WAIT, ids=lambda s: "x".join(map(str, s)))
+def test_linear_ce_results_of_a_call_whose_wait_ran_out_are_nan(binding, shape):
+    """All results of that call, whichever are asked for; with a limit that its waits keep, they are the usual bits; the
+    calls after it are not touched."""
+    c = Ce(*shape, bias=True, ignored=0.1, seed=51)
+    fwd = c.fwd(binding)
+    lse = fwd[2]
+    wants = [("xwb", False), ("x", False), ("w", True), ("b", False)]
+    bwd = [[t for t in c.bwd(binding, lse, want=w, dw_f32=f) if t is not None] for w, f in wants]
+    try:
+        for polls in (0, 1, 2, 1, 4, 1, 8, 16, 50, 400, 0):
+            binding.debug_linear_ce_wait_polls(polls)
+            got = [c.fwd(binding)] + [[t for t in c.bwd(binding, lse, want=w, dw_f32=f) if t is not None] for w, f in wants]
+            torch.cuda.synchronize()
+            for g, ref in zip(got, [fwd] + bwd):
+                failed = bool(torch.isnan(g[0].flatten()[0]))
+                assert failed or polls > 0
+                for a, b in zip(g, ref):
+                    assert bool(torch.isnan(a).all()) if failed else torch.equal(a, b), polls
+    finally:
+        binding.debug_linear_ce_wait_polls(-1)
+    after = [c.fwd(binding)] + [[t for t in c.bwd(binding, lse, want=w, dw_f32=f) if t is not None] for w, f in wants]
+    for g, ref in zip(after, [fwd] + bwd):
+        assert all(torch.equal(a, b) for a, b in zip(g, ref))
