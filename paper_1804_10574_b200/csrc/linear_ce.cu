@@ -1427,7 +1427,8 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
             g.bias_bf16 = prec == P_BF16; g.labels = labels; g.v0 = v0; g.V = out;
             g.lse = lse; g.drow = drow; g.planes = p.dz_planes; g.dz_plane = p.chunk;
             g.db_part = db ? (float *)(base + p.db) : nullptr;
-            const int r = ce_launch<kDz, false, false>(ox, ow, oz, g, prec == P_F32 || db, s);
+            // chains as the forward pass cuts them, whatever is asked for: exp(z - lse) has to see one z
+            const int r = ce_launch<kDz, false, false>(ox, ow, oz, g, true, s);
             if (r < 0) return r;
             n += r;
         }
