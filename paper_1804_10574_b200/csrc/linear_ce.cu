@@ -19,10 +19,11 @@
 //   8192 x 4096 x 65536   forward 1660, backward 1580 in short runs; 1460 and 1360 for seconds on end, under the power cap
 //   4096 x 1024 x 32000   forward 1450, backward 1400; 1390 and 1240
 //
-// The accumulator truncates: a chain of n steps of 16 products ends about n 2^-27 too small (measured: 2048 products
-// 6e-7, 10000 products 1e-5).  That is far below a bf16 result's rounding.  Where a result stays in 32 bits, chains are
-// cut after 128 steps, for fp32 tensors after every block of 128 K values, and the pieces added in registers, rounded to
-// nearest.
+// The accumulator truncates, so that a chain of many steps of 16 products ends too small.  Products of both signs: 2048 of
+// them are off by 3e-7 at most.  Products of one sign, relative to their sum: 2048 of them 2.6e-6, 2^20 2.3e-3, 2^22 2.2e-2,
+// 2^24 a tenth.  Where a result stays in 32 bits, chains are cut after 128 steps, for fp32 tensors after every block of 128 K
+// values, and the pieces added in registers, rounded to nearest.  Where it is rounded to bf16 itself (dx, dW), they are cut
+// after 65536 products (rows, or columns of a chunk): 1.5e-4 by proportion, a twentieth of that rounding.
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,
 // l h are accumulated: what is left out is below 2^-24 of the value.  A block of K values goes through all six, smallest
@@ -62,7 +63,8 @@ constexpr int kStageRing = 192 * 1024;
 constexpr int kOutBuf = 32 * kKBox * 2;  // an epilogue warp's 32 rows of 64 bf16 values on their way out
 constexpr int kCeSmem = kStageRing + kEpiWarps * kOutBuf + 1024;
 constexpr int kMaxSeg = 6;
-constexpr int kPieceBf16 = 2048, kPieceF32 = 256;  // K values (times products) of a chain that need not be cut
+// K values (times products) of a chain that need not be cut: for a 32-bit result of bf16 and of fp32 tensors, for a bf16 result
+constexpr int kPieceBf16 = 2048, kPieceF32 = 256, kPieceOut = 65536;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kLse, kDz, kPartial, kWeightGrad };
@@ -1144,14 +1146,14 @@ bool ce_wide(int M, int N, int splits) {
     return N > kTile && ce_rounds(M, N, 2 * kTile, splits) <= ce_rounds(M, N, kTile, splits);
 }
 
-// exact: the result stays in 32 bits, so that long chains are cut (see the top of the file)
+// exact: the result stays in 32 bits (what chains are cut after: see the top of the file)
 template <int MODE, bool A_MN, bool B_MN>
 int ce_launch(const CeOperand &a, const CeOperand &b, const CeOperand &out, CeGemm &g, bool exact, const Launch &s) {
     g.tiles_m = (g.M + kTile - 1) / kTile;
     if (g.splits < 1) g.splits = 1;
     g.group_m = 16;
     const long chain = (long)g.K * g.n_seg / g.splits;
-    if (exact && chain > (g.n_seg > 2 ? kPieceF32 : kPieceBf16)) return ce_launch_as<MODE, A_MN, B_MN, kTile, true>(a, b, out, g, s);
+    if (chain > (!exact ? kPieceOut : (g.n_seg > 2 ? kPieceF32 : kPieceBf16))) return ce_launch_as<MODE, A_MN, B_MN, kTile, true>(a, b, out, g, s);
     // The softmax's epilogues are long, and a wide tile leaves no accumulator to multiply into meanwhile (forward pass,
     // 4096 x 1024 x 32000: 223 us wide, 200 us narrow, with stages alike); the other products' are short, a wide tile asks
     // a quarter less of the L2 (dW, 8192 x 4096 x 16384: 694 us wide, 720 us narrow), and the rounds decide.

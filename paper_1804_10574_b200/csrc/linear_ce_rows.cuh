@@ -86,7 +86,7 @@ template <int MODE, int NT>
 __global__ void __launch_bounds__(kRowsThreads, 1)
 ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CeRowsArgs g) {
     typedef RowsStage<MODE, NT> St;
-    constexpr int kStages = St::count, kw = St::kw, kPiece = kPieceBf16 / kw;
+    constexpr int kStages = St::count, kw = St::kw, kPiece = (MODE == kPartial ? kPieceOut : kPieceBf16) / kw;
     constexpr bool kMn = MODE == kPartial;  // both operands lie with K outermost
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
@@ -168,7 +168,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         uint32_t s = 0, ph = 0, u = 0;
         for (RowsWalk<MODE, St::kw> w(g); ok && w.more(); w.next()) {
             for (int i0 = w.kb0; i0 < w.kb1 && ok; ++u) {
-                const int i1 = MODE == kPartial ? w.kb1 : min(i0 + kPiece, w.kb1);
+                const int i1 = min(i0 + kPiece, w.kb1);
                 const uint32_t acc = tmem + (u & 1u) * NT;
                 ok = mbar_wait(smem_u32(&acc_empty[u & 1u]), ((u >> 1) & 1u) ^ 1u, wt, 62);
                 tc_fence_after();
@@ -203,7 +203,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         for (RowsWalk<MODE, St::kw> w(g); ok && w.more(); w.next()) {
             const int row = w.at + 32 * quarter + lane;  // vocabulary entry, or column of W
             float v[NT];
-            const int pieces = MODE == kPartial ? 1 : (w.kb1 - w.kb0 + kPiece - 1) / kPiece;
+            const int pieces = (w.kb1 - w.kb0 + kPiece - 1) / kPiece;
             for (int piece = 0; piece < pieces; ++piece, ++u) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&acc_full[u & 1u]), (u >> 1) & 1u, wt, 64));
                 if (!ok) break;

@@ -1089,3 +1089,23 @@ def test_linear_ce_wide_outputs_asked_for_alone(binding, shape):
         within(got, ref, tol, what)
     for k, want in enumerate("xwb"):
         assert torch.equal(c.bwd(binding, lse, want=want)[k], full[k]), want
+
+
+@gpu
+def test_linear_ce_weight_gradient_of_the_most_rows(binding):
+    """2^24 rows, all terms of a sum of one sign: W = 0 makes every probability 1 / 128, and x is in [1, 2)."""
+    B, D, V = 1 << 24, 8, 128
+    g = torch.Generator(device="cuda")
+    g.manual_seed(71)
+    x = (torch.rand(B, D, device="cuda", generator=g) * 0.99 + 1).to(torch.bfloat16)
+    w, labels = torch.zeros(V, D, device="cuda", dtype=torch.bfloat16), torch.zeros(B, device="cuda", dtype=torch.int32)
+    lse, dw = f32(B, fill=math.log(V)), torch.full_like(w, 7.0)
+    ws = torch.empty(binding.linear_ce_workspace_bytes(1, B, D, V, True), dtype=torch.uint8, device="cuda")
+    binding.linear_ce_bwd(1, x, w, None, labels, lse, None, None, None, dw, None, ws, B, D, V)
+    mean = x.double().mean(0)
+    ref = mean[None, :].expand(V, D) / V
+    ref = torch.cat([ref[:1] - mean[None, :], ref[1:]])
+    # dz: 2^-20 of the exponential; 1 / 128 and 1 / 128 - 1 are bf16 values.  Chains of 128 steps that lose four units each;
+    # 2^24 / 2048 pieces added up one after the other, half a unit each of a sum that grows evenly; the factor, the result
+    tol = U[torch.bfloat16] + 2.0 ** -20 + 128 * 4 * 2.0 ** -24 + 8192 / 2 * 2.0 ** -24 + 2.0 ** -23
+    within(dw, ref, tol * ref.abs(), "dW")
