@@ -1109,3 +1109,31 @@ def test_linear_ce_weight_gradient_of_the_most_rows(binding):
     # 2^24 / 2048 pieces added up one after the other, half a unit each of a sum that grows evenly; the factor, the result
     tol = U[torch.bfloat16] + 2.0 ** -20 + 128 * 4 * 2.0 ** -24 + 8192 / 2 * 2.0 ** -24 + 2.0 ** -23
     within(dw, ref, tol * ref.abs(), "dW")
+
+
+@gpu
+@pytest.mark.parametrize("group,C", [(0, 4096), (128, 4096), (0, 4093), (0, 200)])
+def test_add_rmsnorm_8_bit_values_are_the_rounded_quotients(binding, group, C):
+    """y8 is y / scale8 rounded to e4m3, value for value: fp32 tensors, whose y and scale8 are what the kernel divides."""
+    rows = (1 << 24) // C
+    x, res, gamma = rms_inputs(rows, C, 0, 35)
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    q, scale = torch.empty(rows, C, dtype=torch.float8_e4m3fn, device="cuda"), f32(rows, C // (group or C))
+    binding.add_rmsnorm_fwd(0, x, res, gamma, h, y, q, scale, None, rows, C, group)
+    want = (y.view(rows, -1, group or C) / scale[..., None]).to(torch.float8_e4m3fn).view(rows, C)
+    assert int((want.view(torch.uint8) != q.view(torch.uint8)).sum()) == 0
+
+
+@gpu
+def test_add_rmsnorm_to_8_bits_of_an_infinite_value(binding):
+    """y beyond fp32: the scale is infinite, the group's finite values are zero and the infinite one is NaN, as y / scale8 says."""
+    rows, C = 3, 256
+    x, gamma = torch.ones(rows, C, device="cuda"), torch.ones(C, device="cuda")
+    x[1, 7] = 4.0
+    gamma[7] = 3e38
+    q, scale = torch.empty(rows, C, dtype=torch.float8_e4m3fn, device="cuda"), f32(rows, 2)
+    binding.add_rmsnorm_fwd(0, x, None, gamma, None, None, q, scale, None, rows, C, 128)
+    assert math.isinf(float(scale[1, 0])) and torch.isfinite(scale[0]).all() and float(scale[1, 1]) > 0
+    one = q[1].float()
+    assert math.isnan(float(one[7])) and not one[:7].any() and not one[8:128].any() and (one[128:] == 448.0).all()
+    assert float(q[0, 7].float()) == 448.0 and float(q[2, 7].float()) == 448.0
