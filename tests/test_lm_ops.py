@@ -1137,3 +1137,71 @@ def test_add_rmsnorm_to_8_bits_of_an_infinite_value(binding):
     one = q[1].float()
     assert math.isnan(float(one[7])) and not one[:7].any() and not one[8:128].any() and (one[128:] == 448.0).all()
     assert float(q[0, 7].float()) == 448.0 and float(q[2, 7].float()) == 448.0
+
+
+@gpu
+@PREC
+def test_linear_ce_gradients_past_32_bits(binding, prec):
+    """dx and the ends of dW of a projection of more than 2^31 values, few rows and many."""
+    V, D = 131073 + 64, 16384
+    w = torch.empty(V, D, dtype=DT[prec], device="cuda").normal_().mul_(0.01)
+    dw = torch.empty_like(w)
+    for B in (3, 70):
+        c = Ce(B, D, 8, prec, seed=81)
+        c.V, c.w = V, w
+        c.labels = torch.arange(V - B, V, device="cuda", dtype=torch.int32)
+        x = c.x.double()
+        parts = torch.cat([x @ w[i: i + 8192].double().t() for i in range(0, V, 8192)], 1)
+        ref = torch.logsumexp(parts, 1)
+        dx = torch.full_like(c.x, 7.0)
+        ws = torch.empty(binding.linear_ce_workspace_bytes(prec, B, D, V, True), dtype=torch.uint8, device="cuda")
+        binding.linear_ce_bwd(prec, c.x, w, None, c.labels, ref.float(), None, None, dx, dw, None, ws, B, D, V)
+        del ws
+        p = (parts - ref[:, None]).exp() / B
+        dz = p.clone()
+        dz[torch.arange(B), V - B + torch.arange(B)] -= 1.0 / B
+        # logits: a step of 16 products loses four units of 2^-24 of sums below 16384 x 0.8 x 0.8 x 0.01 (six products of fp32
+        # terms share the sum's 24 bits); exp2 and its argument 2^-20
+        tol = 4 * (6 if prec == 0 else 1) * 1024 * 2.0 ** -24 * 110 + 2.0 ** -20
+        edz = p * tol + 2.0 ** -24 / B + dz.abs() * (2.0 ** -8 if prec else 2.0 ** -24)
+        steps = (4 * (6 if prec == 0 else 1) * math.ceil(V / 16) + 80) * 2.0 ** -24
+        want, mass = torch.zeros(B, D, dtype=torch.float64, device="cuda"), torch.zeros(B, D, dtype=torch.float64, device="cuda")
+        for i in range(0, V, 8192):
+            block = w[i: i + 8192].double()
+            want += dz[:, i: i + 8192] @ block
+            mass += (edz[:, i: i + 8192] + steps * dz[:, i: i + 8192].abs()) @ block.abs()
+        within(dx, want, mass + U[dx.dtype] * want.abs(), "dx")
+        for at in (slice(0, 100), slice(V - 100, V)):
+            want, mass = dz[:, at].t() @ x, (edz[:, at] + 1100 * 2.0 ** -24 * dz[:, at].abs()).t() @ x.abs()
+            within(dw[at], want, mass + U[dw.dtype] * want.abs() + 1e-30, "dW")
+
+
+@gpu
+@PREC
+def test_add_rmsnorm_rstd_of_the_widest_rows(binding, prec):
+    """16384 columns: a thread adds at most 32 squares (8 per vector, 4 vectors), a tree over 1024 threads 10 more; half of
+    that after the root; the sum of x and res, the mean, eps: 2; rsqrt: 4 units of 2^-24."""
+    rows, C = 65, 16384
+    x, res, gamma = rms_inputs(rows, C, prec, 37)
+    h, y, rstd = torch.empty_like(x), torch.empty_like(x), f32(rows)
+    binding.add_rmsnorm_fwd(prec, x, res, gamma, h, y, None, None, rstd, rows, C)
+    _, ref, y_ref = rms_reference(x, res, gamma, 1e-6)
+    e = (42 / 2 + 2 + 4) * 2.0 ** -24
+    within(rstd, ref, e * ref, "rstd")
+    within(y, y_ref, (U[x.dtype] + e + 3 * 2.0 ** -24) * y_ref.abs(), "y")
+
+
+def test_philox_of_ones_and_of_the_digits_of_pi():
+    """The other published known answers (Salmon et al., 2011); the fourth word of the counter is always zero in a call, so
+    the ten rounds are written out for all four words here."""
+    def words(c, k):
+        for _ in range(10):
+            p, q = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+            c = [(q >> 32) ^ c[1] ^ k[0], q % 2 ** 32, (p >> 32) ^ c[3] ^ k[1], p % 2 ** 32]
+            k = [(k[0] + 0x9E3779B9) % 2 ** 32, (k[1] + 0xBB67AE85) % 2 ** 32]
+        return c
+
+    one = 2 ** 32 - 1
+    assert words([one] * 4, [one] * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+    assert words([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0]) == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
+    assert words([0x89ABCDEF, 0x01234567, 7, 0], [0x9ABCDEF0, 0x12345678]) == philox(0x123456789ABCDEF0, 0x0123456789ABCDEF, 7, 1)[0].tolist()
