@@ -21,8 +21,8 @@
 //
 // The accumulator truncates, so that a chain of many steps of 16 products ends too small.  Products of both signs: 2048 of
 // them are off by 3e-7 at most.  Products of one sign, relative to their sum: 2048 of them 2.6e-6, 2^20 2.3e-3, 2^22 2.2e-2,
-// 2^24 a tenth.  Where a result stays in 32 bits, chains are cut after 128 steps, for fp32 tensors after every block of 128 K
-// values, and the pieces added in registers, rounded to nearest.  Where it is rounded to bf16 itself (dx, dW), they are cut
+// 2^24 a tenth.  Where a result stays in 32 bits, chains are cut after 128 steps (fewer for a few rows), for fp32 tensors after every
+// block of 128 K values, and the pieces added in registers, rounded to nearest.  Where it is rounded to bf16 itself (dx, dW), they are cut
 // after 65536 products (rows, or columns of a chunk): 1.5e-4 by proportion, a twentieth of that rounding.
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,

@@ -4,7 +4,7 @@
 // 128 rows of an MMA (vocabulary entries, or in the product for dx the columns of W) and the rows of x are its 16, 32 or 64
 // columns; the accumulator has a vocabulary entry per lane and a row of x per column.  Every CTA works alone
 // (cta_group::1) on a stretch of the vocabulary cut at multiples of 32 entries, so that all SMs read the same amount, with
-// 128 KB and more of W in flight.  Measured, one row, 65536 x 2048 (268 MB): z 48 us (5.6 TB/s), dx 45 us (6.0 TB/s); the
+// 128 KB and more of W in flight.  Measured, one row, 65536 x 2048 (268 MB): z 49 us (5.6 TB/s), dx 45 us (6.0 TB/s); the
 // general kernel's 256 x 256 tiles take 85 us.  64 rows: z 58 us (their own loads are half as many bytes as W's).
 //
 //   kLse      per lane the running maximum and sum of every row of x over the CTA's entries, joined over the CTA at
@@ -86,7 +86,10 @@ template <int MODE, int NT>
 __global__ void __launch_bounds__(kRowsThreads, 1)
 ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CeRowsArgs g) {
     typedef RowsStage<MODE, NT> St;
-    constexpr int kStages = St::count, kw = St::kw, kPiece = (MODE == kPartial ? kPieceOut : kPieceBf16) / kw;
+    // Logits stay in 32 bits.  The loads leave the epilogue time to add short chains up, 16 to 64 rows of 2048 columns 256 to
+    // 1024 products long: lse of one row, 65536 x 2048, is 3.7e-7 off 64 bits (8.0e-6 with one chain of 2048) and takes 0.6 us
+    // more; 64 rows 3.6e-6 (7.8e-6) and no time (chains of 256: 7.4e-7 and 8 us).
+    constexpr int kStages = St::count, kw = St::kw, kPiece = (MODE == kPartial ? kPieceOut : 16 * NT) / kw;
     constexpr bool kMn = MODE == kPartial;  // both operands lie with K outermost
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;

@@ -1205,3 +1205,24 @@ def test_philox_of_ones_and_of_the_digits_of_pi():
     assert words([one] * 4, [one] * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
     assert words([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0]) == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
     assert words([0x89ABCDEF, 0x01234567, 7, 0], [0x9ABCDEF0, 0x12345678]) == philox(0x123456789ABCDEF0, 0x0123456789ABCDEF, 7, 1)[0].tolist()
+
+
+@gpu
+@pytest.mark.parametrize("B", [1, 16, 20, 64])
+def test_linear_ce_few_rows_cut_their_chains(binding, B):
+    """Logits whose 2048 products have one sign: chains of 256, 512 or 1024 products (16, 32, 64 rows at most) whose steps of
+    16 lose less than a unit of the sum so far, 2^-23, each, and whose sums are then added rounded to nearest."""
+    D, V = 2048, 1000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(91)
+    c = Ce(B, D, 8, 1, seed=92)
+    c.x = (torch.rand(B, D, device="cuda", generator=g) + 1).bfloat16()
+    c.V, c.w = V, ((torch.rand(V, D, device="cuda", generator=g) + 1) * 2.0 ** -8).bfloat16()
+    z = c.x.double() @ c.w.double().t()
+    ref = torch.logsumexp(z, 1)
+    chain = 256 if B <= 16 else (512 if B <= 32 else 1024)
+    # half of the steps' units, as the sum grows; half a unit of 2^-24 for each of the pieces; lse: exp2, the sums in pieces of 128
+    # and a tree, the logarithm and its sum
+    e = (chain / 16 + 1) / 2 * 2.0 ** -23 + (D / chain + 1) / 2 * 2.0 ** -24
+    tol = e * float(z.max()) + 2.0 ** -21 + 100 * 2.0 ** -24 + 8 * 2.0 ** -24 * float(ref.max())
+    within(c.fwd(binding)[2], ref, tol, "lse")
