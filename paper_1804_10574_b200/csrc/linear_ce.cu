@@ -1233,11 +1233,14 @@ template <int NB> int r32_gradients(const CeR32Args &g, bool dx, const Launch &s
     return n;
 }
 
-// Small heads: one launch per direction on the CUDA cores.  The forward pass has eight CTAs: from 17 rows of bf16 each, the
-// general path's two launches are faster (256 x 64 x 100: 13.3 us, 10.5 us; fp32, which the general path has to split,
-// 14.3 us, 18 us).
+// Small heads: one launch per direction on the CUDA cores.  The eight CTAs of the forward pass take eight rows each at a time,
+// which costs by the size of W; the other paths' two launches cost the same for all of these sizes, 10 us from 65 rows of bf16
+// on (10 to 16 us up to 64).  One pass is faster everywhere (256 x 100: 10.1 us), two passes for a small W (64 x 100, 65 to 128 rows:
+// 8.1 us; 128 x 10: 8.9; 32 x 300: 10.1 and 10.1; 256 x 100: 16.6 and 10.6), three never (64 x 100, 136 rows: 10.6 and 9.9).
+// fp32, which the general path has to split: 256 x 64 x 100 14.3 us, 18 us.
 bool head_fits(int prec, int B, int in, int out, bool backward) {
-    return B <= (backward || prec == P_F32 ? kHeadMaxB : 128) && in <= kHeadMaxD && head_smem(B, in, out) <= (size_t)kHeadSmem;
+    const int most = backward || prec == P_F32 ? kHeadMaxB : (long)in * out <= 8192 ? 16 * kHeadRows : 8 * kHeadRows;
+    return B <= most && in <= kHeadMaxD && head_smem(B, in, out) <= (size_t)kHeadSmem;
 }
 template <typename K> bool head_ready(K kernel, int &ready_dev) {
     int dev = 0;
