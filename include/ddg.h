@@ -409,8 +409,8 @@ ddg_status ddg_linear_ce_fwd(int precision, const void *x, const void *W, const 
  *   dx = dz W [B][in];  dW = dz^T x [out][in];  db = sum_n dz_n [out] fp32; each nullable, one at least is given.
  * g_n = drow[n] (the gradient of row_loss[n]) when drow is given, else dloss / (rows that count) with dloss the gradient
  * of loss (fp32 scalar; NULL = 1); not both.  dx in the element type; dW in the element type, or fp32 when dw_f32 != 0
- * (as ddg_sgd_update reads it).  dz is rounded to bf16 before the products (three bf16 terms for fp32 tensors, two for an
- * fp32 dW of bf16 tensors; small heads are worked in fp32 throughout).  dx may be x; dW may not be W. */
+ * (as ddg_sgd_update reads it).  dz is rounded to bf16 before the products (three bf16 terms for fp32 tensors, two for at
+ * most 32 rows and for an fp32 dW of bf16 tensors; small heads are worked in fp32 throughout).  dx may be x; dW may not be W. */
 ddg_status ddg_linear_ce_bwd(int precision, const void *x, const void *W, const void *bias, const int *labels,
                              const float *lse, const float *dloss, const float *drow, void *dx, void *dW, float *db,
                              void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32, void *stream);

@@ -775,7 +775,8 @@ __global__ void __launch_bounds__(kJoin) ce_join_kernel(const float2 *__restrict
 // dst [rows][planes * plane] bf16: term p of column c at p * plane + c, zero past `cols`.  labels (nullable): rows that do
 // not count become zero, so that what stands in them (NaN among it) stays out of dW.  One launch copies up to two
 // matrices (x and W), by `blocks` blocks each; when `count` is set one more block starts the backward pass's header.
-struct CePackJob { const void *src; bf16 *dst; const int *labels; int rows, blocks; };
+// A job's rows from `again` on are its first ones once more; rows past the source's are zeros.
+struct CePackJob { const void *src; bf16 *dst; const int *labels; int rows, blocks, src_rows, again; };
 template <typename T>
 __global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, const CePackJob job_w, int cols, int plane, int planes, int V, CeHeader *head, int count, int mean,
                                                       const int *__restrict__ labels_of_rows, int rows_of_labels, const float *__restrict__ dloss) {
@@ -815,9 +816,10 @@ __global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, con
         // rows off 16-byte boundaries: a warp per row, two neighbouring columns per lane
         const int lane = threadIdx.x & 31;
         for (int row = first * 8 + (threadIdx.x >> 5); row < job.rows; row += job.blocks * 8) {
-            const int y = labels ? labels[row] : 0;
-            const bool live = !labels || (y >= 0 && y < V);
-            const T *from = src + (size_t)row * cols;
+            const int src_row = row >= job.again ? row - job.again : row;
+            const int y = labels && src_row < job.src_rows ? labels[src_row] : 0;
+            const bool live = src_row < job.src_rows && (!labels || (y >= 0 && y < V));
+            const T *from = src + (size_t)src_row * cols;
             bf16 *to = dst + (size_t)row * planes * plane;
 #pragma unroll 8
             for (int c = 2 * lane; c < plane; c += 64) {
@@ -837,16 +839,17 @@ __global__ void __launch_bounds__(256) ce_pack_kernel(const CePackJob job_x, con
     for (size_t i = (size_t)first * 256 + threadIdx.x; i < total; i += stride) {
         const size_t row = total <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
         const int c = (int)(i - row * per_row) * 8;
+        const size_t src_row = row >= (size_t)job.again ? row - job.again : row;
         float v[8];
-        bool live = true;
-        if (labels) { const int y = labels[row]; live = y >= 0 && y < V; }
+        bool live = src_row < (size_t)job.src_rows;
+        if (live && labels) { const int y = labels[src_row]; live = y >= 0 && y < V; }
         if (live && c < cols) {  // whole vectors: cols is a multiple of their length
             if (sizeof(T) == 2) {
-                load_f<T, 8>(src + row * cols + c, v);
+                load_f<T, 8>(src + src_row * cols + c, v);
             } else {
-                load_f<T, 4>(src + row * cols + c, reinterpret_cast<float(&)[4]>(v[0]));
+                load_f<T, 4>(src + src_row * cols + c, reinterpret_cast<float(&)[4]>(v[0]));
                 if (c + 4 < cols) {
-                    load_f<T, 4>(src + row * cols + c + 4, reinterpret_cast<float(&)[4]>(v[4]));
+                    load_f<T, 4>(src + src_row * cols + c + 4, reinterpret_cast<float(&)[4]>(v[4]));
                 } else {
 #pragma unroll
                     for (int j = 4; j < 8; ++j) v[j] = 0.f;
@@ -1006,6 +1009,8 @@ double ce_rounds(int M, int N, int nt, int splits);
 struct CePlan {
     int planes, plane;       // terms of an element, columns of a term in a packed operand
     int dz_planes, chunk;    // terms of dz, columns of a chunk
+    int dz_term, dz_cols;    // a few rows: columns between two terms of dz, columns of an entry's line
+    int x_rows;              // of the copy of x
     int tiles_m, n_part;
     int splits, dx_ld;
     bool rows, rows32;       // a few rows: the kernels of linear_ce_rows.cuh, of linear_ce_rows32.cuh
@@ -1013,6 +1018,8 @@ struct CePlan {
     size_t part, zlab, sums, x, w, dz, db, dx, bytes;
 };
 
+// Few rows: columns of the MMA that hold the rows of x.
+int rows_columns(int B) { return B <= 16 ? 16 : (B <= 32 ? 32 : 64); }
 // Few rows: CTAs of the forward pass and of dz, at least one unit of the vocabulary each.
 constexpr int kR32PerSm = 3;
 int rows_grid(int out, int sms) { return std::min(std::min(sms, kMostBlocks), (out + kRowsUnit - 1) / kRowsUnit); }
@@ -1045,6 +1052,11 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
     // dW or dx is rounded to 8 bits itself and takes dz rounded once to bf16
     p.dz_planes = prec == P_F32 ? 3 : (dw_f32 ? 2 : 1);
     p.rows = prec == P_BF16 && B <= kRowsMax;
+    if (p.rows) {  // up to 32 rows leave room for a second term in the line, see linear_ce_rows.cuh
+        p.dz_term = rows_columns(B);
+        if (p.dz_term < kRowsPitch) p.dz_planes = 2;
+        p.dz_cols = p.dz_term < kRowsPitch ? kRowsPitch : p.dz_planes * kRowsPitch;
+    }
     p.tiles_m = (B + kTile - 1) / kTile;
     p.n_part = p.rows || p.rows32 ? kMostBlocks * (p.rows32 ? kR32PerSm : 1) : 2 * ((out + ce_width(B, out, 1) - 1) / ce_width(B, out, 1));
     size_t at = sizeof(CeHeader);
@@ -1054,7 +1066,8 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
         p.zlab = take((size_t)B * 4);
         p.sums = take((size_t)B * 16);
     }
-    if (p.pack_x) p.x = take((size_t)B * p.planes * p.plane * 2);
+    p.x_rows = backward && p.rows && p.dz_term < kRowsPitch ? 2 * p.dz_term : B;  // dW = [both terms of dz]^T [x, x]: one product
+    if (p.pack_x) p.x = take((size_t)p.x_rows * p.planes * p.plane * 2);
     if (p.pack_w) p.w = take((size_t)out * p.planes * p.plane * 2);
     if (backward && p.rows32) {
         p.chunk = out;
@@ -1066,7 +1079,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
         p.chunk = out;
         p.dx_ld = up(in, 4);
         p.splits = rows_splits(B, in, out, p.dx_ld);
-        p.dz = take((size_t)out * p.dz_planes * kRowsPitch * 2);
+        p.dz = take((size_t)out * p.dz_cols * 2);
         p.dx = take((size_t)p.splits * B * p.dx_ld * 4);
     } else if (backward) {
         const size_t fit = kDzBytes / ((size_t)B * p.dz_planes * 2) / kTile * kTile;
@@ -1173,15 +1186,17 @@ template <int MODE, int NT> int rows_launch_as(const CUtensorMap &w, const CUten
     launch_k(ce_rows_kernel<MODE, NT>, grid, kRowsThreads, kRowsSmem, s, w, x, g);
     return 1;
 }
-// the columns of the MMA: 16, 32 or 64 rows of x
+// the columns of the MMA: 16, 32 or 64 rows of x; for dx both terms of them where dz has two in a line
 template <int MODE> int rows_launch(const CeOperand &w, const CeOperand &x, CeRowsArgs &g, const Launch &s) {
     g.polls = wait_polls();
-    const int nt = g.B <= 16 ? 16 : (g.B <= 32 ? 32 : 64);
+    constexpr bool partial = MODE == kPartial;
+    const int nt = std::min(kRowsPitch, (partial ? 2 : 1) * rows_columns(g.B));
     CUtensorMap mw, mx;
-    const bool partial = MODE == kPartial;
     if (!ce_map(w.ptr, w.rows, w.cols, w.cols, partial ? kRowsKw : kRowsUnit, &mw) || !ce_map(x.ptr, x.rows, x.cols, x.cols, partial ? kRowsKw : nt, &mx)) return -1;
     const int grid = partial ? std::min(g.tiles * g.splits, std::min(sm_count(), kMostBlocks)) : rows_grid(g.V, sm_count());
-    return nt == 16 ? rows_launch_as<MODE, 16>(mw, mx, g, grid, s) : (nt == 32 ? rows_launch_as<MODE, 32>(mw, mx, g, grid, s) : rows_launch_as<MODE, 64>(mw, mx, g, grid, s));
+    if constexpr (!partial)
+        if (nt == 16) return rows_launch_as<MODE, 16>(mw, mx, g, grid, s);
+    return (nt == 32 ? rows_launch_as<MODE, 32>(mw, mx, g, grid, s) : rows_launch_as<MODE, 64>(mw, mx, g, grid, s));
 }
 
 // terms of A and of B that are multiplied, smallest products first
@@ -1270,8 +1285,8 @@ int grid_for(size_t threads) { return (int)std::max<size_t>(1, std::min<size_t>(
 // Copies x (nullable) and W (nullable) for TMA; backward: labels mask x's rows, and the scale is set.
 int pack(int prec, const void *x, void *x_dst, const void *W, void *w_dst, const int *labels, const CePlan &p, int B, int in, int out, CeHeader *head, bool backward,
          bool mean, const float *dloss, const Launch &s) {
-    CePackJob jx{x, (bf16 *)x_dst, backward ? labels : nullptr, B, x ? grid_for((size_t)B * (p.plane / 8)) : 0};
-    CePackJob jw{W, (bf16 *)w_dst, nullptr, out, W ? grid_for((size_t)out * (p.plane / 8)) : 0};
+    CePackJob jx{x, (bf16 *)x_dst, backward ? labels : nullptr, p.x_rows, x ? grid_for((size_t)p.x_rows * (p.plane / 8)) : 0, B, p.x_rows > B ? p.dz_term : B};
+    CePackJob jw{W, (bf16 *)w_dst, nullptr, out, W ? grid_for((size_t)out * (p.plane / 8)) : 0, out, out};
     const int grid = jx.blocks + jw.blocks + (backward ? 1 : 0);
     if (prec == P_BF16) launch_k(ce_pack_kernel<bf16>, grid, 256, 0, s, jx, jw, in, p.plane, p.planes, out, head, backward ? 1 : 0, mean ? 1 : 0, labels, B, dloss);
     else launch_k(ce_pack_kernel<float>, grid, 256, 0, s, jx, jw, in, p.plane, p.planes, out, head, backward ? 1 : 0, mean ? 1 : 0, labels, B, dloss);
@@ -1392,9 +1407,10 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         g.out_tma = out_bf16 && in % 8 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0;
         const CeOperand o = g.out_tma ? CeOperand{g.out, cols, in} : CeOperand{};
         if (p.rows) {
-            g.K = kRowsPitch;
-            ce_segments(g, p.dz_planes, kRowsPitch, 1, 0);
-            return ce_launch<kWeightGrad, false, true>(CeOperand{dz, out, p.dz_planes * kRowsPitch}, ox, o, g, !out_bf16, s);
+            const bool both = p.x_rows > B;
+            g.K = both ? p.x_rows : kRowsPitch;
+            ce_segments(g, both ? 1 : p.dz_planes, kRowsPitch, 1, 0);
+            return ce_launch<kWeightGrad, false, true>(CeOperand{dz, out, p.dz_cols}, CeOperand{xp, p.x_rows, x_cols}, o, g, !out_bf16, s);
         }
         g.K = B;
         ce_segments(g, p.dz_planes, p.chunk, p.planes, p.plane);
@@ -1414,7 +1430,7 @@ int launch_linear_ce_bwd(int prec, const void *x, const void *W, const void *bia
         if (dx) {
             g.tiles = (in + kHalf - 1) / kHalf; g.splits = p.splits;
             g.dx_part = (float *)(base + p.dx); g.dx_split = (size_t)B * p.dx_ld; g.ld = p.dx_ld;
-            if ((r = rows_launch<kPartial>(ow, CeOperand{dz, out, p.dz_planes * kRowsPitch}, g, s)) < 0) return r;
+            if ((r = rows_launch<kPartial>(ow, CeOperand{dz, out, p.dz_cols}, g, s)) < 0) return r;
             n += r;
         }
         if (dW) {

@@ -9,7 +9,9 @@
 //
 //   kLse      per lane the running maximum and sum of every row of x over the CTA's entries, joined over the CTA at
 //             the end: one (maximum, sum) per CTA and row of x
-//   kDz       dz of an entry for all rows of x: 64 bf16 values, one 128-byte line, [V][planes * 64]; db is the lane's own sum
+//   kDz       dz of an entry for all rows of x: 64 bf16 values, one 128-byte line, [V][planes * 64]; db is the lane's own sum.
+//             Few values of dz may make up a gradient, so that a rounding of them to bf16 would show in it; up to 32 rows
+//             leave half of the line to a second term, which the products for dx and dW take along.
 //   kPartial  dx^T = W^T dz^T in splits of the vocabulary: fp32 [splits][B][ld]
 //
 // dW = dz^T x runs on the general kernel, which only writes here.
@@ -232,7 +234,7 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     float *dst = g.dx_part + split * g.dx_split + row;
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
-                        if (j < g.B) dst[(size_t)j * g.ld] = v[j];
+                        if (j < g.B) dst[(size_t)j * g.ld] = j < NT / 2 && g.B <= NT / 2 ? v[j] + v[j + NT / 2 < NT ? j + NT / 2 : j] : v[j];  // both terms
                 }
                 continue;
             }
@@ -260,19 +262,19 @@ ce_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     total += p;
                 }
                 if (g.db) g.db[row] = total * scale;
-                uint4 *dst = reinterpret_cast<uint4 *>(g.dz + (size_t)row * g.planes * kRowsPitch);
-                for (int p = 0; p < g.planes; ++p, dst += kRowsPitch / 8) {
+                const int planes = NT < kRowsPitch ? 2 : g.planes;
+                uint4 *dst = reinterpret_cast<uint4 *>(g.dz + (size_t)row * (NT < kRowsPitch ? 1 : planes) * kRowsPitch);
+                for (int p = 0; p < planes; ++p, dst += NT / 8) {
 #pragma unroll
-                    for (int j = 0; j < kRowsPitch / 8; ++j) {
-                        uint4 q = make_uint4(0, 0, 0, 0);
-                        if (8 * j < NT) {
-                            const float *f = v + (8 * j < NT ? 8 * j : 0);
-                            q = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
-                        }
-                        dst[j] = q;
+                    for (int j = 0; j < NT / 8; ++j) {
+                        const float *f = v + 8 * j;
+                        dst[j] = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
                     }
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) v[j] -= bf16_round(v[j]);
+                    for (int j = 0; j < NT; ++j) {  // an infinity stays in the first term alone
+                        const float h = bf16_round(v[j]);
+                        v[j] = isinf(h) ? 0.f : v[j] - h;
+                    }
                 }
             }
         }

@@ -1226,3 +1226,28 @@ def test_linear_ce_few_rows_cut_their_chains(binding, B):
     e = (chain / 16 + 1) / 2 * 2.0 ** -23 + (D / chain + 1) / 2 * 2.0 ** -24
     tol = e * float(z.max()) + 2.0 ** -21 + 100 * 2.0 ** -24 + 8 * 2.0 ** -24 * float(ref.max())
     within(c.fwd(binding)[2], ref, tol, "lse")
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(1, 104, 2277), (2, 136, 3000), (5, 392, 900), (16, 200, 3001), (17, 1000, 2000), (32, 72, 5000)], ids=lambda s: "x".join(map(str, s)))
+def test_linear_ce_gradients_of_the_fewest_rows_keep_two_terms_of_dz(binding, shape):
+    """Up to 32 rows of bf16: dz enters the products with 16 bits, so that a gradient that a few of its values make up is off
+    by its own rounding alone."""
+    for ignored in (0.0, 0.3):
+        c = Ce(*shape, 1, True, ignored, seed=95).reference(dloss=0.75)
+        lse = c.lse.float()
+        dx, dw, db = c.bwd(binding, lse, dloss=f32(1, fill=0.75))
+        counted = (c.labels >= 0) & (c.labels < c.V)
+        y = c.labels.clamp(0, c.V - 1).long()[:, None]
+        p = torch.softmax(c.z, 1)
+        g = torch.where(counted, 0.75 / max(1, int(counted.sum())), 0.0)[:, None]
+        dz = (p - torch.zeros_like(p).scatter_(1, y, 1.0)) * g
+        # as in the reference above, with two roundings of 2^-8 of dz one after the other; both terms' products are chains of one
+        # step more
+        ep = (p * (c.ez + c.e_lse[:, None] + 2.0 ** -21 + 2.0 ** -23 * (c.z - c.lse[:, None]).abs()) + 2.0 ** -24) * g
+        edz = ep + 2.0 ** -16 * dz.abs()
+        aw, ax, az = c.w.double().abs(), c.x.double().abs(), dz.abs()
+        steps = (4 * math.ceil(c.V / 16) + 84) * 2.0 ** -24
+        within(dx, c.dx, edz @ aw + steps * (az @ aw) + U[dx.dtype] * c.dx.abs() + 1e-30, "dx")
+        within(dw, c.dw, edz.t() @ ax + 40 * 2.0 ** -24 * (az.t() @ ax) + U[dw.dtype] * c.dw.abs() + 1e-30, "dW")
+        within(db, c.db, c.e_db, "db")
