@@ -20,10 +20,12 @@
 //   4096 x 1024 x 32000   forward 1450, backward 1400; 1390 and 1240
 //
 // The accumulator truncates, so that a chain of many steps of 16 products ends too small.  Products of both signs: 2048 of
-// them are off by 3e-7 at most.  Products of one sign, relative to their sum: 2048 of them 2.6e-6, 2^20 2.3e-3, 2^22 2.2e-2,
-// 2^24 a tenth.  Where a result stays in 32 bits, chains are cut after 128 steps (fewer for a few rows), for fp32 tensors after every
-// block of 128 K values, and the pieces added in registers, rounded to nearest.  Where it is rounded to bf16 itself (dx, dW), they are cut
-// after 65536 products (rows, or columns of a chunk): 1.5e-4 by proportion, a twentieth of that rounding.
+// them are off by 3e-7 at most.  Products of one sign, relative to their sum: 1024 of them 6.6e-7, 2048 2.6e-6, 2^20 2.3e-3,
+// 2^22 2.2e-2, 2^24 a tenth.  Where a result stays in 32 bits, chains are cut after 1024 products (fewer for a few rows), for
+// fp32 tensors after every block of 128 K values, and the pieces added in registers, rounded to nearest: lse of 4096 x 2048 x
+// 32000 is 3.5e-6 off 64 bits, 7.6e-6 with chains of 2048, which take 1 to 5 % less between 1024 and 2048 columns and nothing
+// less elsewhere.  Where the result is rounded to bf16 itself (dx, dW), they are cut after 65536 products (rows, or columns of
+// a chunk): 1.5e-4 by proportion, a twentieth of that rounding.
 //
 // fp32 tensors are split into three bf16 terms each (x = h + m + l to 24 bits) and the products h h, h m, m h, m m, h l,
 // l h are accumulated: what is left out is below 2^-24 of the value.  A block of K values goes through all six, smallest
@@ -64,7 +66,7 @@ constexpr int kOutBuf = 32 * kKBox * 2;  // an epilogue warp's 32 rows of 64 bf1
 constexpr int kCeSmem = kStageRing + kEpiWarps * kOutBuf + 1024;
 constexpr int kMaxSeg = 6;
 // K values (times products) of a chain that need not be cut: for a 32-bit result of bf16 and of fp32 tensors, for a bf16 result
-constexpr int kPieceBf16 = 2048, kPieceF32 = 256, kPieceOut = 65536;
+constexpr int kPieceBf16 = 1024, kPieceF32 = 256, kPieceOut = 65536;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kLse, kDz, kPartial, kWeightGrad };

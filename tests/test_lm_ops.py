@@ -1251,3 +1251,21 @@ def test_linear_ce_gradients_of_the_fewest_rows_keep_two_terms_of_dz(binding, sh
         within(dx, c.dx, edz @ aw + steps * (az @ aw) + U[dx.dtype] * c.dx.abs() + 1e-30, "dx")
         within(dw, c.dw, edz.t() @ ax + 40 * 2.0 ** -24 * (az.t() @ ax) + U[dw.dtype] * c.dw.abs() + 1e-30, "dW")
         within(db, c.db, c.e_db, "db")
+
+
+@gpu
+@pytest.mark.parametrize("B,D,V", [(70, 2048, 300), (600, 4096, 1000)])
+def test_linear_ce_chains_of_logits_are_short(binding, B, D, V):
+    """A product of one and then thousands whose sixteens are a little below the unit of one, 2^-23: what a chain that truncates
+    loses altogether.  At most the first 1024 products (64 steps) are one chain with the one; the others add up unharmed."""
+    c = Ce(B, D, 8, 1, seed=96)
+    c.V = V
+    c.x = torch.ones(B, D, device="cuda").bfloat16()
+    c.w = torch.full((V, D), 0.8984375 * 2.0 ** -27, device="cuda").bfloat16()
+    c.w[:, 0] = 1.0
+    c.labels = torch.zeros(B, device="cuda", dtype=torch.int32)
+    z = 1.0 + (D - 1) * 0.8984375 * 2.0 ** -27
+    loss, row, lse = c.fwd(binding)
+    # every exponential is one, their sum exact; the logarithm of V and its sum with z: two units each of values below 8
+    tol = 65 * 2.0 ** -23 + 2.0 ** -23 + 4 * 2.0 ** -22
+    within(lse, torch.full((B,), math.log(V) + z, dtype=torch.float64, device="cuda"), tol, "lse")
