@@ -450,6 +450,63 @@ ddg_status ddg_dropout_fwd(int precision, const void *x, const void *res, void *
 ddg_status ddg_dropout_bwd(int precision, const void *dy, void *dx, const void *rng, size_t n, float p, unsigned layer,
                            void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * A block around a linear layer that works, and keeps what its backward pass needs, in 8 bits.  A module with K - k + 1
+ * slots of history keeps so many copies of every layer's input: as codes they take half (bf16) or a quarter (fp32) of the
+ * memory, and the layer's forward and backward pass read them as they are.  As above: device pointers to contiguous
+ * tensors on the current device, the calls only enqueue, allocate nothing, can be captured, and give the same bits each time.
+ * --------------------------------------------------------------------------------------------------------- */
+
+/* Rows of codes: q int8 [rows][ddg_act8_pitch(C)], a row's C codes and zeros behind them (which no call reads), on a 16-byte
+ * boundary; scale fp32 [rows].  C <= 2^17.
+ *   m = max(max |x| of the row, 127 2^-126);  scale = m / 127 (at most 8454659 2^98, so that 127 scale is finite);
+ *   q = 127 x / m, rounded once, halves to even.
+ * A row that holds a NaN or an infinity has scale NaN and codes 0: all that is made of it is NaN.
+ * unpack: x = q scale, rounded to the element type. */
+int ddg_act8_pitch(int C); /* C rounded up to a multiple of 16; 0 for a C that is not supported */
+ddg_status ddg_act8_pack(int precision, const void *x, void *q, float *scale, int rows, int C, void *stream);
+ddg_status ddg_act8_unpack(int precision, const void *q, const float *scale, void *x, int rows, int C, void *stream);
+
+/* Fully connected layer on codes: y = xscale[n] wscale[o] (sum_k xq[n][k] Wq[o][k]) + bias[o], with exact integer sums.
+ * xq [B], Wq [out] rows of `in` codes (ddg_act8_pack of x and of W); bias [out] (nullable) in the element type; y [B][out]
+ * in the element type, or fp32 when y_f32 != 0.  At most 2^24 rows and outputs. */
+ddg_status ddg_fc8_fwd(int precision, const void *xq, const float *xscale, const void *Wq, const float *wscale,
+                       const void *bias, void *y, int B, int in, int out, int y_f32, void *stream);
+/* Its gradients, the rounding to codes taken as the identity, from the codes that were kept:
+ *   dx = dy W^ [B][in];  dW = dy^T x^ [out][in];  db = sum_n dy_n [out] fp32; each nullable, one at least is given,
+ * W^ and x^ being what ddg_act8_unpack gives.  dy [B][out] and dx in the element type, dW in the element type, or fp32 when
+ * dw_f32 != 0.  Wq and wscale may be NULL without dx, xq and xscale without dW.  workspace: device, 256-byte aligned,
+ * ddg_fc8_workspace_bytes(...) bytes, contents undefined on entry and exit; two calls that may run at the same time need
+ * one each.  dx may not be dy. */
+size_t ddg_fc8_workspace_bytes(int precision, int B, int in, int out);
+ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const float *xscale, const void *Wq,
+                       const float *wscale, void *dx, void *dW, float *db, void *workspace, size_t workspace_bytes, int B,
+                       int in, int out, int dw_f32, void *stream);
+
+/* Root-mean-square norms after a block and before the next one, with the block's gate and the residual's scale, over (at
+ * most 2^30) rows of C <= 16384 values:
+ *   rstd_post = 1 / sqrt(mean(b^2) + eps);  h = alpha res + gate b rstd_post gamma_post
+ *   rstd_pre = 1 / sqrt(mean(h^2) + eps);   y = h rstd_pre gamma_pre
+ * b, res, gamma_post [C], gamma_pre [C], h, y in the element type; gate (nullable = 1) [ceil(rows / span)][C], row n takes
+ * its row n / span: span = rows for one gate vector, the rows of a sample for a gate per sample, 1 for a gate per row.
+ * y and / or q with qscale (rows of codes, as ddg_act8_pack lays them out) are given; both are taken from the unrounded h.
+ * rstd_post, rstd_pre (nullable) fp32 [rows].  h may be b or res, y too if it is another tensor than h. */
+ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, const void *gate, const void *gamma_post,
+                              const void *gamma_pre, void *h, void *y, void *q, float *qscale, float *rstd_post,
+                              float *rstd_pre, int rows, int C, int span, float alpha, float eps, void *stream);
+/* Its gradients from the stored h, b, rstd_post and rstd_pre; dh (nullable) is the gradient that reaches h past the norm:
+ *   t = dh + rstd_pre (gamma_pre dy - h rstd_pre^2 mean(gamma_pre dy h));  dres = alpha t
+ *   db = rstd_post (gamma_post gate t - b rstd_post^2 mean(gamma_post gate t b))
+ *   dgate = sum over the gate row's rows of t b rstd_post gamma_post (nullable);  dgamma_post = sum gate t b rstd_post
+ *   dgamma_pre = sum dy h rstd_pre
+ * db, dres in the element type; dgate [ceil(rows / span)][C], dgamma_post, dgamma_pre fp32; scratch:
+ * ddg_block_norm_scratch_elems(rows, C, span) floats.  db and dres may each be dy, dh, b or h, not both the same one. */
+size_t ddg_block_norm_scratch_elems(int rows, int C, int span);
+ddg_status ddg_block_norm_bwd(int precision, const void *dy, const void *dh, const void *b, const void *h, const void *gate,
+                              const void *gamma_post, const void *gamma_pre, const float *rstd_post, const float *rstd_pre,
+                              void *db, void *dres, float *dgate, float *dgamma_post, float *dgamma_pre, float *scratch,
+                              int rows, int C, int span, float alpha, void *stream);
+
 /* Fused SGD update over n parameters (Eq. 9 with momentum and weight decay): d = g + wd*w; v = mu*v + d;
  * w -= lr*v; w_version = cast(w).  w, v, g fp32; w_version in the precision's element type. */
 ddg_status ddg_sgd_update(int precision, float *w, float *v, const float *g, void *w_version, size_t n, float lr,

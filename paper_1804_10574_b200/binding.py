@@ -37,7 +37,9 @@ EXPORTS = ["ddg_create", "ddg_step", "ddg_step_host", "ddg_set_lr", "ddg_param_c
            "ddg_piece_times", "ddg_conv3x3_fwd_stats_shared",
            "ddg_step_host_pipelined", "ddg_pipelined_loss", "ddg_conv3x3_dgrad_fused_shared",
            "ddg_linear_ce_workspace_bytes", "ddg_linear_ce_fwd", "ddg_linear_ce_bwd", "ddg_debug_linear_ce_wait_polls", "ddg_rmsnorm_scratch_elems",
-           "ddg_add_rmsnorm_fwd", "ddg_add_rmsnorm_bwd", "ddg_dropout_fwd", "ddg_dropout_bwd"]
+           "ddg_add_rmsnorm_fwd", "ddg_add_rmsnorm_bwd", "ddg_dropout_fwd", "ddg_dropout_bwd",
+           "ddg_act8_pitch", "ddg_act8_pack", "ddg_act8_unpack", "ddg_fc8_fwd", "ddg_fc8_workspace_bytes", "ddg_fc8_bwd", "ddg_block_norm_fwd",
+           "ddg_block_norm_scratch_elems", "ddg_block_norm_bwd"]
 
 
 class Layer(ctypes.Structure):
@@ -132,6 +134,17 @@ _lib.ddg_add_rmsnorm_fwd.argtypes = [_i] + [_vp] * 8 + [_i] * 3 + [_f, _vp]
 _lib.ddg_add_rmsnorm_bwd.argtypes = [_i] + [_vp] * 8 + [_i] * 2 + [_vp]
 _lib.ddg_dropout_fwd.argtypes = [_i] + [_vp] * 4 + [_sz, _f, ctypes.c_uint, _vp]
 _lib.ddg_dropout_bwd.argtypes = [_i] + [_vp] * 3 + [_sz, _f, ctypes.c_uint, _vp]
+_lib.ddg_act8_pitch.argtypes = [_i]
+_lib.ddg_act8_pack.argtypes = [_i] + [_vp] * 3 + [_i] * 2 + [_vp]
+_lib.ddg_act8_unpack.argtypes = [_i] + [_vp] * 3 + [_i] * 2 + [_vp]
+_lib.ddg_fc8_fwd.argtypes = [_i] + [_vp] * 6 + [_i] * 4 + [_vp]
+_lib.ddg_fc8_workspace_bytes.argtypes = [_i] * 4
+_lib.ddg_fc8_workspace_bytes.restype = _sz
+_lib.ddg_fc8_bwd.argtypes = [_i] + [_vp] * 9 + [_sz] + [_i] * 4 + [_vp]
+_lib.ddg_block_norm_fwd.argtypes = [_i] + [_vp] * 11 + [_i] * 3 + [_f, _f, _vp]
+_lib.ddg_block_norm_scratch_elems.argtypes = [_i] * 3
+_lib.ddg_block_norm_scratch_elems.restype = _sz
+_lib.ddg_block_norm_bwd.argtypes = [_i] + [_vp] * 15 + [_i] * 3 + [_f, _vp]
 _lib.ddg_sgd_update.argtypes = [_i, _vp, _vp, _vp, _vp, _sz, _f, _f, _f, _vp]
 
 
@@ -543,3 +556,75 @@ def dropout_bwd(prec, dy, dx, rng, n, p, layer=0, stream=None):
     e = _elem(prec)
     _ok(_lib.ddg_dropout_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dx, n, e, "dx"), _tensor(rng, 2, _I64, "rng"), n, p,
                              layer, stream))
+
+
+# ---- a block around a linear layer in 8 bits ------------------------------------------------------------------------
+_I8 = ("torch.int8",)
+
+
+def act8_pitch(C):
+    """Bytes from a row of C codes to the next: C rounded up to a multiple of 16 (0: C is not supported)."""
+    return _lib.ddg_act8_pitch(C)
+
+
+def act8_pack(prec, x, q, scale, rows, C, stream=None):
+    """Rows to 8-bit codes: q int8 [rows][act8_pitch(C)], scale fp32 [rows]."""
+    _ok(_lib.ddg_act8_pack(prec, _tensor(x, rows * C, _elem(prec), "x"), _tensor(q, rows * act8_pitch(C), _I8, "q"),
+                           _tensor(scale, rows, _F32, "scale"), rows, C, stream))
+
+
+def act8_unpack(prec, q, scale, x, rows, C, stream=None):
+    _ok(_lib.ddg_act8_unpack(prec, _tensor(q, rows * act8_pitch(C), _I8, "q"), _tensor(scale, rows, _F32, "scale"),
+                             _tensor(x, rows * C, _elem(prec), "x"), rows, C, stream))
+
+
+def fc8_fwd(prec, xq, xscale, Wq, wscale, bias, y, B, n_in, n_out, y_f32=False, stream=None):
+    """y = x W^T + bias from the codes of x and of W."""
+    e, pitch = _elem(prec), act8_pitch(n_in)
+    _ok(_lib.ddg_fc8_fwd(prec, _tensor(xq, B * pitch, _I8, "xq"), _tensor(xscale, B, _F32, "xscale"),
+                         _tensor(Wq, n_out * pitch, _I8, "Wq"), _tensor(wscale, n_out, _F32, "wscale"), _tensor(bias, n_out, e, "bias"),
+                         _tensor(y, B * n_out, _F32 if y_f32 else e, "y"), B, n_in, n_out, int(y_f32), stream))
+
+
+def fc8_workspace_bytes(prec, B, n_in, n_out):
+    return _lib.ddg_fc8_workspace_bytes(prec, B, n_in, n_out)
+
+
+def fc8_bwd(prec, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, n_in, n_out, dw_f32=False, stream=None):
+    """Gradients of fc8_fwd from the codes that were kept; workspace: a tensor of fc8_workspace_bytes(prec, B, n_in, n_out) bytes."""
+    e, pitch = _elem(prec), act8_pitch(n_in)
+    ws, ws_bytes = _workspace(workspace)
+    _ok(_lib.ddg_fc8_bwd(prec, _tensor(dy, B * n_out, e, "dy"), _tensor(xq, B * pitch, _I8, "xq"), _tensor(xscale, B, _F32, "xscale"),
+                         _tensor(Wq, n_out * pitch, _I8, "Wq"), _tensor(wscale, n_out, _F32, "wscale"), _tensor(dx, B * n_in, e, "dx"),
+                         _tensor(dW, n_out * n_in, _F32 if dw_f32 else e, "dW"), _tensor(db, n_out, _F32, "db"), ws, ws_bytes,
+                         B, n_in, n_out, int(dw_f32), stream))
+
+
+def _gate_elems(rows, C, span):
+    return -(-rows // span) * C if span > 0 else 0
+
+
+def block_norm_fwd(prec, b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre, rows, C, span, alpha=1.0,
+                   eps=1e-6, stream=None):
+    """h = alpha res + gate rmsnorm(b) gamma_post, y = rmsnorm(h) gamma_pre; span rows share a row of the gate."""
+    e, n = _elem(prec), rows * C
+    _ok(_lib.ddg_block_norm_fwd(prec, _tensor(b, n, e, "b"), _tensor(res, n, e, "res"), _tensor(gate, _gate_elems(rows, C, span), e, "gate"),
+                                _tensor(gamma_post, C, e, "gamma_post"), _tensor(gamma_pre, C, e, "gamma_pre"), _tensor(h, n, e, "h"),
+                                _tensor(y, n, e, "y"), _tensor(q, rows * act8_pitch(C), _I8, "q"), _tensor(qscale, rows, _F32, "qscale"),
+                                _tensor(rstd_post, rows, _F32, "rstd_post"), _tensor(rstd_pre, rows, _F32, "rstd_pre"), rows, C, span, alpha,
+                                eps, stream))
+
+
+def block_norm_scratch_elems(rows, C, span):
+    return _lib.ddg_block_norm_scratch_elems(rows, C, span)
+
+
+def block_norm_bwd(prec, dy, dh, b, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, db, dres, dgate, dgamma_post, dgamma_pre,
+                   scratch, rows, C, span, alpha=1.0, stream=None):
+    e, n, gates = _elem(prec), rows * C, _gate_elems(rows, C, span)
+    _ok(_lib.ddg_block_norm_bwd(prec, _tensor(dy, n, e, "dy"), _tensor(dh, n, e, "dh"), _tensor(b, n, e, "b"), _tensor(h, n, e, "h"),
+                                _tensor(gate, gates, e, "gate"), _tensor(gamma_post, C, e, "gamma_post"), _tensor(gamma_pre, C, e, "gamma_pre"),
+                                _tensor(rstd_post, rows, _F32, "rstd_post"), _tensor(rstd_pre, rows, _F32, "rstd_pre"), _tensor(db, n, e, "db"),
+                                _tensor(dres, n, e, "dres"), _tensor(dgate, gates, _F32, "dgate"), _tensor(dgamma_post, C, _F32, "dgamma_post"),
+                                _tensor(dgamma_pre, C, _F32, "dgamma_pre"),
+                                _tensor(scratch, block_norm_scratch_elems(rows, C, span), _F32, "scratch"), rows, C, span, alpha, stream))

@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libddg.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["engine.cu", "api_kernels.cu", "kernels_elementwise.cu", "kernels_conv_direct.cu", "conv_tc.cu", "fc_tc.cu", "api_noalloc.cu",
-           "linear_ce.cu", "rmsnorm.cu", "dropout.cu", "api_lm.cu"]
+           "linear_ce.cu", "rmsnorm.cu", "dropout.cu", "act8.cu", "fc8.cu", "block_norm.cu", "api_lm.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--expt-relaxed-constexpr",
          "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -1,5 +1,5 @@
-// C-ABI entry points of the operators at the tail of a language-model step (dropout, RMS norm, vocabulary projection with
-// softmax cross entropy).
+// C-ABI entry points of the operators of a language-model step: dropout, RMS norm, vocabulary projection with softmax cross
+// entropy, rows of 8-bit codes, the linear layer on them, the norms around a block.
 #include <math.h>
 #include <stdio.h>
 
@@ -74,6 +74,10 @@ ddg_status dropout(int precision, const void *x, const void *res, void *y, const
     return done(launch_dropout(precision, x, res, y, (const unsigned long long *)rng, n, (unsigned)rint((double)p * 65536.0), layer, (cudaStream_t)stream));
 }
 
+bool fc8_sizes_ok(int B, int in, int out) { return B >= 1 && in >= 1 && out >= 1 && B <= (1 << 24) && in <= kAct8MaxC && out <= (1 << 24); }
+ddg_status codes_check(const void *q, const char *msg) { return misaligned(q, 16) ? refuse(DDG_ERR_INVALID_ARG, msg) : DDG_OK; }
+bool norm_sizes_ok(int rows, int C, int span) { return rows >= 1 && rows <= kRmsMaxRows && C >= 1 && C <= kRmsMaxC && span >= 1; }
+
 }  // namespace
 
 extern "C" {
@@ -141,6 +145,81 @@ ddg_status ddg_dropout_fwd(int precision, const void *x, const void *res, void *
 
 ddg_status ddg_dropout_bwd(int precision, const void *dy, void *dx, const void *rng, size_t n, float p, unsigned layer, void *stream) {
     return dropout(precision, dy, nullptr, dx, rng, n, p, layer, stream);
+}
+
+int ddg_act8_pitch(int C) { return C >= 1 && C <= kAct8MaxC ? act8_pitch(C) : 0; }
+
+ddg_status ddg_act8_pack(int precision, const void *x, void *q, float *scale, int rows, int C, void *stream) {
+    if (bad_prec(precision) || !x || !q || !scale) return DDG_ERR_INVALID_ARG;
+    if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kAct8MaxC) return DDG_ERR_UNSUPPORTED;
+    ddg_status st = codes_check(q, "act8_pack: the codes have to start on a 16-byte boundary");
+    if (st != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
+    return done(launch_act8_pack(precision, x, q, scale, rows, C, (cudaStream_t)stream));
+}
+
+ddg_status ddg_act8_unpack(int precision, const void *q, const float *scale, void *x, int rows, int C, void *stream) {
+    if (bad_prec(precision) || !x || !q || !scale) return DDG_ERR_INVALID_ARG;
+    if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kAct8MaxC) return DDG_ERR_UNSUPPORTED;
+    ddg_status st = codes_check(q, "act8_unpack: the codes have to start on a 16-byte boundary");
+    if (st != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
+    return done(launch_act8_unpack(precision, q, scale, x, rows, C, (cudaStream_t)stream));
+}
+
+ddg_status ddg_fc8_fwd(int precision, const void *xq, const float *xscale, const void *Wq, const float *wscale, const void *bias, void *y, int B, int in, int out,
+                       int y_f32, void *stream) {
+    if (bad_prec(precision) || !xq || !xscale || !Wq || !wscale || !y) return DDG_ERR_INVALID_ARG;
+    if (!fc8_sizes_ok(B, in, out)) return DDG_ERR_UNSUPPORTED;
+    ddg_status st = codes_check(xq, "fc8_fwd: the codes of x have to start on a 16-byte boundary");
+    if (st != DDG_OK || (st = codes_check(Wq, "fc8_fwd: the codes of W have to start on a 16-byte boundary")) != DDG_OK) return st;
+    if ((st = ready({xq, xscale, Wq, wscale, bias, y})) != DDG_OK) return st;
+    if (conv_tc_init() != 0) return DDG_ERR_CUDA;
+    return done(launch_fc8_fwd(precision, xq, xscale, Wq, wscale, bias, y, B, in, out, y_f32, (cudaStream_t)stream));
+}
+
+size_t ddg_fc8_workspace_bytes(int precision, int B, int in, int out) {
+    return !bad_prec(precision) && fc8_sizes_ok(B, in, out) ? fc8_workspace_bytes(precision, B, in, out) : 0;
+}
+
+ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const float *xscale, const void *Wq, const float *wscale, void *dx, void *dW, float *db,
+                       void *workspace, size_t workspace_bytes, int B, int in, int out, int dw_f32, void *stream) {
+    if (bad_prec(precision) || !dy || !workspace || (!dx && !dW && !db) || (dx && (!Wq || !wscale)) || (dW && (!xq || !xscale))) return DDG_ERR_INVALID_ARG;
+    if (!fc8_sizes_ok(B, in, out)) return DDG_ERR_UNSUPPORTED;
+    if (dx == dy) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: dx may not be dy");
+    ddg_status st = codes_check(xq, "fc8_bwd: the codes of x have to start on a 16-byte boundary");
+    if (st != DDG_OK || (st = codes_check(Wq, "fc8_bwd: the codes of W have to start on a 16-byte boundary")) != DDG_OK) return st;
+    if (misaligned(workspace, 256)) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: the workspace has to start on a 256-byte boundary");
+    if (workspace_bytes < fc8_workspace_bytes(precision, B, in, out)) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: the workspace is smaller than ddg_fc8_workspace_bytes says");
+    if ((st = ready({dy, xq, xscale, Wq, wscale, dx, dW, db, workspace})) != DDG_OK) return st;
+    if (conv_tc_init() != 0) return DDG_ERR_CUDA;
+    return done(launch_fc8_bwd(precision, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, in, out, dw_f32, (cudaStream_t)stream));
+}
+
+ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, const void *gate, const void *gamma_post, const void *gamma_pre, void *h, void *y, void *q,
+                              float *qscale, float *rstd_post, float *rstd_pre, int rows, int C, int span, float alpha, float eps, void *stream) {
+    if (bad_prec(precision) || !b || !res || !gamma_post || !gamma_pre || !h || (!y && !q) || (q == nullptr) != (qscale == nullptr)) return DDG_ERR_INVALID_ARG;
+    if (!(eps >= 0.f) || isinf(eps)) return refuse(DDG_ERR_INVALID_ARG, "block_norm: eps has to be finite and not negative");
+    if (!isfinite(alpha)) return refuse(DDG_ERR_INVALID_ARG, "block_norm: alpha has to be finite");
+    if (y == h) return refuse(DDG_ERR_INVALID_ARG, "block_norm: y may not be h");
+    if (!norm_sizes_ok(rows, C, span)) return DDG_ERR_UNSUPPORTED;
+    ddg_status st = codes_check(q, "block_norm: the codes have to start on a 16-byte boundary");
+    if (st != DDG_OK || (st = ready({b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre})) != DDG_OK) return st;
+    return done(launch_block_norm_fwd(precision, b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre, rows, C, span, alpha, eps, (cudaStream_t)stream));
+}
+
+size_t ddg_block_norm_scratch_elems(int rows, int C, int span) { return norm_sizes_ok(rows, C, span) ? block_norm_scratch_elems(rows, C, span) : 0; }
+
+ddg_status ddg_block_norm_bwd(int precision, const void *dy, const void *dh, const void *b, const void *h, const void *gate, const void *gamma_post,
+                              const void *gamma_pre, const float *rstd_post, const float *rstd_pre, void *db, void *dres, float *dgate, float *dgamma_post,
+                              float *dgamma_pre, float *scratch, int rows, int C, int span, float alpha, void *stream) {
+    if (bad_prec(precision) || !dy || !b || !h || !gamma_post || !gamma_pre || !rstd_post || !rstd_pre || !db || !dres || !dgamma_post || !dgamma_pre || !scratch || (dgate && !gate))
+        return DDG_ERR_INVALID_ARG;
+    if (db == dres) return refuse(DDG_ERR_INVALID_ARG, "block_norm: db may not be dres");
+    if (!isfinite(alpha)) return refuse(DDG_ERR_INVALID_ARG, "block_norm: alpha has to be finite");
+    if (!norm_sizes_ok(rows, C, span)) return DDG_ERR_UNSUPPORTED;
+    const ddg_status st = ready({dy, dh, b, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, db, dres, dgate, dgamma_post, dgamma_pre, scratch});
+    if (st != DDG_OK) return st;
+    return done(launch_block_norm_bwd(precision, dy, dh, b, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, db, dres, dgate, dgamma_post, dgamma_pre, scratch, rows, C,
+                                      span, alpha, (cudaStream_t)stream));
 }
 
 }  // extern "C"

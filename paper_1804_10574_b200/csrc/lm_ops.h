@@ -1,5 +1,5 @@
-// Launchers of the operators at the tail of a language-model step: dropout, RMS norm, vocabulary projection with softmax
-// cross entropy.  As in kernels.h every launcher only enqueues on the given stream; it returns the number of launches it
+// Launchers of the operators of a language-model step: dropout, RMS norm, vocabulary projection with softmax cross entropy;
+// the norms around a block, rows of 8-bit codes and the linear layer on them.  As in kernels.h every launcher only enqueues on the given stream; it returns the number of launches it
 // issued, or a negative value when it refused.
 #pragma once
 #include <cuda_runtime.h>
@@ -35,5 +35,27 @@ int launch_add_rmsnorm_bwd(int prec, const void *dy, const void *dh, const void 
 // res nullable; threshold = drop probability in units of 2^-16
 int launch_dropout(int prec, const void *x, const void *res, void *y, const unsigned long long *rng, size_t n,
                    unsigned threshold, unsigned layer, Launch s);
+
+// ---- rows of 8-bit codes (act8.cu) -----------------------------------------------------------------------------------
+// bytes from a row of codes to the next: rows that TMA can read
+inline int act8_pitch(int C) { return (C + 15) / 16 * 16; }
+constexpr int kAct8MaxC = 1 << 17;  // products of so many codes sum up to less than 2^31
+int launch_act8_pack(int prec, const void *x, void *q, float *scale, int rows, int C, Launch s);
+int launch_act8_unpack(int prec, const void *q, const float *scale, void *x, int rows, int C, Launch s);
+
+// ---- linear layer on 8-bit codes (fc8.cu) ----------------------------------------------------------------------------
+int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, const float *ws, const void *bias, void *y, int B, int in, int out, int y_f32, Launch s);
+size_t fc8_workspace_bytes(int prec, int B, int in, int out);
+int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, void *ws_mem, int B, int in,
+                   int out, int dw_f32, Launch s);
+
+// ---- norms around a block (block_norm.cu) ----------------------------------------------------------------------------
+// span: rows that share a row of the gate
+int launch_block_norm_fwd(int prec, const void *b, const void *res, const void *gate, const void *post, const void *pre, void *h, void *y, void *q, float *scale,
+                          float *rstd_post, float *rstd_pre, int rows, int C, int span, float alpha, float eps, Launch s);
+size_t block_norm_scratch_elems(int rows, int C, int span);
+int launch_block_norm_bwd(int prec, const void *dy, const void *dh, const void *b, const void *h, const void *gate, const void *post, const void *pre,
+                          const float *rstd_post, const float *rstd_pre, void *db, void *dres, float *dgate, float *dpost, float *dpre, float *scratch, int rows, int C,
+                          int span, float alpha, Launch s);
 
 }  // namespace ddg
