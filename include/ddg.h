@@ -483,6 +483,11 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
                        const float *wscale, void *dx, void *dW, float *db, void *workspace, size_t workspace_bytes, int B,
                        int in, int out, int dw_f32, void *stream);
 
+/* Diagnostics, as ddg_debug_linear_ce_wait_polls: the bounded device-side waits of the ddg_fc8_* calls that this thread
+ * enqueues from now on give up after `polls` polls (0: at once); negative: the default, about a second.  What a block whose
+ * wait ran out was to write is NaN. */
+void ddg_debug_fc8_wait_polls(int polls);
+
 /* Root-mean-square norms after a block and before the next one, with the block's gate and the residual's scale, over (at
  * most 2^30) rows of C <= 16384 values:
  *   rstd_post = 1 / sqrt(mean(b^2) + eps);  h = alpha res + gate b rstd_post gamma_post

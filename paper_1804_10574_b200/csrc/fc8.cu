@@ -1,137 +1,752 @@
-// Fully connected layer on rows of 8-bit codes (act8.cuh): y = (xq xs)(wq ws)^T + bias from 32-bit integer sums, and the
-// gradients of the layer from the codes that were kept, dx = dy w^, dW = dy^T x^, db = sum dy, with w^ and x^ what the codes
-// stand for in the element type.
+// Fully connected layer on rows of 8-bit codes (act8.cuh).
+//
+//   forward    y_no = xs_n ws_o (sum_k xq_nk wq_ok) + b_o        32-bit integer sums, exact
+//   backward   dx = dy w^;  dW = dy^T x^;  db = sum_n dy_n       w^, x^: what the codes stand for in the element type
+//
+// The products run on one tcgen05 kernel, CTA pairs on tiles of 256 rows (pair_mma.cuh).  What bounds it: the forward pass
+// 2 B in out multiply-adds of 8-bit integers (kind::i8, twice the rate of bf16 by the same bytes of operands), the backward
+// pass twice as many of bf16.  The codes are the operands of the forward pass as they lie.  For the backward pass a first
+// kernel writes what they stand for as bf16 to the workspace, beside the sums for db, and dy where TMA cannot read it.
+//
+// fp32: a code is a bf16 value as it is, so that only dy times the scale (which belongs to the summed index in both products)
+// has to be split, into three bf16 terms: three products where two split operands would take six.
+//
+// The accumulator of bf16 products truncates, so that long chains end too small (by 2.3e-3 after 2^20 products of one sign):
+// where a result stays in 32 bits, chains are cut after 1024 products and the pieces added in registers, rounded to nearest;
+// where it is rounded to bf16 itself, after 65536 (1.5e-4 by proportion, a twentieth of that rounding).  Integer sums are exact.
 #include <algorithm>
 
 #include "act8.cuh"
 #include "common.cuh"
 #include "lm_ops.h"
+#include "pair_mma.cuh"
 
 namespace ddg {
 
 namespace {
 
-constexpr int kT = 64;
+constexpr int kStageKw = 256;                    // bytes of K of a stage: two swizzle rows, eight MMA steps
+constexpr int kBlockBytes = kHalf * kStageKw;    // one operand's 128 rows
+constexpr int kStageBytes = 2 * kBlockBytes;
+constexpr int kStages = 192 * 1024 / kStageBytes;
+constexpr int kEpiWarps = 8;                     // two per TMEM lane quarter, each half of an accumulator's columns
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBuf + 1024;
+static_assert(kSmem + 1536 <= 227 * 1024, "with the barriers and the epilogue's columns");
+constexpr int kMostPlanes = 3;
+constexpr int kPieceF32 = 1024, kPieceOut = 65536;  // K values of a chain: 32-bit results, bf16 results
+constexpr int kPairs = 74;                       // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
 
-template <typename T, typename TY>
-__global__ void __launch_bounds__(256) fc8_fwd_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq, const float *__restrict__ ws,
-                                                      const T *__restrict__ bias, TY *__restrict__ y, int B, int in, int out, int pitch) {
-    __shared__ int sx[kT][17], sw[kT][17];
+enum Mode { kForward, kGrad };
+enum Store { kBoxes, kRows };                    // results leave by a tensor map, or a line at a time
+
+struct MmArgs {
+    int M, N;                 // rows of A, rows of B (columns of the result)
+    int kblocks, n_seg;       // K blocks of a segment; segments: bf16 terms of A
+    int a_off[kMostPlanes];   // where a segment's term starts: in K (K-major A) or in M
+    int tiles_m, tiles_n, splits, group_m;
+    int width;                // columns of a tile: at most 256, a multiple of 64, alike for all tiles of a launch
+    int b_bytes;              // of B in a stage and CTA
+    int piece;                // steps of the K range (K blocks times segments) of a chain (with PROMOTE)
+    int tail;                 // MMA steps in a segment's last K block
+    const float *row_scale, *col_scale;  // forward
+    const void *bias;         // forward, nullable
+    int bias_bf16;
+    void *out;                // [splits][M][ld]
+    int out_bf16, store, ld;
+    size_t out_split;         // elements
+    unsigned polls;           // of a bounded wait
+};
+
+// All tiles of a split, in bands of group_m tile rows that are walked column by column, so that the operands of the tiles in
+// flight stay in the L2.
+struct MmTile { int split, m, n; };
+__device__ __forceinline__ MmTile mm_tile(const MmArgs &g, int item) {
+    const int per = g.tiles_m * g.tiles_n, split = g.splits == 1 ? 0 : item / per;
+    unsigned r = (unsigned)(item - split * per);
+    const unsigned band = r / (unsigned)(g.group_m * g.tiles_n);
+    r -= band * g.group_m * g.tiles_n;
+    const unsigned rows = min(g.group_m, g.tiles_m - (int)band * g.group_m), n = r / rows;
+    return MmTile{split, (int)(band * g.group_m + r - n * rows), (int)n};
+}
+// steps of the K range of a split: at most 2^22 K blocks and segments, times 148 splits, in 32 bits
+__device__ __forceinline__ void mm_range(const MmArgs &g, int split, int &i0, int &i1) {
+    const unsigned n = (unsigned)(g.kblocks * g.n_seg);
+    i0 = 0;
+    i1 = (int)n;
+    if (g.splits > 1) {
+        i0 = (int)(n * (unsigned)split / (unsigned)g.splits);
+        i1 = (int)(n * (unsigned)(split + 1) / (unsigned)g.splits);
+    }
+}
+__device__ __forceinline__ int mm_piece_end(const MmArgs &g, int i, int i1) { return min(i + g.piece - (int)((unsigned)i % (unsigned)g.piece), i1); }
+
+// 64 columns of the warp's 32 rows, v: sums as they stand in tensor memory, at columns col .. of row `row`.
+// s0, s1 and b0, b1: scale and bias of the columns, a lane each; s_col: 32 floats of the warp's own.
+template <int MODE>
+__device__ __forceinline__ void mm_finish(const MmArgs &g, const CUtensorMap *map_out, uint32_t buf, float *v, int split, int row, int col, int lane, float row_scale,
+                                          float *s_col, float s0, float s1, float b0, float b1) {
+    if (MODE == kForward) {
+        auto spread = [&](float of_lane, auto each) {  // a register of each lane's to all rows, 32 columns
+            __syncwarp();  // what stood there has been read
+            s_col[lane] = of_lane;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 t = *reinterpret_cast<const float4 *>(s_col + j);
+                each(j, t.x); each(j + 1, t.y); each(j + 2, t.z); each(j + 3, t.w);
+            }
+        };
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            spread(q ? s1 : s0, [&](int j, float t) { v[32 * q + j] = (float)__float_as_int(v[32 * q + j]) * row_scale * t; });
+            if (g.bias) spread(q ? b1 : b0, [&](int j, float t) { v[32 * q + j] += t; });
+        }
+    }
+    const int row0 = row - lane;
+    if (row0 >= g.M) return;
+    if (g.store == kBoxes) {
+        if (g.out_bf16) store_box(map_out, buf, lane, col, row0, v);
+        else store_box_f32(map_out, buf, lane, col, row0, v);
+    } else if (g.out_bf16) {
+        store_rows<true>((uint16_t *)g.out + split * g.out_split, buf, lane, row0, g.M, col, g.ld, v);
+    } else {
+        store_rows<false>((float *)g.out + split * g.out_split, buf, lane, row0, g.M, col, g.ld, v);
+    }
+}
+
+// A_MN / B_MN: the operand lies with M / N innermost (its rows are K values) instead of K.  I8: codes, exact sums.
+// PROMOTE: an accumulator holds at most g.piece steps, the epilogue adds the pieces.
+template <int MODE, bool A_MN, bool B_MN, bool PROMOTE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ MmArgs g) {
+    constexpr bool kI8 = MODE == kForward;
+    static_assert(!kI8 || (!A_MN && !B_MN && !PROMOTE), "codes lie with K innermost and their sums are exact");
+    constexpr int kElem = kI8 ? 1 : 2, kw = kStageKw / kElem, kBox = 128 / kElem;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
+    __shared__ uint32_t tmem_holder, s_peer;
+    __shared__ int abort_flag;
+    __shared__ float4 s_cols[MODE == kForward ? kEpiWarps : 1][8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const Waiter wt{&abort_flag, &abort_flag, g.polls};
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 2 * kEpiWarps); }
+        mbar_init(smem_u32(&drained), 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_holder)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
     pdl_launch();
-    pdl_wait();
-    const int m0 = blockIdx.y * kT, n0 = blockIdx.x * kT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    int acc[4][4] = {};
-    for (int k0 = 0; k0 < in; k0 += 64) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kT * 16; i += 256) {
-            const int r = i >> 4, c = i & 15, k = k0 + 4 * c;
-            auto word = [&](const int8_t *p, int row, int rows) {
-                if (row >= rows || k >= in) return 0;
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(p + (size_t)row * pitch + k);
-                return (int)(in - k >= 4 ? w : w & ((1u << (8 * (in - k))) - 1u));  // what stands behind a row's codes is not read
+    pdl_wait();  // nothing above touches global memory
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // both CTAs' barriers are ready
+    tc_fence_after();
+    const uint32_t tmem = tmem_holder;
+    const int n_items = g.tiles_m * g.tiles_n * g.splits;
+    const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    // Copies into stage s of this CTA's halves of A and B: one step of the K range.
+    auto load_step = [&](uint32_t s, int seg, int k, int m0, int n0) {
+        if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + g.b_bytes));
+        const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
+        const uint32_t a = base + s * kStageBytes, b = a + kBlockBytes;
+        // K-major: a box is 128 bytes of K of 128 rows.  MN-major: 64 rows of kw K values.
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (A_MN) tma_load_pair(a + j * (kBlockBytes / 2), &map_a, bar, g.a_off[seg] + m0 + kBox * j, k);
+            else tma_load_pair(a + j * (kHalf * 128), &map_a, bar, g.a_off[seg] + k + kBox * j, m0);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (B_MN && j * kBox >= g.width / 2) break;
+            if (B_MN) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, n0 + kBox * j, k);
+            else tma_load_pair(b + j * (kHalf * 128), &map_b, bar, k + kBox * j, n0);
+        }
+    };
+    uint32_t issued = 0;   // steps that this CTA's thread of the loads has issued
+    bool issuer = false;   // the thread of the pair that issues the products
+
+    if (warp == 0) {
+        if (lane == 0) {  // loads
+            bool ok = true;
+            uint32_t s = 0, ph = 0;
+            for (int item = first; item < n_items && ok; item += step) {
+                const MmTile t = mm_tile(g, item);
+                int i0, i1;
+                mm_range(g, t.split, i0, i1);
+                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * g.width + (int)rank * (g.width / 2);
+                int kb = i0 == 0 ? 0 : i0 / g.n_seg, seg = i0 - kb * g.n_seg;
+                for (int i = i0; i < i1; ++i) {
+                    if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 71)) { ok = false; break; }
+                    load_step(s, seg, kb * kw, m0, n0);
+                    ++issued;
+                    if (++seg == g.n_seg) { seg = 0; ++kb; }
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            // Products, for both CTAs: the whole warp walks a straight loop and one elected lane issues; the waits for an
+            // accumulator stand outside.
+            issuer = elect_one();
+            // 32-bit results: fp32 (1) or int32 (2); operands: bf16 (1) of kind::f16, signed (1) of kind::i8
+            const uint32_t idesc = ((kI8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(g.width >> 3) << 17) |
+                                   ((uint32_t)(kTile >> 4) << 24);
+            // K-major: a step of K is 32 bytes of a swizzle row, the next 128 bytes 16 KB further.  MN-major: a step is 16 rows of
+            // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
+            const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
+            const uint64_t bd0 = B_MN ? make_desc(base + kBlockBytes, 1024, 2u, kBlockBytes / 2) : make_desc(base + kBlockBytes, 1024, 2u);
+            auto multiply = [&](uint32_t s, uint32_t acc, bool fresh, int steps) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (k >= steps) break;
+                    const uint32_t at = s * (kStageBytes >> 4), kk = (uint32_t)((k >> 2) * (kHalf * 128 >> 4) + (k & 3) * 2);
+                    const uint64_t a = ad0 + (uint64_t)(at + (A_MN ? 128u * k : kk)), b = bd0 + (uint64_t)(at + (B_MN ? 128u * k : kk));
+                    if (kI8) mma_pair_i8(tmem + acc * kTile, a, b, idesc, !fresh || k > 0);
+                    else mma_pair(tmem + acc * kTile, a, b, idesc, !fresh || k > 0);
+                }
             };
-            sx[r][c] = word(xq, m0 + r, B);
-            sw[r][c] = word(wq, n0 + r, out);
+            bool ok = true;
+            uint32_t s = 0, ph = 0, u = 0;  // stage, its parity, accumulators used so far
+            const int short_from = (g.kblocks - 1) * g.n_seg;  // the last K block has g.tail steps
+            for (int item = first; item < n_items && ok; item += step) {
+                int i0, i1;
+                mm_range(g, g.splits == 1 ? 0 : item / (g.tiles_m * g.tiles_n), i0, i1);
+                for (; i0 < i1; ++u) {
+                    const int end = PROMOTE ? mm_piece_end(g, i0, i1) : i1;
+                    const uint32_t acc = u & 1u;
+                    ok = mbar_wait(smem_u32(&full[s]), ph, wt, 73) && mbar_wait(smem_u32(&acc_empty[acc]), ((u >> 1) & 1u) ^ 1u, wt, 72);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (issuer) {
+                        multiply(s, acc, true, i0 >= short_from ? g.tail : 8);
+                        commit_pair(smem_u32(&empty[s]));
+                    }
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                    for (int i = i0 + 1; i < end; ++i) {
+                        if (!mbar_wait(smem_u32(&full[s]), ph, wt, 73)) { ok = false; break; }
+                        tc_fence_after();
+                        if (issuer) {
+                            if (i >= short_from) multiply(s, acc, false, g.tail);
+                            else multiply(s, acc, false, 8);
+                            commit_pair(smem_u32(&empty[s]));
+                        }
+                        if (++s == kStages) { s = 0; ph ^= 1u; }
+                    }
+                    if (!ok) break;
+                    if (issuer) commit_pair(smem_u32(&acc_full[acc]));
+                    i0 = end;
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        float *const s_col = reinterpret_cast<float *>(s_cols[MODE == kForward ? warp - 2 : 0]);
+        const uint32_t buf = base + kStages * kStageBytes + (uint32_t)(warp - 2) * kOutBuf;
+        uint32_t u = 0;
+        bool ok = true;
+        for (int item = first; item < n_items; item += step) {
+            const MmTile t = mm_tile(g, item);
+            const int row = t.m * kTile + (int)rank * kHalf + 32 * quarter + lane;
+            const int col0 = t.n * g.width + half * kHalf, live = min(g.width - half * kHalf, g.N - col0);
+            int pieces = 1;
+            if (PROMOTE) {
+                int i0, i1;
+                mm_range(g, t.split, i0, i1);
+                pieces = 0;
+                for (int i = i0; i < i1; i = mm_piece_end(g, i, i1)) ++pieces;
+            }
+            float cs[4] = {}, cb[4] = {}, rs = 0.f;  // loaded while the products run
+            if (MODE == kForward) {
+                rs = row < g.M ? g.row_scale[row] : 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = min(col0 + 32 * q + lane, g.N - 1);
+                    cs[q] = g.col_scale[c];
+                    if (g.bias) cb[q] = g.bias_bf16 ? to_f(((const bf16 *)g.bias)[c]) : ((const float *)g.bias)[c];
+                }
+            }
+            float v[PROMOTE ? kHalf : kKBox];
+            if (PROMOTE) {
+#pragma unroll
+                for (int j = 0; j < kHalf; ++j) v[PROMOTE ? j : 0] = 0.f;
+            }
+#pragma unroll 1
+            for (int piece = 0; piece < pieces && ok; ++piece, ++u) {
+                const uint32_t acc = u & 1u;
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&acc_full[acc]), (u >> 1) & 1u, wt, 74));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t taddr = tmem + acc * kTile + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(half * kHalf);
+                auto hand_back = [&]() {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(map_rank(smem_u32(&acc_empty[acc]), 0));
+                };
+                if (!PROMOTE) {
+                    // 64 columns at a time in a loop that is not unrolled: short code
+#pragma unroll 1
+                    for (int c = 0; c < kHalf; c += kKBox) {
+                        if (c < live) {
+#pragma unroll
+                            for (int j = 0; j < kKBox; j += 32)
+                                tc_ld32(taddr + (uint32_t)(c + j), reinterpret_cast<float(&)[16]>(v[j]), reinterpret_cast<float(&)[16]>(v[j + 16]));
+                            tc_wait_ld();
+                        }
+                        if (c == kHalf - kKBox) hand_back();
+                        if (c < live) mm_finish<MODE>(g, &map_out, buf, v, t.split, row, col0 + c, lane, rs, s_col, c == 0 ? cs[0] : cs[2], c == 0 ? cs[1] : cs[3], c == 0 ? cb[0] : cb[2], c == 0 ? cb[1] : cb[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += 16) {
+                        float w[16];
+                        tc_ld16(taddr + (uint32_t)c, w);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[c + j] += w[j];
+                    }
+                    hand_back();
+                }
+            }
+            if (!ok) {  // what this tile and the ones after it should have become
+                for (int r = 0; r < 32 && row - lane + r < g.M; ++r)
+                    for (int c = lane; c < live; c += 32) {
+                        const size_t at = t.split * g.out_split + (size_t)(row - lane + r) * g.ld + col0 + c;
+                        if (g.out_bf16) ((uint16_t *)g.out)[at] = 0x7fff; else ((uint32_t *)g.out)[at] = 0x7fffffffu;
+                    }
+                continue;
+            }
+            if (PROMOTE) {
+#pragma unroll
+                for (int c = 0; c < kHalf; c += kKBox)
+                    if (c < live) mm_finish<MODE>(g, &map_out, buf, v + (PROMOTE ? c : 0), t.split, row, col0 + c, lane, rs, s_col, 0.f, 0.f, 0.f, 0.f);
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(smem_u32(&s_peer), rank ^ 1u)), "r"(issued | (abort_flag ? kGaveUp : 0u)) : "memory");
+    cluster_sync();
+    if (abort_flag || (s_peer & kGaveUp)) {
+        // A wait of the pair ran out, so that products or copies may still be in flight; they would land in the shared memory
+        // and TMEM of whoever has them next.  The products end by themselves, and after them nothing reads the stages.  A
+        // step that only one of the CTAs has issued is completed by the other (any box will do), so that the barriers of all
+        // steps complete: a step is at most kStages ahead of the products, so that no two of one stage are open.
+        if (issuer) commit_pair(smem_u32(&drained));
+        if (threadIdx.x == 0) mbar_drain(smem_u32(&drained), 0);
+        __syncthreads();
+        cluster_sync();
+        if (threadIdx.x == 0) {
+            const uint32_t peer = s_peer & ~kGaveUp, last = max(issued, peer);
+            for (uint32_t i = issued; i < peer; ++i) load_step(i % kStages, 0, 0, 0, 0);
+            if (rank == 0)
+                for (uint32_t i = last > kStages ? last - kStages : 0; i < last; ++i) mbar_drain(smem_u32(&full[i % kStages]), (i / kStages) & 1u);
         }
         __syncthreads();
-#pragma unroll
-        for (int c = 0; c < 16; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(sx[ty + 16 * i][c], sw[tx + 16 * j][c], acc[i][j]);
+        cluster_sync();
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m < B && n < out) y[(size_t)m * out + n] = from_f<TY>((float)acc[i][j] * xs[m] * ws[n] + (bias ? to_f(bias[n]) : 0.f));
-        }
+    // no MMA of the pair reads this CTA's shared memory or writes its TMEM any more
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+    cluster_sync();
 }
 
-// C[M][N] = sum_k A(m, k) value(B[k][n]): A is dy (K-major for dx, M-major for dW), B rows of codes with a scale each.
-template <typename T, typename TC, bool A_MN>
-__global__ void __launch_bounds__(256) fc8_grad_kernel(const T *__restrict__ a, const int8_t *__restrict__ q, const float *__restrict__ scale, TC *__restrict__ c, int M, int N, int K,
-                                                       int lda, int pitch) {
-    __shared__ float sa[16][kT + 1], sb[16][kT + 1];
+// ---- before the products of the backward pass ------------------------------------------------------------------------
+// Codes to bf16, in rows of `plane`: times their scale, or as they are (scale nullable).
+struct CodesJob { const int8_t *q; const float *scale; bf16 *dst; int rows, pitch, plane, blocks; };
+// dy to bf16 terms in rows of planes * plane, times a factor per row or column (nullable); zeros behind a row's columns.
+struct TermsJob { const void *src; bf16 *dst; const float *row_scale, *col_scale; int rows, cols, plane, planes, blocks; };
+// sums of dy over `chunk` rows: part[row chunk][cols]
+struct SumsJob { const void *src; float *part; int rows, cols, chunk, blocks, vec; };
+struct PrepArgs { CodesJob codes[2]; TermsJob terms[2]; SumsJob sums; };
+
+__device__ __forceinline__ void prep_codes(const CodesJob &j, int block) {
+    const unsigned per_row = j.pitch / 16;
+    const size_t units = (size_t)j.rows * per_row;
+    for (size_t i = (size_t)block * 256 + threadIdx.x; i < units; i += (size_t)j.blocks * 256) {
+        const size_t row = units <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
+        const int c = (int)(i - row * per_row) * 16;
+        const uint4 w = *reinterpret_cast<const uint4 *>(j.q + row * j.pitch + c);
+        const float s = j.scale ? j.scale[row] : 1.f;
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        uint32_t out[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t x = word[k / 2] >> (16 * (k % 2));
+            out[k] = pack2((float)(int8_t)x * s, (float)(int8_t)(x >> 8) * s);
+        }
+        st_global_32(j.dst + row * j.plane + c, out);
+    }
+}
+
+template <typename T> __device__ __forceinline__ void prep_terms(const TermsJob &j, int block) {
+    // a warp per row, two neighbouring columns per lane
+    const int lane = threadIdx.x & 31;
+    auto rest = [](float v) {  // an infinity or NaN stays in the first term alone
+        const float h = bf16_round(v);
+        return isinf(h) || isnan(h) ? 0.f : v - h;
+    };
+    for (int row = block * 8 + (threadIdx.x >> 5); row < j.rows; row += j.blocks * 8) {
+        const T *from = (const T *)j.src + (size_t)row * j.cols;
+        bf16 *to = j.dst + (size_t)row * j.planes * j.plane;
+        const float rs = j.row_scale ? j.row_scale[row] : 1.f;
+#pragma unroll 4
+        for (int c = 2 * lane; c < j.plane; c += 64) {
+            float a = c < j.cols ? to_f(from[c]) * rs : 0.f, b = c + 1 < j.cols ? to_f(from[c + 1]) * rs : 0.f;
+            if (j.col_scale) {
+                if (c < j.cols) a *= j.col_scale[c];
+                if (c + 1 < j.cols) b *= j.col_scale[c + 1];
+            }
+            for (int p = 0; p < j.planes; ++p) {
+                *reinterpret_cast<uint32_t *>(to + (size_t)p * j.plane + c) = pack2(a, b);
+                a = rest(a);
+                b = rest(b);
+            }
+        }
+    }
+}
+
+// 64 columns of a chunk of rows per block; 8 values per thread where rows start on 16-byte boundaries, else one
+template <typename T> __device__ __forceinline__ void prep_sums(const SumsJob &j, int block) {
+    __shared__ float fold[32][65];
+    const int groups = (j.cols + 63) / 64, chunk = block / groups, c0 = (block - chunk * groups) * 64;
+    const int r0 = chunk * j.chunk, r1 = min(j.rows, r0 + j.chunk);
+    if (j.vec) {
+        constexpr int N = Vec16<T>::N;
+        const int lanes = 64 / N, l = threadIdx.x % lanes, r = threadIdx.x / lanes, step = 256 / lanes;  // 32 (bf16) or 16 rows at a time
+        float a[N] = {};
+        if (c0 + l * N < j.cols) {
+#pragma unroll 4
+            for (int row = r0 + r; row < r1; row += step) {
+                float v[N];
+                load_f<T, N>((const T *)j.src + (size_t)row * j.cols + c0 + l * N, v);
+#pragma unroll
+                for (int k = 0; k < N; ++k) a[k] += v[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) fold[r][l * N + k] = a[k];
+        __syncthreads();
+        if (threadIdx.x < 64 && c0 + (int)threadIdx.x < j.cols) {
+            float s = 0.f;
+            for (int k = 0; k < step; ++k) s += fold[k][threadIdx.x];
+            j.part[(size_t)chunk * j.cols + c0 + threadIdx.x] = s;
+        }
+    } else {
+        const int l = threadIdx.x & 63, r = threadIdx.x >> 6;
+        float a = 0.f;
+        if (c0 + l < j.cols) {
+#pragma unroll 4
+            for (int row = r0 + r; row < r1; row += 4) a += to_f(((const T *)j.src)[(size_t)row * j.cols + c0 + l]);
+        }
+        fold[r][l] = a;
+        __syncthreads();
+        if (r == 0 && c0 + l < j.cols) j.part[(size_t)chunk * j.cols + c0 + l] = ((fold[0][l] + fold[1][l]) + fold[2][l]) + fold[3][l];
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(256) fc8_prep_kernel(const __grid_constant__ PrepArgs g) {
     pdl_launch();
     pdl_wait();
-    const int m0 = blockIdx.y * kT, n0 = blockIdx.x * kT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < K; k0 += 16) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < 16 * kT; i += 256) {
-            const int k = A_MN ? i / kT : i % 16, m = A_MN ? i % kT : i / 16;
-            sa[k][m] = k0 + k < K && m0 + m < M ? to_f(A_MN ? a[(size_t)(k0 + k) * lda + m0 + m] : a[(size_t)(m0 + m) * lda + k0 + k]) : 0.f;
-            const int kb = i / kT, n = i % kT;
-            sb[kb][n] = k0 + kb < K && n0 + n < N ? act8_value<T>(q[(size_t)(k0 + kb) * pitch + n0 + n], scale[k0 + kb]) : 0.f;
-        }
-        __syncthreads();
+    int block = blockIdx.x;
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty + 16 * i], sb[k][tx + 16 * j], acc[i][j]);
+    for (int k = 0; k < 2; ++k) {
+        if (block < g.codes[k].blocks) { prep_codes(g.codes[k], block); return; }
+        block -= g.codes[k].blocks;
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m < M && n < N) c[(size_t)m * N + n] = from_f<TC>(acc[i][j]);
-        }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (block < g.terms[k].blocks) { prep_terms<T>(g.terms[k], block); return; }
+        block -= g.terms[k].blocks;
+    }
+    prep_sums<T>(g.sums, block);
 }
 
-template <typename T> __global__ void __launch_bounds__(256) fc8_db_kernel(const T *__restrict__ dy, float *__restrict__ db, int B, int out) {
+// ---- after the products of the backward pass -------------------------------------------------------------------------
+// Sums of the parts of up to three results, in index order: dx and dW where their K range was split, db.
+struct JoinJob { const float *part; void *out; size_t stride, total; int parts, ld, cols, out_bf16, vec, blocks; };
+struct JoinArgs { JoinJob job[3]; };
+__global__ void __launch_bounds__(256) fc8_join_kernel(const __grid_constant__ JoinArgs g) {
+    pdl_launch();
+    pdl_wait();
+    int block = blockIdx.x, k = 0;
+    while (k < 2 && block >= g.job[k].blocks) block -= g.job[k++].blocks;
+    const JoinJob &j = g.job[k];
+    for (size_t i = (size_t)block * 256 + threadIdx.x; i < j.total; i += (size_t)j.blocks * 256) {  // groups of four columns
+        const size_t row = i / (j.ld / 4);
+        const int c = (int)(i - row * (j.ld / 4)) * 4;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < j.parts; ++s) {
+            const float4 q = *reinterpret_cast<const float4 *>(j.part + s * j.stride + row * j.ld + c);
+            v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+        }
+        const size_t at = row * j.cols + c;
+        if (j.vec && c + 4 <= j.cols) {
+            if (j.out_bf16) store_f<bf16, 4>((bf16 *)j.out + at, v); else store_f<float, 4>((float *)j.out + at, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < j.cols) {
+                    if (j.out_bf16) ((bf16 *)j.out)[at + e] = from_f<bf16>(v[e]); else ((float *)j.out)[at + e] = v[e];
+                }
+        }
+    }
+}
+// db alone: a column per thread and warp, parts in index order
+__global__ void __launch_bounds__(256) fc8_db_kernel(const float *__restrict__ part, float *__restrict__ db, int parts, int cols) {
     __shared__ float fold[8][32];
     pdl_launch();
     pdl_wait();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float a = 0.f;
-    if (c < out)
-        for (int r = w; r < B; r += 8) a += to_f(dy[(size_t)r * out + c]);
+    if (c < cols) {
+#pragma unroll 4
+        for (int i = w; i < parts; i += 8) a += part[(size_t)i * cols + c];
+    }
     fold[w][lane] = a;
     __syncthreads();
-    if (w == 0 && c < out) {
+    if (w == 0 && c < cols) {
         for (int i = 1; i < 8; ++i) a += fold[i][lane];
         db[c] = a;
     }
 }
 
-template <typename T, typename TW>
-int bwd_as(const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, int B, int in, int out, const Launch &s) {
-    const int pitch = act8_pitch(in);
-    int n = 0;
-    if (dx) {
-        launch_k(fc8_grad_kernel<T, T, false>, dim3((in + kT - 1) / kT, (B + kT - 1) / kT), 256, 0, s, (const T *)dy, (const int8_t *)wq, ws, (T *)dx, B, in, out, out, pitch);
-        ++n;
-    }
-    if (dW) {
-        launch_k(fc8_grad_kernel<T, TW, true>, dim3((in + kT - 1) / kT, (out + kT - 1) / kT), 256, 0, s, (const T *)dy, (const int8_t *)xq, xs, (TW *)dW, out, in, B, out, pitch);
-        ++n;
-    }
-    if (db) {
-        launch_k(fc8_db_kernel<T>, (out + 31) / 32, 256, 0, s, (const T *)dy, db, B, out);
-        ++n;
-    }
+// ---- host side -------------------------------------------------------------------------------------------------------
+int up(int v, int to) { return (v + to - 1) / to * to; }
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+int sm_count() {
+    int dev = 0, n = 148;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     return n;
 }
 
-}  // namespace
+thread_local int t_wait_polls = -1;  // polls of a bounded wait, for the calls of this thread (negative: the default)
 
-int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, const float *ws, const void *bias, void *y, int B, int in, int out, int y_f32, Launch s) {
-    const dim3 grid((out + kT - 1) / kT, (B + kT - 1) / kT);
-    const int pitch = act8_pitch(in);
-    if (prec == P_F32) launch_k(fc8_fwd_kernel<float, float>, grid, 256, 0, s, (const int8_t *)xq, xs, (const int8_t *)wq, ws, (const float *)bias, (float *)y, B, in, out, pitch);
-    else if (y_f32) launch_k(fc8_fwd_kernel<bf16, float>, grid, 256, 0, s, (const int8_t *)xq, xs, (const int8_t *)wq, ws, (const bf16 *)bias, (float *)y, B, in, out, pitch);
-    else launch_k(fc8_fwd_kernel<bf16, bf16>, grid, 256, 0, s, (const int8_t *)xq, xs, (const int8_t *)wq, ws, (const bf16 *)bias, (bf16 *)y, B, in, out, pitch);
+// Columns of the tiles of M x N (times splits): at most 256, as many tiles as that takes, alike.  Where that leaves CTA pairs
+// without work, narrower ones: half of a tile's loads, A's, stay.
+int mm_width(int M, int N, int splits) {
+    const long rows = (long)((M + kTile - 1) / kTile) * splits;
+    int best = kTile;
+    double least = 1e30;
+    for (int most = kTile; most >= kKBox; most /= 2) {
+        const int tiles = (N + most - 1) / most, width = ((N + tiles - 1) / tiles + kKBox - 1) / kKBox * kKBox;
+        const double t = (double)((rows * tiles + kPairs - 1) / kPairs) * (0.5 + 0.5 * width / kTile);
+        if (t < 0.98 * least) { least = t; best = width; }
+        if (rows * tiles >= kPairs) break;
+    }
+    return best;
+}
+// Rounds of the GPU's CTA pairs that the tiles (times splits) take, in units of a 256 x 256 tile of the whole K.
+double mm_rounds(int M, int N, int splits) {
+    const int width = mm_width(M, N, splits);
+    const long items = (long)((M + kTile - 1) / kTile) * ((N + width - 1) / width) * splits;
+    return (double)((items + kPairs - 1) / kPairs) * (0.5 + 0.5 * width / kTile) / splits;
+}
+// Splits of K (steps of 128 values), where the tiles alone fill the GPU badly; each costs a write and a read of its sums.
+// Seconds by 1.4 PFLOP/s and 6 TB/s.
+int mm_splits(int M, int N, int steps) {
+    const long tiles = (long)((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+    const int most = (int)std::max<long>(1, std::min<long>(2 * kPairs / tiles, steps / 4));
+    int best = 1;
+    double least = 1e30;
+    for (int i = 1; i <= 10; ++i) {  // 1 to 8, and one or two rounds of pairs
+        const int n = (int)std::min<long>(most, i <= 8 ? i : (i - 8) * kPairs / std::max<long>(1, tiles));
+        if (n < 1) continue;
+        const double t = mm_rounds(M, N, n) * 2.0 * kTile * kTile * 128.0 * steps * kPairs / 1.4e15 + (n > 1 ? 3e-6 + 8.0 * n * M * up(N, 4) / 6e12 : 0.0);
+        if (t < least) { least = t; best = n; }
+    }
+    return best;
+}
+
+// An operand: a row-major matrix in memory; ld: elements from a row to the next.
+struct Operand { const void *ptr; int rows, cols; size_t ld; };
+
+// most_chain: K values of a chain (with PROMOTE)
+template <int MODE, bool A_MN, bool B_MN, bool PROMOTE>
+int mm_launch_as(const Operand &a, const Operand &b, MmArgs &g, int K, int most_chain, const Launch &s) {
+    constexpr bool kI8 = MODE == kForward;
+    constexpr int es = kI8 ? 1 : 2, kw = kStageKw / es;
+    constexpr CUtensorMapDataType type = kI8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    g.kblocks = (K + kw - 1) / kw;
+    g.tail = (K - (g.kblocks - 1) * kw + 32 / es - 1) / (32 / es);
+    g.piece = most_chain / kw;
+    g.tiles_m = (g.M + kTile - 1) / kTile;
+    g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
+    g.width = mm_width(g.M, g.N, g.splits);
+    g.tiles_n = (g.N + g.width - 1) / g.width;
+    g.group_m = 16;
+    const int b_rows = g.width / 2;
+    g.b_bytes = (B_MN ? up(b_rows, kKBox) : b_rows) * kStageKw;
+    const long items = (long)g.tiles_m * g.tiles_n * g.splits;
+    if (items > 0x7fffffff) return -1;
+    CUtensorMap ma, mb, mo{};
+    if (!box_map(type, es, a.ptr, a.rows, a.cols, a.ld, A_MN ? kw : kHalf, &ma) || !box_map(type, es, b.ptr, b.rows, b.cols, b.ld, B_MN ? kw : b_rows, &mb)) return -1;
+    if (g.store == kBoxes &&
+        !box_map(g.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, g.out_bf16 ? 2 : 4, g.out, g.M, g.N, g.ld, 32, &mo)) return -1;
+    static thread_local int ready_dev = -1;  // the attribute belongs to a device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
+        ready_dev = dev;
+    }
+    g.polls = t_wait_polls >= 0 ? (unsigned)t_wait_polls : kSpinLimit;
+    launch_k(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, 2 * (int)std::min<long>(items, sm_count() / 2), kThreads, kSmem, s, ma, mb, mo, g);
     return 1;
 }
 
-size_t fc8_workspace_bytes(int, int, int, int) { return 256; }
+// Where the results go: whole results by a tensor map when their rows keep to 16 bytes.
+void mm_out(MmArgs &g, void *out, bool is_bf16, int ld) {
+    g.out = out; g.out_bf16 = is_bf16; g.ld = ld;
+    g.store = g.splits == 1 && ld * (is_bf16 ? 2 : 4) % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 ? kBoxes : kRows;
+}
 
-int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, void *, int B, int in, int out,
+struct BwdPlan {
+    int planes;              // bf16 terms of dy
+    bool copy_dy;            // dy is not read in place: fp32, or rows that TMA cannot read
+    int plane_in, plane_out; // columns of a row of codes as bf16, of a term of dy
+    int dx_splits, dw_splits, ld;
+    int chunk, chunks;       // rows of dy that are summed up at a time for db
+    size_t x, w, dy[2], dx, dw, db, bytes;
+};
+BwdPlan bwd_plan(int prec, int B, int in, int out) {
+    BwdPlan p{};
+    p.planes = prec == P_F32 ? kMostPlanes : 1;
+    p.plane_in = up(in, 64);
+    p.plane_out = prec == P_F32 ? up(out, 128) : up(out, 64);  // fp32: a K block never reaches into the next term
+    p.ld = up(in, 4);
+    const int kw = kStageKw / 2;
+    p.dx_splits = mm_splits(B, in, (out + kw - 1) / kw * p.planes);
+    p.dw_splits = mm_splits(out, in, (B + kw - 1) / kw * p.planes);
+    p.chunk = std::max(64, (B + 127) / 128);
+    p.chunks = (B + p.chunk - 1) / p.chunk;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
+    p.x = take((size_t)B * p.plane_in * 2);
+    p.w = take((size_t)out * p.plane_in * 2);
+    for (int k = 0; k < (prec == P_F32 ? 2 : 1); ++k) p.dy[k] = take((size_t)B * p.planes * p.plane_out * 2);  // also for a bf16 dy that starts anywhere
+    if (p.dx_splits > 1) p.dx = take((size_t)p.dx_splits * B * p.ld * 4);
+    if (p.dw_splits > 1) p.dw = take((size_t)p.dw_splits * out * p.ld * 4);
+    p.db = take((size_t)p.chunks * out * 4);
+    p.bytes = at;
+    return p;
+}
+
+int blocks_for(size_t threads) { return (int)std::max<size_t>(1, std::min<size_t>((threads + 255) / 256, 148 * 8)); }
+
+}  // namespace
+
+void fc8_wait_polls(int polls) { t_wait_polls = polls; }
+
+int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, const float *ws, const void *bias, void *y, int B, int in, int out, int y_f32, Launch s) {
+    const int pitch = act8_pitch(in);
+    MmArgs g{};
+    g.M = B; g.N = out; g.n_seg = 1; g.splits = 1;
+    g.row_scale = xs; g.col_scale = ws; g.bias = bias; g.bias_bf16 = prec == P_BF16;
+    mm_out(g, y, prec == P_BF16 && !y_f32, out);
+    return mm_launch_as<kForward, false, false, false>(Operand{xq, B, in, (size_t)pitch}, Operand{wq, out, in, (size_t)pitch}, g, in, in, s);
+}
+
+size_t fc8_workspace_bytes(int prec, int B, int in, int out) { return bwd_plan(prec, B, in, out).bytes; }
+
+int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, void *ws_mem, int B, int in, int out,
                    int dw_f32, Launch s) {
-    if (prec == P_F32) return bwd_as<float, float>(dy, xq, xs, wq, ws, dx, dW, db, B, in, out, s);
-    return dw_f32 ? bwd_as<bf16, float>(dy, xq, xs, wq, ws, dx, dW, db, B, in, out, s) : bwd_as<bf16, bf16>(dy, xq, xs, wq, ws, dx, dW, db, B, in, out, s);
+    const BwdPlan p = bwd_plan(prec, B, in, out);
+    uint8_t *base = (uint8_t *)ws_mem;
+    const int pitch = act8_pitch(in);
+    const bool f32 = prec == P_F32, aligned = (reinterpret_cast<uintptr_t>(dy) & 15) == 0, copy = f32 || out % 8 != 0 || !aligned;
+    PrepArgs prep{};
+    int n = 0, blocks = 0;
+    auto codes = [&](int k, const void *q, const float *scale, size_t at, int rows) {
+        prep.codes[k] = CodesJob{(const int8_t *)q, f32 ? nullptr : scale, (bf16 *)(base + at), rows, pitch, p.plane_in, blocks_for((size_t)rows * (pitch / 16))};
+        blocks += prep.codes[k].blocks;
+    };
+    auto terms = [&](int k, const float *row_scale, const float *col_scale) {
+        prep.terms[k] = TermsJob{dy, (bf16 *)(base + p.dy[k]), row_scale, col_scale, B, out, p.plane_out, p.planes, blocks_for((size_t)B * 32)};
+        blocks += prep.terms[k].blocks;
+    };
+    if (dx) codes(0, wq, ws, p.w, out);
+    if (dW) codes(1, xq, xs, p.x, B);
+    if (f32) {
+        if (dx) terms(0, nullptr, ws);
+        if (dW) terms(1, xs, nullptr);
+    } else if (copy && (dx || dW)) {
+        terms(0, nullptr, nullptr);
+    }
+    if (db) {
+        prep.sums = SumsJob{dy, (float *)(base + p.db), B, out, p.chunk, p.chunks * ((out + 63) / 64), out % (f32 ? 4 : 8) == 0 && aligned};
+        blocks += prep.sums.blocks;
+    }
+    if (f32) launch_k(fc8_prep_kernel<float>, blocks, 256, 0, s, prep); else launch_k(fc8_prep_kernel<bf16>, blocks, 256, 0, s, prep);
+    ++n;
+    const int dy_cols = copy ? (f32 ? p.planes * p.plane_out : out) : out;
+    const size_t dy_ld = copy ? (size_t)p.planes * p.plane_out : (size_t)out;
+    auto operand = [&](int k) { return Operand{copy ? base + p.dy[f32 ? k : 0] : dy, B, dy_cols, dy_ld}; };
+    auto segments = [&](MmArgs &g) {  // the smallest terms first
+        g.n_seg = p.planes;
+        for (int i = 0; i < p.planes; ++i) g.a_off[i] = (p.planes - 1 - i) * p.plane_out;
+    };
+    JoinArgs join{};
+    int join_blocks = 0, joins = 0;
+    auto joined = [&](const MmArgs &g, size_t part, void *to, bool is_bf16) {
+        const size_t total = (size_t)g.M * (g.ld / 4);
+        join.job[joins++] = JoinJob{(const float *)(base + part), to, g.out_split, total, g.splits, g.ld, in, is_bf16, in % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & (is_bf16 ? 7 : 15)) == 0,
+                                    blocks_for(total)};
+        join_blocks += join.job[joins - 1].blocks;
+    };
+    auto product = [&](auto a_mn, const Operand &a, const Operand &b, int M, int K, int splits, size_t part, void *to, bool is_bf16) {
+        constexpr bool A_MN = decltype(a_mn)::value;
+        MmArgs g{};
+        g.M = M; g.N = in; g.splits = splits;
+        segments(g);
+        if (splits > 1) {
+            g.splits = splits;
+            mm_out(g, base + part, false, p.ld);
+            g.out_split = (size_t)M * p.ld;
+        } else {
+            mm_out(g, to, is_bf16, in);
+        }
+        const int most = is_bf16 ? kPieceOut : kPieceF32;
+        const int r = (long)K * g.n_seg / splits > most ? mm_launch_as<kGrad, A_MN, true, true>(a, b, g, K, most, s) : mm_launch_as<kGrad, A_MN, true, false>(a, b, g, K, most, s);
+        if (r > 0 && splits > 1) joined(g, part, to, is_bf16);
+        return r;
+    };
+    const bool dw_bf16 = !f32 && !dw_f32;
+    int r;
+    if (dx) {
+        if ((r = product(std::false_type{}, operand(0), Operand{base + p.w, out, in, (size_t)p.plane_in}, B, out, p.dx_splits, p.dx, dx, !f32)) < 0) return r;
+        n += r;
+    }
+    if (dW) {
+        if ((r = product(std::true_type{}, operand(1), Operand{base + p.x, B, in, (size_t)p.plane_in}, out, B, p.dw_splits, p.dw, dW, dw_bf16)) < 0) return r;
+        n += r;
+    }
+    if (join_blocks) {
+        launch_k(fc8_join_kernel, join_blocks, 256, 0, s, join);
+        ++n;
+    }
+    if (db) {
+        launch_k(fc8_db_kernel, (out + 31) / 32, 256, 0, s, (const float *)(base + p.db), db, p.chunks, out);
+        ++n;
+    }
+    return n;
 }
 
 }  // namespace ddg

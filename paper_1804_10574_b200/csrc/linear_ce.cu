@@ -41,15 +41,13 @@
 #include "common.cuh"
 #include "conv_tc.h"
 #include "lm_ops.h"
+#include "pair_mma.cuh"
 #include "tc_common.cuh"
 
 namespace ddg {
 
 namespace {
 
-constexpr int kTile = 256;        // rows of a tile of the CTA pair, columns of an accumulator
-constexpr int kHalf = 128;        // rows of A, and of B per accumulator, that one CTA of the pair loads
-constexpr int kKBox = 64;         // K values of a box: 128 bytes of bf16, one swizzle row
 // A stage, per CTA: 128 rows of A and 128 or 256 of B, 128 or 64 K values wide.  The thread that issues the products spends
 // a few hundred cycles on a stage (two barriers, eight descriptors), which has to stay below the 1024 cycles that they
 // take: with 64 K values the narrow tile kept the tensor cores 80 % busy (4096 x 1024 x 32000), with 128 91 %.
@@ -62,7 +60,6 @@ template <int NT> struct Stage {  // NT: columns of a tile
 constexpr int kEpiWarps = 8;      // two per TMEM lane quarter, each half of an accumulator's columns
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kStageRing = 192 * 1024;
-constexpr int kOutBuf = 32 * kKBox * 2;  // an epilogue warp's 32 rows of 64 bf16 values on their way out
 constexpr int kCeSmem = kStageRing + kEpiWarps * kOutBuf + 1024;
 constexpr int kMaxSeg = 6;
 // K values (times products) of a chain that need not be cut: for a 32-bit result of bf16 and of fp32 tensors, for a bf16 result
@@ -117,44 +114,6 @@ struct CeGemm {
     int pairs;                // CTA pairs of the launch
 };
 
-// Hands an accumulator back.  What it orders are the tcgen05 loads before the fence, not memory: a releasing arrival would
-// wait for the stores of the tile before (gradient of the logits, 4096 x 512 x 16384: 94 us with it, 89 us without).
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-// one half of a stage: lands in this CTA's shared memory, counts on the barrier of the pair's first CTA
-__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, uint32_t cluster_bar, int c0, int c1) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(c0), "r"(c1)
-        : "memory");
-}
-__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-__device__ __forceinline__ bool elect_one() {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
-    return ok != 0;
-}
-// arrives on the barrier at this offset in both CTAs when the MMAs issued so far are done
-__device__ __forceinline__ void commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
-// Waits for work that is known to be in flight, which ends by itself: the limit is there for broken hardware alone.
-__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
-    for (unsigned i = 0; i < kSpinLimit; ++i) {
-        if (mbar_try(bar, parity)) return;
-        if (i > 4096) __nanosleep(64);
-    }
-}
-constexpr uint32_t kGaveUp = 1u << 31;
 __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 // Which tile a work item is: all tiles of a split, in bands of group_m tile rows that are walked column by column, so
@@ -184,12 +143,6 @@ __device__ __forceinline__ CeTile ce_tile(const CeGemm &g, int item, int split) 
     return CeTile{(int)(band * g.group_m + r - n * rows), (int)n};
 }
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ float bf16_round(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
-
 __device__ __forceinline__ float load_bias(const void *bias, int is_bf16, int c) {
     return is_bf16 ? __bfloat162float(((const bf16 *)bias)[c]) : ((const float *)bias)[c];
 }
@@ -211,63 +164,6 @@ __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
 
 __device__ __forceinline__ void red_add4(float *p, float a, float b, float c, float d) {
     asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
-}
-
-// 64 columns of the warp's 32 rows as bf16 to (x, y) of a matrix, through shared memory: whole 128-byte lines leave by
-// TMA, and rows and columns past the matrix are clipped.  (Gradient of the logits, 4096 x 512 x 16384: 62 us; with stores
-// of 64 bytes a thread, straight from registers, 89 us.)
-__device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t buf, int lane, int x, int y, const float *v) {
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the box before has been read
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < 8; ++j)  // the 128-byte swizzle of the map
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(pack2(v[8 * j], v[8 * j + 1])),
-                     "r"(pack2(v[8 * j + 2], v[8 * j + 3])), "r"(pack2(v[8 * j + 4], v[8 * j + 5])), "r"(pack2(v[8 * j + 6], v[8 * j + 7]))
-                     : "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) {
-        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(buf), "r"(x), "r"(y) : "memory");
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-    }
-}
-
-// The same for matrices that a tensor map cannot write (rows off 16-byte boundaries, fp32): rows row0 .. of a [rows][n]
-// matrix, columns col .. col + 63 as far as there are; the lanes write neighbouring values of a row.  (7244 x 3955 x 223,
-// forward and backward: 230 us; with a row per lane, two bytes at a time, here and in the copies, 499 us.)
-template <bool BF16>
-__device__ __forceinline__ void store_rows(void *out, uint32_t buf, int lane, int row0, int rows, int col, int n, const float *v) {
-    const int last = min(32, rows - row0);
-#pragma unroll
-    for (int half = 0; half < (BF16 ? 1 : 2); ++half) {  // 128 bytes of a row at a time
-        __syncwarp();  // what stood there has been read
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float *f = v + (BF16 ? 8 * j : 32 * half + 4 * j);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(BF16 ? pack2(f[0], f[1]) : __float_as_uint(f[0])),
-                         "r"(BF16 ? pack2(f[2], f[3]) : __float_as_uint(f[1])), "r"(BF16 ? pack2(f[BF16 ? 4 : 0], f[BF16 ? 5 : 0]) : __float_as_uint(f[2])),
-                         "r"(BF16 ? pack2(f[BF16 ? 6 : 0], f[BF16 ? 7 : 0]) : __float_as_uint(f[3])) : "memory");
-        }
-        __syncwarp();
-        const int c = col + 32 * half + lane;
-#pragma unroll 4
-        for (int r = 0; r < last; ++r) {
-            const size_t at = (size_t)(row0 + r) * n + c;
-            if (BF16) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {  // columns lane and lane + 32
-                    const int e = lane + 32 * k;
-                    uint16_t w;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(buf + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2));
-                    if (c + 32 * k < n) reinterpret_cast<uint16_t *>(out)[at + 32 * k] = w;
-                }
-            } else {
-                float w;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
-                if (c < n) reinterpret_cast<float *>(out)[at] = w;
-            }
-        }
-    }
 }
 
 // What a thread knows of its row, and the softmax's running maximum and sum over the row's 128 columns.
@@ -1108,15 +1004,7 @@ CePlan ce_plan(int prec, int B, int in, int out, bool backward, bool dw_f32) {
 }
 
 bool ce_map(const void *ptr, int rows, int cols, size_t ld, int box_rows, CUtensorMap *out) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = tc_encode_fn();
-    if (!enc) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-    cuuint32_t box[2] = {(cuuint32_t)kKBox, (cuuint32_t)box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return box_map(CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ptr, rows, cols, ld, box_rows, out);
 }
 
 // An operand: a row-major bf16 matrix in memory.

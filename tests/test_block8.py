@@ -770,3 +770,30 @@ def test_block8_tensor_arguments_are_checked_in_the_binding(binding):
         a = {**dict(x=x, q=q), **bad}
         with pytest.raises(ValueError):
             binding.act8_pack(0, a["x"], a["q"], P, 4, 8)
+
+
+# ---- bounded waits --------------------------------------------------------------------------------------------------
+# every way of a call that waits on the device: one row, a few, tiles, with splits, with chains that are cut, fp32
+WAYS_THAT_WAIT = [(1, 4096, 700, 1), (20, 2048, 300, 1), (100, 4096, 640, 1), (300, 136, 777, 1), (700, 2200, 1100, 1), (300, 8200, 70, 1), (2100, 264, 1000, 0), (130, 72, 2057, 0)]
+
+
+@gpu
+@pytest.mark.parametrize("shape", WAYS_THAT_WAIT, ids=ids)
+def test_fc8_waits_that_run_out(binding, shape):
+    """With limits of few polls and of none, each kernel lets its copies and products land and returns; what was not computed is
+    NaN, the rest the usual bits; the calls after it are not touched."""
+    c = Fc(*shape, bias=True, seed=51)
+    step = lambda: [c.fwd(binding)] + [t for f in (False, True) for t in c.bwd(binding, "xw", f)[:2]]  # noqa: E731
+    ref = step()
+    try:
+        for polls in (0, 1, 2, 1, 4, 1, 8, 16, 50, 400, 0):
+            binding.debug_fc8_wait_polls(polls)
+            got = step()
+            torch.cuda.synchronize()
+            for a, b in zip(got, ref):
+                lost = torch.isnan(a)
+                assert torch.equal(torch.where(lost, b, a), b)
+                assert polls > 0 or bool(lost.all())
+    finally:
+        binding.debug_fc8_wait_polls(-1)
+    assert all(torch.equal(a, b) for a, b in zip(step(), ref))
