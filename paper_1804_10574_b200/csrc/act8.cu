@@ -54,15 +54,7 @@ __global__ void __launch_bounds__(rms_max_threads(VEC, ITER)) act8_pack_kernel(c
     for (int i = 0; i < ITER; ++i) {
         const int c = (i * tpr + t) * VEC;
         if (c < C) {
-            if (VEC == 1) {
-                to[c] = (int8_t)act8_code(v[i][0], r);
-            } else {
-                uint32_t w[(VEC + 3) / 4];
-#pragma unroll
-                for (int j = 0; j < VEC / 4; ++j) w[j] = act8_pack4(act8_code(v[i][4 * j], r), act8_code(v[i][4 * j + 1], r), act8_code(v[i][4 * j + 2], r), act8_code(v[i][4 * j + 3], r));
-                if (VEC == 8) *reinterpret_cast<uint2 *>(to + c) = make_uint2(w[0], w[VEC == 8 ? 1 : 0]);
-                else *reinterpret_cast<uint32_t *>(to + c) = w[0];
-            }
+            act8_store<sizeof(T) == 2, VEC>(to + c, v[i], r);
         }
     }
     for (int c = C + t; c < pitch; c += tpr) to[c] = 0;

@@ -3,7 +3,7 @@
 // scale of an fp32 row up to FLT_MAX is rounded down, so that 127 scale is finite.
 // A row that holds a NaN or an infinity has scale NaN and codes 0: all that is made of it is NaN.
 #pragma once
-#include "common.cuh"
+#include "f32x2.cuh"
 
 namespace ddg {
 
@@ -34,8 +34,77 @@ __device__ __forceinline__ int act8_code(float x, const Act8Row &r) {
     return (int)n;
 }
 
-__device__ __forceinline__ uint32_t act8_pack4(int a, int b, int c, int d) {
-    return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
+// N codes at once, in the words' bytes.  t = 127 x / m rounded by adding 1.5 x 2^23, which leaves the whole number in the sum's
+// low byte.
+//   BF16 (x and m are bf16 values): 127 x is exact (here 127 / 128 x, and m / 128), and the quotient corrected by its remainder (Markstein, 1990) is exactly a
+//   border where it is one, as x = m / 2 is, and else nearer to the quotient than any border (2^-17 at least).
+//   else: x inv, with one test for all of them whether a border is so near that it could decide; then they are formed in 64 bits.
+template <bool BF16, int N> __device__ __forceinline__ void act8_codes(const F2 (&x)[N / 2], const Act8Row &r, uint32_t (&w)[(N + 3) / 4]) {
+    constexpr float kRound = 12582912.f;
+    const F2 inv = f2(r.inv), up = f2(kRound);
+    uint32_t n[N];
+    float off = 0.f;
+    const F2 inv_m = f2(r.inv * (128.f / 127.f)), neg_m = f2(-r.top * 0x1p-7f), by = f2(127.f * 0x1p-7f);  // all by 2^-7: nothing overflows
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+        F2 t;
+        if (BF16) {
+            const F2 x127 = x[k] * by;
+            t = x127 * inv_m;
+            t = fma2(fma2(t, neg_m, x127), inv_m, t);
+        } else {
+            t = x[k] * inv;
+        }
+        const F2 s = t + up;
+        const float2 sp = parts(s);
+        n[2 * k] = __float_as_uint(sp.x);
+        n[2 * k + 1] = __float_as_uint(sp.y);
+        if (!BF16) {
+            const float2 d = parts(fma2(s + f2(-kRound), f2(-1.f), t));
+            off = fmaxf(off, fmaxf(fabsf(d.x), fabsf(d.y)));
+        }
+    }
+    if (!BF16 && off > 0.5f - 0x1p-13f) {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) {
+            const float2 p = parts(x[k]);
+            n[2 * k] = (uint32_t)act8_code(p.x, r);
+            n[2 * k + 1] = (uint32_t)act8_code(p.y, r);
+        }
+    }
+    const uint32_t keep = r.inv == 0.f ? 0u : 0xffffffffu;  // a row of codes 0, whatever stands in it
+#pragma unroll
+    for (int k = 0; k < N; k += 4)
+        w[k / 4] = keep & __byte_perm(__byte_perm(n[k], n[k + 1], 0x0040), N > 2 ? __byte_perm(n[N > 2 ? k + 2 : 0], n[N > 2 ? k + 3 : 0], 0x0040) : 0u, 0x5410);
+}
+
+// VEC codes, 1, 4 or 8, on a boundary of as many bytes.
+template <bool BF16, int VEC> __device__ __forceinline__ void act8_store(int8_t *to, const float (&v)[VEC], const Act8Row &r) {
+    if constexpr (VEC == 1) {
+        *to = (int8_t)act8_code(v[0], r);
+    } else {
+        F2 x[VEC / 2];
+        uint32_t w[VEC / 4];
+#pragma unroll
+        for (int j = 0; j < VEC / 2; ++j) x[j] = f2(v[2 * j], v[2 * j + 1]);
+        act8_codes<BF16, VEC>(x, r, w);
+        if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(to) = w[0];
+    }
+}
+
+// A thread's pairs (see row_ring.cuh) to a row of codes.
+template <bool BF16, int VEC, int ITER> __device__ __forceinline__ void act8_share_store(int8_t *row, int C, const F2 (&v)[VEC * ITER / 2], const Act8Row &r) {
+    uint32_t w[(VEC * ITER + 3) / 4];
+    act8_codes<BF16, VEC * ITER>(v, r, w);
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int c = (i * blockDim.x + threadIdx.x) * VEC;
+        if (c >= C) continue;
+        if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[2 * i], w[2 * i + 1]);
+        else if constexpr (VEC == 4) *reinterpret_cast<uint32_t *>(row + c) = w[i];
+        else row[c] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+    }
 }
 
 // What a code stands for, in the element type.

@@ -16,6 +16,7 @@
 #include "common.cuh"
 #include "lm_ops.h"
 #include "row_io.cuh"
+#include "row_ring.cuh"
 
 namespace ddg {
 
@@ -111,20 +112,132 @@ block_norm_fwd_kernel(const T *b, const T *res, const T *__restrict__ gate, cons
     for (int i = 0; i < ITER; ++i) {
         const int c = (i * tpr + t) * VEC - phase;
         if (c < C) {
-            int k[VEC];
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) k[j] = act8_code(v[i][j], code);
-            if (SHIFT || VEC == 1) {
+            if (SHIFT) {
 #pragma unroll
                 for (int j = 0; j < VEC; ++j)
-                    if (c + j >= 0 && c + j < C) to[c + j] = (int8_t)k[j];
+                    if (c + j >= 0 && c + j < C) to[c + j] = (int8_t)act8_code(v[i][j], code);
             } else {
-#pragma unroll
-                for (int j = 0; j < VEC / 4; ++j) *reinterpret_cast<uint32_t *>(to + c + 4 * j) = act8_pack4(k[4 * j], k[VEC > 1 ? 4 * j + 1 : 0], k[VEC > 1 ? 4 * j + 2 : 0], k[VEC > 1 ? 4 * j + 3 : 0]);
+                act8_store<false, VEC>(to + c, v[i], code);
             }
         }
     }
     for (int c = C + t; c < pitch; c += tpr) to[c] = 0;
+}
+
+struct BlockNormFwd {
+    const void *b, *res, *gate, *post, *pre;
+    void *h, *y;
+    int8_t *q;
+    float *scale, *rstd_post, *rstd_pre;
+    int rows, C, pitch, span;
+    float alpha, eps;
+};
+
+// The same for many rows: resident blocks walk stretches of them, the rows ahead on their way through shared memory.
+template <typename T, int VEC, int ITER>
+__global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __grid_constant__ BlockNormFwd g, const __grid_constant__ RingShape shape) {
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    __shared__ uint64_t full[kRingMostStages];
+    __shared__ __align__(16) float red[6][32];
+    __shared__ int abort_flag;
+    const int threads = blockDim.x, t = threadIdx.x, C = g.C;
+    RowRing<2> ring(shape, smem_u32(ring_smem), full, &abort_flag);
+    if (t == 0) ring.init();
+    if (t < 32) {
+#pragma unroll
+        for (int k = 0; k < 6; ++k) red[k][t] = 0.f;
+    }
+    __syncthreads();
+    pdl_launch();
+    pdl_wait();
+    const int first = (int)((long)g.rows * blockIdx.x / gridDim.x), last = (int)((long)g.rows * (blockIdx.x + 1) / gridDim.x);
+    const void *const src[2] = {g.b, g.res};
+    if (t == 0)
+        for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, src);
+    constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
+    typedef Share<T, VEC, ITER> Row;
+    Row pre;
+    F2 pg[P];   // gamma_post times the gate
+    pre.load((const T *)g.pre, C);
+    int left = 0;  // rows that pg is for
+    const float inv_c = 1.f / (float)C;
+    const F2 alpha = f2(g.alpha);
+    uint32_t round = 0;
+    for (int row = first; row < last; ++row) {
+        if (left == 0) {
+            Row w;
+            w.load((const T *)g.post, C);
+#pragma unroll
+            for (int k = 0; k < P; ++k) pg[k] = w.pair(k);
+            left = 1 << 30;
+            if (g.gate) {
+                w.load((const T *)g.gate + (size_t)(row / g.span) * C, C);
+#pragma unroll
+                for (int k = 0; k < P; ++k) pg[k] = pg[k] * w.pair(k);
+                left = g.span - row % g.span;
+            }
+        }
+        --left;
+        const bool ok = ring.wait();
+        const size_t start = (size_t)row * C;
+        const uint32_t slot_b = ring.slot(0), slot_res = ring.slot(1);
+        const RingRow at = ring_row(shape, row);
+        ring.next();
+        F2 v[P], s2 = f2(0.f);
+        float sum[1];
+#pragma unroll
+        for (int i = 0; i < P / G; ++i) {
+            F2 in[G];
+            slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, i, in);
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                v[i * G + j] = in[j];
+                s2 = fma2(in[j], in[j], s2);
+            }
+        }
+        sum[0] = ok ? sum2(s2) : __int_as_float(0x7fffffff);  // a row that did not come is NaN
+        ring_sum<1>(sum, red, round);
+        if (t == 0 && row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, src);
+        const float r1 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
+        s2 = f2(0.f);
+#pragma unroll
+        for (int i = 0; i < P / G; ++i) {
+            F2 res[G];
+            slot_load<T, VEC>(slot_res, at, (const T *)g.res + start, C, i, res);
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                const int k = i * G + j;
+                res[j] = v[k] = fma2(alpha, res[j], v[k] * f2(r1) * pg[k]);
+                s2 = fma2(v[k], v[k], s2);
+            }
+            group_store<T, VEC>((T *)g.h + start, C, i, res);
+        }
+        sum[0] = sum2(s2);
+        ring_sum<1>(sum, red, round);
+        const float r2 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
+        if (t == 0) {
+            if (g.rstd_post) g.rstd_post[row] = r1;
+            if (g.rstd_pre) g.rstd_pre[row] = r2;
+        }
+#pragma unroll
+        for (int k = 0; k < P; ++k) v[k] = v[k] * f2(r2) * pre.pair(k);
+        if (g.y) share_store<T, VEC, ITER>((T *)g.y + start, C, v);
+        if (!g.q) continue;
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const float2 p = parts(v[k]);
+            top = max(top, max(__float_as_uint(p.x) & 0x7fffffffu, __float_as_uint(p.y) & 0x7fffffffu));
+        }
+        top = ring_max(top, red, round);
+        float s;
+        const Act8Row code = act8_row(top, s);
+        if (t == 0) g.scale[row] = s;
+        int8_t *to = g.q + (size_t)row * g.pitch;
+        act8_share_store<false, VEC, ITER>(to, C, v, code);
+        for (int c = C + t; c < g.pitch; c += threads) to[c] = 0;
+    }
+    if (t == 0) ring.drain();
 }
 
 struct BlockNormBwd {
@@ -137,8 +250,17 @@ struct BlockNormBwd {
     int rows, C, span, gates;
     int parts;        // a gate's rows are worked in so many stretches
     int per_block;    // a stretch is a block's, else (rows that are one warp's) a warp's
+    int several;      // a block may have more than one stretch
     float alpha;
 };
+
+// Rows [r0, r1) of a stretch.  The last gate's may be fewer than its stretches, so that some are empty.
+__device__ __forceinline__ void norm_stretch(const BlockNormBwd &g, int unit, int &gate, int &r0, int &r1) {
+    gate = unit / g.parts;
+    const int part = unit - gate * g.parts, first = gate * g.span, len = min(g.span, g.rows - first);
+    r0 = first + (int)((long)len * part / g.parts);
+    r1 = first + (int)((long)len * (part + 1) / g.parts);
+}
 
 // Three sums over the threads of a row.
 __device__ __forceinline__ void row_sum3(float (&v)[3], bool one_warp, float (*red)[32]) {
@@ -193,9 +315,8 @@ __global__ void __launch_bounds__(WARP ? 256 : rms_max_threads(VEC, ITER), 1) bl
     };
     const int units = g.gates * g.parts, walkers = own ? gridDim.x * warps : gridDim.x;
     for (int unit = own ? blockIdx.x * warps + warp : blockIdx.x; unit < units; unit += walkers) {
-        const int gate = unit / g.parts, part = unit - gate * g.parts;
-        const int first = gate * g.span, len = min(g.span, g.rows - first);
-        const int r0 = first + (int)((long)len * part / g.parts), r1 = first + (int)((long)len * (part + 1) / g.parts);
+        int gate, r0, r1;
+        norm_stretch(g, unit, gate, r0, r1);
         const T *gate_row = g.gate ? (const T *)g.gate + (size_t)gate * C : nullptr;
 #pragma unroll
         for (int i = 0; i < ITER; ++i)
@@ -260,6 +381,162 @@ __global__ void __launch_bounds__(WARP ? 256 : rms_max_threads(VEC, ITER), 1) bl
     leave(a_pre, g.part + (size_t)blockIdx.x * 2 * C + C, WARP);
 }
 
+// The rows of a block, one after the other.
+struct NormRows {
+    const BlockNormBwd &g;
+    int unit, row, end;
+    __device__ __forceinline__ explicit NormRows(const BlockNormBwd &a) : g(a), unit(blockIdx.x) { enter(); }
+    __device__ __forceinline__ bool more() const { return unit < g.gates * g.parts; }
+    __device__ __forceinline__ void enter() {
+        for (; more(); unit += gridDim.x) {
+            int gate;
+            norm_stretch(g, unit, gate, row, end);
+            if (row < end) return;
+        }
+    }
+    __device__ __forceinline__ void next() {
+        if (++row < end) return;
+        unit += gridDim.x;
+        enter();
+    }
+};
+
+// The same for many wide rows: stretches of rows that share a gate are dealt out to resident blocks, the rows ahead on their
+// way through shared memory.  Over a stretch one sum per column, of t b rstd_post, gives both dgate (times gamma_post) and
+// the stretch's share of dgamma_post (times the gate).
+template <typename T, int VEC, int ITER>
+__global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __grid_constant__ BlockNormBwd g, const __grid_constant__ RingShape shape) {
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    __shared__ uint64_t full[kRingMostStages];
+    __shared__ __align__(16) float red[6][32];
+    __shared__ int abort_flag;
+    const int threads = blockDim.x, t = threadIdx.x, C = g.C;
+    // share of dgamma_post over several stretches: [C], a thread its own columns
+    float *const a_post = g.several ? reinterpret_cast<float *>(ring_smem + (size_t)shape.stages * 4 * shape.slot_bytes) : nullptr;
+    if (a_post)
+        for (int c = t; c < C; c += threads) a_post[c] = 0.f;  // (a barrier follows)
+    RowRing<4> ring(shape, smem_u32(ring_smem), full, &abort_flag);
+    if (t == 0) ring.init();
+    if (t < 32) {
+#pragma unroll
+        for (int k = 0; k < 6; ++k) red[k][t] = 0.f;
+    }
+    __syncthreads();
+    pdl_launch();
+    pdl_wait();
+    const void *const src[4] = {g.dy, g.h, g.b, g.dh};
+    NormRows ahead(g);
+    if (t == 0)
+        for (int i = 0; i < shape.stages && ahead.more(); ++i, ahead.next()) ring.copy(ahead.row, src);
+    constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
+    typedef Share<T, VEC, ITER> Row;
+    Row pre;
+    F2 a_pre[P], a_unit[P], pg[P];  // pg: gamma_post times the gate
+    pre.load((const T *)g.pre, C);
+#pragma unroll
+    for (int k = 0; k < P; ++k) a_pre[k] = f2(0.f);
+    const float inv_c = 1.f / (float)C;
+    const F2 alpha = f2(g.alpha);
+    uint32_t round = 0;
+    bool begun = false;  // there is a row before this one
+    for (int unit = blockIdx.x; unit < g.gates * g.parts; unit += gridDim.x) {
+        int gate, r0, r1;
+        norm_stretch(g, unit, gate, r0, r1);
+        const T *gate_row = g.gate ? (const T *)g.gate + (size_t)gate * C : nullptr;
+        {
+            Row w;
+            w.load((const T *)g.post, C);
+#pragma unroll
+            for (int k = 0; k < P; ++k) pg[k] = w.pair(k);
+            if (gate_row) {
+                w.load(gate_row, C);
+#pragma unroll
+                for (int k = 0; k < P; ++k) pg[k] = pg[k] * w.pair(k);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < P; ++k) a_unit[k] = f2(0.f);
+        for (int row = r0; row < r1; ++row) {
+            const float s1 = g.rstd_post[row], s2 = g.rstd_pre[row];
+            const bool ok = ring.wait();
+            const uint32_t slot_dy = ring.slot(0), slot_h = ring.slot(1), slot_b = ring.slot(2), slot_dh = ring.slot(3);
+            const RingRow at = ring_row(shape, row);
+            const size_t start = (size_t)row * C;
+            ring.next();
+            F2 q0 = f2(0.f), q1 = f2(0.f), q2 = f2(0.f), dy[G], h[G], b[G], dh[G];
+            auto load = [&](int i) {
+                slot_load<T, VEC>(slot_dy, at, (const T *)g.dy + start, C, i, dy);
+                slot_load<T, VEC>(slot_h, at, (const T *)g.h + start, C, i, h);
+                slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, i, b);
+                if (g.dh) slot_load<T, VEC>(slot_dh, at, (const T *)g.dh + start, C, i, dh);
+            };
+#pragma unroll
+            for (int i = 0; i < P / G; ++i) {
+                load(i);
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    const F2 w2 = pre.pair(i * G + j) * dy[j], w = pg[i * G + j] * b[j];
+                    const F2 base = g.dh ? fma2(f2(s2), w2, dh[j]) : f2(s2) * w2;
+                    q0 = fma2(w2, h[j], q0);
+                    q1 = fma2(w, base, q1);
+                    q2 = fma2(w, h[j], q2);
+                }
+            }
+            float sum[3] = {ok ? sum2(q0) : __int_as_float(0x7fffffff), sum2(q1), sum2(q2)};  // a row that did not come is NaN
+            ring_sum<3>(sum, red, round);
+            if (t == 0 && begun && ahead.more()) {
+                ring.copy(ahead.row, src);
+                ahead.next();
+            }
+            begun = true;
+            const float c2 = sum[0] * inv_c * s2 * s2 * s2, c1 = (sum[1] - c2 * sum[2]) * inv_c * s1 * s1;
+#pragma unroll
+            for (int i = 0; i < P / G; ++i) {
+                load(i);
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    const int k = i * G + j;
+                    const F2 x = b[j] * f2(s1), ds = pre.pair(k) * dy[j];
+                    const F2 base = g.dh ? fma2(f2(s2), ds, dh[j]) : f2(s2) * ds;
+                    const F2 tt = fma2(f2(-c2), h[j], base);
+                    a_unit[k] = fma2(tt, x, a_unit[k]);
+                    a_pre[k] = fma2(dy[j], h[j] * f2(s2), a_pre[k]);
+                    b[j] = fma2(pg[k], f2(s1) * tt, f2(-c1) * x);
+                    h[j] = alpha * tt;
+                }
+                group_store<T, VEC>((T *)g.dres + start, C, i, h);
+                group_store<T, VEC>((T *)g.db + start, C, i, b);
+            }
+        }
+        // the stretch's one sum times the gate: its share of dgamma_post; times gamma_post: dgate's
+        const bool final = unit + gridDim.x >= g.gates * g.parts;
+        Row w;
+        if (gate_row) w.load(gate_row, C);
+        F2 v[P];
+#pragma unroll
+        for (int k = 0; k < P; ++k) v[k] = gate_row ? w.pair(k) * a_unit[k] : a_unit[k];
+        if (a_post) {
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const int c = VEC > 1 ? ((2 * k / VEC) * threads + t) * VEC + 2 * k % VEC : 2 * k * threads + t, d = VEC > 1 ? c + 1 : c + threads;  // columns of the pair
+                if (c < C) v[k] = f2(a_post[c], d < C ? a_post[d] : 0.f) + v[k];
+                const float2 p = parts(v[k]);
+                if (c < C) a_post[c] = p.x;
+                if (d < C) a_post[d] = p.y;
+            }
+        }
+        if (final) share_store_f32<VEC, ITER>(g.part + (size_t)blockIdx.x * 2 * C, C, v);
+        if (g.dgate) {
+            w.load((const T *)g.post, C);
+#pragma unroll
+            for (int k = 0; k < P; ++k) a_unit[k] = a_unit[k] * w.pair(k);
+            share_store_f32<VEC, ITER>(g.parts > 1 ? g.piece + (size_t)unit * C : g.dgate + (size_t)gate * C, C, a_unit);
+        }
+    }
+    share_store_f32<VEC, ITER>(g.part + (size_t)blockIdx.x * 2 * C + C, C, a_pre);
+    if (t == 0) ring.drain();
+}
+
 // Shares in index order per warp, warps in index order, 32 columns per block.  blockIdx.y: dpost, dpre, then the gate's rows.
 __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const float *__restrict__ part, const float *__restrict__ piece, int blocks, int parts, float *__restrict__ dpost,
                                                                float *__restrict__ dpre, float *__restrict__ dgate, int C) {
@@ -283,23 +560,44 @@ __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const float *__re
     }
 }
 
+// Whether the rows go through shared memory, by how many threads each (`iter` vectors of a row per thread), and in how many
+// blocks per SM.  A row's reductions cost every one of its warps about as much as 200 values, so that few warps a row and several
+// rows at a time are faster than a whole SM per row.
+constexpr size_t kRingSmem = 216 * 1024;
+struct RingPlan { int threads, iter, per_sm; size_t smem; };
+RingPlan ring_plan(int rows, int C, int vec, int es, int tensors) {
+    RingPlan p{};
+    if (rows < 2 * 148) return p;
+    p.iter = vec == 1 ? 8 : (tensors == 2 ? 4 : 2);
+    const int threads = ring_threads((C + vec - 1) / vec, p.iter);
+    if (threads < 64 || threads > 512) return p;
+    p.per_sm = std::min(8, std::max(1, 512 / threads));
+    const size_t sums = tensors == 4 ? (size_t)C * 4 : 0;  // backward: a sum per column
+    // two stages at least
+    while (p.per_sm > 1 && ring_shape(1, C * es, tensors, kRingSmem / p.per_sm / 16 * 16 - sums, 0).stages < 2) --p.per_sm;
+    p.smem = kRingSmem / p.per_sm / 16 * 16;
+    if (p.smem > sums && ring_shape(1, C * es, tensors, p.smem - sums, 0).stages >= 2) p.threads = threads;
+    return p;
+}
+
 // How the rows of a backward pass are dealt out: `blocks` of the launch, stretches per gate, a block or a warp a stretch.
-struct BwdPlan { RmsPlan row; int blocks, parts, per_block; };
-BwdPlan bwd_plan(int rows, int C, int span, int vec) {
-    BwdPlan p;
+struct BwdPlan { RingPlan ring; RmsPlan row; int blocks, parts, per_block; };
+BwdPlan bwd_plan(int rows, int C, int span, int vec, int es, bool ring) {
+    BwdPlan p{};
+    if (ring) p.ring = ring_plan(rows, C, vec, es, 4);
     p.row = rms_plan(C / vec, vec > 1, 2, 256);
-    const bool warp = p.row.tpr == 32;
-    const int gates = (rows - 1) / span + 1;
-    const int most = 148 * (warp ? 2 : std::max(1, (p.row.iter == 1 ? 1024 : 512) / p.row.threads));
+    const bool warp = p.ring.threads == 0 && p.row.tpr == 32;
+    const int gates = (rows - 1) / span + 1, longest = std::min(span, rows);
+    const int most = 148 * (p.ring.threads ? p.ring.per_sm : (warp ? 2 : std::max(1, (p.row.iter == 1 ? 1024 : 512) / p.row.threads)));
     // rounds of the resident blocks, in rows; leaving a stretch's share costs about a row
     double best = 1e30;
     if (warp) {
         p.parts = 1;
         p.per_block = 0;
-        best = (double)((gates - 1) / (most * 8) + 1) * (std::min(span, rows) + 1);
+        best = (double)((gates - 1) / (most * 8) + 1) * (longest + 1);
     }
-    for (int n = 1; n <= std::min(std::min(span, rows), 2 * most / gates + 1); ++n) {
-        const int len = (std::min(span, rows) - 1) / n + 1, steps = warp ? (len - 1) / 8 + 1 : len;
+    for (int n = 1; n <= std::min(longest, 2 * most / gates + 1); ++n) {
+        const int len = (longest - 1) / n + 1, steps = warp ? (len - 1) / 8 + 1 : len;
         const double t = (double)(((long)gates * n - 1) / most + 1) * (steps + 1);
         if (t < best) { best = t; p.parts = n; p.per_block = 1; }
     }
@@ -311,13 +609,26 @@ size_t bwd_scratch(const BwdPlan &p, int rows, int C, int span) {
     return ((size_t)p.blocks * 2 + (p.parts > 1 ? (size_t)((rows - 1) / span + 1) * p.parts : 0)) * C;
 }
 
-template <typename T, int VEC, bool SHIFT>
-int fwd_as(const void *b, const void *res, const void *gate, const void *post, const void *pre, void *h, void *y, void *q, float *scale, float *rstd_post,
-           float *rstd_pre, int rows, int C, int span, float alpha, float eps, const Launch &s) {
-    const RmsPlan p = rms_plan(rms_nvec(C, VEC, SHIFT), VEC > 1, 4, 128);
+template <typename K> bool ring_ready(K kernel, int &ready_dev) {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem) != cudaSuccess) return false;
+        ready_dev = dev;
+    }
+    return true;
+}
+template <typename T, int VEC, int ITER> int fwd_ring(const BlockNormFwd &g, const RingPlan &p, const Launch &s) {
+    static thread_local int ready = -1;
+    if (!ring_ready(block_norm_fwd_ring_kernel<T, VEC, ITER>, ready)) return -1;
+    launch_k(block_norm_fwd_ring_kernel<T, VEC, ITER>, std::min(g.rows, 148 * p.per_sm), p.threads, p.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 2, p.smem, kSpinLimit));
+    return 1;
+}
+template <typename T, int VEC, bool SHIFT> int fwd_as(const BlockNormFwd &g, const Launch &s) {
+    const RmsPlan p = rms_plan(rms_nvec(g.C, VEC, SHIFT), VEC > 1, 4, 128);
     auto go = [&](auto kernel) {
-        launch_k(kernel, (rows - 1) / p.rpb + 1, p.threads, 0, s, (const T *)b, (const T *)res, (const T *)gate, (const T *)post, (const T *)pre, (T *)h, (T *)y, (int8_t *)q,
-                 scale, rstd_post, rstd_pre, rows, C, act8_pitch(C), p.tpr, span, alpha, eps);
+        launch_k(kernel, (g.rows - 1) / p.rpb + 1, p.threads, 0, s, (const T *)g.b, (const T *)g.res, (const T *)g.gate, (const T *)g.post, (const T *)g.pre, (T *)g.h, (T *)g.y, g.q,
+                 g.scale, g.rstd_post, g.rstd_pre, g.rows, g.C, g.pitch, p.tpr, g.span, g.alpha, g.eps);
     };
     switch (p.iter) {
     case 1: go(block_norm_fwd_kernel<T, VEC, 1, SHIFT>); break;
@@ -330,14 +641,25 @@ int fwd_as(const void *b, const void *res, const void *gate, const void *post, c
     return 1;
 }
 
-template <typename T, int VEC> int bwd_as(BlockNormBwd &g, float *scratch, float *dpost, float *dpre, const Launch &s) {
-    const BwdPlan p = bwd_plan(g.rows, g.C, g.span, VEC);
+template <typename T, int VEC, int ITER> int bwd_ring(const BlockNormBwd &g, const BwdPlan &p, const Launch &s) {
+    static thread_local int ready = -1;
+    if (!ring_ready(block_norm_bwd_ring_kernel<T, VEC, ITER>, ready)) return -1;
+    launch_k(block_norm_bwd_ring_kernel<T, VEC, ITER>, p.blocks, p.ring.threads, p.ring.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), kSpinLimit));
+    return 1;
+}
+
+template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scratch, float *dpost, float *dpre, const Launch &s) {
+    const BwdPlan p = bwd_plan(g.rows, g.C, g.span, VEC, sizeof(T), ring);
     g.parts = p.parts; g.per_block = p.per_block;
     g.part = scratch;
     g.piece = scratch + (size_t)p.blocks * 2 * g.C;
     const size_t smem = p.row.tpr == 32 ? (size_t)8 * ((g.C + 3) & ~3) * sizeof(float) : 0;
     auto go = [&](auto kernel) { launch_k(kernel, p.blocks, p.row.threads, smem, s, g); };
-    if (p.row.tpr == 32) {
+    if (p.ring.threads) {
+        g.several = (long)g.gates * g.parts > p.blocks;
+        const int r = bwd_ring<T, VEC, VEC == 1 ? 8 : 2>(g, p, s);
+        if (r < 0) return r;
+    } else if (p.row.tpr == 32) {
         if (p.row.iter == 1) go(block_norm_bwd_kernel<T, VEC, 1, true>); else go(block_norm_bwd_kernel<T, VEC, 2, true>);
     } else {
         switch (p.row.iter) {
@@ -357,21 +679,30 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, float *scratch, float
 }  // namespace
 
 size_t block_norm_scratch_elems(int rows, int C, int span) {
-    size_t most = bwd_scratch(bwd_plan(rows, C, span, 1), rows, C, span);
-    for (int vec : {4, 8})
-        if (C % vec == 0) most = std::max(most, bwd_scratch(bwd_plan(rows, C, span, vec), rows, C, span));
+    size_t most = 0;
+    for (int vec : {1, 4, 8})
+        for (int es : {2, 4})
+            for (bool ring : {false, true})
+                if (C % vec == 0) most = std::max(most, bwd_scratch(bwd_plan(rows, C, span, vec, es, ring), rows, C, span));
     return most;
 }
 
 int launch_block_norm_fwd(int prec, const void *b, const void *res, const void *gate, const void *post, const void *pre, void *h, void *y, void *q, float *scale,
                           float *rstd_post, float *rstd_pre, int rows, int C, int span, float alpha, float eps, Launch s) {
-    const int vec = prec == P_BF16 ? 8 : 4;
+    const int vec = prec == P_BF16 ? 8 : 4, es = (int)elem_size(prec);
     bool aligned = true;
     for (const void *p : {b, res, gate, post, pre, (const void *)h, (const void *)y}) aligned = aligned && vec_ok(p);
     const bool v = C % vec == 0 && aligned, shift = C % vec != 0 && aligned && rms_shift_fits(C, vec);
-    auto go = [&](auto f) { return f(b, res, gate, post, pre, h, y, q, scale, rstd_post, rstd_pre, rows, C, span, alpha, eps, s); };
-    if (prec == P_BF16) return v ? go(fwd_as<bf16, 8, false>) : (shift ? go(fwd_as<bf16, 8, true>) : go(fwd_as<bf16, 1, false>));
-    return v ? go(fwd_as<float, 4, false>) : (shift ? go(fwd_as<float, 4, true>) : go(fwd_as<float, 1, false>));
+    const BlockNormFwd g{b, res, gate, post, pre, h, y, (int8_t *)q, scale, rstd_post, rstd_pre, rows, C, act8_pitch(C), span, alpha, eps};
+    if (vec_ok(b) && vec_ok(res)) {
+        const RingPlan p = ring_plan(rows, C, v ? vec : 1, es, 2);
+        if (p.threads) {
+            if (prec == P_BF16) return v ? fwd_ring<bf16, 8, 4>(g, p, s) : fwd_ring<bf16, 1, 8>(g, p, s);
+            return v ? fwd_ring<float, 4, 4>(g, p, s) : fwd_ring<float, 1, 8>(g, p, s);
+        }
+    }
+    if (prec == P_BF16) return v ? fwd_as<bf16, 8, false>(g, s) : (shift ? fwd_as<bf16, 8, true>(g, s) : fwd_as<bf16, 1, false>(g, s));
+    return v ? fwd_as<float, 4, false>(g, s) : (shift ? fwd_as<float, 4, true>(g, s) : fwd_as<float, 1, false>(g, s));
 }
 
 int launch_block_norm_bwd(int prec, const void *dy, const void *dh, const void *b, const void *h, const void *gate, const void *post, const void *pre,
@@ -380,11 +711,12 @@ int launch_block_norm_bwd(int prec, const void *dy, const void *dh, const void *
     const int vec = prec == P_BF16 ? 8 : 4;
     bool v = C % vec == 0;
     for (const void *p : {dy, dh, b, h, gate, post, pre, (const void *)db, (const void *)dres, (const void *)dgate, (const void *)scratch}) v = v && vec_ok(p);
+    const bool ring = vec_ok(dy) && vec_ok(dh) && vec_ok(b) && vec_ok(h);
     BlockNormBwd g{};
     g.dy = dy; g.dh = dh; g.b = b; g.h = h; g.gate = gate; g.post = post; g.pre = pre; g.rstd_post = rstd_post; g.rstd_pre = rstd_pre;
     g.db = db; g.dres = dres; g.dgate = dgate; g.rows = rows; g.C = C; g.span = span; g.gates = (rows - 1) / span + 1; g.alpha = alpha;
-    if (prec == P_BF16) return v ? bwd_as<bf16, 8>(g, scratch, dpost, dpre, s) : bwd_as<bf16, 1>(g, scratch, dpost, dpre, s);
-    return v ? bwd_as<float, 4>(g, scratch, dpost, dpre, s) : bwd_as<float, 1>(g, scratch, dpost, dpre, s);
+    if (prec == P_BF16) return v ? bwd_as<bf16, 8>(g, ring, scratch, dpost, dpre, s) : bwd_as<bf16, 1>(g, ring, scratch, dpost, dpre, s);
+    return v ? bwd_as<float, 4>(g, ring, scratch, dpost, dpre, s) : bwd_as<float, 1>(g, ring, scratch, dpost, dpre, s);
 }
 
 }  // namespace ddg

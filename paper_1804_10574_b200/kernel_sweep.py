@@ -1,5 +1,5 @@
-"""Per-kernel sweep over the ResNet-110 layer shapes, and over the tail of a language-model step (dropout, RMS norm,
-vocabulary projection with cross entropy), through the single-kernel C-ABI entry points.
+"""Per-kernel sweep over the ResNet-110 layer shapes, over the tail of a language-model step (dropout, RMS norm, vocabulary
+projection with cross entropy) and over a block around a linear layer in 8 bits, through the single-kernel C-ABI entry points.
 
     python -m paper_1804_10574_b200.kernel_sweep [--batch 1024] [--only NAME] [--iters 20] [--json] [--warm]
 
@@ -101,7 +101,7 @@ def cases(B):
     w, v, gr = (torch.randn(n, device="cuda") for _ in range(3))
     wv = torch.empty(n, dtype=bf, device="cuda")
     out.append(("sgd_update 1.73M params", lambda: binding.sgd_update(1, w, v, gr, wv, n, 0.01, 0.9, 5e-4), n * 22, 0.0, 0, (w, v, gr, wv)))
-    return out + tail_cases(B)
+    return out + tail_cases(B) + block_cases(B)
 
 
 def tail_cases(B, D=1024, V=32000):
@@ -131,6 +131,35 @@ def tail_cases(B, D=1024, V=32000):
         ("linear_ce_fwd " + wtag, lambda: binding.linear_ce_fwd(1, x, w, None, labels, loss, None, lse, ws, B, D, V), n + V * D * 2, flops, 1, keep),
         ("linear_ce_bwd " + wtag, lambda: binding.linear_ce_bwd(1, x, w, None, labels, lse, None, None, dx, dw, None, ws, B, D, V),
          2 * (n + V * D * 2), 2 * flops, 1, keep),
+    ]
+
+
+def block_cases(B, D=4096, F=4096):
+    """A block around a linear layer in 8 bits, on B rows: norms with gate and residual scale, rows of codes, the layer's
+    product on codes and its gradients."""
+    bf = torch.bfloat16
+    b, res, dy, dh = (torch.randn(B, D, device="cuda").to(bf) for _ in range(4))
+    gate, post, pre = (torch.ones(1, D, device="cuda").to(bf) for _ in range(3))
+    w, dz = (torch.randn(F, D, device="cuda") * D ** -0.5).to(bf), torch.randn(B, F, device="cuda").to(bf)
+    h, y, db, dres, z, dw = torch.empty_like(b), torch.empty_like(b), torch.empty_like(b), torch.empty_like(b), torch.empty_like(dz), torch.empty(F, D, device="cuda")
+    q, wq = (torch.empty(n, binding.act8_pitch(D), dtype=torch.int8, device="cuda") for n in (B, F))
+    r1, r2, qs, ws, dg, dp1, dp2, dbias = (torch.ones(n, device="cuda") for n in (B, B, B, F, D, D, D, F))
+    sc = torch.empty(binding.block_norm_scratch_elems(B, D, B), device="cuda")
+    work = torch.empty(binding.fc8_workspace_bytes(1, B, D, F), dtype=torch.uint8, device="cuda")
+    keep = (b, res, dy, dh, gate, post, pre, w, dz, h, y, db, dres, z, dw, q, wq, r1, r2, qs, ws, dg, dp1, dp2, dbias, sc, work)
+    binding.act8_pack(1, w, wq, ws, F, D)
+    binding.act8_pack(1, b, q, qs, B, D)
+    n, wn, flops, tag, wtag = B * D * 2, F * D, 2.0 * B * D * F, "%dx%d" % (B, D), "%dx%dx%d" % (B, D, F)
+    return [
+        ("block_norm_fwd " + tag, lambda: binding.block_norm_fwd(1, b, res, gate, post, pre, h, y, None, None, r1, r2, B, D, B), 4 * n, 0.0, 0, keep),
+        ("block_norm_fwd codes " + tag, lambda: binding.block_norm_fwd(1, b, res, gate, post, pre, h, None, q, qs, r1, r2, B, D, B), 3 * n + n // 2, 0.0, 0, keep),
+        ("block_norm_bwd " + tag, lambda: binding.block_norm_bwd(1, dy, dh, b, h, gate, post, pre, r1, r2, db, dres, dg, dp1, dp2, sc, B, D, B), 6 * n, 0.0, 0, keep),
+        ("act8_pack " + tag, lambda: binding.act8_pack(1, b, q, qs, B, D), n + n // 2, 0.0, 0, keep),
+        ("act8_unpack " + tag, lambda: binding.act8_unpack(1, q, qs, y, B, D), n + n // 2, 0.0, 0, keep),
+        ("fc8_fwd " + wtag, lambda: binding.fc8_fwd(1, q, qs, wq, ws, None, z, B, D, F), B * D + wn + B * F * 2, flops, 1, keep),
+        ("fc8_bwd dx " + wtag, lambda: binding.fc8_bwd(1, dz, None, None, wq, ws, db, None, None, work, B, D, F), wn + B * F * 2 + n, flops, 1, keep),
+        ("fc8_bwd dW " + wtag, lambda: binding.fc8_bwd(1, dz, q, qs, None, None, None, dw, None, work, B, D, F, True), B * D + B * F * 2 + 4 * wn, flops, 1, keep),
+        ("fc8_bwd dx dW db " + wtag, lambda: binding.fc8_bwd(1, dz, q, qs, wq, ws, db, dw, dbias, work, B, D, F, True), B * D + wn + B * F * 2 + n + 4 * wn, 2 * flops, 1, keep),
     ]
 
 
