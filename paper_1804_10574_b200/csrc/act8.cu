@@ -8,6 +8,7 @@
 #include "common.cuh"
 #include "lm_ops.h"
 #include "row_io.cuh"
+#include "row_ring.cuh"
 
 namespace ddg {
 
@@ -54,10 +55,64 @@ __global__ void __launch_bounds__(rms_max_threads(VEC, ITER)) act8_pack_kernel(c
     for (int i = 0; i < ITER; ++i) {
         const int c = (i * tpr + t) * VEC;
         if (c < C) {
-            act8_store<sizeof(T) == 2, VEC>(to + c, v[i], r);
+            act8_store<sizeof(T) == 2 ? kBf16 : kF32, VEC>(to + c, v[i], r);
         }
     }
     for (int c = C + t; c < pitch; c += tpr) to[c] = 0;
+}
+
+// The same for many rows: resident blocks walk stretches of them, the rows ahead on their way through shared memory.
+template <typename T, int VEC, int ITER>
+__global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restrict__ x, int8_t *__restrict__ q, float *__restrict__ scale, int rows, int C, int pitch,
+                                                                const __grid_constant__ RingShape shape) {
+    constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    __shared__ uint64_t full[kRingMostStages];
+    __shared__ __align__(16) float red[6][32];
+    __shared__ int abort_flag;
+    const int t = threadIdx.x;
+    RowRing<1> ring(shape, smem_u32(ring_smem), full, &abort_flag);
+    if (t == 0) ring.init();
+    if (t < 32) {
+#pragma unroll
+        for (int k = 0; k < 6; ++k) red[k][t] = 0.f;
+    }
+    __syncthreads();
+    pdl_launch();
+    pdl_wait();
+    const int first = (int)((long)rows * blockIdx.x / gridDim.x), last = (int)((long)rows * (blockIdx.x + 1) / gridDim.x);
+    const void *const src[1] = {x};
+    if (t == 0)
+        for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, src);
+    uint32_t round = 0;
+    for (int row = first; row < last; ++row) {
+        const bool ok = ring.wait();
+        const uint32_t slot = ring.slot(0);
+        const RingRow at = ring_row(shape, row);
+        ring.next();
+        F2 v[P];
+        uint32_t top = ok ? 0u : 0x7fffffffu;  // a row that did not come is NaN
+#pragma unroll
+        for (int i = 0; i < P / G; ++i) {
+            F2 in[G];
+            slot_load<T, VEC>(slot, at, x + (size_t)row * C, C, i, in);
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                v[i * G + j] = in[j];
+                const float2 p = parts(in[j]);
+                top = max(top, max(magnitude_bits(p.x), magnitude_bits(p.y)));
+            }
+        }
+        top = ring_max(top, red, round);
+        if (t == 0 && row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, src);
+        float s;
+        const Act8Row r = act8_row(top, s);
+        if (t == 0) scale[row] = s;
+        int8_t *to = q + (size_t)row * pitch;
+        act8_share_store<sizeof(T) == 2 ? kBf16 : kF32, VEC, ITER>(to, C, v, r);
+        for (int c = C + t; c < pitch; c += blockDim.x) to[c] = 0;
+    }
+    if (t == 0) ring.drain();
 }
 
 // Rows of more values than a block's registers hold: read twice, the second time out of the L2.
@@ -79,31 +134,45 @@ __global__ void __launch_bounds__(1024) act8_pack_wide_kernel(const T *__restric
     for (int c = threadIdx.x; c < pitch; c += 1024) to[c] = c < C ? (int8_t)act8_code(to_f(from[c]), r) : (int8_t)0;
 }
 
-// 16 codes of a row per thread.
+// 16 codes of a row at a time, four of them on their way per thread.
 template <typename T>
 __global__ void __launch_bounds__(256) act8_unpack_kernel(const int8_t *__restrict__ q, const float *__restrict__ scale, T *__restrict__ x, size_t units, int C, int pitch, int vec) {
+    constexpr int kAhead = 4;
     pdl_launch();
     pdl_wait();
     const unsigned per_row = pitch / 16;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (size_t)gridDim.x * 256) {
-        const size_t row = units <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
-        const int c = (int)(i - row * per_row) * 16;
-        const uint4 w = *reinterpret_cast<const uint4 *>(q + row * pitch + c);
-        const float s = scale[row];
-        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-        T *to = x + row * C + c;
-        float v[16];
+    for (size_t i0 = (size_t)blockIdx.x * (256 * kAhead) + threadIdx.x; i0 < units; i0 += (size_t)gridDim.x * (256 * kAhead)) {
+        uint4 w[kAhead];
+        float s[kAhead];
+        size_t row[kAhead];
+        int col[kAhead];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = (float)(int8_t)(word[j / 4] >> (8 * (j % 4))) * s;
-        constexpr int N = Vec16<T>::N;
-        if (vec) {
+        for (int u = 0; u < kAhead; ++u) {
+            const size_t i = min(i0 + 256 * u, units - 1);
+            row[u] = units <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
+            col[u] = (int)(i - row[u] * per_row) * 16;
+            w[u] = *reinterpret_cast<const uint4 *>(q + row[u] * pitch + col[u]);
+            s[u] = scale[row[u]];
+        }
 #pragma unroll
-            for (int j = 0; j < 16; j += N)
-                if (c + j < C) store_f<T, N>(to + j, reinterpret_cast<const float(&)[N]>(v[j]));
-        } else {
+        for (int u = 0; u < kAhead; ++u) {
+            if (i0 + 256 * u >= units) break;
+            const uint32_t word[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+            const int c = col[u];
+            T *to = x + row[u] * C + c;
+            float v[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (c + j < C) to[j] = from_f<T>(v[j]);
+            for (int j = 0; j < 16; ++j) v[j] = (float)(int8_t)(word[j / 4] >> (8 * (j % 4))) * s[u];
+            constexpr int N = Vec16<T>::N;
+            if (vec) {
+#pragma unroll
+                for (int j = 0; j < 16; j += N)
+                    if (c + j < C) store_f<T, N>(to + j, reinterpret_cast<const float(&)[N]>(v[j]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (c + j < C) to[j] = from_f<T>(v[j]);
+            }
         }
     }
 }
@@ -123,6 +192,14 @@ template <typename T, int VEC> int pack_as(const void *x, void *q, float *scale,
     return 1;
 }
 
+template <typename T, int VEC, int ITER> int pack_ring(const void *x, void *q, float *scale, int rows, int C, const RingPlan &p, const Launch &s) {
+    static thread_local int ready = -1;
+    if (!ring_ready(act8_pack_ring_kernel<T, VEC, ITER>, ready)) return -1;
+    launch_k(act8_pack_ring_kernel<T, VEC, ITER>, std::min(rows, 148 * p.per_sm), p.threads, p.smem, s, (const T *)x, (int8_t *)q, scale, rows, C, act8_pitch(C),
+             ring_shape(rows, C * (int)sizeof(T), 1, p.smem, kSpinLimit));
+    return 1;
+}
+
 template <typename T> int pack_wide(const void *x, void *q, float *scale, int rows, int C, const Launch &s) {
     launch_k(act8_pack_wide_kernel<T>, rows, 1024, 0, s, (const T *)x, (int8_t *)q, scale, C, act8_pitch(C));
     return 1;
@@ -131,7 +208,7 @@ template <typename T> int pack_wide(const void *x, void *q, float *scale, int ro
 template <typename T> int unpack_as(const void *q, const float *scale, void *x, int rows, int C, const Launch &s) {
     const int pitch = act8_pitch(C);
     const size_t units = (size_t)rows * (pitch / 16);
-    const int grid = (int)std::min<size_t>((units + 255) / 256, 148 * 16), vec = C % Vec16<T>::N == 0 && vec_ok(x);
+    const int grid = (int)std::min<size_t>((units + 1023) / 1024, 148 * 8), vec = C % Vec16<T>::N == 0 && vec_ok(x);
     launch_k(act8_unpack_kernel<T>, grid, 256, 0, s, (const int8_t *)q, scale, (T *)x, units, C, pitch, vec);
     return 1;
 }
@@ -140,6 +217,14 @@ template <typename T> int unpack_as(const void *q, const float *scale, void *x, 
 
 int launch_act8_pack(int prec, const void *x, void *q, float *scale, int rows, int C, Launch s) {
     const bool vec = vec_ok(x) && C % (prec == P_BF16 ? 8 : 4) == 0;
+    const int per_vec = vec ? (prec == P_BF16 ? 8 : 4) : 1, iter = vec ? 4 : 8;
+    if (rows >= 2 * 148 && vec_ok(x) && ring_threads((C + per_vec - 1) / per_vec, iter) >= 64) {  // narrow rows are a warp's of the other kernel
+        const RingPlan p = ring_plan(C, C * (int)elem_size(prec), per_vec, iter, 1, 0);
+        if (p.threads) {
+            if (prec == P_BF16) return vec ? pack_ring<bf16, 8, 4>(x, q, scale, rows, C, p, s) : pack_ring<bf16, 1, 8>(x, q, scale, rows, C, p, s);
+            return vec ? pack_ring<float, 4, 4>(x, q, scale, rows, C, p, s) : pack_ring<float, 1, 8>(x, q, scale, rows, C, p, s);
+        }
+    }
     if (C > kRmsMaxC) return prec == P_BF16 ? pack_wide<bf16>(x, q, scale, rows, C, s) : pack_wide<float>(x, q, scale, rows, C, s);
     if (prec == P_BF16) return vec ? pack_as<bf16, 8>(x, q, scale, rows, C, s) : pack_as<bf16, 1>(x, q, scale, rows, C, s);
     return vec ? pack_as<float, 4>(x, q, scale, rows, C, s) : pack_as<float, 1>(x, q, scale, rows, C, s);

@@ -36,10 +36,13 @@ __device__ __forceinline__ int act8_code(float x, const Act8Row &r) {
 
 // N codes at once, in the words' bytes.  t = 127 x / m rounded by adding 1.5 x 2^23, which leaves the whole number in the sum's
 // low byte.
-//   BF16 (x and m are bf16 values): 127 x is exact (here 127 / 128 x, and m / 128), and the quotient corrected by its remainder (Markstein, 1990) is exactly a
-//   border where it is one, as x = m / 2 is, and else nearer to the quotient than any border (2^-17 at least).
-//   else: x inv, with one test for all of them whether a border is so near that it could decide; then they are formed in 64 bits.
-template <bool BF16, int N> __device__ __forceinline__ void act8_codes(const F2 (&x)[N / 2], const Act8Row &r, uint32_t (&w)[(N + 3) / 4]) {
+//   kBf16 (x and m are bf16 values): 127 x is exact (here 127 / 128 x, and m / 128), and the quotient corrected by its remainder
+//     (Markstein, 1990) is exactly a border where it is one, as x = m / 2 is, and else nearer to the quotient than any border
+//     (2^-17 at least).
+//   kF32: x inv, with one test for all of them whether a border is so near that it could decide; then they are formed in 64 bits.
+//   kNear: x inv, less than 2^-15 of a step off, where x is itself a rounded result.
+enum Act8Kind { kBf16, kF32, kNear };
+template <Act8Kind KIND, int N> __device__ __forceinline__ void act8_codes(const F2 (&x)[N / 2], const Act8Row &r, uint32_t (&w)[(N + 3) / 4]) {
     constexpr float kRound = 12582912.f;
     const F2 inv = f2(r.inv), up = f2(kRound);
     uint32_t n[N];
@@ -48,7 +51,7 @@ template <bool BF16, int N> __device__ __forceinline__ void act8_codes(const F2 
 #pragma unroll
     for (int k = 0; k < N / 2; ++k) {
         F2 t;
-        if (BF16) {
+        if (KIND == kBf16) {
             const F2 x127 = x[k] * by;
             t = x127 * inv_m;
             t = fma2(fma2(t, neg_m, x127), inv_m, t);
@@ -59,12 +62,12 @@ template <bool BF16, int N> __device__ __forceinline__ void act8_codes(const F2 
         const float2 sp = parts(s);
         n[2 * k] = __float_as_uint(sp.x);
         n[2 * k + 1] = __float_as_uint(sp.y);
-        if (!BF16) {
+        if (KIND == kF32) {
             const float2 d = parts(fma2(s + f2(-kRound), f2(-1.f), t));
             off = fmaxf(off, fmaxf(fabsf(d.x), fabsf(d.y)));
         }
     }
-    if (!BF16 && off > 0.5f - 0x1p-13f) {
+    if (KIND == kF32 && off > 0.5f - 0x1p-14f) {
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) {
             const float2 p = parts(x[k]);
@@ -79,7 +82,7 @@ template <bool BF16, int N> __device__ __forceinline__ void act8_codes(const F2 
 }
 
 // VEC codes, 1, 4 or 8, on a boundary of as many bytes.
-template <bool BF16, int VEC> __device__ __forceinline__ void act8_store(int8_t *to, const float (&v)[VEC], const Act8Row &r) {
+template <Act8Kind KIND, int VEC> __device__ __forceinline__ void act8_store(int8_t *to, const float (&v)[VEC], const Act8Row &r) {
     if constexpr (VEC == 1) {
         *to = (int8_t)act8_code(v[0], r);
     } else {
@@ -87,23 +90,35 @@ template <bool BF16, int VEC> __device__ __forceinline__ void act8_store(int8_t 
         uint32_t w[VEC / 4];
 #pragma unroll
         for (int j = 0; j < VEC / 2; ++j) x[j] = f2(v[2 * j], v[2 * j + 1]);
-        act8_codes<BF16, VEC>(x, r, w);
+        act8_codes<KIND, VEC>(x, r, w);
         if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t *>(to) = w[0];
     }
 }
 
 // A thread's pairs (see row_ring.cuh) to a row of codes.
-template <bool BF16, int VEC, int ITER> __device__ __forceinline__ void act8_share_store(int8_t *row, int C, const F2 (&v)[VEC * ITER / 2], const Act8Row &r) {
-    uint32_t w[(VEC * ITER + 3) / 4];
-    act8_codes<BF16, VEC * ITER>(v, r, w);
+template <Act8Kind KIND, int VEC, int ITER> __device__ __forceinline__ void act8_share_store(int8_t *row, int C, const F2 (&v)[VEC * ITER / 2], const Act8Row &r) {
+    if constexpr (VEC > 1) {
 #pragma unroll
-    for (int i = 0; i < ITER; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        if (c >= C) continue;
-        if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[2 * i], w[2 * i + 1]);
-        else if constexpr (VEC == 4) *reinterpret_cast<uint32_t *>(row + c) = w[i];
-        else row[c] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * blockDim.x + threadIdx.x) * VEC;
+            F2 x[VEC / 2];
+            uint32_t w[VEC / 4];
+#pragma unroll
+            for (int j = 0; j < VEC / 2; ++j) x[j] = v[i * VEC / 2 + j];
+            act8_codes<KIND, VEC>(x, r, w);
+            if (c >= C) continue;
+            if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t *>(row + c) = w[0];
+        }
+    } else {
+        uint32_t w[(ITER + 3) / 4];
+        act8_codes<KIND, ITER>(v, r, w);
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = i * blockDim.x + threadIdx.x;
+            if (c < C) row[c] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+        }
     }
 }
 

@@ -117,7 +117,7 @@ block_norm_fwd_kernel(const T *b, const T *res, const T *__restrict__ gate, cons
                 for (int j = 0; j < VEC; ++j)
                     if (c + j >= 0 && c + j < C) to[c + j] = (int8_t)act8_code(v[i][j], code);
             } else {
-                act8_store<false, VEC>(to + c, v[i], code);
+                act8_store<kNear, VEC>(to + c, v[i], code);
             }
         }
     }
@@ -134,7 +134,7 @@ struct BlockNormFwd {
 };
 
 // The same for many rows: resident blocks walk stretches of them, the rows ahead on their way through shared memory.
-template <typename T, int VEC, int ITER>
+template <typename T, int VEC, int ITER, bool CODES>
 __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __grid_constant__ BlockNormFwd g, const __grid_constant__ RingShape shape) {
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t full[kRingMostStages];
@@ -200,6 +200,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
         if (t == 0 && row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, src);
         const float r1 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
         s2 = f2(0.f);
+        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 res[G];
@@ -207,34 +208,34 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 const int k = i * G + j;
-                res[j] = v[k] = fma2(alpha, res[j], v[k] * f2(r1) * pg[k]);
-                s2 = fma2(v[k], v[k], s2);
+                res[j] = fma2(alpha, res[j], v[k] * f2(r1) * pg[k]);
+                s2 = fma2(res[j], res[j], s2);
+                v[k] = res[j] * pre.pair(k);
+                if (CODES) {
+                    const float2 p = parts(v[k]);
+                    top = max(top, max(__float_as_uint(p.x) & 0x7fffffffu, __float_as_uint(p.y) & 0x7fffffffu));
+                }
             }
             group_store<T, VEC>((T *)g.h + start, C, i, res);
         }
         sum[0] = sum2(s2);
-        ring_sum<1>(sum, red, round);
+        if (CODES) ring_sum_max(sum[0], top, red, round);
+        else ring_sum<1>(sum, red, round);
         const float r2 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
         if (t == 0) {
             if (g.rstd_post) g.rstd_post[row] = r1;
             if (g.rstd_pre) g.rstd_pre[row] = r2;
         }
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[k] = v[k] * f2(r2) * pre.pair(k);
+        for (int k = 0; k < P; ++k) v[k] = v[k] * f2(r2);
         if (g.y) share_store<T, VEC, ITER>((T *)g.y + start, C, v);
-        if (!g.q) continue;
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const float2 p = parts(v[k]);
-            top = max(top, max(__float_as_uint(p.x) & 0x7fffffffu, __float_as_uint(p.y) & 0x7fffffffu));
-        }
-        top = ring_max(top, red, round);
+        if (!CODES) continue;
+        // the largest |y| is the largest |h gamma_pre| times rstd_pre: known with the sum
         float s;
-        const Act8Row code = act8_row(top, s);
+        const Act8Row code = act8_row(__float_as_uint(__uint_as_float(top) * r2) & 0x7fffffffu, s);
         if (t == 0) g.scale[row] = s;
         int8_t *to = g.q + (size_t)row * g.pitch;
-        act8_share_store<false, VEC, ITER>(to, C, v, code);
+        act8_share_store<kNear, VEC, ITER>(to, C, v, code);
         for (int c = C + t; c < g.pitch; c += threads) to[c] = 0;
     }
     if (t == 0) ring.drain();
@@ -563,28 +564,17 @@ __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const float *__re
 // Whether the rows go through shared memory, by how many threads each (`iter` vectors of a row per thread), and in how many
 // blocks per SM.  A row's reductions cost every one of its warps about as much as 200 values, so that few warps a row and several
 // rows at a time are faster than a whole SM per row.
-constexpr size_t kRingSmem = 216 * 1024;
-struct RingPlan { int threads, iter, per_sm; size_t smem; };
-RingPlan ring_plan(int rows, int C, int vec, int es, int tensors) {
-    RingPlan p{};
-    if (rows < 2 * 148) return p;
-    p.iter = vec == 1 ? 8 : (tensors == 2 ? 4 : 2);
-    const int threads = ring_threads((C + vec - 1) / vec, p.iter);
-    if (threads < 64 || threads > 512) return p;
-    p.per_sm = std::min(8, std::max(1, 512 / threads));
-    const size_t sums = tensors == 4 ? (size_t)C * 4 : 0;  // backward: a sum per column
-    // two stages at least
-    while (p.per_sm > 1 && ring_shape(1, C * es, tensors, kRingSmem / p.per_sm / 16 * 16 - sums, 0).stages < 2) --p.per_sm;
-    p.smem = kRingSmem / p.per_sm / 16 * 16;
-    if (p.smem > sums && ring_shape(1, C * es, tensors, p.smem - sums, 0).stages >= 2) p.threads = threads;
-    return p;
+RingPlan norm_ring(int rows, int C, int vec, int es, bool backward) {
+    // narrow rows are a warp's of the other kernel
+    if (rows < 2 * 148 || ring_threads((C + vec - 1) / vec, vec == 1 ? 8 : (backward ? 2 : 4)) < 64) return RingPlan{};
+    return backward ? ring_plan(C, C * es, vec, vec == 1 ? 8 : 2, 4, (size_t)C * 4) : ring_plan(C, C * es, vec, vec == 1 ? 8 : 4, 2, 0);
 }
 
 // How the rows of a backward pass are dealt out: `blocks` of the launch, stretches per gate, a block or a warp a stretch.
 struct BwdPlan { RingPlan ring; RmsPlan row; int blocks, parts, per_block; };
 BwdPlan bwd_plan(int rows, int C, int span, int vec, int es, bool ring) {
     BwdPlan p{};
-    if (ring) p.ring = ring_plan(rows, C, vec, es, 4);
+    if (ring) p.ring = norm_ring(rows, C, vec, es, true);
     p.row = rms_plan(C / vec, vec > 1, 2, 256);
     const bool warp = p.ring.threads == 0 && p.row.tpr == 32;
     const int gates = (rows - 1) / span + 1, longest = std::min(span, rows);
@@ -609,19 +599,11 @@ size_t bwd_scratch(const BwdPlan &p, int rows, int C, int span) {
     return ((size_t)p.blocks * 2 + (p.parts > 1 ? (size_t)((rows - 1) / span + 1) * p.parts : 0)) * C;
 }
 
-template <typename K> bool ring_ready(K kernel, int &ready_dev) {
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (ready_dev != dev) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem) != cudaSuccess) return false;
-        ready_dev = dev;
-    }
-    return true;
-}
 template <typename T, int VEC, int ITER> int fwd_ring(const BlockNormFwd &g, const RingPlan &p, const Launch &s) {
-    static thread_local int ready = -1;
-    if (!ring_ready(block_norm_fwd_ring_kernel<T, VEC, ITER>, ready)) return -1;
-    launch_k(block_norm_fwd_ring_kernel<T, VEC, ITER>, std::min(g.rows, 148 * p.per_sm), p.threads, p.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 2, p.smem, kSpinLimit));
+    static thread_local int ready[2] = {-1, -1};
+    auto kernel = g.q ? block_norm_fwd_ring_kernel<T, VEC, ITER, true> : block_norm_fwd_ring_kernel<T, VEC, ITER, false>;
+    if (!ring_ready(kernel, ready[g.q != nullptr])) return -1;
+    launch_k(kernel, std::min(g.rows, 148 * p.per_sm), p.threads, p.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 2, p.smem, kSpinLimit));
     return 1;
 }
 template <typename T, int VEC, bool SHIFT> int fwd_as(const BlockNormFwd &g, const Launch &s) {
@@ -695,7 +677,7 @@ int launch_block_norm_fwd(int prec, const void *b, const void *res, const void *
     const bool v = C % vec == 0 && aligned, shift = C % vec != 0 && aligned && rms_shift_fits(C, vec);
     const BlockNormFwd g{b, res, gate, post, pre, h, y, (int8_t *)q, scale, rstd_post, rstd_pre, rows, C, act8_pitch(C), span, alpha, eps};
     if (vec_ok(b) && vec_ok(res)) {
-        const RingPlan p = ring_plan(rows, C, v ? vec : 1, es, 2);
+        const RingPlan p = norm_ring(rows, C, v ? vec : 1, es, false);
         if (p.threads) {
             if (prec == P_BF16) return v ? fwd_ring<bf16, 8, 4>(g, p, s) : fwd_ring<bf16, 1, 8>(g, p, s);
             return v ? fwd_ring<float, 4, 4>(g, p, s) : fwd_ring<float, 1, 8>(g, p, s);

@@ -173,7 +173,7 @@ template <int VEC, int ITER> __device__ __forceinline__ void share_store_f32(flo
 }
 
 // Sums (or, as bits, maxima) over a row's threads, which are the block: one barrier, buffers of two rounds in turn (red: six
-// times 32 floats, zeros at first, on a 16-byte boundary).
+// times 32 floats, zeros at first, on a 16-byte boundary; what is summed and what is a maximum keep to their own rows).
 template <int N> __device__ __forceinline__ void ring_sum(float (&v)[N], float (*red)[32], uint32_t &round) {
     static_assert(N <= 3, "the buffers' size");
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -197,19 +197,64 @@ template <int N> __device__ __forceinline__ void ring_sum(float (&v)[N], float (
         }
     }
 }
+// A sum and a maximum (of bits) in one round.
+__device__ __forceinline__ void ring_sum_max(float &sum, uint32_t &top, float (*red)[32], uint32_t &round) {
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    sum = warp_sum(sum);
+    top = __reduce_max_sync(0xffffffffu, top);
+    float (*to)[32] = red + (round & 1u) * 3;
+    ++round;
+    if (lane == 0) { to[0][warp] = sum; to[1][warp] = __uint_as_float(top); }
+    __syncthreads();
+    sum = 0.f;
+    for (int w = 0; w < warps; w += 4) {
+        const float4 q = *reinterpret_cast<const float4 *>(&to[0][w]);
+        sum += (q.x + q.y) + (q.z + q.w);
+        const uint4 m = *reinterpret_cast<const uint4 *>(&to[1][w]);
+        top = max(max(top, max(m.x, m.y)), max(m.z, m.w));
+    }
+}
 __device__ __forceinline__ uint32_t ring_max(uint32_t v, float (*red)[32], uint32_t &round) {
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     v = __reduce_max_sync(0xffffffffu, v);
-    float *to = red[(round & 1u) * 3];
+    float *to = red[(round & 1u) * 3 + 1];
     ++round;
     if (lane == 0) to[warp] = __uint_as_float(v);
     __syncthreads();
-    return __reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(to[lane]) : 0u);
+    for (int w = 0; w < warps; w += 4) {
+        const uint4 m = *reinterpret_cast<const uint4 *>(to + w);
+        v = max(max(v, max(m.x, m.y)), max(m.z, m.w));
+    }
+    return v;
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
 // Threads of a row (whole warps) that have `iter` vectors each.
 inline int ring_threads(int nvec, int iter) { return ((nvec + iter - 1) / iter + 31) / 32 * 32; }
+constexpr size_t kRingSmem = 216 * 1024;
+// Blocks of an SM for rows of `threads` threads, and the shared memory of each; `extra` bytes of it are not the ring's.  Two
+// stages at least, else 0 blocks.
+struct RingPlan { int threads, per_sm; size_t smem; };
+inline RingShape ring_shape(int rows, int row_bytes, int tensors, size_t smem, unsigned polls);
+inline RingPlan ring_plan(int C, int row_bytes, int vec, int iter, int tensors, size_t extra) {
+    RingPlan p{};
+    const int threads = std::max(64, ring_threads((C + vec - 1) / vec, iter));
+    if (threads > 512) return p;
+    p.per_sm = std::min(8, std::max(1, 512 / threads));
+    while (p.per_sm > 1 && ring_shape(1, row_bytes, tensors, kRingSmem / p.per_sm / 16 * 16 - extra, 0).stages < 2) --p.per_sm;
+    p.smem = kRingSmem / p.per_sm / 16 * 16;
+    if (p.smem > extra && ring_shape(1, row_bytes, tensors, p.smem - extra, 0).stages >= 2) p.threads = threads;
+    return p;
+}
+template <typename K> bool ring_ready(K kernel, int &ready_dev) {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem) != cudaSuccess) return false;
+        ready_dev = dev;
+    }
+    return true;
+}
 inline RingShape ring_shape(int rows, int row_bytes, int tensors, size_t smem, unsigned polls) {
     RingShape g;
     g.row_bytes = row_bytes;

@@ -49,7 +49,7 @@ def value(q, scale, C, prec):
 
 
 ACT_SHAPES = [(1, 1), (1, 16), (3, 7), (5, 64), (130, 128), (2, 1000), (9, 1021), (33, 1024), (4, 4096), (700, 136), (3, 5000), (2, 8192), (3, 16384), (2, 16383), (1, 16385),
-              (2, 65536), (1, 131072), (1300, 40), (257, 200)]
+              (2, 65536), (1, 131072), (1300, 40), (257, 200), (299, 4096), (400, 8192), (300, 1021), (297, 5000), (310, 2051), (300, 16384)]
 
 
 @gpu
