@@ -586,7 +586,9 @@ BwdPlan bwd_plan(int rows, int C, int span, int vec, int es, bool ring) {
         p.per_block = 0;
         best = (double)((gates - 1) / (most * 8) + 1) * (longest + 1);
     }
-    for (int n = 1; n <= std::min(longest, 2 * most / gates + 1); ++n) {
+    const int even = std::max(1, most / gates);
+    for (int n : {1, even, even + 1, 2 * even}) {
+        if (n > longest) continue;
         const int len = (longest - 1) / n + 1, steps = warp ? (len - 1) / 8 + 1 : len;
         const double t = (double)(((long)gates * n - 1) / most + 1) * (steps + 1);
         if (t < best) { best = t; p.parts = n; p.per_block = 1; }

@@ -366,6 +366,8 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     cluster_sync();
 }
 
+#include "fc8_rows.cuh"
+
 // ---- before the products of the backward pass ------------------------------------------------------------------------
 // Codes to bf16, in rows of `plane`: times their scale, or as they are (scale nullable).
 struct CodesJob { const int8_t *q; const float *scale; bf16 *dst; int rows, pitch, plane, blocks; };
@@ -618,6 +620,53 @@ void mm_out(MmArgs &g, void *out, bool is_bf16, int ld) {
     g.store = g.splits == 1 && ld * (is_bf16 ? 2 : 4) % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 ? kBoxes : kRows;
 }
 
+int rows_columns(int B) { return B <= 16 ? 16 : (B <= 32 ? 32 : (B <= 64 ? 64 : 128)); }
+// CTAs that share a tile's K range: as many as run at the same time, and as leave each more codes than sums (bytes).
+int rows_splits(int nt, int tiles, int in) {
+    return std::max(1, std::min(std::min(kRowsMostSplits, kRowsPerSm * 2 * kPairs / tiles), in / std::max(256, 8 * nt)));
+}
+// Whether the outputs go on the MMA's rows.  Both ways are bound by what an SM brings in (about 95 GB/s each), which the ways of
+// cutting the work up tell, in bytes; a row's sums cost as much as 2 KB.  (us with outputs / with rows of x on the MMA's rows:
+// 1 x 4096 x 16384 14.8 / 24.8; 64 x 4096 x 4096 9.8 / 11.5; 200 x 16384 x 1024 13.7 / 32.4; 256 x 4096 x 16384 25.8 / 18.8.)
+bool rows_fit(int B, int in, int out) {
+#ifdef FORCE_ROWS
+    return B <= FORCE_ROWS;
+#endif
+    const int nt = rows_columns(B), sms = 2 * kPairs;
+    const long tiles = (long)((out + kHalf - 1) / kHalf) * ((B + nt - 1) / nt);
+    if (B <= 32) return true;
+    if (B > 1024 || tiles > kRowsPerSm * sms) return false;
+    const int splits = rows_splits(nt, (int)tiles, in), width = mm_width(B, out, 1);
+    const double mine = (double)((tiles * splits + sms - 1) / sms) * ((in + splits - 1) / splits) * (kHalf + nt) + 2048.0 * nt;
+    const long pairs = (long)((B + kTile - 1) / kTile) * ((out + width - 1) / width);
+    return mine < (double)((pairs + kPairs - 1) / kPairs) * in * (kHalf + width / 2);
+}
+template <int NT> int rows_launch(const CUtensorMap &w, const CUtensorMap &x, const RowsArgs &g, int tiles, const Launch &s) {
+    static thread_local int ready_dev = -1;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (ready_dev != dev) {
+        if (cudaFuncSetAttribute(fc8_rows_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem) != cudaSuccess) return -1;
+        ready_dev = dev;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(tiles * g.splits); cfg.blockDim = dim3(kRowsThreads); cfg.dynamicSmemBytes = kRowsSmem; cfg.stream = s.s;
+    cudaLaunchAttribute attr[2];
+    cfg.attrs = attr;
+    if (g.splits > 1) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = g.splits;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    if (s.pdl == 1) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
+    cudaLaunchKernelEx(&cfg, fc8_rows_kernel<NT>, w, x, g);
+    return 1;
+}
 struct BwdPlan {
     int planes;              // bf16 terms of dy
     bool copy_dy;            // dy is not read in place: fp32, or rows that TMA cannot read
@@ -657,6 +706,23 @@ void fc8_wait_polls(int polls) { t_wait_polls = polls; }
 
 int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, const float *ws, const void *bias, void *y, int B, int in, int out, int y_f32, Launch s) {
     const int pitch = act8_pitch(in);
+    if (rows_fit(B, in, out)) {
+        const int nt = rows_columns(B), tiles = (out + kHalf - 1) / kHalf, x_tiles = (B + nt - 1) / nt, kw = nt <= 32 ? RowsStage<16>::kw : RowsStage<64>::kw;
+        RowsArgs g{};
+        g.B = B; g.out = out; g.tiles = tiles; g.steps = (in + kw - 1) / kw; g.splits = rows_splits(nt, tiles * x_tiles, in);
+        g.tail = (in - (g.steps - 1) * kw + 31) / 32;
+        g.row_scale = xs; g.col_scale = ws; g.bias = bias; g.bias_bf16 = prec == P_BF16; g.y = y; g.out_bf16 = prec == P_BF16 && !y_f32;
+        g.vec = out % 4 == 0 && (reinterpret_cast<uintptr_t>(y) & (g.out_bf16 ? 7 : 15)) == 0;
+        g.polls = t_wait_polls >= 0 ? (unsigned)t_wait_polls : kSpinLimit;
+        CUtensorMap mw, mx;
+        if (!box_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, wq, out, in, pitch, kHalf, &mw) || !box_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, xq, B, in, pitch, nt, &mx)) return -1;
+        switch (nt) {
+        case 16: return rows_launch<16>(mw, mx, g, tiles * x_tiles, s);
+        case 32: return rows_launch<32>(mw, mx, g, tiles * x_tiles, s);
+        case 64: return rows_launch<64>(mw, mx, g, tiles * x_tiles, s);
+        default: return rows_launch<128>(mw, mx, g, tiles * x_tiles, s);
+        }
+    }
     MmArgs g{};
     g.M = B; g.N = out; g.n_seg = 1; g.splits = 1;
     g.row_scale = xs; g.col_scale = ws; g.bias = bias; g.bias_bf16 = prec == P_BF16;
