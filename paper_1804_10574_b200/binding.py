@@ -569,20 +569,24 @@ def act8_pitch(C):
     return _lib.ddg_act8_pitch(C)
 
 
+def _pitch(C):
+    return (C + 15) // 16 * 16
+
+
 def act8_pack(prec, x, q, scale, rows, C, stream=None):
     """Rows to 8-bit codes: q int8 [rows][act8_pitch(C)], scale fp32 [rows]."""
-    _ok(_lib.ddg_act8_pack(prec, _tensor(x, rows * C, _elem(prec), "x"), _tensor(q, rows * act8_pitch(C), _I8, "q"),
+    _ok(_lib.ddg_act8_pack(prec, _tensor(x, rows * C, _elem(prec), "x"), _tensor(q, rows * _pitch(C), _I8, "q"),
                            _tensor(scale, rows, _F32, "scale"), rows, C, stream))
 
 
 def act8_unpack(prec, q, scale, x, rows, C, stream=None):
-    _ok(_lib.ddg_act8_unpack(prec, _tensor(q, rows * act8_pitch(C), _I8, "q"), _tensor(scale, rows, _F32, "scale"),
+    _ok(_lib.ddg_act8_unpack(prec, _tensor(q, rows * _pitch(C), _I8, "q"), _tensor(scale, rows, _F32, "scale"),
                              _tensor(x, rows * C, _elem(prec), "x"), rows, C, stream))
 
 
 def fc8_fwd(prec, xq, xscale, Wq, wscale, bias, y, B, n_in, n_out, y_f32=False, stream=None):
     """y = x W^T + bias from the codes of x and of W."""
-    e, pitch = _elem(prec), act8_pitch(n_in)
+    e, pitch = _elem(prec), _pitch(n_in)
     _ok(_lib.ddg_fc8_fwd(prec, _tensor(xq, B * pitch, _I8, "xq"), _tensor(xscale, B, _F32, "xscale"),
                          _tensor(Wq, n_out * pitch, _I8, "Wq"), _tensor(wscale, n_out, _F32, "wscale"), _tensor(bias, n_out, e, "bias"),
                          _tensor(y, B * n_out, _F32 if y_f32 else e, "y"), B, n_in, n_out, int(y_f32), stream))
@@ -594,7 +598,7 @@ def fc8_workspace_bytes(prec, B, n_in, n_out):
 
 def fc8_bwd(prec, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, n_in, n_out, dw_f32=False, stream=None):
     """Gradients of fc8_fwd from the codes that were kept; workspace: a tensor of fc8_workspace_bytes(prec, B, n_in, n_out) bytes."""
-    e, pitch = _elem(prec), act8_pitch(n_in)
+    e, pitch = _elem(prec), _pitch(n_in)
     ws, ws_bytes = _workspace(workspace)
     _ok(_lib.ddg_fc8_bwd(prec, _tensor(dy, B * n_out, e, "dy"), _tensor(xq, B * pitch, _I8, "xq"), _tensor(xscale, B, _F32, "xscale"),
                          _tensor(Wq, n_out * pitch, _I8, "Wq"), _tensor(wscale, n_out, _F32, "wscale"), _tensor(dx, B * n_in, e, "dx"),
@@ -618,7 +622,7 @@ def block_norm_fwd(prec, b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, r
     e, n = _elem(prec), rows * C
     _ok(_lib.ddg_block_norm_fwd(prec, _tensor(b, n, e, "b"), _tensor(res, n, e, "res"), _tensor(gate, _gate_elems(rows, C, span), e, "gate"),
                                 _tensor(gamma_post, C, e, "gamma_post"), _tensor(gamma_pre, C, e, "gamma_pre"), _tensor(h, n, e, "h"),
-                                _tensor(y, n, e, "y"), _tensor(q, rows * act8_pitch(C), _I8, "q"), _tensor(qscale, rows, _F32, "qscale"),
+                                _tensor(y, n, e, "y"), _tensor(q, rows * _pitch(C), _I8, "q"), _tensor(qscale, rows, _F32, "qscale"),
                                 _tensor(rstd_post, rows, _F32, "rstd_post"), _tensor(rstd_pre, rows, _F32, "rstd_pre"), rows, C, span, alpha,
                                 eps, stream))
 

@@ -371,11 +371,12 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
 // ---- before the products of the backward pass ------------------------------------------------------------------------
 // Codes to bf16, in rows of `plane`: times their scale, or as they are (scale nullable).
 struct CodesJob { const int8_t *q; const float *scale; bf16 *dst; int rows, pitch, plane, blocks; };
-// dy to bf16 terms in rows of planes * plane, times a factor per row or column (nullable); zeros behind a row's columns.
-struct TermsJob { const void *src; bf16 *dst; const float *row_scale, *col_scale; int rows, cols, plane, planes, blocks; };
+// dy to bf16 terms in rows of planes * plane, zeros behind a row's columns: as it is (bf16), or times the columns' factors to
+// by_col (for dx) and times the rows' to by_row (for dW), each nullable.
+struct TermsJob { const void *src; bf16 *plain, *by_col, *by_row; const float *row_scale, *col_scale; int rows, cols, plane, planes, blocks; };
 // sums of dy over `chunk` rows: part[row chunk][cols]
 struct SumsJob { const void *src; float *part; int rows, cols, chunk, blocks, vec; };
-struct PrepArgs { CodesJob codes[2]; TermsJob terms[2]; SumsJob sums; };
+struct PrepArgs { CodesJob codes[2]; TermsJob terms; SumsJob sums; };
 
 __device__ __forceinline__ void prep_codes(const CodesJob &j, int block) {
     const unsigned per_row = j.pitch / 16;
@@ -396,29 +397,43 @@ __device__ __forceinline__ void prep_codes(const CodesJob &j, int block) {
     }
 }
 
+constexpr int kSumRows = 512;   // so many rows are summed up for db in one go
+constexpr int kTermCols = 256;  // columns of a row that a warp has at a time, two neighbours per lane
 template <typename T> __device__ __forceinline__ void prep_terms(const TermsJob &j, int block) {
-    // a warp per row, two neighbouring columns per lane
     const int lane = threadIdx.x & 31;
-    auto rest = [](float v) {  // an infinity or NaN stays in the first term alone
-        const float h = bf16_round(v);
-        return isinf(h) || isnan(h) ? 0.f : v - h;
+    const unsigned per_row = (j.plane + kTermCols - 1) / kTermCols;
+    const size_t items = (size_t)j.rows * per_row;
+    auto leave = [&](bf16 *to, float a, float b) {
+        for (int p = 0; p < j.planes; ++p, to += j.plane) {
+            const float ha = bf16_round(a), hb = bf16_round(b);
+            *reinterpret_cast<uint32_t *>(to) = pack2(ha, hb);
+            // an infinity or NaN stays in the first term alone
+            a = isinf(ha) || isnan(ha) ? 0.f : a - ha;
+            b = isinf(hb) || isnan(hb) ? 0.f : b - hb;
+        }
     };
-    for (int row = block * 8 + (threadIdx.x >> 5); row < j.rows; row += j.blocks * 8) {
-        const T *from = (const T *)j.src + (size_t)row * j.cols;
-        bf16 *to = j.dst + (size_t)row * j.planes * j.plane;
-        const float rs = j.row_scale ? j.row_scale[row] : 1.f;
-#pragma unroll 4
-        for (int c = 2 * lane; c < j.plane; c += 64) {
-            float a = c < j.cols ? to_f(from[c]) * rs : 0.f, b = c + 1 < j.cols ? to_f(from[c + 1]) * rs : 0.f;
-            if (j.col_scale) {
-                if (c < j.cols) a *= j.col_scale[c];
-                if (c + 1 < j.cols) b *= j.col_scale[c + 1];
+    for (size_t i = (size_t)block * 8 + (threadIdx.x >> 5); i < items; i += (size_t)j.blocks * 8) {
+        const size_t row = items <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
+        const int c0 = (int)(i - row * per_row) * kTermCols + 2 * lane;
+        const T *from = (const T *)j.src + row * j.cols;
+        float v[kTermCols / 64][2], cs[kTermCols / 64][2];
+#pragma unroll
+        for (int k = 0; k < kTermCols / 64; ++k)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c = c0 + 64 * k + e;
+                v[k][e] = c < j.cols ? to_f(from[c]) : 0.f;
+                cs[k][e] = j.by_col && c < j.cols ? j.col_scale[c] : 0.f;
             }
-            for (int p = 0; p < j.planes; ++p) {
-                *reinterpret_cast<uint32_t *>(to + (size_t)p * j.plane + c) = pack2(a, b);
-                a = rest(a);
-                b = rest(b);
-            }
+        const float rs = j.by_row ? j.row_scale[row] : 0.f;
+        const size_t at = row * j.planes * j.plane;
+#pragma unroll
+        for (int k = 0; k < kTermCols / 64; ++k) {
+            const int c = c0 + 64 * k;
+            if (c >= j.plane) break;
+            if (j.plain) *reinterpret_cast<uint32_t *>(j.plain + at + c) = pack2(v[k][0], v[k][1]);
+            if (j.by_col) leave(j.by_col + at + c, c < j.cols ? v[k][0] * cs[k][0] : 0.f, c + 1 < j.cols ? v[k][1] * cs[k][1] : 0.f);
+            if (j.by_row) leave(j.by_row + at + c, c < j.cols ? v[k][0] * rs : 0.f, c + 1 < j.cols ? v[k][1] * rs : 0.f);
         }
     }
 }
@@ -471,11 +486,8 @@ template <typename T> __global__ void __launch_bounds__(256) fc8_prep_kernel(con
         if (block < g.codes[k].blocks) { prep_codes(g.codes[k], block); return; }
         block -= g.codes[k].blocks;
     }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        if (block < g.terms[k].blocks) { prep_terms<T>(g.terms[k], block); return; }
-        block -= g.terms[k].blocks;
-    }
+    if (block < g.terms.blocks) { prep_terms<T>(g.terms, block); return; }
+    block -= g.terms.blocks;
     prep_sums<T>(g.sums, block);
 }
 
@@ -684,7 +696,7 @@ BwdPlan bwd_plan(int prec, int B, int in, int out) {
     const int kw = kStageKw / 2;
     p.dx_splits = mm_splits(B, in, (out + kw - 1) / kw * p.planes);
     p.dw_splits = mm_splits(out, in, (B + kw - 1) / kw * p.planes);
-    p.chunk = std::max(64, (B + 127) / 128);
+    p.chunk = B <= kSumRows ? B : std::max(256, (B + 127) / 128);
     p.chunks = (B + p.chunk - 1) / p.chunk;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
@@ -744,20 +756,16 @@ int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, co
         prep.codes[k] = CodesJob{(const int8_t *)q, f32 ? nullptr : scale, (bf16 *)(base + at), rows, pitch, p.plane_in, blocks_for((size_t)rows * (pitch / 16))};
         blocks += prep.codes[k].blocks;
     };
-    auto terms = [&](int k, const float *row_scale, const float *col_scale) {
-        prep.terms[k] = TermsJob{dy, (bf16 *)(base + p.dy[k]), row_scale, col_scale, B, out, p.plane_out, p.planes, blocks_for((size_t)B * 32)};
-        blocks += prep.terms[k].blocks;
-    };
     if (dx) codes(0, wq, ws, p.w, out);
     if (dW) codes(1, xq, xs, p.x, B);
-    if (f32) {
-        if (dx) terms(0, nullptr, ws);
-        if (dW) terms(1, xs, nullptr);
-    } else if (copy && (dx || dW)) {
-        terms(0, nullptr, nullptr);
+    if (copy && (dx || dW)) {
+        auto to = [&](int k, bool wanted) { return wanted ? (bf16 *)(base + p.dy[k]) : nullptr; };
+        prep.terms = TermsJob{dy, to(0, !f32), to(0, f32 && dx), to(1, f32 && dW), xs, ws, B, out, p.plane_out, p.planes,
+                              blocks_for((size_t)B * ((p.plane_out + kTermCols - 1) / kTermCols) * 32)};
+        blocks += prep.terms.blocks;
     }
     if (db) {
-        prep.sums = SumsJob{dy, (float *)(base + p.db), B, out, p.chunk, p.chunks * ((out + 63) / 64), out % (f32 ? 4 : 8) == 0 && aligned};
+        prep.sums = SumsJob{dy, p.chunks > 1 ? (float *)(base + p.db) : db, B, out, p.chunk, p.chunks * ((out + 63) / 64), out % (f32 ? 4 : 8) == 0 && aligned};
         blocks += prep.sums.blocks;
     }
     if (f32) launch_k(fc8_prep_kernel<float>, blocks, 256, 0, s, prep); else launch_k(fc8_prep_kernel<bf16>, blocks, 256, 0, s, prep);
@@ -808,7 +816,7 @@ int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, co
         launch_k(fc8_join_kernel, join_blocks, 256, 0, s, join);
         ++n;
     }
-    if (db) {
+    if (db && p.chunks > 1) {
         launch_k(fc8_db_kernel, (out + 31) / 32, 256, 0, s, (const float *)(base + p.db), db, p.chunks, out);
         ++n;
     }

@@ -72,14 +72,22 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsPerSm) fc8_rows_kernel(cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_holder)), "r"(kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    const int i0 = (int)((long)g.steps * rank / g.splits), i1 = (int)((long)g.steps * (rank + 1) / g.splits);  // not empty: splits <= steps
     pdl_launch();
+    // The first stages of W come into the L2 while the kernel before still runs.  That reads nothing: the L2 is where the memory's
+    // values are the same for all, and what that kernel may yet write of W is written there.
+    if (threadIdx.x == 0) {
+        for (int i = i0; i < min(i1, i0 + 2 * kCount); ++i)
+#pragma unroll
+            for (int j = 0; j < St::kw / 128; ++j)
+                asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(&map_w), "r"(i * St::kw + 128 * j), "r"(o0) : "memory");
+    }
     pdl_wait();
     for (int j = threadIdx.x; j < rows; j += kRowsThreads) s_scale[j] = g.row_scale[j0 + j];
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
-    const int i0 = (int)((long)g.steps * rank / g.splits), i1 = (int)((long)g.steps * (rank + 1) / g.splits);  // not empty: splits <= steps
     uint32_t issued = 0;
     bool issuer = false, ok = true;
     if (warp == 0) {

@@ -155,7 +155,7 @@ class Fc:
         ew = (4 * parts * math.ceil(self.B / 16) + 16) * E * mw + u * mw
         dx, dw, db = dy @ w, dy.t() @ x, dy.sum(0)
         ut = U[DT[self.prec]]
-        return (dx, ex + ut * dx.abs() + 1e-30), (dw, ew + (ut if dw_u is None else dw_u) * dw.abs() + 1e-30), (db, (math.ceil(self.B / 8) + 16) * E * dy.abs().sum(0))
+        return (dx, ex + ut * dx.abs() + 1e-30), (dw, ew + (ut if dw_u is None else dw_u) * dw.abs() + 1e-30), (db, (math.ceil(self.B / 4) + 16) * E * dy.abs().sum(0))  # no chain of additions is longer
 
     def fwd(self, b, y_f32=False, stream=None, y=None):
         y = torch.full((self.B, self.V), 7.0, dtype=torch.float32 if y_f32 else DT[self.prec], device="cuda") if y is None else y
