@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     __shared__ uint64_t full[kRingMostStages];
     __shared__ __align__(16) float red[6][32];
     __shared__ int abort_flag;
-    const int t = threadIdx.x;
+    const int t = threadIdx.x, threads = blockDim.x;
     RowRing<1> ring(shape, smem_u32(ring_smem), full, &abort_flag);
     if (t == 0) ring.init();
     if (t < 32) {
@@ -81,9 +81,8 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     pdl_launch();
     pdl_wait();
     const int first = (int)((long)rows * blockIdx.x / gridDim.x), last = (int)((long)rows * (blockIdx.x + 1) / gridDim.x);
-    const void *const src[1] = {x};
-    if (t == 0)
-        for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, src);
+    ring.sources({x});
+    for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row);
     uint32_t round = 0;
     for (int row = first; row < last; ++row) {
         const bool ok = ring.wait();
@@ -95,7 +94,7 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 in[G];
-            slot_load<T, VEC>(slot, at, x + (size_t)row * C, C, i, in);
+            slot_load<T, VEC>(slot, at, x + (size_t)row * C, C, threads, i, in);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 v[i * G + j] = in[j];
@@ -103,14 +102,14 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
                 top = max(top, max(magnitude_bits(p.x), magnitude_bits(p.y)));
             }
         }
-        top = ring_max(top, red, round);
-        if (t == 0 && row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, src);
+        top = ring_max(top, threads >> 5, red, round);
+        if (row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages);
         float s;
         const Act8Row r = act8_row(top, s);
         if (t == 0) scale[row] = s;
         int8_t *to = q + (size_t)row * pitch;
-        act8_share_store<sizeof(T) == 2 ? kBf16 : kF32, VEC, ITER>(to, C, v, r);
-        for (int c = C + t; c < pitch; c += blockDim.x) to[c] = 0;
+        act8_share_store<sizeof(T) == 2 ? kBf16 : kF32, VEC, ITER>(to, C, threads, v, r);
+        for (int c = C + t; c < pitch; c += threads) to[c] = 0;
     }
     if (t == 0) ring.drain();
 }
@@ -164,7 +163,15 @@ __global__ void __launch_bounds__(256) act8_unpack_kernel(const int8_t *__restri
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = (float)(int8_t)(word[j / 4] >> (8 * (j % 4))) * s[u];
             constexpr int N = Vec16<T>::N;
-            if (vec) {
+            if (vec == 2) {  // whole 32-byte sectors
+#pragma unroll
+                for (int j = 0; j < 16; j += 2 * N) {
+                    uint32_t o[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = sizeof(T) == 2 ? pack2(v[sizeof(T) == 2 ? 2 * k : 0], v[sizeof(T) == 2 ? 2 * k + 1 : 0]) : __float_as_uint(v[(j + k) % 16]);
+                    st_global_32(to + j, o);
+                }
+            } else if (vec) {
 #pragma unroll
                 for (int j = 0; j < 16; j += N)
                     if (c + j < C) store_f<T, N>(to + j, reinterpret_cast<const float(&)[N]>(v[j]));
@@ -208,7 +215,7 @@ template <typename T> int pack_wide(const void *x, void *q, float *scale, int ro
 template <typename T> int unpack_as(const void *q, const float *scale, void *x, int rows, int C, const Launch &s) {
     const int pitch = act8_pitch(C);
     const size_t units = (size_t)rows * (pitch / 16);
-    const int grid = (int)std::min<size_t>((units + 1023) / 1024, 148 * 8), vec = C % Vec16<T>::N == 0 && vec_ok(x);
+    const int grid = (int)std::min<size_t>((units + 1023) / 1024, 148 * 8), vec = C % 16 == 0 && (reinterpret_cast<uintptr_t>(x) & 31) == 0 ? 2 : C % Vec16<T>::N == 0 && vec_ok(x);
     launch_k(act8_unpack_kernel<T>, grid, 256, 0, s, (const int8_t *)q, scale, (T *)x, units, C, pitch, vec);
     return 1;
 }

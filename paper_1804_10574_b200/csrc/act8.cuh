@@ -97,11 +97,11 @@ template <Act8Kind KIND, int VEC> __device__ __forceinline__ void act8_store(int
 }
 
 // A thread's pairs (see row_ring.cuh) to a row of codes.
-template <Act8Kind KIND, int VEC, int ITER> __device__ __forceinline__ void act8_share_store(int8_t *row, int C, const F2 (&v)[VEC * ITER / 2], const Act8Row &r) {
+template <Act8Kind KIND, int VEC, int ITER> __device__ __forceinline__ void act8_share_store(int8_t *row, int C, int threads, const F2 (&v)[VEC * ITER / 2], const Act8Row &r) {
     if constexpr (VEC > 1) {
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
+            const int c = (i * threads + threadIdx.x) * VEC;
             F2 x[VEC / 2];
             uint32_t w[VEC / 4];
 #pragma unroll
@@ -116,7 +116,7 @@ template <Act8Kind KIND, int VEC, int ITER> __device__ __forceinline__ void act8
         act8_codes<KIND, ITER>(v, r, w);
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = i * blockDim.x + threadIdx.x;
+            const int c = i * threads + threadIdx.x;
             if (c < C) row[c] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
         }
     }

@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "act8.cuh"
+#include "cluster.cuh"
 #include "common.cuh"
 #include "lm_ops.h"
 #include "row_io.cuh"
@@ -151,14 +152,13 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
     pdl_launch();
     pdl_wait();
     const int first = (int)((long)g.rows * blockIdx.x / gridDim.x), last = (int)((long)g.rows * (blockIdx.x + 1) / gridDim.x);
-    const void *const src[2] = {g.b, g.res};
-    if (t == 0)
-        for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, src);
+    ring.sources({g.b, g.res});
+    for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row);
     constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
     typedef Share<T, VEC, ITER> Row;
     Row pre;
     F2 pg[P];   // gamma_post times the gate
-    pre.load((const T *)g.pre, C);
+    pre.load((const T *)g.pre, C, threads);
     int left = 0;  // rows that pg is for
     const float inv_c = 1.f / (float)C;
     const F2 alpha = f2(g.alpha);
@@ -166,12 +166,12 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
     for (int row = first; row < last; ++row) {
         if (left == 0) {
             Row w;
-            w.load((const T *)g.post, C);
+            w.load((const T *)g.post, C, threads);
 #pragma unroll
             for (int k = 0; k < P; ++k) pg[k] = w.pair(k);
             left = 1 << 30;
             if (g.gate) {
-                w.load((const T *)g.gate + (size_t)(row / g.span) * C, C);
+                w.load((const T *)g.gate + (size_t)(row / g.span) * C, C, threads);
 #pragma unroll
                 for (int k = 0; k < P; ++k) pg[k] = pg[k] * w.pair(k);
                 left = g.span - row % g.span;
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 in[G];
-            slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, i, in);
+            slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, threads, i, in);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 v[i * G + j] = in[j];
@@ -196,15 +196,15 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
             }
         }
         sum[0] = ok ? sum2(s2) : __int_as_float(0x7fffffff);  // a row that did not come is NaN
-        ring_sum<1>(sum, red, round);
-        if (t == 0 && row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, src);
+        ring_sum<1>(sum, threads >> 5, red, round);
+        if (row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages);
         const float r1 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
         s2 = f2(0.f);
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 res[G];
-            slot_load<T, VEC>(slot_res, at, (const T *)g.res + start, C, i, res);
+            slot_load<T, VEC>(slot_res, at, (const T *)g.res + start, C, threads, i, res);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 const int k = i * G + j;
@@ -216,11 +216,11 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
                     top = max(top, max(__float_as_uint(p.x) & 0x7fffffffu, __float_as_uint(p.y) & 0x7fffffffu));
                 }
             }
-            group_store<T, VEC>((T *)g.h + start, C, i, res);
+            group_store<T, VEC>((T *)g.h + start, C, threads, i, res);
         }
         sum[0] = sum2(s2);
-        if (CODES) ring_sum_max(sum[0], top, red, round);
-        else ring_sum<1>(sum, red, round);
+        if (CODES) ring_sum_max(sum[0], top, threads >> 5, red, round);
+        else ring_sum<1>(sum, threads >> 5, red, round);
         const float r2 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
         if (t == 0) {
             if (g.rstd_post) g.rstd_post[row] = r1;
@@ -228,14 +228,14 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
         }
 #pragma unroll
         for (int k = 0; k < P; ++k) v[k] = v[k] * f2(r2);
-        if (g.y) share_store<T, VEC, ITER>((T *)g.y + start, C, v);
+        if (g.y) share_store<T, VEC, ITER>((T *)g.y + start, C, threads, v);
         if (!CODES) continue;
         // the largest |y| is the largest |h gamma_pre| times rstd_pre: known with the sum
         float s;
         const Act8Row code = act8_row(__float_as_uint(__uint_as_float(top) * r2) & 0x7fffffffu, s);
         if (t == 0) g.scale[row] = s;
         int8_t *to = g.q + (size_t)row * g.pitch;
-        act8_share_store<kNear, VEC, ITER>(to, C, v, code);
+        act8_share_store<kNear, VEC, ITER>(to, C, threads, v, code);
         for (int c = C + t; c < g.pitch; c += threads) to[c] = 0;
     }
     if (t == 0) ring.drain();
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     // share of dgamma_post over several stretches: [C], a thread its own columns
     float *const a_post = g.several ? reinterpret_cast<float *>(ring_smem + (size_t)shape.stages * 4 * shape.slot_bytes) : nullptr;
     if (a_post)
-        for (int c = t; c < C; c += threads) a_post[c] = 0.f;  // (a barrier follows)
+        for (int c = t; c < C; c += blockDim.x) a_post[c] = 0.f;  // (a barrier follows)
     RowRing<4> ring(shape, smem_u32(ring_smem), full, &abort_flag);
     if (t == 0) ring.init();
     if (t < 32) {
@@ -425,17 +425,16 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     __syncthreads();
     pdl_launch();
     pdl_wait();
-    const void *const src[4] = {g.dy, g.h, g.b, g.dh};
+    ring.sources({g.dy, g.h, g.b, g.dh});
     NormRows ahead(g);
-    if (t == 0)
-        for (int i = 0; i < shape.stages && ahead.more(); ++i, ahead.next()) ring.copy(ahead.row, src);
+    for (int i = 0; i < shape.stages && ahead.more(); ++i, ahead.next()) ring.copy(ahead.row);
     constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
     typedef Share<T, VEC, ITER> Row;
-    Row pre;
     F2 a_pre[P], a_unit[P], pg[P];  // pg: gamma_post times the gate
-    pre.load((const T *)g.pre, C);
 #pragma unroll
-    for (int k = 0; k < P; ++k) a_pre[k] = f2(0.f);
+    for (int k = 0; k < P; ++k) a_pre[k] = a_unit[k] = pg[k] = f2(0.f);  // (a cluster's last blocks may have no stretch)
+    Row pre;
+    pre.load((const T *)g.pre, C, threads);
     const float inv_c = 1.f / (float)C;
     const F2 alpha = f2(g.alpha);
     uint32_t round = 0;
@@ -446,19 +445,22 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
         const T *gate_row = g.gate ? (const T *)g.gate + (size_t)gate * C : nullptr;
         {
             Row w;
-            w.load((const T *)g.post, C);
+            w.load((const T *)g.post, C, threads);
 #pragma unroll
             for (int k = 0; k < P; ++k) pg[k] = w.pair(k);
             if (gate_row) {
-                w.load(gate_row, C);
+                w.load(gate_row, C, threads);
 #pragma unroll
                 for (int k = 0; k < P; ++k) pg[k] = pg[k] * w.pair(k);
             }
         }
 #pragma unroll
         for (int k = 0; k < P; ++k) a_unit[k] = f2(0.f);
+        float next1 = 0.f, next2 = 0.f;
+        if (r0 < r1) { next1 = g.rstd_post[r0]; next2 = g.rstd_pre[r0]; }
         for (int row = r0; row < r1; ++row) {
-            const float s1 = g.rstd_post[row], s2 = g.rstd_pre[row];
+            const float s1 = next1, s2 = next2;  // loaded a row ahead
+            if (row + 1 < r1) { next1 = g.rstd_post[row + 1]; next2 = g.rstd_pre[row + 1]; }
             const bool ok = ring.wait();
             const uint32_t slot_dy = ring.slot(0), slot_h = ring.slot(1), slot_b = ring.slot(2), slot_dh = ring.slot(3);
             const RingRow at = ring_row(shape, row);
@@ -466,10 +468,10 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
             ring.next();
             F2 q0 = f2(0.f), q1 = f2(0.f), q2 = f2(0.f), dy[G], h[G], b[G], dh[G];
             auto load = [&](int i) {
-                slot_load<T, VEC>(slot_dy, at, (const T *)g.dy + start, C, i, dy);
-                slot_load<T, VEC>(slot_h, at, (const T *)g.h + start, C, i, h);
-                slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, i, b);
-                if (g.dh) slot_load<T, VEC>(slot_dh, at, (const T *)g.dh + start, C, i, dh);
+                slot_load<T, VEC>(slot_dy, at, (const T *)g.dy + start, C, threads, i, dy);
+                slot_load<T, VEC>(slot_h, at, (const T *)g.h + start, C, threads, i, h);
+                slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, threads, i, b);
+                if (g.dh) slot_load<T, VEC>(slot_dh, at, (const T *)g.dh + start, C, threads, i, dh);
             };
 #pragma unroll
             for (int i = 0; i < P / G; ++i) {
@@ -484,9 +486,9 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
                 }
             }
             float sum[3] = {ok ? sum2(q0) : __int_as_float(0x7fffffff), sum2(q1), sum2(q2)};  // a row that did not come is NaN
-            ring_sum<3>(sum, red, round);
-            if (t == 0 && begun && ahead.more()) {
-                ring.copy(ahead.row, src);
+            ring_sum<3>(sum, threads >> 5, red, round);
+            if (begun && ahead.more()) {
+                ring.copy(ahead.row);
                 ahead.next();
             }
             begun = true;
@@ -505,49 +507,79 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
                     b[j] = fma2(pg[k], f2(s1) * tt, f2(-c1) * x);
                     h[j] = alpha * tt;
                 }
-                group_store<T, VEC>((T *)g.dres + start, C, i, h);
-                group_store<T, VEC>((T *)g.db + start, C, i, b);
+                group_store<T, VEC>((T *)g.dres + start, C, threads, i, h);
+                group_store<T, VEC>((T *)g.db + start, C, threads, i, b);
             }
         }
-        // the stretch's one sum times the gate: its share of dgamma_post; times gamma_post: dgate's
-        const bool final = unit + gridDim.x >= g.gates * g.parts;
-        Row w;
-        if (gate_row) w.load(gate_row, C);
-        F2 v[P];
-#pragma unroll
-        for (int k = 0; k < P; ++k) v[k] = gate_row ? w.pair(k) * a_unit[k] : a_unit[k];
-        if (a_post) {
+        // The stretch's one sum times the gate is its share of dgamma_post; times gamma_post, dgate's.  With one gate for all rows
+        // both products are left to the folding kernel.
+        if (g.gates > 1) {
+            Row w;
+            if (gate_row) w.load(gate_row, C, threads);
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                const int c = VEC > 1 ? ((2 * k / VEC) * threads + t) * VEC + 2 * k % VEC : 2 * k * threads + t, d = VEC > 1 ? c + 1 : c + threads;  // columns of the pair
-                if (c < C) v[k] = f2(a_post[c], d < C ? a_post[d] : 0.f) + v[k];
-                const float2 p = parts(v[k]);
-                if (c < C) a_post[c] = p.x;
-                if (d < C) a_post[d] = p.y;
+                const F2 v = gate_row ? w.pair(k) * a_unit[k] : a_unit[k];
+                if (a_post) {
+                    const int c = VEC > 1 ? ((2 * k / VEC) * threads + t) * VEC + 2 * k % VEC : 2 * k * threads + t, d = VEC > 1 ? c + 1 : c + threads;  // columns of the pair
+                    const float2 p = parts(v);
+                    if (c < C) a_post[c] += p.x;
+                    if (d < C) a_post[d] += p.y;
+                } else {
+                    pg[k] = v;  // the block's only stretch: pg has done its work
+                }
+            }
+            if (g.dgate) {
+                w.load((const T *)g.post, C, threads);
+#pragma unroll
+                for (int k = 0; k < P; ++k) a_unit[k] = a_unit[k] * w.pair(k);
+                share_store_f32<VEC, ITER>(g.parts > 1 ? g.piece + (size_t)unit * C : g.dgate + (size_t)gate * C, C, threads, a_unit);
             }
         }
-        if (final) share_store_f32<VEC, ITER>(g.part + (size_t)blockIdx.x * 2 * C, C, v);
-        if (g.dgate) {
-            w.load((const T *)g.post, C);
-#pragma unroll
-            for (int k = 0; k < P; ++k) a_unit[k] = a_unit[k] * w.pair(k);
-            share_store_f32<VEC, ITER>(g.parts > 1 ? g.piece + (size_t)unit * C : g.dgate + (size_t)gate * C, C, a_unit);
-        }
     }
-    share_store_f32<VEC, ITER>(g.part + (size_t)blockIdx.x * 2 * C + C, C, a_pre);
     if (t == 0) ring.drain();
+    // The block's shares of the two sums over all rows take the ring's place; the cluster's blocks add theirs up, a slice of the
+    // columns each, blocks in index order.
+    __syncthreads();
+    float *const mine = reinterpret_cast<float *>(ring_smem);
+    const int pitch = (C + 3) & ~3;
+    if (a_post) {
+        for (int c = t; c < C; c += threads) mine[c] = a_post[c];  // (another place: the stages are in front of it)
+    } else {
+        share_store_f32<VEC, ITER>(mine, C, threads, g.gates > 1 ? pg : a_unit);
+    }
+    share_store_f32<VEC, ITER>(mine + pitch, C, threads, a_pre);
+    cluster_sync();
+    uint32_t blocks;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
+    const uint32_t rank = cluster_rank(), at = smem_u32(mine);
+    float *const to = g.part + (size_t)(blockIdx.x / blocks) * 2 * C;
+    for (int c = (int)(rank * blockDim.x) + t; c < C; c += (int)(blocks * blockDim.x)) {
+        float post[8] = {}, pre_sum[8] = {};
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r)
+            if (r < blocks) {
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(post[r]) : "r"(map_rank(at + 4u * c, r)));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(pre_sum[r]) : "r"(map_rank(at + 4u * (pitch + c), r)));
+            }
+#pragma unroll
+        for (int r = 1; r < 8; ++r) { post[0] += post[r]; pre_sum[0] += pre_sum[r]; }
+        to[c] = post[0];
+        to[C + c] = pre_sum[0];
+    }
+    cluster_sync();  // no block leaves while its shares are read
 }
 
 // Shares in index order per warp, warps in index order, 32 columns per block.  blockIdx.y: dpost, dpre, then the gate's rows.
-__global__ void __launch_bounds__(1024) block_norm_fold_kernel(const float *__restrict__ part, const float *__restrict__ piece, int blocks, int parts, float *__restrict__ dpost,
-                                                               float *__restrict__ dpre, float *__restrict__ dgate, int C) {
+// gate and post (nullable): the first shares are still to be multiplied with the one gate, for dpost, and with gamma_post, for dgate.
+struct NormFold { const float *part, *piece; float *dpost, *dpre, *dgate; const void *gate, *post; int n, parts, C, one_gate; };
+template <typename T> __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const __grid_constant__ NormFold g) {
     __shared__ float fold[32][32];
     pdl_launch();
     pdl_wait();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, what = blockIdx.y, gate = what - 2;
-    const float *from = what < 2 ? part + (size_t)what * C : piece + (size_t)gate * parts * C;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, C = g.C, c = blockIdx.x * 32 + lane, what = blockIdx.y, gate = what - 2;
+    const float *from = what < 2 ? g.part + (size_t)what * C : g.piece + (size_t)gate * g.parts * C;
     const size_t stride = what < 2 ? 2 * (size_t)C : (size_t)C;
-    const int n = what < 2 ? blocks : parts;
+    const int n = what < 2 ? g.n : g.parts;
     float a = 0.f;
     if (c < C) {
 #pragma unroll 8
@@ -557,7 +589,11 @@ __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const float *__re
     __syncthreads();
     if (w == 0 && c < C) {
         for (int i = 1; i < 32; ++i) a += fold[i][lane];
-        (what == 0 ? dpost : (what == 1 ? dpre : dgate + (size_t)gate * C))[c] = a;
+        if (what == 0 && g.one_gate) {
+            if (g.dgate) g.dgate[c] = a * to_f(((const T *)g.post)[c]);
+            if (g.gate) a *= to_f(((const T *)g.gate)[c]);
+        }
+        (what == 0 ? g.dpost : (what == 1 ? g.dpre : g.dgate + (size_t)gate * C))[c] = a;
     }
 }
 
@@ -567,17 +603,21 @@ __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const float *__re
 RingPlan norm_ring(int rows, int C, int vec, int es, bool backward) {
     // narrow rows are a warp's of the other kernel
     if (rows < 2 * 148 || ring_threads((C + vec - 1) / vec, vec == 1 ? 8 : (backward ? 2 : 4)) < 64) return RingPlan{};
-    return backward ? ring_plan(C, C * es, vec, vec == 1 ? 8 : 2, 4, (size_t)C * 4) : ring_plan(C, C * es, vec, vec == 1 ? 8 : 4, 2, 0);
+    if (!backward) return ring_plan(C, C * es, vec, vec == 1 ? 8 : 4, 2, 0);
+    return ring_plan(C, C * es, vec, vec == 1 ? 8 : 2, 4, (size_t)C * 4);
 }
 
 // How the rows of a backward pass are dealt out: `blocks` of the launch, stretches per gate, a block or a warp a stretch.
-struct BwdPlan { RingPlan ring; RmsPlan row; int blocks, parts, per_block; };
+// cluster: blocks of the ring kernel that add up their shares before they leave them.
+struct BwdPlan { RingPlan ring; RmsPlan row; int blocks, parts, per_block, cluster; };
 BwdPlan bwd_plan(int rows, int C, int span, int vec, int es, bool ring) {
     BwdPlan p{};
     if (ring) p.ring = norm_ring(rows, C, vec, es, true);
     p.row = rms_plan(C / vec, vec > 1, 2, 256);
     const bool warp = p.ring.threads == 0 && p.row.tpr == 32;
     const int gates = (rows - 1) / span + 1, longest = std::min(span, rows);
+    p.cluster = 1;
+    if (p.ring.threads && p.ring.per_sm > 1) p.cluster = 2;  // (of larger clusters the GPU holds fewer blocks than of single ones)
     const int most = 148 * (p.ring.threads ? p.ring.per_sm : (warp ? 2 : std::max(1, (p.row.iter == 1 ? 1024 : 512) / p.row.threads)));
     // rounds of the resident blocks, in rows; leaving a stretch's share costs about a row
     double best = 1e30;
@@ -595,6 +635,7 @@ BwdPlan bwd_plan(int rows, int C, int span, int vec, int es, bool ring) {
     }
     const long units = (long)gates * p.parts;
     p.blocks = (int)std::min<long>(most, p.per_block ? units : (units + 7) / 8);
+    p.blocks = (p.blocks + p.cluster - 1) / p.cluster * p.cluster;
     return p;
 }
 size_t bwd_scratch(const BwdPlan &p, int rows, int C, int span) {
@@ -628,7 +669,17 @@ template <typename T, int VEC, bool SHIFT> int fwd_as(const BlockNormFwd &g, con
 template <typename T, int VEC, int ITER> int bwd_ring(const BlockNormBwd &g, const BwdPlan &p, const Launch &s) {
     static thread_local int ready = -1;
     if (!ring_ready(block_norm_bwd_ring_kernel<T, VEC, ITER>, ready)) return -1;
-    launch_k(block_norm_bwd_ring_kernel<T, VEC, ITER>, p.blocks, p.ring.threads, p.ring.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), kSpinLimit));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.blocks); cfg.blockDim = dim3(p.ring.threads); cfg.dynamicSmemBytes = p.ring.smem; cfg.stream = s.s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = p.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = s.pdl == 1 ? 2 : 1;
+    cudaLaunchKernelEx(&cfg, block_norm_bwd_ring_kernel<T, VEC, ITER>, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), kSpinLimit));
     return 1;
 }
 
@@ -640,7 +691,7 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scr
     const size_t smem = p.row.tpr == 32 ? (size_t)8 * ((g.C + 3) & ~3) * sizeof(float) : 0;
     auto go = [&](auto kernel) { launch_k(kernel, p.blocks, p.row.threads, smem, s, g); };
     if (p.ring.threads) {
-        g.several = (long)g.gates * g.parts > p.blocks;
+        g.several = (long)g.gates * g.parts > p.blocks;  // (with one gate never: its stretches are no more than the blocks)
         const int r = bwd_ring<T, VEC, VEC == 1 ? 8 : 2>(g, p, s);
         if (r < 0) return r;
     } else if (p.row.tpr == 32) {
@@ -655,8 +706,9 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scr
         default: return -1;
         }
     }
-    launch_k(block_norm_fold_kernel, dim3((g.C + 31) / 32, 2 + (g.dgate && p.parts > 1 ? g.gates : 0)), 1024, 0, s, (const float *)g.part, (const float *)g.piece, p.blocks,
-             p.parts, dpost, dpre, g.dgate, g.C);
+    const bool ring_one = p.ring.threads && g.gates == 1;
+    const NormFold fold{g.part, g.piece, dpost, dpre, g.dgate, g.gate, g.post, p.ring.threads ? p.blocks / p.cluster : p.blocks, p.parts, g.C, ring_one};
+    launch_k(block_norm_fold_kernel<T>, dim3((g.C + 31) / 32, 2 + (g.dgate && p.parts > 1 && !ring_one ? g.gates : 0)), 1024, 0, s, fold);
     return 2;
 }
 

@@ -1,4 +1,4 @@
-// Rows on their way through shared memory: a block's first thread copies the rows that the block will work on, several ahead,
+// Rows on their way through shared memory: a block copies the rows that it will work on, several ahead,
 // by bulk copies (TMA without a tensor map) into a ring of stages.  The threads read their values from there as often as they
 // need them; after the first barrier of the next row's reductions, when all are done with a row, its stage takes another.
 // Memory stays busy through the reductions, without registers for what is on the way or for what is needed again.
@@ -36,34 +36,43 @@ template <int TENSORS> struct RowRing {
     uint32_t base;      // shared memory of the stages
     uint64_t *full;
     Waiter wt;
-    uint32_t stage, parity, issued;
+    uint32_t stage, parity;  // of the row that is read next
+    uint32_t head, issued;   // stage that is filled next; rows that this thread had copied
+    const uint8_t *src[TENSORS];  // nullptr: a tensor that is not there
+    int tensors;
 
     __device__ __forceinline__ RowRing(const RingShape &shape, uint32_t smem, uint64_t *full_, int *abort_flag)
-        : g(shape), base(smem), full(full_), wt{abort_flag, abort_flag, shape.polls}, stage(0), parity(0), issued(0) {}
+        : g(shape), base(smem), full(full_), wt{abort_flag, abort_flag, shape.polls}, stage(0), parity(0), head(0), issued(0), tensors(0) {}
 
     __device__ __forceinline__ void init() {  // by one thread, before a barrier of the block
         for (int i = 0; i < g.stages; ++i) mbar_init(smem_u32(&full[i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *wt.abort_flag = 0;
     }
-    // By the copying thread: the next row into the stage that is free.  A tensor that is not there (nullptr) is left out.  Nothing
-    // is copied any more once a wait ran out.
-    __device__ __forceinline__ void copy(int row, const void *const (&src)[TENSORS]) {
-        if (*wt.abort_flag) return;
-        const size_t at = (size_t)row * g.row_bytes, from = at & ~(size_t)15, to = min((at + g.row_bytes + 15) & ~(size_t)15, g.floor16);
-        const uint32_t s = issued % (uint32_t)g.stages, bytes = to > from ? (uint32_t)(to - from) : 0u, bar = smem_u32(&full[s]);
-        int n = 0;
+    __device__ __forceinline__ void sources(const void *const (&all)[TENSORS]) {
 #pragma unroll
-        for (int k = 0; k < TENSORS; ++k) n += src[k] != nullptr;
-        mbar_expect_tx(bar, bytes * n);
-        if (bytes) {
+        for (int k = 0; k < TENSORS; ++k) {
+            src[k] = (const uint8_t *)all[k];
+            tensors += all[k] != nullptr;
+        }
+    }
+    // By all threads: the next row into the stage that is free.  The first lane of each warp issues a share of the copies: each
+    // takes its warp a few hundred cycles.  Nothing is copied any more once a wait ran out.
+    __device__ __forceinline__ void copy(int row) {
+        const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+        if ((threadIdx.x & 31) == 0 && warp < TENSORS && !*wt.abort_flag) {
+            const size_t at = (size_t)row * g.row_bytes, from = at & ~(size_t)15, to = min((at + g.row_bytes + 15) & ~(size_t)15, g.floor16);
+            const uint32_t bytes = to > from ? (uint32_t)(to - from) : 0u, bar = smem_u32(&full[head]);
+            // (what lands before the barrier expects it is counted all the same: its phase ends with this arrival)
+            if (warp == 0) mbar_expect_tx(bar, bytes * tensors);
 #pragma unroll
             for (int k = 0; k < TENSORS; ++k)
-                if (src[k]) bulk_copy_g2s(base + (s * TENSORS + k) * g.slot_bytes, (const uint8_t *)src[k] + from, bytes, bar);
+                if (k % min(warps, TENSORS) == warp && src[k] && bytes) bulk_copy_g2s(base + (head * TENSORS + k) * g.slot_bytes, src[k] + from, bytes, bar);
+            ++issued;
         }
-        ++issued;
+        if (++head == (uint32_t)g.stages) head = 0;
     }
-    // The copying thread, at its end: what it issued has landed, whatever became of the readers.
+    // The first thread, at its end: what was issued has landed, whatever became of the readers.
     __device__ __forceinline__ void drain() {
         for (uint32_t i = issued > (uint32_t)g.stages ? issued - g.stages : 0; i < issued; ++i) mbar_drain(smem_u32(&full[i % g.stages]), (i / g.stages) & 1u);
     }
@@ -78,11 +87,16 @@ template <int TENSORS> struct RowRing {
 template <int VEC> constexpr int kGroup = VEC > 1 ? VEC / 2 : 1;  // pairs
 
 // Group i of a row in a slot.  Value c stands at phase + c * sizeof(T); vectors: phase 0, and all of the row is there.
-template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_t slot, const RingRow &at, const T *row, int C, int i, F2 (&v)[kGroup<VEC>]) {
+template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_t slot, const RingRow &at, const T *row, int C, int threads, int i, F2 (&v)[kGroup<VEC>]) {
     if constexpr (VEC > 1) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
+        const int c = (i * threads + threadIdx.x) * VEC;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (c < C) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(slot + c * (uint32_t)sizeof(T)));
+        const uint32_t from = slot + c * (uint32_t)sizeof(T);
+        if constexpr (VEC * sizeof(T) == 16) {
+            if (c < C) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from));
+        } else {
+            if (c < C) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from));
+        }
 #pragma unroll
         for (int j = 0; j < VEC / 2; ++j) {
             if constexpr (sizeof(T) == 2) v[j] = bf16_pair(w[j]);
@@ -92,18 +106,17 @@ template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_
         float e[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int c = (2 * i + j) * blockDim.x + threadIdx.x;
-            if (c >= C) {
-                e[j] = 0.f;
-            } else if (c * (int)sizeof(T) >= at.valid) {
-                e[j] = to_f(row[c]);
+            const int c = (2 * i + j) * threads + threadIdx.x, in = min(c, C - 1);
+            if (at.valid < C * (int)sizeof(T) && in * (int)sizeof(T) >= at.valid) {  // the last row's last few
+                e[j] = to_f(row[in]);
             } else if constexpr (sizeof(T) == 2) {
                 uint16_t w;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(slot + at.phase + c * 2u));
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(slot + at.phase + in * 2u));
                 e[j] = __uint_as_float((uint32_t)w << 16);
             } else {
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(e[j]) : "r"(slot + at.phase + c * 4u));
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(e[j]) : "r"(slot + at.phase + in * 4u));
             }
+            e[j] = c < C ? e[j] : 0.f;
         }
         v[0] = f2(e[0], e[1]);
     }
@@ -111,14 +124,22 @@ template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_
 // A thread's share of what all rows have in common, as it lies in memory.
 template <typename T, int VEC, int ITER> struct Share {
     static constexpr int N = VEC * ITER;
-    static_assert(N % 2 == 0 && (VEC == 1 || VEC * sizeof(T) == 16), "whole units or single values");
+    static_assert(N % 2 == 0 && (VEC == 1 || VEC * sizeof(T) == 8 || VEC * sizeof(T) == 16), "vectors of 8 or 16 bytes, or single values");
+    typedef Pack<T, VEC> Vec;
     alignas(16) T e[N];
-    __device__ __forceinline__ void load(const T *row, int C) {
+    __device__ __forceinline__ void load(const T *row, int C, int threads) {
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * blockDim.x + threadIdx.x) * VEC;
-            if constexpr (VEC > 1) *reinterpret_cast<uint4 *>(e + i * VEC) = c < C ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0u, 0u, 0u, 0u);
-            else e[i] = c < C ? row[c] : from_f<T>(0.f);
+            const int c = (i * threads + threadIdx.x) * VEC;
+            if constexpr (VEC > 1) {
+                Vec p;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.v[j] = from_f<T>(0.f);
+                if (c < C) p = *reinterpret_cast<const Vec *>(row + c);
+                *reinterpret_cast<Vec *>(e + i * VEC) = p;
+            } else {
+                e[i] = c < C ? row[c] : from_f<T>(0.f);
+            }
         }
     }
     __device__ __forceinline__ F2 pair(int k) const {  // values 2k and 2k + 1
@@ -127,38 +148,42 @@ template <typename T, int VEC, int ITER> struct Share {
     }
 };
 // Group i to a row in memory, in the element type.
-template <typename T, int VEC> __device__ __forceinline__ void group_store(T *row, int C, int i, const F2 (&v)[kGroup<VEC>]) {
+template <typename T, int VEC> __device__ __forceinline__ void group_store(T *row, int C, int threads, int i, const F2 (&v)[kGroup<VEC>]) {
     if constexpr (VEC > 1) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
-        uint32_t w[4];
+        const int c = (i * threads + threadIdx.x) * VEC;
+        constexpr int W = VEC * sizeof(T) / 4;
+        uint32_t w[W];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < W; ++j) {
             if constexpr (sizeof(T) == 2) w[j] = to_bf16_pair(v[j]);
             else w[j] = __float_as_uint(j % 2 ? parts(v[j / 2]).y : parts(v[j / 2]).x);
         }
-        if (c < C) *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (c < C) {
+            if constexpr (W == 4) *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
+        }
     } else {
-        const int c = 2 * i * blockDim.x + threadIdx.x, d = c + blockDim.x;
+        const int c = 2 * i * threads + threadIdx.x, d = c + threads;
         const float2 p = parts(v[0]);
         if (c < C) row[c] = from_f<T>(p.x);
         if (d < C) row[d] = from_f<T>(p.y);
     }
 }
-template <typename T, int VEC, int ITER> __device__ __forceinline__ void share_store(T *row, int C, const F2 (&v)[VEC * ITER / 2]) {
+template <typename T, int VEC, int ITER> __device__ __forceinline__ void share_store(T *row, int C, int threads, const F2 (&v)[VEC * ITER / 2]) {
     constexpr int G = kGroup<VEC>;
 #pragma unroll
     for (int i = 0; i < VEC * ITER / 2 / G; ++i) {
         F2 g[G];
 #pragma unroll
         for (int j = 0; j < G; ++j) g[j] = v[i * G + j];
-        group_store<T, VEC>(row, C, i, g);
+        group_store<T, VEC>(row, C, threads, i, g);
     }
 }
 // The same as fp32; the row starts on a 16-byte boundary (VEC > 1).
-template <int VEC, int ITER> __device__ __forceinline__ void share_store_f32(float *row, int C, const F2 (&v)[VEC * ITER / 2]) {
+template <int VEC, int ITER> __device__ __forceinline__ void share_store_f32(float *row, int C, int threads, const F2 (&v)[VEC * ITER / 2]) {
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * VEC;
+        const int c = (i * threads + threadIdx.x) * VEC;
         if (c >= C) continue;
         if constexpr (VEC > 1) {
 #pragma unroll
@@ -172,11 +197,11 @@ template <int VEC, int ITER> __device__ __forceinline__ void share_store_f32(flo
     }
 }
 
-// Sums (or, as bits, maxima) over a row's threads, which are the block: one barrier, buffers of two rounds in turn (red: six
+// Sums (or, as bits, maxima) over the threads of `warps` warps, the block's first ones: one barrier of the block, buffers of two rounds in turn (red: six
 // times 32 floats, zeros at first, on a 16-byte boundary; what is summed and what is a maximum keep to their own rows).
-template <int N> __device__ __forceinline__ void ring_sum(float (&v)[N], float (*red)[32], uint32_t &round) {
+template <int N> __device__ __forceinline__ void ring_sum(float (&v)[N], int warps, float (*red)[32], uint32_t &round) {
     static_assert(N <= 3, "the buffers' size");
-    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
     float (*to)[32] = red + (round & 1u) * 3;
@@ -198,8 +223,8 @@ template <int N> __device__ __forceinline__ void ring_sum(float (&v)[N], float (
     }
 }
 // A sum and a maximum (of bits) in one round.
-__device__ __forceinline__ void ring_sum_max(float &sum, uint32_t &top, float (*red)[32], uint32_t &round) {
-    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ void ring_sum_max(float &sum, uint32_t &top, int warps, float (*red)[32], uint32_t &round) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     sum = warp_sum(sum);
     top = __reduce_max_sync(0xffffffffu, top);
     float (*to)[32] = red + (round & 1u) * 3;
@@ -214,8 +239,8 @@ __device__ __forceinline__ void ring_sum_max(float &sum, uint32_t &top, float (*
         top = max(max(top, max(m.x, m.y)), max(m.z, m.w));
     }
 }
-__device__ __forceinline__ uint32_t ring_max(uint32_t v, float (*red)[32], uint32_t &round) {
-    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ uint32_t ring_max(uint32_t v, int warps, float (*red)[32], uint32_t &round) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     v = __reduce_max_sync(0xffffffffu, v);
     float *to = red[(round & 1u) * 3 + 1];
     ++round;
@@ -231,18 +256,21 @@ __device__ __forceinline__ uint32_t ring_max(uint32_t v, float (*red)[32], uint3
 // ---- host side -------------------------------------------------------------------------------------------------------
 // Threads of a row (whole warps) that have `iter` vectors each.
 inline int ring_threads(int nvec, int iter) { return ((nvec + iter - 1) / iter + 31) / 32 * 32; }
-constexpr size_t kRingSmem = 216 * 1024;
+// Dynamic shared memory of a block, of per_sm that an SM holds: what it has (228 KB) less 1 KB of the system's and 1 KB of
+// variables for each.
+inline size_t ring_smem_of(int per_sm) { return (size_t)(226 * 1024 / per_sm - 2048) / 16 * 16; }
 // Blocks of an SM for rows of `threads` threads, and the shared memory of each; `extra` bytes of it are not the ring's.  Two
 // stages at least, else 0 blocks.
 struct RingPlan { int threads, per_sm; size_t smem; };
 inline RingShape ring_shape(int rows, int row_bytes, int tensors, size_t smem, unsigned polls);
-inline RingPlan ring_plan(int C, int row_bytes, int vec, int iter, int tensors, size_t extra) {
+// `registers` of a thread and `more` threads of a block besides the row's limit the blocks too.
+inline RingPlan ring_plan(int C, int row_bytes, int vec, int iter, int tensors, size_t extra, int registers = 128, int more = 0) {
     RingPlan p{};
     const int threads = std::max(64, ring_threads((C + vec - 1) / vec, iter));
     if (threads > 512) return p;
-    p.per_sm = std::min(8, std::max(1, 512 / threads));
-    while (p.per_sm > 1 && ring_shape(1, row_bytes, tensors, kRingSmem / p.per_sm / 16 * 16 - extra, 0).stages < 2) --p.per_sm;
-    p.smem = kRingSmem / p.per_sm / 16 * 16;
+    p.per_sm = std::min(8, 65536 / (registers * (threads + more)));
+    while (p.per_sm > 1 && ring_shape(1, row_bytes, tensors, ring_smem_of(p.per_sm) - extra, 0).stages < 2) --p.per_sm;
+    p.smem = ring_smem_of(p.per_sm);
     if (p.smem > extra && ring_shape(1, row_bytes, tensors, p.smem - extra, 0).stages >= 2) p.threads = threads;
     return p;
 }
@@ -250,7 +278,7 @@ template <typename K> bool ring_ready(K kernel, int &ready_dev) {
     int dev = 0;
     cudaGetDevice(&dev);
     if (ready_dev != dev) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem) != cudaSuccess) return false;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring_smem_of(1)) != cudaSuccess) return false;
         ready_dev = dev;
     }
     return true;
