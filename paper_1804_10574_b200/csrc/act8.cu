@@ -85,16 +85,16 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row);
     uint32_t round = 0;
     for (int row = first; row < last; ++row) {
-        const bool ok = ring.wait();
+        const bool ok = ring.wait<T, VEC>(row);
         const uint32_t slot = ring.slot(0);
-        const RingRow at = ring_row(shape, row);
+        const int phase = ring_phase(shape, row);
         ring.next();
         F2 v[P];
         uint32_t top = ok ? 0u : 0x7fffffffu;  // a row that did not come is NaN
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 in[G];
-            slot_load<T, VEC>(slot, at, x + (size_t)row * C, C, threads, i, in);
+            slot_load<T, VEC>(slot, phase, C, threads, i, in);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 v[i * G + j] = in[j];
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(1024) act8_pack_wide_kernel(const T *__restric
 
 // 16 codes of a row at a time, four of them on their way per thread.
 template <typename T>
-__global__ void __launch_bounds__(256) act8_unpack_kernel(const int8_t *__restrict__ q, const float *__restrict__ scale, T *__restrict__ x, size_t units, int C, int pitch, int vec) {
+__global__ void __launch_bounds__(256) act8_unpack_kernel(const int8_t *__restrict__ q, const float *__restrict__ scale, T *__restrict__ x, size_t units, int C, int pitch, int whole) {
     constexpr int kAhead = 4;
     pdl_launch();
     pdl_wait();
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(256) act8_unpack_kernel(const int8_t *__restri
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = (float)(int8_t)(word[j / 4] >> (8 * (j % 4))) * s[u];
             constexpr int N = Vec16<T>::N;
-            if (vec == 2) {  // whole 32-byte sectors
+            if (whole) {  // 32-byte sectors
 #pragma unroll
                 for (int j = 0; j < 16; j += 2 * N) {
                     uint32_t o[8];
@@ -171,16 +171,35 @@ __global__ void __launch_bounds__(256) act8_unpack_kernel(const int8_t *__restri
                     for (int k = 0; k < 8; ++k) o[k] = sizeof(T) == 2 ? pack2(v[sizeof(T) == 2 ? 2 * k : 0], v[sizeof(T) == 2 ? 2 * k + 1 : 0]) : __float_as_uint(v[(j + k) % 16]);
                     st_global_32(to + j, o);
                 }
-            } else if (vec) {
+            } else {
 #pragma unroll
                 for (int j = 0; j < 16; j += N)
                     if (c + j < C) store_f<T, N>(to + j, reinterpret_cast<const float(&)[N]>(v[j]));
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c + j < C) to[j] = from_f<T>(v[j]);
             }
         }
+    }
+}
+
+// Rows that keep to no boundary: 256 codes of a row per warp at a time, neighbouring ones to neighbouring lanes.
+template <typename T>
+__global__ void __launch_bounds__(256) act8_unpack_any_kernel(const int8_t *__restrict__ q, const float *__restrict__ scale, T *__restrict__ x, size_t units, int C, int pitch) {
+    constexpr int kCols = 256;
+    pdl_launch();
+    pdl_wait();
+    const unsigned per_row = (C + kCols - 1) / kCols;
+    const int lane = threadIdx.x & 31;
+    for (size_t i = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < units; i += (size_t)gridDim.x * 8) {
+        const size_t row = units <= 0xffffffffu ? (unsigned)i / per_row : i / per_row;
+        const int c0 = (int)(i - row * per_row) * kCols + lane;
+        const int8_t *from = q + row * pitch;
+        const float s = scale[row];
+        int8_t v[kCols / 32];
+#pragma unroll
+        for (int k = 0; k < kCols / 32; ++k)
+            if (c0 + 32 * k < C) v[k] = from[c0 + 32 * k];
+#pragma unroll
+        for (int k = 0; k < kCols / 32; ++k)
+            if (c0 + 32 * k < C) x[row * C + c0 + 32 * k] = from_f<T>((float)v[k] * s);
     }
 }
 
@@ -214,9 +233,14 @@ template <typename T> int pack_wide(const void *x, void *q, float *scale, int ro
 
 template <typename T> int unpack_as(const void *q, const float *scale, void *x, int rows, int C, const Launch &s) {
     const int pitch = act8_pitch(C);
+    if (C % Vec16<T>::N != 0 || !vec_ok(x)) {
+        const size_t units = (size_t)rows * ((C + 255) / 256);
+        launch_k(act8_unpack_any_kernel<T>, (int)std::min<size_t>((units + 7) / 8, 148 * 16), 256, 0, s, (const int8_t *)q, scale, (T *)x, units, C, pitch);
+        return 1;
+    }
     const size_t units = (size_t)rows * (pitch / 16);
-    const int grid = (int)std::min<size_t>((units + 1023) / 1024, 148 * 8), vec = C % 16 == 0 && (reinterpret_cast<uintptr_t>(x) & 31) == 0 ? 2 : C % Vec16<T>::N == 0 && vec_ok(x);
-    launch_k(act8_unpack_kernel<T>, grid, 256, 0, s, (const int8_t *)q, scale, (T *)x, units, C, pitch, vec);
+    const int whole = C % 16 == 0 && (reinterpret_cast<uintptr_t>(x) & 31) == 0;
+    launch_k(act8_unpack_kernel<T>, (int)std::min<size_t>((units + 1023) / 1024, 148 * 8), 256, 0, s, (const int8_t *)q, scale, (T *)x, units, C, pitch, whole);
     return 1;
 }
 
@@ -226,7 +250,7 @@ int launch_act8_pack(int prec, const void *x, void *q, float *scale, int rows, i
     const bool vec = vec_ok(x) && C % (prec == P_BF16 ? 8 : 4) == 0;
     const int per_vec = vec ? (prec == P_BF16 ? 8 : 4) : 1, iter = vec ? 4 : 8;
     if (rows >= 2 * 148 && vec_ok(x) && ring_threads((C + per_vec - 1) / per_vec, iter) >= 64) {  // narrow rows are a warp's of the other kernel
-        const RingPlan p = ring_plan(C, C * (int)elem_size(prec), per_vec, iter, 1, 0);
+        const RingPlan p = ring_plan(C, C * (int)elem_size(prec), per_vec, iter, 1, 0, 96);
         if (p.threads) {
             if (prec == P_BF16) return vec ? pack_ring<bf16, 8, 4>(x, q, scale, rows, C, p, s) : pack_ring<bf16, 1, 8>(x, q, scale, rows, C, p, s);
             return vec ? pack_ring<float, 4, 4>(x, q, scale, rows, C, p, s) : pack_ring<float, 1, 8>(x, q, scale, rows, C, p, s);

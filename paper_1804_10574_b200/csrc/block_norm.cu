@@ -178,17 +178,17 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
             }
         }
         --left;
-        const bool ok = ring.wait();
+        const bool ok = ring.wait<T, VEC>(row);
         const size_t start = (size_t)row * C;
         const uint32_t slot_b = ring.slot(0), slot_res = ring.slot(1);
-        const RingRow at = ring_row(shape, row);
+        const int phase = ring_phase(shape, row);
         ring.next();
         F2 v[P], s2 = f2(0.f);
         float sum[1];
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 in[G];
-            slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, threads, i, in);
+            slot_load<T, VEC>(slot_b, phase, C, threads, i, in);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 v[i * G + j] = in[j];
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 res[G];
-            slot_load<T, VEC>(slot_res, at, (const T *)g.res + start, C, threads, i, res);
+            slot_load<T, VEC>(slot_res, phase, C, threads, i, res);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 const int k = i * G + j;
@@ -279,11 +279,14 @@ __device__ __forceinline__ void row_sum3(float (&v)[3], bool one_warp, float (*r
     for (int k = 0; k < 3; ++k) v[k] = warp_sum(lane < nw ? red[k][lane] : 0.f);
 }
 
-// Stretches of rows that share a gate are dealt out to blocks (or warps): dgate's share stays in registers over a stretch,
-// those of dpost and dpre over all of a block's.  A row is written after it was read, by the threads that read it, so that
-// db and dres may be any of the tensors read row by row.
+// Stretches of rows that share a gate are dealt out to blocks, or to warps where a row is one warp's.  Over a stretch one sum per
+// column, of t b rstd_post, gives both dgate (times gamma_post) and the stretch's share of dgamma_post (times the gate).  A row is
+// written after it was read, by the threads that read it, so that db and dres may be any of the tensors read row by row.  A
+// warp's next row is loaded before this one is worked on where registers allow (ITER = 1).
 template <typename T, int VEC, int ITER, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : rms_max_threads(VEC, ITER), 1) block_norm_bwd_kernel(const BlockNormBwd g) {
+__global__ void __launch_bounds__(WARP ? 256 : rms_max_threads(VEC, ITER), WARP && ITER == 1 ? 2 : 1) block_norm_bwd_kernel(const BlockNormBwd g) {
+    constexpr bool kAhead = WARP && ITER == 1;
+    constexpr int N = VEC * ITER, P = (N + 1) / 2;  // values of a thread, pairs of them (the last one's second may be no value)
     __shared__ float red[3][32];
     extern __shared__ float shares[];  // WARP: [warps][C]
     pdl_launch();
@@ -291,18 +294,44 @@ __global__ void __launch_bounds__(WARP ? 256 : rms_max_threads(VEC, ITER), 1) bl
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, C = g.C, pitch = (C + 3) & ~3;
     const int tpr = WARP ? 32 : blockDim.x, t = WARP ? (threadIdx.x & 31) : threadIdx.x;
     const bool own = WARP && !g.per_block;  // a stretch is the warp's
-    float a_post[ITER][VEC], a_pre[ITER][VEC], a_gate[ITER][VEC];
+    struct Row {
+        Pack<T, VEC> v[ITER];
+        __device__ __forceinline__ void load(const void *from, int t, int tpr, int C) {
 #pragma unroll
-    for (int i = 0; i < ITER; ++i)
+            for (int i = 0; i < ITER; ++i) {
+                const int c = (i * tpr + t) * VEC;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) a_post[i][j] = a_pre[i][j] = 0.f;
-    // a block's share of a vector of C to `to`; through shared memory where its warps have shares of their own
-    auto leave = [&](float (&v)[ITER][VEC], float *to, bool joined) {
+                for (int j = 0; j < VEC; ++j) v[i].v[j] = from_f<T>(0.f);
+                if (c < C) v[i] = *reinterpret_cast<const Pack<T, VEC> *>((const T *)from + c);
+            }
+        }
+        __device__ __forceinline__ F2 pair(int k) const {
+            if constexpr (sizeof(T) == 2 && VEC > 1) return bf16_pair(reinterpret_cast<const uint32_t *>(&v[2 * k / VEC])[k % (VEC / 2)]);
+            else return f2(to_f(v[2 * k / VEC].v[2 * k % VEC]), 2 * k + 1 < N ? to_f(v[(2 * k + 1) % N / VEC].v[(2 * k + 1) % VEC]) : 0.f);
+        }
+    };
+    auto value = [](const F2 (&v)[P], int i) { const float2 p = parts(v[i / 2]); return i % 2 ? p.y : p.x; };
+    // pairs of a thread as the element type, or as fp32 shares of a vector of C; shares through shared memory where the block's
+    // warps have some of their own
+    auto store = [&](const F2 (&v)[P], void *to) {
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * tpr + t) * VEC;
+            float o[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o[j] = value(v, i * VEC + j);
+            if (c < C) store_f<T, VEC>((T *)to + c, o);
+        }
+    };
+    auto leave = [&](const F2 (&v)[P], float *to, bool joined) {
         float *mine = joined ? shares + warp * pitch : to;
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
             const int c = (i * tpr + t) * VEC;
-            if (c < C) store_share<VEC>(mine + c, v[i]);
+            float o[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o[j] = value(v, i * VEC + j);
+            if (c < C) store_share<VEC>(mine + c, o);
         }
         if (joined) {
             __syncthreads();
@@ -314,68 +343,82 @@ __global__ void __launch_bounds__(WARP ? 256 : rms_max_threads(VEC, ITER), 1) bl
             __syncthreads();
         }
     };
+    F2 a_post[P], a_pre[P], a_unit[P], pg[P];
+    Row pre;
+    pre.load(g.pre, t, tpr, C);
+#pragma unroll
+    for (int k = 0; k < P; ++k) a_post[k] = a_pre[k] = f2(0.f);
+    const float inv_c = 1.f / (float)C;
     const int units = g.gates * g.parts, walkers = own ? gridDim.x * warps : gridDim.x;
     for (int unit = own ? blockIdx.x * warps + warp : blockIdx.x; unit < units; unit += walkers) {
         int gate, r0, r1;
         norm_stretch(g, unit, gate, r0, r1);
         const T *gate_row = g.gate ? (const T *)g.gate + (size_t)gate * C : nullptr;
+        Row w;
+        w.load(g.post, t, tpr, C);
 #pragma unroll
-        for (int i = 0; i < ITER; ++i)
+        for (int k = 0; k < P; ++k) { pg[k] = w.pair(k); a_unit[k] = f2(0.f); }
+        if (gate_row) {
+            w.load(gate_row, t, tpr, C);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) a_gate[i][j] = 0.f;
-        for (int row = r0 + (WARP && !own ? warp : 0); row < r1; row += WARP && !own ? warps : 1) {
-            const size_t at = (size_t)row * C;
-            RawRow<T, VEC, ITER, false> dy, dh, b, h;
-            dy.load((const T *)g.dy + at, t, tpr, C, 0);
-            h.load((const T *)g.h + at, t, tpr, C, 0);
-            b.load((const T *)g.b + at, t, tpr, C, 0);
-            if (g.dh) dh.load((const T *)g.dh + at, t, tpr, C, 0);
-            const float s1 = g.rstd_post[row], s2 = g.rstd_pre[row];
-            float sum[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < ITER; ++i) {
-                const int c = (i * tpr + t) * VEC;
-                if (c < C) {
-                    float wg[VEC], wp[VEC], wr[VEC];
-                    load_f<T, VEC>((const T *)g.post + c, wp);
-                    load_f<T, VEC>((const T *)g.pre + c, wr);
-                    if (gate_row) load_f<T, VEC>(gate_row + c, wg);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float w2 = wr[j] * dy.at(i, j), w = wp[j] * (gate_row ? wg[j] : 1.f) * b.at(i, j);
-                        const float base = fmaf(s2, w2, g.dh ? dh.at(i, j) : 0.f);
-                        sum[0] = fmaf(w2, h.at(i, j), sum[0]);
-                        sum[1] = fmaf(w, base, sum[1]);
-                        sum[2] = fmaf(w, h.at(i, j), sum[2]);
-                    }
-                }
-            }
-            row_sum3(sum, WARP, red);
-            const float c2 = sum[0] / (float)C * s2 * s2 * s2, c1 = (sum[1] - c2 * sum[2]) / (float)C * s1 * s1;
-#pragma unroll
-            for (int i = 0; i < ITER; ++i) {
-                const int c = (i * tpr + t) * VEC;
-                if (c < C) {
-                    float wg[VEC], wp[VEC], wr[VEC], o_res[VEC], o_b[VEC];
-                    load_f<T, VEC>((const T *)g.post + c, wp);
-                    load_f<T, VEC>((const T *)g.pre + c, wr);
-                    if (gate_row) load_f<T, VEC>(gate_row + c, wg);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float base = fmaf(s2, wr[j] * dy.at(i, j), g.dh ? dh.at(i, j) : 0.f);
-                        const float tt = fmaf(-c2, h.at(i, j), base), unit_b = b.at(i, j) * s1, du = gate_row ? wg[j] * tt : tt;
-                        o_res[j] = g.alpha * tt;
-                        o_b[j] = s1 * fmaf(wp[j], du, -c1 * b.at(i, j));
-                        a_gate[i][j] = fmaf(tt, unit_b * wp[j], a_gate[i][j]);
-                        a_post[i][j] = fmaf(du, unit_b, a_post[i][j]);
-                        a_pre[i][j] = fmaf(dy.at(i, j), h.at(i, j) * s2, a_pre[i][j]);
-                    }
-                    store_f<T, VEC>((T *)g.dres + at + c, o_res);
-                    store_f<T, VEC>((T *)g.db + at + c, o_b);
-                }
-            }
+            for (int k = 0; k < P; ++k) pg[k] = pg[k] * w.pair(k);
         }
-        if (g.dgate) leave(a_gate, g.parts > 1 ? g.piece + (size_t)unit * C : g.dgate + (size_t)gate * C, WARP && !own);
+        const int step = WARP && !own ? warps : 1;
+        Row dy, dh, b, h, n_dy, n_dh, n_b, n_h;
+        float s1 = 0.f, s2 = 0.f, n_s1 = 0.f, n_s2 = 0.f;
+        auto load = [&](int row, Row &dy, Row &dh, Row &b, Row &h, float &s1, float &s2) {
+            const size_t at = (size_t)row * C;
+            dy.load((const T *)g.dy + at, t, tpr, C);
+            h.load((const T *)g.h + at, t, tpr, C);
+            b.load((const T *)g.b + at, t, tpr, C);
+            if (g.dh) dh.load((const T *)g.dh + at, t, tpr, C);
+            s1 = g.rstd_post[row];
+            s2 = g.rstd_pre[row];
+        };
+        int row = r0 + (WARP && !own ? warp : 0);
+        if (kAhead && row < r1) load(row, n_dy, n_dh, n_b, n_h, n_s1, n_s2);
+        for (; row < r1; row += step) {
+            if (kAhead) {
+                dy = n_dy; dh = n_dh; b = n_b; h = n_h; s1 = n_s1; s2 = n_s2;
+                if (row + step < r1) load(row + step, n_dy, n_dh, n_b, n_h, n_s1, n_s2);
+            } else {
+                load(row, dy, dh, b, h, s1, s2);
+            }
+            F2 q0 = f2(0.f), q1 = f2(0.f), q2 = f2(0.f);
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const F2 w2 = pre.pair(k) * dy.pair(k), wb = pg[k] * b.pair(k), hk = h.pair(k);
+                const F2 base = g.dh ? fma2(f2(s2), w2, dh.pair(k)) : f2(s2) * w2;
+                q0 = fma2(w2, hk, q0);
+                q1 = fma2(wb, base, q1);
+                q2 = fma2(wb, hk, q2);
+            }
+            float sum[3] = {sum2(q0), sum2(q1), sum2(q2)};
+            row_sum3(sum, WARP, red);
+            const float c2 = sum[0] * inv_c * s2 * s2 * s2, c1 = (sum[1] - c2 * sum[2]) * inv_c * s1 * s1;
+            F2 o_res[P], o_b[P];
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const F2 x = b.pair(k) * f2(s1), d = dy.pair(k), ds = pre.pair(k) * d, hk = h.pair(k);
+                const F2 base = g.dh ? fma2(f2(s2), ds, dh.pair(k)) : f2(s2) * ds;
+                const F2 tt = fma2(f2(-c2), hk, base);
+                a_unit[k] = fma2(tt, x, a_unit[k]);
+                a_pre[k] = fma2(d, hk * f2(s2), a_pre[k]);
+                o_b[k] = fma2(pg[k], f2(s1) * tt, f2(-c1) * x);
+                o_res[k] = f2(g.alpha) * tt;
+            }
+            store(o_res, (T *)g.dres + (size_t)row * C);
+            store(o_b, (T *)g.db + (size_t)row * C);
+        }
+        if (gate_row) w.load(gate_row, t, tpr, C);
+#pragma unroll
+        for (int k = 0; k < P; ++k) a_post[k] = gate_row ? fma2(w.pair(k), a_unit[k], a_post[k]) : a_post[k] + a_unit[k];
+        if (g.dgate) {
+            w.load(g.post, t, tpr, C);
+#pragma unroll
+            for (int k = 0; k < P; ++k) a_unit[k] = a_unit[k] * w.pair(k);
+            leave(a_unit, g.parts > 1 ? g.piece + (size_t)unit * C : g.dgate + (size_t)gate * C, WARP && !own);
+        }
     }
     if (WARP) __syncthreads();
     leave(a_post, g.part + (size_t)blockIdx.x * 2 * C, WARP);
@@ -403,8 +446,7 @@ struct NormRows {
 };
 
 // The same for many wide rows: stretches of rows that share a gate are dealt out to resident blocks, the rows ahead on their
-// way through shared memory.  Over a stretch one sum per column, of t b rstd_post, gives both dgate (times gamma_post) and
-// the stretch's share of dgamma_post (times the gate).
+// way through shared memory.
 template <typename T, int VEC, int ITER>
 __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __grid_constant__ BlockNormBwd g, const __grid_constant__ RingShape shape) {
     extern __shared__ __align__(16) uint8_t ring_smem[];
@@ -461,17 +503,17 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
         for (int row = r0; row < r1; ++row) {
             const float s1 = next1, s2 = next2;  // loaded a row ahead
             if (row + 1 < r1) { next1 = g.rstd_post[row + 1]; next2 = g.rstd_pre[row + 1]; }
-            const bool ok = ring.wait();
+            const bool ok = ring.wait<T, VEC>(row);
             const uint32_t slot_dy = ring.slot(0), slot_h = ring.slot(1), slot_b = ring.slot(2), slot_dh = ring.slot(3);
-            const RingRow at = ring_row(shape, row);
+            const int phase = ring_phase(shape, row);
             const size_t start = (size_t)row * C;
             ring.next();
             F2 q0 = f2(0.f), q1 = f2(0.f), q2 = f2(0.f), dy[G], h[G], b[G], dh[G];
             auto load = [&](int i) {
-                slot_load<T, VEC>(slot_dy, at, (const T *)g.dy + start, C, threads, i, dy);
-                slot_load<T, VEC>(slot_h, at, (const T *)g.h + start, C, threads, i, h);
-                slot_load<T, VEC>(slot_b, at, (const T *)g.b + start, C, threads, i, b);
-                if (g.dh) slot_load<T, VEC>(slot_dh, at, (const T *)g.dh + start, C, threads, i, dh);
+                slot_load<T, VEC>(slot_dy, phase, C, threads, i, dy);
+                slot_load<T, VEC>(slot_h, phase, C, threads, i, h);
+                slot_load<T, VEC>(slot_b, phase, C, threads, i, b);
+                if (g.dh) slot_load<T, VEC>(slot_dh, phase, C, threads, i, dh);
             };
 #pragma unroll
             for (int i = 0; i < P / G; ++i) {

@@ -24,12 +24,8 @@ struct RingShape {
     unsigned polls;   // of a bounded wait
 };
 
-// Where row `row` starts in its slot, and how many of its bytes are there.
-struct RingRow { int phase, valid; };
-__device__ __forceinline__ RingRow ring_row(const RingShape &g, int row) {
-    const size_t at = (size_t)row * g.row_bytes;
-    return RingRow{(int)(at & 15), (int)min((size_t)g.row_bytes, g.floor16 > at ? g.floor16 - at : (size_t)0)};
-}
+// Where row `row` starts in its slot.
+__device__ __forceinline__ int ring_phase(const RingShape &g, int row) { return (int)((size_t)row * g.row_bytes & 15); }
 
 template <int TENSORS> struct RowRing {
     const RingShape &g;
@@ -76,8 +72,26 @@ template <int TENSORS> struct RowRing {
     __device__ __forceinline__ void drain() {
         for (uint32_t i = issued > (uint32_t)g.stages ? issued - g.stages : 0; i < issued; ++i) mbar_drain(smem_u32(&full[i % g.stages]), (i / g.stages) & 1u);
     }
-    // false when the wait ran out (what stands in the stage is not the row)
-    __device__ __forceinline__ bool wait() { return mbar_wait(smem_u32(&full[stage]), parity, wt, 82); }
+    // By all threads: false when the wait ran out (what stands in the stage is not the row).  T: type of the tensors' values, single
+    // ones where rows keep to no boundary.
+    template <typename T, int VEC> __device__ __forceinline__ bool wait(int row) {
+        const bool ok = mbar_wait(smem_u32(&full[stage]), parity, wt, 82);
+        if (VEC == 1 && (size_t)(row + 1) * g.row_bytes > g.floor16) {  // the tensor's last values, which no copy brought
+            const size_t at = (size_t)row * g.row_bytes;
+            const int there = g.floor16 > at ? (int)(g.floor16 - at) / (int)sizeof(T) : 0, all = g.row_bytes / (int)sizeof(T);
+#pragma unroll
+            for (int k = 0; k < TENSORS; ++k)
+                if (src[k])
+                    for (int c = there + threadIdx.x; c < all; c += blockDim.x) {
+                        const uint32_t to = slot(k) + (uint32_t)(at & 15) + c * (uint32_t)sizeof(T);
+                        const uint8_t *from = src[k] + at + c * sizeof(T);
+                        if constexpr (sizeof(T) == 2) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"(*reinterpret_cast<const uint16_t *>(from)) : "memory");
+                        else asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(*reinterpret_cast<const uint32_t *>(from)) : "memory");
+                    }
+            __syncthreads();
+        }
+        return ok;
+    }
     __device__ __forceinline__ uint32_t slot(int tensor) const { return base + (stage * TENSORS + tensor) * g.slot_bytes; }
     __device__ __forceinline__ void next() { if (++stage == (uint32_t)g.stages) { stage = 0; parity ^= 1u; } }
 };
@@ -86,8 +100,8 @@ template <int TENSORS> struct RowRing {
 // vector, or (VEC = 1) two values.  Columns past the row are zeros.
 template <int VEC> constexpr int kGroup = VEC > 1 ? VEC / 2 : 1;  // pairs
 
-// Group i of a row in a slot.  Value c stands at phase + c * sizeof(T); vectors: phase 0, and all of the row is there.
-template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_t slot, const RingRow &at, const T *row, int C, int threads, int i, F2 (&v)[kGroup<VEC>]) {
+// Group i of a row in a slot.  Value c stands at phase + c * sizeof(T) (vectors: phase 0).
+template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_t slot, int phase, int C, int threads, int i, F2 (&v)[kGroup<VEC>]) {
     if constexpr (VEC > 1) {
         const int c = (i * threads + threadIdx.x) * VEC;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
@@ -103,20 +117,19 @@ template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_
             else v[j] = f2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
         }
     } else {
-        float e[2];
+        float e[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int c = (2 * i + j) * threads + threadIdx.x, in = min(c, C - 1);
-            if (at.valid < C * (int)sizeof(T) && in * (int)sizeof(T) >= at.valid) {  // the last row's last few
-                e[j] = to_f(row[in]);
-            } else if constexpr (sizeof(T) == 2) {
-                uint16_t w;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(slot + at.phase + in * 2u));
-                e[j] = __uint_as_float((uint32_t)w << 16);
-            } else {
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(e[j]) : "r"(slot + at.phase + in * 4u));
+            const uint32_t c = (2 * i + j) * threads + threadIdx.x, from = slot + phase + c * (uint32_t)sizeof(T);
+            if (c < (uint32_t)C) {
+                if constexpr (sizeof(T) == 2) {
+                    uint16_t w;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(from));
+                    e[j] = __uint_as_float((uint32_t)w << 16);
+                } else {
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(e[j]) : "r"(from));
+                }
             }
-            e[j] = c < C ? e[j] : 0.f;
         }
         v[0] = f2(e[0], e[1]);
     }
