@@ -483,11 +483,6 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
                        const float *wscale, void *dx, void *dW, float *db, void *workspace, size_t workspace_bytes, int B,
                        int in, int out, int dw_f32, void *stream);
 
-/* Diagnostics, as ddg_debug_linear_ce_wait_polls: the bounded device-side waits of the ddg_fc8_* calls that this thread
- * enqueues from now on give up after `polls` polls (0: at once); negative: the default, about a second.  What a block whose
- * wait ran out was to write is NaN. */
-void ddg_debug_fc8_wait_polls(int polls);
-
 /* Root-mean-square norms after a block and before the next one, with the block's gate and the residual's scale, over (at
  * most 2^30) rows of C <= 16384 values:
  *   rstd_post = 1 / sqrt(mean(b^2) + eps);  h = alpha res + gate b rstd_post gamma_post
@@ -511,6 +506,12 @@ ddg_status ddg_block_norm_bwd(int precision, const void *dy, const void *dh, con
                               const void *gamma_post, const void *gamma_pre, const float *rstd_post, const float *rstd_pre,
                               void *db, void *dres, float *dgate, float *dgamma_post, float *dgamma_pre, float *scratch,
                               int rows, int C, int span, float alpha, void *stream);
+
+/* Diagnostics, as ddg_debug_linear_ce_wait_polls: the bounded device-side waits of the ddg_act8_*, ddg_fc8_* and
+ * ddg_block_norm_* calls that this thread enqueues from now on give up after `polls` polls (0: at once); negative: the
+ * default, a few seconds.  What a block whose wait ran out was still to write is NaN (codes: scale NaN), sums that it has a
+ * share in too; other calls are not touched. */
+void ddg_debug_block8_wait_polls(int polls);
 
 /* Fused SGD update over n parameters (Eq. 9 with momentum and weight decay): d = g + wd*w; v = mu*v + d;
  * w -= lr*v; w_version = cast(w).  w, v, g fp32; w_version in the precision's element type. */

@@ -38,7 +38,7 @@ EXPORTS = ["ddg_create", "ddg_step", "ddg_step_host", "ddg_set_lr", "ddg_param_c
            "ddg_step_host_pipelined", "ddg_pipelined_loss", "ddg_conv3x3_dgrad_fused_shared",
            "ddg_linear_ce_workspace_bytes", "ddg_linear_ce_fwd", "ddg_linear_ce_bwd", "ddg_debug_linear_ce_wait_polls", "ddg_rmsnorm_scratch_elems",
            "ddg_add_rmsnorm_fwd", "ddg_add_rmsnorm_bwd", "ddg_dropout_fwd", "ddg_dropout_bwd",
-           "ddg_act8_pitch", "ddg_act8_pack", "ddg_act8_unpack", "ddg_fc8_fwd", "ddg_fc8_workspace_bytes", "ddg_fc8_bwd", "ddg_debug_fc8_wait_polls", "ddg_block_norm_fwd",
+           "ddg_act8_pitch", "ddg_act8_pack", "ddg_act8_unpack", "ddg_fc8_fwd", "ddg_fc8_workspace_bytes", "ddg_fc8_bwd", "ddg_debug_block8_wait_polls", "ddg_block_norm_fwd",
            "ddg_block_norm_scratch_elems", "ddg_block_norm_bwd"]
 
 
@@ -141,8 +141,8 @@ _lib.ddg_fc8_fwd.argtypes = [_i] + [_vp] * 6 + [_i] * 4 + [_vp]
 _lib.ddg_fc8_workspace_bytes.argtypes = [_i] * 4
 _lib.ddg_fc8_workspace_bytes.restype = _sz
 _lib.ddg_fc8_bwd.argtypes = [_i] + [_vp] * 9 + [_sz] + [_i] * 4 + [_vp]
-_lib.ddg_debug_fc8_wait_polls.argtypes = [_i]
-_lib.ddg_debug_fc8_wait_polls.restype = None
+_lib.ddg_debug_block8_wait_polls.argtypes = [_i]
+_lib.ddg_debug_block8_wait_polls.restype = None
 _lib.ddg_block_norm_fwd.argtypes = [_i] + [_vp] * 11 + [_i] * 3 + [_f, _f, _vp]
 _lib.ddg_block_norm_scratch_elems.argtypes = [_i] * 3
 _lib.ddg_block_norm_scratch_elems.restype = _sz
@@ -606,10 +606,10 @@ def fc8_bwd(prec, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, n_in, n_
                          B, n_in, n_out, int(dw_f32), stream))
 
 
-def debug_fc8_wait_polls(polls):
-    """Diagnostics: the device-side waits of the fc8 calls that this thread enqueues from now on give up after `polls` polls
-    (0: at once); negative: the default."""
-    _lib.ddg_debug_fc8_wait_polls(polls)
+def debug_block8_wait_polls(polls):
+    """Diagnostics: the device-side waits of the act8, fc8 and block_norm calls that this thread enqueues from now on give up
+    after `polls` polls (0: at once); negative: the default."""
+    _lib.ddg_debug_block8_wait_polls(polls)
 
 
 def _gate_elems(rows, C, span):

@@ -222,7 +222,7 @@ template <typename T, int VEC, int ITER> int pack_ring(const void *x, void *q, f
     static thread_local int ready = -1;
     if (!ring_ready(act8_pack_ring_kernel<T, VEC, ITER>, ready)) return -1;
     launch_k(act8_pack_ring_kernel<T, VEC, ITER>, std::min(rows, 148 * p.per_sm), p.threads, p.smem, s, (const T *)x, (int8_t *)q, scale, rows, C, act8_pitch(C),
-             ring_shape(rows, C * (int)sizeof(T), 1, p.smem, kSpinLimit));
+             ring_shape(rows, C * (int)sizeof(T), 1, p.smem, block8_polls()));
     return 1;
 }
 

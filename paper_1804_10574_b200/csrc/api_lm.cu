@@ -194,7 +194,7 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
     return done(launch_fc8_bwd(precision, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, in, out, dw_f32, (cudaStream_t)stream));
 }
 
-void ddg_debug_fc8_wait_polls(int polls) { fc8_wait_polls(polls); }
+void ddg_debug_block8_wait_polls(int polls) { block8_wait_polls(polls); }
 
 ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, const void *gate, const void *gamma_post, const void *gamma_pre, void *h, void *y, void *q,
                               float *qscale, float *rstd_post, float *rstd_pre, int rows, int C, int span, float alpha, float eps, void *stream) {

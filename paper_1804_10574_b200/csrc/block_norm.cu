@@ -501,9 +501,8 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
         float next1 = 0.f, next2 = 0.f;
         if (r0 < r1) { next1 = g.rstd_post[r0]; next2 = g.rstd_pre[r0]; }
         for (int row = r0; row < r1; ++row) {
-            const float s1 = next1, s2 = next2;  // loaded a row ahead
-            if (row + 1 < r1) { next1 = g.rstd_post[row + 1]; next2 = g.rstd_pre[row + 1]; }
-            const bool ok = ring.wait<T, VEC>(row);
+            const float s1 = next1, s2 = ring.wait<T, VEC>(row) ? next2 : __int_as_float(0x7fffffff);  // a row that did not come is NaN
+            if (row + 1 < r1) { next1 = g.rstd_post[row + 1]; next2 = g.rstd_pre[row + 1]; }  // a row ahead
             const uint32_t slot_dy = ring.slot(0), slot_h = ring.slot(1), slot_b = ring.slot(2), slot_dh = ring.slot(3);
             const int phase = ring_phase(shape, row);
             const size_t start = (size_t)row * C;
@@ -527,7 +526,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
                     q2 = fma2(w, h[j], q2);
                 }
             }
-            float sum[3] = {ok ? sum2(q0) : __int_as_float(0x7fffffff), sum2(q1), sum2(q2)};  // a row that did not come is NaN
+            float sum[3] = {sum2(q0), sum2(q1), sum2(q2)};
             ring_sum<3>(sum, threads >> 5, red, round);
             if (begun && ahead.more()) {
                 ring.copy(ahead.row);
@@ -688,7 +687,7 @@ template <typename T, int VEC, int ITER> int fwd_ring(const BlockNormFwd &g, con
     static thread_local int ready[2] = {-1, -1};
     auto kernel = g.q ? block_norm_fwd_ring_kernel<T, VEC, ITER, true> : block_norm_fwd_ring_kernel<T, VEC, ITER, false>;
     if (!ring_ready(kernel, ready[g.q != nullptr])) return -1;
-    launch_k(kernel, std::min(g.rows, 148 * p.per_sm), p.threads, p.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 2, p.smem, kSpinLimit));
+    launch_k(kernel, std::min(g.rows, 148 * p.per_sm), p.threads, p.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 2, p.smem, block8_polls()));
     return 1;
 }
 template <typename T, int VEC, bool SHIFT> int fwd_as(const BlockNormFwd &g, const Launch &s) {
@@ -721,7 +720,7 @@ template <typename T, int VEC, int ITER> int bwd_ring(const BlockNormBwd &g, con
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = s.pdl == 1 ? 2 : 1;
-    cudaLaunchKernelEx(&cfg, block_norm_bwd_ring_kernel<T, VEC, ITER>, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), kSpinLimit));
+    cudaLaunchKernelEx(&cfg, block_norm_bwd_ring_kernel<T, VEC, ITER>, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), block8_polls()));
     return 1;
 }
 

@@ -621,7 +621,7 @@ int mm_launch_as(const Operand &a, const Operand &b, MmArgs &g, int K, int most_
         if (cudaFuncSetAttribute(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
         ready_dev = dev;
     }
-    g.polls = t_wait_polls >= 0 ? (unsigned)t_wait_polls : kSpinLimit;
+    g.polls = block8_polls();
     launch_k(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, 2 * (int)std::min<long>(items, sm_count() / 2), kThreads, kSmem, s, ma, mb, mo, g);
     return 1;
 }
@@ -714,7 +714,8 @@ int blocks_for(size_t threads) { return (int)std::max<size_t>(1, std::min<size_t
 
 }  // namespace
 
-void fc8_wait_polls(int polls) { t_wait_polls = polls; }
+void block8_wait_polls(int polls) { t_wait_polls = polls; }
+unsigned block8_polls() { return t_wait_polls >= 0 ? (unsigned)t_wait_polls : kSpinLimit; }
 
 int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, const float *ws, const void *bias, void *y, int B, int in, int out, int y_f32, Launch s) {
     const int pitch = act8_pitch(in);
@@ -725,7 +726,7 @@ int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, co
         g.tail = (in - (g.steps - 1) * kw + 31) / 32;
         g.row_scale = xs; g.col_scale = ws; g.bias = bias; g.bias_bf16 = prec == P_BF16; g.y = y; g.out_bf16 = prec == P_BF16 && !y_f32;
         g.vec = out % 4 == 0 && (reinterpret_cast<uintptr_t>(y) & (g.out_bf16 ? 7 : 15)) == 0;
-        g.polls = t_wait_polls >= 0 ? (unsigned)t_wait_polls : kSpinLimit;
+        g.polls = block8_polls();
         CUtensorMap mw, mx;
         if (!box_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, wq, out, in, pitch, kHalf, &mw) || !box_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, xq, B, in, pitch, nt, &mx)) return -1;
         switch (nt) {

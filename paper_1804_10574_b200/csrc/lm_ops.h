@@ -46,8 +46,10 @@ int launch_act8_unpack(int prec, const void *q, const float *scale, void *x, int
 // ---- linear layer on 8-bit codes (fc8.cu) ----------------------------------------------------------------------------
 int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, const float *ws, const void *bias, void *y, int B, int in, int out, int y_f32, Launch s);
 size_t fc8_workspace_bytes(int prec, int B, int in, int out);
-// Polls before a device-side wait of the calls of this thread gives up; negative: the default.
-void fc8_wait_polls(int polls);
+// Polls before a device-side wait of the calls of this thread gives up (these operators and the rows of codes and norms that go
+// through shared memory); negative: the default.
+void block8_wait_polls(int polls);
+unsigned block8_polls();
 int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, void *ws_mem, int B, int in,
                    int out, int dw_f32, Launch s);
 

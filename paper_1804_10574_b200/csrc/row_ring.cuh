@@ -36,9 +36,10 @@ template <int TENSORS> struct RowRing {
     uint32_t head, issued;   // stage that is filled next; rows that this thread had copied
     const uint8_t *src[TENSORS];  // nullptr: a tensor that is not there
     int tensors;
+    bool lost;
 
     __device__ __forceinline__ RowRing(const RingShape &shape, uint32_t smem, uint64_t *full_, int *abort_flag)
-        : g(shape), base(smem), full(full_), wt{abort_flag, abort_flag, shape.polls}, stage(0), parity(0), head(0), issued(0), tensors(0) {}
+        : g(shape), base(smem), full(full_), wt{abort_flag, abort_flag, shape.polls}, stage(0), parity(0), head(0), issued(0), tensors(0), lost(false) {}
 
     __device__ __forceinline__ void init() {  // by one thread, before a barrier of the block
         for (int i = 0; i < g.stages; ++i) mbar_init(smem_u32(&full[i]), 1);
@@ -72,10 +73,10 @@ template <int TENSORS> struct RowRing {
     __device__ __forceinline__ void drain() {
         for (uint32_t i = issued > (uint32_t)g.stages ? issued - g.stages : 0; i < issued; ++i) mbar_drain(smem_u32(&full[i % g.stages]), (i / g.stages) & 1u);
     }
-    // By all threads: false when the wait ran out (what stands in the stage is not the row).  T: type of the tensors' values, single
+    // By all threads: false when a wait of the thread ran out, this one or one before (what stands in the stage may not be the row).  T: type of the tensors' values, single
     // ones where rows keep to no boundary.
     template <typename T, int VEC> __device__ __forceinline__ bool wait(int row) {
-        const bool ok = mbar_wait(smem_u32(&full[stage]), parity, wt, 82);
+        lost = lost || !mbar_wait(smem_u32(&full[stage]), parity, wt, 82);
         if (VEC == 1 && (size_t)(row + 1) * g.row_bytes > g.floor16) {  // the tensor's last values, which no copy brought
             const size_t at = (size_t)row * g.row_bytes;
             const int there = g.floor16 > at ? (int)(g.floor16 - at) / (int)sizeof(T) : 0, all = g.row_bytes / (int)sizeof(T);
@@ -90,7 +91,7 @@ template <int TENSORS> struct RowRing {
                     }
             __syncthreads();
         }
-        return ok;
+        return !lost;
     }
     __device__ __forceinline__ uint32_t slot(int tensor) const { return base + (stage * TENSORS + tensor) * g.slot_bytes; }
     __device__ __forceinline__ void next() { if (++stage == (uint32_t)g.stages) { stage = 0; parity ^= 1u; } }
