@@ -35,6 +35,7 @@ constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBuf + 1024;
 static_assert(kSmem + 1536 <= 227 * 1024, "with the barriers and the epilogue's columns");
 constexpr int kMostPlanes = 3;
 constexpr int kPieceF32 = 1024, kPieceOut = 65536;  // K values of a chain: 32-bit results, bf16 results
+constexpr int kSmallMost = 128, kSmallMostIn = 1024;  // rows and outputs, inputs of layers whose gradients are one launch
 constexpr int kPairs = 74;                       // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
 
 enum Mode { kForward, kGrad };
@@ -45,8 +46,9 @@ struct MmArgs {
     int kblocks, n_seg;       // K blocks of a segment; segments: bf16 terms of A
     int a_off[kMostPlanes];   // where a segment's term starts: in K (K-major A) or in M
     int tiles_m, tiles_n, splits, group_m;
-    int width;                // columns of a tile: at most 256, a multiple of 64, alike for all tiles of a launch
-    int b_bytes;              // of B in a stage and CTA
+    int width;                // columns of a tile: at most 256, a multiple of 64
+    int full, cut;            // tiles (times splits) of that width; the others are cut into so many parts
+    int items, b_box;         // pieces of work; rows of a box of K-major B
     int piece;                // steps of the K range (K blocks times segments) of a chain (with PROMOTE)
     int tail;                 // MMA steps in a segment's last K block
     const float *row_scale, *col_scale;  // forward
@@ -59,15 +61,21 @@ struct MmArgs {
 };
 
 // All tiles of a split, in bands of group_m tile rows that are walked column by column, so that the operands of the tiles in
-// flight stay in the L2.
-struct MmTile { int split, m, n; };
+// flight stay in the L2.  The tiles that would make a last round of the CTA pairs with few of them at work are cut into
+// narrower ones.
+__device__ __forceinline__ int mm_width_of(const MmArgs &g, int item) { return item < g.full ? g.width : g.width / g.cut; }
+__device__ __forceinline__ int mm_split_of(const MmArgs &g, int item) {
+    return g.splits == 1 ? 0 : (item < g.full ? item : g.full + (item - g.full) / g.cut) / (g.tiles_m * g.tiles_n);
+}
+struct MmTile { int split, m, col, width; };  // tile row, first column
 __device__ __forceinline__ MmTile mm_tile(const MmArgs &g, int item) {
-    const int per = g.tiles_m * g.tiles_n, split = g.splits == 1 ? 0 : item / per;
-    unsigned r = (unsigned)(item - split * per);
+    const int tail = item - g.full, tile = tail < 0 ? item : g.full + tail / g.cut, part = tail < 0 ? 0 : tail % g.cut, width = mm_width_of(g, item);
+    const int per = g.tiles_m * g.tiles_n, split = g.splits == 1 ? 0 : tile / per;
+    unsigned r = (unsigned)(tile - split * per);
     const unsigned band = r / (unsigned)(g.group_m * g.tiles_n);
     r -= band * g.group_m * g.tiles_n;
     const unsigned rows = min(g.group_m, g.tiles_m - (int)band * g.group_m), n = r / rows;
-    return MmTile{split, (int)(band * g.group_m + r - n * rows), (int)n};
+    return MmTile{split, (int)(band * g.group_m + r - n * rows), (int)n * g.width + part * width, width};
 }
 // steps of the K range of a split: at most 2^22 K blocks and segments, times 148 splits, in 32 bits
 __device__ __forceinline__ void mm_range(const MmArgs &g, int split, int &i0, int &i1) {
@@ -150,11 +158,12 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     cluster_sync();  // both CTAs' barriers are ready
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
-    const int n_items = g.tiles_m * g.tiles_n * g.splits;
+    const int n_items = g.items;
     const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
     // Copies into stage s of this CTA's halves of A and B: one step of the K range.
-    auto load_step = [&](uint32_t s, int seg, int k, int m0, int n0) {
-        if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + g.b_bytes));
+    auto load_step = [&](uint32_t s, int seg, int k, int m0, int n0, int width) {
+        const int half = width / 2;  // columns of this CTA
+        if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + (B_MN ? (half + kBox - 1) / kBox * kBox : half) * kStageKw));
         const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
         const uint32_t a = base + s * kStageBytes, b = a + kBlockBytes;
         // K-major: a box is 128 bytes of K of 128 rows.  MN-major: 64 rows of kw K values.
@@ -165,9 +174,11 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if (B_MN && j * kBox >= g.width / 2) break;
-            if (B_MN) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, n0 + kBox * j, k);
-            else tma_load_pair(b + j * (kHalf * 128), &map_b, bar, k + kBox * j, n0);
+            if (B_MN) {
+                if (j * kBox < half) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, n0 + kBox * j, k);
+            } else {
+                for (int r = 0; r < half; r += g.b_box) tma_load_pair(b + j * (kHalf * 128) + r * 128, &map_b, bar, k + kBox * j, n0 + r);
+            }
         }
     };
     uint32_t issued = 0;   // steps that this CTA's thread of the loads has issued
@@ -181,11 +192,11 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                 const MmTile t = mm_tile(g, item);
                 int i0, i1;
                 mm_range(g, t.split, i0, i1);
-                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.n * g.width + (int)rank * (g.width / 2);
+                const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.col + (int)rank * (t.width / 2);
                 int kb = i0 == 0 ? 0 : i0 / g.n_seg, seg = i0 - kb * g.n_seg;
                 for (int i = i0; i < i1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 71)) { ok = false; break; }
-                    load_step(s, seg, kb * kw, m0, n0);
+                    load_step(s, seg, kb * kw, m0, n0, t.width);
                     ++issued;
                     if (++seg == g.n_seg) { seg = 0; ++kb; }
                     if (++s == kStages) { s = 0; ph ^= 1u; }
@@ -199,8 +210,8 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             // accumulator stand outside.
             issuer = elect_one();
             // 32-bit results: fp32 (1) or int32 (2); operands: bf16 (1) of kind::f16, signed (1) of kind::i8
-            const uint32_t idesc = ((kI8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(g.width >> 3) << 17) |
-                                   ((uint32_t)(kTile >> 4) << 24);
+            const uint32_t idesc_tile = ((kI8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kTile >> 4) << 24);
+            uint32_t idesc = 0;
             // K-major: a step of K is 32 bytes of a swizzle row, the next 128 bytes 16 KB further.  MN-major: a step is 16 rows of
             // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
             const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
@@ -220,7 +231,8 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             const int short_from = (g.kblocks - 1) * g.n_seg;  // the last K block has g.tail steps
             for (int item = first; item < n_items && ok; item += step) {
                 int i0, i1;
-                mm_range(g, g.splits == 1 ? 0 : item / (g.tiles_m * g.tiles_n), i0, i1);
+                mm_range(g, mm_split_of(g, item), i0, i1);
+                idesc = idesc_tile | ((uint32_t)(mm_width_of(g, item) >> 3) << 17);
                 for (; i0 < i1; ++u) {
                     const int end = PROMOTE ? mm_piece_end(g, i0, i1) : i1;
                     const uint32_t acc = u & 1u;
@@ -258,7 +270,7 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         for (int item = first; item < n_items; item += step) {
             const MmTile t = mm_tile(g, item);
             const int row = t.m * kTile + (int)rank * kHalf + 32 * quarter + lane;
-            const int col0 = t.n * g.width + half * kHalf, live = min(g.width - half * kHalf, g.N - col0);
+            const int col0 = t.col + half * kHalf, live = min(t.width - half * kHalf, g.N - col0);
             int pieces = 1;
             if (PROMOTE) {
                 int i0, i1;
@@ -343,7 +355,7 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     if (abort_flag || (s_peer & kGaveUp)) {
         // A wait of the pair ran out, so that products or copies may still be in flight; they would land in the shared memory
         // and TMEM of whoever has them next.  The products end by themselves, and after them nothing reads the stages.  A
-        // step that only one of the CTAs has issued is completed by the other (any box will do), so that the barriers of all
+        // step that only one of the CTAs has issued is completed by the other (any boxes of the same size will do), so that the barriers of all
         // steps complete: a step is at most kStages ahead of the products, so that no two of one stage are open.
         if (issuer) commit_pair(smem_u32(&drained));
         if (threadIdx.x == 0) mbar_drain(smem_u32(&drained), 0);
@@ -351,7 +363,16 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         cluster_sync();
         if (threadIdx.x == 0) {
             const uint32_t peer = s_peer & ~kGaveUp, last = max(issued, peer);
-            for (uint32_t i = issued; i < peer; ++i) load_step(i % kStages, 0, 0, 0, 0);
+            int item = first, left = 0;  // the item that a step is of: how many steps up to its end
+            for (uint32_t i = 0; i < peer; ++i, --left) {
+                if (i > 0 && left == 0) item += step;
+                if (left == 0) {
+                    int i0, i1;
+                    mm_range(g, mm_split_of(g, item), i0, i1);
+                    left = i1 - i0;
+                }
+                if (i >= issued) load_step(i % kStages, 0, 0, 0, 0, mm_width_of(g, item));
+            }
             if (rank == 0)
                 for (uint32_t i = last > kStages ? last - kStages : 0; i < last; ++i) mbar_drain(smem_u32(&full[i % kStages]), (i / kStages) & 1u);
         }
@@ -367,6 +388,8 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
 }
 
 #include "fc8_rows.cuh"
+
+#include "fc8_small.cuh"
 
 // ---- before the products of the backward pass ------------------------------------------------------------------------
 // Codes to bf16, in rows of `plane`: times their scale, or as they are (scale nullable).
@@ -589,6 +612,21 @@ int mm_splits(int M, int N, int steps) {
     return best;
 }
 
+// The tiles of the last round of the CTA pairs, where it is not full, are halved or quartered if that is done sooner: half of a
+// part's loads, A's, stay.
+void mm_cut(MmArgs &g, int tiles, int pairs) {
+    const int rest = tiles > pairs ? tiles % pairs : 0;
+    g.full = tiles;
+    g.cut = 1;
+    double least = 0.95;
+    for (int c = 2; c <= 4 && rest; c *= 2) {
+        if (g.width % (c * kKBox) != 0) break;
+        const double t = (double)((rest * c + pairs - 1) / pairs) * (0.5 + 0.5 / c);
+        if (t < least) { least = t; g.cut = c; g.full = tiles - rest; }
+    }
+    g.items = g.full + (tiles - g.full) * g.cut;
+}
+
 // An operand: a row-major matrix in memory; ld: elements from a row to the next.
 struct Operand { const void *ptr; int rows, cols; size_t ld; };
 
@@ -606,12 +644,13 @@ int mm_launch_as(const Operand &a, const Operand &b, MmArgs &g, int K, int most_
     g.width = mm_width(g.M, g.N, g.splits);
     g.tiles_n = (g.N + g.width - 1) / g.width;
     g.group_m = 16;
-    const int b_rows = g.width / 2;
-    g.b_bytes = (B_MN ? up(b_rows, kKBox) : b_rows) * kStageKw;
-    const long items = (long)g.tiles_m * g.tiles_n * g.splits;
-    if (items > 0x7fffffff) return -1;
+    const long tiles = (long)g.tiles_m * g.tiles_n * g.splits;
+    const int pairs = sm_count() / 2;
+    if (tiles > 0x7fffffff / 4) return -1;
+    mm_cut(g, (int)tiles, pairs);
+    g.b_box = g.width / g.cut / 2;
     CUtensorMap ma, mb, mo{};
-    if (!box_map(type, es, a.ptr, a.rows, a.cols, a.ld, A_MN ? kw : kHalf, &ma) || !box_map(type, es, b.ptr, b.rows, b.cols, b.ld, B_MN ? kw : b_rows, &mb)) return -1;
+    if (!box_map(type, es, a.ptr, a.rows, a.cols, a.ld, A_MN ? kw : kHalf, &ma) || !box_map(type, es, b.ptr, b.rows, b.cols, b.ld, B_MN ? kw : g.b_box, &mb)) return -1;
     if (g.store == kBoxes &&
         !box_map(g.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, g.out_bf16 ? 2 : 4, g.out, g.M, g.N, g.ld, 32, &mo)) return -1;
     static thread_local int ready_dev = -1;  // the attribute belongs to a device
@@ -622,7 +661,7 @@ int mm_launch_as(const Operand &a, const Operand &b, MmArgs &g, int K, int most_
         ready_dev = dev;
     }
     g.polls = block8_polls();
-    launch_k(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, 2 * (int)std::min<long>(items, sm_count() / 2), kThreads, kSmem, s, ma, mb, mo, g);
+    launch_k(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, 2 * std::min(g.items, pairs), kThreads, kSmem, s, ma, mb, mo, g);
     return 1;
 }
 
@@ -641,9 +680,6 @@ int rows_splits(int nt, int tiles, int in) {
 // cutting the work up tell, in bytes; a row's sums cost as much as 2 KB.  (us with outputs / with rows of x on the MMA's rows:
 // 1 x 4096 x 16384 14.8 / 24.8; 64 x 4096 x 4096 9.8 / 11.5; 200 x 16384 x 1024 13.7 / 32.4; 256 x 4096 x 16384 25.8 / 18.8.)
 bool rows_fit(int B, int in, int out) {
-#ifdef FORCE_ROWS
-    return B <= FORCE_ROWS;
-#endif
     const int nt = rows_columns(B), sms = 2 * kPairs;
     const long tiles = (long)((out + kHalf - 1) / kHalf) * ((B + nt - 1) / nt);
     if (B <= 32) return true;
@@ -710,6 +746,12 @@ BwdPlan bwd_plan(int prec, int B, int in, int out) {
     return p;
 }
 
+// us of the gradients in one launch / in three or four, on the device and with the host: 128 x 128 x 128 bf16 6.4 / 11.6 and
+// 10.5 / 20.6, fp32 4.9 / 14.1; 128 x 1024 x 128 9.0 / 13.2; 256 x 256 x 256 bf16 14.5 / 13.2.
+bool small_fit(int B, int in, int out) {
+    return B <= kSmallMost && out <= kSmallMost && in <= kSmallMostIn;
+}
+
 int blocks_for(size_t threads) { return (int)std::max<size_t>(1, std::min<size_t>((threads + 255) / 256, 148 * 8)); }
 
 }  // namespace
@@ -745,8 +787,22 @@ int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, co
 
 size_t fc8_workspace_bytes(int prec, int B, int in, int out) { return bwd_plan(prec, B, in, out).bytes; }
 
+template <typename T, typename TW>
+static int small_bwd(const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, int B, int in, int out, const Launch &s) {
+    SmallArgs g{dy, (const int8_t *)xq, (const int8_t *)wq, xs, ws, dx, dW, db, B, in, out, act8_pitch(in)};
+    const int tiles_n = (in + kSmallN - 1) / kSmallN;
+    g.dx_tiles = dx ? (B + kSmallM - 1) / kSmallM * tiles_n : 0;
+    g.dw_tiles = dW ? (out + kSmallM - 1) / kSmallM * tiles_n : 0;
+    launch_k(fc8_small_bwd_kernel<T, TW>, g.dx_tiles + g.dw_tiles + (db ? (out + 63) / 64 : 0), 256, 0, s, g);
+    return 1;
+}
+
 int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, const void *wq, const float *ws, void *dx, void *dW, float *db, void *ws_mem, int B, int in, int out,
                    int dw_f32, Launch s) {
+    if (small_fit(B, in, out)) {
+        if (prec == P_F32) return small_bwd<float, float>(dy, xq, xs, wq, ws, dx, dW, db, B, in, out, s);
+        return dw_f32 ? small_bwd<bf16, float>(dy, xq, xs, wq, ws, dx, dW, db, B, in, out, s) : small_bwd<bf16, bf16>(dy, xq, xs, wq, ws, dx, dW, db, B, in, out, s);
+    }
     const BwdPlan p = bwd_plan(prec, B, in, out);
     uint8_t *base = (uint8_t *)ws_mem;
     const int pitch = act8_pitch(in);

@@ -175,7 +175,7 @@ class Fc:
 
 FC_SHAPES = [(1, 1, 1), (1, 16, 16), (1, 64, 100), (3, 5, 7), (1, 4096, 513), (2, 1000, 4099), (16, 256, 2000), (17, 130, 257), (33, 1000, 1001), (64, 2048, 640), (65, 128, 640),
              (128, 128, 128), (130, 72, 257), (200, 4097, 300), (257, 264, 513), (300, 521, 1000), (511, 16, 255), (700, 2200, 90), (2050, 136, 520), (40, 8200, 33),
-             (1100, 300, 2000)]
+             (1100, 300, 2000), (2200, 72, 2300), (2200, 2300, 136), (136, 2300, 2200), (1300, 1408, 3000)]
 
 
 @gpu
@@ -774,7 +774,8 @@ def test_block8_tensor_arguments_are_checked_in_the_binding(binding):
 
 # ---- bounded waits --------------------------------------------------------------------------------------------------
 # every way of a call that waits on the device: one row, a few, tiles, with splits, with chains that are cut, fp32
-WAYS_THAT_WAIT = [(1, 4096, 700, 1), (20, 2048, 300, 1), (100, 4096, 640, 1), (300, 136, 777, 1), (700, 2200, 1100, 1), (300, 8200, 70, 1), (2100, 264, 1000, 0), (130, 72, 2057, 0)]
+WAYS_THAT_WAIT = [(1, 4096, 700, 1), (20, 2048, 300, 1), (100, 4096, 640, 1), (300, 136, 777, 1), (700, 2200, 1100, 1), (300, 8200, 70, 1), (2100, 264, 1000, 0), (130, 72, 2057, 0), (2200, 1000, 2300, 1), (2200, 2300, 1000, 1),
+                 (300, 2300, 2200, 1)]
 
 
 @gpu
