@@ -3,10 +3,14 @@
 //   forward    y_no = xs_n ws_o (sum_k xq_nk wq_ok) + b_o        32-bit integer sums, exact
 //   backward   dx = dy w^;  dW = dy^T x^;  db = sum_n dy_n       w^, x^: what the codes stand for in the element type
 //
-// The products run on one tcgen05 kernel, CTA pairs on tiles of 256 rows (pair_mma.cuh).  What bounds it: the forward pass
-// 2 B in out multiply-adds of 8-bit integers (kind::i8, twice the rate of bf16 by the same bytes of operands), the backward
-// pass twice as many of bf16.  The codes are the operands of the forward pass as they lie.  For the backward pass a first
-// kernel writes what they stand for as bf16 to the workspace, beside the sums for db, and dy where TMA cannot read it.
+// The products run on one tcgen05 kernel, CTA pairs on tiles of 256 x 256 (pair_mma.cuh); a few rows (fc8_rows.cuh) and the
+// gradients of small layers (fc8_small.cuh) have kernels of their own.  What bounds it: the forward pass B in out multiply-adds of
+// 8-bit integers (kind::i8, twice the rate of bf16 by the same bytes of operands), the backward pass twice as many of bf16.
+// The codes are the operands of the forward pass as they lie.  For the backward pass a first kernel writes what they stand for as
+// bf16 to the workspace (the codes' rows times their scales, 46 us of the 1490 that the gradients of 8192 x 4096 x 16384 take),
+// beside the sums for db, and dy where TMA cannot read it.  Measured: forward 8192 x 4096 x 4096 87.6 us (3140 TOP/s), 16384 x
+// 4096 x 16384 690 to 780 us (3180 to 2820, the power cap); backward, 8192 x 4096 x 16384, dx 694 us (1584 TFLOP/s), dW as fp32
+// 716 us (1535), each by itself.
 //
 // fp32: a code is a bf16 value as it is, so that only dy times the scale (which belongs to the summed index in both products)
 // has to be split, into three bf16 terms: three products where two split operands would take six.

@@ -3,7 +3,8 @@
 // With B rows a code of W is multiplied B times: for few rows the bytes of W bound the time.  So W is the operand with the 128
 // rows of an MMA (outputs) and the rows of x are its 16 to 128 columns.  A tile of 128 outputs is a cluster's: its CTAs share the
 // K range, so that all SMs read W however few tiles there are, and add their integer sums, which are exact in any order, over
-// one another's shared memory: one launch, no workspace.
+// one another's shared memory: one launch, no workspace.  Measured: one row, 4096 x 16384 (67 MB) 14.5 us (4.6 TB/s; the tiles of
+// 256 rows take 24.8), 16384 x 4096 15 us (58), 4096 x 4096 6.8 us (17.5); 64 rows, 4096 x 16384 17 us.
 constexpr int kRowsThreads = 64 + 128;         // loads, products, four epilogue warps
 constexpr int kRowsPerSm = 2;                  // CTAs of an SM: clusters of whole SMs leave some of them idle
 constexpr int kRowsSmem = 104 * 1024;
