@@ -72,9 +72,9 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t full[kRingMostStages];
     __shared__ __align__(16) float red[6][32];
-    __shared__ int abort_flag;
+    __shared__ int flags[2];
     const int t = threadIdx.x, threads = blockDim.x;
-    RowRing<1> ring(shape, smem_u32(ring_smem), full, &abort_flag);
+    RowRing<1> ring(shape, smem_u32(ring_smem), full, flags);
     if (t == 0) ring.init();
     if (t < 32) {
 #pragma unroll
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     pdl_wait();
     const int first = (int)((long)rows * blockIdx.x / gridDim.x), last = (int)((long)rows * (blockIdx.x + 1) / gridDim.x);
     ring.sources({x});
-    for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row);
+    for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, -1);
     uint32_t round = 0;
     for (int row = first; row < last; ++row) {
         const bool ok = ring.wait<T, VEC>(row);
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
             }
         }
         top = ring_max(top, threads >> 5, red, round);
-        if (row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages);
+        if (row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, row);
         float s;
         const Act8Row r = act8_row(top, s);
         if (t == 0) scale[row] = s;

@@ -148,9 +148,9 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t full[kRingMostStages];
     __shared__ __align__(16) float red[6][32];
-    __shared__ int abort_flag;
+    __shared__ int flags[2];
     const int threads = blockDim.x, t = threadIdx.x, C = g.C;
-    RowRing<2> ring(shape, smem_u32(ring_smem), full, &abort_flag);
+    RowRing<2> ring(shape, smem_u32(ring_smem), full, flags);
     if (t == 0) ring.init();
     if (t < 32) {
 #pragma unroll
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
     pdl_wait();
     const int first = (int)((long)g.rows * blockIdx.x / gridDim.x), last = (int)((long)g.rows * (blockIdx.x + 1) / gridDim.x);
     ring.sources({g.b, g.res});
-    for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row);
+    for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, -1);
     constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
     typedef Share<T, VEC, ITER> Row;
     Row pre;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
         }
         sum[0] = ok ? sum2(s2) : __int_as_float(0x7fffffff);  // a row that did not come is NaN
         ring_sum<1>(sum, threads >> 5, red, round);
-        if (row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages);
+        if (row > first && row - 1 + shape.stages < last) ring.copy(row - 1 + shape.stages, row);
         const float r1 = rsqrtf(fmaf(sum[0], inv_c, g.eps));
         s2 = f2(0.f);
         uint32_t top = 0;
@@ -460,13 +460,13 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t full[kRingMostStages];
     __shared__ __align__(16) float red[6][32];
-    __shared__ int abort_flag;
+    __shared__ int flags[2];
     const int threads = blockDim.x, t = threadIdx.x, C = g.C;
     // share of dgamma_post over several stretches: [C], a thread its own columns
     float *const a_post = g.several ? reinterpret_cast<float *>(ring_smem + (size_t)shape.stages * 4 * shape.slot_bytes) : nullptr;
     if (a_post)
         for (int c = t; c < C; c += blockDim.x) a_post[c] = 0.f;  // (a barrier follows)
-    RowRing<4> ring(shape, smem_u32(ring_smem), full, &abort_flag);
+    RowRing<4> ring(shape, smem_u32(ring_smem), full, flags);
     if (t == 0) ring.init();
     if (t < 32) {
 #pragma unroll
@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     pdl_wait();
     ring.sources({g.dy, g.h, g.b, g.dh});
     NormRows ahead(g);
-    for (int i = 0; i < shape.stages && ahead.more(); ++i, ahead.next()) ring.copy(ahead.row);
+    for (int i = 0; i < shape.stages && ahead.more(); ++i, ahead.next()) ring.copy(ahead.row, -1);
     constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
     typedef Share<T, VEC, ITER> Row;
     F2 a_pre[P], a_unit[P], pg[P];  // pg: gamma_post times the gate
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
             float sum[3] = {sum2(q0), sum2(q1), sum2(q2)};
             ring_sum<3>(sum, threads >> 5, red, round);
             if (begun && ahead.more()) {
-                ring.copy(ahead.row);
+                ring.copy(ahead.row, row);
                 ahead.next();
             }
             begun = true;

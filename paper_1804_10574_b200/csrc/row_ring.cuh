@@ -1,6 +1,6 @@
-// Rows on their way through shared memory: a block copies the rows that it will work on, several ahead,
-// by bulk copies (TMA without a tensor map) into a ring of stages.  The threads read their values from there as often as they
-// need them; after the first barrier of the next row's reductions, when all are done with a row, its stage takes another.
+// Rows on their way through shared memory: a block copies the rows that it will work on, several ahead, by bulk copies (TMA
+// without a tensor map) into a ring of stages.  The threads read their values from there as often as they need them; after the
+// first barrier of the next row's reductions, when all are done with a row, its stage takes another.
 // Memory stays busy through the reductions, without registers for what is on the way or for what is needed again.
 //
 // A bulk copy moves whole 16-byte units.  Tensors start on 16-byte boundaries; a row that does not is copied from the boundary
@@ -32,19 +32,21 @@ template <int TENSORS> struct RowRing {
     uint32_t base;      // shared memory of the stages
     uint64_t *full;
     Waiter wt;
+    int *lost_at;       // shared memory: the first row whose wait ran out (rows come in ascending order)
     uint32_t stage, parity;  // of the row that is read next
     uint32_t head, issued;   // stage that is filled next; rows that this thread had copied
     const uint8_t *src[TENSORS];  // nullptr: a tensor that is not there
     int tensors;
     bool lost;
 
-    __device__ __forceinline__ RowRing(const RingShape &shape, uint32_t smem, uint64_t *full_, int *abort_flag)
-        : g(shape), base(smem), full(full_), wt{abort_flag, abort_flag, shape.polls}, stage(0), parity(0), head(0), issued(0), tensors(0), lost(false) {}
+    __device__ __forceinline__ RowRing(const RingShape &shape, uint32_t smem, uint64_t *full_, int (&flags)[2])
+        : g(shape), base(smem), full(full_), wt{&flags[0], &flags[0], shape.polls}, lost_at(&flags[1]), stage(0), parity(0), head(0), issued(0), tensors(0), lost(false) {}
 
     __device__ __forceinline__ void init() {  // by one thread, before a barrier of the block
         for (int i = 0; i < g.stages; ++i) mbar_init(smem_u32(&full[i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *wt.abort_flag = 0;
+        *lost_at = 0x7fffffff;
     }
     __device__ __forceinline__ void sources(const void *const (&all)[TENSORS]) {
 #pragma unroll
@@ -53,11 +55,13 @@ template <int TENSORS> struct RowRing {
             tensors += all[k] != nullptr;
         }
     }
-    // By all threads: the next row into the stage that is free.  The first lane of each warp issues a share of the copies: each
-    // takes its warp a few hundred cycles.  Nothing is copied any more once a wait ran out.
-    __device__ __forceinline__ void copy(int row) {
+    // By all threads: a row into the stage that is free, while row `now` is worked on (-1: none yet), after a barrier behind the
+    // wait for that.  The first lane of each warp issues a share of the copies: each takes its warp a few hundred cycles.  Once a
+    // wait for this row or one before ran out nothing is copied any more; the barrier has made that the same for all warps, so
+    // that a stage gets all of its copies or none, and the first thread knows what is on the way.
+    __device__ __forceinline__ void copy(int row, int now) {
         const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
-        if ((threadIdx.x & 31) == 0 && warp < TENSORS && !*wt.abort_flag) {
+        if ((threadIdx.x & 31) == 0 && warp < TENSORS && *(volatile int *)lost_at > now) {
             const size_t at = (size_t)row * g.row_bytes, from = at & ~(size_t)15, to = min((at + g.row_bytes + 15) & ~(size_t)15, g.floor16);
             const uint32_t bytes = to > from ? (uint32_t)(to - from) : 0u, bar = smem_u32(&full[head]);
             // (what lands before the barrier expects it is counted all the same: its phase ends with this arrival)
@@ -73,10 +77,13 @@ template <int TENSORS> struct RowRing {
     __device__ __forceinline__ void drain() {
         for (uint32_t i = issued > (uint32_t)g.stages ? issued - g.stages : 0; i < issued; ++i) mbar_drain(smem_u32(&full[i % g.stages]), (i / g.stages) & 1u);
     }
-    // By all threads: false when a wait of the thread ran out, this one or one before (what stands in the stage may not be the row).  T: type of the tensors' values, single
-    // ones where rows keep to no boundary.
+    // By all threads: false when a wait of the thread ran out, this one or one before (what stands in the stage may not be the
+    // row).  T: type of the tensors' values, VEC = 1 where rows keep to no boundary.
     template <typename T, int VEC> __device__ __forceinline__ bool wait(int row) {
-        lost = lost || !mbar_wait(smem_u32(&full[stage]), parity, wt, 82);
+        if (!lost && !mbar_wait(smem_u32(&full[stage]), parity, wt, 82)) {
+            lost = true;
+            atomicMin(lost_at, row);
+        }
         if (VEC == 1 && (size_t)(row + 1) * g.row_bytes > g.floor16) {  // the tensor's last values, which no copy brought
             const size_t at = (size_t)row * g.row_bytes;
             const int there = g.floor16 > at ? (int)(g.floor16 - at) / (int)sizeof(T) : 0, all = g.row_bytes / (int)sizeof(T);
