@@ -45,9 +45,10 @@ constexpr int kPairs = 74;                       // CTA pairs of the GPU: the sp
 enum Mode { kForward, kGrad };
 enum Store { kBoxes, kRows };                    // results leave by a tensor map, or a line at a time
 
-struct MmArgs {
+struct MmArgs {           // a product
     int M, N;                 // rows of A, rows of B (columns of the result)
     int kblocks, n_seg;       // K blocks of a segment; segments: bf16 terms of A
+    int a_mn;                 // gradients: A lies with M innermost (its rows are K values) instead of K
     int a_off[kMostPlanes];   // where a segment's term starts: in K (K-major A) or in M
     int tiles_m, tiles_n, splits, group_m;
     int width;                // columns of a tile: at most 256, a multiple of 64
@@ -61,8 +62,20 @@ struct MmArgs {
     void *out;                // [splits][M][ld]
     int out_bf16, store, ld;
     size_t out_split;         // elements
+    int box_rows;             // rows of the result's tensor map from a split to the next
     unsigned polls;           // of a bounded wait
 };
+// The products of a launch, both gradients or one product: the items of the first, then those of the second.
+constexpr int jobs_of(int mode) { return mode == kGrad ? 2 : 1; }
+template <int JOBS> struct MmJobs { MmArgs job[JOBS]; };
+template <int JOBS> struct MmMaps { CUtensorMap a[JOBS], b[JOBS], out[JOBS]; };
+template <int JOBS> __device__ __forceinline__ int mm_items(const MmJobs<JOBS> &all) { return JOBS == 1 ? all.job[0].items : all.job[0].items + all.job[JOBS - 1].items; }
+// the product that an item belongs to; the item becomes the product's own
+template <int JOBS> __device__ __forceinline__ int mm_job(const MmJobs<JOBS> &all, int &item) {
+    if (JOBS == 1 || item < all.job[0].items) return 0;
+    item -= all.job[0].items;
+    return JOBS - 1;
+}
 
 // All tiles of a split, in bands of group_m tile rows that are walked column by column, so that the operands of the tiles in
 // flight stay in the L2.  The tiles that would make a last round of the CTA pairs with few of them at work are cut into
@@ -119,21 +132,27 @@ __device__ __forceinline__ void mm_finish(const MmArgs &g, const CUtensorMap *ma
     if (row0 >= g.M) return;
     if (g.store == kBoxes) {
         if (g.out_bf16) store_box(map_out, buf, lane, col, row0, v);
-        else store_box_f32(map_out, buf, lane, col, row0, v);
-    } else if (g.out_bf16) {
+        else store_box_f32(map_out, buf, lane, col, row0 + split * g.box_rows, v);
+        return;
+    }
+    if (MODE == kGrad) {  // the buffer may hold a box of the other product that is still on its way out
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
+    if (g.out_bf16) {
         store_rows<true>((uint16_t *)g.out + split * g.out_split, buf, lane, row0, g.M, col, g.ld, v);
     } else {
         store_rows<false>((float *)g.out + split * g.out_split, buf, lane, row0, g.M, col, g.ld, v);
     }
 }
 
-// A_MN / B_MN: the operand lies with M / N innermost (its rows are K values) instead of K.  I8: codes, exact sums.
-// PROMOTE: an accumulator holds at most g.piece steps, the epilogue adds the pieces.
-template <int MODE, bool A_MN, bool B_MN, bool PROMOTE>
+// Gradients: B lies with N innermost, A as its product says.  PROMOTE: an accumulator holds at most `piece` steps, the epilogue
+// adds the pieces.
+template <int MODE, bool PROMOTE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ MmArgs g) {
-    constexpr bool kI8 = MODE == kForward;
-    static_assert(!kI8 || (!A_MN && !B_MN && !PROMOTE), "codes lie with K innermost and their sums are exact");
+mm_kernel(const __grid_constant__ MmMaps<jobs_of(MODE)> maps, const __grid_constant__ MmJobs<jobs_of(MODE)> all) {
+    constexpr bool kI8 = MODE == kForward, B_MN = !kI8;
+    static_assert(!kI8 || !PROMOTE, "sums of codes are exact");
     constexpr int kElem = kI8 ? 1 : 2, kw = kStageKw / kElem, kBox = 128 / kElem;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
@@ -143,7 +162,7 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const Waiter wt{&abort_flag, &abort_flag, g.polls};
+    const Waiter wt{&abort_flag, &abort_flag, all.job[0].polls};
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 2 * kEpiWarps); }
@@ -162,10 +181,12 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     cluster_sync();  // both CTAs' barriers are ready
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
-    const int n_items = g.items;
+    const int n_items = mm_items(all);
     const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
     // Copies into stage s of this CTA's halves of A and B: one step of the K range.
-    auto load_step = [&](uint32_t s, int seg, int k, int m0, int n0, int width) {
+    auto load_step = [&](uint32_t s, int job, int seg, int k, int m0, int n0, int width) {
+        const MmArgs &g = all.job[job];
+        const CUtensorMap *map_a = &maps.a[job], *map_b = &maps.b[job];
         const int half = width / 2;  // columns of this CTA
         if (rank == 0) mbar_expect_tx(smem_u32(&full[s]), 2u * (uint32_t)(kBlockBytes + (B_MN ? (half + kBox - 1) / kBox * kBox : half) * kStageKw));
         const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
@@ -173,15 +194,15 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         // K-major: a box is 128 bytes of K of 128 rows.  MN-major: 64 rows of kw K values.
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if (A_MN) tma_load_pair(a + j * (kBlockBytes / 2), &map_a, bar, g.a_off[seg] + m0 + kBox * j, k);
-            else tma_load_pair(a + j * (kHalf * 128), &map_a, bar, g.a_off[seg] + k + kBox * j, m0);
+            if (!kI8 && g.a_mn) tma_load_pair(a + j * (kBlockBytes / 2), map_a, bar, g.a_off[seg] + m0 + kBox * j, k);
+            else tma_load_pair(a + j * (kHalf * 128), map_a, bar, g.a_off[seg] + k + kBox * j, m0);
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             if (B_MN) {
-                if (j * kBox < half) tma_load_pair(b + j * (kBlockBytes / 2), &map_b, bar, n0 + kBox * j, k);
+                if (j * kBox < half) tma_load_pair(b + j * (kBlockBytes / 2), map_b, bar, n0 + kBox * j, k);
             } else {
-                for (int r = 0; r < half; r += g.b_box) tma_load_pair(b + j * (kHalf * 128) + r * 128, &map_b, bar, k + kBox * j, n0 + r);
+                for (int r = 0; r < half; r += g.b_box) tma_load_pair(b + j * (kHalf * 128) + r * 128, map_b, bar, k + kBox * j, n0 + r);
             }
         }
     };
@@ -193,14 +214,17 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             bool ok = true;
             uint32_t s = 0, ph = 0;
             for (int item = first; item < n_items && ok; item += step) {
-                const MmTile t = mm_tile(g, item);
+                int own = item;
+                const int job = mm_job(all, own);
+                const MmArgs &g = all.job[job];
+                const MmTile t = mm_tile(g, own);
                 int i0, i1;
                 mm_range(g, t.split, i0, i1);
                 const int m0 = t.m * kTile + (int)rank * kHalf, n0 = t.col + (int)rank * (t.width / 2);
                 int kb = i0 == 0 ? 0 : i0 / g.n_seg, seg = i0 - kb * g.n_seg;
                 for (int i = i0; i < i1; ++i) {
                     if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1u, wt, 71)) { ok = false; break; }
-                    load_step(s, seg, kb * kw, m0, n0, t.width);
+                    load_step(s, job, seg, kb * kw, m0, n0, t.width);
                     ++issued;
                     if (++seg == g.n_seg) { seg = 0; ++kb; }
                     if (++s == kStages) { s = 0; ph ^= 1u; }
@@ -214,29 +238,33 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             // accumulator stand outside.
             issuer = elect_one();
             // 32-bit results: fp32 (1) or int32 (2); operands: bf16 (1) of kind::f16, signed (1) of kind::i8
-            const uint32_t idesc_tile = ((kI8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kTile >> 4) << 24);
+            const uint32_t idesc_tile = ((kI8 ? 2u : 1u) << 4) | (1u << 7) | (1u << 10) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kTile >> 4) << 24);
             uint32_t idesc = 0;
+            bool a_mn = false;
             // K-major: a step of K is 32 bytes of a swizzle row, the next 128 bytes 16 KB further.  MN-major: a step is 16 rows of
             // 128 bytes; the next 64 of the 128 M / N values lie half a block further.
-            const uint64_t ad0 = A_MN ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
+            uint64_t ad0 = 0;
             const uint64_t bd0 = B_MN ? make_desc(base + kBlockBytes, 1024, 2u, kBlockBytes / 2) : make_desc(base + kBlockBytes, 1024, 2u);
             auto multiply = [&](uint32_t s, uint32_t acc, bool fresh, int steps) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     if (k >= steps) break;
                     const uint32_t at = s * (kStageBytes >> 4), kk = (uint32_t)((k >> 2) * (kHalf * 128 >> 4) + (k & 3) * 2);
-                    const uint64_t a = ad0 + (uint64_t)(at + (A_MN ? 128u * k : kk)), b = bd0 + (uint64_t)(at + (B_MN ? 128u * k : kk));
+                    const uint64_t a = ad0 + (uint64_t)(at + (a_mn ? 128u * k : kk)), b = bd0 + (uint64_t)(at + (B_MN ? 128u * k : kk));
                     if (kI8) mma_pair_i8(tmem + acc * kTile, a, b, idesc, !fresh || k > 0);
                     else mma_pair(tmem + acc * kTile, a, b, idesc, !fresh || k > 0);
                 }
             };
             bool ok = true;
             uint32_t s = 0, ph = 0, u = 0;  // stage, its parity, accumulators used so far
-            const int short_from = (g.kblocks - 1) * g.n_seg;  // the last K block has g.tail steps
             for (int item = first; item < n_items && ok; item += step) {
-                int i0, i1;
-                mm_range(g, mm_split_of(g, item), i0, i1);
-                idesc = idesc_tile | ((uint32_t)(mm_width_of(g, item) >> 3) << 17);
+                int own = item, i0, i1;
+                const MmArgs &g = all.job[mm_job(all, own)];
+                const int short_from = (g.kblocks - 1) * g.n_seg;  // the last K block has g.tail steps
+                mm_range(g, mm_split_of(g, own), i0, i1);
+                a_mn = !kI8 && g.a_mn;
+                ad0 = a_mn ? make_desc(base, 1024, 2u, kBlockBytes / 2) : make_desc(base, 1024, 2u);
+                idesc = idesc_tile | (a_mn ? 1u << 15 : 0u) | ((uint32_t)(mm_width_of(g, own) >> 3) << 17);
                 for (; i0 < i1; ++u) {
                     const int end = PROMOTE ? mm_piece_end(g, i0, i1) : i1;
                     const uint32_t acc = u & 1u;
@@ -272,7 +300,11 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         uint32_t u = 0;
         bool ok = true;
         for (int item = first; item < n_items; item += step) {
-            const MmTile t = mm_tile(g, item);
+            int own = item;
+            const int job = mm_job(all, own);
+            const MmArgs &g = all.job[job];
+            const CUtensorMap *map_out = &maps.out[job];
+            const MmTile t = mm_tile(g, own);
             const int row = t.m * kTile + (int)rank * kHalf + 32 * quarter + lane;
             const int col0 = t.col + half * kHalf, live = min(t.width - half * kHalf, g.N - col0);
             int pieces = 1;
@@ -320,7 +352,7 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                             tc_wait_ld();
                         }
                         if (c == kHalf - kKBox) hand_back();
-                        if (c < live) mm_finish<MODE>(g, &map_out, buf, v, t.split, row, col0 + c, lane, rs, s_col, c == 0 ? cs[0] : cs[2], c == 0 ? cs[1] : cs[3], c == 0 ? cb[0] : cb[2], c == 0 ? cb[1] : cb[3]);
+                        if (c < live) mm_finish<MODE>(g, map_out, buf, v, t.split, row, col0 + c, lane, rs, s_col, c == 0 ? cs[0] : cs[2], c == 0 ? cs[1] : cs[3], c == 0 ? cb[0] : cb[2], c == 0 ? cb[1] : cb[3]);
                     }
                 } else {
 #pragma unroll
@@ -345,7 +377,7 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             if (PROMOTE) {
 #pragma unroll
                 for (int c = 0; c < kHalf; c += kKBox)
-                    if (c < live) mm_finish<MODE>(g, &map_out, buf, v + (PROMOTE ? c : 0), t.split, row, col0 + c, lane, rs, s_col, 0.f, 0.f, 0.f, 0.f);
+                    if (c < live) mm_finish<MODE>(g, map_out, buf, v + (PROMOTE ? c : 0), t.split, row, col0 + c, lane, rs, s_col, 0.f, 0.f, 0.f, 0.f);
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -367,15 +399,17 @@ mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         cluster_sync();
         if (threadIdx.x == 0) {
             const uint32_t peer = s_peer & ~kGaveUp, last = max(issued, peer);
-            int item = first, left = 0;  // the item that a step is of: how many steps up to its end
+            int item = first, left = 0, job = 0, width = 0;  // the item that a step is of: how many steps up to its end
             for (uint32_t i = 0; i < peer; ++i, --left) {
                 if (i > 0 && left == 0) item += step;
                 if (left == 0) {
-                    int i0, i1;
-                    mm_range(g, mm_split_of(g, item), i0, i1);
+                    int own = item, i0, i1;
+                    job = mm_job(all, own);
+                    mm_range(all.job[job], mm_split_of(all.job[job], own), i0, i1);
                     left = i1 - i0;
+                    width = mm_width_of(all.job[job], own);
                 }
-                if (i >= issued) load_step(i % kStages, 0, 0, 0, 0, mm_width_of(g, item));
+                if (i >= issued) load_step(i % kStages, job, 0, 0, 0, 0, width);
             }
             if (rank == 0)
                 for (uint32_t i = last > kStages ? last - kStages : 0; i < last; ++i) mbar_drain(smem_u32(&full[i % kStages]), (i / kStages) & 1u);
@@ -424,7 +458,6 @@ __device__ __forceinline__ void prep_codes(const CodesJob &j, int block) {
     }
 }
 
-constexpr int kSumRows = 512;   // so many rows are summed up for db in one go
 constexpr int kTermCols = 256;  // columns of a row that a warp has at a time, two neighbours per lane
 template <typename T> __device__ __forceinline__ void prep_terms(const TermsJob &j, int block) {
     const int lane = threadIdx.x & 31;
@@ -519,14 +552,31 @@ template <typename T> __global__ void __launch_bounds__(256) fc8_prep_kernel(con
 }
 
 // ---- after the products of the backward pass -------------------------------------------------------------------------
-// Sums of the parts of up to three results, in index order: dx and dW where their K range was split, db.
+// Sums of parts, in index order: of dx and dW where their K range was split, of db (a column per thread and warp).
 struct JoinJob { const float *part; void *out; size_t stride, total; int parts, ld, cols, out_bf16, vec, blocks; };
-struct JoinArgs { JoinJob job[3]; };
+struct JoinSums { const float *part; float *db; int parts, cols; };
+struct JoinArgs { JoinJob job[2]; JoinSums sums; };
+__device__ __forceinline__ void join_sums(const JoinSums &j, int block) {
+    __shared__ float fold[8][32];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = block * 32 + lane;
+    float a = 0.f;
+    if (c < j.cols) {
+#pragma unroll 4
+        for (int i = w; i < j.parts; i += 8) a += j.part[(size_t)i * j.cols + c];
+    }
+    fold[w][lane] = a;
+    __syncthreads();
+    if (w == 0 && c < j.cols) {
+        for (int i = 1; i < 8; ++i) a += fold[i][lane];
+        j.db[c] = a;
+    }
+}
 __global__ void __launch_bounds__(256) fc8_join_kernel(const __grid_constant__ JoinArgs g) {
     pdl_launch();
     pdl_wait();
     int block = blockIdx.x, k = 0;
-    while (k < 2 && block >= g.job[k].blocks) block -= g.job[k++].blocks;
+    for (; k < 2 && block >= g.job[k].blocks; ++k) block -= g.job[k].blocks;
+    if (k == 2) { join_sums(g.sums, block); return; }
     const JoinJob &j = g.job[k];
     for (size_t i = (size_t)block * 256 + threadIdx.x; i < j.total; i += (size_t)j.blocks * 256) {  // groups of four columns
         const size_t row = i / (j.ld / 4);
@@ -549,24 +599,6 @@ __global__ void __launch_bounds__(256) fc8_join_kernel(const __grid_constant__ J
         }
     }
 }
-// db alone: a column per thread and warp, parts in index order
-__global__ void __launch_bounds__(256) fc8_db_kernel(const float *__restrict__ part, float *__restrict__ db, int parts, int cols) {
-    __shared__ float fold[8][32];
-    pdl_launch();
-    pdl_wait();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    float a = 0.f;
-    if (c < cols) {
-#pragma unroll 4
-        for (int i = w; i < parts; i += 8) a += part[(size_t)i * cols + c];
-    }
-    fold[w][lane] = a;
-    __syncthreads();
-    if (w == 0 && c < cols) {
-        for (int i = 1; i < 8; ++i) a += fold[i][lane];
-        db[c] = a;
-    }
-}
 
 // ---- host side -------------------------------------------------------------------------------------------------------
 int up(int v, int to) { return (v + to - 1) / to * to; }
@@ -580,52 +612,78 @@ int sm_count() {
 
 thread_local int t_wait_polls = -1;  // polls of a bounded wait, for the calls of this thread (negative: the default)
 
-// Columns of the tiles of M x N (times splits): at most 256, as many tiles as that takes, alike.  Where that leaves CTA pairs
-// without work, narrower ones: half of a tile's loads, A's, stay.
-int mm_width(int M, int N, int splits) {
+// Columns of the tiles of M x N (times splits): at most 256, as many tiles as that takes, alike.  Where that leaves some of the
+// CTA pairs that the product may count on without work, narrower ones: half of a tile's loads, A's, stay.
+double mm_weight(int width) { return 0.5 + 0.5 * width / kTile; }
+int mm_width(int M, int N, int splits, int pairs) {
     const long rows = (long)((M + kTile - 1) / kTile) * splits;
     int best = kTile;
     double least = 1e30;
     for (int most = kTile; most >= kKBox; most /= 2) {
         const int tiles = (N + most - 1) / most, width = ((N + tiles - 1) / tiles + kKBox - 1) / kKBox * kKBox;
-        const double t = (double)((rows * tiles + kPairs - 1) / kPairs) * (0.5 + 0.5 * width / kTile);
+        const double t = (double)((rows * tiles + pairs - 1) / pairs) * mm_weight(width);
         if (t < 0.98 * least) { least = t; best = width; }
-        if (rows * tiles >= kPairs) break;
-    }
-    return best;
-}
-// Rounds of the GPU's CTA pairs that the tiles (times splits) take, in units of a 256 x 256 tile of the whole K.
-double mm_rounds(int M, int N, int splits) {
-    const int width = mm_width(M, N, splits);
-    const long items = (long)((M + kTile - 1) / kTile) * ((N + width - 1) / width) * splits;
-    return (double)((items + kPairs - 1) / kPairs) * (0.5 + 0.5 * width / kTile) / splits;
-}
-// Splits of K (steps of 128 values), where the tiles alone fill the GPU badly; each costs a write and a read of its sums.
-// Seconds by 1.4 PFLOP/s and 6 TB/s.
-int mm_splits(int M, int N, int steps) {
-    const long tiles = (long)((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
-    const int most = (int)std::max<long>(1, std::min<long>(2 * kPairs / tiles, steps / 4));
-    int best = 1;
-    double least = 1e30;
-    for (int i = 1; i <= 10; ++i) {  // 1 to 8, and one or two rounds of pairs
-        const int n = (int)std::min<long>(most, i <= 8 ? i : (i - 8) * kPairs / std::max<long>(1, tiles));
-        if (n < 1) continue;
-        const double t = mm_rounds(M, N, n) * 2.0 * kTile * kTile * 128.0 * steps * kPairs / 1.4e15 + (n > 1 ? 3e-6 + 8.0 * n * M * up(N, 4) / 6e12 : 0.0);
-        if (t < least) { least = t; best = n; }
+        if (rows * tiles >= pairs) break;
     }
     return best;
 }
 
-// The tiles of the last round of the CTA pairs, where it is not full, are halved or quartered if that is done sooner: half of a
-// part's loads, A's, stay.
-void mm_cut(MmArgs &g, int tiles, int pairs) {
-    const int rest = tiles > pairs ? tiles % pairs : 0;
+// A way to do a product: splits of K (steps of 128 values) where the tiles alone fill the GPU badly; each costs a write and a
+// read of its sums.  Seconds by 1.4 PFLOP/s and 6 TB/s.
+struct MmWay { int splits, width; long items; double each, sums; };
+constexpr int kMostWays = 10;
+int mm_ways(int M, int N, int steps, int pairs, MmWay (&way)[kMostWays]) {
+    const long rows = (M + kTile - 1) / kTile, tiles = rows * ((N + kTile - 1) / kTile);
+    const int most = (int)std::max<long>(1, std::min<long>(2 * kPairs / tiles, steps / 4));
+    int n = 0;
+    for (int i = 1; i <= kMostWays; ++i) {  // 1 to 8, and one or two rounds of pairs
+        const int splits = (int)std::min<long>(most, i <= 8 ? i : (i - 8) * kPairs / std::max<long>(1, tiles));
+        if (splits < 1 || (n && splits <= way[n - 1].splits)) continue;
+        MmWay &w = way[n++];
+        w.splits = splits;
+        w.width = mm_width(M, N, splits, pairs);
+        w.items = rows * ((N + w.width - 1) / w.width) * splits;
+        w.each = mm_weight(w.width) / splits * 2.0 * kTile * kTile * 128.0 * steps * kPairs / 1.4e15;
+        w.sums = splits > 1 ? 8.0 * splits * M * up(N, 4) / 6e12 : 0.0;
+    }
+    return n;
+}
+// How long two products take in a launch, the longer items first, dealt out to the CTA pairs in turn, and the launch that adds up
+// the splits.
+double mm_time(const MmWay &a, const MmWay &b) {
+    const long whole_a = a.items / kPairs, rest_a = a.items % kPairs, whole_b = b.items / kPairs, rest_b = b.items % kPairs;
+    const double t = a.sums + b.sums + (a.splits > 1 || b.splits > 1 ? 3e-6 : 0.0) + whole_a * a.each + whole_b * b.each;
+    if (rest_a + rest_b > kPairs) return t + a.each + b.each;
+    return t + std::max(rest_a ? a.each : 0.0, rest_b ? b.each : 0.0);
+}
+// Both in one launch, unless they keep the pairs busy for more than eight rounds: there a launch less is nothing, and pairs out of
+// step bring operands from memory twice.  (us in one / in two: 512 x 512 x 512 8.5 / 15, fp32 1000 x 512 x 2000 28 / 40, 4096 x
+// 4096 x 4096 201 / 211, fp32 635 / 700; 8192 x 4096 x 4096 419 / 414, fp32 8192 x 8192 x 8192 5250 / 5120.)
+bool mm_together(const MmWay &dx, const MmWay &dw) { return dx.items + dw.items <= 8 * kPairs; }
+// Both gradients share the CTA pairs: each is planned for half of them.  One that is asked for alone is split the same way, so
+// that its sums are the same to the last bit.
+void mm_plan(const int (&sizes)[2][3], MmWay &dx, MmWay &dw) {
+    MmWay way[2][kMostWays];
+    int n[2];
+    for (int k = 0; k < 2; ++k) n[k] = mm_ways(sizes[k][0], sizes[k][1], sizes[k][2], kPairs / 2, way[k]);
+    double least = 1e30;
+    for (int i = 0; i < n[0]; ++i)
+        for (int j = 0; j < n[1]; ++j) {
+            const double t = mm_time(way[0][i], way[1][j]);
+            if (t < least) { least = t; dx = way[0][i]; dw = way[1][j]; }
+        }
+}
+
+// The tiles of the last round of the CTA pairs (so many come before these), where it is not full, are halved or quartered if that
+// is done sooner: half of a part's loads, A's, stay.
+void mm_cut(MmArgs &g, int before, int tiles, int pairs) {
+    const int rest = before + tiles > pairs ? std::min((before + tiles) % pairs, tiles) : 0;
     g.full = tiles;
     g.cut = 1;
     double least = 0.95;
     for (int c = 2; c <= 4 && rest; c *= 2) {
         if (g.width % (c * kKBox) != 0) break;
-        const double t = (double)((rest * c + pairs - 1) / pairs) * (0.5 + 0.5 / c);
+        const double t = (double)((rest * c + pairs - 1) / pairs) * mm_weight(kTile / c);
         if (t < least) { least = t; g.cut = c; g.full = tiles - rest; }
     }
     g.items = g.full + (tiles - g.full) * g.cut;
@@ -634,45 +692,61 @@ void mm_cut(MmArgs &g, int tiles, int pairs) {
 // An operand: a row-major matrix in memory; ld: elements from a row to the next.
 struct Operand { const void *ptr; int rows, cols; size_t ld; };
 
-// most_chain: K values of a chain (with PROMOTE)
-template <int MODE, bool A_MN, bool B_MN, bool PROMOTE>
-int mm_launch_as(const Operand &a, const Operand &b, MmArgs &g, int K, int most_chain, const Launch &s) {
-    constexpr bool kI8 = MODE == kForward;
-    constexpr int es = kI8 ? 1 : 2, kw = kStageKw / es;
-    constexpr CUtensorMapDataType type = kI8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    g.kblocks = (K + kw - 1) / kw;
-    g.tail = (K - (g.kblocks - 1) * kw + 32 / es - 1) / (32 / es);
-    g.piece = most_chain / kw;
-    g.tiles_m = (g.M + kTile - 1) / kTile;
-    g.splits = std::max(1, std::min(g.splits, g.kblocks * g.n_seg));
-    g.width = mm_width(g.M, g.N, g.splits);
-    g.tiles_n = (g.N + g.width - 1) / g.width;
-    g.group_m = 16;
-    const long tiles = (long)g.tiles_m * g.tiles_n * g.splits;
-    const int pairs = sm_count() / 2;
-    if (tiles > 0x7fffffff / 4) return -1;
-    mm_cut(g, (int)tiles, pairs);
-    g.b_box = g.width / g.cut / 2;
-    CUtensorMap ma, mb, mo{};
-    if (!box_map(type, es, a.ptr, a.rows, a.cols, a.ld, A_MN ? kw : kHalf, &ma) || !box_map(type, es, b.ptr, b.rows, b.cols, b.ld, B_MN ? kw : g.b_box, &mb)) return -1;
-    if (g.store == kBoxes &&
-        !box_map(g.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, g.out_bf16 ? 2 : 4, g.out, g.M, g.N, g.ld, 32, &mo)) return -1;
-    static thread_local int ready_dev = -1;  // the attribute belongs to a device
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (ready_dev != dev) {
-        if (cudaFuncSetAttribute(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
-        ready_dev = dev;
-    }
-    g.polls = block8_polls();
-    launch_k(mm_kernel<MODE, A_MN, B_MN, PROMOTE>, 2 * std::min(g.items, pairs), kThreads, kSmem, s, ma, mb, mo, g);
-    return 1;
-}
+// One of the products of a launch: what its sizes say, with g.M, N, n_seg, splits, width and where the results go.
+// most_chain: K values of a chain (with PROMOTE).
+template <int MODE> struct MmLaunch {
+    static constexpr int kJobs = jobs_of(MODE), kBytes = MODE == kForward ? 1 : 2, kw = kStageKw / kBytes;
+    MmMaps<kJobs> maps{};
+    MmJobs<kJobs> all{};
+    int n = 0, items = 0;
+    int pairs = sm_count() / 2;
 
-// Where the results go: whole results by a tensor map when their rows keep to 16 bytes.
+    // last: no other product comes behind this one
+    bool add(const Operand &a, const Operand &b, MmArgs g, int K, int most_chain, bool last) {
+        g.kblocks = (K + kw - 1) / kw;
+        g.tail = (K - (g.kblocks - 1) * kw + 32 / kBytes - 1) / (32 / kBytes);
+        g.piece = most_chain / kw;
+        g.tiles_m = (g.M + kTile - 1) / kTile;
+        g.tiles_n = (g.N + g.width - 1) / g.width;
+        g.group_m = 16;
+        g.polls = block8_polls();
+        const long tiles = (long)g.tiles_m * g.tiles_n * g.splits;
+        if (tiles > 0x7fffffff / 16) return false;
+        g.full = g.items = (int)tiles;
+        g.cut = 1;
+        if (last) mm_cut(g, items, (int)tiles, pairs);
+        g.b_box = g.width / g.cut / 2;
+        constexpr CUtensorMapDataType type = MODE == kForward ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+        if (!box_map(type, kBytes, a.ptr, a.rows, a.cols, a.ld, g.a_mn ? kw : kHalf, &maps.a[n]) ||
+            !box_map(type, kBytes, b.ptr, b.rows, b.cols, b.ld, MODE == kGrad ? kw : g.b_box, &maps.b[n]))
+            return false;
+        if (g.store == kBoxes && !box_map(g.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, g.out_bf16 ? 2 : 4, g.out,
+                                          g.splits > 1 ? g.splits * g.box_rows : g.M, g.splits > 1 ? g.ld : g.N, g.ld, 32, &maps.out[n]))
+            return false;
+        all.job[n++] = g;
+        items += g.items;
+        return true;
+    }
+    template <bool PROMOTE> int run(const Launch &s) {
+        static thread_local int ready_dev = -1;  // the attribute belongs to a device
+        int dev = 0;
+        cudaGetDevice(&dev);
+        if (ready_dev != dev) {
+            if (cudaFuncSetAttribute(mm_kernel<MODE, PROMOTE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
+            ready_dev = dev;
+        }
+        launch_k(mm_kernel<MODE, PROMOTE>, 2 * std::min(items, pairs), kThreads, kSmem, s, maps, all);
+        return 1;
+    }
+};
+
+// Where the results go: by a tensor map when their rows keep to 16 bytes.  Splits' sums lie one behind the other, with room for a
+// box's rows behind the last.
 void mm_out(MmArgs &g, void *out, bool is_bf16, int ld) {
     g.out = out; g.out_bf16 = is_bf16; g.ld = ld;
-    g.store = g.splits == 1 && ld * (is_bf16 ? 2 : 4) % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 ? kBoxes : kRows;
+    g.box_rows = up(g.M, 32);
+    g.out_split = (size_t)g.box_rows * ld;
+    g.store = ld * (is_bf16 ? 2 : 4) % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 ? kBoxes : kRows;
 }
 
 int rows_columns(int B) { return B <= 16 ? 16 : (B <= 32 ? 32 : (B <= 64 ? 64 : 128)); }
@@ -688,7 +762,7 @@ bool rows_fit(int B, int in, int out) {
     const long tiles = (long)((out + kHalf - 1) / kHalf) * ((B + nt - 1) / nt);
     if (B <= 32) return true;
     if (B > 1024 || tiles > kRowsPerSm * sms) return false;
-    const int splits = rows_splits(nt, (int)tiles, in), width = mm_width(B, out, 1);
+    const int splits = rows_splits(nt, (int)tiles, in), width = mm_width(B, out, 1, kPairs);
     const double mine = (double)((tiles * splits + sms - 1) / sms) * ((in + splits - 1) / splits) * (kHalf + nt) + 2048.0 * nt;
     const long pairs = (long)((B + kTile - 1) / kTile) * ((out + width - 1) / width);
     return mine < (double)((pairs + kPairs - 1) / kPairs) * in * (kHalf + width / 2);
@@ -723,7 +797,8 @@ struct BwdPlan {
     int planes;              // bf16 terms of dy
     bool copy_dy;            // dy is not read in place: fp32, or rows that TMA cannot read
     int plane_in, plane_out; // columns of a row of codes as bf16, of a term of dy
-    int dx_splits, dw_splits, ld;
+    MmWay dx_way, dw_way;
+    int ld;
     int chunk, chunks;       // rows of dy that are summed up at a time for db
     size_t x, w, dy[2], dx, dw, db, bytes;
 };
@@ -734,17 +809,19 @@ BwdPlan bwd_plan(int prec, int B, int in, int out) {
     p.plane_out = prec == P_F32 ? up(out, 128) : up(out, 64);  // fp32: a K block never reaches into the next term
     p.ld = up(in, 4);
     const int kw = kStageKw / 2;
-    p.dx_splits = mm_splits(B, in, (out + kw - 1) / kw * p.planes);
-    p.dw_splits = mm_splits(out, in, (B + kw - 1) / kw * p.planes);
-    p.chunk = B <= kSumRows ? B : std::max(256, (B + 127) / 128);
+    const int sizes[2][3] = {{B, in, (out + kw - 1) / kw * p.planes}, {out, in, (B + kw - 1) / kw * p.planes}};
+    mm_plan(sizes, p.dx_way, p.dw_way);
+    // so that a thread has 8 rows to add up (the join that the splits take adds up db's too), or some more where that saves a launch
+    const int sum_rows = (out % 8 == 0 ? 128 : 32) * (p.dx_way.splits > 1 || p.dw_way.splits > 1 ? 1 : 4);
+    p.chunk = B <= sum_rows ? B : std::max(std::min(sum_rows, 256), (B + 127) / 128);
     p.chunks = (B + p.chunk - 1) / p.chunk;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += up256(bytes); return r; };
     p.x = take((size_t)B * p.plane_in * 2);
     p.w = take((size_t)out * p.plane_in * 2);
     for (int k = 0; k < (prec == P_F32 ? 2 : 1); ++k) p.dy[k] = take((size_t)B * p.planes * p.plane_out * 2);  // also for a bf16 dy that starts anywhere
-    if (p.dx_splits > 1) p.dx = take((size_t)p.dx_splits * B * p.ld * 4);
-    if (p.dw_splits > 1) p.dw = take((size_t)p.dw_splits * out * p.ld * 4);
+    if (p.dx_way.splits > 1) p.dx = take((size_t)p.dx_way.splits * up(B, 32) * p.ld * 4);
+    if (p.dw_way.splits > 1) p.dw = take((size_t)p.dw_way.splits * up(out, 32) * p.ld * 4);
     p.db = take((size_t)p.chunks * out * 4);
     p.bytes = at;
     return p;
@@ -783,10 +860,11 @@ int launch_fc8_fwd(int prec, const void *xq, const float *xs, const void *wq, co
         }
     }
     MmArgs g{};
-    g.M = B; g.N = out; g.n_seg = 1; g.splits = 1;
+    g.M = B; g.N = out; g.n_seg = 1; g.splits = 1; g.width = mm_width(B, out, 1, kPairs);
     g.row_scale = xs; g.col_scale = ws; g.bias = bias; g.bias_bf16 = prec == P_BF16;
     mm_out(g, y, prec == P_BF16 && !y_f32, out);
-    return mm_launch_as<kForward, false, false, false>(Operand{xq, B, in, (size_t)pitch}, Operand{wq, out, in, (size_t)pitch}, g, in, in, s);
+    MmLaunch<kForward> mm;
+    return mm.add(Operand{xq, B, in, (size_t)pitch}, Operand{wq, out, in, (size_t)pitch}, g, in, in, true) ? mm.run<false>(s) : -1;
 }
 
 size_t fc8_workspace_bytes(int prec, int B, int in, int out) { return bwd_plan(prec, B, in, out).bytes; }
@@ -846,39 +924,43 @@ int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, co
                                     blocks_for(total)};
         join_blocks += join.job[joins - 1].blocks;
     };
-    auto product = [&](auto a_mn, const Operand &a, const Operand &b, int M, int K, int splits, size_t part, void *to, bool is_bf16) {
-        constexpr bool A_MN = decltype(a_mn)::value;
+    const bool dw_bf16 = !f32 && !dw_f32;
+    const bool together = dx && dW && mm_together(p.dx_way, p.dw_way), dw_first = together && p.dw_way.each > p.dx_way.each;
+    MmLaunch<kGrad> mm;
+    bool promote = false;
+    auto product = [&](bool a_mn, const Operand &a, const Operand &b, int M, int K, const MmWay &way, size_t part, void *to, bool is_bf16, bool last) {
         MmArgs g{};
-        g.M = M; g.N = in; g.splits = splits;
+        g.M = M; g.N = in; g.splits = way.splits; g.width = together ? way.width : mm_width(M, in, way.splits, kPairs); g.a_mn = a_mn;
         segments(g);
-        if (splits > 1) {
-            g.splits = splits;
-            mm_out(g, base + part, false, p.ld);
-            g.out_split = (size_t)M * p.ld;
-        } else {
-            mm_out(g, to, is_bf16, in);
-        }
+        if (g.splits > 1) mm_out(g, base + part, false, p.ld); else mm_out(g, to, is_bf16, in);
         const int most = is_bf16 ? kPieceOut : kPieceF32;
-        const int r = (long)K * g.n_seg / splits > most ? mm_launch_as<kGrad, A_MN, true, true>(a, b, g, K, most, s) : mm_launch_as<kGrad, A_MN, true, false>(a, b, g, K, most, s);
-        if (r > 0 && splits > 1) joined(g, part, to, is_bf16);
+        promote = promote || (long)K * g.n_seg / g.splits > most;
+        if (g.splits > 1) joined(g, part, to, is_bf16);
+        return mm.add(a, b, g, K, most, last);
+    };
+    auto run = [&]() {
+        const int r = promote ? mm.run<true>(s) : mm.run<false>(s);
+        mm = MmLaunch<kGrad>();
+        promote = false;
         return r;
     };
-    const bool dw_bf16 = !f32 && !dw_f32;
-    int r;
-    if (dx) {
-        if ((r = product(std::false_type{}, operand(0), Operand{base + p.w, out, in, (size_t)p.plane_in}, B, out, p.dx_splits, p.dx, dx, !f32)) < 0) return r;
+    for (int k = 0; k < 2; ++k) {
+        const bool of_x = (k == 0) != dw_first, last = k == 1 || !together;
+        if (!(of_x ? dx : dW)) continue;
+        if (!(of_x ? product(false, operand(0), Operand{base + p.w, out, in, (size_t)p.plane_in}, B, out, p.dx_way, p.dx, dx, !f32, last)
+                   : product(true, operand(1), Operand{base + p.x, B, in, (size_t)p.plane_in}, out, B, p.dw_way, p.dw, dW, dw_bf16, last)))
+            return -1;
+        if (!last) continue;
+        const int r = run();
+        if (r < 0) return r;
         n += r;
     }
-    if (dW) {
-        if ((r = product(std::true_type{}, operand(1), Operand{base + p.x, B, in, (size_t)p.plane_in}, out, B, p.dw_splits, p.dw, dW, dw_bf16)) < 0) return r;
-        n += r;
+    if (db && p.chunks > 1) {
+        join.sums = JoinSums{(const float *)(base + p.db), db, p.chunks, out};
+        join_blocks += (out + 31) / 32;
     }
     if (join_blocks) {
         launch_k(fc8_join_kernel, join_blocks, 256, 0, s, join);
-        ++n;
-    }
-    if (db && p.chunks > 1) {
-        launch_k(fc8_db_kernel, (out + 31) / 32, 256, 0, s, (const float *)(base + p.db), db, p.chunks, out);
         ++n;
     }
     return n;
