@@ -124,7 +124,7 @@ __device__ __forceinline__ void store_rows(void *out, uint32_t buf, int lane, in
         }
         __syncwarp();
         const int c = col + 32 * half + lane;
-#pragma unroll 4
+#pragma unroll 8
         for (int r = 0; r < last; ++r) {
             const size_t at = (size_t)(row0 + r) * n + c;
             if (BF16) {
