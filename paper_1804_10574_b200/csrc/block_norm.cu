@@ -455,7 +455,8 @@ struct NormRows {
 
 // The same for many wide rows: stretches of rows that share a gate are dealt out to resident blocks, the rows ahead on their
 // way through shared memory.
-template <typename T, int VEC, int ITER>
+// FULL: the block's threads have just the row's columns.
+template <typename T, int VEC, int ITER, bool FULL>
 __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __grid_constant__ BlockNormBwd g, const __grid_constant__ RingShape shape) {
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t full[kRingMostStages];
@@ -517,10 +518,10 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
             ring.next();
             F2 q0 = f2(0.f), q1 = f2(0.f), q2 = f2(0.f), dy[G], h[G], b[G], dh[G];
             auto load = [&](int i) {
-                slot_load<T, VEC>(slot_dy, phase, C, threads, i, dy);
-                slot_load<T, VEC>(slot_h, phase, C, threads, i, h);
-                slot_load<T, VEC>(slot_b, phase, C, threads, i, b);
-                if (g.dh) slot_load<T, VEC>(slot_dh, phase, C, threads, i, dh);
+                slot_load<T, VEC, FULL>(slot_dy, phase, C, threads, i, dy);
+                slot_load<T, VEC, FULL>(slot_h, phase, C, threads, i, h);
+                slot_load<T, VEC, FULL>(slot_b, phase, C, threads, i, b);
+                if (g.dh) slot_load<T, VEC, FULL>(slot_dh, phase, C, threads, i, dh);
             };
 #pragma unroll
             for (int i = 0; i < P / G; ++i) {
@@ -556,8 +557,8 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
                     b[j] = fma2(pg[k], f2(s1) * tt, f2(-c1) * x);
                     h[j] = alpha * tt;
                 }
-                group_store<T, VEC>((T *)g.dres + start, C, threads, i, h);
-                group_store<T, VEC>((T *)g.db + start, C, threads, i, b);
+                group_store<T, VEC, FULL>((T *)g.dres + start, C, threads, i, h);
+                group_store<T, VEC, FULL>((T *)g.db + start, C, threads, i, b);
             }
         }
         // The stretch's one sum times the gate is its share of dgamma_post; times gamma_post, dgate's.  With one gate for all rows
@@ -713,9 +714,9 @@ template <typename T, int VEC, bool SHIFT> int fwd_as(const BlockNormFwd &g, con
     return 1;
 }
 
-template <typename T, int VEC, int ITER> int bwd_ring(const BlockNormBwd &g, const BwdPlan &p, const Launch &s) {
+template <typename T, int VEC, int ITER, bool FULL> int bwd_ring(const BlockNormBwd &g, const BwdPlan &p, const Launch &s) {
     static thread_local int ready = -1;
-    if (!ring_ready(block_norm_bwd_ring_kernel<T, VEC, ITER>, ready)) return -1;
+    if (!ring_ready(block_norm_bwd_ring_kernel<T, VEC, ITER, FULL>, ready)) return -1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.blocks); cfg.blockDim = dim3(p.ring.threads); cfg.dynamicSmemBytes = p.ring.smem; cfg.stream = s.s;
     cudaLaunchAttribute attr[2];
@@ -726,7 +727,7 @@ template <typename T, int VEC, int ITER> int bwd_ring(const BlockNormBwd &g, con
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = s.pdl == 1 ? 2 : 1;
-    cudaLaunchKernelEx(&cfg, block_norm_bwd_ring_kernel<T, VEC, ITER>, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), block8_polls()));
+    cudaLaunchKernelEx(&cfg, block_norm_bwd_ring_kernel<T, VEC, ITER, FULL>, g, ring_shape(g.rows, g.C * (int)sizeof(T), 4, p.ring.smem - (g.several ? (size_t)g.C * 4 : 0), block8_polls()));
     return 1;
 }
 
@@ -739,7 +740,8 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scr
     auto go = [&](auto kernel) { launch_k(kernel, p.blocks, p.row.threads, smem, s, g); };
     if (p.ring.threads) {
         g.several = (long)g.gates * g.parts > p.blocks;  // (with one gate never: its stretches are no more than the blocks)
-        const int r = bwd_ring<T, VEC, VEC == 1 ? 8 : 2>(g, p, s);
+        constexpr int ITER = VEC == 1 ? 8 : 2;
+        const int r = VEC > 1 && p.ring.threads * VEC * ITER == g.C ? bwd_ring<T, VEC, ITER, (VEC > 1)>(g, p, s) : bwd_ring<T, VEC, ITER, false>(g, p, s);
         if (r < 0) return r;
     } else if (p.row.tpr == 32) {
         if (p.row.iter == 1) go(block_norm_bwd_kernel<T, VEC, 1, true>); else go(block_norm_bwd_kernel<T, VEC, 2, true>);

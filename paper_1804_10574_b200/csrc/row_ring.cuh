@@ -109,15 +109,16 @@ template <int TENSORS> struct RowRing {
 template <int VEC> constexpr int kGroup = VEC > 1 ? VEC / 2 : 1;  // pairs
 
 // Group i of a row in a slot.  Value c stands at phase + c * sizeof(T) (vectors: phase 0).
-template <typename T, int VEC> __device__ __forceinline__ void slot_load(uint32_t slot, int phase, int C, int threads, int i, F2 (&v)[kGroup<VEC>]) {
+// FULL: no thread's columns lie past the row.
+template <typename T, int VEC, bool FULL = false> __device__ __forceinline__ void slot_load(uint32_t slot, int phase, int C, int threads, int i, F2 (&v)[kGroup<VEC>]) {
     if constexpr (VEC > 1) {
         const int c = (i * threads + threadIdx.x) * VEC;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         const uint32_t from = slot + c * (uint32_t)sizeof(T);
         if constexpr (VEC * sizeof(T) == 16) {
-            if (c < C) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from));
+            if (FULL || c < C) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from));
         } else {
-            if (c < C) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from));
+            if (FULL || c < C) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from));
         }
 #pragma unroll
         for (int j = 0; j < VEC / 2; ++j) {
@@ -169,7 +170,7 @@ template <typename T, int VEC, int ITER> struct Share {
     }
 };
 // Group i to a row in memory, in the element type.
-template <typename T, int VEC> __device__ __forceinline__ void group_store(T *row, int C, int threads, int i, const F2 (&v)[kGroup<VEC>]) {
+template <typename T, int VEC, bool FULL = false> __device__ __forceinline__ void group_store(T *row, int C, int threads, int i, const F2 (&v)[kGroup<VEC>]) {
     if constexpr (VEC > 1) {
         const int c = (i * threads + threadIdx.x) * VEC;
         constexpr int W = VEC * sizeof(T) / 4;
@@ -179,7 +180,7 @@ template <typename T, int VEC> __device__ __forceinline__ void group_store(T *ro
             if constexpr (sizeof(T) == 2) w[j] = to_bf16_pair(v[j]);
             else w[j] = __float_as_uint(j % 2 ? parts(v[j / 2]).y : parts(v[j / 2]).x);
         }
-        if (c < C) {
+        if (FULL || c < C) {
             if constexpr (W == 4) *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
             else *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
         }
@@ -233,15 +234,18 @@ template <int N> __device__ __forceinline__ void ring_sum(float (&v)[N], int war
     }
     __syncthreads();
     // the warps' sums in index order, four at a time (those of warps that are not there are zeros)
+    F2 s[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = 0.f;
+    for (int k = 0; k < N; ++k) s[k] = f2(0.f);
     for (int w = 0; w < warps; w += 4) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const float4 q = *reinterpret_cast<const float4 *>(&to[k][w]);
-            v[k] += (q.x + q.y) + (q.z + q.w);
+            s[k] = (s[k] + f2(q.x, q.y)) + f2(q.z, q.w);
         }
     }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = sum2(s[k]);
 }
 // A sum and a maximum (of bits) in one round.
 __device__ __forceinline__ void ring_sum_max(float &sum, uint32_t &top, int warps, float (*red)[32], uint32_t &round) {
@@ -252,13 +256,14 @@ __device__ __forceinline__ void ring_sum_max(float &sum, uint32_t &top, int warp
     ++round;
     if (lane == 0) { to[0][warp] = sum; to[1][warp] = __uint_as_float(top); }
     __syncthreads();
-    sum = 0.f;
+    F2 s = f2(0.f);
     for (int w = 0; w < warps; w += 4) {
         const float4 q = *reinterpret_cast<const float4 *>(&to[0][w]);
-        sum += (q.x + q.y) + (q.z + q.w);
+        s = (s + f2(q.x, q.y)) + f2(q.z, q.w);  // as ring_sum does
         const uint4 m = *reinterpret_cast<const uint4 *>(&to[1][w]);
         top = max(max(top, max(m.x, m.y)), max(m.z, m.w));
     }
+    sum = sum2(s);
 }
 __device__ __forceinline__ uint32_t ring_max(uint32_t v, int warps, float (*red)[32], uint32_t &round) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
