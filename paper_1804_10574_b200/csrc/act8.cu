@@ -74,7 +74,8 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     __shared__ __align__(16) float red[6][32];
     __shared__ int flags[2];
     const int t = threadIdx.x, threads = blockDim.x;
-    RowRing<1> ring(shape, smem_u32(ring_smem), full, flags);
+    __shared__ const uint8_t *list[1];
+    RowRing<1> ring(shape, smem_u32(ring_smem), full, flags, list, {x});
     if (t == 0) ring.init();
     if (t < 32) {
 #pragma unroll
@@ -84,7 +85,6 @@ __global__ void __launch_bounds__(512, 1) act8_pack_ring_kernel(const T *__restr
     pdl_launch();
     pdl_wait();
     const int first = (int)((long)rows * blockIdx.x / gridDim.x), last = (int)((long)rows * (blockIdx.x + 1) / gridDim.x);
-    ring.sources({x});
     for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, -1);
     uint32_t round = 0;
     for (int row = first; row < last; ++row) {

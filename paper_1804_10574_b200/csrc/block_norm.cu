@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
     __shared__ __align__(16) float red[6][32];
     __shared__ int flags[2];
     const int threads = blockDim.x, t = threadIdx.x, C = g.C;
-    RowRing<2> ring(shape, smem_u32(ring_smem), full, flags);
+    __shared__ const uint8_t *list[2];
+    RowRing<2> ring(shape, smem_u32(ring_smem), full, flags, list, {g.b, g.res});
     if (t == 0) ring.init();
     if (t < 32) {
 #pragma unroll
@@ -160,7 +161,6 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
     pdl_launch();
     pdl_wait();
     const int first = (int)((long)g.rows * blockIdx.x / gridDim.x), last = (int)((long)g.rows * (blockIdx.x + 1) / gridDim.x);
-    ring.sources({g.b, g.res});
     for (int row = first; row < min(first + shape.stages, last); ++row) ring.copy(row, -1);
     constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
     typedef Share<T, VEC, ITER> Row;
@@ -467,7 +467,8 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     float *const a_post = g.several ? reinterpret_cast<float *>(ring_smem + (size_t)shape.stages * 4 * shape.slot_bytes) : nullptr;
     if (a_post)
         for (int c = t; c < C; c += blockDim.x) a_post[c] = 0.f;  // (a barrier follows)
-    RowRing<4> ring(shape, smem_u32(ring_smem), full, flags);
+    __shared__ const uint8_t *list[4];
+    RowRing<4> ring(shape, smem_u32(ring_smem), full, flags, list, {g.dy, g.h, g.b, g.dh});
     if (t == 0) ring.init();
     if (t < 32) {
 #pragma unroll
@@ -476,7 +477,6 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     __syncthreads();
     pdl_launch();
     pdl_wait();
-    ring.sources({g.dy, g.h, g.b, g.dh});
     NormRows ahead(g);
     for (int i = 0; i < shape.stages && ahead.more(); ++i, ahead.next()) ring.copy(ahead.row, -1);
     constexpr int P = VEC * ITER / 2, G = kGroup<VEC>;  // pairs of a thread, of a group
