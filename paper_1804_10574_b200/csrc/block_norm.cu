@@ -16,7 +16,7 @@
 // each of its warps some hundred cycles, so that few warps a row and two to eight rows at a time on an SM are faster than a row per
 // SM, and arithmetic on pairs (f32x2.cuh) takes half the instructions.  Fewer rows, and rows that one warp holds, stay in
 // registers.  Measured (bf16): 8192 x 4096 forward 48.7 us (5.5 TB/s), to codes 43.6 us (5.4 TB/s), backward with the folding
-// kernel 80.7 us (5.0 TB/s); with a row in registers 87, 104 and 146 us.  8192 x 1021: 25, 29 and 49 us; 30000 x 256: 13, 14 and
+// kernel 75.8 us (5.3 TB/s); with a row in registers 87, 104 and 146 us.  8192 x 1021: 25, 29 and 49 us; 30000 x 256: 13, 14 and
 // 26 us.
 #include <algorithm>
 
@@ -455,7 +455,7 @@ struct NormRows {
 
 // The same for many wide rows: stretches of rows that share a gate are dealt out to resident blocks, the rows ahead on their
 // way through shared memory.
-// FULL: the block's threads have just the row's columns.
+// FULL: the block's threads have just the row's columns: no masks (8192 x 8192 148 us, 155 with them).
 template <typename T, int VEC, int ITER, bool FULL>
 __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __grid_constant__ BlockNormBwd g, const __grid_constant__ RingShape shape) {
     extern __shared__ __align__(16) uint8_t ring_smem[];

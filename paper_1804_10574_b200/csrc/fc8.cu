@@ -829,8 +829,9 @@ BwdPlan bwd_plan(int prec, int B, int in, int out) {
     return p;
 }
 
-// us of the gradients in one launch / in three or four, on the device and with the host: 128 x 128 x 128 bf16 6.4 / 11.6 and
-// 10.5 / 20.6, fp32 4.9 / 14.1; 128 x 1024 x 128 9.0 / 13.2; 256 x 256 x 256 bf16 14.5 / 13.2.
+// us of the gradients in one launch / in two or three, recorded and by calls (which wait for the host): 128 x 128 x 128 bf16 6.3 /
+// 6.8 and 9.9 / 16, fp32 5.2 / 8.0 and 8.0 / 11.9; 128 x 512 x 128 fp32 9.0 / 8.0 and 8.0 / 11.8; 128 x 1024 x 128 bf16 11.1 /
+// 6.9 and 11.2 / 16; 256 x 256 x 256 bf16 14.5 / 7.7 and 14.5 / 12.
 bool small_fit(int B, int in, int out) {
     return B <= kSmallMost && out <= kSmallMost && in <= kSmallMostIn;
 }
