@@ -202,6 +202,21 @@ def test_fc8_backward(binding, shape, prec):
 
 @gpu
 @PREC
+@pytest.mark.parametrize("shape", [(3000, 300, 200), (200, 300, 3000), (2600, 8200, 2604), (5000, 4100, 2300)], ids=ids)
+def test_fc8_gradients_that_share_a_launch(binding, shape, prec):
+    """Either product the longer one, their K ranges split or not; so many tiles that each has a launch of its own; both results
+    the same bits as alone."""
+    for dw_f32 in (False, True):
+        c = Fc(*shape, prec, seed=8)
+        full = c.bwd(binding, dw_f32=dw_f32)
+        for got, (ref, tol), what in zip(full, c.grads_ref(E if dw_f32 else None), ("dx", "dW", "db")):
+            within(got, ref, tol, what)
+        for k, want in enumerate("xw"):
+            assert torch.equal(c.bwd(binding, want, dw_f32)[k], full[k]), want
+
+
+@gpu
+@PREC
 @pytest.mark.parametrize("shape", [(1, 64, 100), (45, 136, 1000), (300, 136, 777), (140, 2000, 90)], ids=ids)
 def test_fc8_gradients_asked_for_alone(binding, shape, prec):
     """The same bits whichever are asked for, and again."""
