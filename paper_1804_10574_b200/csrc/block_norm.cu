@@ -15,7 +15,7 @@
 // From 296 rows on resident blocks walk the rows, which come through shared memory (row_ring.cuh): a row's reductions cost
 // each of its warps some hundred cycles, so that few warps a row and two to eight rows at a time on an SM are faster than a row per
 // SM, and arithmetic on pairs (f32x2.cuh) takes half the instructions.  Fewer rows, and rows that one warp holds, stay in
-// registers.  Measured (bf16): 8192 x 4096 forward 48.7 us (5.5 TB/s), to codes 43.6 us (5.4 TB/s), backward with the folding
+// registers.  Measured (bf16): 8192 x 4096 forward 49.0 us (5.5 TB/s), to codes 43.6 us (5.4 TB/s), backward with the folding
 // kernel 75.8 us (5.3 TB/s); with a row in registers 87, 104 and 146 us.  8192 x 1021: 25, 29 and 49 us; 30000 x 256: 13, 14 and
 // 26 us.
 #include <algorithm>
@@ -143,7 +143,9 @@ struct BlockNormFwd {
 };
 
 // The same for many rows: resident blocks walk stretches of them, the rows ahead on their way through shared memory.
-template <typename T, int VEC, int ITER, bool CODES>
+// FULL: the block's threads have just the row's columns: no masks (8192 x 8192 95.5 us, 99.0 with them; to codes 8192 x 6144 72,
+// 60 with them, for want of registers: not there).
+template <typename T, int VEC, int ITER, bool CODES, bool FULL>
 __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __grid_constant__ BlockNormFwd g, const __grid_constant__ RingShape shape) {
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t full[kRingMostStages];
@@ -196,7 +198,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 in[G];
-            slot_load<T, VEC>(slot_b, phase, C, threads, i, in);
+            slot_load<T, VEC, FULL>(slot_b, phase, C, threads, i, in);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 v[i * G + j] = in[j];
@@ -212,7 +214,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < P / G; ++i) {
             F2 res[G];
-            slot_load<T, VEC>(slot_res, phase, C, threads, i, res);
+            slot_load<T, VEC, FULL>(slot_res, phase, C, threads, i, res);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 const int k = i * G + j;
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
                     top = max(top, max(__float_as_uint(p.x) & 0x7fffffffu, __float_as_uint(p.y) & 0x7fffffffu));
                 }
             }
-            group_store<T, VEC>((T *)g.h + start, C, threads, i, res);
+            group_store<T, VEC, FULL>((T *)g.h + start, C, threads, i, res);
         }
         sum[0] = sum2(s2);
         if (CODES) ring_sum_max(sum[0], top, threads >> 5, red, round);
@@ -236,7 +238,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_fwd_ring_kernel(const __gri
         }
 #pragma unroll
         for (int k = 0; k < P; ++k) v[k] = v[k] * f2(r2);
-        if (g.y) share_store<T, VEC, ITER>((T *)g.y + start, C, threads, v);
+        if (g.y) share_store<T, VEC, ITER, FULL>((T *)g.y + start, C, threads, v);
         if (!CODES) continue;
         // the largest |y| is the largest |h gamma_pre| times rstd_pre: known with the sum
         float s;
@@ -690,12 +692,15 @@ size_t bwd_scratch(const BwdPlan &p, int rows, int C, int span) {
     return ((size_t)p.blocks * 2 + (p.parts > 1 ? (size_t)((rows - 1) / span + 1) * p.parts : 0)) * C;
 }
 
-template <typename T, int VEC, int ITER> int fwd_ring(const BlockNormFwd &g, const RingPlan &p, const Launch &s) {
+template <typename T, int VEC, int ITER, bool FULL> int fwd_ring_as(const BlockNormFwd &g, const RingPlan &p, const Launch &s) {
     static thread_local int ready[2] = {-1, -1};
-    auto kernel = g.q ? block_norm_fwd_ring_kernel<T, VEC, ITER, true> : block_norm_fwd_ring_kernel<T, VEC, ITER, false>;
+    auto kernel = g.q ? block_norm_fwd_ring_kernel<T, VEC, ITER, true, false> : block_norm_fwd_ring_kernel<T, VEC, ITER, false, FULL>;
     if (!ring_ready(kernel, ready[g.q != nullptr])) return -1;
     launch_k(kernel, std::min(g.rows, 148 * p.per_sm), p.threads, p.smem, s, g, ring_shape(g.rows, g.C * (int)sizeof(T), 2, p.smem, block8_polls()));
     return 1;
+}
+template <typename T, int VEC, int ITER> int fwd_ring(const BlockNormFwd &g, const RingPlan &p, const Launch &s) {
+    return VEC > 1 && !g.q && p.threads * VEC * ITER == g.C ? fwd_ring_as<T, VEC, ITER, (VEC > 1)>(g, p, s) : fwd_ring_as<T, VEC, ITER, false>(g, p, s);
 }
 template <typename T, int VEC, bool SHIFT> int fwd_as(const BlockNormFwd &g, const Launch &s) {
     const RmsPlan p = rms_plan(rms_nvec(g.C, VEC, SHIFT), VEC > 1, 4, 128);

@@ -203,14 +203,14 @@ template <typename T, int VEC, bool FULL = false> __device__ __forceinline__ voi
         if (d < C) row[d] = from_f<T>(p.y);
     }
 }
-template <typename T, int VEC, int ITER> __device__ __forceinline__ void share_store(T *row, int C, int threads, const F2 (&v)[VEC * ITER / 2]) {
+template <typename T, int VEC, int ITER, bool FULL = false> __device__ __forceinline__ void share_store(T *row, int C, int threads, const F2 (&v)[VEC * ITER / 2]) {
     constexpr int G = kGroup<VEC>;
 #pragma unroll
     for (int i = 0; i < VEC * ITER / 2 / G; ++i) {
         F2 g[G];
 #pragma unroll
         for (int j = 0; j < G; ++j) g[j] = v[i * G + j];
-        group_store<T, VEC>(row, C, threads, i, g);
+        group_store<T, VEC, FULL>(row, C, threads, i, g);
     }
 }
 // The same as fp32; the row starts on a 16-byte boundary (VEC > 1).
