@@ -652,9 +652,11 @@ template <typename T> __global__ void __launch_bounds__(1024) block_norm_fold_ke
 // Whether the rows go through shared memory: 16 (backward) or 32 values of a row per thread.
 RingPlan norm_ring(int rows, int C, int vec, int es, bool backward) {
     // narrow rows are a warp's of the other kernel
-    if (rows < 2 * 148 || ring_threads((C + vec - 1) / vec, vec == 1 ? 8 : (backward ? 2 : 4)) < 64) return RingPlan{};
-    if (!backward) return ring_plan(C, C * es, vec, vec == 1 ? 8 : 4, 2, 0);
-    return ring_plan(C, C * es, vec, vec == 1 ? 8 : 2, 4, (size_t)C * 4);
+    int iter = vec == 1 ? 8 : (backward ? 2 : 4);
+    // backward, rows of 49 to 64 vectors: one per thread (100000 x 512: 141 us, 162 with two in a warp's registers; x 384: alike)
+    if (backward && vec > 1 && C / vec > 48 && C / vec <= 64) iter = 1;
+    if (rows < 2 * 148 || ring_threads((C + vec - 1) / vec, iter) < 64) return RingPlan{};
+    return ring_plan(C, C * es, vec, iter, backward ? 4 : 2, backward ? (size_t)C * 4 : 0);
 }
 
 // How the rows of a backward pass are dealt out: `blocks` of the launch, stretches per gate, a block or a warp a stretch.
@@ -677,8 +679,7 @@ BwdPlan bwd_plan(int rows, int C, int span, int vec, int es, bool ring) {
         best = (double)((gates - 1) / (most * 8) + 1) * (longest + 1);
     }
     const int even = std::max(1, most / gates);
-    for (int n : {1, even, even + 1, 2 * even}) {
-        if (n > longest) continue;
+    for (int n : {1, std::min(even, longest), std::min(even + 1, longest), std::min(2 * even, longest)}) {
         const int len = (longest - 1) / n + 1, steps = warp ? (len - 1) / 8 + 1 : len;
         const double t = (double)(((long)gates * n - 1) / most + 1) * (steps + 1);
         if (t < best) { best = t; p.parts = n; p.per_block = 1; }
@@ -745,8 +746,11 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scr
     auto go = [&](auto kernel) { launch_k(kernel, p.blocks, p.row.threads, smem, s, g); };
     if (p.ring.threads) {
         g.several = (long)g.gates * g.parts > p.blocks;  // (with one gate never: its stretches are no more than the blocks)
-        constexpr int ITER = VEC == 1 ? 8 : 2;
-        const int r = VEC > 1 && p.ring.threads * VEC * ITER == g.C ? bwd_ring<T, VEC, ITER, (VEC > 1)>(g, p, s) : bwd_ring<T, VEC, ITER, false>(g, p, s);
+        constexpr int ITER = VEC == 1 ? 8 : 2, SHORT = VEC == 1 ? 8 : 1;
+        const bool fills = VEC > 1 && p.ring.threads * VEC * p.ring.iter == g.C;
+        int r;
+        if (p.ring.iter == ITER) r = fills ? bwd_ring<T, VEC, ITER, (VEC > 1)>(g, p, s) : bwd_ring<T, VEC, ITER, false>(g, p, s);
+        else r = fills ? bwd_ring<T, VEC, SHORT, (VEC > 1)>(g, p, s) : bwd_ring<T, VEC, SHORT, false>(g, p, s);
         if (r < 0) return r;
     } else if (p.row.tpr == 32) {
         if (p.row.iter == 1) go(block_norm_bwd_kernel<T, VEC, 1, true>); else go(block_norm_bwd_kernel<T, VEC, 2, true>);

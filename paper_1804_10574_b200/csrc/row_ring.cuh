@@ -299,13 +299,14 @@ inline int ring_threads(int nvec, int iter) { return ((nvec + iter - 1) / iter +
 inline size_t ring_smem_of(int per_sm) { return (size_t)(226 * 1024 / per_sm - 2048) / 16 * 16; }
 // Blocks of an SM for rows of `threads` threads, and the shared memory of each; `extra` bytes of it are not the ring's.  Two
 // stages at least, else 0 blocks.
-struct RingPlan { int threads, per_sm; size_t smem; };
+struct RingPlan { int threads, per_sm; size_t smem; int iter; };
 inline RingShape ring_shape(int rows, int row_bytes, int tensors, size_t smem, unsigned polls);
 // `registers` of a thread and `more` threads of a block besides the row's limit the blocks too.
 inline RingPlan ring_plan(int C, int row_bytes, int vec, int iter, int tensors, size_t extra, int registers = 128, int more = 0) {
     RingPlan p{};
     const int threads = std::max(64, ring_threads((C + vec - 1) / vec, iter));
     if (threads > 512) return p;
+    p.iter = iter;
     p.per_sm = std::min(8, 65536 / (registers * (threads + more)));
     while (p.per_sm > 1 && ring_shape(1, row_bytes, tensors, ring_smem_of(p.per_sm) - extra, 0).stages < 2) --p.per_sm;
     p.smem = ring_smem_of(p.per_sm);
