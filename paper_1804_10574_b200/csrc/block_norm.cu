@@ -512,7 +512,9 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
         float next1 = 0.f, next2 = 0.f;
         if (r0 < r1) { next1 = g.rstd_post[r0]; next2 = g.rstd_pre[r0]; }
         for (int row = r0; row < r1; ++row) {
-            const float s1 = next1, s2 = ring.wait<T, VEC>(row) ? next2 : __int_as_float(0x7fffffff);  // a row that did not come is NaN
+            const float s1 = next1;
+            float s2 = next2;
+            ring.wait<T, VEC>(row);
             if (row + 1 < r1) { next1 = g.rstd_post[row + 1]; next2 = g.rstd_pre[row + 1]; }  // a row ahead
             const uint32_t slot_dy = ring.slot(0), slot_h = ring.slot(1), slot_b = ring.slot(2), slot_dh = ring.slot(3);
             const int phase = ring_phase(shape, row);
@@ -539,6 +541,7 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
             }
             float sum[3] = {sum2(q0), sum2(q1), sum2(q2)};
             ring_sum<3>(sum, threads >> 5, red, round);
+            if (ring.lost_by(row)) s2 = __int_as_float(0x7fffffff);  // a row that did not come, to any thread, is NaN: all that follows has s2 in it
             if (begun && ahead.more()) {
                 ring.copy(ahead.row, row);
                 ahead.next();

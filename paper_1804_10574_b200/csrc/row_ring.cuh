@@ -66,7 +66,7 @@ template <int TENSORS> struct RowRing {
     // that a stage gets all of its copies or none, and the first thread knows what is on the way.
     __device__ __forceinline__ void copy(int row, int now) {
         const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
-        if ((threadIdx.x & 31) == 0 && warp < TENSORS && *(volatile int *)lost_at > now) {
+        if ((threadIdx.x & 31) == 0 && warp < TENSORS && !lost_by(now)) {
             const size_t at = (size_t)row * g.row_bytes, from = at & ~(size_t)15, to = min((at + g.row_bytes + 15) & ~(size_t)15, g.floor16);
             const uint32_t bytes = to > from ? (uint32_t)(to - from) : 0u, bar = smem_u32(&full[head]);
             // (what lands before the barrier expects it is counted all the same: its phase ends with this arrival)
@@ -112,6 +112,9 @@ template <int TENSORS> struct RowRing {
         }
         return !lost;
     }
+    // Whether any thread's wait for this row or one before ran out.  Behind a barrier that follows the wait for the row all threads
+    // get the same answer: what a faster one's wait for the next row may add is a later row.
+    __device__ __forceinline__ bool lost_by(int row) const { return *(volatile int *)lost_at <= row; }
     __device__ __forceinline__ uint32_t slot(int tensor) const { return base + (stage * TENSORS + tensor) * g.slot_bytes; }
     __device__ __forceinline__ void next() { if (++stage == (uint32_t)g.stages) { stage = 0; parity ^= 1u; } }
 };

@@ -836,6 +836,42 @@ def test_rows_through_shared_memory_whose_waits_run_out(binding, rows, C, prec):
     assert all(torch.equal(a, b) for a, b in zip(step(), ref))
 
 
+@gpu
+@PREC
+@pytest.mark.parametrize("rows,C,span", [(320, 1021, 320), (3000, 640, 7), (900, 4096, 1), (8192, 4096, 8192)])
+def test_rows_through_shared_memory_whose_waits_run_out_in_some_threads(binding, rows, C, span, prec):
+    """With limits of a few polls a row may have come for some threads of its block and not for others, most of all while other
+    work keeps the memory busy: every value is NaN or the usual bits, sums included, and a row is NaN as a whole."""
+    c = Norm(rows, C, prec, span, seed=56).reference()
+    h, r1, r2 = c.h.to(DT[prec]), c.r1[:, 0].float(), c.r2[:, 0].float()
+    side, busy = torch.cuda.Stream(), torch.empty(2, 1 << 30, dtype=torch.uint8, device="cuda")
+
+    def step():
+        to_codes = c.fwd(binding, False, True)
+        return list(c.bwd(binding, h, r1, r2)) + list(c.fwd(binding, True, False)[:2]) + [to_codes[0], to_codes[3], pack(binding, c.b, prec)[1]]
+
+    ref = step()
+    try:
+        for polls in (1,) * 40 + (2, 3, 4, 8):
+            binding.debug_block8_wait_polls(polls)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                busy[0].copy_(busy[1])
+                busy[1].copy_(busy[0])
+            got = step()
+            torch.cuda.synchronize()
+            for k, (a, b) in enumerate(zip(got, ref)):
+                lost = torch.isnan(a)
+                assert torch.equal(torch.where(lost, b, a), b), (polls, k)
+                if k in (0, 1, 5, 6, 7):  # db, dres, h, y, h
+                    assert torch.equal(lost.all(1), lost.any(1)), (polls, k)
+            # a block that lost a row has a share in the sums over all rows
+            assert not torch.isnan(got[0]).any() or (torch.isnan(got[3]).all() and torch.isnan(got[4]).all()), polls
+    finally:
+        binding.debug_block8_wait_polls(-1)
+    assert all(torch.equal(a, b) for a, b in zip(step(), ref))
+
+
 # ---- long sums, large tensors ---------------------------------------------------------------------------------------
 @gpu
 def test_fc8_weight_gradient_of_many_rows_keeps_its_precision(binding):
