@@ -647,6 +647,30 @@ def test_block_norm_recorded_and_at_once(binding, prec):
         assert all(torch.equal(p, q) for p, q in zip(out, refs[1]))
 
 
+@gpu
+def test_block_norm_more_gates_than_a_grid_has_rows(binding):
+    """65600 rows of the gate, each gate's rows worked in two stretches (so many gates are almost a whole number of rounds of the
+    resident blocks, so that halves end sooner), in place: the rows repeat after ten gates, so that the results do too."""
+    C, span, times = 65, 90, 6560
+    c = Norm(10 * span, C, 1, span, seed=57).reference()
+    h, r1, r2 = c.h.to(torch.bfloat16), c.r1[:, 0].float(), c.r2[:, 0].float()
+    refs = c.grads_ref(h, r1, r2)
+    rows = c.rows * times
+    dy, dh, b, h, gate = (t.repeat(times, 1) for t in (c.dy, c.dh, c.b, h, c.gate))
+    r1, r2 = r1.repeat(times), r2.repeat(times)
+    dg, dpost, dpre, scratch = f32(10 * times, C), f32(C), f32(C), f32(binding.block_norm_scratch_elems(rows, C, span), fill=NAN)
+    binding.block_norm_bwd(1, dy, dh, b, h, gate, c.post, c.pre, r1, r2, dh, dy, dg, dpost, dpre, scratch, rows, C, span, ALPHA)
+    for got, (ref, tol), what in zip((dh, dy, dg), refs, ("db", "dres", "dgate")):
+        for k in (0, 1, times // 2, times - 2, times - 1):
+            n = ref.shape[0]
+            within(got[k * n:(k + 1) * n], ref, tol, what)
+        assert torch.equal(got.view(times, -1), got[: ref.shape[0]].reshape(1, -1).expand(times, -1)), what
+    for got, (ref, tol), what in zip((dpost, dpre), refs[3:], ("dgamma_post", "dgamma_pre")):
+        # chains of additions: of the rows of a block (all SMs have one at least), of the blocks' sums
+        mass = tol / ((c.rows + 64) * E)
+        within(got, times * ref, (rows / 148 + 2 * span + 2048 + 54) * E * times * mass, what)
+
+
 # ---- together -------------------------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("prec,rows,D,F,span", [(1, 300, 264, 520, 100), (0, 130, 72, 257, 130), (1, 24, 1024, 4096, 1)])
