@@ -39,6 +39,7 @@ constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBuf + 1024;
 static_assert(kSmem + 1536 <= 227 * 1024, "with the barriers and the epilogue's columns");
 constexpr int kMostPlanes = 3;
 constexpr int kPieceF32 = 1024, kPieceOut = 65536;  // K values of a chain: 32-bit results, bf16 results
+constexpr int kWhole = 1 << 30;                  // a chain that is not cut
 constexpr int kSmallMost = 128, kSmallMostIn = 1024;  // rows and outputs, inputs of layers whose gradients are one launch
 constexpr int kPairs = 74;                       // CTA pairs of the GPU: the splits of a plan (and with them the workspace) go by this number
 
@@ -937,9 +938,10 @@ int launch_fc8_bwd(int prec, const void *dy, const void *xq, const float *xs, co
         segments(g);
         if (g.splits > 1) mm_out(g, base + part, false, p.ld); else mm_out(g, to, is_bf16, in);
         const int most = is_bf16 ? kPieceOut : kPieceF32;
-        promote = promote || (long)K * g.n_seg / g.splits > most;
+        const bool cut = (long)K * g.n_seg / g.splits > most;  // by the product's own sizes, whatever it shares the launch with
+        promote = promote || cut;
         if (g.splits > 1) joined(g, part, to, is_bf16);
-        return mm.add(a, b, g, K, most, last);
+        return mm.add(a, b, g, K, cut ? most : kWhole, last);
     };
     auto run = [&]() {
         const int r = promote ? mm.run<true>(s) : mm.run<false>(s);

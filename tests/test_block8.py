@@ -216,6 +216,18 @@ def test_fc8_gradients_that_share_a_launch(binding, shape, prec):
 
 
 @gpu
+@pytest.mark.parametrize("shape", [(289, 896, 363), (483, 962, 2782), (300, 1024, 4096), (2782, 962, 483), (1400, 520, 340)], ids=ids)
+def test_fc8_gradients_whose_chains_are_cut_in_one_product_only(binding, shape):
+    """fp32: chains of one product end within the limit, those of the other are cut; the bits are those of each alone."""
+    c = Fc(*shape, 0, seed=58)
+    full = c.bwd(binding)
+    for got, (ref, tol), what in zip(full, c.grads_ref(E), ("dx", "dW", "db")):
+        within(got, ref, tol, what)
+    for k, want in enumerate("xw"):
+        assert torch.equal(c.bwd(binding, want)[k], full[k]), want
+
+
+@gpu
 @PREC
 @pytest.mark.parametrize("shape", [(1, 64, 100), (45, 136, 1000), (300, 136, 777), (140, 2000, 90)], ids=ids)
 def test_fc8_gradients_asked_for_alone(binding, shape, prec):
