@@ -487,8 +487,8 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
  * most 2^30) rows of C <= 16384 values:
  *   rstd_post = 1 / sqrt(mean(b^2) + eps);  h = alpha res + gate b rstd_post gamma_post
  *   rstd_pre = 1 / sqrt(mean(h^2) + eps);   y = h rstd_pre gamma_pre
- * b, res, gamma_post [C], gamma_pre [C], h, y in the element type; gate (nullable = 1) [ceil(rows / span)][C], row n takes
- * its row n / span: span = rows for one gate vector, the rows of a sample for a gate per sample, 1 for a gate per row.
+ * b, res, gamma_post [C], gamma_pre [C], h, y in the element type; gate (nullable = 1, whatever the span) [ceil(rows / span)][C], row n
+ * takes its row n / span: span = rows for one gate vector, the rows of a sample for a gate per sample, 1 for a gate per row.
  * y and / or q with qscale (rows of codes, as ddg_act8_pack lays them out) are given; both are taken from the unrounded h.
  * rstd_post, rstd_pre (nullable) fp32 [rows].  h may be b or res, y too if it is another tensor than h. */
 ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, const void *gate, const void *gamma_post,

@@ -784,10 +784,11 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scr
 
 size_t block_norm_scratch_elems(int rows, int C, int span) {
     size_t most = 0;
-    for (int vec : {1, 4, 8})
-        for (int es : {2, 4})
-            for (bool ring : {false, true})
-                if (C % vec == 0) most = std::max(most, bwd_scratch(bwd_plan(rows, C, span, vec, es, ring), rows, C, span));
+    for (int of : {span, rows})  // with a gate, without
+        for (int vec : {1, 4, 8})
+            for (int es : {2, 4})
+                for (bool ring : {false, true})
+                    if (C % vec == 0) most = std::max(most, bwd_scratch(bwd_plan(rows, C, of, vec, es, ring), rows, C, of));
     return most;
 }
 
@@ -812,6 +813,7 @@ int launch_block_norm_fwd(int prec, const void *b, const void *res, const void *
 int launch_block_norm_bwd(int prec, const void *dy, const void *dh, const void *b, const void *h, const void *gate, const void *post, const void *pre,
                           const float *rstd_post, const float *rstd_pre, void *db, void *dres, float *dgate, float *dpost, float *dpre, float *scratch, int rows, int C,
                           int span, float alpha, Launch s) {
+    if (!gate) span = rows;  // no gate is one gate for all rows
     const int vec = prec == P_BF16 ? 8 : 4;
     bool v = C % vec == 0;
     for (const void *p : {dy, dh, b, h, gate, post, pre, (const void *)db, (const void *)dres, (const void *)dgate, (const void *)scratch}) v = v && vec_ok(p);

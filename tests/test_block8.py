@@ -683,6 +683,19 @@ def test_block_norm_more_gates_than_a_grid_has_rows(binding):
         within(got, times * ref, (rows / 148 + 2 * span + 2048 + 54) * E * times * mass, what)
 
 
+@gpu
+@PREC
+@pytest.mark.parametrize("rows,C", [(20, 264), (700, 1021), (900, 4096)])
+def test_block_norm_without_a_gate_does_not_depend_on_span(binding, rows, C, prec):
+    got = []
+    for span in (rows, 1, 7, 2 * rows):
+        c = Norm(rows, C, prec, span, False, seed=59).reference()
+        h, r1, r2 = c.h.to(DT[prec]), c.r1[:, 0].float(), c.r2[:, 0].float()
+        got.append(c.fwd(binding, True, True)[:4] + tuple(t for t in c.bwd(binding, h, r1, r2) if t is not None))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
 # ---- together -------------------------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("prec,rows,D,F,span", [(1, 300, 264, 520, 100), (0, 130, 72, 257, 130), (1, 24, 1024, 4096, 1)])
