@@ -107,10 +107,15 @@ __device__ __forceinline__ void mm_range(const MmArgs &g, int split, int &i0, in
 }
 __device__ __forceinline__ int mm_piece_end(const MmArgs &g, int i, int i1) { return min(i + g.piece - (int)((unsigned)i % (unsigned)g.piece), i1); }
 
+// The scale of a row of x as a factor `by` and a power of two `up`: a sum of codes (at most 2^31) times by is finite, and so is what
+// comes after it where y is.  Scales up to 2^64, all but those of rows past 10^21, are by themselves.
+struct RowScale { float by, up; };
+__device__ __forceinline__ RowScale row_scale_of(float s) { return s > 0x1p64f ? RowScale{s * 0x1p-64f, 0x1p64f} : RowScale{s, 1.f}; }
+
 // 64 columns of the warp's 32 rows, v: sums as they stand in tensor memory, at columns col .. of row `row`.
 // s0, s1 and b0, b1: scale and bias of the columns, a lane each; s_col: 32 floats of the warp's own.
 template <int MODE>
-__device__ __forceinline__ void mm_finish(const MmArgs &g, const CUtensorMap *map_out, uint32_t buf, float *v, int split, int row, int col, int lane, float row_scale,
+__device__ __forceinline__ void mm_finish(const MmArgs &g, const CUtensorMap *map_out, uint32_t buf, float *v, int split, int row, int col, int lane, const RowScale &rs,
                                           float *s_col, float s0, float s1, float b0, float b1) {
     if (MODE == kForward) {
         auto spread = [&](float of_lane, auto each) {  // a register of each lane's to all rows, 32 columns
@@ -125,7 +130,11 @@ __device__ __forceinline__ void mm_finish(const MmArgs &g, const CUtensorMap *ma
         };
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            spread(q ? s1 : s0, [&](int j, float t) { v[32 * q + j] = (float)__float_as_int(v[32 * q + j]) * row_scale * t; });
+            spread(q ? s1 : s0, [&](int j, float t) { v[32 * q + j] = (float)__float_as_int(v[32 * q + j]) * rs.by * t; });
+            if (__any_sync(0xffffffffu, rs.up != 1.f)) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[32 * q + j] *= rs.up;
+            }
             if (g.bias) spread(q ? b1 : b0, [&](int j, float t) { v[32 * q + j] += t; });
         }
     }
@@ -315,9 +324,10 @@ mm_kernel(const __grid_constant__ MmMaps<jobs_of(MODE)> maps, const __grid_const
                 pieces = 0;
                 for (int i = i0; i < i1; i = mm_piece_end(g, i, i1)) ++pieces;
             }
-            float cs[4] = {}, cb[4] = {}, rs = 0.f;  // loaded while the products run
+            float cs[4] = {}, cb[4] = {};  // loaded while the products run
+            RowScale rs{0.f, 1.f};
             if (MODE == kForward) {
-                rs = row < g.M ? g.row_scale[row] : 0.f;
+                rs = row_scale_of(row < g.M ? g.row_scale[row] : 0.f);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = min(col0 + 32 * q + lane, g.N - 1);

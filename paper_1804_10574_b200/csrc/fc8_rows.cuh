@@ -166,7 +166,11 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsPerSm) fc8_rows_kernel(cons
             asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(f) : "r"(map_rank(smem_u32(&abort_flag), r)));
             failed |= f;
         }
-        auto result = [&](int acc, int j, float cs, float bias) { return failed ? lost : (float)acc * s_scale[j] * cs + bias; };
+        auto result = [&](int acc, int j, float cs, float bias) {
+            const RowScale rs = row_scale_of(s_scale[j]);
+            const float most = 3.402823466e38f, up = cs * rs.up;  // (past that only a sum of zero is finite)
+            return failed ? lost : (float)acc * rs.by * (up > most ? most : up) + bias;
+        };
         if (g.vec) {
             const int o = o0 + 4 * (threadIdx.x % 32);  // 192 threads are whole rows of 32 groups
             float cs[4] = {}, bias[4] = {};

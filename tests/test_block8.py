@@ -261,6 +261,21 @@ def test_fc8_largest_sums(binding, shape, prec):
 
 @gpu
 @PREC
+@pytest.mark.parametrize("shape", [(3, 4096, 100), (300, 2048, 260), (40, 1000, 33)], ids=ids)
+def test_fc8_scales_of_unlike_size(binding, shape, prec):
+    """Rows of x near the type's largest values and small weights, and the other way round: the products are of ordinary size."""
+    for s, bias in ((2.0 ** 117, False), (2.0 ** -117, True), (2.0 ** 90, True)):
+        c = Fc(*shape, prec, bias, seed=60)
+        c.xq[0, : c.D] = 127
+        c.wq[:2, : c.D] = 127
+        c.xs *= s
+        c.ws /= s
+        y, tol = c.y_ref(U[DT[prec]])
+        within(c.fwd(binding), y, tol, "y")
+
+
+@gpu
+@PREC
 def test_fc8_does_not_read_behind_a_rows_codes(binding, prec):
     """Whatever stands in the bytes that fill a row up."""
     for shape in ((1, 1001, 300), (40, 71, 130), (300, 521, 270)):
