@@ -474,7 +474,8 @@ ddg_status ddg_fc8_fwd(int precision, const void *xq, const float *xscale, const
                        const void *bias, void *y, int B, int in, int out, int y_f32, void *stream);
 /* Its gradients, the rounding to codes taken as the identity, from the codes that were kept:
  *   dx = dy W^ [B][in];  dW = dy^T x^ [out][in];  db = sum_n dy_n [out] fp32; each nullable, one at least is given,
- * W^ and x^ being what ddg_act8_unpack gives.  dy [B][out] and dx in the element type, dW in the element type, or fp32 when
+ * W^ and x^ being what ddg_act8_unpack gives (fp32: dy times the scale is split into three bf16 terms, which hold all of its
+ * bits from about 1e-33 on; smaller products lose the lowest).  dy [B][out] and dx in the element type, dW in the element type, or fp32 when
  * dw_f32 != 0.  Wq and wscale may be NULL without dx, xq and xscale without dW.  workspace: device, 256-byte aligned,
  * ddg_fc8_workspace_bytes(...) bytes, contents undefined on entry and exit; two calls that may run at the same time need
  * one each.  dx may not be dy. */

@@ -474,13 +474,25 @@ template <typename T> __device__ __forceinline__ void prep_terms(const TermsJob 
     const int lane = threadIdx.x & 31;
     const unsigned per_row = (j.plane + kTermCols - 1) / kTermCols;
     const size_t items = (size_t)j.rows * per_row;
+    // a's first term; a becomes the rest.  An infinity or NaN stays in the first term alone; what the rounding alone would make
+    // infinite is bf16's largest value, and the rest is the next term's.
+    auto first_of = [](float &a) {
+        constexpr float kMost = 0x1.fep127f;
+        float h = bf16_round(a), rest = a - h;
+        if (!(fabsf(h) <= kMost)) {
+            if (fabsf(a) < INFINITY) { h = copysignf(kMost, a); rest = a - h; } else rest = 0.f;
+        }
+        a = rest;
+        return h;
+    };
     auto leave = [&](bf16 *to, float a, float b) {
-        for (int p = 0; p < j.planes; ++p, to += j.plane) {
-            const float ha = bf16_round(a), hb = bf16_round(b);
+        float ha = first_of(a), hb = first_of(b);
+        for (int p = 1;; ++p) {
             *reinterpret_cast<uint32_t *>(to) = pack2(ha, hb);
-            // an infinity or NaN stays in the first term alone
-            a = isinf(ha) || isnan(ha) ? 0.f : a - ha;
-            b = isinf(hb) || isnan(hb) ? 0.f : b - hb;
+            if (p >= j.planes) break;
+            to += j.plane;
+            ha = bf16_round(a); hb = bf16_round(b);
+            a -= ha; b -= hb;
         }
     };
     for (size_t i = (size_t)block * 8 + (threadIdx.x >> 5); i < items; i += (size_t)j.blocks * 8) {

@@ -310,6 +310,28 @@ def test_fc8_rows_that_are_not_numbers(binding, shape, prec):
 
 
 @gpu
+def test_fc8_gradient_of_products_past_the_largest_bf16(binding):
+    """fp32: dy times the scale may be up to the largest fp32 value, which is past bf16's; it has to reach neither its columns of
+    codes 0 nor, as an infinity, the others."""
+    B, D, V = 300, 72, 200
+    c = Fc(B, D, V, 0, seed=61)
+    c.dy.zero_()
+    big = 3.3999e38
+    c.dy[5, 9], c.dy[7, 150] = big, -big
+    c.ws.fill_(1.0)
+    c.xs.fill_(1.0)
+    for q in (c.wq, c.xq):
+        q[:, :D] = (torch.arange(D, device="cuda") % 3 - 1).to(torch.int8)
+    dx, dw, _ = c.bwd(binding, "xw")
+    e = torch.zeros(B, D, dtype=torch.float64, device="cuda")
+    e[5], e[7] = big * c.wq[9, :D].double(), -big * c.wq[150, :D].double()
+    within(dx, e, 16 * E * e.abs(), "dx")
+    e = torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    e[9], e[150] = big * c.xq[5, :D].double(), -big * c.xq[7, :D].double()
+    within(dw, e, 16 * E * e.abs(), "dW")
+
+
+@gpu
 def test_fc8_gradient_against_differences(binding):
     """The layer is linear in what the codes stand for: steps of whole codes change <dy, y> by the gradients' products."""
     c = Fc(37, 200, 150, 0, seed=11)
