@@ -454,7 +454,8 @@ ddg_status ddg_dropout_bwd(int precision, const void *dy, void *dx, const void *
  * A block around a linear layer that works, and keeps what its backward pass needs, in 8 bits.  A module with K - k + 1
  * slots of history keeps so many copies of every layer's input: as codes they take half (bf16) or a quarter (fp32) of the
  * memory, and the layer's forward and backward pass read them as they are.  As above: device pointers to contiguous
- * tensors on the current device, the calls only enqueue, allocate nothing, can be captured, and give the same bits each time.
+ * tensors on the current device, which start on a boundary of their values at least, the calls only enqueue, allocate nothing, can be
+ * captured, and give the same bits each time.
  * --------------------------------------------------------------------------------------------------------- */
 
 /* Rows of codes: q int8 [rows][ddg_act8_pitch(C)], a row's C codes and zeros behind them (which no call reads), on a 16-byte

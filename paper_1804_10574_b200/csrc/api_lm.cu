@@ -75,6 +75,14 @@ ddg_status dropout(int precision, const void *x, const void *res, void *y, const
 }
 
 bool fc8_sizes_ok(int B, int in, int out) { return B >= 1 && in >= 1 && out >= 1 && B <= (1 << 24) && in <= kAct8MaxC && out <= (1 << 24); }
+// Tensors of the element type and of 32-bit values have to start on a boundary of their own values: the kernels read them so at least.
+ddg_status values_check(int precision, std::initializer_list<const void *> elems, std::initializer_list<const void *> words) {
+    for (const void *p : elems)
+        if (misaligned(p, precision == DDG_BF16 ? 2 : 4)) return refuse(DDG_ERR_INVALID_ARG, "a tensor does not start on a boundary of its element type");
+    for (const void *p : words)
+        if (misaligned(p, 4)) return refuse(DDG_ERR_INVALID_ARG, "a tensor of 32-bit values does not start on a 4-byte boundary");
+    return DDG_OK;
+}
 ddg_status codes_check(const void *q, const char *msg) { return misaligned(q, 16) ? refuse(DDG_ERR_INVALID_ARG, msg) : DDG_OK; }
 bool norm_sizes_ok(int rows, int C, int span) { return rows >= 1 && rows <= kRmsMaxRows && C >= 1 && C <= kRmsMaxC && span >= 1; }
 
@@ -153,7 +161,7 @@ ddg_status ddg_act8_pack(int precision, const void *x, void *q, float *scale, in
     if (bad_prec(precision) || !x || !q || !scale) return DDG_ERR_INVALID_ARG;
     if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kAct8MaxC) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(q, "act8_pack: the codes have to start on a 16-byte boundary");
-    if (st != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
+    if (st != DDG_OK || (st = values_check(precision, {x}, {scale})) != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
     return done(launch_act8_pack(precision, x, q, scale, rows, C, (cudaStream_t)stream));
 }
 
@@ -161,7 +169,7 @@ ddg_status ddg_act8_unpack(int precision, const void *q, const float *scale, voi
     if (bad_prec(precision) || !x || !q || !scale) return DDG_ERR_INVALID_ARG;
     if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kAct8MaxC) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(q, "act8_unpack: the codes have to start on a 16-byte boundary");
-    if (st != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
+    if (st != DDG_OK || (st = values_check(precision, {x}, {scale})) != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
     return done(launch_act8_unpack(precision, q, scale, x, rows, C, (cudaStream_t)stream));
 }
 
@@ -171,6 +179,7 @@ ddg_status ddg_fc8_fwd(int precision, const void *xq, const float *xscale, const
     if (!fc8_sizes_ok(B, in, out)) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(xq, "fc8_fwd: the codes of x have to start on a 16-byte boundary");
     if (st != DDG_OK || (st = codes_check(Wq, "fc8_fwd: the codes of W have to start on a 16-byte boundary")) != DDG_OK) return st;
+    if ((st = values_check(y_f32 ? DDG_FP32 : precision, {y}, {xscale, wscale})) != DDG_OK || (st = values_check(precision, {bias}, {})) != DDG_OK) return st;
     if ((st = ready({xq, xscale, Wq, wscale, bias, y})) != DDG_OK) return st;
     if (conv_tc_init() != 0) return DDG_ERR_CUDA;
     return done(launch_fc8_fwd(precision, xq, xscale, Wq, wscale, bias, y, B, in, out, y_f32, (cudaStream_t)stream));
@@ -189,6 +198,7 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
     if (st != DDG_OK || (st = codes_check(Wq, "fc8_bwd: the codes of W have to start on a 16-byte boundary")) != DDG_OK) return st;
     if (misaligned(workspace, 256)) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: the workspace has to start on a 256-byte boundary");
     if (workspace_bytes < fc8_workspace_bytes(precision, B, in, out)) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: the workspace is smaller than ddg_fc8_workspace_bytes says");
+    if ((st = values_check(precision, {dy, dx}, {xscale, wscale, db})) != DDG_OK || (st = values_check(dw_f32 ? DDG_FP32 : precision, {dW}, {})) != DDG_OK) return st;
     if ((st = ready({dy, xq, xscale, Wq, wscale, dx, dW, db, workspace})) != DDG_OK) return st;
     if (conv_tc_init() != 0) return DDG_ERR_CUDA;
     return done(launch_fc8_bwd(precision, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, in, out, dw_f32, (cudaStream_t)stream));
@@ -204,7 +214,8 @@ ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, con
     if (y == h) return refuse(DDG_ERR_INVALID_ARG, "block_norm: y may not be h");
     if (!norm_sizes_ok(rows, C, span)) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(q, "block_norm: the codes have to start on a 16-byte boundary");
-    if (st != DDG_OK || (st = ready({b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre})) != DDG_OK) return st;
+    if (st != DDG_OK || (st = values_check(precision, {b, res, gate, gamma_post, gamma_pre, h, y}, {qscale, rstd_post, rstd_pre})) != DDG_OK) return st;
+    if ((st = ready({b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre})) != DDG_OK) return st;
     return done(launch_block_norm_fwd(precision, b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre, rows, C, span, alpha, eps, (cudaStream_t)stream));
 }
 
@@ -218,7 +229,9 @@ ddg_status ddg_block_norm_bwd(int precision, const void *dy, const void *dh, con
     if (db == dres) return refuse(DDG_ERR_INVALID_ARG, "block_norm: db may not be dres");
     if (!isfinite(alpha)) return refuse(DDG_ERR_INVALID_ARG, "block_norm: alpha has to be finite");
     if (!norm_sizes_ok(rows, C, span)) return DDG_ERR_UNSUPPORTED;
-    const ddg_status st = ready({dy, dh, b, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, db, dres, dgate, dgamma_post, dgamma_pre, scratch});
+    ddg_status st = values_check(precision, {dy, dh, b, h, gate, gamma_post, gamma_pre, db, dres}, {rstd_post, rstd_pre, dgate, dgamma_post, dgamma_pre, scratch});
+    if (st != DDG_OK) return st;
+    st = ready({dy, dh, b, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, db, dres, dgate, dgamma_post, dgamma_pre, scratch});
     if (st != DDG_OK) return st;
     return done(launch_block_norm_bwd(precision, dy, dh, b, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, db, dres, dgate, dgamma_post, dgamma_pre, scratch, rows, C,
                                       span, alpha, (cudaStream_t)stream));

@@ -865,6 +865,31 @@ def test_block_norm_refusals(binding):
     assert binding.block_norm_scratch_elems(2, 8, 2) > 0
 
 
+def test_block8_refuses_tensors_off_their_values_boundaries(binding):
+    """An address that is no multiple of the value's size would fault in the kernels."""
+    need = binding.fc8_workspace_bytes(0, 4, 64, 100)
+    calls = [
+        (binding.act8_pack, dict(x=P, q=P, s=P), (3, 64), "x", "s"),
+        (binding.act8_unpack, dict(q=P, s=P, x=P), (3, 64), "x", "s"),
+        (binding.fc8_fwd, dict(xq=P, xs=P, wq=P, ws=P, bias=P, y=P), (4, 64, 100), "bias y", "xs ws"),
+        (binding.fc8_bwd, dict(dy=P, xq=P, xs=P, wq=P, ws=P, dx=2 * P, dw=3 * P, db=P, work=Ws(need)), (4, 64, 100), "dy dx dw", "xs ws db"),
+        (binding.block_norm_fwd, dict(b=P, res=P, gate=P, post=P, pre=P, h=P, y=2 * P, q=4 * P, s=P, r1=P, r2=P), (3, 256, 3), "b res gate post pre h y", "s r1 r2"),
+        (binding.block_norm_bwd, dict(dy=P, dh=P, b=P, h=P, gate=P, post=P, pre=P, r1=P, r2=P, db=P, dres=2 * P, dg=P, dpost=P, dpre=P, scratch=P), (3, 256, 3),
+         "dy dh b h gate post pre db dres", "r1 r2 dg dpost dpre scratch"),
+    ]
+    for fn, args, sizes, elems, words in calls:
+        for prec in (0, 1):
+            for name in elems.split() + words.split():
+                off = (1,) if prec and name in elems.split() else (1, 2, 3)
+                for by in off:
+                    kw = {**args, name: args[name] + by}
+                    assert status(fn, prec, *kw.values(), *sizes) == 1, (fn.__name__, name, prec, by)
+                    assert b"boundary" in binding.lib().ddg_last_error(None)
+    # 32-bit results of 16-bit layers
+    assert status(binding.fc8_fwd, 1, P, P, P, P, None, P + 2, 4, 64, 100, True) == 1
+    assert status(binding.fc8_bwd, 1, P, P, P, P, P, None, P + 2, None, Ws(need), 4, 64, 100, True) == 1
+
+
 def test_block8_tensor_arguments_are_checked_in_the_binding(binding):
     x, q = torch.zeros(4, 8), torch.zeros(4, 16, dtype=torch.int8)
     for bad in (dict(x=x.t()), dict(x=x.half()), dict(x=x[:2]), dict(q=q[:, :8]), dict(q=q.float()), dict(q=q[:3])):
