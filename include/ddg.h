@@ -455,7 +455,7 @@ ddg_status ddg_dropout_bwd(int precision, const void *dy, void *dx, const void *
  * slots of history keeps so many copies of every layer's input: as codes they take half (bf16) or a quarter (fp32) of the
  * memory, and the layer's forward and backward pass read them as they are.  As above: device pointers to contiguous
  * tensors on the current device, which start on a boundary of their values at least, the calls only enqueue, allocate nothing, can be
- * captured, and give the same bits each time.
+ * captured, and give the same bits each time.  An output overlaps no other tensor of its call but where it is said that it may be one.
  * --------------------------------------------------------------------------------------------------------- */
 
 /* Rows of codes: q int8 [rows][ddg_act8_pitch(C)], a row's C codes and zeros behind them (which no call reads), on a 16-byte
@@ -479,7 +479,7 @@ ddg_status ddg_fc8_fwd(int precision, const void *xq, const float *xscale, const
  * bits from about 1e-33 on; smaller products lose the lowest).  dy [B][out] and dx in the element type, dW in the element type, or fp32 when
  * dw_f32 != 0.  Wq and wscale may be NULL without dx, xq and xscale without dW.  workspace: device, 256-byte aligned,
  * ddg_fc8_workspace_bytes(...) bytes, contents undefined on entry and exit; two calls that may run at the same time need
- * one each.  dx may not be dy. */
+ * one each.  dx may not be dy, dW neither dy nor dx. */
 size_t ddg_fc8_workspace_bytes(int precision, int B, int in, int out);
 ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const float *xscale, const void *Wq,
                        const float *wscale, void *dx, void *dW, float *db, void *workspace, size_t workspace_bytes, int B,

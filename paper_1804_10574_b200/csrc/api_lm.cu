@@ -83,6 +83,12 @@ ddg_status values_check(int precision, std::initializer_list<const void *> elems
         if (misaligned(p, 4)) return refuse(DDG_ERR_INVALID_ARG, "a tensor of 32-bit values does not start on a 4-byte boundary");
     return DDG_OK;
 }
+// An output that is read or written as something else too, by other blocks of the same launch.
+ddg_status own_place_check(const void *out, std::initializer_list<const void *> others, const char *msg) {
+    for (const void *p : others)
+        if (out && out == p) return refuse(DDG_ERR_INVALID_ARG, msg);
+    return DDG_OK;
+}
 ddg_status codes_check(const void *q, const char *msg) { return misaligned(q, 16) ? refuse(DDG_ERR_INVALID_ARG, msg) : DDG_OK; }
 bool norm_sizes_ok(int rows, int C, int span) { return rows >= 1 && rows <= kRmsMaxRows && C >= 1 && C <= kRmsMaxC && span >= 1; }
 
@@ -161,7 +167,7 @@ ddg_status ddg_act8_pack(int precision, const void *x, void *q, float *scale, in
     if (bad_prec(precision) || !x || !q || !scale) return DDG_ERR_INVALID_ARG;
     if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kAct8MaxC) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(q, "act8_pack: the codes have to start on a 16-byte boundary");
-    if (st != DDG_OK || (st = values_check(precision, {x}, {scale})) != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
+    if (st != DDG_OK || (st = values_check(precision, {x}, {scale})) != DDG_OK || (st = own_place_check(q, {x}, "act8_pack: the codes may not be x")) != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
     return done(launch_act8_pack(precision, x, q, scale, rows, C, (cudaStream_t)stream));
 }
 
@@ -169,7 +175,7 @@ ddg_status ddg_act8_unpack(int precision, const void *q, const float *scale, voi
     if (bad_prec(precision) || !x || !q || !scale) return DDG_ERR_INVALID_ARG;
     if (rows < 1 || rows > kRmsMaxRows || C < 1 || C > kAct8MaxC) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(q, "act8_unpack: the codes have to start on a 16-byte boundary");
-    if (st != DDG_OK || (st = values_check(precision, {x}, {scale})) != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
+    if (st != DDG_OK || (st = values_check(precision, {x}, {scale})) != DDG_OK || (st = own_place_check(q, {x}, "act8_unpack: the codes may not be x")) != DDG_OK || (st = ready({x, q, scale})) != DDG_OK) return st;
     return done(launch_act8_unpack(precision, q, scale, x, rows, C, (cudaStream_t)stream));
 }
 
@@ -199,6 +205,7 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
     if (misaligned(workspace, 256)) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: the workspace has to start on a 256-byte boundary");
     if (workspace_bytes < fc8_workspace_bytes(precision, B, in, out)) return refuse(DDG_ERR_INVALID_ARG, "fc8_bwd: the workspace is smaller than ddg_fc8_workspace_bytes says");
     if ((st = values_check(precision, {dy, dx}, {xscale, wscale, db})) != DDG_OK || (st = values_check(dw_f32 ? DDG_FP32 : precision, {dW}, {})) != DDG_OK) return st;
+    if ((st = own_place_check(dW, {dy, dx}, "fc8_bwd: dW may be neither dy nor dx")) != DDG_OK) return st;
     if ((st = ready({dy, xq, xscale, Wq, wscale, dx, dW, db, workspace})) != DDG_OK) return st;
     if (conv_tc_init() != 0) return DDG_ERR_CUDA;
     return done(launch_fc8_bwd(precision, dy, xq, xscale, Wq, wscale, dx, dW, db, workspace, B, in, out, dw_f32, (cudaStream_t)stream));
@@ -215,6 +222,7 @@ ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, con
     if (!norm_sizes_ok(rows, C, span)) return DDG_ERR_UNSUPPORTED;
     ddg_status st = codes_check(q, "block_norm: the codes have to start on a 16-byte boundary");
     if (st != DDG_OK || (st = values_check(precision, {b, res, gate, gamma_post, gamma_pre, h, y}, {qscale, rstd_post, rstd_pre})) != DDG_OK) return st;
+    if ((st = own_place_check(q, {b, res, h, y}, "block_norm: the codes need a place of their own")) != DDG_OK) return st;
     if ((st = ready({b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre})) != DDG_OK) return st;
     return done(launch_block_norm_fwd(precision, b, res, gate, gamma_post, gamma_pre, h, y, q, qscale, rstd_post, rstd_pre, rows, C, span, alpha, eps, (cudaStream_t)stream));
 }

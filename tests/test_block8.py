@@ -890,6 +890,19 @@ def test_block8_refuses_tensors_off_their_values_boundaries(binding):
     assert status(binding.fc8_bwd, 1, P, P, P, P, P, None, P + 2, None, Ws(need), 4, 64, 100, True) == 1
 
 
+def test_block8_refuses_outputs_over_what_other_blocks_read(binding):
+    last = lambda: binding.lib().ddg_last_error(None)  # noqa: E731
+    assert status(binding.act8_pack, 1, P, P, P, 3, 64) == 1 and b"may not be x" in last()
+    assert status(binding.act8_unpack, 1, P, P, P, 3, 64) == 1 and b"may not be x" in last()
+    need = binding.fc8_workspace_bytes(1, 64, 64, 64)
+    bwd = lambda dx, dw: status(binding.fc8_bwd, 1, P, P, P, P, P, dx, dw, None, Ws(need), 64, 64, 64)  # noqa: E731
+    assert bwd(2 * P, P) == 1 and b"dW" in last() and bwd(None, P) == 1 and bwd(2 * P, 2 * P) == 1 and b"dW" in last()
+    for over in range(4):
+        t = [2 * P, 3 * P, 4 * P, 5 * P]  # b, res, h, y
+        t[over] = P
+        assert status(binding.block_norm_fwd, 1, t[0], t[1], None, P, P, t[2], t[3], P, P, None, None, 3, 256, 3) == 1 and b"place of their own" in last()
+
+
 def test_block8_tensor_arguments_are_checked_in_the_binding(binding):
     x, q = torch.zeros(4, 8), torch.zeros(4, 16, dtype=torch.int8)
     for bad in (dict(x=x.t()), dict(x=x.half()), dict(x=x[:2]), dict(q=q[:, :8]), dict(q=q.float()), dict(q=q[:3])):
