@@ -996,6 +996,131 @@ def test_rows_through_shared_memory_whose_waits_run_out_in_some_threads(binding,
     assert all(torch.equal(a, b) for a, b in zip(step(), ref))
 
 
+# ---- rows through shared memory: as the tests of few rows above -----------------------------------------------------------
+@gpu
+@PREC
+@pytest.mark.parametrize("rows,C,span", [(2000, 640, 1), (1000, 4096, 1), (1500, 1021, 2), (900, 1536, 2), (400, 8192, 1), (2300, 512, 1), (601, 3000, 5)])
+def test_block_norm_several_stretches_of_a_block(binding, rows, C, span, prec):
+    """More gates than resident blocks: a block's share of dgamma_post comes out of several stretches."""
+    for dh in (True, False):
+        c = Norm(rows, C, prec, span, seed=62).reference()
+        h, r1, r2 = c.h.to(DT[prec]), c.r1[:, 0].float(), c.r2[:, 0].float()
+        got, refs = c.bwd(binding, h, r1, r2, dh), c.grads_ref(h, r1, r2, dh)
+        for g, (ref, tol), what in zip(got, refs, ("db", "dres", "dgate", "dgamma_post", "dgamma_pre")):
+            within(g, ref, tol, what)
+        again = c.bwd(binding, h, r1, r2, dh, dgate=False)
+        assert all(torch.equal(a, b) for k, (a, b) in enumerate(zip(got, again)) if k != 2)
+    got, y, q, s, _, _ = c.fwd(binding, True, True)
+    within(got, c.h, c.e_h + U[h.dtype] * c.h.abs(), "h")
+    within(y, c.y, c.e_y + U[h.dtype] * c.y.abs(), "y")
+    within(q[:, :C].double() * s.double()[:, None], c.y, s.double()[:, None] * (0.5 + 2.0 ** -12) + 2 * c.e_y.amax(1, keepdim=True), "codes")
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("rows,C,span", [(700, 640, 100), (400, 1021, 7), (601, 2933, 1), (320, 4096, 320)])
+def test_block_norm_of_many_rows_in_place(binding, rows, C, span, prec):
+    """h and y over b and res; db and dres over what the backward pass reads; rows whose 16-byte units are shared too."""
+    c = Norm(rows, C, prec, span, seed=63).reference()
+    h, y, _, _, r1, r2 = c.fwd(binding)
+    for a, b in (("b", "res"), ("res", "b")):
+        k = Norm(rows, C, prec, span, seed=63)
+        h2, y2, _, _, _, _ = k.fwd(binding, h=getattr(k, a), y=getattr(k, b))
+        assert torch.equal(h2, h) and torch.equal(y2, y)
+    ref = c.bwd(binding, h, r1, r2)
+    for a, b in (("dy", "dh"), ("dh", "b"), ("b", "dy"), ("h", "dh"), ("b", "h"), ("h", "dy")):
+        k = Norm(rows, C, prec, span, seed=63)
+        k.h = h.clone()
+        got = k.bwd(binding, k.h, r1, r2, db=getattr(k, a), dres=getattr(k, b))
+        assert all(torch.equal(p, q) for p, q in zip(got, ref)), (a, b)
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("C", [640, 1021, 2048])
+def test_block_norm_special_rows_among_many(binding, C, prec):
+    """Rows of zeros, NaN and infinities are their own, in the gradients too; sums over rows show them."""
+    rows = 400
+    c = Norm(rows, C, prec, 1, seed=64)
+    clean = c.fwd(binding, True, True)
+    clean_grads = c.bwd(binding, clean[0], clean[4], clean[5])
+    c.b[1], c.res[1] = 0.0, 0.0
+    c.b[200, 7], c.res[399, C - 1], c.b[0, 0] = NAN, INF, -INF
+    c.gate[40] = 0.0
+    h, y, q, s, r1, r2 = c.fwd(binding, True, True)
+    assert not h[1].any() and not y[1].any() and not q[1].any() and float(s[1]) == 2.0 ** -126
+    for r in (200, 399, 0):
+        assert math.isnan(float(s[r])) and not q[r].any()
+    assert torch.isnan(y[200]).all()
+    assert torch.equal(h[40], (ALPHA * c.res[40].float()).to(h.dtype))
+    same = torch.ones(rows, dtype=torch.bool, device="cuda")
+    same[[0, 1, 40, 200, 399]] = False
+    for a, b in zip((h, y, q, s, r1, r2), clean):
+        assert torch.equal(a[same], b[same])
+    db, dres, dg, dpost, dpre = c.bwd(binding, h, r1, r2)
+    for a, b in zip((db, dres, dg), clean_grads):
+        assert torch.equal(a[same], b[same]) and torch.isnan(a[200].float()).all() and torch.isfinite(a[[1, 40]].float()).all()
+    assert torch.isnan(dpost).all() and torch.isnan(dpre).all()
+
+
+@gpu
+@PREC
+@pytest.mark.parametrize("C", [1021, 2048, 8192])
+def test_act8_special_rows_among_many(binding, C, prec):
+    rows = 320
+    x = randn(rows, C, seed=65, prec=prec)
+    clean = pack(binding, x, prec)
+    x[1] = 0.0
+    x[2] = randn(C, seed=5, prec=prec) * 2.0 ** -130
+    x[3, 7] = torch.finfo(x.dtype).max
+    x[4, 9], x[300, 3], x[319, C - 1], x[0, 0] = NAN, INF, -INF, NAN
+    q, scale = pack(binding, x, prec)
+    bad = [0, 4, 300, 319]
+    for r in bad:
+        assert math.isnan(float(scale[r])) and not q[r].any()
+    good = [r for r in range(rows) if r not in bad]
+    ref, s = codes(x[good])
+    assert torch.equal(q[good][:, :C].double(), ref) and torch.equal(scale[good], s)
+    back = torch.empty_like(x)
+    binding.act8_unpack(prec, q, scale, back, rows, C)
+    assert torch.isnan(back[bad]).all() and torch.isfinite(back[good]).all() and not back[1].any()
+    assert torch.equal(q[5:300], clean[0][5:300]) and torch.equal(scale[5:300], clean[1][5:300])
+
+
+@gpu
+@PREC
+def test_many_rows_off_16_byte_boundaries_and_rows_behind(binding, prec):
+    """Tensors that start anywhere, one at a time and all; rows behind the last are left as they were."""
+    def off(t):
+        store = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
+        store[1:] = t.flatten()
+        return store[1:].view(t.shape)
+    for rows, C in ((330, 1024), (310, 1021)):
+        names = ("b", "res", "gate", "post", "pre", "dy", "dh")
+        for which in [(n,) for n in names] + [names]:
+            c = Norm(rows, C, prec, 10, seed=66).reference()
+            for n in which:
+                setattr(c, n, off(getattr(c, n)))
+            h, y, q, s, r1, r2 = c.fwd(binding, True, True)
+            within(h, c.h, c.e_h + U[h.dtype] * c.h.abs(), "h")
+            within(y, c.y, c.e_y + U[h.dtype] * c.y.abs(), "y")
+            for g, (ref, tol), what in zip(c.bwd(binding, h, r1, r2), c.grads_ref(h, r1, r2), ("db", "dres", "dgate", "dgamma_post", "dgamma_pre")):
+                within(g, ref, tol, what)
+        # fewer rows than the buffers have
+        n = rows - 3
+        h, y, db, dres, q, s = (torch.full_like(t, 7.0) for t in (c.b, c.b, c.b, c.b, q, s))
+        binding.block_norm_fwd(prec, c.b, c.res, c.gate, c.post, c.pre, h, y, q, s, r1, r2, n, C, 10, ALPHA, EPS)
+        dg, dpost, dpre, scratch = f32(*c.gate.shape), f32(C), f32(C), f32(binding.block_norm_scratch_elems(n, C, 10) + 64)
+        binding.block_norm_bwd(prec, c.dy, c.dh, c.b, h, c.gate, c.post, c.pre, r1, r2, db, dres, dg, dpost, dpre, scratch, n, C, 10, ALPHA)
+        assert all((t[n:] == 7).all() for t in (h, y, db, dres, q, s)) and (scratch[-64:] == 7).all()
+        assert not any((t[:n] == 7).all(1).any() for t in (h, y, db, dres))
+        q2, s2 = torch.full_like(q, 7), f32(rows)
+        binding.act8_pack(prec, c.b, q2, s2, n, C)
+        assert (q2[n:] == 7).all() and (s2[n:] == 7).all()
+        ref, sr = codes(c.b[:n])
+        assert torch.equal(q2[:n, :C].double(), ref) and torch.equal(s2[:n], sr)
+
+
 # ---- long sums, large tensors ---------------------------------------------------------------------------------------
 @gpu
 def test_fc8_weight_gradient_of_many_rows_keeps_its_precision(binding):
