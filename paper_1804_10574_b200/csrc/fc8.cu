@@ -705,10 +705,10 @@ void mm_cut(MmArgs &g, int before, int tiles, int pairs) {
     const int rest = before + tiles > pairs ? std::min((before + tiles) % pairs, tiles) : 0;
     g.full = tiles;
     g.cut = 1;
-    double least = 0.95;
+    double least = 0.95 * mm_weight(g.width);
     for (int c = 2; c <= 4 && rest; c *= 2) {
         if (g.width % (c * kKBox) != 0) break;
-        const double t = (double)((rest * c + pairs - 1) / pairs) * mm_weight(kTile / c);
+        const double t = (double)((rest * c + pairs - 1) / pairs) * mm_weight(g.width / c);
         if (t < least) { least = t; g.cut = c; g.full = tiles - rest; }
     }
     g.items = g.full + (tiles - g.full) * g.cut;

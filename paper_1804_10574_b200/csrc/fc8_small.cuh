@@ -11,7 +11,7 @@ struct SmallArgs {
     void *dx, *dW;
     float *db;
     int B, in, out, pitch;
-    int dx_tiles, dw_tiles, dw_f32;
+    int dx_tiles, dw_tiles;
 };
 
 // C[M][N] = sum_k A(m, k) value(q[k][n]), K <= kSmallK: A is dy, K-major for dx, M-major (transposed) for dW

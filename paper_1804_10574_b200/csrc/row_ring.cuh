@@ -304,13 +304,13 @@ inline size_t ring_smem_of(int per_sm) { return (size_t)(226 * 1024 / per_sm - 2
 // stages at least, else 0 blocks.
 struct RingPlan { int threads, per_sm; size_t smem; int iter; };
 inline RingShape ring_shape(int rows, int row_bytes, int tensors, size_t smem, unsigned polls);
-// `registers` of a thread and `more` threads of a block besides the row's limit the blocks too.
-inline RingPlan ring_plan(int C, int row_bytes, int vec, int iter, int tensors, size_t extra, int registers = 128, int more = 0) {
+// `registers` of a thread limit the blocks too.
+inline RingPlan ring_plan(int C, int row_bytes, int vec, int iter, int tensors, size_t extra, int registers = 128) {
     RingPlan p{};
     const int threads = std::max(64, ring_threads((C + vec - 1) / vec, iter));
     if (threads > 512) return p;
     p.iter = iter;
-    p.per_sm = std::min(8, 65536 / (registers * (threads + more)));
+    p.per_sm = std::min(8, 65536 / (registers * threads));
     while (p.per_sm > 1 && ring_shape(1, row_bytes, tensors, ring_smem_of(p.per_sm) - extra, 0).stages < 2) --p.per_sm;
     p.smem = ring_smem_of(p.per_sm);
     if (p.smem > extra && ring_shape(1, row_bytes, tensors, p.smem - extra, 0).stages >= 2) p.threads = threads;
