@@ -624,37 +624,34 @@ __global__ void __launch_bounds__(512, 1) block_norm_bwd_ring_kernel(const __gri
     cluster_sync();  // no block leaves while its shares are read
 }
 
-// Shares in index order per warp, warps in index order, 32 columns per block.  Sums: dpost, dpre, then the gate's rows, dealt out to
-// blockIdx.y (of which a grid has fewer than there may be gates).
+// Shares in index order per warp, warps in index order, 32 columns per block.  blockIdx.y: dpost, dpre, then the gate's rows.
+// MORE: the gates past the rows of a grid, from sum `first` on (an offset for all launches: 695 x 6736, 13 rows a gate, 60 us
+// instead of 55).
 // gate and post (nullable): the first shares are still to be multiplied with the one gate, for dpost, and with gamma_post, for dgate.
 constexpr int kFoldMostY = 65535;
-struct NormFold { const float *part, *piece; float *dpost, *dpre, *dgate; const void *gate, *post; int n, parts, C, one_gate, sums; };
-template <typename T> __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const __grid_constant__ NormFold g) {
+struct NormFold { const float *part, *piece; float *dpost, *dpre, *dgate; const void *gate, *post; int n, parts, C, one_gate, first; };
+template <typename T, bool MORE> __global__ void __launch_bounds__(1024) block_norm_fold_kernel(const __grid_constant__ NormFold g) {
     __shared__ float fold[32][32];
     pdl_launch();
     pdl_wait();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, C = g.C, c = blockIdx.x * 32 + lane;
-    for (int what = blockIdx.y; what < g.sums; what += gridDim.y) {
-        const int gate = what - 2;
-        const float *from = what < 2 ? g.part + (size_t)what * C : g.piece + (size_t)gate * g.parts * C;
-        const size_t stride = what < 2 ? 2 * (size_t)C : (size_t)C;
-        const int n = what < 2 ? g.n : g.parts;
-        float a = 0.f;
-        if (c < C) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, C = g.C, c = blockIdx.x * 32 + lane, what = (MORE ? g.first : 0) + blockIdx.y, gate = what - 2;
+    const float *from = what < 2 ? g.part + (size_t)what * C : g.piece + (size_t)gate * g.parts * C;
+    const size_t stride = what < 2 ? 2 * (size_t)C : (size_t)C;
+    const int n = what < 2 ? g.n : g.parts;
+    float a = 0.f;
+    if (c < C) {
 #pragma unroll 8
-            for (int i = w; i < n; i += 32) a += from[i * stride + c];
+        for (int i = w; i < n; i += 32) a += from[i * stride + c];
+    }
+    fold[w][lane] = a;
+    __syncthreads();
+    if (w == 0 && c < C) {
+        for (int i = 1; i < 32; ++i) a += fold[i][lane];
+        if (what == 0 && g.one_gate) {
+            if (g.dgate) g.dgate[c] = a * to_f(((const T *)g.post)[c]);
+            if (g.gate) a *= to_f(((const T *)g.gate)[c]);
         }
-        fold[w][lane] = a;
-        __syncthreads();
-        if (w == 0 && c < C) {
-            for (int i = 1; i < 32; ++i) a += fold[i][lane];
-            if (what == 0 && g.one_gate) {
-                if (g.dgate) g.dgate[c] = a * to_f(((const T *)g.post)[c]);
-                if (g.gate) a *= to_f(((const T *)g.gate)[c]);
-            }
-            (what == 0 ? g.dpost : (what == 1 ? g.dpre : g.dgate + (size_t)gate * C))[c] = a;
-        }
-        __syncthreads();  // the shares have been read
+        (what == 0 ? g.dpost : (what == 1 ? g.dpre : g.dgate + (size_t)gate * C))[c] = a;
     }
 }
 
@@ -775,9 +772,11 @@ template <typename T, int VEC> int bwd_as(BlockNormBwd &g, bool ring, float *scr
     }
     const bool ring_one = p.ring.threads && g.gates == 1;
     const int sums = 2 + (g.dgate && p.parts > 1 && !ring_one ? g.gates : 0);
-    const NormFold fold{g.part, g.piece, dpost, dpre, g.dgate, g.gate, g.post, p.ring.threads ? p.blocks / p.cluster : p.blocks, p.parts, g.C, ring_one, sums};
-    launch_k(block_norm_fold_kernel<T>, dim3((g.C + 31) / 32, std::min(sums, kFoldMostY)), 1024, 0, s, fold);
-    return 2;
+    NormFold fold{g.part, g.piece, dpost, dpre, g.dgate, g.gate, g.post, p.ring.threads ? p.blocks / p.cluster : p.blocks, p.parts, g.C, ring_one, 0};
+    int launches = 1;
+    for (; fold.first < sums; fold.first += kFoldMostY, ++launches)
+        launch_k(fold.first ? block_norm_fold_kernel<T, true> : block_norm_fold_kernel<T, false>, dim3((g.C + 31) / 32, std::min(sums - fold.first, kFoldMostY)), 1024, 0, s, fold);
+    return launches;
 }
 
 }  // namespace
