@@ -458,8 +458,8 @@ ddg_status ddg_dropout_bwd(int precision, const void *dy, void *dx, const void *
  * captured, and give the same bits each time.  An output overlaps no other tensor of its call but where it is said that it may be one.
  * --------------------------------------------------------------------------------------------------------- */
 
-/* Rows of codes: q int8 [rows][ddg_act8_pitch(C)], a row's C codes and zeros behind them (which no call reads), on a 16-byte
- * boundary; scale fp32 [rows].  C <= 2^17.
+/* Rows of codes: q int8 [rows][ddg_act8_pitch(C)], a row's C codes and zeros behind them (which have no effect on any call), on a
+ * 16-byte boundary; scale fp32 [rows].  C <= 2^17, at most 2^30 rows.
  *   m = max(max |x| of the row, 127 2^-126);  scale = m / 127 (at most 8454659 2^98, so that 127 scale is finite);
  *   q = 127 x / m, rounded once, halves to even.
  * A row that holds a NaN or an infinity has scale NaN and codes 0: all that is made of it is NaN.
@@ -492,7 +492,8 @@ ddg_status ddg_fc8_bwd(int precision, const void *dy, const void *xq, const floa
  * b, res, gamma_post [C], gamma_pre [C], h, y in the element type; gate (nullable = 1, whatever the span) [ceil(rows / span)][C], row n
  * takes its row n / span: span = rows for one gate vector, the rows of a sample for a gate per sample, 1 for a gate per row.
  * y and / or q with qscale (rows of codes, as ddg_act8_pack lays them out) are given; both are taken from the unrounded h.
- * rstd_post, rstd_pre (nullable) fp32 [rows].  h may be b or res, y too if it is another tensor than h. */
+ * rstd_post, rstd_pre (nullable) fp32 [rows]; squares are summed in 32 bits, so that rstd is 0 where they pass its range.  h may be
+ * b or res, y too if it is another tensor than h. */
 ddg_status ddg_block_norm_fwd(int precision, const void *b, const void *res, const void *gate, const void *gamma_post,
                               const void *gamma_pre, void *h, void *y, void *q, float *qscale, float *rstd_post,
                               float *rstd_pre, int rows, int C, int span, float alpha, float eps, void *stream);

@@ -16,8 +16,8 @@
 // each of its warps some hundred cycles, so that few warps a row and two to eight rows at a time on an SM are faster than a row per
 // SM, and arithmetic on pairs (f32x2.cuh) takes half the instructions.  Fewer rows, and rows that one warp holds, stay in
 // registers.  Measured (bf16): 8192 x 4096 forward 49.0 us (5.5 TB/s), to codes 43.6 us (5.4 TB/s), backward with the folding
-// kernel 75.8 us (5.3 TB/s); with a row in registers 87, 104 and 146 us.  8192 x 1021: 25, 29 and 49 us; 30000 x 256: 13, 14 and
-// 26 us.
+// kernel 75.8 us (5.3 TB/s); with a row in registers 87, 104 and 146 us.  8192 x 1021: 25, 29 and 46 us; 30000 x 256: 13, 14 and
+// 26 us.  With a gate per row, which no copy brings ahead, 8192 x 4096 takes 60 us forward and 188 backward.
 #include <algorithm>
 
 #include "act8.cuh"
